@@ -65,7 +65,14 @@ enum {
 
 /* Operation selector for bitlinear_workspace_bytes. */
 typedef enum { BL_OP_PACK = 0, BL_OP_QUANT = 1, BL_OP_FORWARD = 2, BL_OP_BACKWARD = 3,
-               BL_OP_LN_BACKWARD = 4, BL_OP_FORWARD_NONNEG = 5, BL_OP_MATMUL = 6 } bl_op;
+               BL_OP_LN_BACKWARD = 4, BL_OP_FORWARD_NONNEG = 5, BL_OP_MATMUL = 6, BL_OP_ROUTE = 7,
+               BL_OP_QUANT_NONLINEAR = 8 } bl_op;
+
+/* Non-linear functions of bitlinear_quant_nonlinear: max(u, 0), max(u, 0)^2, u Phi(u), u / (1 + e^-u). */
+typedef enum { BL_FN_RELU = 0, BL_FN_RELU2 = 1, BL_FN_GELU = 2, BL_FN_SILU = 3 } bl_fn;
+
+/* Element types where a call offers a choice. */
+typedef enum { BL_F32 = 0, BL_BF16 = 1 } bl_type;
 
 /* host: size in bytes of the packed-weight blob for an [N,K] matrix (0 on bad
  * shape).  The blob is the library's own tiled 1-bit layout (1 bit per weight,
@@ -303,6 +310,103 @@ int bitlinear_layernorm_backward(const float* dXhat, const float* X, int64_t M, 
                                  int groups_k, const float* ln_gain, float ln_eps, float* dX,
                                  float* dgain, float* dbias, void* workspace,
                                  size_t workspace_bytes, void* stream);
+
+/* ---- Mixtures of BitLinear layers ("experts") ---------------------------------------------------
+ * A router gives each of M tokens top_k of `experts` weight matrices.  A token's choice j is choice
+ * t * top_k + j; sorted by expert the choices are SLOTS, T = M * top_k of them.  A feed-forward
+ * network of experts is
+ *   bitlinear_quant_act (tokens) -> bitlinear_route -> bitlinear_matmul_experts (into the experts, codes
+ *   read through `order`) -> bitlinear_quant_nonlinear (slots) -> bitlinear_matmul_experts (out of the
+ *   experts, order = NULL) -> bitlinear_combine
+ * and its backward
+ *   bitlinear_combine_backward -> bitlinear_backward_ste_experts -> bitlinear_nonlinear_backward ->
+ *   bitlinear_backward_ste_experts -> bitlinear_combine (weights = NULL: the sum over a token's
+ *   slots) -> bitlinear_layernorm_backward.
+ * Where an expert's slots begin stays in device memory (`offsets`): nothing waits for the router.
+ * Slots behind offsets[experts] (choices that name no expert) are neither read nor written.
+ * Limits: experts 1..256, top_k 1..64, M * top_k <= 2^30 (else BL_ERR_SHAPE); bitlinear_route takes up to
+ * 2^24 choices, the products K <= 65536 (else BL_ERR_UNSUPPORTED).
+ *   packed  `experts` consecutive blobs of bitlinear_packed_bytes(N, K, 0) bytes, one bitlinear_pack_weights
+ *           call each (N % 16 == 0 and experts <= 64: bitlinear_pack_weights_grouped of the [experts * N, K]
+ *           matrix with groups_n = experts writes the same bytes)
+ *   beta    fp32 [experts]
+ *   order, position, offsets   as bitlinear_route writes them
+ *
+ * host: scratch bytes of an operation on M tokens: BL_OP_ROUTE (0 up to 4096 choices; N, K of no
+ * account), BL_OP_QUANT_NONLINEAR (rows = M * top_k; 0 per token), BL_OP_BACKWARD
+ * (bitlinear_backward_ste_experts).  0 for anything invalid as well. */
+size_t bitlinear_workspace_bytes_experts(int op, int64_t M, int top_k, int64_t N, int64_t K,
+                                         int experts, int granularity);
+
+/* A stable sort of the choices by expert.
+ *   expert    in   int32 [M][top_k]; a number outside 0 .. experts-1 (padding, a dropped choice): no slot
+ *   order     out  int32 [T]: the choice in each slot, ascending inside an expert; -1 behind the last
+ *   position  out  int32 [M][top_k]: the slot of each choice, or -1
+ *   offsets   out  int32 [experts + 1]: expert e has the slots offsets[e] .. offsets[e + 1] - 1 */
+int bitlinear_route(const int32_t* expert, int64_t M, int top_k, int experts, int32_t* order,
+                    int32_t* position, int32_t* offsets, void* workspace, size_t workspace_bytes,
+                    void* stream);
+
+/* Eq. 7 + Eq. 11 with a weight matrix per expert: for the slots s of expert e
+ *   Y[s,n] = (sum_k codes[r,k] W~_e[n,k]) * (beta_e * gamma_r / 128),   r = order[s] / top_k,
+ * codes int8 [M,K], gamma fp32 [M] (or [1]), rowsum int32 [M] as bitlinear_quant_act writes them; with
+ * order = NULL r = s and codes, gamma and rowsum have T rows (bitlinear_quant_nonlinear's).
+ *   Y      out  fp32 [T,N] (int32 with BL_FLAG_OUT_ACC_I32) */
+int bitlinear_matmul_experts(const int8_t* codes, const float* gamma, const int32_t* rowsum,
+                             int64_t M, int top_k, int64_t K, const int32_t* order,
+                             const int32_t* offsets, int experts, const void* packed, int64_t N,
+                             const float* beta, int granularity, unsigned flags, float* Y,
+                             void* stream);
+
+/* Section 2.2 for such a product (Sign, Clip and rounding are identity, alpha, beta, gamma constants):
+ *   dX[s,k]   = beta_e sum_n dY[s,n] W~_e[n,k]                    fp32 [T,K], or NULL
+ *   dW[e,n,k] = sum_{s of e} dY[s,n] codes[r,k] gamma_r / 128      fp32 [experts,N,K], or NULL;
+ *               zeros for an expert without slots
+ *   dY   in  bf16 [T,N] as bitlinear_combine_backward and bitlinear_nonlinear_backward write it
+ * With a gamma per tensor both products are exact but for their fp32 sums; with one per token gamma_r / 128
+ * is folded into row s of dY, which is then rounded to bf16 a second time. */
+int bitlinear_backward_ste_experts(const void* dY, int64_t M, int top_k, int64_t N, int64_t K,
+                                   const int8_t* codes, const float* gamma, int granularity,
+                                   const int32_t* order, const int32_t* offsets, int experts,
+                                   const void* packed, const float* beta, float* dX, float* dW,
+                                   void* workspace, size_t workspace_bytes, void* stream);
+
+/* Slots back to tokens: Y[t,n] = sum_j weights[t,j] * slots[position[t,j], n], added in fp32 in the order
+ * of j; choices without a slot add nothing, a token without any gets zeros.
+ *   slots in fp32 [T,N];  weights in fp32 [M][top_k] or NULL (ones);  Y out fp32 [M,N] */
+int bitlinear_combine(const float* slots, const int32_t* position, const float* weights, int64_t M,
+                      int top_k, int64_t N, float* Y, void* stream);
+
+/* Its gradient: dslots[position[t,j]] = weights[t,j] * dY[t] (bf16 [T,N], rounded once) and
+ * dweights[t,j] = sum_n dY[t,n] * slots[position[t,j], n] (fp32 [M][top_k] or NULL; 0 without a slot).
+ * slots may be NULL when dweights is. */
+int bitlinear_combine_backward(const float* dY, const float* slots, const int32_t* position,
+                               const float* weights, int64_t M, int top_k, int64_t N, void* dslots,
+                               float* dweights, void* stream);
+
+/* Between the two projections of a feed-forward network (of experts, or a plain one): a non-linear function,
+ * Eq. 12's LayerNorm and Eq. 4-5's quantiser in one pass, with an 8-bit checkpoint of the input for the
+ * backward pass.  codes, gamma and rowsum are those of bitlinear_quant_act on f(U), no gain and no bias.
+ *   U            in   fp32 [M,K], K <= 32768 (else BL_ERR_UNSUPPORTED)
+ *   fn                a bl_fn
+ *   rows         in   int32 [1] (device) or NULL: only rows below it are read and written (of a routed batch:
+ *                     offsets + experts)
+ *   check        out  int8 [M,K] or NULL: rne(u * (127 / m)), m the largest magnitude of each 128
+ *                     consecutive elements of a row (the last ones of a row may be fewer)
+ *   check_scale  out  fp32 [M][(K + 127) / 128]: m / 127
+ *   workspace         per tensor only: bitlinear_workspace_bytes_experts(BL_OP_QUANT_NONLINEAR, M, 1, ...) */
+int bitlinear_quant_nonlinear(const float* U, int64_t M, int64_t K, int fn, float ln_eps,
+                              const int32_t* rows, int granularity, int8_t* codes, float* gamma,
+                              int32_t* rowsum, int8_t* check, float* check_scale, void* workspace,
+                              size_t workspace_bytes, void* stream);
+
+/* The derivative of x^ = LN(f(u)) at v = check * check_scale, applied to dXhat (the dX of the product behind):
+ *   h = f(v), n = (h - mean h) * rstd,  dU = f'(v) * rstd * (dXhat - mean(dXhat) - n mean(dXhat * n))
+ * with f'(0) = 0 for the rectifiers.  dU: [M,K] of `type` (BL_BF16: as bitlinear_backward_ste_experts reads
+ * it, rounded once; BL_F32: as bitlinear_backward_ste reads it); 16-byte aligned, not on dXhat.  rows as above. */
+int bitlinear_nonlinear_backward(const float* dXhat, const int8_t* check, const float* check_scale,
+                                 int64_t M, int64_t K, int fn, float ln_eps, const int32_t* rows,
+                                 int type, void* dU, void* stream);
 
 /* Measurement aid, no part of the layer: one launch that only reads `bytes` (a multiple of 16)
  * of device memory at `src` with the access pattern of the small-batch GEMM's weight stream

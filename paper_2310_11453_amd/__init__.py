@@ -13,4 +13,8 @@ from .binding import (  # noqa: F401
     bitlinear_forward_nonneg, bitlinear_matmul_nonneg, bitlinear_quant_act_nonneg,
     bitlinear_weight_rowsums, bitlinear_weight_rowsums_grouped, forward_workspace_layout, set_tuning,
     bitlinear_forward_static, probe_read,
+    BF16, F32, FUNCTIONS, OP_QUANT_NONLINEAR, OP_ROUTE,
+    bitlinear_backward_ste_experts, bitlinear_combine, bitlinear_combine_backward, bitlinear_matmul_experts,
+    bitlinear_nonlinear_backward, bitlinear_pack_weights_experts, bitlinear_quant_nonlinear, bitlinear_route,
+    workspace_bytes_experts,
 )

@@ -18,7 +18,9 @@ BL_OK = 0
 GAMMA_PER_TOKEN, GAMMA_PER_TENSOR = 0, 1
 FLAG_SKIP_LN, FLAG_OUT_ACC_I32, FLAG_BETA_CENTERED = 1, 2, 4
 OP_PACK, OP_QUANT, OP_FORWARD, OP_BACKWARD, OP_LN_BACKWARD, OP_FORWARD_NONNEG = 0, 1, 2, 3, 4, 5
-OP_MATMUL = 6
+OP_MATMUL, OP_ROUTE, OP_QUANT_NONLINEAR = 6, 7, 8
+FUNCTIONS = {"relu": 0, "relu2": 1, "gelu": 2, "silu": 3}
+F32, BF16 = 0, 1
 
 EXPORTS = (
     "bitlinear_packed_bytes", "bitlinear_workspace_bytes", "bitlinear_pack_weights",
@@ -31,6 +33,9 @@ EXPORTS = (
     "bitlinear_forward_nonneg", "bitlinear_forward_workspace_layout", "bitlinear_set_tuning",
     "bitlinear_forward_static", "bitlinear_probe_read", "bitlinear_weight_rowsums_grouped",
     "bitlinear_quant_act_grouped_nonneg", "bitlinear_forward_grouped_nonneg",
+    "bitlinear_workspace_bytes_experts", "bitlinear_route", "bitlinear_matmul_experts",
+    "bitlinear_backward_ste_experts", "bitlinear_combine", "bitlinear_combine_backward",
+    "bitlinear_quant_nonlinear", "bitlinear_nonlinear_backward",
 )
 
 _lib = None
@@ -102,6 +107,23 @@ def load_library() -> ctypes.CDLL:
     lib.bitlinear_forward_grouped_nonneg.restype = ci
     lib.bitlinear_forward_grouped_nonneg.argtypes = [vp, i64, i64, vp, i64, ci, ci, vp, vp, vp, vp, cf,
                                                      ci, u32, vp, vp, sz, vp]
+    lib.bitlinear_workspace_bytes_experts.restype = sz
+    lib.bitlinear_workspace_bytes_experts.argtypes = [ci, i64, ci, i64, i64, ci, ci]
+    lib.bitlinear_route.restype = ci
+    lib.bitlinear_route.argtypes = [vp, i64, ci, ci, vp, vp, vp, vp, sz, vp]
+    lib.bitlinear_matmul_experts.restype = ci
+    lib.bitlinear_matmul_experts.argtypes = [vp, vp, vp, i64, ci, i64, vp, vp, ci, vp, i64, vp, ci, u32, vp, vp]
+    lib.bitlinear_backward_ste_experts.restype = ci
+    lib.bitlinear_backward_ste_experts.argtypes = [vp, i64, ci, i64, i64, vp, vp, ci, vp, vp, ci, vp, vp, vp, vp,
+                                                   vp, sz, vp]
+    lib.bitlinear_combine.restype = ci
+    lib.bitlinear_combine.argtypes = [vp, vp, vp, i64, ci, i64, vp, vp]
+    lib.bitlinear_combine_backward.restype = ci
+    lib.bitlinear_combine_backward.argtypes = [vp, vp, vp, vp, i64, ci, i64, vp, vp, vp]
+    lib.bitlinear_quant_nonlinear.restype = ci
+    lib.bitlinear_quant_nonlinear.argtypes = [vp, i64, i64, ci, cf, vp, ci, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.bitlinear_nonlinear_backward.restype = ci
+    lib.bitlinear_nonlinear_backward.argtypes = [vp, vp, vp, i64, i64, ci, cf, vp, ci, vp, vp]
     lib.bitlinear_probe_read.restype = ci
     lib.bitlinear_probe_read.argtypes = [vp, sz, ci, ci, vp, vp]
     lib.bitlinear_forward_workspace_layout.restype = ci
@@ -465,4 +487,199 @@ def bitlinear_forward_nonneg(X: torch.Tensor, packed: torch.Tensor, N: int, beta
             _ptr(beta, torch.float32), _ptr(wsum, torch.int32), _ptr(ln_gain, torch.float32),
             _ptr(ln_bias, torch.float32), ln_eps, _gran(per_tensor), flags, _ptr(out), _ptr(ws),
             ws.numel(), _stream()), "bitlinear_forward_grouped_nonneg")
+    return out
+
+
+# ---- Mixtures of BitLinear layers ("experts") ------------------------------------------------
+def _given(dev, t: torch.Tensor, dtype, *shape):
+    """Pointer of an operand that has to lie on `dev` and have this type and shape."""
+    if t.device != dev:
+        raise BitLinearError(f"tensors on {dev} and {t.device}")
+    if tuple(t.shape) != shape:
+        raise BitLinearError(f"expected a tensor of shape {shape}, got {tuple(t.shape)}")
+    return _ptr(t, dtype)
+
+
+def _here(t: torch.Tensor):
+    """t's device, which has to be the current one: the launch goes to its current stream."""
+    if not t.is_cuda:
+        raise BitLinearError("tensor is not on the GPU")
+    if t.device.index != torch.cuda.current_device():
+        raise BitLinearError(f"tensor on {t.device}, current device {torch.cuda.current_device()}")
+    return t.device
+
+
+def workspace_bytes_experts(op: int, M: int, top_k: int, N: int, K: int, experts: int,
+                            per_tensor: bool = False) -> int:
+    return int(load_library().bitlinear_workspace_bytes_experts(op, M, top_k, N, K, experts, _gran(per_tensor)))
+
+
+def _scratch(need: int, workspace: torch.Tensor | None, dev):
+    """(pointer, bytes) of what the caller brought, or of a new buffer where one is needed."""
+    if workspace is None:
+        if not need:
+            return None, 0, None
+        workspace = _workspace(need, dev)
+    return _given(dev, workspace, torch.uint8, workspace.numel()), workspace.numel(), workspace
+
+
+def bitlinear_pack_weights_experts(W: torch.Tensor, flags: int = 0):
+    """Eq. 1-3, 12 for each expert of W [experts, N, K].  Returns (packed [experts, bytes], alpha [experts],
+    beta [experts])."""
+    lib, dev = load_library(), _here(W)
+    E, N, K = W.shape
+    nbytes = packed_bytes(N, K, flags)
+    if nbytes == 0:
+        _check(-2, "bitlinear_pack_weights")
+    packed = torch.empty((E, nbytes), dtype=torch.uint8, device=dev)
+    alpha = torch.empty(E, dtype=torch.float32, device=dev)
+    beta = torch.empty(E, dtype=torch.float32, device=dev)
+    ws = _workspace(workspace_bytes(OP_PACK, 0, N, K), dev)
+    src = _ptr(W, torch.float32)
+    for e in range(E):
+        _check(lib.bitlinear_pack_weights(src + 4 * e * N * K, N, K, flags, packed.data_ptr() + e * nbytes,
+                                          alpha.data_ptr() + 4 * e, beta.data_ptr() + 4 * e, _ptr(ws), ws.numel(),
+                                          _stream()), "bitlinear_pack_weights")
+    return packed, alpha, beta
+
+
+def bitlinear_route(expert: torch.Tensor, experts: int, workspace: torch.Tensor | None = None):
+    """The router's choices int32 [M, top_k] sorted by expert.  Returns (order [M * top_k], position [M, top_k],
+    offsets [experts + 1]), int32."""
+    lib, dev = load_library(), _here(expert)
+    M, top_k = expert.shape
+    order = torch.empty(M * top_k, dtype=torch.int32, device=dev)
+    position = torch.empty((M, top_k), dtype=torch.int32, device=dev)
+    offsets = torch.empty(experts + 1, dtype=torch.int32, device=dev) if M else torch.zeros(
+        experts + 1, dtype=torch.int32, device=dev)
+    ws, ws_bytes, _keep = _scratch(workspace_bytes_experts(OP_ROUTE, M, top_k, 0, 0, experts), workspace, dev)
+    _check(lib.bitlinear_route(_ptr(expert, torch.int32), M, top_k, experts, order.data_ptr(), position.data_ptr(),
+                               offsets.data_ptr(), ws, ws_bytes, _stream()), "bitlinear_route")
+    return order, position, offsets
+
+
+def _slots(codes, offsets, order, top_k):
+    """(M, top_k, T): the slots that `codes` serve, through `order` or one a row."""
+    M = codes.shape[0]
+    if order is None:
+        return M, 1, M
+    return M, top_k, M * top_k
+
+
+def bitlinear_matmul_experts(codes: torch.Tensor, gamma: torch.Tensor, rowsum: torch.Tensor, packed: torch.Tensor,
+                             N: int, beta: torch.Tensor, offsets: torch.Tensor, order: torch.Tensor | None = None,
+                             top_k: int = 1, per_tensor: bool = False, flags: int = 0,
+                             out: torch.Tensor | None = None) -> torch.Tensor:
+    """Eq. 7 + Eq. 11 with a weight matrix per expert: [slots, N] from the codes of tokens (through `order`, top_k slots
+    a token) or of the slots themselves.  Slots without an expert are left as they were in `out`."""
+    lib, dev = load_library(), _here(codes)
+    M, top_k, T = _slots(codes, offsets, order, top_k)
+    K, E = codes.shape[1], offsets.numel() - 1
+    dtype = torch.int32 if flags & FLAG_OUT_ACC_I32 else torch.float32
+    if out is None:
+        out = torch.empty((T, N), dtype=dtype, device=dev)
+    _check(lib.bitlinear_matmul_experts(
+        _ptr(codes, torch.int8), _given(dev, gamma, torch.float32, 1 if per_tensor else M),
+        _given(dev, rowsum, torch.int32, M), M, top_k, K, None if order is None else _given(dev, order, torch.int32, T),
+        _given(dev, offsets, torch.int32, E + 1), E, _given(dev, packed, torch.uint8, E, packed_bytes(N, K)), N,
+        _given(dev, beta, torch.float32, E), _gran(per_tensor), flags, _given(dev, out, dtype, T, N), _stream()),
+        "bitlinear_matmul_experts")
+    return out
+
+
+def bitlinear_backward_ste_experts(dY: torch.Tensor, codes: torch.Tensor, gamma: torch.Tensor,
+                                   packed: torch.Tensor | None, beta: torch.Tensor | None, offsets: torch.Tensor,
+                                   order: torch.Tensor | None = None, top_k: int = 1, per_tensor: bool = False,
+                                   want_dx: bool = True, want_dw: bool = True, workspace: torch.Tensor | None = None):
+    """Section 2.2 (STE) for bitlinear_matmul_experts, dY bf16 [slots, N].  Returns (dX fp32 [slots, K] or None,
+    dW fp32 [experts, N, K] or None)."""
+    lib, dev = load_library(), _here(codes)
+    M, top_k, T = _slots(codes, offsets, order, top_k)
+    K, E, N = codes.shape[1], offsets.numel() - 1, dY.shape[1]
+    dX = torch.empty((T, K), dtype=torch.float32, device=dev) if want_dx else None
+    dW = torch.empty((E, N, K), dtype=torch.float32, device=dev) if want_dw else None
+    ws, ws_bytes, _keep = _scratch(workspace_bytes_experts(OP_BACKWARD, M, top_k, N, K, E, per_tensor), workspace, dev)
+    _check(lib.bitlinear_backward_ste_experts(
+        _given(dev, dY, torch.bfloat16, T, N), M, top_k, N, K, _ptr(codes, torch.int8),
+        _given(dev, gamma, torch.float32, 1 if per_tensor else M), _gran(per_tensor),
+        None if order is None else _given(dev, order, torch.int32, T), _given(dev, offsets, torch.int32, E + 1), E,
+        None if packed is None else _given(dev, packed, torch.uint8, E, packed_bytes(N, K)),
+        None if beta is None else _given(dev, beta, torch.float32, E), _ptr(dX), _ptr(dW), ws, ws_bytes, _stream()),
+        "bitlinear_backward_ste_experts")
+    return dX, dW
+
+
+def bitlinear_combine(slots: torch.Tensor, position: torch.Tensor, weights: torch.Tensor | None = None,
+                      out: torch.Tensor | None = None) -> torch.Tensor:
+    """Slots [M * top_k, N] back to tokens [M, N], with the router's weights [M, top_k] (None: ones)."""
+    lib, dev = load_library(), _here(slots)
+    (M, top_k), N = position.shape, slots.shape[1]
+    if out is None:
+        out = torch.empty((M, N), dtype=torch.float32, device=dev)
+    _check(lib.bitlinear_combine(
+        _given(dev, slots, torch.float32, M * top_k, N), _given(dev, position, torch.int32, M, top_k),
+        None if weights is None else _given(dev, weights, torch.float32, M, top_k), M, top_k, N,
+        _given(dev, out, torch.float32, M, N), _stream()), "bitlinear_combine")
+    return out
+
+
+def bitlinear_combine_backward(dY: torch.Tensor, slots: torch.Tensor | None, position: torch.Tensor,
+                               weights: torch.Tensor | None = None, out: torch.Tensor | None = None):
+    """Gradient of bitlinear_combine.  Returns (dslots bf16 [M * top_k, N], dweights fp32 [M, top_k], or None without
+    `slots`).  Rows of slots that no choice has are left as they were in `out`."""
+    lib, dev = load_library(), _here(dY)
+    (M, top_k), N = position.shape, dY.shape[1]
+    if out is None:
+        out = torch.empty((M * top_k, N), dtype=torch.bfloat16, device=dev)
+    dweights = None if slots is None else torch.empty((M, top_k), dtype=torch.float32, device=dev)
+    _check(lib.bitlinear_combine_backward(
+        _given(dev, dY, torch.float32, M, N), None if slots is None else _given(dev, slots, torch.float32, M * top_k, N),
+        _given(dev, position, torch.int32, M, top_k),
+        None if weights is None else _given(dev, weights, torch.float32, M, top_k), M, top_k, N,
+        _given(dev, out, torch.bfloat16, M * top_k, N), _ptr(dweights), _stream()), "bitlinear_combine_backward")
+    return out, dweights
+
+
+def _function(fn: str) -> int:
+    if fn not in FUNCTIONS:
+        raise BitLinearError(f"unknown function {fn!r}: one of {', '.join(FUNCTIONS)}")
+    return FUNCTIONS[fn]
+
+
+def bitlinear_quant_nonlinear(U: torch.Tensor, fn: str = "gelu", ln_eps: float = 1e-5, per_tensor: bool = False,
+                              checkpoint: bool = False, rows: torch.Tensor | None = None,
+                              workspace: torch.Tensor | None = None):
+    """Function, LayerNorm and quantiser of U [M, K] in one pass.  Returns (codes, gamma, rowsum, check int8 [M, K],
+    check_scale fp32 [M, ceil(K / 128)]), the last two None without `checkpoint`.  rows: int32 [1], rows that exist."""
+    lib, dev = load_library(), _here(U)
+    M, K = U.shape
+    codes = torch.empty((M, K), dtype=torch.int8, device=dev)
+    gamma = torch.empty(1 if per_tensor else M, dtype=torch.float32, device=dev)
+    rowsum = torch.empty(M, dtype=torch.int32, device=dev)
+    check = torch.empty((M, K), dtype=torch.int8, device=dev) if checkpoint else None
+    scale = torch.empty((M, (K + 127) // 128), dtype=torch.float32, device=dev) if checkpoint else None
+    ws, ws_bytes, _keep = _scratch(workspace_bytes_experts(OP_QUANT_NONLINEAR, M, 1, 0, 0, 0, per_tensor), workspace, dev)
+    _check(lib.bitlinear_quant_nonlinear(
+        _ptr(U, torch.float32), M, K, _function(fn), ln_eps, None if rows is None else _given(dev, rows, torch.int32, 1),
+        _gran(per_tensor), codes.data_ptr(), gamma.data_ptr(), rowsum.data_ptr(), _ptr(check), _ptr(scale), ws, ws_bytes,
+        _stream()), "bitlinear_quant_nonlinear")
+    return codes, gamma, rowsum, check, scale
+
+
+def bitlinear_nonlinear_backward(dXhat: torch.Tensor, check: torch.Tensor, check_scale: torch.Tensor, fn: str = "gelu",
+                                 ln_eps: float = 1e-5, rows: torch.Tensor | None = None,
+                                 dtype: torch.dtype = torch.bfloat16, out: torch.Tensor | None = None) -> torch.Tensor:
+    """From the gradient of the normalised input of the next product to that of U, at the checkpoint: bf16 (as
+    bitlinear_backward_ste_experts reads it) or fp32 (bitlinear_backward_ste)."""
+    lib, dev = load_library(), _here(dXhat)
+    M, K = dXhat.shape
+    if dtype not in (torch.bfloat16, torch.float32):
+        raise BitLinearError(f"expected torch.bfloat16 or torch.float32, got {dtype}")
+    if out is None:
+        out = torch.empty((M, K), dtype=dtype, device=dev)
+    _check(lib.bitlinear_nonlinear_backward(
+        _ptr(dXhat, torch.float32), _given(dev, check, torch.int8, M, K),
+        _given(dev, check_scale, torch.float32, M, (K + 127) // 128), M, K, _function(fn), ln_eps,
+        None if rows is None else _given(dev, rows, torch.int32, 1), BF16 if dtype == torch.bfloat16 else F32,
+        _given(dev, out, dtype, M, K), _stream()), "bitlinear_nonlinear_backward")
     return out

@@ -15,7 +15,8 @@ CSRC = PKG / "csrc"
 OBJ = PKG / "_build"
 LIB = PKG / "libbitlinear.so"
 SOURCES = ["pack.hip", "quant.hip", "gemm_decode.hip", "gemm_tokens.hip", "gemm_prefill.hip", "gemm_mid.hip",
-           "gemm_stream.hip", "backward.hip", "ln_backward.hip", "api.hip"]
+           "gemm_stream.hip", "backward.hip", "ln_backward.hip", "route.hip", "experts.hip",
+           "experts_backward.hip", "nonlinear.hip", "api.hip", "api_experts.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [

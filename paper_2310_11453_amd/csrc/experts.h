@@ -1,0 +1,99 @@
+// Host-side launchers of the operators of a mixture of BitLinear layers; called from api_experts.hip only.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "common.h"
+
+namespace bl {
+
+constexpr int kMaxExperts = 256;
+constexpr int64_t kMaxRouteSlots = (int64_t)1 << 24;
+
+// route.hip
+struct RouteArgs {
+    const int32_t* expert;  // [T]
+    uint32_t T, E;
+    int32_t *order, *position, *offsets;
+    uint32_t* counts;  // [route_blocks][E], several blocks only
+};
+int64_t route_blocks(int64_t T);
+hipError_t launch_route(const RouteArgs& a, hipStream_t s);
+
+struct CombineArgs {
+    const float* slots;  // [T][N]; backward: may be null (no dweights)
+    const int32_t* position;
+    const float* weights;  // [M][top_k] or null: ones
+    int64_t M, N, T;
+    int top_k;
+    const float* dY;   // backward
+    float* Y;          // forward: [M][N]
+    uint16_t* dSlots;  // backward: bf16 [T][N]
+    float* dWeights;   // backward: [M][top_k] or null
+};
+hipError_t launch_combine(const CombineArgs& a, hipStream_t s);
+hipError_t launch_combine_backward(const CombineArgs& a, hipStream_t s);
+
+// nonlinear.hip
+constexpr int64_t kMaxNonlinearK = 32768;
+constexpr int kCheckBlock = 128;  // elements of a row that share a scale of the checkpoint
+struct NonlinearArgs {
+    const float* U;
+    int64_t M, K;
+    float eps;
+    double inv_k;         // 1 / K (set by the launcher)
+    const int32_t* rows;  // device: rows that exist, or null: all M
+    int8_t* codes;
+    float* gamma;
+    int32_t* rowsum;     // or null
+    int8_t* check;       // or null: no checkpoint
+    float* check_scale;  // [M][ceil(K / 128)]
+    bool per_tensor;
+    double* rowstats;     // per tensor: [M][2]
+    uint32_t* gmax_bits;  // per tensor: [1]
+    const float* dXhat;   // backward
+    void* dU;             // backward: fp32 or bf16
+    bool bf16;
+};
+hipError_t launch_quant_nonlinear(const NonlinearArgs& a, int fn, hipStream_t s);
+hipError_t launch_nonlinear_backward(const NonlinearArgs& a, int fn, hipStream_t s);
+
+// experts.hip, experts_backward.hip
+// Slot s of expert e, offsets[e] <= s < offsets[e + 1], is row order[s] / top_k of the codes (order null: row s).
+struct ExpertsArgs {
+    const int8_t* codes;
+    const float* gamma;
+    const int32_t* rowsum;
+    int64_t rows;  // of the codes
+    int64_t T, K, N;
+    const int32_t* order;
+    int top_k;
+    const int32_t* offsets;  // [E + 1]
+    int E;
+    const uint32_t* packed;  // E blobs
+    const float* beta;       // [E]
+    bool per_tensor, out_acc;
+    float* Y;
+    const uint16_t* dY;  // backward: bf16 [T][N]
+    float *dX, *dW;
+    void* workspace;
+    size_t workspace_bytes;
+};
+hipError_t launch_matmul_experts(const ExpertsArgs& a, hipStream_t s);
+size_t experts_backward_bytes(int64_t T, int64_t N, int64_t K, int E);
+hipError_t launch_experts_backward(const ExpertsArgs& a, hipStream_t s);
+
+#ifdef __HIPCC__
+// Segments come from memory: what is read of them is held to 0 .. T, so that no value of theirs leads out of a tensor.
+__device__ inline int slot_bound(const int32_t* offsets, int e, int T) {
+    const int v = offsets[e];
+    return v < 0 ? 0 : v < T ? v : T;
+}
+// the row of the codes that slot s reads
+__device__ inline uint32_t code_row(const int32_t* order, uint32_t top_k, uint32_t rows, uint32_t s) {
+    const uint32_t r = order ? (uint32_t)order[s] / top_k : s;
+    return r < rows ? r : rows - 1;
+}
+#endif
+
+}  // namespace bl

@@ -1,0 +1,330 @@
+// Between the two projections of a feed-forward network of BitLinear layers: a non-linear function f, the LayerNorm of
+// Eq. 12 and the 8-bit quantiser of Eq. 4-5 in one pass over the first projection's output u, with an optional 8-bit
+// checkpoint of u; and the backward pass, from that checkpoint.
+//   forward    h = f(u), x^ = (h - mean h) / sqrt(var h + eps), gamma = max|x^|, code = clamp(rne(x^ * (128 / gamma)))
+//              checkpoint, per block b of 128 elements of a row: c = rne(u * (127 / amax_b)), kept beside amax_b / 127
+//   backward   v = c * (amax_b / 127), h = f(v), n = (h - mean h) / sqrt(var h + eps)
+//              du = f'(v) * (g - mean g - n mean(g n)) / sqrt(var h + eps),  g = the gradient of x^
+// The backward is the derivative of the forward at v, exactly: its statistics are those of f(v), which come out of the row
+// that is in registers anyway, and nothing but the checkpoint has to be kept (1.03 bytes an element where u has four).
+// f and f' are evaluated in fp32, the sums of a row in fp64 (as in the quantiser and in the LayerNorm backward).
+// Bound by HBM: 4 bytes read and 1 (with the checkpoint 2) written an element, twice the reading with a gamma per
+// tensor; backward 5 read, 2 or 4 written.
+#include "common.h"
+#include "experts.h"
+#include "kernels.h"
+#include "rowops.h"
+
+namespace bl {
+
+enum Fn { kRelu = 0, kRelu2 = 1, kGelu = 2, kSilu = 3 };
+enum RowMode { kOnce = 0, kRowStats = 1, kRowApply = 2 };
+
+template <int FN>
+__device__ inline float fn_value(float u) {
+    if constexpr (FN == kRelu) return u > 0.f ? u : 0.f;
+    else if constexpr (FN == kRelu2) return u > 0.f ? u * u : 0.f;
+    else if constexpr (FN == kGelu) return 0.5f * u * (1.f + erff(u * 0.70710678118654752f));
+    else return u / (1.f + expf(-u));
+}
+template <int FN>
+__device__ inline float fn_slope(float u) {
+    if constexpr (FN == kRelu) {
+        return u > 0.f ? 1.f : 0.f;
+    } else if constexpr (FN == kRelu2) {
+        return u > 0.f ? 2.f * u : 0.f;
+    } else if constexpr (FN == kGelu) {
+        return 0.5f * (1.f + erff(u * 0.70710678118654752f)) + u * (0.39894228040143268f * expf(-0.5f * u * u));
+    } else {
+        const float s = 1.f / (1.f + expf(-u));
+        return s + u * s * (1.f - s);
+    }
+}
+
+// the largest value of 32 lanes, one half of a wave
+__device__ inline float half_wave_max(float v) {
+    v = max_raw(v, dpp_mov<0xB1>(v));
+    v = max_raw(v, dpp_mov<0x4E>(v));
+    v = max_raw(v, dpp_mov<0x141>(v));
+    v = max_raw(v, dpp_mov<0x140>(v));
+    float lo, hi;
+    lane_swap<false>(v, lo, hi);
+    return max_raw(lo, hi);
+}
+
+// WPR waves share a row, a lane holds NV float4 of it.  kRowStats and kRowApply: the two passes of a gamma per tensor; the
+// first leaves the row's statistics in rowstats and its largest magnitude where its codes will be, which nobody
+// writes before the second.
+template <int FN, int WPR, int NV, int MODE>
+__global__ __launch_bounds__((WPR < 4 ? 4 : WPR) * kWave) void nonlinear_rows(NonlinearArgs a) {
+    constexpr int NW = WPR < 4 ? 4 : WPR, RPW = NW / WPR, RT = WPR * kWave;
+    __shared__ double sm_k[2 * NW];
+    __shared__ float sm_f[2 * NW];
+    __shared__ int smi[NW];
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
+    const int rw = wave / WPR, wr = wave % WPR;
+    const int t = wr * kWave + (threadIdx.x & (kWave - 1));
+    const int64_t M = a.rows ? (*a.rows < a.M ? *a.rows : a.M) : a.M;
+    int64_t row = (int64_t)blockIdx.x * RPW + rw;
+    if ((int64_t)blockIdx.x * RPW >= M) return;  // uniform for the workgroup
+    const bool live = row < M;
+    if (!live) row = M - 1;
+    const int K4 = (int)(a.K / 4);
+    const float4* __restrict__ x4 = reinterpret_cast<const float4*>(a.U + row * a.K);
+
+    float4 v[NV];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        const int idx = t + j * RT;
+        v[j] = x4[(uint32_t)(idx < K4 ? idx : K4 - 1)];
+    }
+    const float first = fn_value<FN>(a.U[row * a.K]);
+
+    if (MODE != kRowApply && a.check) {  // uniform
+        uint32_t* __restrict__ c4 = reinterpret_cast<uint32_t*>(a.check + row * a.K);
+        const int blocks = (int)((a.K + kCheckBlock - 1) / kCheckBlock);
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const int idx = t + j * RT;
+            const bool in = idx < K4;
+            const float4 x = v[j];
+            const float big = half_wave_max(in ? max_raw(max_raw(fabsf(x.x), fabsf(x.y)), max_raw(fabsf(x.z), fabsf(x.w))) : 0.f);
+            const float up = big > 0.f ? 127.f / big : 0.f;
+            if (in && live) {
+                c4[idx] = code_word(x.x * up, x.y * up, x.z * up, x.w * up, -127.f);
+                if ((t & 31) == 0) a.check_scale[row * blocks + (idx >> 5)] = big / 127.f;
+            }
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        v[j].x = fn_value<FN>(v[j].x);
+        v[j].y = fn_value<FN>(v[j].y);
+        v[j].z = fn_value<FN>(v[j].z);
+        v[j].w = fn_value<FN>(v[j].w);
+    }
+
+    const float cf = stats_centre(first);
+    const double c = (double)cf;
+    RowNorm n;
+    float amax = 0.f;
+    if constexpr (MODE == kRowApply) {
+        n.shift = a.rowstats[2 * row];
+        n.rstd = a.rowstats[2 * row + 1];
+    } else {
+        RowStats rs;
+        rs.mx = cf;
+        rs.nmn = -cf;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            if (K4 < (j + 1) * RT) {  // uniform: this piece of the row is ragged
+                const bool in = t + j * RT < K4;
+                v[j].x = in ? v[j].x : cf;
+                v[j].y = in ? v[j].y : cf;
+                v[j].z = in ? v[j].z : cf;
+                v[j].w = in ? v[j].w : cf;
+            }
+            double d[4];
+            stats_add(rs, v[j], c, d);
+        }
+        PairStats st = stats_wave(rs);
+        if constexpr (WPR > 1) {
+            stats_leave(st, sm_k, sm_f, wave);
+            __syncthreads();
+            st = stats_fold(sm_k + 2 * rw * WPR, sm_f + 2 * rw * WPR, WPR);
+        }
+        float lo, hi;
+        n = stats_finish(st, c, a.inv_k, (double)a.eps, lo, hi);
+        amax = fmaxf(fabsf(lo), fabsf(hi));  // h -> x^ is monotone
+        if constexpr (MODE == kRowStats) {
+            if (t == 0 && live) {
+                a.rowstats[2 * row] = n.shift;
+                a.rowstats[2 * row + 1] = n.rstd;
+                reinterpret_cast<uint32_t*>(a.codes)[row] = __float_as_uint(amax);
+            }
+            return;
+        }
+    }
+    const float gamma = fmaxf(MODE == kRowApply ? __uint_as_float(*a.gmax_bits) : amax, 1e-5f);
+    const float scale = 128.0f / gamma;
+    int sum = 0;
+    uint32_t* __restrict__ q4 = reinterpret_cast<uint32_t*>(a.codes + row * a.K);
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        const int idx = t + j * RT;
+        const uint32_t wd = code_word(normalised(n, (double)v[j].x - c) * scale, normalised(n, (double)v[j].y - c) * scale,
+                                      normalised(n, (double)v[j].z - c) * scale, normalised(n, (double)v[j].w - c) * scale);
+        if (idx < K4) {
+            sum = __builtin_amdgcn_sdot4((int)wd, 0x01010101, sum, false);
+            if (live) q4[(uint32_t)idx] = wd;
+        }
+    }
+    if (a.rowsum) {  // uniform
+        sum = row_reduce<WPR>(sum, OpSum{}, smi, rw, wr);
+        if (t == 0 && live) a.rowsum[row] = sum;
+    }
+    if (t == 0 && live && (MODE == kOnce || row == 0)) a.gamma[row] = gamma;
+}
+
+// the largest of the rows' magnitudes (non-negative floats order like their bit patterns)
+__global__ __launch_bounds__(1024) void nonlinear_fold(NonlinearArgs a) {
+    constexpr int NW = 16;
+    __shared__ float sm[NW];
+    const int64_t M = a.rows ? (*a.rows < a.M ? *a.rows : a.M) : a.M;
+    float most = 0.f;
+#pragma unroll 8
+    for (int64_t i = threadIdx.x; i < M; i += 1024) most = max_raw(most, reinterpret_cast<const float*>(a.codes)[i]);
+    most = wave_reduce(most, OpMax{});
+    if (threadIdx.x % kWave == 0) sm[threadIdx.x / kWave] = most;
+    __syncthreads();
+    if (threadIdx.x >= kWave) return;
+    most = fold_slots<NW>(sm, OpMax{});
+    if (threadIdx.x == 0) *a.gmax_bits = __float_as_uint(most);
+}
+
+// ---- backward -----------------------------------------------------------------------------------------
+__device__ inline uint32_t bf16_word(float lo, float hi) {
+    auto rne = [](float v) {
+        uint32_t u = __float_as_uint(v);
+        u += 0x7fffu + ((u >> 16) & 1u);
+        return u >> 16;
+    };
+    return rne(lo) | rne(hi) << 16;
+}
+
+template <int FN, int WPR, int NV>
+__global__ __launch_bounds__((WPR < 4 ? 4 : WPR) * kWave) void nonlinear_backward_rows(NonlinearArgs a) {
+    constexpr int NW = WPR < 4 ? 4 : WPR, RPW = NW / WPR, RT = WPR * kWave;
+    __shared__ double smd[4][NW];
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
+    const int rw = wave / WPR, wr = wave % WPR;
+    const int t = wr * kWave + (threadIdx.x & (kWave - 1));
+    const int64_t M = a.rows ? (*a.rows < a.M ? *a.rows : a.M) : a.M;
+    int64_t row = (int64_t)blockIdx.x * RPW + rw;
+    if ((int64_t)blockIdx.x * RPW >= M) return;  // uniform for the workgroup
+    const bool live = row < M;
+    if (!live) row = M - 1;
+    const int K4 = (int)(a.K / 4);
+    const int blocks = (int)((a.K + kCheckBlock - 1) / kCheckBlock);
+    const float4* __restrict__ g4 = reinterpret_cast<const float4*>(a.dXhat + row * a.K);
+    const uint32_t* __restrict__ c4 = reinterpret_cast<const uint32_t*>(a.check + row * a.K);
+
+    float4 g[NV], v[NV];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        const int idx = t + j * RT, at = idx < K4 ? idx : K4 - 1;
+        g[j] = g4[at];
+        const uint32_t q = c4[at];
+        const float sc = a.check_scale[row * blocks + (at >> 5)];
+        v[j].x = (float)(int8_t)q * sc;
+        v[j].y = (float)(int8_t)(q >> 8) * sc;
+        v[j].z = (float)(int8_t)(q >> 16) * sc;
+        v[j].w = (float)(int8_t)(q >> 24) * sc;
+    }
+    // sums about an element of the row, so that a large common offset costs nothing
+    const double c = (double)fn_value<FN>((float)a.check[row * a.K] * a.check_scale[row * blocks]);
+    double s[4] = {0.0, 0.0, 0.0, 0.0};  // of h - c, (h - c)^2, g, g (h - c)
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        if (t + j * RT >= K4) continue;
+        auto add = [&](float u, float d) {
+            const double h = (double)fn_value<FN>(u) - c;
+            s[0] += h;
+            s[1] = fma(h, h, s[1]);
+            s[2] += (double)d;
+            s[3] = fma((double)d, h, s[3]);
+        };
+        add(v[j].x, g[j].x);
+        add(v[j].y, g[j].y);
+        add(v[j].z, g[j].z);
+        add(v[j].w, g[j].w);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) s[i] = wave_reduce(s[i], OpSum{});
+    if constexpr (WPR > 1) {
+        if ((threadIdx.x & (kWave - 1)) == 0)
+            for (int i = 0; i < 4; ++i) smd[i][wave] = s[i];
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[i] = fold_slots<WPR>(smd[i] + rw * WPR, OpSum{});
+    }
+    const double dm = s[0] * a.inv_k, var = fmax(fma(-dm, dm, s[1] * a.inv_k), 0.0);
+    const double rstd = rsqrt64(var + (double)a.eps);
+    const float r = (float)rstd;
+    const float m1 = (float)(s[2] * a.inv_k), m2 = (float)((s[3] - dm * s[2]) * rstd * a.inv_k);
+    const double nshift = -(dm * rstd);
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        const int idx = t + j * RT;
+        auto du = [&](float u, float d) {
+            const float n = (float)fma((double)fn_value<FN>(u) - c, rstd, nshift);
+            return r * ((d - m1) - n * m2) * fn_slope<FN>(u);
+        };
+        const float x = du(v[j].x, g[j].x), y = du(v[j].y, g[j].y), z = du(v[j].z, g[j].z), w = du(v[j].w, g[j].w);
+        if (idx < K4 && live) {
+            if (a.bf16) reinterpret_cast<uint2*>(reinterpret_cast<uint16_t*>(a.dU) + row * a.K)[idx] = make_uint2(bf16_word(x, y), bf16_word(z, w));
+            else reinterpret_cast<float4*>(reinterpret_cast<float*>(a.dU) + row * a.K)[idx] = make_float4(x, y, z, w);
+        }
+    }
+}
+
+// Waves a row and float4 a lane: enough waves that the chip has about sixteen a CU, at most eight float4 a lane.
+struct RowShape {
+    int wpr, nv;
+};
+static RowShape row_shape(int64_t M, int64_t K) {
+    constexpr RowShape shapes[] = {{1, 2}, {1, 4}, {1, 8}, {4, 2}, {4, 4}, {4, 8}, {8, 4}, {8, 8}, {16, 8}};
+    const int64_t K4 = K / 4;
+    for (const RowShape& q : shapes) {
+        if (K4 > (int64_t)q.wpr * kWave * q.nv) continue;
+        if (q.wpr == 1 && M < 2048 && K4 >= 4 * kWave * 2) continue;  // few rows: more waves share one
+        return q;
+    }
+    return {16, 8};
+}
+
+template <int FN, int WPR, int NV>
+static void launch_forward(const NonlinearArgs& a, hipStream_t s) {
+    constexpr int NW = WPR < 4 ? 4 : WPR, RPW = NW / WPR;
+    const unsigned grid = (unsigned)((a.M + RPW - 1) / RPW);
+    if (!a.per_tensor) {
+        nonlinear_rows<FN, WPR, NV, kOnce><<<grid, NW * kWave, 0, s>>>(a);
+        return;
+    }
+    nonlinear_rows<FN, WPR, NV, kRowStats><<<grid, NW * kWave, 0, s>>>(a);
+    nonlinear_fold<<<1, 1024, 0, s>>>(a);
+    nonlinear_rows<FN, WPR, NV, kRowApply><<<grid, NW * kWave, 0, s>>>(a);
+}
+template <int FN, int WPR, int NV>
+static void launch_backward_rows(const NonlinearArgs& a, hipStream_t s) {
+    constexpr int NW = WPR < 4 ? 4 : WPR, RPW = NW / WPR;
+    nonlinear_backward_rows<FN, WPR, NV><<<(unsigned)((a.M + RPW - 1) / RPW), NW * kWave, 0, s>>>(a);
+}
+
+template <int FN>
+static hipError_t launch_fn(const NonlinearArgs& a_in, bool backward, hipStream_t s) {
+    NonlinearArgs a = a_in;
+    a.inv_k = 1.0 / (double)a.K;
+    const RowShape q = row_shape(a.M, a.K);
+#define BL_ROWS(W, V)                                        \
+    if (q.wpr == W && q.nv == V) {                           \
+        if (backward) launch_backward_rows<FN, W, V>(a, s);  \
+        else launch_forward<FN, W, V>(a, s);                 \
+    }
+    BL_ROWS(1, 2) BL_ROWS(1, 4) BL_ROWS(1, 8) BL_ROWS(4, 2) BL_ROWS(4, 4) BL_ROWS(4, 8) BL_ROWS(8, 4) BL_ROWS(8, 8)
+    BL_ROWS(16, 8)
+#undef BL_ROWS
+    return hipGetLastError();
+}
+static hipError_t launch_any(const NonlinearArgs& a, int fn, bool backward, hipStream_t s) {
+    switch (fn) {
+        case kRelu: return launch_fn<kRelu>(a, backward, s);
+        case kRelu2: return launch_fn<kRelu2>(a, backward, s);
+        case kGelu: return launch_fn<kGelu>(a, backward, s);
+        default: return launch_fn<kSilu>(a, backward, s);
+    }
+}
+hipError_t launch_quant_nonlinear(const NonlinearArgs& a, int fn, hipStream_t s) { return launch_any(a, fn, false, s); }
+hipError_t launch_nonlinear_backward(const NonlinearArgs& a, int fn, hipStream_t s) { return launch_any(a, fn, true, s); }
+
+}  // namespace bl
