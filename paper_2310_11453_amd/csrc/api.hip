@@ -29,7 +29,7 @@ const TuningField kTuningFields[] = {
     {"quant_wpr", &Tuning::quant_wpr},           {"bwd_ring", &Tuning::bwd_ring},
     {"bwd_grid", &Tuning::bwd_grid},             {"bwd_rowmajor", &Tuning::bwd_rowmajor},
     {"bwd_splits", &Tuning::bwd_splits},         {"bwd_dx", &Tuning::bwd_dx},
-    {"mid_kernel", &Tuning::mid_kernel},
+    {"mid_kernel", &Tuning::mid_kernel},         {"experts_tile", &Tuning::experts_tile},
 };
 Tuning g_tuning{};
 bool g_tuning_init = false;

@@ -94,6 +94,48 @@ __device__ inline uint32_t code_row(const int32_t* order, uint32_t top_k, uint32
     const uint32_t r = order ? (uint32_t)order[s] / top_k : s;
     return r < rows ? r : rows - 1;
 }
+
+// Rows of tiles of BM slots: expert e has those from `first[e]` on, its slots begin at `slot[e]`.
+struct ExpertTiles {
+    int first[kMaxExperts + 1], slot[kMaxExperts + 1];
+};
+// Counts them, all threads of a workgroup of 256 or more; their number.
+__device__ inline int expert_tiles(const int32_t* offsets, int E, int T, int BM, ExpertTiles& sm) {
+    const int e = (int)threadIdx.x, l = e & (kWave - 1);
+    if (e < kMaxExperts) {
+        const int from = e < E ? slot_bound(offsets, e, T) : 0, to = e < E ? slot_bound(offsets, e + 1, T) : 0;
+        int v = to > from ? (to - from + BM - 1) / BM : 0;
+#pragma unroll
+        for (int d = 1; d < kWave; d <<= 1) {
+            const int o = __shfl_up(v, d, kWave);
+            if (l >= d) v += o;
+        }
+        sm.first[e + 1] = v;
+        if (e < E) sm.slot[e] = from, sm.slot[e + 1] = to;
+    }
+    __syncthreads();
+    int lower = 0;
+    if (e < kMaxExperts)
+        for (int i = kWave; i <= e; i += kWave) lower += sm.first[i];
+    __syncthreads();
+    if (e < kMaxExperts) sm.first[e + 1] += lower;
+    if (e == 0) sm.first[0] = 0;
+    __syncthreads();
+    return sm.first[E];
+}
+// The expert of a row of tiles, and where that row's slots begin and the expert's end.
+__device__ inline int expert_of_tile(const ExpertTiles& sm, int E, int tile, int BM, int& from, int& to) {
+    int lo = 0, hi = E - 1;  // the last expert whose first row of tiles is not behind `tile`
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) / 2;
+        if (sm.first[mid] <= tile) lo = mid;
+        else hi = mid - 1;
+    }
+    lo = __builtin_amdgcn_readfirstlane(lo);
+    from = __builtin_amdgcn_readfirstlane(sm.slot[lo] + (tile - sm.first[lo]) * BM);
+    to = __builtin_amdgcn_readfirstlane(sm.slot[lo + 1]);
+    return lo;
+}
 #endif
 
 }  // namespace bl

@@ -3,6 +3,7 @@
 // Few rows an expert: bound by the packed weights of the experts that have any.
 #include "common.h"
 #include "experts.h"
+#include "kernels.h"
 
 namespace bl {
 
@@ -91,6 +92,17 @@ __global__ __launch_bounds__(rows::kMaxWaves* kWave) void experts_rows_kernel(Ex
 }
 
 hipError_t launch_matmul_experts(const ExpertsArgs& a, hipStream_t s) {
+    const int force = tuning().experts_tile;
+    const int tile = force ? force : a.T / a.E > 160 ? 2 : a.T / a.E > 32 ? 1 : 4;
+    if (tile <= 2 && (int64_t)a.rows * a.K < (int64_t)1 << 32) {
+        GemmArgs g{};
+        g.codes = a.codes; g.gamma = a.gamma; g.rowsum = a.rowsum; g.M = a.T; g.K = a.K; g.N = a.N;
+        g.packed = a.packed; g.beta = a.beta; g.per_tensor = a.per_tensor; g.out_acc = a.out_acc; g.Y = a.Y;
+        g.ldy = a.N; g.ldq = a.K; g.gstride = 1; g.beta_rows = a.N;
+        g.offsets = a.offsets; g.order = a.order; g.experts = a.E; g.top_k = a.top_k; g.rows = (uint32_t)a.rows;
+        g.blob = tiles_n(a.N) * tiles_k(a.K) * 256;
+        return launch_experts_tiles(g, tile, s);
+    }
     const int64_t TN = tiles_n(a.N), TK = tiles_k(a.K);
     const int W = (int)(TK < rows::kMaxWaves ? TK : rows::kMaxWaves);
     const dim3 grid((unsigned)((TN + rows::kTiles - 1) / rows::kTiles), (unsigned)(a.T < a.E ? a.T : a.E));

@@ -41,6 +41,7 @@
 // fence: a fence would drain every DMA in flight).  After that barrier stage st+1 is
 // readable and the buffer of stage st-1 is free, so the DMA of stage st+NS-1 goes there.
 #include "common.h"
+#include "experts.h"
 #include "kernels.h"
 #include "ring.h"
 
@@ -137,7 +138,9 @@ __device__ inline void lds_write_b32(uint32_t ad, uint32_t v) {
 // Persistent: gridDim.x workgroups (one per CU) walk the tiles t = blockIdx.x, + gridDim.x, ...
 // GEN = false: the plain layer (one beta, Y = result): nothing of what follows costs anything.
 // GEN = true adds beta per column group (Eq. 13) and the shift term of Eq. 6.
-template <int BM, int BN, int WM, int WN, int NS, bool GEN>
+// EXP = true: a mixture of experts (the fields of GemmArgs say what it reads).  Where an expert's rows begin is in device
+// memory, so every workgroup counts the experts' rows of tiles for itself (ExpertTiles) and the grid is a bound.
+template <int BM, int BN, int WM, int WN, int NS, bool GEN, bool EXP = false>
 __global__ __launch_bounds__(WM * WN * 64, 2) void gemm_prefill_kernel(GemmArgs a, int grid_m,
                                                                         int grid_n, int xbm) {
     constexpr int THREADS = WM * WN * kWave;
@@ -171,6 +174,8 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void gemm_prefill_kernel(GemmArgs 
     // chunks whose look-ahead stays inside K and that have a successor chunk
     const int64_t main_chunks = kfull >= NS + 7 ? (kfull - NS - 7) / 8 + 1 : 0;
     const int64_t TKp = a.tk_pitch ? a.tk_pitch : tiles_k(a.K);  // tiles per tile row in memory
+    __shared__ std::conditional_t<EXP, ExpertTiles, int> smE;
+    if constexpr (EXP) grid_m = expert_tiles(a.offsets, a.experts, (int)a.M, BM, smE);
     const int ntiles = grid_m * grid_n;
 
     // Tile order.  Workgroups are dealt round-robin to the 8 XCDs, each with its own L2; give
@@ -179,9 +184,30 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void gemm_prefill_kernel(GemmArgs 
     // band the rows fastest: an XCD's range is then a block of xbm x (range / xbm) tiles and it
     // fetches xbm row blocks of codes (BM x K bytes each) and range / xbm column blocks of packed
     // weights (BN x K / 8 bytes each).  xbm = 1 unless the host asks otherwise (see launch_tile).
-    auto tile_origin = [&](int t, int64_t& m0, int64_t& n0) {
+    // A mixture's tiles are as many as its tokens make them: the XCDs' ranges differ by a tile then.  end, e: where the
+    // rows of the tile's expert end, and which it is.
+    auto tile_origin = [&](int t, int64_t& m0, int64_t& n0, int64_t& end, int& e) {
         int logical = t;
         const int G = (int)gridDim.x;
+        end = M;
+        e = 0;
+        if constexpr (EXP) {
+            if ((G & 7) == 0) {
+                const int x = t & 7, q = ((t % G) >> 3) + (t / G) * (G >> 3);
+                logical = (int)((int64_t)ntiles * x / 8) + q;
+                if (logical >= (int)((int64_t)ntiles * (x + 1) / 8)) logical = -1;
+            } else if (t >= ntiles) {
+                logical = -1;
+            }
+            m0 = n0 = -1;
+            if (logical < 0) return;
+            int from, to;
+            e = expert_of_tile(smE, a.experts, logical / grid_n, BM, from, to);
+            m0 = from;
+            end = to;
+            n0 = (int64_t)(logical % grid_n) * BN;
+            return;
+        }
         if ((ntiles & 7) == 0 && (G & 7) == 0) {
             const int q = ((t % G) >> 3) + (t / G) * (G >> 3);  // index inside the XCD's range
             logical = (t & 7) * (ntiles >> 3) + q;
@@ -207,16 +233,18 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void gemm_prefill_kernel(GemmArgs 
     int gseg[P];
     const int8_t* gbase = a.codes;
     const uint32_t* bsrc[NBW];
-    auto setup_dma = [&](int64_t m0, int64_t n0) {
+    auto setup_dma = [&](int64_t m0, int64_t n0, int64_t end, int e) {
 #pragma unroll
         for (int q = 0; q < P; ++q) {
             const int slot = q * THREADS + threadIdx.x;
             int row = slot >> 2;
             gseg[q] = ((slot & 3) ^ ((row >> 2) & 3)) * 16;
-            if (m0 + row > M - 1) row = (int)(M - 1 - m0);
-            goff[q] = (uint32_t)row * (uint32_t)a.ldq + gseg[q];
+            if (m0 + row > (EXP ? end : M) - 1) row = (int)((EXP ? end : M) - 1 - m0);
+            if constexpr (EXP)  // rows * ldq < 2^32
+                goff[q] = code_row(a.order, (uint32_t)a.top_k, a.rows, (uint32_t)(m0 + row)) * (uint32_t)a.ldq + gseg[q];
+            else goff[q] = (uint32_t)row * (uint32_t)a.ldq + gseg[q];
         }
-        gbase = a.codes + m0 * a.ldq;
+        gbase = EXP ? a.codes : a.codes + m0 * a.ldq;
         // packed weights: tile t of the block goes to smB + t KiB, lane for lane as it lies in
         // memory; wave w moves tiles w, w + NWAVES, ...  Columns past N read a valid tile.
 #pragma unroll
@@ -224,6 +252,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void gemm_prefill_kernel(GemmArgs 
             int64_t tn = (n0 >> 4) + w + q * NWAVES;
             if (tn > TN - 1) tn = TN - 1;
             bsrc[q] = a.packed + tile_dword_offset(tn, 0, TKp) + l * 4;
+            if constexpr (EXP) bsrc[q] += e * a.blob;
         }
     };
     const uint32_t lds_wave = (uint32_t)(w * kWave * 16);
@@ -338,11 +367,11 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void gemm_prefill_kernel(GemmArgs 
         else dma();
     };
 
-    int t = (int)blockIdx.x, parity = 0;
-    int64_t m0, n0;
-    tile_origin(t, m0, n0);
+    int t = (int)blockIdx.x, parity = 0, expert;
+    int64_t m0, n0, end;
+    tile_origin(t, m0, n0, end, expert);
     if (m0 < 0) return;  // uniform for the whole workgroup
-    setup_dma(m0, n0);
+    setup_dma(m0, n0, end, expert);
     issue_tile_start();
 
     while (true) {
@@ -378,12 +407,13 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void gemm_prefill_kernel(GemmArgs 
             }
         } else {
             // per-row dequantisation scale (Eq. 11) and row sum of the codes, for the epilogue
-            const float beta = *a.beta;
+            const float beta = EXP ? a.beta[expert] : *a.beta;
             for (int r = threadIdx.x; r < BM; r += THREADS) {
-                const int64_t m = m0 + r;
+                int64_t m = m0 + r;
                 float sc = 0.f;
                 int rs = 0;
-                if (m < M) {
+                if (m < (EXP ? end : M)) {
+                    if constexpr (EXP) m = code_row(a.order, (uint32_t)a.top_k, a.rows, (uint32_t)m);
                     sc = (beta * (a.per_tensor ? a.gamma[0] : a.gamma[m])) / 128.0f;
                     rs = a.rowsum[m];
                 }
@@ -419,10 +449,11 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void gemm_prefill_kernel(GemmArgs 
         // Every wave is done with the LDS ring: start the next tile's stream, then store.
         block_barrier();
         const int t_next = t + (int)gridDim.x;
-        int64_t m0n = -1, n0n = -1;
-        if (t_next < ntiles) tile_origin(t_next, m0n, n0n);
+        int64_t m0n = -1, n0n = -1, endn = 0;
+        int expertn = 0;
+        if (t_next < ntiles || EXP) tile_origin(t_next, m0n, n0n, endn, expertn);
         if (m0n >= 0) {
-            setup_dma(m0n, n0n);
+            setup_dma(m0n, n0n, endn, expertn);
             issue_tile_start();
         }
 
@@ -450,7 +481,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void gemm_prefill_kernel(GemmArgs 
             v4i rs4;
             float e = 0.f;
             store_tile<MI, NI, (BM < 256)>(
-                a.Y + (m0 + wrow) * a.ldy + n0 + wcolumn, a.ldy, M - m0 - wrow, a.N - n0 - wcolumn, j, g2,
+                a.Y + (m0 + wrow) * a.ldy + n0 + wcolumn, a.ldy, (EXP ? end : M) - m0 - wrow, a.N - n0 - wcolumn, j, g2,
                 [&](int mi, int rq) {
                     lds_read_rows(sc4, rs4, sc_base + (32 * mi + 8 * rq) * 4, rs_base + (32 * mi + 8 * rq) * 4);
                 },
@@ -467,7 +498,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void gemm_prefill_kernel(GemmArgs 
                 });
         };
         if (!a.out_acc &&  // uniform
-            (BM < 256 || (m0 + BM <= M && n0 + BN <= a.N && a.ldy < (1 << 24)))) {
+            (BM < 256 || (m0 + BM <= (EXP ? end : M) && n0 + BN <= a.N && a.ldy < (1 << 24)))) {
             if (GEN && a.eta) store_plain(std::integral_constant<bool, GEN>{});
             else store_plain(std::false_type{});
         } else {
@@ -486,7 +517,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void gemm_prefill_kernel(GemmArgs 
                     for (int rr = 0; rr < 4; ++rr) {
                         const int r = rq * 4 + rr;
                         const int64_t m = m0 + wm * WTM + 32 * mi + 8 * rq + 4 * g2 + rr;
-                        if (m >= M) continue;
+                        if (m >= (EXP ? end : M)) continue;
 #pragma unroll
                         for (int s = 0; s < NI; ++s) {
                             const int64_t n = n0 + wn * WTN + 32 * s + j;
@@ -513,6 +544,8 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void gemm_prefill_kernel(GemmArgs 
         t = t_next;
         m0 = m0n;
         n0 = n0n;
+        end = endn;
+        expert = expertn;
         parity ^= 1;
     }
 }
@@ -852,6 +885,20 @@ static void launch_tile(const GemmArgs& a, hipStream_t s) {
     else
         gemm_prefill_kernel<BM, BN, WM, WN, NS, true>
             <<<(unsigned)grid, WM * WN * kWave, 0, s>>>(a, grid_m, grid_n, xbm);
+}
+
+// A mixture of experts: the tiles of a bound of its rows of tiles, one for every BM slots and one more for each expert.
+template <int BM>
+static void launch_experts_tile(const GemmArgs& a, hipStream_t s) {
+    const int64_t grid_n = (a.N + 255) / 256, most = (a.M / BM + (a.M < a.experts ? a.M : a.experts)) * grid_n;
+    const int grid = (int)(most < num_cus() ? most : num_cus());
+    gemm_prefill_kernel<BM, 256, 2, 4, 8, false, true><<<(unsigned)grid, 512, 0, s>>>(a, 0, (int)grid_n, 1);
+}
+hipError_t launch_experts_tiles(const GemmArgs& a, int tile, hipStream_t s) {
+    if (a.K > kMaxGemmK || (int64_t)a.rows * a.ldq >= (int64_t)1 << 32) return hipErrorInvalidValue;
+    if (tile == 1) launch_experts_tile<128>(a, s);
+    else launch_experts_tile<256>(a, s);
+    return hipGetLastError();
 }
 
 // Kernel and K-slices for M > 64: the cheapest of all by these costs in us, fitted to medians of graph

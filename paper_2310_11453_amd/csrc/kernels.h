@@ -30,6 +30,7 @@ struct Tuning {
     int bwd_splits;        // backward ring kernels: slices of the reduction
     int group_slices;      // grouped layer, M <= 64: every K-group a slice of the grid (work item) of its own
     int mid_kernel;        // accepted, without effect
+    int experts_tile;      // products of experts: 1 = 128 x 256, 2 = 256 x 256, 4 = a few rows at a time
 };
 const Tuning& tuning();
 
@@ -138,6 +139,14 @@ struct GemmArgs {
     float* gamma_out;
     int32_t* rowsum_out;
     float* xhat_out;  // [K]: the normalised row the codes were rounded from
+    // A mixture of experts (launch_experts_tiles, and only it): slots offsets[e] .. offsets[e + 1] - 1 of Y are the rows
+    // of expert e, whose weights are packed + e * blob dwords and whose scale is beta[e]; slot s reads row order[s] /
+    // top_k (order null: s) of the `rows` rows of codes, gamma and rowsum.  M: an upper bound of offsets[experts].
+    const int32_t* offsets;
+    const int32_t* order;
+    int experts, top_k;
+    uint32_t rows;  // rows * ldq < 2^32
+    int64_t blob;
 };
 size_t gemm_split_ws_bytes(int64_t M, int64_t N, int64_t K);
 size_t prefill_split_bytes(int64_t M, int64_t N, int64_t K, bool one_beta);
@@ -152,6 +161,7 @@ bool gemm_tokens_fuses_quant(int64_t M, int64_t K, int64_t N);  // gamma per tok
 hipError_t launch_gemm_tokens(const GemmArgs& a, hipStream_t s);
 int num_cus();  // of the device current at the first call
 hipError_t launch_gemm_prefill(const GemmArgs& a, hipStream_t s);
+hipError_t launch_experts_tiles(const GemmArgs& a, int tile, hipStream_t s);  // tile: 1 = 128 x 256, 2 = 256 x 256
 hipError_t launch_gemm_mid(const GemmArgs& a, hipStream_t s);  // 16 < M <= 64
 hipError_t launch_gemm_mid_tiles(const GemmArgs& a, int bm, int64_t per, hipStream_t s);  // M > 64
 bool launch_gemm_stream(const GemmArgs& a, hipStream_t s);      // 16 < M <= 32; false: not taken

@@ -109,27 +109,34 @@ def test_route_without_tokens(bl):
 # ---- the experts' products -------------------------------------------------------------------------
 # one token; fewer slots than experts; ragged K (one short chunk, several chunks and a part), N that ends inside a tile of 16;
 # around the row counts where an expert's rows fill a tile; more experts than a wave has lanes
+TILES = [0, 1, 2, 4]
 PRODUCTS = [(1, 1, 1, 32, 1), (1, 2, 8, 256, 512), (3, 2, 4, 544, 40), (16, 2, 4, 512, 130), (40, 1, 3, 96, 300),
             (33, 4, 100, 160, 48), (130, 2, 4, 1056, 257), (300, 1, 2, 2048, 136), (700, 2, 5, 640, 520),
             (1500, 2, 3, 416, 264)]
 
 
+# The library picks the tiles from the shape; the experts_tile switch forces each kind.
 @pytest.mark.parametrize("M,top_k,E,K,N", PRODUCTS)
-@pytest.mark.parametrize("gather", [True, False])
-@pytest.mark.parametrize("per_tensor", [False, True])
-def test_products_exact(bl, M, top_k, E, K, N, gather, per_tensor):
-    print(f"products M={M} top_k={top_k} E={E} K={K} N={N} gather={gather} per_tensor={per_tensor}", flush=True)
+@pytest.mark.parametrize("gather,per_tensor", [(True, False), (True, True), (False, False)])
+@pytest.mark.parametrize("tile", TILES)
+def test_products_exact(bl, tuning, M, top_k, E, K, N, gather, per_tensor, tile):
+    print(f"products M={M} top_k={top_k} E={E} K={K} N={N} gather={gather} per_tensor={per_tensor} tile={tile}", flush=True)
+    tuning(f"experts_tile={tile}")
     check_products(bl, M, top_k, E, K, N, gather, per_tensor, choices(M, top_k, E, M + K, unrouted=0.1))
 
 
 @pytest.mark.parametrize("only", [[0], [6], [2, 5]])
 @pytest.mark.parametrize("M", [1, 20, 400, 1100])
-def test_products_when_few_experts_have_all_slots(bl, M, only):
-    print(f"products M={M} only {only}", flush=True)
+@pytest.mark.parametrize("tile", TILES)
+def test_products_when_few_experts_have_all_slots(bl, tuning, M, only, tile):
+    print(f"products M={M} only {only} tile={tile}", flush=True)
+    tuning(f"experts_tile={tile}")
     check_products(bl, M, 2, 7, 288, 272, True, False, choices(M, 2, 7, M, only=only))
 
 
-def test_products_when_no_choice_has_an_expert(bl):
+@pytest.mark.parametrize("tile", TILES)
+def test_products_when_no_choice_has_an_expert(bl, tuning, tile):
+    tuning(f"experts_tile={tile}")
     check_products(bl, 50, 2, 4, 96, 64, True, False, np.full((50, 2), -1, np.int32))
 
 
@@ -398,7 +405,7 @@ def test_mixture_forward_and_backward(bl, M, top_k, E, d, width, per_tensor):
     slots = torch.cat(parts + [torch.zeros(M * top_k - used, d, dtype=torch.float64, device="cuda")])
     has = (s["position"] >= 0).double()
     out = (slots[s["position"].long().clamp_min(0)] * (Wd * has).unsqueeze(2)).sum(1)
-    assert float((Y.double() - out).norm()) <= 1e-5 * float(out.norm()) + 1e-12  # fp32 at each of four steps
+    assert float((Y.double() - out.detach()).norm()) <= 1e-5 * float(out.detach().norm()) + 1e-12  # fp32 at each of four steps
     out.backward(dY.double())
     # gradients pass two roundings to bf16 (2^-8 each at most, 2^-8 again with gammas of tokens): 1.2 % at the very most
     for got, ref in ((dX, Xd.grad), (dW1, W1.grad), (dW2, W2.grad), (dw, Wd.grad)):
