@@ -441,7 +441,8 @@ int bitlinear_probe_read(const void* src, size_t bytes, int workgroups, int thre
  *   bwd_dx=1|2          backward, dX: 256 x 256 or 128 x 256 output tiles
  *   bwd_grid=g, bwd_rowmajor=1   backward ring kernel: workgroups, plain tile order
  *   bwd_splits=n        backward ring kernels: slices of the reduction (tiles of 256 columns)
- *   experts_tile=1|2|4  products of experts: 128 x 256 or 256 x 256 output tiles, or a few rows at a time
+ *   experts_tile=1|2|3|4|5  products of experts: 128 x 256, 256 x 256, 128 x 128 or 64 x 128 output tiles, or a
+ *                       few rows at a time
  * Returns BL_OK, or BL_ERR_UNSUPPORTED (unknown name or bad syntax; nothing changes). */
 int bitlinear_set_tuning(const char* spec);
 

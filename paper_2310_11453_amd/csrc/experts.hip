@@ -8,93 +8,155 @@
 namespace bl {
 
 namespace rows {
-constexpr int kTiles = 4;     // 16-row weight tiles of a workgroup
 constexpr int kMaxWaves = 8;  // share the 512-chunks of K
-constexpr int kTokens = 16;   // slots of a pass
+constexpr int kSlots = 16;    // slots of a workgroup
+struct Args {
+    const int8_t* codes;
+    const uint32_t* packed;
+    const int32_t *offsets, *order;
+    uint32_t T, E, top_k, rows, TN, TK, K, N;
+    int64_t blob;
+    const float *gamma, *beta;
+    const int32_t* rowsum;
+    bool per_tensor, out_acc;
+    float* Y;
+};
 }  // namespace rows
 
-// blockIdx.x: a group of weight tiles, blockIdx.y: the how-manieth expert that has slots.  Wave w takes the 512-chunks w,
-// w + W, ... of K; the weights are the row operand of v_mfma_i32_16x16x64_i8, 16 slots its columns; a lane's 16
-// bytes of a packed tile hold 16 consecutive k of each of eight bit planes, (w >> i) & 0x01010101 is plane i as {0,1}
-// bytes, and sum_k q s = 2 sum_k q b - sum_k q.  The waves' sums meet in LDS.  More than 16 slots: pass after pass.
-__global__ __launch_bounds__(rows::kMaxWaves* kWave) void experts_rows_kernel(ExpertsArgs a, int64_t blob) {
+// blockIdx.x: a group of TILES 16-row weight tiles, blockIdx.y: the how-manieth 16 slots of an expert.  Wave w takes the
+// 512-chunks w, w + W, ... of K; the weights are the row operand of v_mfma_i32_16x16x64_i8, the slots its columns; a
+// lane's 16 bytes of a packed tile hold 16 consecutive k of each of eight bit planes, (w >> i) & 0x01010101 is plane i as
+// {0,1} bytes, and sum_k q s = 2 sum_k q b - sum_k q.  The waves' sums meet in LDS.
+// A launch is a chain of trips to memory: the experts' bounds, then the weights and (in two trips) the codes, whose rows
+// are known only with the order.  So the first chunk's weights are requested as soon as the expert is known and the
+// epilogue's operands with the codes.
+template <int TILES>
+__global__ __launch_bounds__(rows::kMaxWaves* kWave) void experts_rows_kernel(rows::Args a) {
     using namespace rows;
-    __shared__ int red[kMaxWaves][kTiles][kTokens][kTileN + 1];
+    __shared__ int red[kMaxWaves][TILES][kSlots][kTileN + 1];
+    __shared__ float sm_scale[kSlots];
+    __shared__ int sm_sum[kSlots];
     const int W = (int)blockDim.x / kWave;
     const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave), l = threadIdx.x & (kWave - 1);
-    const int T = (int)a.T;
-    int e = -1, left = (int)blockIdx.y;
-    for (int b = 0; b < a.E; b += kWave) {
-        const bool some = b + l < a.E && slot_bound(a.offsets, b + l, T) < slot_bound(a.offsets, b + l + 1, T);
-        uint64_t m = __ballot(some);
-        const int n = __popcll(m);
-        if (left >= n) {
-            left -= n;
-            continue;
-        }
-        for (; left > 0; --left) m &= m - 1;
-        e = b + __ffsll((unsigned long long)m) - 1;
-        break;
-    }
-    if (e < 0) return;  // uniform: fewer experts have slots
-    const int s0 = slot_bound(a.offsets, e, T), s1 = slot_bound(a.offsets, e + 1, T);
-    const int64_t TN = tiles_n(a.N), TK = tiles_k(a.K);
-    const int t0 = (int)blockIdx.x * kTiles, nt = (int)(TN - t0 < kTiles ? TN - t0 : kTiles);
-    const uint32_t* wbase = a.packed + e * blob;
-    const float beta = a.beta[e];
     const int col = l & 15, g = l >> 4;
 
-    for (int m0 = s0; m0 < s1; m0 += kTokens) {
-        const int s = m0 + col < s1 ? m0 + col : s1 - 1;
-        const int8_t* x = a.codes + (int64_t)code_row(a.order, (uint32_t)a.top_k, (uint32_t)a.rows, (uint32_t)s) * a.K;
-        v4i acc[kTiles] = {};
-        for (int64_t c = w; c < TK; c += W) {
-            v4i act[8];
+    // the expert of this workgroup's slots: a lane counts the sixteens of an expert
+    int e = -1, s0 = 0, s1 = 0, left = (int)blockIdx.y;
+    for (int b = 0; b < (int)a.E; b += kWave) {
+        const int at = b + l < (int)a.E ? b + l : (int)a.E - 1;
+        const int from = slot_bound(a.offsets, at, (int)a.T), to = slot_bound(a.offsets, at + 1, (int)a.T);
+        const int n = b + l < (int)a.E && to > from ? (to - from + kSlots - 1) / kSlots : 0;
+        int v = n;
+#pragma unroll
+        for (int d = 1; d < kWave; d <<= 1) {
+            const int o = __shfl_up(v, d, kWave);
+            if (l >= d) v += o;
+        }
+        const uint64_t behind = __ballot(v > left);
+        if (behind) {
+            const int lane = __ffsll((unsigned long long)behind) - 1;
+            e = b + lane;
+            s0 = __builtin_amdgcn_readlane(from, lane) + (left - __builtin_amdgcn_readlane(v - n, lane)) * kSlots;
+            s1 = __builtin_amdgcn_readlane(to, lane);
+            break;
+        }
+        left -= __builtin_amdgcn_readlane(v, kWave - 1);
+    }
+    if (e < 0) return;  // uniform: the grid is a bound
+
+    const uint32_t t0 = blockIdx.x * TILES, last = a.TN - 1;
+    const uint32_t* const wbase = a.packed + e * a.blob;
+    auto load = [&](v4i (&q)[TILES], uint32_t c) {
+#pragma unroll
+        for (int t = 0; t < TILES; ++t) {
+            const uint32_t tn = t0 + t < last ? t0 + t : last;
+            q[t] = __builtin_nontemporal_load(reinterpret_cast<const v4i*>(wbase + ((uint64_t)tn * a.TK + c) * 256 + l * 4));
+        }
+    };
+    v4i q[TILES];
+    load(q, w);
+    const int s = s0 + col < s1 ? s0 + col : s1 - 1;
+    const uint32_t row = code_row(a.order, a.top_k, a.rows, (uint32_t)s);
+    const int8_t* const x = a.codes + (uint64_t)row * a.K + 16 * g;
+    const uint32_t klast = a.K - 16 - 16 * g;  // past the row its last 16 bytes again: the packed bits there are zero
+    float gamma = 0.f;
+    int sum = 0;
+    if (w == 0 && l < kSlots) {
+        gamma = a.gamma[a.per_tensor ? 0 : row];
+        sum = a.rowsum[row];
+    }
+    const float beta = a.beta[e];
+
+    v4i acc[TILES] = {};
+    for (uint32_t c = w; c < a.TK; c += W) {
+        v4i act[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const uint32_t k = c * kChunkK + 64 * i;
+            act[i] = *reinterpret_cast<const v4i*>(x + (int32_t)(k < klast ? k : klast));
+        }
+        if (c != (uint32_t)w) load(q, c);
+#pragma unroll
+        for (int t = 0; t < TILES; ++t)
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                int64_t k = c * kChunkK + 64 * i + 16 * g;
-                if (k > a.K - 16) k = a.K - 16;  // the packed bits there are zero
-                act[i] = *reinterpret_cast<const v4i*>(x + k);
+                v4i b;
+#pragma unroll
+                for (int d = 0; d < 4; ++d) b[d] = (int)(((uint32_t)q[t][d] >> i) & 0x01010101u);
+                acc[t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(b, act[i], acc[t], 0, 0, 0);
             }
-#pragma unroll
-            for (int t = 0; t < kTiles; ++t) {
-                const int tn = t < nt ? t0 + t : t0;
-                const v4i q = *reinterpret_cast<const v4i*>(wbase + tile_dword_offset(tn, c, TK) + l * 4);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    v4i b;
-#pragma unroll
-                    for (int d = 0; d < 4; ++d) b[d] = (int)(((uint32_t)q[d] >> i) & 0x01010101u);
-                    acc[t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(b, act[i], acc[t], 0, 0, 0);
-                }
-            }
-        }
-        // lane: slot col, weight rows 4 g + r of each tile
-#pragma unroll
-        for (int t = 0; t < kTiles; ++t)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) red[w][t][col][4 * g + r] = acc[t][r];
-        __syncthreads();
-        for (int i = threadIdx.x; i < nt * kTokens * kTileN; i += blockDim.x) {
-            const int n16 = i & 15, m = (i >> 4) % kTokens, t = (i >> 4) / kTokens;
-            const int64_t n = (int64_t)(t0 + t) * kTileN + n16;
-            if (m0 + m >= s1 || n >= a.N) continue;
-            int sum = 0;
-            for (int v = 0; v < W; ++v) sum += red[v][t][m][n16];
-            const int64_t r = code_row(a.order, (uint32_t)a.top_k, (uint32_t)a.rows, (uint32_t)(m0 + m));
-            sum = 2 * sum - a.rowsum[r];
-            const int64_t o = (int64_t)(m0 + m) * a.N + n;
-            if (a.out_acc) reinterpret_cast<int*>(a.Y)[o] = sum;
-            else a.Y[o] = (float)sum * ((beta * a.gamma[a.per_tensor ? 0 : r]) / 128.0f);
-        }
-        __syncthreads();
     }
+    // lane: slot col, weight rows 4 g + r of each tile
+#pragma unroll
+    for (int t = 0; t < TILES; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) red[w][t][col][4 * g + r] = acc[t][r];
+    if (w == 0 && l < kSlots) {
+        sm_scale[l] = (beta * gamma) / 128.0f;
+        sm_sum[l] = sum;
+    }
+    __syncthreads();
+    const int n_slots = s1 - s0 < kSlots ? s1 - s0 : kSlots;
+    for (int i = threadIdx.x; i < n_slots * TILES * kTileN; i += blockDim.x) {
+        const int nl = i % (TILES * kTileN), m = i / (TILES * kTileN);
+        const uint32_t n = t0 * kTileN + nl;
+        if (n >= a.N) continue;
+        int v = 0;
+        for (int p = 0; p < W; ++p) v += red[p][nl >> 4][m][nl & 15];
+        v = 2 * v - sm_sum[m];
+        float* const o = a.Y + (uint64_t)(s0 + m) * a.N + n;
+        if (a.out_acc) *reinterpret_cast<int*>(o) = v;
+        else *o = (float)v * sm_scale[m];
+    }
+}
+
+static void launch_rows(const ExpertsArgs& a, hipStream_t s) {
+    const int64_t TN = tiles_n(a.N), TK = tiles_k(a.K);
+    const int64_t A = a.T < a.E ? a.T : a.E, blocks = a.T / rows::kSlots + A;
+    // Tiles of a workgroup: more of them share the fixed chain and the codes, fewer leave no CU idle.
+    int tiles = tuning().decode_tiles;
+    if (!tiles) tiles = blocks * TN < 512 ? 1 : blocks * TN < 1280 || TK < 4 ? 2 : TK >= 8 && blocks * TN < 6144 && blocks * TN > 4096 ? 8 : 4;
+    rows::Args r{};
+    r.codes = a.codes; r.packed = a.packed; r.offsets = a.offsets; r.order = a.order;
+    r.T = (uint32_t)a.T; r.E = (uint32_t)a.E; r.top_k = (uint32_t)a.top_k; r.rows = (uint32_t)a.rows;
+    r.TN = (uint32_t)TN; r.TK = (uint32_t)TK; r.K = (uint32_t)a.K; r.N = (uint32_t)a.N;
+    r.blob = TN * TK * 256;
+    r.gamma = a.gamma; r.beta = a.beta; r.rowsum = a.rowsum;
+    r.per_tensor = a.per_tensor; r.out_acc = a.out_acc; r.Y = a.Y;
+    const unsigned threads = (unsigned)(TK < rows::kMaxWaves ? TK : rows::kMaxWaves) * kWave;
+    auto launch = [&](auto kernel, int n) {
+        kernel<<<dim3((unsigned)((TN + n - 1) / n), (unsigned)blocks), threads, 0, s>>>(r);
+    };
+    if (tiles <= 1) launch(experts_rows_kernel<1>, 1);
+    else if (tiles <= 2) launch(experts_rows_kernel<2>, 2);
+    else if (tiles <= 4) launch(experts_rows_kernel<4>, 4);
+    else launch(experts_rows_kernel<8>, 8);
 }
 
 hipError_t launch_matmul_experts(const ExpertsArgs& a, hipStream_t s) {
     const int force = tuning().experts_tile;
-    const int tile = force ? force : a.T / a.E > 160 ? 2 : a.T / a.E > 32 ? 1 : 4;
-    if (tile <= 2 && (int64_t)a.rows * a.K < (int64_t)1 << 32) {
+    const int tile = force ? force : a.T / a.E > 160 ? 2 : a.T / a.E > 32 ? 1 : 5;
+    if (tile <= 4 && (int64_t)a.rows * a.K < (int64_t)1 << 32) {
         GemmArgs g{};
         g.codes = a.codes; g.gamma = a.gamma; g.rowsum = a.rowsum; g.M = a.T; g.K = a.K; g.N = a.N;
         g.packed = a.packed; g.beta = a.beta; g.per_tensor = a.per_tensor; g.out_acc = a.out_acc; g.Y = a.Y;
@@ -103,10 +165,7 @@ hipError_t launch_matmul_experts(const ExpertsArgs& a, hipStream_t s) {
         g.blob = tiles_n(a.N) * tiles_k(a.K) * 256;
         return launch_experts_tiles(g, tile, s);
     }
-    const int64_t TN = tiles_n(a.N), TK = tiles_k(a.K);
-    const int W = (int)(TK < rows::kMaxWaves ? TK : rows::kMaxWaves);
-    const dim3 grid((unsigned)((TN + rows::kTiles - 1) / rows::kTiles), (unsigned)(a.T < a.E ? a.T : a.E));
-    experts_rows_kernel<<<grid, W * kWave, 0, s>>>(a, tiles_n(a.N) * TK * 256);
+    launch_rows(a, s);
     return hipGetLastError();
 }
 

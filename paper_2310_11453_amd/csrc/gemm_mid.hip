@@ -28,6 +28,7 @@
 // before (the compiler's scheduler is told so with sched_group_barrier), two half-steps ahead of
 // its use, so a wave keeps the matrix pipe fed without help from the other wave of its SIMD.
 #include "common.h"
+#include "experts.h"
 #include "kernels.h"
 #include "ring.h"
 
@@ -93,6 +94,10 @@ struct Args {
     bool per_tensor, out_acc, to_slices;
     float* Y;
     int32_t* split_ws;
+    // a mixture of experts (GemmArgs says what these are)
+    const int32_t *offsets, *order;
+    uint32_t experts, top_k, rows;
+    int64_t blob;
 };
 // n / d by a multiplication where the host found it exact (m = 2^32 / d, rounded up; n d < 2^32)
 __device__ inline uint32_t divided(uint32_t n, uint32_t d, uint32_t m) {
@@ -115,7 +120,9 @@ static uint32_t divisor(int64_t d, int64_t n_max) {
 // gmode 1: a work item is (column tile, one K-group of the layer), split over the workgroup's four.
 // NS = stages in each group's ring.
 // ROWS = false: one row tile (M <= BM).  STREAM: streaming stores (streaming_stores below).
-template <int BM, int NS, bool ROWS, bool STREAM>
+// EXP: a mixture of experts.  Items go expert by expert, inside one the row tiles of a column tile next to each other; how
+// many there are the workgroups count for themselves (the grid is a bound), in what will be the bits' buffer.
+template <int BM, int NS, bool ROWS, bool STREAM, bool EXP = false>
 __global__ __launch_bounds__(mid::THREADS) void gemm_mid_kernel(mid::Args a) {
     using namespace mid;
     constexpr int WM = BM / 64, GW = WM * WN;   // waves of a K-group
@@ -140,9 +147,28 @@ __global__ __launch_bounds__(mid::THREADS) void gemm_mid_kernel(mid::Args a) {
     const int kg = w / GW, wi = w % GW, wm = wi / WN, wn = wi % WN;
     const int tg = threadIdx.x % GT;  // thread inside the K-group
     const int j = l & 31, g2 = l >> 5;
-    const int M = (int)a.M, N = (int)a.N;  // at most 2^30
+    int M = (int)a.M;
+    const int N = (int)a.N;  // at most 2^30
     int tm = 0, tcol = (int)blockIdx.x, sp = (int)blockIdx.y;
-    if constexpr (ROWS) {  // the host rounds the grid up to a multiple of 8
+    int m0 = 0, expert = 0;
+    if constexpr (EXP) {
+        static_assert(sizeof(ExpertTiles) <= sizeof(smB), "room to count in");
+        ExpertTiles& count = *reinterpret_cast<ExpertTiles*>(smB);
+        const int64_t items = (int64_t)expert_tiles(a.offsets, (int)a.experts, M, BM, count) * a.grid_n;
+        const int x = (int)(blockIdx.x & 7), item = (int)(items * x / 8) + (int)(blockIdx.x >> 3);
+        sp = 0;
+        if (item >= (int)(items * (x + 1) / 8)) return;  // uniform for the workgroup
+        int to;
+        expert = expert_of_tile(count, (int)a.experts, item / (int)a.grid_n, BM, m0, to);
+        const int first = __builtin_amdgcn_readfirstlane(count.first[expert]);
+        const int rows = __builtin_amdgcn_readfirstlane(count.first[expert + 1]) - first;
+        const int at = item - first * (int)a.grid_n;
+        tcol = at / rows;
+        m0 = __builtin_amdgcn_readfirstlane(count.slot[expert]) + (at - tcol * rows) * BM;
+        M = to;
+        a.packed += expert * a.blob;
+        __syncthreads();  // the count has been read
+    } else if constexpr (ROWS) {  // the host rounds the grid up to a multiple of 8
         const uint32_t item = (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3);
         if (item >= a.items) return;  // uniform for the workgroup
         const uint32_t rest = divided(item, a.grid_m, a.div_m);
@@ -150,7 +176,7 @@ __global__ __launch_bounds__(mid::THREADS) void gemm_mid_kernel(mid::Args a) {
         sp = a.splits > 1 ? (int)divided(rest, a.grid_n, a.div_n) : 0;
         tcol = (int)(rest - (uint32_t)sp * a.grid_n);
     }
-    const int m0 = ROWS ? tm * BM : 0;
+    if constexpr (!EXP) m0 = ROWS ? tm * BM : 0;
     const int n0 = tcol * BN;
 
     // ---- this item's slice of K, then this group's chunks of it ----------------------------
@@ -187,14 +213,16 @@ __global__ __launch_bounds__(mid::THREADS) void gemm_mid_kernel(mid::Args a) {
     uint8_t* const ringA = smA + kg * (NS * STAGE_BYTES);
     uint8_t* const ringB = smB + kg * ((BN / 16) * 1024);
     // (row offsets fit 32 bits: at most 128 rows of less than 2^22 bytes)
-    const int8_t* const gbase = a.codes + ((uint64_t)(uint32_t)m0 * a.ldq + (uint32_t)k0);
+    const int8_t* const gbase = a.codes + ((EXP ? 0 : (uint64_t)(uint32_t)m0 * a.ldq) + (uint32_t)k0);
     static_assert((GT / 8) % 16 == 0, "the pieces of a thread lie in the same segment of their rows");
     const uint32_t gseg = (uint32_t)(((tg & 7) ^ ((tg >> 4) & 7)) * 16);
     uint32_t grow[P];
 #pragma unroll
     for (int q = 0; q < P; ++q) {
         const int row = q * (GT / 8) + (tg >> 3);
-        grow[q] = __umul24((uint32_t)(row < M - 1 - m0 ? row : M - 1 - m0), a.ldq);
+        const int in = row < M - 1 - m0 ? row : M - 1 - m0;
+        if constexpr (EXP) grow[q] = code_row(a.order, a.top_k, a.rows, (uint32_t)(m0 + in)) * a.ldq;  // < 2^32
+        else grow[q] = __umul24((uint32_t)in, a.ldq);
     }
     const uint32_t klast = K >= 16 ? (uint32_t)K - 16 : 0;
     // uniform base, 32-bit offsets: eight rows of tiles of at most 128 KiB
@@ -241,15 +269,18 @@ __global__ __launch_bounds__(mid::THREADS) void gemm_mid_kernel(mid::Args a) {
     int e0 = 0, e1 = 0, e2 = 0;
     if (!to_slices) {
         if (w < BM / kWave) {
-            const int r = m0 + (int)threadIdx.x;
-            const int64_t m = (int64_t)(r < M ? r : M - 1) * a.gstride, mg = a.per_tensor ? 0 : m;
+            int r = m0 + (int)threadIdx.x;
+            r = r < M ? r : M - 1;
+            if constexpr (EXP) r = (int)code_row(a.order, a.top_k, a.rows, (uint32_t)r);
+            const int64_t m = (int64_t)r * a.gstride, mg = a.per_tensor ? 0 : m;
             e0 = __float_as_int(a.gamma[mg]);
             e1 = a.rowsum[m];
             if (a.eta) e2 = __float_as_int(a.eta[mg]);
         } else if (w == 4 || w == 5) {
             const int c = n0 + (int)threadIdx.x - 4 * kWave, n = c < N ? c : N - 1;
             int64_t at = 0;
-            if ((int)a.beta_rows < N) at = (int64_t)((uint32_t)n / a.beta_rows) * a.beta_stride;
+            if constexpr (EXP) at = expert;
+            else if ((int)a.beta_rows < N) at = (int64_t)((uint32_t)n / a.beta_rows) * a.beta_stride;
             e0 = __float_as_int(a.beta[at]);
             if (a.eta) e1 = a.wsum[n];
         }
@@ -584,6 +615,12 @@ static mid::Args mid_args(const GemmArgs& a, int grid_m, int grid_n, int splits,
     m.to_slices = a.split_k || a.kgroups > 1;
     m.Y = a.Y;
     m.split_ws = a.split_ws;
+    m.offsets = a.offsets;
+    m.order = a.order;
+    m.experts = (uint32_t)a.experts;
+    m.top_k = (uint32_t)a.top_k;
+    m.rows = a.rows;
+    m.blob = a.blob;
     return m;
 }
 
@@ -644,6 +681,19 @@ hipError_t launch_gemm_mid_tiles(const GemmArgs& a_in, int bm, int64_t per, hipS
     if (bm == 64) launch(streaming ? gemm_mid_kernel<64, 4, true, true> : gemm_mid_kernel<64, 4, true, false>);
     else launch(streaming ? gemm_mid_kernel<128, 4, true, true> : gemm_mid_kernel<128, 4, true, false>);
     if (splits > 1) launch_splitk_reduce(a, splits, s);
+    return hipGetLastError();
+}
+
+// A mixture of experts: the items of a bound of its rows of tiles.
+hipError_t launch_experts_mid(const GemmArgs& a, int bm, hipStream_t s) {
+    const int64_t grid_n = (a.N + mid::BN - 1) / mid::BN;
+    const int64_t items = ((a.M / bm + (a.M < a.experts ? a.M : a.experts)) * grid_n + 7) / 8 * 8;
+    if (a.K > kMaxGemmK || items > ((int64_t)1 << 22)) return hipErrorInvalidValue;
+    const mid::Args args = mid_args(a, 0, (int)grid_n, 1, 0);
+    const bool streaming = streaming_stores(a, 1, false);
+    auto launch = [&](auto kernel) { kernel<<<(unsigned)items, mid::THREADS, 0, s>>>(args); };
+    if (bm == 64) launch(streaming ? gemm_mid_kernel<64, 4, true, true, true> : gemm_mid_kernel<64, 4, true, false, true>);
+    else launch(streaming ? gemm_mid_kernel<128, 4, true, true, true> : gemm_mid_kernel<128, 4, true, false, true>);
     return hipGetLastError();
 }
 

@@ -30,7 +30,7 @@ struct Tuning {
     int bwd_splits;        // backward ring kernels: slices of the reduction
     int group_slices;      // grouped layer, M <= 64: every K-group a slice of the grid (work item) of its own
     int mid_kernel;        // accepted, without effect
-    int experts_tile;      // products of experts: 1 = 128 x 256, 2 = 256 x 256, 4 = a few rows at a time
+    int experts_tile;      // products of experts: 1 .. 4 as prefill_tile, 5 = a few rows at a time
 };
 const Tuning& tuning();
 
@@ -161,7 +161,9 @@ bool gemm_tokens_fuses_quant(int64_t M, int64_t K, int64_t N);  // gamma per tok
 hipError_t launch_gemm_tokens(const GemmArgs& a, hipStream_t s);
 int num_cus();  // of the device current at the first call
 hipError_t launch_gemm_prefill(const GemmArgs& a, hipStream_t s);
-hipError_t launch_experts_tiles(const GemmArgs& a, int tile, hipStream_t s);  // tile: 1 = 128 x 256, 2 = 256 x 256
+// tile: 1 = 128 x 256, 2 = 256 x 256; 3 = 128 x 128, 4 = 64 x 128 (launch_experts_mid)
+hipError_t launch_experts_tiles(const GemmArgs& a, int tile, hipStream_t s);
+hipError_t launch_experts_mid(const GemmArgs& a, int bm, hipStream_t s);
 hipError_t launch_gemm_mid(const GemmArgs& a, hipStream_t s);  // 16 < M <= 64
 hipError_t launch_gemm_mid_tiles(const GemmArgs& a, int bm, int64_t per, hipStream_t s);  // M > 64
 bool launch_gemm_stream(const GemmArgs& a, hipStream_t s);      // 16 < M <= 32; false: not taken

@@ -109,7 +109,7 @@ def test_route_without_tokens(bl):
 # ---- the experts' products -------------------------------------------------------------------------
 # one token; fewer slots than experts; ragged K (one short chunk, several chunks and a part), N that ends inside a tile of 16;
 # around the row counts where an expert's rows fill a tile; more experts than a wave has lanes
-TILES = [0, 1, 2, 4]
+TILES = [0, 1, 2, 3, 4, 5]
 PRODUCTS = [(1, 1, 1, 32, 1), (1, 2, 8, 256, 512), (3, 2, 4, 544, 40), (16, 2, 4, 512, 130), (40, 1, 3, 96, 300),
             (33, 4, 100, 160, 48), (130, 2, 4, 1056, 257), (300, 1, 2, 2048, 136), (700, 2, 5, 640, 520),
             (1500, 2, 3, 416, 264)]
