@@ -1,6 +1,8 @@
 // 1-bit x 8-bit products of a mixture of BitLinear layers (Eq. 7 and 11 of arXiv 2310.11453, a weight matrix per expert):
 //   Y[s,n] = (sum_k q[r,k] S_e[n,k]) * (beta_e gamma_r / 128)    for the slots s of expert e, r the row that s reads
 // Few rows an expert: bound by the packed weights of the experts that have any.
+#include <algorithm>
+
 #include "common.h"
 #include "experts.h"
 #include "kernels.h"
@@ -23,9 +25,9 @@ struct Args {
 };
 }  // namespace rows
 
-// blockIdx.x: a group of TILES 16-row weight tiles, blockIdx.y: the how-manieth 16 slots of an expert.  Wave w takes the
-// 512-chunks w, w + W, ... of K; the weights are the row operand of v_mfma_i32_16x16x64_i8, the slots its columns; a
-// lane's 16 bytes of a packed tile hold 16 consecutive k of each of eight bit planes, (w >> i) & 0x01010101 is plane i as
+// blockIdx.x: a group of TILES 16-row weight tiles, blockIdx.y (and z): the how-manieth 16 slots of an expert.  Wave w
+// takes the 512-chunks w, w + W, ... of K; the weights are the row operand of v_mfma_i32_16x16x64_i8, the slots its
+// columns; a lane's 16 bytes of a packed tile hold 16 consecutive k of each of eight bit planes, (w >> i) & 0x01010101 is plane i as
 // {0,1} bytes, and sum_k q s = 2 sum_k q b - sum_k q.  The waves' sums meet in LDS.
 // A launch is a chain of trips to memory: the experts' bounds, then the weights and (in two trips) the codes, whose rows
 // are known only with the order.  So the first chunk's weights are requested as soon as the expert is known and the
@@ -41,7 +43,7 @@ __global__ __launch_bounds__(rows::kMaxWaves* kWave) void experts_rows_kernel(ro
     const int col = l & 15, g = l >> 4;
 
     // the expert of this workgroup's slots: a lane counts the sixteens of an expert
-    int e = -1, s0 = 0, s1 = 0, left = (int)blockIdx.y;
+    int e = -1, s0 = 0, s1 = 0, left = (int)(blockIdx.z * gridDim.y + blockIdx.y);
     for (int b = 0; b < (int)a.E; b += kWave) {
         const int at = b + l < (int)a.E ? b + l : (int)a.E - 1;
         const int from = slot_bound(a.offsets, at, (int)a.T), to = slot_bound(a.offsets, at + 1, (int)a.T);
@@ -70,7 +72,8 @@ __global__ __launch_bounds__(rows::kMaxWaves* kWave) void experts_rows_kernel(ro
 #pragma unroll
         for (int t = 0; t < TILES; ++t) {
             const uint32_t tn = t0 + t < last ? t0 + t : last;
-            q[t] = __builtin_nontemporal_load(reinterpret_cast<const v4i*>(wbase + ((uint64_t)tn * a.TK + c) * 256 + l * 4));
+            const uint32_t* const at = wbase + ((uint64_t)tn * a.TK + c) * 256 + l * 4;
+            q[t] = __builtin_nontemporal_load(reinterpret_cast<const v4i*>(at));
         }
     };
     v4i q[TILES];
@@ -78,7 +81,7 @@ __global__ __launch_bounds__(rows::kMaxWaves* kWave) void experts_rows_kernel(ro
     const int s = s0 + col < s1 ? s0 + col : s1 - 1;
     const uint32_t row = code_row(a.order, a.top_k, a.rows, (uint32_t)s);
     const int8_t* const x = a.codes + (uint64_t)row * a.K + 16 * g;
-    const uint32_t klast = a.K - 16 - 16 * g;  // past the row its last 16 bytes again: the packed bits there are zero
+    const int klast = (int)a.K - 16 - 16 * g;  // past the row its last 16 bytes again: the packed bits there are zero
     float gamma = 0.f;
     int sum = 0;
     if (w == 0 && l < kSlots) {
@@ -92,8 +95,8 @@ __global__ __launch_bounds__(rows::kMaxWaves* kWave) void experts_rows_kernel(ro
         v4i act[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const uint32_t k = c * kChunkK + 64 * i;
-            act[i] = *reinterpret_cast<const v4i*>(x + (int32_t)(k < klast ? k : klast));
+            const int k = (int)c * kChunkK + 64 * i;
+            act[i] = *reinterpret_cast<const v4i*>(x + (k < klast ? k : klast));
         }
         if (c != (uint32_t)w) load(q, c);
 #pragma unroll
@@ -133,9 +136,12 @@ __global__ __launch_bounds__(rows::kMaxWaves* kWave) void experts_rows_kernel(ro
 static void launch_rows(const ExpertsArgs& a, hipStream_t s) {
     const int64_t TN = tiles_n(a.N), TK = tiles_k(a.K);
     const int64_t A = a.T < a.E ? a.T : a.E, blocks = a.T / rows::kSlots + A;
-    // Tiles of a workgroup: more of them share the fixed chain and the codes, fewer leave no CU idle.
+    // Tiles of a workgroup: more of them share the fixed chain and the codes, fewer leave no CU idle.  us with 2 / 4 / 8, T
+    // slots of E experts: T = 32, E = 8, 2048 -> 2048 5.5 / 6.1 / 7.4, 8192 -> 2048 9.7 / 8.4 / 10.9; T = 96, E = 16, 4096 ->
+    // 4096 17.4 / 14.0 / 13.5; T = 200, E = 16, 2048 -> 8192 24.4 / 21.5 / 23.5.
     int tiles = tuning().decode_tiles;
-    if (!tiles) tiles = blocks * TN < 512 ? 1 : blocks * TN < 1280 || TK < 4 ? 2 : TK >= 8 && blocks * TN < 6144 && blocks * TN > 4096 ? 8 : 4;
+    const int64_t all = blocks * TN;
+    if (!tiles) tiles = all < 512 ? 1 : all < 1280 || TK < 4 ? 2 : TK >= 8 && all > 4096 && all < 6144 ? 8 : 4;
     rows::Args r{};
     r.codes = a.codes; r.packed = a.packed; r.offsets = a.offsets; r.order = a.order;
     r.T = (uint32_t)a.T; r.E = (uint32_t)a.E; r.top_k = (uint32_t)a.top_k; r.rows = (uint32_t)a.rows;
@@ -145,7 +151,9 @@ static void launch_rows(const ExpertsArgs& a, hipStream_t s) {
     r.per_tensor = a.per_tensor; r.out_acc = a.out_acc; r.Y = a.Y;
     const unsigned threads = (unsigned)(TK < rows::kMaxWaves ? TK : rows::kMaxWaves) * kWave;
     auto launch = [&](auto kernel, int n) {
-        kernel<<<dim3((unsigned)((TN + n - 1) / n), (unsigned)blocks), threads, 0, s>>>(r);
+        const int64_t most = 32768;  // of a dimension of a grid, which the bound may pass
+        const dim3 grid((unsigned)((TN + n - 1) / n), (unsigned)(blocks < most ? blocks : most), (unsigned)((blocks + most - 1) / most));
+        kernel<<<grid, threads, 0, s>>>(r);
     };
     if (tiles <= 1) launch(experts_rows_kernel<1>, 1);
     else if (tiles <= 2) launch(experts_rows_kernel<2>, 2);
@@ -153,10 +161,38 @@ static void launch_rows(const ExpertsArgs& a, hipStream_t s) {
     else launch(experts_rows_kernel<8>, 8);
 }
 
+// The kernel: the cheapest by these costs in us, fitted to graph replays under each of them over 260 shapes (1 to 16384
+// slots, 2 to 32 experts of uneven popularity, K and N of 256 to 8192).  How the slots fall on the experts is not known
+// here: an expert's last row of tiles is taken to be half full, and a round to be 0.4 of a round longer than they say.
+//   128 x 256 tiles   0.3 + rounds (7.3 + 0.37 n)    n stages of 64 k, c chunks of 512
+//   256 x 256        -3.5 + rounds (17.5 + 0.62 n)
+//   128 x 128         0.2 + rounds (6.8 + 2.84 c / 2)
+//   64 x 128          0.6 + rounds (5.75 + 3.14 c / 4)
+//   16 slots at a time  2.8 + 1.3 c / 8 + (0.06 c + 0.19) per 16 x 16 outputs and CU
+// 0.9 % slower than the best of the five on average, 21 % at most (118 slots, 3 experts, 3232 -> 7902: 16.2, 13.4 as 64 x
+// 128).  The extremes, 16 slots at a time / 128 x 256: 64 slots, 8 experts, 4096 -> 4096 10.0 / 29; 8900 slots, 12
+// experts, 3840 -> 4808 787 / 181.
+static int experts_plan(const ExpertsArgs& a) {
+    const double cus = num_cus(), T = (double)a.T, A = (double)(a.T < a.E ? a.T : a.E);
+    const double c = (double)tiles_k(a.K), n = (double)((a.K + 63) / 64);
+    auto up = [](double v) { return (double)(int64_t)(v + 0.999999); };
+    auto rows_of_tiles = [&](double bm) { return std::max(0.9 * A, T / bm + 0.5 * A); };
+    auto rounds = [&](double bm, int64_t bn) {
+        return std::max(1.0, rows_of_tiles(bm) * (double)((a.N + bn - 1) / bn) / cus + 0.4);
+    };
+    const double small = rows_of_tiles(16) * (double)tiles_n(a.N) / cus;
+    const double us[5] = {0.3 + rounds(128, 256) * (7.3 + 0.37 * n), -3.5 + rounds(256, 256) * (17.5 + 0.62 * n),
+                          0.2 + rounds(128, 128) * (6.8 + 2.84 * up(c / 2)),
+                          0.6 + rounds(64, 128) * (5.75 + 3.14 * up(c / 4)),
+                          2.8 + 1.3 * up(c / 8) + (0.06 * c + 0.19) * small};
+    return 1 + (int)(std::min_element(us, us + 5) - us);
+}
+
 hipError_t launch_matmul_experts(const ExpertsArgs& a, hipStream_t s) {
-    const int force = tuning().experts_tile;
-    const int tile = force ? force : a.T / a.E > 160 ? 2 : a.T / a.E > 32 ? 1 : 5;
-    if (tile <= 4 && (int64_t)a.rows * a.K < (int64_t)1 << 32) {
+    // the tiled kernels keep offsets into all of the codes in 32 bits
+    int tile = tuning().experts_tile ? tuning().experts_tile : experts_plan(a);
+    if ((int64_t)a.rows * a.K >= (int64_t)1 << 32) tile = 5;
+    if (tile <= 4) {
         GemmArgs g{};
         g.codes = a.codes; g.gamma = a.gamma; g.rowsum = a.rowsum; g.M = a.T; g.K = a.K; g.N = a.N;
         g.packed = a.packed; g.beta = a.beta; g.per_tensor = a.per_tensor; g.out_acc = a.out_acc; g.Y = a.Y;

@@ -688,7 +688,7 @@ hipError_t launch_gemm_mid_tiles(const GemmArgs& a_in, int bm, int64_t per, hipS
 hipError_t launch_experts_mid(const GemmArgs& a, int bm, hipStream_t s) {
     const int64_t grid_n = (a.N + mid::BN - 1) / mid::BN;
     const int64_t items = ((a.M / bm + (a.M < a.experts ? a.M : a.experts)) * grid_n + 7) / 8 * 8;
-    if (a.K > kMaxGemmK || items > ((int64_t)1 << 22)) return hipErrorInvalidValue;
+    if (a.K > kMaxGemmK || items > ((int64_t)1 << 22)) return hipErrorInvalidValue;  // (launch_experts_tiles sees to it)
     const mid::Args args = mid_args(a, 0, (int)grid_n, 1, 0);
     const bool streaming = streaming_stores(a, 1, false);
     auto launch = [&](auto kernel) { kernel<<<(unsigned)items, mid::THREADS, 0, s>>>(args); };

@@ -896,9 +896,10 @@ static void launch_experts_tile(const GemmArgs& a, hipStream_t s) {
 }
 hipError_t launch_experts_tiles(const GemmArgs& a, int tile, hipStream_t s) {
     if (a.K > kMaxGemmK || (int64_t)a.rows * a.ldq >= (int64_t)1 << 32) return hipErrorInvalidValue;
-    if (tile >= 3) return launch_experts_mid(a, tile == 3 ? 128 : 64, s);
-    if (tile == 1) launch_experts_tile<128>(a, s);
-    else launch_experts_tile<256>(a, s);
+    const int64_t tiles = (a.M / 64 + a.experts) * ((a.N + 127) / 128);
+    if (tile >= 3 && tiles < ((int64_t)1 << 22)) return launch_experts_mid(a, tile == 3 ? 128 : 64, s);  // a grid of them
+    if (tile == 2) launch_experts_tile<256>(a, s);
+    else launch_experts_tile<128>(a, s);
     return hipGetLastError();
 }
 
