@@ -19,6 +19,7 @@
 // preparation passes are HBM-bound and small next to the 2*M*N*K flops of each product.
 
 #include "common.h"
+#include "experts.h"
 #include "kernels.h"
 #include "ring.h"
 
@@ -256,6 +257,15 @@ struct RingSlices {
     int splits, per;  // per: stages of 32 r in a slice
 };
 
+// A mixture of experts (EXP): the product is one for each expert, over its own slots.  dX^: the slots are rows of A and C,
+// S and the scale are the expert's.  dW: they are the reduction, whose stages the copies hold expert after expert, none
+// with fewer than `least` (so that every slice has one); C is [E][I][J].  Which slots are whose is in device memory: the
+// workgroups count for themselves.
+struct ExpertsRing {
+    const int32_t* offsets;
+    int E, T, least;
+};
+
 // ---- C[I][J] = scale * sum_r A[I][r] B[J][r], bf16 operands, fp32 accumulation -----------------
 // Workgroup tile T x T, four waves of T/2 x T/2, persistent over the tiles.  T = 256: 4 x 4 MFMA tiles a
 // wave, one workgroup per CU; T = 128 (few stages or few tiles, dw_plan): 2 x 2, two workgroups per CU.
@@ -310,14 +320,14 @@ __device__ inline void wide_wait(v4i (&a)[2], v4i (&b)[2]) {
     asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(a[0]), "+v"(a[1]), "+v"(b[0]), "+v"(b[1]));
 }
 
-template <int T, int NS, bool SPLIT>
+template <int T, int NS, bool SPLIT, bool EXP = false>
 __global__ __launch_bounds__(256, T == 256 ? 1 : 2) void gemm_tn_bf16_wide(const uint16_t* __restrict__ A,
                                                             const uint16_t* __restrict__ B,
                                                             int64_t I, int64_t J, int64_t Rp,
                                                             const float* __restrict__ scale_ptr,
                                                             float scale_mul, float* __restrict__ C,
                                                             int grid_i, int grid_j, int blk_i,
-                                                            int blk_j, RingSlices sl) {
+                                                            int blk_j, RingSlices sl, ExpertsRing ex) {
     constexpr int BM = T, BN = T, WN = 2, THREADS = 256, WTM = T / 2, WTN = T / 2, MI = T / 64, NI = T / 64;
     constexpr int PA = BM * 4 / THREADS, PB = BN * 4 / THREADS, P = PA + PB;
     constexpr int A_BYTES = BM * 64, STAGE_BYTES = (BM + BN) * 64;
@@ -328,7 +338,11 @@ __global__ __launch_bounds__(256, T == 256 ? 1 : 2) void gemm_tn_bf16_wide(const
     const int wm = w / WN, wn = w % WN;
     const int j = l & 31, g2 = l >> 5;
     const int nst_all = (int)(Rp / 32);
-    const int nitems = grid_i * grid_j * (SPLIT ? sl.splits : 1);
+    __shared__ std::conditional_t<EXP, ExpertTiles, int> smE;
+    if constexpr (EXP) expert_tiles(ex.offsets, ex.E, ex.T, 32, smE, ex.least);
+    const int rows_i = EXP ? grid_i * ex.E : grid_i;  // rows of tiles
+    const int nitems = rows_i * grid_j * (SPLIT ? sl.splits : 1);
+    int expert = 0;  // of the tile whose origin was asked for last
     int nst = nst_all;  // stages of the current work item, the first one st0 (SPLIT)
     int st0 = 0;
     // groups of NS stages whose look-ahead stage st+NS-1 exists for every stage of the group
@@ -340,11 +354,24 @@ __global__ __launch_bounds__(256, T == 256 ? 1 : 2) void gemm_tn_bf16_wide(const
             i0 = (int64_t)(tile / grid_j) * BM;
             j0 = (int64_t)(tile % grid_j) * BN;
         } else {
-            ring_tile_origin(t, (int)gridDim.x, grid_i, grid_j, blk_i, blk_j, BM, BN, i0, j0);
+            ring_tile_origin(t, (int)gridDim.x, rows_i, grid_j, blk_i, blk_j, BM, BN, i0, j0);
+        }
+        if constexpr (EXP) {
+            if (i0 < 0) return;
+            const int row = (int)(i0 / BM);
+            expert = row / grid_i;
+            i0 = (int64_t)(row - expert * grid_i) * BM;
         }
     };
     auto set_slice = [&](int t) {
-        if constexpr (SPLIT) {
+        if constexpr (EXP) {
+            const int first = __builtin_amdgcn_readfirstlane(smE.first[expert]);
+            const int n = __builtin_amdgcn_readfirstlane(smE.first[expert + 1]) - first;
+            const int k = SPLIT ? t % sl.splits : 0, of = SPLIT ? sl.splits : 1;
+            st0 = first + n * k / of;
+            nst = first + n * (k + 1) / of - st0;  // one or more: n >= least >= the slices
+            main_groups = nst >= 2 * NS - 1 ? (nst - (2 * NS - 1)) / NS + 1 : 0;
+        } else if constexpr (SPLIT) {
             st0 = (t % sl.splits) * sl.per;
             nst = nst_all - st0 < sl.per ? nst_all - st0 : sl.per;
             main_groups = nst >= 2 * NS - 1 ? (nst - (2 * NS - 1)) / NS + 1 : 0;
@@ -440,7 +467,7 @@ __global__ __launch_bounds__(256, T == 256 ? 1 : 2) void gemm_tn_bf16_wide(const
         });
     };
 
-    const float scale = (scale_ptr ? *scale_ptr : 1.0f) * scale_mul;
+    float scale = (scale_ptr ? *scale_ptr : 1.0f) * scale_mul;
     int t = (int)blockIdx.x;
     int64_t i0, j0;
     tile_origin(t, i0, j0);
@@ -449,6 +476,7 @@ __global__ __launch_bounds__(256, T == 256 ? 1 : 2) void gemm_tn_bf16_wide(const
     setup_dma(i0, j0);
     issue_tile_start();
 
+    int current = expert;
     while (true) {
 #pragma unroll
         for (int mi = 0; mi < MI; ++mi)
@@ -471,7 +499,14 @@ __global__ __launch_bounds__(256, T == 256 ? 1 : 2) void gemm_tn_bf16_wide(const
         const int t_next = t + (int)gridDim.x;
         int64_t i0n = -1, j0n = -1;
         if (t_next < nitems) tile_origin(t_next, i0n, j0n);
-        float* const Cs = SPLIT ? C + (int64_t)(t % sl.splits) * I * J : C;
+        float* Cs = SPLIT ? C + (int64_t)(t % sl.splits) * (EXP ? ex.E : 1) * I * J : C;
+        float sc = scale;
+        if constexpr (EXP) {
+            Cs += (int64_t)current * I * J;
+            // nothing but zeros of an expert without slots, whatever gamma is
+            if (smE.from[current] == smE.to[current]) sc = 0.f;
+            current = expert;
+        }
         if (i0n >= 0) {
             set_slice(t_next);
             setup_dma(i0n, j0n);
@@ -483,7 +518,7 @@ __global__ __launch_bounds__(256, T == 256 ? 1 : 2) void gemm_tn_bf16_wide(const
             const int64_t jb = j0 + __builtin_amdgcn_readfirstlane(wn * WTN);
             if constexpr (T < 256) {
                 store_tile<MI, NI, true>(Cs + ib * J + jb, J, I - ib, J - jb, j, g2, [](int, int) {},
-                                         [&](int mi, int r, int s) { return scale * acc[mi][s][r]; });
+                                         [&](int mi, int r, int s) { return sc * acc[mi][s][r]; });
             } else  // with 256 accumulators the walk of store_tile spills 29 registers and gains nothing
 #pragma unroll
                 for (int mi = 0; mi < MI; ++mi)
@@ -494,7 +529,7 @@ __global__ __launch_bounds__(256, T == 256 ? 1 : 2) void gemm_tn_bf16_wide(const
 #pragma unroll
                         for (int s = 0; s < NI; ++s) {
                             const int64_t jj = j0 + wn * WTN + 32 * s + j;
-                            if (jj < J) __builtin_nontemporal_store(scale * acc[mi][s][r], &Cs[i * J + jj]);
+                            if (jj < J) __builtin_nontemporal_store(sc * acc[mi][s][r], &Cs[i * J + jj]);
                         }
                     }
         }
@@ -552,14 +587,14 @@ __device__ inline void a_words_wait(v4i (&a)[2], uint32_t (&wd)[2]) {
     asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(a[0]), "+v"(a[1]), "+v"(wd[0]), "+v"(wd[1]));
 }
 
-template <int BM, int NS, bool SPLIT>
+template <int BM, int NS, bool SPLIT, bool EXP = false>
 __global__ __launch_bounds__(512, BM == 256 ? 2 : 4) void gemm_tn_signs_ring(const uint16_t* __restrict__ A,
                                                              const uint32_t* __restrict__ Sw,
                                                              int64_t I, int64_t J, int64_t Rp,
                                                              const float* __restrict__ scale_ptr,
                                                              float scale_mul, float* __restrict__ C,
                                                              int grid_i, int grid_j, int blk_i,
-                                                             int blk_j, RingSlices sl) {
+                                                             int blk_j, RingSlices sl, ExpertsRing ex) {
     constexpr int BN = 256, WN = 4, THREADS = 512, WTM = BM / 2, WTN = 64, MI = WTM / 32, NI = 2;
     constexpr int PA = BM * 4 / THREADS, P = PA + 1;  // DMA operations per thread and stage
     constexpr int STAGE_BYTES = BM * 64;
@@ -571,13 +606,36 @@ __global__ __launch_bounds__(512, BM == 256 ? 2 : 4) void gemm_tn_signs_ring(con
     const int wm = w / WN, wn = w % WN;
     const int j = l & 31, g2 = l >> 5;
     const int nst_all = (int)(Rp / 32);
+    __shared__ std::conditional_t<EXP, ExpertTiles, int> smE;
+    if constexpr (EXP) grid_i = expert_tiles(ex.offsets, ex.E, ex.T, BM, smE);
     const int nitems = grid_i * grid_j * (SPLIT ? sl.splits : 1);
+    int expert = 0;   // of the tile whose origin was asked for last,
+    int64_t end = 0;  // whose rows end here
     int nst = nst_all;  // stages of the current work item, the first one st0 (SPLIT)
     int st0 = 0;
     int main_groups = nst >= 2 * NS - 1 ? (nst - (2 * NS - 1)) / NS + 1 : 0;
 
     auto tile_origin = [&](int t, int64_t& i0, int64_t& j0) {
-        if constexpr (SPLIT) {
+        if constexpr (EXP) {
+            // a contiguous range of the tiles for each XCD (their numbers differ by one); slices of a tile in turn
+            int logical = t;
+            if constexpr (SPLIT) {
+                logical = t < nitems ? t / sl.splits : -1;
+            } else if ((gridDim.x & 7) == 0) {
+                const int G = (int)gridDim.x, x = t & 7, q = ((t % G) >> 3) + (t / G) * (G >> 3);
+                logical = (int)((int64_t)nitems * x / 8) + q;
+                if (logical >= (int)((int64_t)nitems * (x + 1) / 8)) logical = -1;
+            } else if (t >= nitems) {
+                logical = -1;
+            }
+            i0 = j0 = -1;
+            if (logical < 0) return;
+            int from, to;
+            expert = expert_of_tile(smE, ex.E, logical / grid_j, BM, from, to);
+            i0 = from;
+            end = to;
+            j0 = (int64_t)(logical % grid_j) * BN;
+        } else if constexpr (SPLIT) {
             const int tile = t / sl.splits;
             i0 = (int64_t)(tile / grid_j) * BM;
             j0 = (int64_t)(tile % grid_j) * BN;
@@ -602,13 +660,13 @@ __global__ __launch_bounds__(512, BM == 256 ? 2 : 4) void gemm_tn_signs_ring(con
             const int slot = q * THREADS + threadIdx.x;
             int row = slot >> 2;
             const int seg = ((slot & 3) ^ ((row >> 2) & 3)) * 16;
-            if (i0 + row > I - 1) row = (int)(I - 1 - i0);
+            if (i0 + row > (EXP ? end : I) - 1) row = (int)((EXP ? end : I) - 1 - i0);
             goffA[q] = (uint32_t)row * 64 + seg;
         }
         baseA = reinterpret_cast<const uint8_t*>(A) + (st0 * I + i0) * 64;
         int64_t col = j0 + wn * WTN + l;  // columns past J re-read the last one (never stored)
         if (col > J - 1) col = J - 1;
-        wsrc = Sw + (int64_t)st0 * J + col;
+        wsrc = Sw + ((EXP ? (int64_t)expert * nst_all : 0) + st0) * J + col;
     };
     const uint32_t lds_wave = (uint32_t)(w * kWave * 16);
     // sign words of stage sb (the last stage's again when sb does not exist) into slot sb % NS
@@ -710,7 +768,7 @@ __global__ __launch_bounds__(512, BM == 256 ? 2 : 4) void gemm_tn_signs_ring(con
         for (int s = 0; s < NI; ++s) wcur[s] = wnext[s];
     };
 
-    const float scale = (scale_ptr ? *scale_ptr : 1.0f) * scale_mul;
+    const float scale = EXP ? 1.0f : (scale_ptr ? *scale_ptr : 1.0f) * scale_mul;
     int t = (int)blockIdx.x;
     int64_t i0, j0;
     tile_origin(t, i0, j0);
@@ -719,6 +777,8 @@ __global__ __launch_bounds__(512, BM == 256 ? 2 : 4) void gemm_tn_signs_ring(con
     setup_dma(i0, j0);
     issue_tile_start();
 
+    int current = expert;
+    int64_t rows_end = end;
     while (true) {
 #pragma unroll
         for (int mi = 0; mi < MI; ++mi)
@@ -747,7 +807,7 @@ __global__ __launch_bounds__(512, BM == 256 ? 2 : 4) void gemm_tn_signs_ring(con
         block_barrier();
         const int t_next = t + (int)gridDim.x;
         int64_t i0n = -1, j0n = -1;
-        if (t_next < nitems) tile_origin(t_next, i0n, j0n);
+        if (t_next < nitems || EXP) tile_origin(t_next, i0n, j0n);
         float* const Cs = SPLIT ? C + (int64_t)(t % sl.splits) * I * J : C;
         if (i0n >= 0) {
             set_slice(t_next);
@@ -758,8 +818,10 @@ __global__ __launch_bounds__(512, BM == 256 ? 2 : 4) void gemm_tn_signs_ring(con
         {
             const int64_t ib = i0 + __builtin_amdgcn_readfirstlane(wm * WTM);
             const int64_t jb = j0 + __builtin_amdgcn_readfirstlane(wn * WTN);
-            store_tile<MI, NI, true>(Cs + ib * J + jb, J, I - ib, J - jb, j, g2, [](int, int) {},
-                               [&](int mi, int r, int s) { return scale * acc[mi][s][r]; });
+            const float sc = EXP ? scale_ptr[current] : scale;  // EXP: the expert's, in every slice
+            store_tile<MI, NI, true>(Cs + ib * J + jb, J, (EXP ? rows_end : I) - ib, J - jb, j, g2, [](int, int) {},
+                               [&](int mi, int r, int s) { return sc * acc[mi][s][r]; });
+            if constexpr (EXP) current = expert, rows_end = end;
         }
         if (i0n < 0) break;
         t = t_next;
@@ -967,14 +1029,14 @@ static void launch_gemm_tn(const uint16_t* A, const uint16_t* B, int64_t I, int6
     if (slices_bytes(p, I, J) > part_bytes) p = unsliced(p, Rp);
     if (p.sl.splits > 1) {
         gemm_tn_bf16_wide<256, 4, true><<<(unsigned)p.grid, 256, 0, s>>>(
-            A, B, I, J, Rp, nullptr, 1.0f, part, p.gi, p.gj, 0, 0, p.sl);
+            A, B, I, J, Rp, nullptr, 1.0f, part, p.gi, p.gj, 0, 0, p.sl, {});
         launch_fold(part, p, I * J, scale_ptr, scale_mul, C, s);
     } else if (p.tile == 256) {
         gemm_tn_bf16_wide<256, 4, false><<<(unsigned)p.grid, 256, 0, s>>>(
-            A, B, I, J, Rp, scale_ptr, scale_mul, C, p.gi, p.gj, p.blk_i, p.blk_j, p.sl);
+            A, B, I, J, Rp, scale_ptr, scale_mul, C, p.gi, p.gj, p.blk_i, p.blk_j, p.sl, {});
     } else {
         gemm_tn_bf16_wide<128, 4, false><<<(unsigned)p.grid, 256, 0, s>>>(
-            A, B, I, J, Rp, scale_ptr, scale_mul, C, p.gi, p.gj, p.blk_i, p.blk_j, p.sl);
+            A, B, I, J, Rp, scale_ptr, scale_mul, C, p.gi, p.gj, p.blk_i, p.blk_j, p.sl, {});
     }
 }
 
@@ -1026,12 +1088,12 @@ hipError_t launch_backward(const BackwardArgs& a, hipStream_t s) {
         if (slices_bytes(p, M, K) > part_bytes) p = unsliced(p, Np);
         if (p.sl.splits > 1) {
             const auto kernel = p.tile == 256 ? gemm_tn_signs_ring<256, 4, true> : gemm_tn_signs_ring<128, 4, true>;
-            kernel<<<(unsigned)p.grid, 512, 0, s>>>(g, Sw, M, K, Np, nullptr, 1.0f, part, p.gi, p.gj, 0, 0, p.sl);
+            kernel<<<(unsigned)p.grid, 512, 0, s>>>(g, Sw, M, K, Np, nullptr, 1.0f, part, p.gi, p.gj, 0, 0, p.sl, {});
             launch_fold(part, p, M * K, a.beta, 1.0f, a.dX, s);
         } else {
             const auto kernel = p.tile == 256 ? gemm_tn_signs_ring<256, 4, false> : gemm_tn_signs_ring<128, 4, false>;
             kernel<<<(unsigned)p.grid, 512, 0, s>>>(g, Sw, M, K, Np, a.beta, 1.0f, a.dX, p.gi, p.gj, p.blk_i, p.blk_j,
-                                                    p.sl);
+                                                    p.sl, {});
         }
     }
     if (a.dW) {
@@ -1039,6 +1101,104 @@ hipError_t launch_backward(const BackwardArgs& a, hipStream_t s) {
                        a.per_tensor ? 1.0f / 128.0f : 1.0f, a.dW, part, part_bytes, s);
     }
     return hipGetLastError();
+}
+
+// ---- mixtures of experts ------------------------------------------------------------------------------
+// out[r] = slice 0 + slice 1 + ..., rows behind the last slot left alone
+template <bool VEC>
+__global__ __launch_bounds__(256) void fold_expert_rows(const float* __restrict__ part, int splits, int64_t T, int64_t J,
+                                                        const int32_t* __restrict__ end, float* __restrict__ out) {
+    constexpr int E = VEC ? 4 : 1;
+    const int64_t used = (*end < 0 ? 0 : *end < T ? *end : T) * J;
+    for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * E; i < used; i += (int64_t)gridDim.x * 256 * E) {
+        if constexpr (VEC) {
+            v4f v = *reinterpret_cast<const v4f*>(part + i);
+#pragma unroll 4
+            for (int s = 1; s < splits; ++s) v += *reinterpret_cast<const v4f*>(part + s * T * J + i);
+            *reinterpret_cast<v4f*>(out + i) = v;
+        } else {
+            float v = part[i];
+            for (int s = 1; s < splits; ++s) v += part[s * T * J + i];
+            out[i] = v;
+        }
+    }
+}
+// dW of every expert; zeros where it has no slots, whatever gamma is
+template <bool VEC>
+__global__ __launch_bounds__(256) void fold_expert_weights(const float* __restrict__ part, int splits, int64_t count, int E,
+                                                           int T, const int32_t* __restrict__ offsets,
+                                                           const float* __restrict__ gamma, float* __restrict__ out) {
+    constexpr int W = VEC ? 4 : 1;
+    const int e = (int)blockIdx.y;
+    const bool some = slot_bound(offsets, e, T) < slot_bound(offsets, e + 1, T);
+    const float scale = !some ? 0.f : gamma ? *gamma * (1.0f / 128.0f) : 1.f;
+    part += e * count;
+    out += e * count;
+    for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * W; i < count; i += (int64_t)gridDim.x * 256 * W) {
+        if constexpr (VEC) {
+            v4f v = *reinterpret_cast<const v4f*>(part + i);
+#pragma unroll 4
+            for (int s = 1; s < splits; ++s) v += *reinterpret_cast<const v4f*>(part + s * E * count + i);
+            *reinterpret_cast<v4f*>(out + i) = v * scale;
+        } else {
+            float v = part[i];
+            for (int s = 1; s < splits; ++s) v += part[s * E * count + i];
+            out[i] = v * scale;
+        }
+    }
+}
+
+ExpertsBackwardPlan experts_backward_plan(int64_t T, int64_t N, int64_t K, int E) {
+    const Tuning& t = tuning();
+    ExpertsBackwardPlan p{1, 1, 1, 1};
+    const int64_t cus = ring_cus(), A = T < E ? T : E;
+    const int64_t rows = T / 256 + (A + 1) / 2, tiles = rows * ((K + 255) / 256);
+    if (t.bwd_dx) p.dx_tile = t.bwd_dx;
+    else p.dx_tile = tiles >= cus ? 1 : 2;
+    if (t.bwd_ring) p.dw_tile = t.bwd_ring;
+    else p.dw_tile = T / E >= 512 ? 1 : 2;
+    if (t.bwd_splits > 1) p.dx_splits = p.dw_splits = t.bwd_splits < 16 ? t.bwd_splits : 16;
+    const int64_t nst = (N + 31) / 32;
+    if (p.dx_splits > nst) p.dx_splits = (int)nst;
+    return p;
+}
+
+void launch_experts_dx(const ExpertsOperands& a, const ExpertsBackwardPlan& p, hipStream_t s) {
+    const int64_t Np = pad32(a.N), nst = Np / 32, bm = p.dx_tile == 1 ? 256 : 128, gj = (a.K + 255) / 256;
+    const ExpertsRing ex{a.offsets, a.E, (int)a.T, 0};
+    const int64_t most = most_tiles(a.T, a.E, (int)bm, 0) * gj, cap = (int64_t)ring_cus() * (bm == 256 ? 1 : 2);
+    const int64_t per = (nst + p.dx_splits - 1) / p.dx_splits;
+    const RingSlices sl{(int)((nst + per - 1) / per), (int)per};
+    const int64_t items = most * sl.splits;
+    const unsigned grid = (unsigned)(items < cap ? items : cap);
+    const bool cut = sl.splits > 1;
+    const auto kernel = cut ? (bm == 256 ? gemm_tn_signs_ring<256, 4, true, true> : gemm_tn_signs_ring<128, 4, true, true>)
+                            : (bm == 256 ? gemm_tn_signs_ring<256, 4, false, true> : gemm_tn_signs_ring<128, 4, false, true>);
+    kernel<<<grid, 512, 0, s>>>(a.g, a.Sw, a.T, a.K, Np, a.beta, 1.0f, cut ? a.part : a.dX, 0, (int)gj, 0, 0, sl, ex);
+    if (!cut) return;
+    const bool vec = ((uintptr_t)a.dX & 15) == 0;  // K % 32 == 0
+    const int64_t wide = (a.T * a.K / (vec ? 4 : 1) + 255) / 256;
+    const auto fold = vec ? fold_expert_rows<true> : fold_expert_rows<false>;
+    fold<<<(unsigned)(wide < 8192 ? wide : 8192), 256, 0, s>>>(a.part, sl.splits, a.T, a.K, a.offsets + a.E, a.dX);
+}
+
+void launch_experts_dw(const ExpertsOperands& a, const ExpertsBackwardPlan& p, hipStream_t s) {
+    const int64_t T = p.dw_tile == 1 ? 256 : 128, gi = (a.N + T - 1) / T, gj = (a.K + T - 1) / T;
+    const ExpertsRing ex{a.offsets, a.E, (int)a.T, a.least};
+    const RingSlices sl{p.dw_splits, 0};
+    const int64_t items = gi * gj * a.E * sl.splits, cap = (int64_t)ring_cus() * (T == 256 ? 1 : 2);
+    const unsigned grid = (unsigned)(items < cap ? items : cap);
+    const bool cut = sl.splits > 1;
+    const auto kernel = cut ? (T == 256 ? gemm_tn_bf16_wide<256, 4, true, true> : gemm_tn_bf16_wide<128, 4, true, true>)
+                            : (T == 256 ? gemm_tn_bf16_wide<256, 4, false, true> : gemm_tn_bf16_wide<128, 4, false, true>);
+    kernel<<<grid, 256, 0, s>>>(a.gwT, a.qT, a.N, a.K, 0, cut ? nullptr : a.gamma,
+                                a.gamma && !cut ? 1.0f / 128.0f : 1.0f, cut ? a.part : a.dW, (int)gi, (int)gj, 0, 0, sl, ex);
+    if (!cut) return;
+    const bool vec = ((uintptr_t)a.dW & 15) == 0;
+    const int64_t count = a.N * a.K, wide = (count / (vec ? 4 : 1) + 255) / 256;
+    const auto fold = vec ? fold_expert_weights<true> : fold_expert_weights<false>;
+    fold<<<dim3((unsigned)(wide < 4096 ? wide : 4096), (unsigned)a.E), 256, 0, s>>>(a.part, sl.splits, count, a.E, (int)a.T,
+                                                                                   a.offsets, a.gamma, a.dW);
 }
 
 }  // namespace bl

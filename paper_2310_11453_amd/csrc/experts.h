@@ -80,6 +80,25 @@ struct ExpertsArgs {
     size_t workspace_bytes;
 };
 hipError_t launch_matmul_experts(const ExpertsArgs& a, hipStream_t s);
+
+// backward.hip: the two products of the backward from the copies that experts_backward.hip makes of their operands.
+// Reduction indices in blocks of 32 as there (block_offset): g [T rows][Np], Sw [E][Np / 32][K]; gwT [N rows] and qT [K
+// rows] over the slots of expert after expert, each expert's filled up with zeros to whole blocks and to `least` of them.
+struct ExpertsOperands {
+    const uint16_t *g, *gwT, *qT;
+    const uint32_t* Sw;
+    const int32_t* offsets;
+    int E, least;
+    int64_t T, N, K;
+    const float *beta, *gamma;  // gamma: of the tensor, or null
+    float *dX, *dW, *part;      // part: sums of slices of the reductions
+};
+struct ExpertsBackwardPlan {
+    int dx_tile, dx_splits, dw_tile, dw_splits;
+};
+ExpertsBackwardPlan experts_backward_plan(int64_t T, int64_t N, int64_t K, int E);
+void launch_experts_dx(const ExpertsOperands& a, const ExpertsBackwardPlan& p, hipStream_t s);
+void launch_experts_dw(const ExpertsOperands& a, const ExpertsBackwardPlan& p, hipStream_t s);
 size_t experts_backward_bytes(int64_t T, int64_t N, int64_t K, int E);
 hipError_t launch_experts_backward(const ExpertsArgs& a, hipStream_t s);
 
@@ -95,30 +114,40 @@ __device__ inline uint32_t code_row(const int32_t* order, uint32_t top_k, uint32
     return r < rows ? r : rows - 1;
 }
 
-// Rows of tiles of BM slots: expert e has those from `first[e]` on, its slots begin at `slot[e]`.
+// Rows of tiles of BM slots: expert e has those from first[e] on, its slots are from[e] .. to[e] - 1.
 struct ExpertTiles {
-    int first[kMaxExperts + 1], slot[kMaxExperts + 1];
+    int first[kMaxExperts + 1], from[kMaxExperts], to[kMaxExperts];
 };
-// Counts them, all threads of a workgroup of 256 or more; their number.
-__device__ inline int expert_tiles(const int32_t* offsets, int E, int T, int BM, ExpertTiles& sm) {
+// What offsets as bitlinear_route leaves them come to at most, of E experts with `least` rows of tiles or more each.
+__host__ __device__ inline int64_t most_tiles(int64_t T, int64_t E, int BM, int least) {
+    return T / BM + (least ? E * least : T < E ? T : E);
+}
+// Counts them (no expert has fewer than `least`), all threads of a workgroup of 256 or more; their number, which no
+// value of `offsets` takes past most_tiles.
+__device__ inline int expert_tiles(const int32_t* offsets, int E, int T, int BM, ExpertTiles& sm, int least = 0) {
     const int e = (int)threadIdx.x, l = e & (kWave - 1);
     if (e < kMaxExperts) {
         const int from = e < E ? slot_bound(offsets, e, T) : 0, to = e < E ? slot_bound(offsets, e + 1, T) : 0;
         int v = to > from ? (to - from + BM - 1) / BM : 0;
+        if (v < least && e < E) v = least;
+        sm.from[e] = from;
+        sm.to[e] = to > from ? to : from;
 #pragma unroll
         for (int d = 1; d < kWave; d <<= 1) {
             const int o = __shfl_up(v, d, kWave);
             if (l >= d) v += o;
         }
         sm.first[e + 1] = v;
-        if (e < E) sm.slot[e] = from, sm.slot[e + 1] = to;
     }
     __syncthreads();
     int lower = 0;
     if (e < kMaxExperts)
         for (int i = kWave; i <= e; i += kWave) lower += sm.first[i];
     __syncthreads();
-    if (e < kMaxExperts) sm.first[e + 1] += lower;
+    if (e < kMaxExperts) {
+        const int most = (int)most_tiles(T, E, BM, least), v = sm.first[e + 1] + lower;
+        sm.first[e + 1] = v < most ? v : most;
+    }
     if (e == 0) sm.first[0] = 0;
     __syncthreads();
     return sm.first[E];
@@ -132,8 +161,8 @@ __device__ inline int expert_of_tile(const ExpertTiles& sm, int E, int tile, int
         else hi = mid - 1;
     }
     lo = __builtin_amdgcn_readfirstlane(lo);
-    from = __builtin_amdgcn_readfirstlane(sm.slot[lo] + (tile - sm.first[lo]) * BM);
-    to = __builtin_amdgcn_readfirstlane(sm.slot[lo + 1]);
+    from = __builtin_amdgcn_readfirstlane(sm.from[lo] + (tile - sm.first[lo]) * BM);
+    to = __builtin_amdgcn_readfirstlane(sm.to[lo]);
     return lo;
 }
 #endif

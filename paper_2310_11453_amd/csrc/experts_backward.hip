@@ -1,97 +1,238 @@
 // Straight-through backward of the products of a mixture of BitLinear layers (arXiv 2310.11453, Section 2.2):
 //   dXs[s,k]  = beta_e sum_n dY[s,n] S_e[n,k]             for the slots s of expert e
 //   dW_e[n,k] = sum_{s of e} dY[s,n] q[r,k] gamma_r/128    r the row that s reads; zeros where e has no slots
-// dY is bf16.
+// dY is bf16, +-1 and the codes are exact in bf16.  As in the plain layer (backward.hip, whose kernels take the products),
+// every operand is first written once in the layout they read:
+//   g    [T][Np]       rows of dY                                 (A operand of dX, reduction over N)
+//   Sw   [E][Np/32][K] the signs of 32 weight rows of a column    (B operand of dX)
+//   gwT  [N][slots]    dY transposed, with a gamma per token scaled and rounded again   (A operand of dW)
+//   qT   [K][slots]    codes transposed, gathered through the order                     (B operand of dW)
+// The slots of the last two are those of expert after expert, each expert's filled up with zeros to whole blocks of 32:
+// a stage of the products is such a block and belongs to one expert.
 #include "common.h"
 #include "experts.h"
+#include "kernels.h"
 
 namespace bl {
 
-__device__ inline float bf16_value(uint16_t v) { return __uint_as_float((uint32_t)v << 16); }
+namespace exb {
+constexpr int kTile = 64;  // 64 x 64 elements of an item
+typedef uint16_t CastTile[kTile][kTile + 2];
 
-// the sign of weight (n, k) of a blob
-__device__ inline float sign_at(const uint32_t* blob, int64_t TK, int64_t n, int64_t k) {
-    const int kl = (int)(k & (kChunkK - 1));
-    const int i = kl >> 6, g = (kl & 63) >> 4, d = (kl & 15) >> 2, j = kl & 3;
-    const uint32_t w = blob[tile_dword_offset(n >> 4, k >> 9, TK) + (g * 16 + (n & 15)) * 4 + d];
-    return (w >> (8 * j + i)) & 1 ? 1.f : -1.f;
+struct Args {
+    const uint16_t* dY;
+    const int8_t* codes;
+    const uint32_t* packed;
+    const float* row_gamma;  // null: per tensor
+    const int32_t *offsets, *order;
+    uint32_t top_k, rows;
+    int E, T, least;
+    uint16_t *g, *gwT, *qT;  // what is not wanted is null
+    uint32_t* Sw;
+    int64_t N, K, Np, blob;
+    uint32_t bits_items, code_items, items;    // items: of all three parts
+    uint32_t bits_x, bits_y, code_x, dy_x;     // items in a row of each part; rows of sign words of an expert
+};
+}  // namespace exb
+
+__device__ inline uint32_t to_bf16(float v) {
+    uint32_t u = __float_as_uint(v);
+    u += 0x7fffu + ((u >> 16) & 1u);
+    return u >> 16;
+}
+// (block_offset of backward.hip)
+__device__ inline int64_t copy_offset(int64_t row, int64_t r, int64_t R) { return ((r >> 5) * R + row) * 32 + (r & 31); }
+
+// Rows of a tile: 16 at a time are in one block of 32 slots, i.e. of one expert.
+struct SlotRow {
+    int slot;     // -1: filled up
+    bool exists;  // the block does
+};
+__device__ inline SlotRow slot_row(const ExpertTiles& count, int E, int blocks, int r) {
+    const int b = r >> 5;
+    if (b >= blocks) return {-1, false};
+    int from, to;
+    expert_of_tile(count, E, b, 32, from, to);
+    const int s = from + (r & 31);
+    return {s < to ? s : -1, true};
 }
 
-// 64 x 64 outputs a workgroup, 4 x 4 a thread, 16 reduction elements at a time through LDS
-__global__ __launch_bounds__(256) void experts_dx_kernel(ExpertsArgs a, int64_t blob) {
-    __shared__ float A[16][65], B[16][65];
-    const int T = (int)a.T, tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-    const int64_t k0 = (int64_t)blockIdx.x * 64, TK = tiles_k(a.K);
-    for (int e = 0; e < a.E; ++e) {
-        const int s0 = slot_bound(a.offsets, e, T), s1 = slot_bound(a.offsets, e + 1, T);
-        for (int m0 = s0 + (int)blockIdx.y * 64; m0 < s1; m0 += (int)gridDim.y * 64) {
-            float acc[4][4] = {};
-            for (int64_t n0 = 0; n0 < a.N; n0 += 16) {
-                __syncthreads();
-                for (int i = threadIdx.x; i < 16 * 64; i += 256) {
-                    const int r = i & 15, c = i >> 4, cc = i & 63, rr = i >> 6;
-                    A[r][c] = m0 + c < s1 && n0 + r < a.N ? bf16_value(a.dY[(int64_t)(m0 + c) * a.N + n0 + r]) : 0.f;
-                    B[rr][cc] = n0 + rr < a.N && k0 + cc < a.K ? sign_at(a.packed + e * blob, TK, n0 + rr, k0 + cc) : 0.f;
+// dY (bf16) -> g and gwT, or codes -> qT.  VEC: four elements a load.
+template <bool CODES, bool VEC>
+__device__ inline void copy_tile(const exb::Args& a, const ExpertTiles& count, int blocks, int r0, int64_t c0,
+                                 exb::CastTile& tile) {
+    const int64_t C = CODES ? a.K : a.N;
+    const int cl = ((int)threadIdx.x & 15) * 4;
+    const int64_t c = c0 + cl;
+#pragma unroll
+    for (int it = 0; it < 4; ++it) {
+        const int rl = it * 16 + (int)(threadIdx.x >> 4);
+        const SlotRow sr = slot_row(count, a.E, blocks, r0 + rl);
+        uint32_t lo = 0, hi = 0;
+        if (sr.slot >= 0 && c < C) {
+            if constexpr (CODES) {
+                const int8_t* const src = a.codes + (int64_t)code_row(a.order, a.top_k, a.rows, (uint32_t)sr.slot) * C + c;
+                const char4 t = *reinterpret_cast<const char4*>(src);  // K % 32 == 0
+                lo = to_bf16((float)t.x) | to_bf16((float)t.y) << 16;
+                hi = to_bf16((float)t.z) | to_bf16((float)t.w) << 16;
+            } else {
+                const uint16_t* const src = a.dY + (int64_t)sr.slot * C + c;
+                if constexpr (VEC) {
+                    const uint2 t = *reinterpret_cast<const uint2*>(src);
+                    lo = t.x, hi = t.y;
+                } else {
+                    lo = src[0] | (c + 1 < C ? (uint32_t)src[1] << 16 : 0);
+                    hi = (c + 2 < C ? src[2] : 0) | (c + 3 < C ? (uint32_t)src[3] << 16 : 0);
                 }
-                __syncthreads();
-                for (int r = 0; r < 16; ++r)
-#pragma unroll
-                    for (int y = 0; y < 4; ++y)
-#pragma unroll
-                        for (int x = 0; x < 4; ++x) acc[y][x] += A[r][ty + 16 * y] * B[r][tx + 16 * x];
             }
-            const float beta = a.beta[e];
-            for (int y = 0; y < 4; ++y)
-                for (int x = 0; x < 4; ++x) {
-                    const int64_t m = m0 + ty + 16 * y, k = k0 + tx + 16 * x;
-                    if (m < s1 && k < a.K) a.dX[m * a.K + k] = beta * acc[y][x];
-                }
         }
+        if constexpr (!CODES) {
+            if (a.g && sr.slot >= 0 && c < a.Np)
+                *reinterpret_cast<uint2*>(a.g + copy_offset(sr.slot, c, a.T)) = make_uint2(lo, hi);
+            if (!a.gwT) continue;  // uniform
+            if (a.row_gamma && sr.slot >= 0) {
+                const float sc = a.row_gamma[code_row(a.order, a.top_k, a.rows, (uint32_t)sr.slot)] / 128.0f;
+                auto scaled = [&](uint32_t v) {
+                    return to_bf16(__uint_as_float(v << 16) * sc) | to_bf16(__uint_as_float(v & 0xffff0000u) * sc) << 16;
+                };
+                lo = scaled(lo);
+                hi = scaled(hi);
+            }
+        }
+        uint32_t* const t32 = reinterpret_cast<uint32_t*>(&tile[rl][cl]);
+        t32[0] = lo;
+        t32[1] = hi;
+    }
+    uint16_t* const tr = CODES ? a.qT : a.gwT;
+    if (!tr) return;
+    __syncthreads();
+#pragma unroll
+    for (int it = 0; it < 4; ++it) {
+        const int idx = it * 256 + (int)threadIdx.x;
+        const int cc = idx >> 4, rl = (idx & 15) * 4;
+        const int64_t col = c0 + cc;
+        const int r = r0 + rl;
+        if (col < C && r < blocks * 32)
+            *reinterpret_cast<uint2*>(tr + copy_offset(col, r, C)) =
+                make_uint2((uint32_t)tile[rl][cc] | ((uint32_t)tile[rl + 1][cc] << 16),
+                           (uint32_t)tile[rl + 2][cc] | ((uint32_t)tile[rl + 3][cc] << 16));
     }
 }
 
-__global__ __launch_bounds__(256) void experts_dw_kernel(ExpertsArgs a) {
-    __shared__ float A[16][65], B[16][65];
-    const int T = (int)a.T, tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-    const int64_t k0 = (int64_t)blockIdx.x * 64, n0 = (int64_t)blockIdx.y * 64;
-    for (int e = (int)blockIdx.z; e < a.E; e += (int)gridDim.z) {
-        const int s0 = slot_bound(a.offsets, e, T), s1 = slot_bound(a.offsets, e + 1, T);
-        float acc[4][4] = {};
-        for (int m0 = s0; m0 < s1; m0 += 16) {
-            __syncthreads();
-            for (int i = threadIdx.x; i < 16 * 64; i += 256) {
-                const int c = i & 63, m = m0 + (i >> 6);
-                const bool in = m < s1;
-                const int64_t r = code_row(a.order, (uint32_t)a.top_k, (uint32_t)a.rows, (uint32_t)(in ? m : s0));
-                const float g = in && n0 + c < a.N ? bf16_value(a.dY[(int64_t)m * a.N + n0 + c]) : 0.f;
-                A[i >> 6][c] = a.per_tensor ? g : g * (a.gamma[r] / 128.f);
-                B[i >> 6][c] = in && k0 + c < a.K ? (float)a.codes[r * a.K + k0 + c] : 0.f;
-            }
-            __syncthreads();
-            for (int r = 0; r < 16; ++r)
+// signs of 32 weight rows x 512 columns of an expert (the bit layout of a word: bits_transpose_tile of backward.hip)
+__device__ inline void words_tile(const exb::Args& a, int e, int64_t sw, int64_t tk, uint32_t (&sm)[2][256]) {
+    const int64_t TN = tiles_n(a.N), TK = tiles_k(a.K);
+    for (int t = 0; t < 2; ++t)
+        sm[t][threadIdx.x] =
+            2 * sw + t < TN ? a.packed[e * a.blob + tile_dword_offset(2 * sw + t, tk, TK) + threadIdx.x] : 0u;
+    __syncthreads();
+    for (int it = 0; it < 2; ++it) {
+        const int kl = it * 256 + (int)threadIdx.x;
+        const int64_t k = tk * kChunkK + kl;
+        if (k >= a.K) continue;
+        const int i = kl >> 6, g = (kl & 63) >> 4, d = (kl & 15) >> 2, j = kl & 3;
+        uint32_t word = 0;
 #pragma unroll
-                for (int y = 0; y < 4; ++y)
-#pragma unroll
-                    for (int x = 0; x < 4; ++x) acc[y][x] += A[r][ty + 16 * y] * B[r][tx + 16 * x];
+        for (int r = 0; r < 32; ++r) {
+            const uint32_t dw = sm[r >> 4][(g * 16 + (r & 15)) * 4 + d];
+            const uint32_t minus = ((dw >> (8 * j + i)) & 1u) ^ 1u;
+            word |= minus << (8 * (r >> 4) + 4 * ((r & 15) >> 3) + ((r & 7) >> 1) + 16 * (r & 1));
         }
-        const float scale = a.per_tensor ? *a.gamma / 128.f : 1.f;
-        for (int y = 0; y < 4; ++y)
-            for (int x = 0; x < 4; ++x) {
-                const int64_t n = n0 + ty + 16 * y, k = k0 + tx + 16 * x;
-                if (n < a.N && k < a.K) a.dW[((int64_t)e * a.N + n) * a.K + k] = scale * acc[y][x];
-            }
+        a.Sw[(e * (a.Np / 32) + sw) * a.K + k] = word;
     }
 }
 
-size_t experts_backward_bytes(int64_t, int64_t, int64_t, int) { return 256; }
+template <bool VEC>
+__global__ __launch_bounds__(256) void prepare_expert_operands(exb::Args a) {
+    __shared__ ExpertTiles count;
+    __shared__ __attribute__((aligned(8))) union {
+        exb::CastTile tile;
+        uint32_t words[2][256];
+    } sm;
+    const int blocks = expert_tiles(a.offsets, a.E, a.T, 32, count, a.least);
+    for (uint32_t it = blockIdx.x; it < a.items; it += gridDim.x) {
+        if (it != blockIdx.x) __syncthreads();  // the item before has been read
+        uint32_t i = it;
+        if (i < a.bits_items) {
+            const uint32_t y = i / a.bits_x;  // 512 columns fastest
+            words_tile(a, (int)(y / a.bits_y), y % a.bits_y, i % a.bits_x, sm.words);
+            continue;
+        }
+        i -= a.bits_items;
+        const bool codes = i < a.code_items;
+        if (!codes) i -= a.code_items;
+        const uint32_t x = codes ? a.code_x : a.dy_x;
+        const int r0 = (int)(i / x) * exb::kTile;
+        if (r0 >= blocks * 32) continue;  // uniform: the grid is a bound
+        if (codes) copy_tile<true, true>(a, count, blocks, r0, (int64_t)(i % x) * exb::kTile, sm.tile);
+        else copy_tile<false, VEC>(a, count, blocks, r0, (int64_t)(i % x) * exb::kTile, sm.tile);
+    }
+}
+
+namespace {
+int64_t pad32(int64_t v) { return (v + 31) / 32 * 32; }
+struct ExpertsWs {
+    size_t words, gwT, qT, part, total;
+};
+ExpertsWs experts_ws(int64_t T, int64_t N, int64_t K, int E, const ExpertsBackwardPlan& p) {
+    auto al = [](size_t v) { return (v + 255) & ~(size_t)255; };
+    const int64_t Np = pad32(N), slots = most_tiles(T, E, 32, p.dw_splits) * 32;
+    ExpertsWs w{};
+    w.words = al((size_t)T * Np * 2);
+    w.gwT = w.words + al((size_t)E * (Np / 32) * K * 4);
+    w.qT = w.gwT + al((size_t)N * slots * 2);
+    w.part = w.qT + al((size_t)K * slots * 2);
+    // one product after the other
+    const size_t dx = p.dx_splits > 1 ? (size_t)p.dx_splits * T * K * 4 : 0;
+    const size_t dw = p.dw_splits > 1 ? (size_t)p.dw_splits * E * N * K * 4 : 0;
+    w.total = w.part + (dx > dw ? dx : dw);
+    return w;
+}
+}  // namespace
+
+size_t experts_backward_bytes(int64_t T, int64_t N, int64_t K, int E) {
+    return experts_ws(T, N, K, E, experts_backward_plan(T, N, K, E)).total;
+}
 
 hipError_t launch_experts_backward(const ExpertsArgs& a, hipStream_t s) {
-    const unsigned kt = (unsigned)((a.K + 63) / 64);
+    const ExpertsBackwardPlan p = experts_backward_plan(a.T, a.N, a.K, a.E);
+    const ExpertsWs ws = experts_ws(a.T, a.N, a.K, a.E, p);
+    char* const base = (char*)a.workspace;
+    exb::Args b{};
+    b.dY = a.dY; b.codes = a.codes; b.packed = a.packed;
+    b.row_gamma = a.per_tensor ? nullptr : a.gamma;
+    b.offsets = a.offsets; b.order = a.order; b.top_k = (uint32_t)a.top_k; b.rows = (uint32_t)a.rows;
+    b.E = a.E; b.T = (int)a.T; b.least = p.dw_splits;
     if (a.dX) {
-        const int64_t mt = (a.T + 63) / 64;
-        experts_dx_kernel<<<dim3(kt, (unsigned)(mt < 65535 ? mt : 65535)), 256, 0, s>>>(a, tiles_n(a.N) * tiles_k(a.K) * 256);
+        b.g = (uint16_t*)base;
+        b.Sw = (uint32_t*)(base + ws.words);
     }
-    if (a.dW) experts_dw_kernel<<<dim3(kt, (unsigned)((a.N + 63) / 64), (unsigned)a.E), 256, 0, s>>>(a);
+    if (a.dW) {
+        b.gwT = (uint16_t*)(base + ws.gwT);
+        b.qT = (uint16_t*)(base + ws.qT);
+    }
+    b.N = a.N; b.K = a.K; b.Np = pad32(a.N);
+    b.blob = tiles_n(a.N) * tiles_k(a.K) * 256;
+    auto tiles = [](int64_t v) { return (v + exb::kTile - 1) / exb::kTile; };
+    const int64_t rows = tiles(most_tiles(a.T, a.E, 32, b.least) * 32);
+    b.bits_x = (uint32_t)tiles_k(a.K);
+    b.bits_y = (uint32_t)(b.Np / 32);
+    b.code_x = (uint32_t)tiles(a.K);
+    b.dy_x = (uint32_t)tiles(b.g ? b.Np : b.N);
+    const int64_t bits = a.dX ? (int64_t)a.E * b.bits_y * b.bits_x : 0, codes = a.dW ? rows * b.code_x : 0;
+    const int64_t items = bits + codes + rows * b.dy_x;
+    if (items >= (int64_t)1 << 32) return hipErrorInvalidValue;
+    b.bits_items = (uint32_t)bits;
+    b.code_items = (uint32_t)codes;
+    b.items = (uint32_t)items;
+    const unsigned grid = (unsigned)(items < (1 << 23) ? items : (1 << 23));
+    if (a.N % 4 == 0 && ((uintptr_t)a.dY & 7) == 0) prepare_expert_operands<true><<<grid, 256, 0, s>>>(b);
+    else prepare_expert_operands<false><<<grid, 256, 0, s>>>(b);
+
+    ExpertsOperands o{b.g, b.gwT, b.qT, b.Sw, a.offsets, a.E, b.least, a.T, a.N, a.K, a.beta,
+                      a.per_tensor ? a.gamma : nullptr, a.dX, a.dW, (float*)(base + ws.part)};
+    if (a.dX) launch_experts_dx(o, p, s);
+    if (a.dW) launch_experts_dw(o, p, s);
     return hipGetLastError();
 }
 

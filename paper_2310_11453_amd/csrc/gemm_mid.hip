@@ -164,7 +164,7 @@ __global__ __launch_bounds__(mid::THREADS) void gemm_mid_kernel(mid::Args a) {
         const int rows = __builtin_amdgcn_readfirstlane(count.first[expert + 1]) - first;
         const int at = item - first * (int)a.grid_n;
         tcol = at / rows;
-        m0 = __builtin_amdgcn_readfirstlane(count.slot[expert]) + (at - tcol * rows) * BM;
+        m0 = __builtin_amdgcn_readfirstlane(count.from[expert]) + (at - tcol * rows) * BM;
         M = to;
         a.packed += expert * a.blob;
         __syncthreads();  // the count has been read
@@ -687,7 +687,7 @@ hipError_t launch_gemm_mid_tiles(const GemmArgs& a_in, int bm, int64_t per, hipS
 // A mixture of experts: the items of a bound of its rows of tiles.
 hipError_t launch_experts_mid(const GemmArgs& a, int bm, hipStream_t s) {
     const int64_t grid_n = (a.N + mid::BN - 1) / mid::BN;
-    const int64_t items = ((a.M / bm + (a.M < a.experts ? a.M : a.experts)) * grid_n + 7) / 8 * 8;
+    const int64_t items = (most_tiles(a.M, a.experts, bm, 0) * grid_n + 7) / 8 * 8;
     if (a.K > kMaxGemmK || items > ((int64_t)1 << 22)) return hipErrorInvalidValue;  // (launch_experts_tiles sees to it)
     const mid::Args args = mid_args(a, 0, (int)grid_n, 1, 0);
     const bool streaming = streaming_stores(a, 1, false);

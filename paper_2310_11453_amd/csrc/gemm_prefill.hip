@@ -890,7 +890,7 @@ static void launch_tile(const GemmArgs& a, hipStream_t s) {
 // A mixture of experts: the tiles of a bound of its rows of tiles, one for every BM slots and one more for each expert.
 template <int BM>
 static void launch_experts_tile(const GemmArgs& a, hipStream_t s) {
-    const int64_t grid_n = (a.N + 255) / 256, most = (a.M / BM + (a.M < a.experts ? a.M : a.experts)) * grid_n;
+    const int64_t grid_n = (a.N + 255) / 256, most = most_tiles(a.M, a.experts, BM, 0) * grid_n;
     const int grid = (int)(most < num_cus() ? most : num_cus());
     gemm_prefill_kernel<BM, 256, 2, 4, 8, false, true><<<(unsigned)grid, 512, 0, s>>>(a, 0, (int)grid_n, 1);
 }

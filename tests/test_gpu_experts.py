@@ -193,6 +193,19 @@ def test_backward(bl, M, top_k, E, K, N, gather, per_tensor):
     check_backward(bl, M, top_k, E, K, N, gather, per_tensor, choices(M, top_k, E, M + K, unrouted=0.1))
 
 
+# Both tiles of either product, slices of the reductions (more of them than an expert has blocks of 32 slots), and fewer
+# workgroups than tiles.
+@pytest.mark.parametrize("spec", ["bwd_dx=1,bwd_ring=1", "bwd_dx=2,bwd_ring=2", "bwd_dx=1,bwd_ring=1,bwd_splits=3",
+                                  "bwd_dx=2,bwd_ring=2,bwd_splits=5", "bwd_dx=1,bwd_ring=2,bwd_grid=8",
+                                  "bwd_dx=2,bwd_ring=1,bwd_grid=4", "bwd_splits=16,bwd_grid=8"])
+@pytest.mark.parametrize("M,top_k,E,K,N", [(5, 3, 4, 544, 33), (130, 1, 2, 160, 130), (700, 2, 5, 288, 520)])
+def test_backward_variants(bl, tuning, M, top_k, E, K, N, spec):
+    print(f"backward M={M} top_k={top_k} E={E} K={K} N={N} {spec}", flush=True)
+    tuning(spec)
+    check_backward(bl, M, top_k, E, K, N, True, True, choices(M, top_k, E, M + K, unrouted=0.1))
+    check_backward(bl, M, top_k, E, K, N, True, True, choices(M, top_k, E, M, only=[1]))
+
+
 @pytest.mark.parametrize("only", [[0], [4]])
 @pytest.mark.parametrize("M", [1, 33, 300])
 def test_backward_when_one_expert_has_all_slots(bl, M, only):
