@@ -340,8 +340,7 @@ __global__ __launch_bounds__(256, T == 256 ? 1 : 2) void gemm_tn_bf16_wide(const
     const int nst_all = (int)(Rp / 32);
     __shared__ std::conditional_t<EXP, ExpertTiles, int> smE;
     if constexpr (EXP) expert_tiles(ex.offsets, ex.E, ex.T, 32, smE, ex.least);
-    const int rows_i = EXP ? grid_i * ex.E : grid_i;  // rows of tiles
-    const int nitems = rows_i * grid_j * (SPLIT ? sl.splits : 1);
+    const int nitems = (EXP ? ex.E : 1) * grid_i * grid_j * (SPLIT ? sl.splits : 1);
     int expert = 0;  // of the tile whose origin was asked for last
     int nst = nst_all;  // stages of the current work item, the first one st0 (SPLIT)
     int st0 = 0;
@@ -349,18 +348,36 @@ __global__ __launch_bounds__(256, T == 256 ? 1 : 2) void gemm_tn_bf16_wide(const
     int main_groups = nst >= 2 * NS - 1 ? (nst - (2 * NS - 1)) / NS + 1 : 0;
 
     auto tile_origin = [&](int t, int64_t& i0, int64_t& j0) {
+        if constexpr (EXP) {
+            // Each XCD gets a contiguous eighth of every expert's tiles.  (An eighth of all tiles is an expert each of eight,
+            // and the one with the most slots sets the time: 8192 slots of 8 experts, 2048 -> 8192, 524 us, so 346.)
+            const int per = grid_i * grid_j;
+            int tile = SPLIT ? t / sl.splits : t;
+            expert = tile / per;
+            tile -= expert * per;
+            if (!SPLIT && per >= 64 && (gridDim.x & 7) == 0) {
+                const int G = (int)gridDim.x, x = t & 7, q = ((t % G) >> 3) + (t / G) * (G >> 3);
+                const int first = per * x / 8, len = per * (x + 1) / 8 - first;
+                expert = q / len;
+                tile = first + q - expert * len;
+            }
+            // In bands of H rows of tiles, the rows fastest: what an XCD runs together is about square.  Calls in 128 x 128
+            // tiles, rows of tiles one by one / in bands of 8: 4480 slots of 7 experts 2048 -> 8192 302 / 233, 6560 of 5
+            // 4096 -> 4096 345 / 286, 16128 of 9 4096 -> 1024 253 / 243; bands of 2, 4, 8 and 16, 8192 of 8 2048 -> 8192 743,
+            // 698, 730, 737.
+            constexpr int H = 4;
+            const int band = tile / (H * grid_j), rem = tile - band * H * grid_j;
+            const int rows = grid_i - band * H < H ? grid_i - band * H : H;
+            i0 = expert < ex.E ? (int64_t)(band * H + rem % rows) * BM : -1;
+            j0 = (int64_t)(rem / rows) * BN;
+            return;
+        }
         if constexpr (SPLIT) {
             const int tile = t / sl.splits;
             i0 = (int64_t)(tile / grid_j) * BM;
             j0 = (int64_t)(tile % grid_j) * BN;
         } else {
-            ring_tile_origin(t, (int)gridDim.x, rows_i, grid_j, blk_i, blk_j, BM, BN, i0, j0);
-        }
-        if constexpr (EXP) {
-            if (i0 < 0) return;
-            const int row = (int)(i0 / BM);
-            expert = row / grid_i;
-            i0 = (int64_t)(row - expert * grid_i) * BM;
+            ring_tile_origin(t, (int)gridDim.x, grid_i, grid_j, blk_i, blk_j, BM, BN, i0, j0);
         }
     };
     auto set_slice = [&](int t) {
@@ -498,7 +515,7 @@ __global__ __launch_bounds__(256, T == 256 ? 1 : 2) void gemm_tn_bf16_wide(const
         block_barrier();
         const int t_next = t + (int)gridDim.x;
         int64_t i0n = -1, j0n = -1;
-        if (t_next < nitems) tile_origin(t_next, i0n, j0n);
+        if (t_next < nitems || (EXP && !SPLIT)) tile_origin(t_next, i0n, j0n);
         float* Cs = SPLIT ? C + (int64_t)(t % sl.splits) * (EXP ? ex.E : 1) * I * J : C;
         float sc = scale;
         if constexpr (EXP) {
@@ -1148,18 +1165,46 @@ __global__ __launch_bounds__(256) void fold_expert_weights(const float* __restri
     }
 }
 
+// The tiles and slices that cost least, by the costs in us that the plain layer's plans take.  How the slots fall on the
+// experts is not known here: an expert's last row of tiles is taken to be half full, its reduction of average length.
 ExpertsBackwardPlan experts_backward_plan(int64_t T, int64_t N, int64_t K, int E) {
+    constexpr RingCost kDxWide{0.615, 12.0, 5.0, 6.0}, kDxRows{0.33, 5.0, 5.0, 6.0}, kDxAlone{0.39, 2.0, 5.0, 6.0};
+    constexpr RingCost kDwWide{0.68, 12.8, 5.0, 6.0}, kDwSmall{0.172, 2.3, 5.0, 6.0}, kDwAlone{0.226, 3.6, 5.0, 6.0};
     const Tuning& t = tuning();
+    const double cus = ring_cus(), A = (double)(T < E ? T : E);
+    auto tiles_of = [](int64_t v, int64_t b) { return (double)((v + b - 1) / b); };
+    auto us = [&](RingCost c, double tiles, double stages, int n, double bytes, double unsure) {
+        double rounds = tiles * n / cus + unsure;
+        if (rounds < 1.0) rounds = 1.0;
+        return rounds * (c.stage * stages / n + c.item) + (n > 1 ? c.fold + n * bytes * 2e-6 / c.rate : 0.0);
+    };
     ExpertsBackwardPlan p{1, 1, 1, 1};
-    const int64_t cus = ring_cus(), A = T < E ? T : E;
-    const int64_t rows = T / 256 + (A + 1) / 2, tiles = rows * ((K + 255) / 256);
-    if (t.bwd_dx) p.dx_tile = t.bwd_dx;
-    else p.dx_tile = tiles >= cus ? 1 : 2;
-    if (t.bwd_ring) p.dw_tile = t.bwd_ring;
-    else p.dw_tile = T / E >= 512 ? 1 : 2;
-    if (t.bwd_splits > 1) p.dx_splits = p.dw_splits = t.bwd_splits < 16 ? t.bwd_splits : 16;
-    const int64_t nst = (N + 31) / 32;
-    if (p.dx_splits > nst) p.dx_splits = (int)nst;
+    double dx_us = 1e30, dw_us = 1e30;
+    const double nst = tiles_of(N, 32), rst = (double)T / 32.0 / E + 0.5;
+    for (int tile = 1; tile <= 2; ++tile)
+        for (int n = 1; n <= 16; n *= 2) {
+            const bool wide = tile == 1;
+            if ((!t.bwd_dx || t.bwd_dx == tile) && (n == 1 || nst >= 8 * n)) {
+                const double rows = (double)T / (wide ? 256 : 128) + 0.5 * A;
+                const double tiles = (rows > 0.9 * A ? rows : 0.9 * A) * tiles_of(K, 256);
+                const RingCost c = wide ? kDxWide : tiles * n > cus ? kDxRows : kDxAlone;
+                const double v = us(c, tiles, nst, n, (double)T * (double)K * 4.0, 0.4);
+                if (v < dx_us) dx_us = v, p.dx_tile = tile, p.dx_splits = n;
+            }
+            if ((!t.bwd_ring || t.bwd_ring == tile) && (n == 1 || rst >= 8 * n)) {
+                const double tiles = E * tiles_of(N, wide ? 256 : 128) * tiles_of(K, wide ? 256 : 128);
+                const RingCost c = wide ? kDwWide : tiles * n > cus ? kDwSmall : kDwAlone;
+                // operands that do not stay in the 256 MB cache cost the small tiles, which read them more often, more (8192
+                // slots of 8 experts 2048 -> 8192, 168 MB: 657 in the large ones, 698; half the slots 410 / 384)
+                const double more = !wide && (double)(N + K) * (double)T * 2.0 > 1.4e8 ? 1.2 : 1.0;
+                const double v = us(c, tiles, more * rst, n, (double)E * (double)N * (double)K * 4.0, 0.2);
+                if (v < dw_us) dw_us = v, p.dw_tile = tile, p.dw_splits = n;
+            }
+        }
+    if (t.bwd_splits > 0) {
+        p.dx_splits = p.dw_splits = t.bwd_splits < 16 ? t.bwd_splits : 16;
+        if (p.dx_splits > nst) p.dx_splits = (int)nst;
+    }
     return p;
 }
 

@@ -16,8 +16,10 @@
 namespace bl {
 
 namespace exb {
-constexpr int kTile = 64;  // 64 x 64 elements of an item
-typedef uint16_t CastTile[kTile][kTile + 2];
+// An item of the copies: 64 slots x 128 columns, transposed through LDS (the pitch is odd in dwords, so that the rows that
+// a lane's eight reads of a column come from are on different banks).
+constexpr int kRows = 64, kCols = 128;
+typedef uint16_t CastTile[kRows][kCols + 2];
 
 struct Args {
     const uint16_t* dY;
@@ -43,65 +45,73 @@ __device__ inline uint32_t to_bf16(float v) {
 // (block_offset of backward.hip)
 __device__ inline int64_t copy_offset(int64_t row, int64_t r, int64_t R) { return ((r >> 5) * R + row) * 32 + (r & 31); }
 
-// Rows of a tile: 16 at a time are in one block of 32 slots, i.e. of one expert.
-struct SlotRow {
-    int slot;     // -1: filled up
-    bool exists;  // the block does
-};
-__device__ inline SlotRow slot_row(const ExpertTiles& count, int E, int blocks, int r) {
-    const int b = r >> 5;
-    if (b >= blocks) return {-1, false};
-    int from, to;
-    expert_of_tile(count, E, b, 32, from, to);
-    const int s = from + (r & 31);
-    return {s < to ? s : -1, true};
-}
-
-// dY (bf16) -> g and gwT, or codes -> qT.  VEC: four elements a load.
+// dY (bf16) -> g and gwT, or codes -> qT.  VEC: a thread's eight elements are one load.  Everything that an item reads is
+// requested before the first of it is used.
 template <bool CODES, bool VEC>
 __device__ inline void copy_tile(const exb::Args& a, const ExpertTiles& count, int blocks, int r0, int64_t c0,
                                  exb::CastTile& tile) {
+    using namespace exb;
     const int64_t C = CODES ? a.K : a.N;
-    const int cl = ((int)threadIdx.x & 15) * 4;
+    const int cl = ((int)threadIdx.x & 15) * 8, rt = (int)threadIdx.x >> 4;
     const int64_t c = c0 + cl;
+    int slot[4];  // of rows rt + 16 it; -1: filled up.  Rows 0 .. 31 of the item are a block, of one expert, 32 .. 63 another
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        int from = 0, to = 0;
+        if ((r0 >> 5) + h < blocks) expert_of_tile(count, a.E, (r0 >> 5) + h, 32, from, to);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) slot[2 * h + i] = from + rt + 16 * i < to ? from + rt + 16 * i : -1;
+    }
+    uint32_t v[4][4] = {};  // eight bf16 a row
+    float gamma[4];
+    uint32_t row[4];
+#pragma unroll
+    for (int it = 0; it < 4; ++it)
+        if (slot[it] >= 0 && (CODES || a.row_gamma)) row[it] = code_row(a.order, a.top_k, a.rows, (uint32_t)slot[it]);
 #pragma unroll
     for (int it = 0; it < 4; ++it) {
-        const int rl = it * 16 + (int)(threadIdx.x >> 4);
-        const SlotRow sr = slot_row(count, a.E, blocks, r0 + rl);
-        uint32_t lo = 0, hi = 0;
-        if (sr.slot >= 0 && c < C) {
-            if constexpr (CODES) {
-                const int8_t* const src = a.codes + (int64_t)code_row(a.order, a.top_k, a.rows, (uint32_t)sr.slot) * C + c;
-                const char4 t = *reinterpret_cast<const char4*>(src);  // K % 32 == 0
-                lo = to_bf16((float)t.x) | to_bf16((float)t.y) << 16;
-                hi = to_bf16((float)t.z) | to_bf16((float)t.w) << 16;
+        if (slot[it] < 0 || c >= C) continue;
+        if constexpr (CODES) {  // K % 32 == 0
+            const int8_t* const src = a.codes + (int64_t)row[it] * C + c;
+            const uint2 t = *reinterpret_cast<const uint2*>(src);
+            v[it][0] = t.x, v[it][1] = t.y;
+        } else {
+            const uint16_t* const src = a.dY + (int64_t)slot[it] * C + c;
+            if constexpr (VEC) {
+                const uint4 t = *reinterpret_cast<const uint4*>(src);
+                v[it][0] = t.x, v[it][1] = t.y, v[it][2] = t.z, v[it][3] = t.w;
             } else {
-                const uint16_t* const src = a.dY + (int64_t)sr.slot * C + c;
-                if constexpr (VEC) {
-                    const uint2 t = *reinterpret_cast<const uint2*>(src);
-                    lo = t.x, hi = t.y;
-                } else {
-                    lo = src[0] | (c + 1 < C ? (uint32_t)src[1] << 16 : 0);
-                    hi = (c + 2 < C ? src[2] : 0) | (c + 3 < C ? (uint32_t)src[3] << 16 : 0);
-                }
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    v[it][e] = (c + 2 * e < C ? src[2 * e] : 0) | (c + 2 * e + 1 < C ? (uint32_t)src[2 * e + 1] << 16 : 0);
             }
+            if (a.row_gamma) gamma[it] = a.row_gamma[row[it]];
         }
-        if constexpr (!CODES) {
-            if (a.g && sr.slot >= 0 && c < a.Np)
-                *reinterpret_cast<uint2*>(a.g + copy_offset(sr.slot, c, a.T)) = make_uint2(lo, hi);
-            if (!a.gwT) continue;  // uniform
-            if (a.row_gamma && sr.slot >= 0) {
-                const float sc = a.row_gamma[code_row(a.order, a.top_k, a.rows, (uint32_t)sr.slot)] / 128.0f;
-                auto scaled = [&](uint32_t v) {
-                    return to_bf16(__uint_as_float(v << 16) * sc) | to_bf16(__uint_as_float(v & 0xffff0000u) * sc) << 16;
-                };
-                lo = scaled(lo);
-                hi = scaled(hi);
+    }
+#pragma unroll
+    for (int it = 0; it < 4; ++it) {
+        const int rl = rt + 16 * it;
+        if constexpr (CODES) {
+            const uint32_t lo = v[it][0], hi = v[it][1];
+            auto pair = [](uint32_t w, int sh) {
+                return to_bf16((float)(int8_t)(w >> sh)) | to_bf16((float)(int8_t)(w >> (sh + 8))) << 16;
+            };
+            v[it][0] = pair(lo, 0), v[it][1] = pair(lo, 16), v[it][2] = pair(hi, 0), v[it][3] = pair(hi, 16);
+        } else {
+            if (a.g && slot[it] >= 0 && c < a.Np)
+                *reinterpret_cast<uint4*>(a.g + copy_offset(slot[it], c, a.T)) =
+                    make_uint4(v[it][0], v[it][1], v[it][2], v[it][3]);
+            if (a.row_gamma && slot[it] >= 0 && c < C) {
+                const float sc = gamma[it] / 128.0f;
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    v[it][e] = to_bf16(__uint_as_float(v[it][e] << 16) * sc) |
+                               to_bf16(__uint_as_float(v[it][e] & 0xffff0000u) * sc) << 16;
             }
         }
         uint32_t* const t32 = reinterpret_cast<uint32_t*>(&tile[rl][cl]);
-        t32[0] = lo;
-        t32[1] = hi;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) t32[e] = v[it][e];
     }
     uint16_t* const tr = CODES ? a.qT : a.gwT;
     if (!tr) return;
@@ -109,13 +119,13 @@ __device__ inline void copy_tile(const exb::Args& a, const ExpertTiles& count, i
 #pragma unroll
     for (int it = 0; it < 4; ++it) {
         const int idx = it * 256 + (int)threadIdx.x;
-        const int cc = idx >> 4, rl = (idx & 15) * 4;
+        const int cc = idx >> 3, rl = (idx & 7) * 8;
         const int64_t col = c0 + cc;
-        const int r = r0 + rl;
-        if (col < C && r < blocks * 32)
-            *reinterpret_cast<uint2*>(tr + copy_offset(col, r, C)) =
-                make_uint2((uint32_t)tile[rl][cc] | ((uint32_t)tile[rl + 1][cc] << 16),
-                           (uint32_t)tile[rl + 2][cc] | ((uint32_t)tile[rl + 3][cc] << 16));
+        if (col >= C || r0 + rl >= blocks * 32) continue;
+        uint32_t o[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] = (uint32_t)tile[rl + 2 * e][cc] | (uint32_t)tile[rl + 2 * e + 1][cc] << 16;
+        *reinterpret_cast<uint4*>(tr + copy_offset(col, r0 + rl, C)) = make_uint4(o[0], o[1], o[2], o[3]);
     }
 }
 
@@ -145,7 +155,7 @@ __device__ inline void words_tile(const exb::Args& a, int e, int64_t sw, int64_t
 template <bool VEC>
 __global__ __launch_bounds__(256) void prepare_expert_operands(exb::Args a) {
     __shared__ ExpertTiles count;
-    __shared__ __attribute__((aligned(8))) union {
+    __shared__ __attribute__((aligned(16))) union {
         exb::CastTile tile;
         uint32_t words[2][256];
     } sm;
@@ -162,10 +172,10 @@ __global__ __launch_bounds__(256) void prepare_expert_operands(exb::Args a) {
         const bool codes = i < a.code_items;
         if (!codes) i -= a.code_items;
         const uint32_t x = codes ? a.code_x : a.dy_x;
-        const int r0 = (int)(i / x) * exb::kTile;
+        const int r0 = (int)(i / x) * exb::kRows;
         if (r0 >= blocks * 32) continue;  // uniform: the grid is a bound
-        if (codes) copy_tile<true, true>(a, count, blocks, r0, (int64_t)(i % x) * exb::kTile, sm.tile);
-        else copy_tile<false, VEC>(a, count, blocks, r0, (int64_t)(i % x) * exb::kTile, sm.tile);
+        if (codes) copy_tile<true, true>(a, count, blocks, r0, (int64_t)(i % x) * exb::kCols, sm.tile);
+        else copy_tile<false, VEC>(a, count, blocks, r0, (int64_t)(i % x) * exb::kCols, sm.tile);
     }
 }
 
@@ -213,8 +223,8 @@ hipError_t launch_experts_backward(const ExpertsArgs& a, hipStream_t s) {
     }
     b.N = a.N; b.K = a.K; b.Np = pad32(a.N);
     b.blob = tiles_n(a.N) * tiles_k(a.K) * 256;
-    auto tiles = [](int64_t v) { return (v + exb::kTile - 1) / exb::kTile; };
-    const int64_t rows = tiles(most_tiles(a.T, a.E, 32, b.least) * 32);
+    auto tiles = [](int64_t v) { return (v + exb::kCols - 1) / exb::kCols; };
+    const int64_t rows = (most_tiles(a.T, a.E, 32, b.least) + 1) / 2;
     b.bits_x = (uint32_t)tiles_k(a.K);
     b.bits_y = (uint32_t)(b.Np / 32);
     b.code_x = (uint32_t)tiles(a.K);
@@ -226,7 +236,7 @@ hipError_t launch_experts_backward(const ExpertsArgs& a, hipStream_t s) {
     b.code_items = (uint32_t)codes;
     b.items = (uint32_t)items;
     const unsigned grid = (unsigned)(items < (1 << 23) ? items : (1 << 23));
-    if (a.N % 4 == 0 && ((uintptr_t)a.dY & 7) == 0) prepare_expert_operands<true><<<grid, 256, 0, s>>>(b);
+    if (a.N % 8 == 0 && ((uintptr_t)a.dY & 15) == 0) prepare_expert_operands<true><<<grid, 256, 0, s>>>(b);
     else prepare_expert_operands<false><<<grid, 256, 0, s>>>(b);
 
     ExpertsOperands o{b.g, b.gwT, b.qT, b.Sw, a.offsets, a.E, b.least, a.T, a.N, a.K, a.beta,
