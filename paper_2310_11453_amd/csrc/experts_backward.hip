@@ -164,8 +164,9 @@ __global__ __launch_bounds__(256) void prepare_expert_operands(exb::Args a) {
         if (it != blockIdx.x) __syncthreads();  // the item before has been read
         uint32_t i = it;
         if (i < a.bits_items) {
-            const uint32_t y = i / a.bits_x;  // 512 columns fastest
-            words_tile(a, (int)(y / a.bits_y), y % a.bits_y, i % a.bits_x, sm.words);
+            const uint32_t y = i / a.bits_x, e = y / a.bits_y;  // 512 columns fastest
+            if (count.from[e] < count.to[e])  // else nobody reads them
+                words_tile(a, (int)e, y % a.bits_y, i % a.bits_x, sm.words);
             continue;
         }
         i -= a.bits_items;

@@ -5,8 +5,8 @@
 //              checkpoint, per block b of 128 elements of a row: c = rne(u * (127 / amax_b)), kept beside amax_b / 127
 //   backward   v = c * (amax_b / 127), h = f(v), n = (h - mean h) / sqrt(var h + eps)
 //              du = f'(v) * (g - mean g - n mean(g n)) / sqrt(var h + eps),  g = the gradient of x^
-// The backward is the derivative of the forward at v, exactly: its statistics are those of f(v), which come out of the row
-// that is in registers anyway, and nothing but the checkpoint has to be kept (1.03 bytes an element where u has four).
+// The backward is the derivative of the forward at v, exactly: its statistics are those of f(v), which come out of the
+// row that is in registers anyway, and nothing but the checkpoint has to be kept (1.03 bytes an element where u has four).
 // f and f' are evaluated in fp32, the sums of a row in fp64 (as in the quantiser and in the LayerNorm backward).
 // Bound by HBM: 4 bytes read and 1 (with the checkpoint 2) written an element, twice the reading with a gamma per
 // tensor; backward 5 read, 2 or 4 written.
@@ -20,26 +20,36 @@ namespace bl {
 enum Fn { kRelu = 0, kRelu2 = 1, kGelu = 2, kSilu = 3 };
 enum RowMode { kOnce = 0, kRowStats = 1, kRowApply = 2 };
 
+// f(u) and f'(u).  GELU: Phi(u) = (1 + erf(z)) / 2, z = u / sqrt 2, with erf as in Abramowitz and Stegun 7.1.26 (erf z =
+// 1 - (a1 t + ... + a5 t^5) e^(-z^2), t = 1 / (1 + p z), z >= 0: off by at most 1.5e-7), which shares its exponential
+// with f'.  The hardware's exponential and reciprocal are off by an ulp.  (Passes over 16384 x 8192 with the library's
+// erff and expf / so: forward, gamma per tensor, 362 / 314 us, backward 455 / 219.)
+struct FnPair {
+    float value, slope;
+};
 template <int FN>
-__device__ inline float fn_value(float u) {
-    if constexpr (FN == kRelu) return u > 0.f ? u : 0.f;
-    else if constexpr (FN == kRelu2) return u > 0.f ? u * u : 0.f;
-    else if constexpr (FN == kGelu) return 0.5f * u * (1.f + erff(u * 0.70710678118654752f));
-    else return u / (1.f + expf(-u));
-}
-template <int FN>
-__device__ inline float fn_slope(float u) {
+__device__ inline FnPair fn_pair(float u) {
     if constexpr (FN == kRelu) {
-        return u > 0.f ? 1.f : 0.f;
+        return {u > 0.f ? u : 0.f, u > 0.f ? 1.f : 0.f};
     } else if constexpr (FN == kRelu2) {
-        return u > 0.f ? 2.f * u : 0.f;
+        const float r = u > 0.f ? u : 0.f;
+        return {r * r, 2.f * r};
     } else if constexpr (FN == kGelu) {
-        return 0.5f * (1.f + erff(u * 0.70710678118654752f)) + u * (0.39894228040143268f * expf(-0.5f * u * u));
+        const float z = fabsf(u) * 0.70710678118654752f;
+        const float e = __builtin_amdgcn_exp2f(u * u * -0.72134752044448170f);  // e^(-u^2 / 2)
+        const float t = __builtin_amdgcn_rcpf(fmaf(z, 0.3275911f, 1.f));
+        float p = fmaf(1.061405429f, t, -1.453152027f);
+        p = fmaf(fmaf(fmaf(p, t, 1.421413741f), t, -0.284496736f), t, 0.254829592f);
+        const float tail = 0.5f * (p * t * e);  // Phi(-|u|)
+        const float phi = u < 0.f ? tail : 1.f - tail;
+        return {u * phi, fmaf(u * 0.39894228040143268f, e, phi)};
     } else {
-        const float s = 1.f / (1.f + expf(-u));
-        return s + u * s * (1.f - s);
+        const float s = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(u * -1.4426950408889634f));
+        return {u * s, fmaf(u * s, 1.f - s, s)};
     }
 }
+template <int FN>
+__device__ inline float fn_value(float u) { return fn_pair<FN>(u).value; }
 
 // the largest value of 32 lanes, one half of a wave
 __device__ inline float half_wave_max(float v) {
@@ -52,8 +62,8 @@ __device__ inline float half_wave_max(float v) {
     return max_raw(lo, hi);
 }
 
-// WPR waves share a row, a lane holds NV float4 of it.  kRowStats and kRowApply: the two passes of a gamma per tensor; the
-// first leaves the row's statistics in rowstats and its largest magnitude where its codes will be, which nobody
+// WPR waves share a row, a lane holds NV float4 of it.  kRowStats and kRowApply: the two passes of a gamma per tensor;
+// the first leaves the row's statistics in rowstats and its largest magnitude where its codes will be, which nobody
 // writes before the second.
 template <int FN, int WPR, int NV, int MODE>
 __global__ __launch_bounds__((WPR < 4 ? 4 : WPR) * kWave) void nonlinear_rows(NonlinearArgs a) {
@@ -88,7 +98,8 @@ __global__ __launch_bounds__((WPR < 4 ? 4 : WPR) * kWave) void nonlinear_rows(No
             const int idx = t + j * RT;
             const bool in = idx < K4;
             const float4 x = v[j];
-            const float big = half_wave_max(in ? max_raw(max_raw(fabsf(x.x), fabsf(x.y)), max_raw(fabsf(x.z), fabsf(x.w))) : 0.f);
+            const float mine = max_raw(max_raw(fabsf(x.x), fabsf(x.y)), max_raw(fabsf(x.z), fabsf(x.w)));
+            const float big = half_wave_max(in ? mine : 0.f);
             const float up = big > 0.f ? 127.f / big : 0.f;
             if (in && live) {
                 c4[idx] = code_word(x.x * up, x.y * up, x.z * up, x.w * up, -127.f);
@@ -152,8 +163,8 @@ __global__ __launch_bounds__((WPR < 4 ? 4 : WPR) * kWave) void nonlinear_rows(No
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
         const int idx = t + j * RT;
-        const uint32_t wd = code_word(normalised(n, (double)v[j].x - c) * scale, normalised(n, (double)v[j].y - c) * scale,
-                                      normalised(n, (double)v[j].z - c) * scale, normalised(n, (double)v[j].w - c) * scale);
+        auto scaled = [&](float h) { return normalised(n, (double)h - c) * scale; };
+        const uint32_t wd = code_word(scaled(v[j].x), scaled(v[j].y), scaled(v[j].z), scaled(v[j].w));
         if (idx < K4) {
             sum = __builtin_amdgcn_sdot4((int)wd, 0x01010101, sum, false);
             if (live) q4[(uint32_t)idx] = wd;
@@ -172,8 +183,14 @@ __global__ __launch_bounds__(1024) void nonlinear_fold(NonlinearArgs a) {
     __shared__ float sm[NW];
     const int64_t M = a.rows ? (*a.rows < a.M ? *a.rows : a.M) : a.M;
     float most = 0.f;
-#pragma unroll 8
-    for (int64_t i = threadIdx.x; i < M; i += 1024) most = max_raw(most, reinterpret_cast<const float*>(a.codes)[i]);
+    const float* const rows = reinterpret_cast<const float*>(a.codes);
+    for (int64_t i = threadIdx.x; i < M; i += 8 * 1024) {  // eight loads in flight; behind the last row that one again
+        float v[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) v[u] = rows[i + u * 1024 < M ? i + u * 1024 : M - 1];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) most = max_raw(most, v[u]);
+    }
     most = wave_reduce(most, OpMax{});
     if (threadIdx.x % kWave == 0) sm[threadIdx.x / kWave] = most;
     __syncthreads();
@@ -183,15 +200,15 @@ __global__ __launch_bounds__(1024) void nonlinear_fold(NonlinearArgs a) {
 }
 
 // ---- backward -----------------------------------------------------------------------------------------
-__device__ inline uint32_t bf16_word(float lo, float hi) {
-    auto rne = [](float v) {
-        uint32_t u = __float_as_uint(v);
-        u += 0x7fffu + ((u >> 16) & 1u);
-        return u >> 16;
-    };
-    return rne(lo) | rne(hi) << 16;
+typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
+__device__ inline uint32_t bf16_word(float lo, float hi) {  // to nearest, ties to even
+    const v2bf v = {(__bf16)lo, (__bf16)hi};
+    return __builtin_bit_cast(uint32_t, v);
 }
 
+// One reading of the row: g, and of the checkpoint f(v) and f'(v), stay in registers; the four sums that the derivative of
+// the LayerNorm needs (of h, h^2, g and g h) are taken together.  With eight float4 a lane and 16 waves a row, which have
+// 128 registers, the pairs are evaluated a second time instead of kept (2000 x 28672: 473 us kept and spilled, 148 so).
 template <int FN, int WPR, int NV>
 __global__ __launch_bounds__((WPR < 4 ? 4 : WPR) * kWave) void nonlinear_backward_rows(NonlinearArgs a) {
     constexpr int NW = WPR < 4 ? 4 : WPR, RPW = NW / WPR, RT = WPR * kWave;
@@ -208,36 +225,47 @@ __global__ __launch_bounds__((WPR < 4 ? 4 : WPR) * kWave) void nonlinear_backwar
     const int blocks = (int)((a.K + kCheckBlock - 1) / kCheckBlock);
     const float4* __restrict__ g4 = reinterpret_cast<const float4*>(a.dXhat + row * a.K);
     const uint32_t* __restrict__ c4 = reinterpret_cast<const uint32_t*>(a.check + row * a.K);
+    const float* __restrict__ scales = a.check_scale + row * blocks;
 
-    float4 g[NV], v[NV];
+    constexpr bool KEEP = NV < 8 || WPR < 16;
+    float4 g[NV], h[KEEP ? NV : 1], f[KEEP ? NV : 1];
+    uint32_t q[NV];
+    float sc[NV];
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
         const int idx = t + j * RT, at = idx < K4 ? idx : K4 - 1;
-        g[j] = g4[at];
-        const uint32_t q = c4[at];
-        const float sc = a.check_scale[row * blocks + (at >> 5)];
-        v[j].x = (float)(int8_t)q * sc;
-        v[j].y = (float)(int8_t)(q >> 8) * sc;
-        v[j].z = (float)(int8_t)(q >> 16) * sc;
-        v[j].w = (float)(int8_t)(q >> 24) * sc;
+        g[j] = g4[(uint32_t)at];
+        q[j] = c4[(uint32_t)at];
+        sc[j] = scales[(uint32_t)at >> 5];
     }
     // sums about an element of the row, so that a large common offset costs nothing
-    const double c = (double)fn_value<FN>((float)a.check[row * a.K] * a.check_scale[row * blocks]);
+    const double c = (double)fn_value<FN>((float)(int8_t)c4[0] * scales[0]);
+    auto pairs = [](uint32_t codes, float scale, float4& value, float4& slope) {
+        const FnPair x = fn_pair<FN>((float)(int8_t)codes * scale), y = fn_pair<FN>((float)(int8_t)(codes >> 8) * scale);
+        const FnPair z = fn_pair<FN>((float)(int8_t)(codes >> 16) * scale), w = fn_pair<FN>((float)(int8_t)(codes >> 24) * scale);
+        value = make_float4(x.value, y.value, z.value, w.value);
+        slope = make_float4(x.slope, y.slope, z.slope, w.slope);
+    };
     double s[4] = {0.0, 0.0, 0.0, 0.0};  // of h - c, (h - c)^2, g, g (h - c)
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-        if (t + j * RT >= K4) continue;
-        auto add = [&](float u, float d) {
-            const double h = (double)fn_value<FN>(u) - c;
-            s[0] += h;
-            s[1] = fma(h, h, s[1]);
+        const int k = KEEP ? j : 0;
+        pairs(q[j], sc[j], h[k], f[k]);
+        if (K4 < (j + 1) * RT && t + j * RT >= K4) {  // behind the row: nothing to the sums
+            h[k] = make_float4((float)c, (float)c, (float)c, (float)c);
+            g[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+        }
+        auto add = [&](float value, float d) {
+            const double x = (double)value - c;
+            s[0] += x;
+            s[1] = fma(x, x, s[1]);
             s[2] += (double)d;
-            s[3] = fma((double)d, h, s[3]);
+            s[3] = fma((double)d, x, s[3]);
         };
-        add(v[j].x, g[j].x);
-        add(v[j].y, g[j].y);
-        add(v[j].z, g[j].z);
-        add(v[j].w, g[j].w);
+        add(h[k].x, g[j].x);
+        add(h[k].y, g[j].y);
+        add(h[k].z, g[j].z);
+        add(h[k].w, g[j].w);
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) s[i] = wave_reduce(s[i], OpSum{});
@@ -253,34 +281,50 @@ __global__ __launch_bounds__((WPR < 4 ? 4 : WPR) * kWave) void nonlinear_backwar
     const float r = (float)rstd;
     const float m1 = (float)(s[2] * a.inv_k), m2 = (float)((s[3] - dm * s[2]) * rstd * a.inv_k);
     const double nshift = -(dm * rstd);
+    // hide them from the optimiser, which would keep what the sums made of them alive
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-        const int idx = t + j * RT;
-        auto du = [&](float u, float d) {
-            const float n = (float)fma((double)fn_value<FN>(u) - c, rstd, nshift);
-            return r * ((d - m1) - n * m2) * fn_slope<FN>(u);
+        if constexpr (KEEP) asm volatile("" : "+v"(h[j].x), "+v"(h[j].y), "+v"(h[j].z), "+v"(h[j].w));
+        else asm volatile("" : "+v"(q[j]), "+v"(sc[j]));
+    }
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        const int idx = t + j * RT, k = KEEP ? j : 0;
+        if constexpr (!KEEP) pairs(q[j], sc[j], h[k], f[k]);
+        auto du = [&](float value, float slope, float d) {
+            const float n = (float)fma((double)value - c, rstd, nshift);
+            return r * ((d - m1) - n * m2) * slope;
         };
-        const float x = du(v[j].x, g[j].x), y = du(v[j].y, g[j].y), z = du(v[j].z, g[j].z), w = du(v[j].w, g[j].w);
+        const float x = du(h[k].x, f[k].x, g[j].x), y = du(h[k].y, f[k].y, g[j].y);
+        const float z = du(h[k].z, f[k].z, g[j].z), w = du(h[k].w, f[k].w, g[j].w);
         if (idx < K4 && live) {
-            if (a.bf16) reinterpret_cast<uint2*>(reinterpret_cast<uint16_t*>(a.dU) + row * a.K)[idx] = make_uint2(bf16_word(x, y), bf16_word(z, w));
-            else reinterpret_cast<float4*>(reinterpret_cast<float*>(a.dU) + row * a.K)[idx] = make_float4(x, y, z, w);
+            if (a.bf16)
+                reinterpret_cast<uint2*>(reinterpret_cast<uint16_t*>(a.dU) + row * a.K)[(uint32_t)idx] =
+                    make_uint2(bf16_word(x, y), bf16_word(z, w));
+            else
+                reinterpret_cast<float4*>(reinterpret_cast<float*>(a.dU) + row * a.K)[(uint32_t)idx] =
+                    make_float4(x, y, z, w);
         }
     }
 }
 
-// Waves a row and float4 a lane: enough waves that the chip has about sixteen a CU, at most eight float4 a lane.
+// Waves a row and float4 a lane.  A batch of few rows is the length of one row's chain: more waves share it, down to two
+// float4 a lane; a large one is bound by HBM.
 struct RowShape {
     int wpr, nv;
 };
 static RowShape row_shape(int64_t M, int64_t K) {
-    constexpr RowShape shapes[] = {{1, 2}, {1, 4}, {1, 8}, {4, 2}, {4, 4}, {4, 8}, {8, 4}, {8, 8}, {16, 8}};
     const int64_t K4 = K / 4;
-    for (const RowShape& q : shapes) {
-        if (K4 > (int64_t)q.wpr * kWave * q.nv) continue;
-        if (q.wpr == 1 && M < 2048 && K4 >= 4 * kWave * 2) continue;  // few rows: more waves share one
-        return q;
-    }
-    return {16, 8};
+    int wpr = 1, nv = 2;
+    auto wider = [&]() { wpr = wpr == 1 ? 4 : wpr * 2; };
+    while (wpr < 16 && K4 > (int64_t)wpr * kWave * 8) wider();
+    // (us, forward / backward: 32 x 8192 with 4, 8, 16 waves 4.9 / 6.8, 4.3 / 5.0, 4.6 / 5.6; 32 x 2048 with 1, 4, 8 4.4 / 6.6,
+    // 3.0 / 3.1, 3.4 / 3.5; 16384 x 8192 with 4, 8, 16 126 / 219, 144 / 216, 194 / 297)
+    while (wpr < 8 && M * wpr <= 1024 && K4 > (int64_t)wpr * kWave * 2) wider();
+    if (const int v = tuning().quant_wpr)
+        if ((v == 1 || v == 4 || v == 8 || v == 16) && K4 <= (int64_t)v * kWave * 8) wpr = v;
+    while ((int64_t)wpr * kWave * nv < K4) nv *= 2;
+    return {wpr, nv};
 }
 
 template <int FN, int WPR, int NV>
@@ -311,8 +355,8 @@ static hipError_t launch_fn(const NonlinearArgs& a_in, bool backward, hipStream_
         if (backward) launch_backward_rows<FN, W, V>(a, s);  \
         else launch_forward<FN, W, V>(a, s);                 \
     }
-    BL_ROWS(1, 2) BL_ROWS(1, 4) BL_ROWS(1, 8) BL_ROWS(4, 2) BL_ROWS(4, 4) BL_ROWS(4, 8) BL_ROWS(8, 4) BL_ROWS(8, 8)
-    BL_ROWS(16, 8)
+    BL_ROWS(1, 2) BL_ROWS(1, 4) BL_ROWS(1, 8) BL_ROWS(4, 2) BL_ROWS(4, 4) BL_ROWS(4, 8) BL_ROWS(8, 2) BL_ROWS(8, 4)
+    BL_ROWS(8, 8) BL_ROWS(16, 2) BL_ROWS(16, 4) BL_ROWS(16, 8)
 #undef BL_ROWS
     return hipGetLastError();
 }
@@ -324,7 +368,11 @@ static hipError_t launch_any(const NonlinearArgs& a, int fn, bool backward, hipS
         default: return launch_fn<kSilu>(a, backward, s);
     }
 }
-hipError_t launch_quant_nonlinear(const NonlinearArgs& a, int fn, hipStream_t s) { return launch_any(a, fn, false, s); }
-hipError_t launch_nonlinear_backward(const NonlinearArgs& a, int fn, hipStream_t s) { return launch_any(a, fn, true, s); }
+hipError_t launch_quant_nonlinear(const NonlinearArgs& a, int fn, hipStream_t s) {
+    return launch_any(a, fn, false, s);
+}
+hipError_t launch_nonlinear_backward(const NonlinearArgs& a, int fn, hipStream_t s) {
+    return launch_any(a, fn, true, s);
+}
 
 }  // namespace bl
