@@ -492,21 +492,30 @@ def bitlinear_forward_nonneg(X: torch.Tensor, packed: torch.Tensor, N: int, beta
 
 # ---- Mixtures of BitLinear layers ("experts") ------------------------------------------------
 def _given(dev, t: torch.Tensor, dtype, *shape):
-    """Pointer of an operand that has to lie on `dev` and have this type and shape."""
+    """Pointer of an operand that has to lie on `dev`, be contiguous and have this type and shape.  (One test for all: a
+    call of a few tokens is as long as what Python does for it.)"""
+    if t.device == dev and t.shape == shape and t.dtype == dtype and t.is_contiguous():
+        return t.data_ptr()
     if t.device != dev:
         raise BitLinearError(f"tensors on {dev} and {t.device}")
-    if tuple(t.shape) != shape:
+    if t.shape != shape:
         raise BitLinearError(f"expected a tensor of shape {shape}, got {tuple(t.shape)}")
     return _ptr(t, dtype)
 
 
 def _here(t: torch.Tensor):
     """t's device, which has to be the current one: the launch goes to its current stream."""
-    if not t.is_cuda:
+    dev = t.device
+    if dev.type != "cuda":
         raise BitLinearError("tensor is not on the GPU")
-    if t.device.index != torch.cuda.current_device():
-        raise BitLinearError(f"tensor on {t.device}, current device {torch.cuda.current_device()}")
-    return t.device
+    if dev.index != torch._C._cuda_getDevice():
+        raise BitLinearError(f"tensor on {dev}, current device {torch.cuda.current_device()}")
+    return dev
+
+
+def _blob_bytes(N: int, K: int) -> int:
+    """packed_bytes(N, K) of a shape that the call itself checks."""
+    return (N + 15) // 16 * ((K + 511) // 512) * 1024
 
 
 def workspace_bytes_experts(op: int, M: int, top_k: int, N: int, K: int, experts: int,
@@ -552,13 +561,14 @@ def bitlinear_route(expert: torch.Tensor, experts: int, workspace: torch.Tensor 
     position = torch.empty((M, top_k), dtype=torch.int32, device=dev)
     offsets = torch.empty(experts + 1, dtype=torch.int32, device=dev) if M else torch.zeros(
         experts + 1, dtype=torch.int32, device=dev)
-    ws, ws_bytes, _keep = _scratch(workspace_bytes_experts(OP_ROUTE, M, top_k, 0, 0, experts), workspace, dev)
+    need = workspace_bytes_experts(OP_ROUTE, M, top_k, 0, 0, experts) if M * top_k > 4096 else 0
+    ws, ws_bytes, _keep = _scratch(need, workspace, dev)
     _check(lib.bitlinear_route(_ptr(expert, torch.int32), M, top_k, experts, order.data_ptr(), position.data_ptr(),
                                offsets.data_ptr(), ws, ws_bytes, _stream()), "bitlinear_route")
     return order, position, offsets
 
 
-def _slots(codes, offsets, order, top_k):
+def _slots(codes, order, top_k):
     """(M, top_k, T): the slots that `codes` serve, through `order` or one a row."""
     M = codes.shape[0]
     if order is None:
@@ -573,7 +583,7 @@ def bitlinear_matmul_experts(codes: torch.Tensor, gamma: torch.Tensor, rowsum: t
     """Eq. 7 + Eq. 11 with a weight matrix per expert: [slots, N] from the codes of tokens (through `order`, top_k slots
     a token) or of the slots themselves.  Slots without an expert are left as they were in `out`."""
     lib, dev = load_library(), _here(codes)
-    M, top_k, T = _slots(codes, offsets, order, top_k)
+    M, top_k, T = _slots(codes, order, top_k)
     K, E = codes.shape[1], offsets.numel() - 1
     dtype = torch.int32 if flags & FLAG_OUT_ACC_I32 else torch.float32
     if out is None:
@@ -581,7 +591,7 @@ def bitlinear_matmul_experts(codes: torch.Tensor, gamma: torch.Tensor, rowsum: t
     _check(lib.bitlinear_matmul_experts(
         _ptr(codes, torch.int8), _given(dev, gamma, torch.float32, 1 if per_tensor else M),
         _given(dev, rowsum, torch.int32, M), M, top_k, K, None if order is None else _given(dev, order, torch.int32, T),
-        _given(dev, offsets, torch.int32, E + 1), E, _given(dev, packed, torch.uint8, E, packed_bytes(N, K)), N,
+        _given(dev, offsets, torch.int32, E + 1), E, _given(dev, packed, torch.uint8, E, _blob_bytes(N, K)), N,
         _given(dev, beta, torch.float32, E), _gran(per_tensor), flags, _given(dev, out, dtype, T, N), _stream()),
         "bitlinear_matmul_experts")
     return out
@@ -594,7 +604,7 @@ def bitlinear_backward_ste_experts(dY: torch.Tensor, codes: torch.Tensor, gamma:
     """Section 2.2 (STE) for bitlinear_matmul_experts, dY bf16 [slots, N].  Returns (dX fp32 [slots, K] or None,
     dW fp32 [experts, N, K] or None)."""
     lib, dev = load_library(), _here(codes)
-    M, top_k, T = _slots(codes, offsets, order, top_k)
+    M, top_k, T = _slots(codes, order, top_k)
     K, E, N = codes.shape[1], offsets.numel() - 1, dY.shape[1]
     dX = torch.empty((T, K), dtype=torch.float32, device=dev) if want_dx else None
     dW = torch.empty((E, N, K), dtype=torch.float32, device=dev) if want_dw else None
@@ -603,7 +613,7 @@ def bitlinear_backward_ste_experts(dY: torch.Tensor, codes: torch.Tensor, gamma:
         _given(dev, dY, torch.bfloat16, T, N), M, top_k, N, K, _ptr(codes, torch.int8),
         _given(dev, gamma, torch.float32, 1 if per_tensor else M), _gran(per_tensor),
         None if order is None else _given(dev, order, torch.int32, T), _given(dev, offsets, torch.int32, E + 1), E,
-        None if packed is None else _given(dev, packed, torch.uint8, E, packed_bytes(N, K)),
+        None if packed is None else _given(dev, packed, torch.uint8, E, _blob_bytes(N, K)),
         None if beta is None else _given(dev, beta, torch.float32, E), _ptr(dX), _ptr(dW), ws, ws_bytes, _stream()),
         "bitlinear_backward_ste_experts")
     return dX, dW
@@ -658,7 +668,8 @@ def bitlinear_quant_nonlinear(U: torch.Tensor, fn: str = "gelu", ln_eps: float =
     rowsum = torch.empty(M, dtype=torch.int32, device=dev)
     check = torch.empty((M, K), dtype=torch.int8, device=dev) if checkpoint else None
     scale = torch.empty((M, (K + 127) // 128), dtype=torch.float32, device=dev) if checkpoint else None
-    ws, ws_bytes, _keep = _scratch(workspace_bytes_experts(OP_QUANT_NONLINEAR, M, 1, 0, 0, 0, per_tensor), workspace, dev)
+    need = workspace_bytes_experts(OP_QUANT_NONLINEAR, M, 1, 0, 0, 0, True) if per_tensor else 0
+    ws, ws_bytes, _keep = _scratch(need, workspace, dev)
     _check(lib.bitlinear_quant_nonlinear(
         _ptr(U, torch.float32), M, K, _function(fn), ln_eps, None if rows is None else _given(dev, rows, torch.int32, 1),
         _gran(per_tensor), codes.data_ptr(), gamma.data_ptr(), rowsum.data_ptr(), _ptr(check), _ptr(scale), ws, ws_bytes,

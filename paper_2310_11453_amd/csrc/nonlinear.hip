@@ -20,10 +20,19 @@ namespace bl {
 enum Fn { kRelu = 0, kRelu2 = 1, kGelu = 2, kSilu = 3 };
 enum RowMode { kOnce = 0, kRowStats = 1, kRowApply = 2 };
 
-// f(u) and f'(u).  GELU: Phi(u) = (1 + erf(z)) / 2, z = u / sqrt 2, with erf as in Abramowitz and Stegun 7.1.26 (erf z =
-// 1 - (a1 t + ... + a5 t^5) e^(-z^2), t = 1 / (1 + p z), z >= 0: off by at most 1.5e-7), which shares its exponential
-// with f'.  The hardware's exponential and reciprocal are off by an ulp.  (Passes over 16384 x 8192 with the library's
-// erff and expf / so: forward, gamma per tensor, 362 / 314 us, backward 455 / 219.)
+// f(u) of the forward, whose codes are decided next to a border: the library's functions, an ulp or so off.
+template <int FN>
+__device__ inline float fn_value(float u) {
+    if constexpr (FN == kRelu) return u > 0.f ? u : 0.f;
+    else if constexpr (FN == kRelu2) return u > 0.f ? u * u : 0.f;
+    else if constexpr (FN == kGelu) return 0.5f * u * (1.f + erff(u * 0.70710678118654752f));
+    else return u / (1.f + expf(-u));
+}
+// f(v) and f'(v) of the backward, where they are factors of a gradient.  GELU: Phi(u) = (1 + erf(z)) / 2, z = u / sqrt 2,
+// with erf as in Abramowitz and Stegun 7.1.26 (erf z = 1 - (a1 t + ... + a5 t^5) e^(-z^2), t = 1 / (1 + p z), z >= 0: off
+// by at most 1.5e-7), which shares its exponential with f'.  The hardware's exponential and reciprocal are off by an ulp.
+// (16384 x 8192 with the library's erff and expf 455 us, 219 so.  The forward would gain 14 %, and a code in a million
+// fall on the other side of a border.)
 struct FnPair {
     float value, slope;
 };
@@ -48,9 +57,6 @@ __device__ inline FnPair fn_pair(float u) {
         return {u * s, fmaf(u * s, 1.f - s, s)};
     }
 }
-template <int FN>
-__device__ inline float fn_value(float u) { return fn_pair<FN>(u).value; }
-
 // the largest value of 32 lanes, one half of a wave
 __device__ inline float half_wave_max(float v) {
     v = max_raw(v, dpp_mov<0xB1>(v));
@@ -239,7 +245,7 @@ __global__ __launch_bounds__((WPR < 4 ? 4 : WPR) * kWave) void nonlinear_backwar
         sc[j] = scales[(uint32_t)at >> 5];
     }
     // sums about an element of the row, so that a large common offset costs nothing
-    const double c = (double)fn_value<FN>((float)(int8_t)c4[0] * scales[0]);
+    const double c = (double)fn_pair<FN>((float)(int8_t)c4[0] * scales[0]).value;
     auto pairs = [](uint32_t codes, float scale, float4& value, float4& slope) {
         const FnPair x = fn_pair<FN>((float)(int8_t)codes * scale), y = fn_pair<FN>((float)(int8_t)(codes >> 8) * scale);
         const FnPair z = fn_pair<FN>((float)(int8_t)(codes >> 16) * scale), w = fn_pair<FN>((float)(int8_t)(codes >> 24) * scale);
