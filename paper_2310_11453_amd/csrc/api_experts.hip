@@ -112,6 +112,7 @@ int bitlinear_backward_ste_experts(const void* dY, int64_t M, int top_k, int64_t
     if (!dY || !gamma || !offsets) return BL_ERR_NULL;
     if (dX && (!packed || !beta)) return BL_ERR_NULL;
     if (dW && !codes) return BL_ERR_NULL;
+    if (dX && experts_dy_direct(N) && ((uintptr_t)dY & 15)) return BL_ERR_UNSUPPORTED;  // read 16 bytes at a time
     if (!workspace || workspace_bytes < experts_backward_bytes(M * top_k, N, K, experts) + 256) return BL_ERR_WORKSPACE;
     ExpertsArgs a = experts_args(codes, gamma, M, top_k, N, K, order, offsets, experts, packed, beta, granularity);
     a.dY = (const uint16_t*)dY; a.dX = dX; a.dW = dW;

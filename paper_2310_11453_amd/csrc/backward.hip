@@ -264,6 +264,8 @@ struct RingSlices {
 struct ExpertsRing {
     const int32_t* offsets;
     int E, T, least;
+    uint32_t a_pitch;  // dX: bytes from a row of A to the next, and from a stage to the next
+    int64_t a_step;
 };
 
 // ---- C[I][J] = scale * sum_r A[I][r] B[J][r], bf16 operands, fp32 accumulation -----------------
@@ -678,9 +680,9 @@ __global__ __launch_bounds__(512, BM == 256 ? 2 : 4) void gemm_tn_signs_ring(con
             int row = slot >> 2;
             const int seg = ((slot & 3) ^ ((row >> 2) & 3)) * 16;
             if (i0 + row > (EXP ? end : I) - 1) row = (int)((EXP ? end : I) - 1 - i0);
-            goffA[q] = (uint32_t)row * 64 + seg;
+            goffA[q] = (uint32_t)row * (EXP ? ex.a_pitch : 64u) + seg;
         }
-        baseA = reinterpret_cast<const uint8_t*>(A) + (st0 * I + i0) * 64;
+        baseA = reinterpret_cast<const uint8_t*>(A) + (EXP ? i0 * ex.a_pitch + st0 * ex.a_step : (st0 * I + i0) * 64);
         int64_t col = j0 + wn * WTN + l;  // columns past J re-read the last one (never stored)
         if (col > J - 1) col = J - 1;
         wsrc = Sw + ((EXP ? (int64_t)expert * nst_all : 0) + st0) * J + col;
@@ -700,7 +702,7 @@ __global__ __launch_bounds__(512, BM == 256 ? 2 : 4) void gemm_tn_signs_ring(con
 #pragma unroll
         for (int q = 0; q < PA; ++q)
             __builtin_amdgcn_global_load_lds(
-                (const void*)(baseA + src_st * I * 64 + goffA[q]),
+                (const void*)(baseA + src_st * (EXP ? ex.a_step : I * 64) + goffA[q]),
                 (__attribute__((address_space(3))) void*)(dst + q * THREADS * 16), 16, 0, 0);
     };
     auto issue_tile_start = [&]() {
@@ -1210,7 +1212,8 @@ ExpertsBackwardPlan experts_backward_plan(int64_t T, int64_t N, int64_t K, int E
 
 void launch_experts_dx(const ExpertsOperands& a, const ExpertsBackwardPlan& p, hipStream_t s) {
     const int64_t Np = pad32(a.N), nst = Np / 32, bm = p.dx_tile == 1 ? 256 : 128, gj = (a.K + 255) / 256;
-    const ExpertsRing ex{a.offsets, a.E, (int)a.T, 0};
+    const ExpertsRing ex = a.direct ? ExpertsRing{a.offsets, a.E, (int)a.T, 0, (uint32_t)(a.N * 2), 64}
+                                    : ExpertsRing{a.offsets, a.E, (int)a.T, 0, 64, a.T * 64};
     const int64_t most = most_tiles(a.T, a.E, (int)bm, 0) * gj, cap = (int64_t)ring_cus() * (bm == 256 ? 1 : 2);
     const int64_t per = (nst + p.dx_splits - 1) / p.dx_splits;
     const RingSlices sl{(int)((nst + per - 1) / per), (int)per};
@@ -1229,7 +1232,7 @@ void launch_experts_dx(const ExpertsOperands& a, const ExpertsBackwardPlan& p, h
 
 void launch_experts_dw(const ExpertsOperands& a, const ExpertsBackwardPlan& p, hipStream_t s) {
     const int64_t T = p.dw_tile == 1 ? 256 : 128, gi = (a.N + T - 1) / T, gj = (a.K + T - 1) / T;
-    const ExpertsRing ex{a.offsets, a.E, (int)a.T, a.least};
+    const ExpertsRing ex{a.offsets, a.E, (int)a.T, a.least, 0, 0};
     const RingSlices sl{p.dw_splits, 0};
     const int64_t items = gi * gj * a.E * sl.splits, cap = (int64_t)ring_cus() * (T == 256 ? 1 : 2);
     const unsigned grid = (unsigned)(items < cap ? items : cap);

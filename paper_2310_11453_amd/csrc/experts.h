@@ -82,11 +82,12 @@ struct ExpertsArgs {
 hipError_t launch_matmul_experts(const ExpertsArgs& a, hipStream_t s);
 
 // backward.hip: the two products of the backward from the copies that experts_backward.hip makes of their operands.
-// Reduction indices in blocks of 32 as there (block_offset): g [T rows][Np], Sw [E][Np / 32][K]; gwT [N rows] and qT [K
+// Reduction indices in blocks of 32 as there (block_offset): g [T rows][Np] (direct: dY itself, by rows), Sw [E][Np / 32][K]; gwT [N rows] and qT [K
 // rows] over the slots of expert after expert, each expert's filled up with zeros to whole blocks and to `least` of them.
 struct ExpertsOperands {
     const uint16_t *g, *gwT, *qT;
     const uint32_t* Sw;
+    bool direct;
     const int32_t* offsets;
     int E, least;
     int64_t T, N, K;
@@ -99,6 +100,8 @@ struct ExpertsBackwardPlan {
 ExpertsBackwardPlan experts_backward_plan(int64_t T, int64_t N, int64_t K, int E);
 void launch_experts_dx(const ExpertsOperands& a, const ExpertsBackwardPlan& p, hipStream_t s);
 void launch_experts_dw(const ExpertsOperands& a, const ExpertsBackwardPlan& p, hipStream_t s);
+// dX reads dY where it lies; else a copy in whole stages of 32 columns is made.
+inline bool experts_dy_direct(int64_t N) { return N % 32 == 0 && N < (1 << 23); }
 size_t experts_backward_bytes(int64_t T, int64_t N, int64_t K, int E);
 hipError_t launch_experts_backward(const ExpertsArgs& a, hipStream_t s);
 

@@ -3,7 +3,9 @@
 //   dW_e[n,k] = sum_{s of e} dY[s,n] q[r,k] gamma_r/128    r the row that s reads; zeros where e has no slots
 // dY is bf16, +-1 and the codes are exact in bf16.  As in the plain layer (backward.hip, whose kernels take the products),
 // every operand is first written once in the layout they read:
-//   g    [T][Np]       rows of dY                                 (A operand of dX, reduction over N)
+//   g    [T][Np]       rows of dY                                 (A operand of dX, reduction over N; not where N is a
+//                      multiple of 32: the product reads dY itself, at the same speed, and the copies for 8192 slots 2048 ->
+//                      8192 take 86 us instead of 105)
 //   Sw   [E][Np/32][K] the signs of 32 weight rows of a column    (B operand of dX)
 //   gwT  [N][slots]    dY transposed, with a gamma per token scaled and rounded again   (A operand of dW)
 //   qT   [K][slots]    codes transposed, gathered through the order                     (B operand of dW)
@@ -189,7 +191,7 @@ ExpertsWs experts_ws(int64_t T, int64_t N, int64_t K, int E, const ExpertsBackwa
     auto al = [](size_t v) { return (v + 255) & ~(size_t)255; };
     const int64_t Np = pad32(N), slots = most_tiles(T, E, 32, p.dw_splits) * 32;
     ExpertsWs w{};
-    w.words = al((size_t)T * Np * 2);
+    w.words = experts_dy_direct(N) ? 0 : al((size_t)T * Np * 2);
     w.gwT = w.words + al((size_t)E * (Np / 32) * K * 4);
     w.qT = w.gwT + al((size_t)N * slots * 2);
     w.part = w.qT + al((size_t)K * slots * 2);
@@ -215,7 +217,7 @@ hipError_t launch_experts_backward(const ExpertsArgs& a, hipStream_t s) {
     b.offsets = a.offsets; b.order = a.order; b.top_k = (uint32_t)a.top_k; b.rows = (uint32_t)a.rows;
     b.E = a.E; b.T = (int)a.T; b.least = p.dw_splits;
     if (a.dX) {
-        b.g = (uint16_t*)base;
+        b.g = experts_dy_direct(a.N) ? nullptr : (uint16_t*)base;
         b.Sw = (uint32_t*)(base + ws.words);
     }
     if (a.dW) {
@@ -231,7 +233,7 @@ hipError_t launch_experts_backward(const ExpertsArgs& a, hipStream_t s) {
     b.code_x = (uint32_t)tiles(a.K);
     b.dy_x = (uint32_t)tiles(b.g ? b.Np : b.N);
     const int64_t bits = a.dX ? (int64_t)a.E * b.bits_y * b.bits_x : 0, codes = a.dW ? rows * b.code_x : 0;
-    const int64_t items = bits + codes + rows * b.dy_x;
+    const int64_t items = bits + codes + (b.g || b.gwT ? rows * b.dy_x : 0);
     if (items >= (int64_t)1 << 32) return hipErrorInvalidValue;
     b.bits_items = (uint32_t)bits;
     b.code_items = (uint32_t)codes;
@@ -240,7 +242,8 @@ hipError_t launch_experts_backward(const ExpertsArgs& a, hipStream_t s) {
     if (a.N % 8 == 0 && ((uintptr_t)a.dY & 15) == 0) prepare_expert_operands<true><<<grid, 256, 0, s>>>(b);
     else prepare_expert_operands<false><<<grid, 256, 0, s>>>(b);
 
-    ExpertsOperands o{b.g, b.gwT, b.qT, b.Sw, a.offsets, a.E, b.least, a.T, a.N, a.K, a.beta,
+    const bool direct = experts_dy_direct(a.N);
+    ExpertsOperands o{direct ? a.dY : b.g, b.gwT, b.qT, b.Sw, direct, a.offsets, a.E, b.least, a.T, a.N, a.K, a.beta,
                       a.per_tensor ? a.gamma : nullptr, a.dX, a.dW, (float*)(base + ws.part)};
     if (a.dX) launch_experts_dx(o, p, s);
     if (a.dW) launch_experts_dw(o, p, s);
