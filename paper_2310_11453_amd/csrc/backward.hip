@@ -266,7 +266,33 @@ struct ExpertsRing {
     int E, T, least;
     uint32_t a_pitch;  // dX: bytes from a row of A to the next, and from a stage to the next
     int64_t a_step;
+    float* part;  // dX: room for a tile of every workgroup; slices (0, 1: none) of a tile at most
+    int slices;
 };
+
+// dX of a mixture.  An XCD's G / 8 workgroups take a contiguous range of the tiles (the ranges differ by one), round after
+// round; the tiles of the last, partial round are cut along the reduction where that fills the XCD, each slice's sum going
+// to the workgroup's place in `part` for fold_expert_tails.  Few tiles are a partial round too.
+struct TailPlan {
+    int first, full, tail, n;  // tiles in whole rounds, behind them, and the slices of each of those
+};
+__device__ inline TailPlan tail_plan(int tiles, int x, int S, int stages, int slices) {
+    TailPlan p;
+    p.first = (int)((int64_t)tiles * x / 8);
+    const int len = (int)((int64_t)tiles * (x + 1) / 8) - p.first;
+    p.full = len / S * S;
+    p.tail = len - p.full;
+    p.n = 1;
+    // Twice the slices while that saves more than their sums cost to write and read: with n of them 0.39 us a stage and
+    // 1 / n against 0.42 us for each of an XCD's tails and n (128 x 256 tiles; 256 x 256 0.62 and 0.84).  666 slots of 4
+    // experts 1024 -> 4096 take 67 us in 16 slices, 51 in 4.  Two would gain what a CU's second workgroup is worth.
+    if (p.tail > 0)
+        while (2 * p.n <= slices && 2 * p.n * p.tail <= S && stages >= 16 * p.n &&
+               5 * stages > 12 * p.tail * p.n * p.n)
+            p.n *= 2;
+    if (p.n < 4) p.n = 1;
+    return p;
+}
 
 // ---- C[I][J] = scale * sum_r A[I][r] B[J][r], bf16 operands, fp32 accumulation -----------------
 // Workgroup tile T x T, four waves of T/2 x T/2, persistent over the tiles.  T = 256: 4 x 4 MFMA tiles a
@@ -629,31 +655,35 @@ __global__ __launch_bounds__(512, BM == 256 ? 2 : 4) void gemm_tn_signs_ring(con
     if constexpr (EXP) grid_i = expert_tiles(ex.offsets, ex.E, ex.T, BM, smE);
     const int nitems = grid_i * grid_j * (SPLIT ? sl.splits : 1);
     int expert = 0;   // of the tile whose origin was asked for last,
-    int64_t end = 0;  // whose rows end here
+    int64_t end = 0;  // whose rows end here,
+    int slice = -1;   // and where its sum goes (-1: to C)
     int nst = nst_all;  // stages of the current work item, the first one st0 (SPLIT)
     int st0 = 0;
     int main_groups = nst >= 2 * NS - 1 ? (nst - (2 * NS - 1)) / NS + 1 : 0;
 
     auto tile_origin = [&](int t, int64_t& i0, int64_t& j0) {
         if constexpr (EXP) {
-            // a contiguous range of the tiles for each XCD (their numbers differ by one); slices of a tile in turn
-            int logical = t;
-            if constexpr (SPLIT) {
-                logical = t < nitems ? t / sl.splits : -1;
-            } else if ((gridDim.x & 7) == 0) {
-                const int G = (int)gridDim.x, x = t & 7, q = ((t % G) >> 3) + (t / G) * (G >> 3);
-                logical = (int)((int64_t)nitems * x / 8) + q;
-                if (logical >= (int)((int64_t)nitems * (x + 1) / 8)) logical = -1;
-            } else if (t >= nitems) {
-                logical = -1;
-            }
             i0 = j0 = -1;
-            if (logical < 0) return;
+            slice = -1;
+            const int G = (int)gridDim.x, S = G >> 3, x = t & 7, q = ((t % G) >> 3) + (t / G) * S;  // G % 8 == 0
+            const TailPlan p = tail_plan(nitems, x, S, nst_all, ex.slices);
+            const int k = q - p.full;
+            int tile = p.first + q;
+            if (k >= p.tail * p.n) return;
+            st0 = 0;
+            nst = nst_all;
+            if (k >= 0 && p.n > 1) {
+                tile = p.first + p.full + k / p.n;
+                slice = x * S + k;  // the workgroup's place
+                st0 = nst_all * (k % p.n) / p.n;
+                nst = nst_all * (k % p.n + 1) / p.n - st0;
+            }
+            main_groups = nst >= 2 * NS - 1 ? (nst - (2 * NS - 1)) / NS + 1 : 0;
             int from, to;
-            expert = expert_of_tile(smE, ex.E, logical / grid_j, BM, from, to);
+            expert = expert_of_tile(smE, ex.E, tile / grid_j, BM, from, to);
             i0 = from;
             end = to;
-            j0 = (int64_t)(logical % grid_j) * BN;
+            j0 = (int64_t)(tile % grid_j) * BN;
         } else if constexpr (SPLIT) {
             const int tile = t / sl.splits;
             i0 = (int64_t)(tile / grid_j) * BM;
@@ -796,7 +826,7 @@ __global__ __launch_bounds__(512, BM == 256 ? 2 : 4) void gemm_tn_signs_ring(con
     setup_dma(i0, j0);
     issue_tile_start();
 
-    int current = expert;
+    int current = expert, place = slice;
     int64_t rows_end = end;
     while (true) {
 #pragma unroll
@@ -838,9 +868,11 @@ __global__ __launch_bounds__(512, BM == 256 ? 2 : 4) void gemm_tn_signs_ring(con
             const int64_t ib = i0 + __builtin_amdgcn_readfirstlane(wm * WTM);
             const int64_t jb = j0 + __builtin_amdgcn_readfirstlane(wn * WTN);
             const float sc = EXP ? scale_ptr[current] : scale;  // EXP: the expert's, in every slice
-            store_tile<MI, NI, true>(Cs + ib * J + jb, J, (EXP ? rows_end : I) - ib, J - jb, j, g2, [](int, int) {},
+            const bool apart = EXP && place >= 0;  // a whole tile, rows of 256
+            float* const at = apart ? ex.part + (int64_t)place * BM * BN + (ib - i0) * BN + (jb - j0) : Cs + ib * J + jb;
+            store_tile<MI, NI, true>(at, apart ? BN : J, apart ? BM : (EXP ? rows_end : I) - ib, apart ? BN : J - jb, j, g2, [](int, int) {},
                                [&](int mi, int r, int s) { return sc * acc[mi][s][r]; });
-            if constexpr (EXP) current = expert, rows_end = end;
+            if constexpr (EXP) current = expert, rows_end = end, place = slice;
         }
         if (i0n < 0) break;
         t = t_next;
@@ -1123,23 +1155,43 @@ hipError_t launch_backward(const BackwardArgs& a, hipStream_t s) {
 }
 
 // ---- mixtures of experts ------------------------------------------------------------------------------
-// out[r] = slice 0 + slice 1 + ..., rows behind the last slot left alone
-template <bool VEC>
-__global__ __launch_bounds__(256) void fold_expert_rows(const float* __restrict__ part, int splits, int64_t T, int64_t J,
-                                                        const int32_t* __restrict__ end, float* __restrict__ out) {
-    constexpr int E = VEC ? 4 : 1;
-    const int64_t used = (*end < 0 ? 0 : *end < T ? *end : T) * J;
-    for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * E; i < used; i += (int64_t)gridDim.x * 256 * E) {
-        if constexpr (VEC) {
-            v4f v = *reinterpret_cast<const v4f*>(part + i);
-#pragma unroll 4
-            for (int s = 1; s < splits; ++s) v += *reinterpret_cast<const v4f*>(part + s * T * J + i);
-            *reinterpret_cast<v4f*>(out + i) = v;
-        } else {
-            float v = part[i];
-            for (int s = 1; s < splits; ++s) v += part[s * T * J + i];
-            out[i] = v;
+// dX of the tiles that gemm_tn_signs_ring cut (tail_plan): the slices' sums added in the order 0, 1, ...  Whether there are
+// any is known here only, so the grid is small and its workgroups take 1024 elements of a tile in turn; a thread has all
+// its slices' loads in flight.
+template <int BM>
+__global__ __launch_bounds__(256) void fold_expert_tails(ExpertsRing ex, int S, int stages, int grid_j, int64_t J,
+                                                         float* __restrict__ C) {
+    constexpr int BN = 256, PIECES = BM / 4;
+    __shared__ ExpertTiles count;
+    const int tiles = expert_tiles(ex.offsets, ex.E, ex.T, BM, count) * grid_j;
+    int item = (int)blockIdx.x;
+    for (int x = 0; x < 8; ++x) {
+        const TailPlan p = tail_plan(tiles, x, S, stages, ex.slices);
+        const int items = p.n > 1 ? p.tail * PIECES : 0;
+        for (; item < items; item += (int)gridDim.x) {
+            const int i = item / PIECES, tile = p.first + p.full + i;
+            int from, to;
+            expert_of_tile(count, ex.E, tile / grid_j, BM, from, to);
+            const int r = item % PIECES * 4 + (int)(threadIdx.x >> 6), c = (int)(threadIdx.x & 63) * 4;
+            const int64_t col = (int64_t)(tile % grid_j) * BN + c;
+            if (from + r >= to || col >= J) continue;  // J % 32 == 0
+            const float* const src = ex.part + ((int64_t)x * S + (int64_t)i * p.n) * BM * BN + r * BN + c;
+            auto sum = [&](auto slices) {
+                constexpr int N = decltype(slices)::value;
+                v4f v[N];
+#pragma unroll
+                for (int k = 0; k < N; ++k) v[k] = *reinterpret_cast<const v4f*>(src + (int64_t)k * BM * BN);
+#pragma unroll
+                for (int k = 1; k < N; ++k) v[0] += v[k];
+                float* const dst = C + (int64_t)(from + r) * J + col;
+                if (((uintptr_t)C & 15) == 0) *reinterpret_cast<v4f*>(dst) = v[0];
+                else dst[0] = v[0][0], dst[1] = v[0][1], dst[2] = v[0][2], dst[3] = v[0][3];
+            };
+            if (p.n == 4) sum(std::integral_constant<int, 4>{});
+            else if (p.n == 8) sum(std::integral_constant<int, 8>{});
+            else sum(std::integral_constant<int, 16>{});
         }
+        item -= items;
     }
 }
 // dW of every expert; zeros where it has no slots, whatever gamma is
@@ -1167,72 +1219,82 @@ __global__ __launch_bounds__(256) void fold_expert_weights(const float* __restri
     }
 }
 
-// The tiles and slices that cost least, by the costs in us that the plain layer's plans take.  How the slots fall on the
-// experts is not known here: an expert's last row of tiles is taken to be half full, its reduction of average length.
+// The tiles that cost least, by the costs in us that the plain layer's plans take, and the slices of dW.  How the slots fall
+// on the experts is not known here: an expert's last row of tiles is taken to be half full, its reduction of average
+// length.
 ExpertsBackwardPlan experts_backward_plan(int64_t T, int64_t N, int64_t K, int E) {
     constexpr RingCost kDxWide{0.615, 12.0, 5.0, 6.0}, kDxRows{0.33, 5.0, 5.0, 6.0}, kDxAlone{0.39, 2.0, 5.0, 6.0};
     constexpr RingCost kDwWide{0.68, 12.8, 5.0, 6.0}, kDwSmall{0.172, 2.3, 5.0, 6.0}, kDwAlone{0.226, 3.6, 5.0, 6.0};
     const Tuning& t = tuning();
     const double cus = ring_cus(), A = (double)(T < E ? T : E);
     auto tiles_of = [](int64_t v, int64_t b) { return (double)((v + b - 1) / b); };
-    auto us = [&](RingCost c, double tiles, double stages, int n, double bytes, double unsure) {
-        double rounds = tiles * n / cus + unsure;
-        if (rounds < 1.0) rounds = 1.0;
-        return rounds * (c.stage * stages / n + c.item) + (n > 1 ? c.fold + n * bytes * 2e-6 / c.rate : 0.0);
-    };
+    const int force = t.bwd_splits < 0 ? 0 : t.bwd_splits < 16 ? t.bwd_splits : 16;
+    const double nst = tiles_of(N, 32), rst = (double)T / 32.0 / E + 0.5;
     ExpertsBackwardPlan p{1, 1, 1, 1};
     double dx_us = 1e30, dw_us = 1e30;
-    const double nst = tiles_of(N, 32), rst = (double)T / 32.0 / E + 0.5;
+    for (int tile = 1; tile <= 2; ++tile) {
+        const bool wide = tile == 1;
+        if (t.bwd_dx && t.bwd_dx != tile) continue;
+        const double rows = (double)T / (wide ? 256 : 128) + 0.5 * A, slots = wide ? cus : 2.0 * cus;
+        const double tiles = (rows > 0.9 * A ? rows : 0.9 * A) * tiles_of(K, 256);
+        const double whole = (double)(int64_t)(tiles / slots), tail = tiles - whole * slots;
+        // Slices of the last round's tiles cost a launch, 4.5 us, also where the device finds nothing to cut: few tiles, or
+        // more than a round of long ones (a quarter of the rounds end so, and save most of 0.39 us a stage then).
+        const bool cut = force ? force > 1 : tiles < 0.3 * slots ? nst >= 32 && 5 * nst > 6 * tiles
+                                                                         : tiles > 0.9 * slots && nst >= 96;
+        int n = 1;  // as tail_plan does
+        while (cut && n < 16 && 2 * n * tail <= slots && nst >= 16 * n && 5 * nst > 1.5 * tail * n * n) n *= 2;
+        if (n < 4) n = 1;
+        const RingCost round = wide ? kDxWide : kDxRows, last = wide ? kDxWide : tail * n > cus ? kDxRows : kDxAlone;
+        const double per_slot = wide ? 1.0 : 2.0;
+        const double v = whole * per_slot * (round.stage * nst + round.item) +
+                         (wide || tail * n <= cus ? 1.0 : 2.0) * (last.stage * nst / n + last.item) +
+                         (n > 1 ? 5.0 + (wide ? 0.1 : 0.05) * tail * n : 0.0);
+        if (v < dx_us) dx_us = v, p.dx_tile = tile, p.dx_slices = !cut ? 1 : force ? force : 16;
+    }
     for (int tile = 1; tile <= 2; ++tile)
         for (int n = 1; n <= 16; n *= 2) {
             const bool wide = tile == 1;
-            if ((!t.bwd_dx || t.bwd_dx == tile) && (n == 1 || nst >= 8 * n)) {
-                const double rows = (double)T / (wide ? 256 : 128) + 0.5 * A;
-                const double tiles = (rows > 0.9 * A ? rows : 0.9 * A) * tiles_of(K, 256);
-                const RingCost c = wide ? kDxWide : tiles * n > cus ? kDxRows : kDxAlone;
-                const double v = us(c, tiles, nst, n, (double)T * (double)K * 4.0, 0.4);
-                if (v < dx_us) dx_us = v, p.dx_tile = tile, p.dx_splits = n;
-            }
-            if ((!t.bwd_ring || t.bwd_ring == tile) && (n == 1 || rst >= 8 * n)) {
-                const double tiles = E * tiles_of(N, wide ? 256 : 128) * tiles_of(K, wide ? 256 : 128);
-                const RingCost c = wide ? kDwWide : tiles * n > cus ? kDwSmall : kDwAlone;
-                // operands that do not stay in the 256 MB cache cost the small tiles, which read them more often, more (8192
-                // slots of 8 experts 2048 -> 8192, 168 MB: 657 in the large ones, 698; half the slots 410 / 384)
-                const double more = !wide && (double)(N + K) * (double)T * 2.0 > 1.4e8 ? 1.2 : 1.0;
-                const double v = us(c, tiles, more * rst, n, (double)E * (double)N * (double)K * 4.0, 0.2);
-                if (v < dw_us) dw_us = v, p.dw_tile = tile, p.dw_splits = n;
-            }
+            if ((t.bwd_ring && t.bwd_ring != tile) || (n > 1 && rst < 8 * n)) continue;
+            const double tiles = E * tiles_of(N, wide ? 256 : 128) * tiles_of(K, wide ? 256 : 128);
+            const RingCost c = wide ? kDwWide : tiles * n > cus ? kDwSmall : kDwAlone;
+            // operands that do not stay in the 256 MB cache cost the small tiles, which read them more often, more (8192
+            // slots of 8 experts 2048 -> 8192, 168 MB: 657 in the large ones, 698; half the slots 410 / 384)
+            const double more = !wide && (double)(N + K) * (double)T * 2.0 > 1.4e8 ? 1.2 : 1.0;
+            const double rounds = tiles * n / cus + 0.2, bytes = (double)E * (double)N * (double)K * 4.0;
+            const double v = (rounds < 1.0 ? 1.0 : rounds) * (c.stage * more * rst / n + c.item) +
+                             (n > 1 ? c.fold + n * bytes * 2e-6 / c.rate : 0.0);
+            if (v < dw_us) dw_us = v, p.dw_tile = tile, p.dw_splits = n;
         }
-    if (t.bwd_splits > 0) {
-        p.dx_splits = p.dw_splits = t.bwd_splits < 16 ? t.bwd_splits : 16;
-        if (p.dx_splits > nst) p.dx_splits = (int)nst;
-    }
+    if (force) p.dw_splits = force;
     return p;
 }
 
+// Workgroups of dX: a multiple of the XCDs, enough for the slices of few tiles.
+static int dx_grid(int64_t T, int64_t K, int E, const ExpertsBackwardPlan& p) {
+    const int64_t bm = p.dx_tile == 1 ? 256 : 128, cap = (int64_t)ring_cus() * (bm == 256 ? 1 : 2);
+    const int64_t most = most_tiles(T, E, (int)bm, 0) * ((K + 255) / 256) * p.dx_slices;
+    return (int)((most < cap ? most : cap) + 7) / 8 * 8;
+}
+size_t experts_dx_part_bytes(int64_t T, int64_t K, int E, const ExpertsBackwardPlan& p) {
+    return p.dx_slices > 1 ? (size_t)dx_grid(T, K, E, p) * (p.dx_tile == 1 ? 256 : 128) * 256 * 4 : 0;
+}
+
 void launch_experts_dx(const ExpertsOperands& a, const ExpertsBackwardPlan& p, hipStream_t s) {
-    const int64_t Np = pad32(a.N), nst = Np / 32, bm = p.dx_tile == 1 ? 256 : 128, gj = (a.K + 255) / 256;
-    const ExpertsRing ex = a.direct ? ExpertsRing{a.offsets, a.E, (int)a.T, 0, (uint32_t)(a.N * 2), 64}
-                                    : ExpertsRing{a.offsets, a.E, (int)a.T, 0, 64, a.T * 64};
-    const int64_t most = most_tiles(a.T, a.E, (int)bm, 0) * gj, cap = (int64_t)ring_cus() * (bm == 256 ? 1 : 2);
-    const int64_t per = (nst + p.dx_splits - 1) / p.dx_splits;
-    const RingSlices sl{(int)((nst + per - 1) / per), (int)per};
-    const int64_t items = most * sl.splits;
-    const unsigned grid = (unsigned)(items < cap ? items : cap);
-    const bool cut = sl.splits > 1;
-    const auto kernel = cut ? (bm == 256 ? gemm_tn_signs_ring<256, 4, true, true> : gemm_tn_signs_ring<128, 4, true, true>)
-                            : (bm == 256 ? gemm_tn_signs_ring<256, 4, false, true> : gemm_tn_signs_ring<128, 4, false, true>);
-    kernel<<<grid, 512, 0, s>>>(a.g, a.Sw, a.T, a.K, Np, a.beta, 1.0f, cut ? a.part : a.dX, 0, (int)gj, 0, 0, sl, ex);
-    if (!cut) return;
-    const bool vec = ((uintptr_t)a.dX & 15) == 0;  // K % 32 == 0
-    const int64_t wide = (a.T * a.K / (vec ? 4 : 1) + 255) / 256;
-    const auto fold = vec ? fold_expert_rows<true> : fold_expert_rows<false>;
-    fold<<<(unsigned)(wide < 8192 ? wide : 8192), 256, 0, s>>>(a.part, sl.splits, a.T, a.K, a.offsets + a.E, a.dX);
+    const int64_t Np = pad32(a.N), nst = Np / 32, gj = (a.K + 255) / 256;
+    ExpertsRing ex{a.offsets, a.E, (int)a.T, 0, 64, a.T * 64, a.part, p.dx_slices};
+    if (a.direct) ex.a_pitch = (uint32_t)(a.N * 2), ex.a_step = 64;
+    const int grid = dx_grid(a.T, a.K, a.E, p), S = grid / 8;
+    const auto kernel = p.dx_tile == 1 ? gemm_tn_signs_ring<256, 4, false, true> : gemm_tn_signs_ring<128, 4, false, true>;
+    kernel<<<(unsigned)grid, 512, 0, s>>>(a.g, a.Sw, a.T, a.K, Np, a.beta, 1.0f, a.dX, 0, (int)gj, 0, 0, {}, ex);
+    if (p.dx_slices < 4 || S < 4 || nst < 32) return;  // tail_plan cuts nothing
+    const auto fold = p.dx_tile == 1 ? fold_expert_tails<256> : fold_expert_tails<128>;
+    fold<<<512, 256, 0, s>>>(ex, S, (int)nst, (int)gj, a.K, a.dX);
 }
 
 void launch_experts_dw(const ExpertsOperands& a, const ExpertsBackwardPlan& p, hipStream_t s) {
     const int64_t T = p.dw_tile == 1 ? 256 : 128, gi = (a.N + T - 1) / T, gj = (a.K + T - 1) / T;
-    const ExpertsRing ex{a.offsets, a.E, (int)a.T, a.least, 0, 0};
+    const ExpertsRing ex{a.offsets, a.E, (int)a.T, a.least, 0, 0, nullptr, 0};
     const RingSlices sl{p.dw_splits, 0};
     const int64_t items = gi * gj * a.E * sl.splits, cap = (int64_t)ring_cus() * (T == 256 ? 1 : 2);
     const unsigned grid = (unsigned)(items < cap ? items : cap);

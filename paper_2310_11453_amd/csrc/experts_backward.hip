@@ -196,7 +196,7 @@ ExpertsWs experts_ws(int64_t T, int64_t N, int64_t K, int E, const ExpertsBackwa
     w.qT = w.gwT + al((size_t)N * slots * 2);
     w.part = w.qT + al((size_t)K * slots * 2);
     // one product after the other
-    const size_t dx = p.dx_splits > 1 ? (size_t)p.dx_splits * T * K * 4 : 0;
+    const size_t dx = experts_dx_part_bytes(T, K, E, p);
     const size_t dw = p.dw_splits > 1 ? (size_t)p.dw_splits * E * N * K * 4 : 0;
     w.total = w.part + (dx > dw ? dx : dw);
     return w;

@@ -198,12 +198,32 @@ def test_backward(bl, M, top_k, E, K, N, gather, per_tensor):
 @pytest.mark.parametrize("spec", ["bwd_dx=1,bwd_ring=1", "bwd_dx=2,bwd_ring=2", "bwd_dx=1,bwd_ring=1,bwd_splits=3",
                                   "bwd_dx=2,bwd_ring=2,bwd_splits=5", "bwd_dx=1,bwd_ring=2,bwd_grid=8",
                                   "bwd_dx=2,bwd_ring=1,bwd_grid=4", "bwd_splits=16,bwd_grid=8"])
-@pytest.mark.parametrize("M,top_k,E,K,N", [(5, 3, 4, 544, 33), (130, 1, 2, 160, 130), (700, 2, 5, 288, 520)])
+@pytest.mark.parametrize("M,top_k,E,K,N", [(5, 3, 4, 544, 33), (130, 1, 2, 160, 130), (700, 2, 5, 288, 520),
+                                           (40, 2, 3, 544, 2080)])
 def test_backward_variants(bl, tuning, M, top_k, E, K, N, spec):
     print(f"backward M={M} top_k={top_k} E={E} K={K} N={N} {spec}", flush=True)
     tuning(spec)
     check_backward(bl, M, top_k, E, K, N, True, True, choices(M, top_k, E, M + K, unrouted=0.1))
     check_backward(bl, M, top_k, E, K, N, True, True, choices(M, top_k, E, M, only=[1]))
+
+
+# dX in whole rounds of workgroups and a last one whose tiles are cut into slices: the number of slots moves the last round
+# through nothing, a tile and more tiles than leave room for slices.  On integers, so exact.
+@pytest.mark.parametrize("M", [1, 129, 500, 1000, 1040, 1100, 1500, 1900, 2048])
+@pytest.mark.parametrize("spec", ["bwd_dx=2,bwd_grid=32", "bwd_dx=1,bwd_grid=64", "bwd_dx=2,bwd_grid=32,bwd_splits=4",
+                                  "bwd_dx=2,bwd_grid=32,bwd_splits=1", ""])
+def test_backward_dx_rounds(bl, tuning, M, spec):
+    print(f"backward dX rounds M={M} {spec}", flush=True)
+    tuning(spec)
+    top_k, E, K, N = 2, 3, 800, 2080
+    c = make(bl, M, top_k, E, K, N, True, True, choices(M, top_k, E, M, unrouted=0.05))
+    dY = torch.randint(-4, 5, (c["T"], N), generator=torch.Generator().manual_seed(1)).to(torch.bfloat16)
+    one = torch.ones(1, device="cuda")
+    dx, _ = bl.bitlinear_backward_ste_experts(dY.cuda(), c["codes"].cuda(), one, c["packed"], one.expand(E).contiguous(),
+                                              **c["calls"], want_dw=False)
+    for e in range(E):
+        mine = slice(c["offsets"][e], c["offsets"][e + 1])
+        assert torch.equal(dx[mine].cpu().double(), dY[mine].double() @ c["signs"][e].double())
 
 
 @pytest.mark.parametrize("only", [[0], [4]])
