@@ -868,10 +868,10 @@ __global__ __launch_bounds__(512, BM == 256 ? 2 : 4) void gemm_tn_signs_ring(con
             const int64_t ib = i0 + __builtin_amdgcn_readfirstlane(wm * WTM);
             const int64_t jb = j0 + __builtin_amdgcn_readfirstlane(wn * WTN);
             const float sc = EXP ? scale_ptr[current] : scale;  // EXP: the expert's, in every slice
-            const bool apart = EXP && place >= 0;  // a whole tile, rows of 256
+            const bool apart = EXP && place >= 0;  // rows of 256
             float* const at = apart ? ex.part + (int64_t)place * BM * BN + (ib - i0) * BN + (jb - j0) : Cs + ib * J + jb;
-            store_tile<MI, NI, true>(at, apart ? BN : J, apart ? BM : (EXP ? rows_end : I) - ib, apart ? BN : J - jb, j, g2, [](int, int) {},
-                               [&](int mi, int r, int s) { return sc * acc[mi][s][r]; });
+            store_tile<MI, NI, true>(at, apart ? BN : J, (EXP ? rows_end : I) - ib, apart ? BN : J - jb, j, g2,
+                               [](int, int) {}, [&](int mi, int r, int s) { return sc * acc[mi][s][r]; });
             if constexpr (EXP) current = expert, rows_end = end, place = slice;
         }
         if (i0n < 0) break;
@@ -1156,42 +1156,38 @@ hipError_t launch_backward(const BackwardArgs& a, hipStream_t s) {
 
 // ---- mixtures of experts ------------------------------------------------------------------------------
 // dX of the tiles that gemm_tn_signs_ring cut (tail_plan): the slices' sums added in the order 0, 1, ...  Whether there are
-// any is known here only, so the grid is small and its workgroups take 1024 elements of a tile in turn; a thread has all
-// its slices' loads in flight.
+// any is known here only, so the grid is small and its workgroups take 1024 elements of a tile in turn, those of the XCD
+// that wrote them; a thread has all its slices' loads in flight.
 template <int BM>
 __global__ __launch_bounds__(256) void fold_expert_tails(ExpertsRing ex, int S, int stages, int grid_j, int64_t J,
                                                          float* __restrict__ C) {
     constexpr int BN = 256, PIECES = BM / 4;
     __shared__ ExpertTiles count;
-    const int tiles = expert_tiles(ex.offsets, ex.E, ex.T, BM, count) * grid_j;
-    int item = (int)blockIdx.x;
-    for (int x = 0; x < 8; ++x) {
-        const TailPlan p = tail_plan(tiles, x, S, stages, ex.slices);
-        const int items = p.n > 1 ? p.tail * PIECES : 0;
-        for (; item < items; item += (int)gridDim.x) {
-            const int i = item / PIECES, tile = p.first + p.full + i;
-            int from, to;
-            expert_of_tile(count, ex.E, tile / grid_j, BM, from, to);
-            const int r = item % PIECES * 4 + (int)(threadIdx.x >> 6), c = (int)(threadIdx.x & 63) * 4;
-            const int64_t col = (int64_t)(tile % grid_j) * BN + c;
-            if (from + r >= to || col >= J) continue;  // J % 32 == 0
-            const float* const src = ex.part + ((int64_t)x * S + (int64_t)i * p.n) * BM * BN + r * BN + c;
-            auto sum = [&](auto slices) {
-                constexpr int N = decltype(slices)::value;
-                v4f v[N];
+    const int tiles = expert_tiles(ex.offsets, ex.E, ex.T, BM, count) * grid_j, x = (int)blockIdx.x & 7;
+    const TailPlan p = tail_plan(tiles, x, S, stages, ex.slices);
+    const int items = p.n > 1 ? p.tail * PIECES : 0;
+    for (int item = (int)blockIdx.x >> 3; item < items; item += (int)gridDim.x >> 3) {
+        const int i = item / PIECES, tile = p.first + p.full + i;
+        int from, to;
+        expert_of_tile(count, ex.E, tile / grid_j, BM, from, to);
+        const int r = item % PIECES * 4 + (int)(threadIdx.x >> 6), c = (int)(threadIdx.x & 63) * 4;
+        const int64_t col = (int64_t)(tile % grid_j) * BN + c;
+        if (from + r >= to || col >= J) continue;  // J % 32 == 0
+        const float* const src = ex.part + ((int64_t)x * S + (int64_t)i * p.n) * BM * BN + r * BN + c;
+        auto sum = [&](auto slices) {
+            constexpr int N = decltype(slices)::value;
+            v4f v[N];
 #pragma unroll
-                for (int k = 0; k < N; ++k) v[k] = *reinterpret_cast<const v4f*>(src + (int64_t)k * BM * BN);
+            for (int k = 0; k < N; ++k) v[k] = *reinterpret_cast<const v4f*>(src + (int64_t)k * BM * BN);
 #pragma unroll
-                for (int k = 1; k < N; ++k) v[0] += v[k];
-                float* const dst = C + (int64_t)(from + r) * J + col;
-                if (((uintptr_t)C & 15) == 0) *reinterpret_cast<v4f*>(dst) = v[0];
-                else dst[0] = v[0][0], dst[1] = v[0][1], dst[2] = v[0][2], dst[3] = v[0][3];
-            };
-            if (p.n == 4) sum(std::integral_constant<int, 4>{});
-            else if (p.n == 8) sum(std::integral_constant<int, 8>{});
-            else sum(std::integral_constant<int, 16>{});
-        }
-        item -= items;
+            for (int k = 1; k < N; ++k) v[0] += v[k];
+            float* const dst = C + (int64_t)(from + r) * J + col;
+            if (((uintptr_t)C & 15) == 0) *reinterpret_cast<v4f*>(dst) = v[0];
+            else dst[0] = v[0][0], dst[1] = v[0][1], dst[2] = v[0][2], dst[3] = v[0][3];
+        };
+        if (p.n == 4) sum(std::integral_constant<int, 4>{});
+        else if (p.n == 8) sum(std::integral_constant<int, 8>{});
+        else sum(std::integral_constant<int, 16>{});
     }
 }
 // dW of every expert; zeros where it has no slots, whatever gamma is
@@ -1289,7 +1285,7 @@ void launch_experts_dx(const ExpertsOperands& a, const ExpertsBackwardPlan& p, h
     kernel<<<(unsigned)grid, 512, 0, s>>>(a.g, a.Sw, a.T, a.K, Np, a.beta, 1.0f, a.dX, 0, (int)gj, 0, 0, {}, ex);
     if (p.dx_slices < 4 || S < 4 || nst < 32) return;  // tail_plan cuts nothing
     const auto fold = p.dx_tile == 1 ? fold_expert_tails<256> : fold_expert_tails<128>;
-    fold<<<512, 256, 0, s>>>(ex, S, (int)nst, (int)gj, a.K, a.dX);
+    fold<<<1024, 256, 0, s>>>(ex, S, (int)nst, (int)gj, a.K, a.dX);
 }
 
 void launch_experts_dw(const ExpertsOperands& a, const ExpertsBackwardPlan& p, hipStream_t s) {

@@ -82,8 +82,9 @@ struct ExpertsArgs {
 hipError_t launch_matmul_experts(const ExpertsArgs& a, hipStream_t s);
 
 // backward.hip: the two products of the backward from the copies that experts_backward.hip makes of their operands.
-// Reduction indices in blocks of 32 as there (block_offset): g [T rows][Np] (direct: dY itself, by rows), Sw [E][Np / 32][K]; gwT [N rows] and qT [K
-// rows] over the slots of expert after expert, each expert's filled up with zeros to whole blocks and to `least` of them.
+// Reduction indices in blocks of 32 as there (block_offset): g [T rows][Np] (direct: dY itself, by rows), Sw
+// [E][Np / 32][K]; gwT [N rows] and qT [K rows] over the slots of expert after expert, each expert's filled up with zeros to
+// whole blocks and to `least` of them.
 struct ExpertsOperands {
     const uint16_t *g, *gwT, *qT;
     const uint32_t* Sw;
@@ -126,34 +127,42 @@ struct ExpertTiles {
 __host__ __device__ inline int64_t most_tiles(int64_t T, int64_t E, int BM, int least) {
     return T / BM + (least ? E * least : T < E ? T : E);
 }
+// v of this lane and of those below it, all lanes active
+__device__ inline int wave_sums(int v) {
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, true);  // within rows of 16 lanes: from 1,
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, true);  // 2,
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, true);  // 4
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, true);  // and 8 lanes below;
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, true);  // the last lane of rows 0 and 2 to rows 1 and 3;
+    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, true);  // lane 31 to rows 2 and 3
+    return v;
+}
 // Counts them (no expert has fewer than `least`), all threads of a workgroup of 256 or more; their number, which no
-// value of `offsets` takes past most_tiles.
+// value of `offsets` takes past most_tiles.  Every workgroup of a product does this before its first load.
 __device__ inline int expert_tiles(const int32_t* offsets, int E, int T, int BM, ExpertTiles& sm, int least = 0) {
-    const int e = (int)threadIdx.x, l = e & (kWave - 1);
-    if (e < kMaxExperts) {
+    const int e = (int)threadIdx.x, most = (int)most_tiles(T, E, BM, least);
+    const bool mine = e < kMaxExperts && (e & -kWave) < E;  // whole waves
+    if (mine) {
         const int from = e < E ? slot_bound(offsets, e, T) : 0, to = e < E ? slot_bound(offsets, e + 1, T) : 0;
         int v = to > from ? (to - from + BM - 1) / BM : 0;
         if (v < least && e < E) v = least;
         sm.from[e] = from;
         sm.to[e] = to > from ? to : from;
-#pragma unroll
-        for (int d = 1; d < kWave; d <<= 1) {
-            const int o = __shfl_up(v, d, kWave);
-            if (l >= d) v += o;
-        }
-        sm.first[e + 1] = v;
-    }
-    __syncthreads();
-    int lower = 0;
-    if (e < kMaxExperts)
-        for (int i = kWave; i <= e; i += kWave) lower += sm.first[i];
-    __syncthreads();
-    if (e < kMaxExperts) {
-        const int most = (int)most_tiles(T, E, BM, least), v = sm.first[e + 1] + lower;
-        sm.first[e + 1] = v < most ? v : most;
+        v = wave_sums(v);
+        sm.first[e + 1] = E > kWave ? v : v < most ? v : most;
     }
     if (e == 0) sm.first[0] = 0;
     __syncthreads();
+    if (E > kWave) {
+        int v = 0;
+        if (mine) {
+            v = sm.first[e + 1];
+            for (int i = kWave; i <= e; i += kWave) v += sm.first[i];
+        }
+        __syncthreads();
+        if (mine) sm.first[e + 1] = v < most ? v : most;
+        __syncthreads();
+    }
     return sm.first[E];
 }
 // The expert of a row of tiles, and where that row's slots begin and the expert's end.
