@@ -257,10 +257,10 @@ struct RingSlices {
     int splits, per;  // per: stages of 32 r in a slice
 };
 
-// A mixture of experts (EXP): the product is one for each expert, over its own slots.  dX^: the slots are rows of A and C,
-// S and the scale are the expert's.  dW: they are the reduction, whose stages the copies hold expert after expert, none
-// with fewer than `least` (so that every slice has one); C is [E][I][J].  Which slots are whose is in device memory: the
-// workgroups count for themselves.
+// A mixture of experts (EXP): the product is one for each expert, over its own slots.  dX^: the slots are rows of A and
+// C, S and the scale are the expert's.  dW: they are the reduction, whose stages the copies hold expert after expert,
+// none with fewer than `least` (so that every slice has one); C is [E][I][J].  Which slots are whose is in device
+// memory: the workgroups count for themselves.
 struct ExpertsRing {
     const int32_t* offsets;
     int E, T, least;
@@ -270,9 +270,9 @@ struct ExpertsRing {
     int slices;
 };
 
-// dX of a mixture.  An XCD's G / 8 workgroups take a contiguous range of the tiles (the ranges differ by one), round after
-// round; the tiles of the last, partial round are cut along the reduction where that fills the XCD, each slice's sum going
-// to the workgroup's place in `part` for fold_expert_tails.  Few tiles are a partial round too.
+// dX of a mixture.  An XCD's G / 8 workgroups take a contiguous range of the tiles (the ranges differ by one), round
+// after round; the tiles of the last, partial round are cut along the reduction where that fills the XCD, each slice's
+// sum going to the workgroup's place in `part` for fold_expert_tails.  Few tiles are a partial round too.
 struct TailPlan {
     int first, full, tail, n;  // tiles in whole rounds, behind them, and the slices of each of those
 };
@@ -284,8 +284,8 @@ __device__ inline TailPlan tail_plan(int tiles, int x, int S, int stages, int sl
     p.tail = len - p.full;
     p.n = 1;
     // Twice the slices while that saves more than their sums cost to write and read: with n of them 0.39 us a stage and
-    // 1 / n against 0.42 us for each of an XCD's tails and n (128 x 256 tiles; 256 x 256 0.62 and 0.84).  666 slots of 4
-    // experts 1024 -> 4096 take 67 us in 16 slices, 51 in 4.  Two would gain what a CU's second workgroup is worth.
+    // 1 / n against 0.42 us for each of an XCD's tails and n (128 x 256 tiles; 256 x 256 0.62 and 0.84).  666 slots of
+    // 4 experts 1024 -> 4096 take 67 us in 16 slices, 51 in 4.  Two would gain what a CU's second workgroup is worth.
     if (p.tail > 0)
         while (2 * p.n <= slices && 2 * p.n * p.tail <= S && stages >= 16 * p.n &&
                5 * stages > 12 * p.tail * p.n * p.n)
@@ -377,8 +377,9 @@ __global__ __launch_bounds__(256, T == 256 ? 1 : 2) void gemm_tn_bf16_wide(const
 
     auto tile_origin = [&](int t, int64_t& i0, int64_t& j0) {
         if constexpr (EXP) {
-            // Each XCD gets a contiguous eighth of every expert's tiles.  (An eighth of all tiles is an expert each of eight,
-            // and the one with the most slots sets the time: 8192 slots of 8 experts, 2048 -> 8192, 524 us, so 346.)
+            // Each XCD gets a contiguous eighth of every expert's tiles.  (An eighth of all tiles is an expert each of
+            // eight, and the one with the most slots sets the time: 8192 slots of 8 experts, 2048 -> 8192, 524 us, so
+            // 346.)
             const int per = grid_i * grid_j;
             int tile = SPLIT ? t / sl.splits : t;
             expert = tile / per;
@@ -389,10 +390,10 @@ __global__ __launch_bounds__(256, T == 256 ? 1 : 2) void gemm_tn_bf16_wide(const
                 expert = q / len;
                 tile = first + q - expert * len;
             }
-            // In bands of H rows of tiles, the rows fastest: what an XCD runs together is about square.  Calls in 128 x 128
-            // tiles, rows of tiles one by one / in bands of 8: 4480 slots of 7 experts 2048 -> 8192 302 / 233, 6560 of 5
-            // 4096 -> 4096 345 / 286, 16128 of 9 4096 -> 1024 253 / 243; bands of 2, 4, 8 and 16, 8192 of 8 2048 -> 8192 743,
-            // 698, 730, 737.
+            // In bands of H rows of tiles, the rows fastest: what an XCD runs together is about square.  Calls in 128 x
+            // 128 tiles, rows of tiles one by one / in bands of 8: 4480 slots of 7 experts 2048 -> 8192 302 / 233, 6560
+            // of 5 4096 -> 4096 345 / 286, 16128 of 9 4096 -> 1024 253 / 243; bands of 2, 4, 8 and 16, 8192 of 8 2048
+            // -> 8192 743, 698, 730, 737.
             constexpr int H = 4;
             const int band = tile / (H * grid_j), rem = tile - band * H * grid_j;
             const int rows = grid_i - band * H < H ? grid_i - band * H : H;
@@ -869,7 +870,8 @@ __global__ __launch_bounds__(512, BM == 256 ? 2 : 4) void gemm_tn_signs_ring(con
             const int64_t jb = j0 + __builtin_amdgcn_readfirstlane(wn * WTN);
             const float sc = EXP ? scale_ptr[current] : scale;  // EXP: the expert's, in every slice
             const bool apart = EXP && place >= 0;  // rows of 256
-            float* const at = apart ? ex.part + (int64_t)place * BM * BN + (ib - i0) * BN + (jb - j0) : Cs + ib * J + jb;
+            float* const at =
+                apart ? ex.part + (int64_t)place * BM * BN + (ib - i0) * BN + (jb - j0) : Cs + ib * J + jb;
             store_tile<MI, NI, true>(at, apart ? BN : J, (EXP ? rows_end : I) - ib, apart ? BN : J - jb, j, g2,
                                [](int, int) {}, [&](int mi, int r, int s) { return sc * acc[mi][s][r]; });
             if constexpr (EXP) current = expert, rows_end = end, place = slice;
@@ -1155,9 +1157,9 @@ hipError_t launch_backward(const BackwardArgs& a, hipStream_t s) {
 }
 
 // ---- mixtures of experts ------------------------------------------------------------------------------
-// dX of the tiles that gemm_tn_signs_ring cut (tail_plan): the slices' sums added in the order 0, 1, ...  Whether there are
-// any is known here only, so the grid is small and its workgroups take 1024 elements of a tile in turn, those of the XCD
-// that wrote them; a thread has all its slices' loads in flight.
+// dX of the tiles that gemm_tn_signs_ring cut (tail_plan): the slices' sums added in the order 0, 1, ...  Whether there
+// are any is known here only, so the grid is small and its workgroups take 1024 elements of a tile in turn, those of
+// the XCD that wrote them; a thread has all its slices' loads in flight.
 template <int BM>
 __global__ __launch_bounds__(256) void fold_expert_tails(ExpertsRing ex, int S, int stages, int grid_j, int64_t J,
                                                          float* __restrict__ C) {
@@ -1215,9 +1217,9 @@ __global__ __launch_bounds__(256) void fold_expert_weights(const float* __restri
     }
 }
 
-// The tiles that cost least, by the costs in us that the plain layer's plans take, and the slices of dW.  How the slots fall
-// on the experts is not known here: an expert's last row of tiles is taken to be half full, its reduction of average
-// length.
+// The tiles that cost least, by the costs in us that the plain layer's plans take, and the slices of dW.  How the slots
+// fall on the experts is not known here: an expert's last row of tiles is taken to be half full, its reduction of
+// average length.
 ExpertsBackwardPlan experts_backward_plan(int64_t T, int64_t N, int64_t K, int E) {
     constexpr RingCost kDxWide{0.615, 12.0, 5.0, 6.0}, kDxRows{0.33, 5.0, 5.0, 6.0}, kDxAlone{0.39, 2.0, 5.0, 6.0};
     constexpr RingCost kDwWide{0.68, 12.8, 5.0, 6.0}, kDwSmall{0.172, 2.3, 5.0, 6.0}, kDwAlone{0.226, 3.6, 5.0, 6.0};
@@ -1234,8 +1236,9 @@ ExpertsBackwardPlan experts_backward_plan(int64_t T, int64_t N, int64_t K, int E
         const double rows = (double)T / (wide ? 256 : 128) + 0.5 * A, slots = wide ? cus : 2.0 * cus;
         const double tiles = (rows > 0.9 * A ? rows : 0.9 * A) * tiles_of(K, 256);
         const double whole = (double)(int64_t)(tiles / slots), tail = tiles - whole * slots;
-        // Slices of the last round's tiles cost a launch, 4.5 us, also where the device finds nothing to cut: few tiles, or
-        // more than a round of long ones (a quarter of the rounds end so, and save most of 0.39 us a stage then).
+        // Slices of the last round's tiles cost a launch, 4.5 us, also where the device finds nothing to cut: few
+        // tiles, or more than a round of long ones (a quarter of the rounds end so, and save most of 0.39 us a stage
+        // then).
         const bool cut = force ? force > 1 : tiles < 0.3 * slots ? nst >= 32 && 5 * nst > 6 * tiles
                                                                          : tiles > 0.9 * slots && nst >= 96;
         int n = 1;  // as tail_plan does
@@ -1254,8 +1257,8 @@ ExpertsBackwardPlan experts_backward_plan(int64_t T, int64_t N, int64_t K, int E
             if ((t.bwd_ring && t.bwd_ring != tile) || (n > 1 && rst < 8 * n)) continue;
             const double tiles = E * tiles_of(N, wide ? 256 : 128) * tiles_of(K, wide ? 256 : 128);
             const RingCost c = wide ? kDwWide : tiles * n > cus ? kDwSmall : kDwAlone;
-            // operands that do not stay in the 256 MB cache cost the small tiles, which read them more often, more (8192
-            // slots of 8 experts 2048 -> 8192, 168 MB: 657 in the large ones, 698; half the slots 410 / 384)
+            // operands that do not stay in the 256 MB cache cost the small tiles, which read them more often, more
+            // (8192 slots of 8 experts 2048 -> 8192, 168 MB: 657 in the large ones, 698; half the slots 410 / 384)
             const double more = !wide && (double)(N + K) * (double)T * 2.0 > 1.4e8 ? 1.2 : 1.0;
             const double rounds = tiles * n / cus + 0.2, bytes = (double)E * (double)N * (double)K * 4.0;
             const double v = (rounds < 1.0 ? 1.0 : rounds) * (c.stage * more * rst / n + c.item) +
@@ -1281,7 +1284,8 @@ void launch_experts_dx(const ExpertsOperands& a, const ExpertsBackwardPlan& p, h
     ExpertsRing ex{a.offsets, a.E, (int)a.T, 0, 64, a.T * 64, a.part, p.dx_slices};
     if (a.direct) ex.a_pitch = (uint32_t)(a.N * 2), ex.a_step = 64;
     const int grid = dx_grid(a.T, a.K, a.E, p), S = grid / 8;
-    const auto kernel = p.dx_tile == 1 ? gemm_tn_signs_ring<256, 4, false, true> : gemm_tn_signs_ring<128, 4, false, true>;
+    const auto kernel =
+        p.dx_tile == 1 ? gemm_tn_signs_ring<256, 4, false, true> : gemm_tn_signs_ring<128, 4, false, true>;
     kernel<<<(unsigned)grid, 512, 0, s>>>(a.g, a.Sw, a.T, a.K, Np, a.beta, 1.0f, a.dX, 0, (int)gj, 0, 0, {}, ex);
     if (p.dx_slices < 4 || S < 4 || nst < 32) return;  // tail_plan cuts nothing
     const auto fold = p.dx_tile == 1 ? fold_expert_tails<256> : fold_expert_tails<128>;
@@ -1295,8 +1299,9 @@ void launch_experts_dw(const ExpertsOperands& a, const ExpertsBackwardPlan& p, h
     const int64_t items = gi * gj * a.E * sl.splits, cap = (int64_t)ring_cus() * (T == 256 ? 1 : 2);
     const unsigned grid = (unsigned)(items < cap ? items : cap);
     const bool cut = sl.splits > 1;
-    const auto kernel = cut ? (T == 256 ? gemm_tn_bf16_wide<256, 4, true, true> : gemm_tn_bf16_wide<128, 4, true, true>)
-                            : (T == 256 ? gemm_tn_bf16_wide<256, 4, false, true> : gemm_tn_bf16_wide<128, 4, false, true>);
+    const auto kernel =
+        cut ? (T == 256 ? gemm_tn_bf16_wide<256, 4, true, true> : gemm_tn_bf16_wide<128, 4, true, true>)
+            : (T == 256 ? gemm_tn_bf16_wide<256, 4, false, true> : gemm_tn_bf16_wide<128, 4, false, true>);
     kernel<<<grid, 256, 0, s>>>(a.gwT, a.qT, a.N, a.K, 0, cut ? nullptr : a.gamma,
                                 a.gamma && !cut ? 1.0f / 128.0f : 1.0f, cut ? a.part : a.dW, (int)gi, (int)gj, 0, 0, sl, ex);
     if (!cut) return;

@@ -83,8 +83,8 @@ hipError_t launch_matmul_experts(const ExpertsArgs& a, hipStream_t s);
 
 // backward.hip: the two products of the backward from the copies that experts_backward.hip makes of their operands.
 // Reduction indices in blocks of 32 as there (block_offset): g [T rows][Np] (direct: dY itself, by rows), Sw
-// [E][Np / 32][K]; gwT [N rows] and qT [K rows] over the slots of expert after expert, each expert's filled up with zeros to
-// whole blocks and to `least` of them.
+// [E][Np / 32][K]; gwT [N rows] and qT [K rows] over the slots of expert after expert, each expert's filled up with
+// zeros to whole blocks and to `least` of them.
 struct ExpertsOperands {
     const uint16_t *g, *gwT, *qT;
     const uint32_t* Sw;

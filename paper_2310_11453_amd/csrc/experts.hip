@@ -1,4 +1,5 @@
-// 1-bit x 8-bit products of a mixture of BitLinear layers (Eq. 7 and 11 of arXiv 2310.11453, a weight matrix per expert):
+// 1-bit x 8-bit products of a mixture of BitLinear layers (Eq. 7 and 11 of arXiv 2310.11453, a weight matrix per
+// expert):
 //   Y[s,n] = (sum_k q[r,k] S_e[n,k]) * (beta_e gamma_r / 128)    for the slots s of expert e, r the row that s reads
 // Few rows an expert: bound by the packed weights of the experts that have any.
 #include <algorithm>
@@ -27,11 +28,11 @@ struct Args {
 
 // blockIdx.x: a group of TILES 16-row weight tiles, blockIdx.y (and z): the how-manieth 16 slots of an expert.  Wave w
 // takes the 512-chunks w, w + W, ... of K; the weights are the row operand of v_mfma_i32_16x16x64_i8, the slots its
-// columns; a lane's 16 bytes of a packed tile hold 16 consecutive k of each of eight bit planes, (w >> i) & 0x01010101 is plane i as
-// {0,1} bytes, and sum_k q s = 2 sum_k q b - sum_k q.  The waves' sums meet in LDS.
-// A launch is a chain of trips to memory: the experts' bounds, then the weights and (in two trips) the codes, whose rows
-// are known only with the order.  So the first chunk's weights are requested as soon as the expert is known and the
-// epilogue's operands with the codes.
+// columns; a lane's 16 bytes of a packed tile hold 16 consecutive k of each of eight bit planes, (w >> i) & 0x01010101
+// is plane i as {0,1} bytes, and sum_k q s = 2 sum_k q b - sum_k q.  The waves' sums meet in LDS.
+// A launch is a chain of trips to memory: the experts' bounds, then the weights and (in two trips) the codes, whose
+// rows are known only with the order.  So the first chunk's weights are requested as soon as the expert is known and
+// the epilogue's operands with the codes.
 template <int TILES>
 __global__ __launch_bounds__(rows::kMaxWaves* kWave) void experts_rows_kernel(rows::Args a) {
     using namespace rows;
@@ -136,12 +137,13 @@ __global__ __launch_bounds__(rows::kMaxWaves* kWave) void experts_rows_kernel(ro
 static void launch_rows(const ExpertsArgs& a, hipStream_t s) {
     const int64_t TN = tiles_n(a.N), TK = tiles_k(a.K);
     const int64_t A = a.T < a.E ? a.T : a.E, blocks = a.T / rows::kSlots + A;
-    // Tiles of a workgroup: more of them share the fixed chain and the codes, fewer leave no CU idle.  us with 2 / 4 / 8, T
-    // slots of E experts: T = 32, E = 8, 2048 -> 2048 5.5 / 6.1 / 7.4, 8192 -> 2048 9.7 / 8.4 / 10.9; T = 96, E = 16, 4096 ->
-    // 4096 17.4 / 14.0 / 13.5; T = 200, E = 16, 2048 -> 8192 24.4 / 21.5 / 23.5.
+    // Tiles of a workgroup: more of them share the fixed chain and the codes, fewer leave no CU idle; eight leave two
+    // workgroups of a long reduction on a CU.  us with 2 / 4 / 8, T slots of E experts: T = 32, E = 8, 2048 -> 2048 5.5
+    // / 6.1 / 7.4, 8192 -> 2048 9.7 / 8.4 / 10.9; T = 64, E = 32, 6144 -> 2048 18.2 / 15.8 / 14.2; T = 128, E = 32,
+    // 4096 -> 5120 32.1 / 26.1 / 25.0; T = 128, E = 16, 2048 -> 8192 18.3 / 16.4 / 17.7.
     int tiles = tuning().decode_tiles;
     const int64_t all = blocks * TN;
-    if (!tiles) tiles = all < 512 ? 1 : all < 1280 || TK < 4 ? 2 : TK >= 8 && all > 4096 && all < 6144 ? 8 : 4;
+    if (!tiles) tiles = all < 512 ? 1 : all < 1280 || TK < 4 ? 2 : TK >= 8 && all > 4096 ? 8 : 4;
     rows::Args r{};
     r.codes = a.codes; r.packed = a.packed; r.offsets = a.offsets; r.order = a.order;
     r.T = (uint32_t)a.T; r.E = (uint32_t)a.E; r.top_k = (uint32_t)a.top_k; r.rows = (uint32_t)a.rows;
@@ -152,7 +154,8 @@ static void launch_rows(const ExpertsArgs& a, hipStream_t s) {
     const unsigned threads = (unsigned)(TK < rows::kMaxWaves ? TK : rows::kMaxWaves) * kWave;
     auto launch = [&](auto kernel, int n) {
         const int64_t most = 32768;  // of a dimension of a grid, which the bound may pass
-        const dim3 grid((unsigned)((TN + n - 1) / n), (unsigned)(blocks < most ? blocks : most), (unsigned)((blocks + most - 1) / most));
+        const dim3 grid((unsigned)((TN + n - 1) / n), (unsigned)(blocks < most ? blocks : most),
+                        (unsigned)((blocks + most - 1) / most));
         kernel<<<grid, threads, 0, s>>>(r);
     };
     if (tiles <= 1) launch(experts_rows_kernel<1>, 1);
@@ -169,8 +172,8 @@ static void launch_rows(const ExpertsArgs& a, hipStream_t s) {
 //   128 x 128         0.2 + rounds (6.8 + 2.84 c / 2)
 //   64 x 128          0.6 + rounds (5.75 + 3.14 c / 4)
 //   16 slots at a time  2.8 + 1.3 c / 8 + (0.06 c + 0.19) per 16 x 16 outputs and CU
-// 0.9 % slower than the best of the five on average, 21 % at most (118 slots, 3 experts, 3232 -> 7902: 16.2, 13.4 as 64 x
-// 128).  The extremes, 16 slots at a time / 128 x 256: 64 slots, 8 experts, 4096 -> 4096 10.0 / 29; 8900 slots, 12
+// 0.9 % slower than the best of the five on average, 21 % at most (118 slots, 3 experts, 3232 -> 7902: 16.2, 13.4 as 64
+// x 128).  The extremes, 16 slots at a time / 128 x 256: 64 slots, 8 experts, 4096 -> 4096 10.0 / 29; 8900 slots, 12
 // experts, 3840 -> 4808 787 / 181.
 static int experts_plan(const ExpertsArgs& a) {
     const double cus = num_cus(), T = (double)a.T, A = (double)(a.T < a.E ? a.T : a.E);

@@ -1,11 +1,11 @@
 // Straight-through backward of the products of a mixture of BitLinear layers (arXiv 2310.11453, Section 2.2):
 //   dXs[s,k]  = beta_e sum_n dY[s,n] S_e[n,k]             for the slots s of expert e
 //   dW_e[n,k] = sum_{s of e} dY[s,n] q[r,k] gamma_r/128    r the row that s reads; zeros where e has no slots
-// dY is bf16, +-1 and the codes are exact in bf16.  As in the plain layer (backward.hip, whose kernels take the products),
-// every operand is first written once in the layout they read:
+// dY is bf16, +-1 and the codes are exact in bf16.  As in the plain layer (backward.hip, whose kernels take the
+// products), every operand is first written once in the layout they read:
 //   g    [T][Np]       rows of dY                                 (A operand of dX, reduction over N; not where N is a
-//                      multiple of 32: the product reads dY itself, at the same speed, and the copies for 8192 slots 2048 ->
-//                      8192 take 86 us instead of 105)
+//                      multiple of 32: the product reads dY itself, at the same speed, and the copies for 8192 slots
+//                      2048 -> 8192 take 86 us instead of 105)
 //   Sw   [E][Np/32][K] the signs of 32 weight rows of a column    (B operand of dX)
 //   gwT  [N][slots]    dY transposed, with a gamma per token scaled and rounded again   (A operand of dW)
 //   qT   [K][slots]    codes transposed, gathered through the order                     (B operand of dW)
@@ -18,8 +18,8 @@
 namespace bl {
 
 namespace exb {
-// An item of the copies: 64 slots x 128 columns, transposed through LDS (the pitch is odd in dwords, so that the rows that
-// a lane's eight reads of a column come from are on different banks).
+// An item of the copies: 64 slots x 128 columns, transposed through LDS (the pitch is odd in dwords, so that the rows
+// that a lane's eight reads of a column come from are on different banks).
 constexpr int kRows = 64, kCols = 128;
 typedef uint16_t CastTile[kRows][kCols + 2];
 
@@ -45,10 +45,12 @@ __device__ inline uint32_t to_bf16(float v) {
     return u >> 16;
 }
 // (block_offset of backward.hip)
-__device__ inline int64_t copy_offset(int64_t row, int64_t r, int64_t R) { return ((r >> 5) * R + row) * 32 + (r & 31); }
+__device__ inline int64_t copy_offset(int64_t row, int64_t r, int64_t R) {
+    return ((r >> 5) * R + row) * 32 + (r & 31);
+}
 
-// dY (bf16) -> g and gwT, or codes -> qT.  VEC: a thread's eight elements are one load.  Everything that an item reads is
-// requested before the first of it is used.
+// dY (bf16) -> g and gwT, or codes -> qT.  VEC: a thread's eight elements are one load.  Everything that an item reads
+// is requested before the first of it is used.
 template <bool CODES, bool VEC>
 __device__ inline void copy_tile(const exb::Args& a, const ExpertTiles& count, int blocks, int r0, int64_t c0,
                                  exb::CastTile& tile) {
@@ -56,7 +58,8 @@ __device__ inline void copy_tile(const exb::Args& a, const ExpertTiles& count, i
     const int64_t C = CODES ? a.K : a.N;
     const int cl = ((int)threadIdx.x & 15) * 8, rt = (int)threadIdx.x >> 4;
     const int64_t c = c0 + cl;
-    int slot[4];  // of rows rt + 16 it; -1: filled up.  Rows 0 .. 31 of the item are a block, of one expert, 32 .. 63 another
+    // of rows rt + 16 it; -1: filled up.  Rows 0 .. 31 of the item are a block, of one expert, 32 .. 63 another
+    int slot[4];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
         int from = 0, to = 0;
@@ -85,7 +88,8 @@ __device__ inline void copy_tile(const exb::Args& a, const ExpertTiles& count, i
             } else {
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                    v[it][e] = (c + 2 * e < C ? src[2 * e] : 0) | (c + 2 * e + 1 < C ? (uint32_t)src[2 * e + 1] << 16 : 0);
+                    v[it][e] = (c + 2 * e < C ? src[2 * e] : 0) |
+                               (c + 2 * e + 1 < C ? (uint32_t)src[2 * e + 1] << 16 : 0);
             }
             if (a.row_gamma) gamma[it] = a.row_gamma[row[it]];
         }

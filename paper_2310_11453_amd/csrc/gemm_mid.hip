@@ -120,8 +120,8 @@ static uint32_t divisor(int64_t d, int64_t n_max) {
 // gmode 1: a work item is (column tile, one K-group of the layer), split over the workgroup's four.
 // NS = stages in each group's ring.
 // ROWS = false: one row tile (M <= BM).  STREAM: streaming stores (streaming_stores below).
-// EXP: a mixture of experts.  Items go expert by expert, inside one the row tiles of a column tile next to each other; how
-// many there are the workgroups count for themselves (the grid is a bound), in what will be the bits' buffer.
+// EXP: a mixture of experts.  Items go expert by expert, inside one the row tiles of a column tile next to each other;
+// how many there are the workgroups count for themselves (the grid is a bound), in what will be the bits' buffer.
 template <int BM, int NS, bool ROWS, bool STREAM, bool EXP = false>
 __global__ __launch_bounds__(mid::THREADS) void gemm_mid_kernel(mid::Args a) {
     using namespace mid;

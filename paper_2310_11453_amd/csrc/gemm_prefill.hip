@@ -138,8 +138,8 @@ __device__ inline void lds_write_b32(uint32_t ad, uint32_t v) {
 // Persistent: gridDim.x workgroups (one per CU) walk the tiles t = blockIdx.x, + gridDim.x, ...
 // GEN = false: the plain layer (one beta, Y = result): nothing of what follows costs anything.
 // GEN = true adds beta per column group (Eq. 13) and the shift term of Eq. 6.
-// EXP = true: a mixture of experts (the fields of GemmArgs say what it reads).  Where an expert's rows begin is in device
-// memory, so every workgroup counts the experts' rows of tiles for itself (ExpertTiles) and the grid is a bound.
+// EXP = true: a mixture of experts (the fields of GemmArgs say what it reads).  Where an expert's rows begin is in
+// device memory, so every workgroup counts the experts' rows of tiles for itself (ExpertTiles) and the grid is a bound.
 template <int BM, int BN, int WM, int WN, int NS, bool GEN, bool EXP = false>
 __global__ __launch_bounds__(WM * WN * 64, 2) void gemm_prefill_kernel(GemmArgs a, int grid_m,
                                                                         int grid_n, int xbm) {
@@ -241,7 +241,8 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void gemm_prefill_kernel(GemmArgs 
             gseg[q] = ((slot & 3) ^ ((row >> 2) & 3)) * 16;
             if (m0 + row > (EXP ? end : M) - 1) row = (int)((EXP ? end : M) - 1 - m0);
             if constexpr (EXP)  // rows * ldq < 2^32
-                goff[q] = code_row(a.order, (uint32_t)a.top_k, a.rows, (uint32_t)(m0 + row)) * (uint32_t)a.ldq + gseg[q];
+                goff[q] =
+                    code_row(a.order, (uint32_t)a.top_k, a.rows, (uint32_t)(m0 + row)) * (uint32_t)a.ldq + gseg[q];
             else goff[q] = (uint32_t)row * (uint32_t)a.ldq + gseg[q];
         }
         gbase = EXP ? a.codes : a.codes + m0 * a.ldq;

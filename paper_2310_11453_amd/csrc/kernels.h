@@ -139,9 +139,10 @@ struct GemmArgs {
     float* gamma_out;
     int32_t* rowsum_out;
     float* xhat_out;  // [K]: the normalised row the codes were rounded from
-    // A mixture of experts (launch_experts_tiles, and only it): slots offsets[e] .. offsets[e + 1] - 1 of Y are the rows
-    // of expert e, whose weights are packed + e * blob dwords and whose scale is beta[e]; slot s reads row order[s] /
-    // top_k (order null: s) of the `rows` rows of codes, gamma and rowsum.  M: an upper bound of offsets[experts].
+    // A mixture of experts (launch_experts_tiles, and only it): slots offsets[e] .. offsets[e + 1] - 1 of Y are the
+    // rows of expert e, whose weights are packed + e * blob dwords and whose scale is beta[e]; slot s reads row
+    // order[s] / top_k (order null: s) of the `rows` rows of codes, gamma and rowsum.  M: an upper bound of
+    // offsets[experts].
     const int32_t* offsets;
     const int32_t* order;
     int experts, top_k;

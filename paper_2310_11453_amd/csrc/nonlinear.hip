@@ -6,8 +6,8 @@
 //   backward   v = c * (amax_b / 127), h = f(v), n = (h - mean h) / sqrt(var h + eps)
 //              du = f'(v) * (g - mean g - n mean(g n)) / sqrt(var h + eps),  g = the gradient of x^
 // The backward is the derivative of the forward at v, exactly: its statistics are those of f(v), which come out of the
-// row that is in registers anyway, and nothing but the checkpoint has to be kept (1.03 bytes an element where u has four).
-// f and f' are evaluated in fp32, the sums of a row in fp64 (as in the quantiser and in the LayerNorm backward).
+// row that is in registers anyway, and nothing but the checkpoint has to be kept (1.03 bytes an element where u has
+// four).  f and f' are evaluated in fp32, the sums of a row in fp64 (as in the quantiser and in the LayerNorm backward).
 // Bound by HBM: 4 bytes read and 1 (with the checkpoint 2) written an element, twice the reading with a gamma per
 // tensor; backward 5 read, 2 or 4 written.
 #include "common.h"
@@ -28,11 +28,11 @@ __device__ inline float fn_value(float u) {
     else if constexpr (FN == kGelu) return 0.5f * u * (1.f + erff(u * 0.70710678118654752f));
     else return u / (1.f + expf(-u));
 }
-// f(v) and f'(v) of the backward, where they are factors of a gradient.  GELU: Phi(u) = (1 + erf(z)) / 2, z = u / sqrt 2,
-// with erf as in Abramowitz and Stegun 7.1.26 (erf z = 1 - (a1 t + ... + a5 t^5) e^(-z^2), t = 1 / (1 + p z), z >= 0: off
-// by at most 1.5e-7), which shares its exponential with f'.  The hardware's exponential and reciprocal are off by an ulp.
-// (16384 x 8192 with the library's erff and expf 455 us, 219 so.  The forward would gain 14 %, and a code in a million
-// fall on the other side of a border.)
+// f(v) and f'(v) of the backward, where they are factors of a gradient.  GELU: Phi(u) = (1 + erf(z)) / 2, z = u / sqrt
+// 2, with erf as in Abramowitz and Stegun 7.1.26 (erf z = 1 - (a1 t + ... + a5 t^5) e^(-z^2), t = 1 / (1 + p z), z >=
+// 0: off by at most 1.5e-7), which shares its exponential with f'.  The hardware's exponential and reciprocal are off
+// by an ulp.  (16384 x 8192 with the library's erff and expf 455 us, 219 so.  The forward would gain 14 %, and a code in
+// a million fall on the other side of a border.)
 struct FnPair {
     float value, slope;
 };
@@ -212,9 +212,10 @@ __device__ inline uint32_t bf16_word(float lo, float hi) {  // to nearest, ties 
     return __builtin_bit_cast(uint32_t, v);
 }
 
-// One reading of the row: g, and of the checkpoint f(v) and f'(v), stay in registers; the four sums that the derivative of
-// the LayerNorm needs (of h, h^2, g and g h) are taken together.  With eight float4 a lane and 16 waves a row, which have
-// 128 registers, the pairs are evaluated a second time instead of kept (2000 x 28672: 473 us kept and spilled, 148 so).
+// One reading of the row: g, and of the checkpoint f(v) and f'(v), stay in registers; the four sums that the derivative
+// of the LayerNorm needs (of h, h^2, g and g h) are taken together.  With eight float4 a lane and 16 waves a row, which
+// have 128 registers, the pairs are evaluated a second time instead of kept (2000 x 28672: 473 us kept and spilled, 148
+// so).
 template <int FN, int WPR, int NV>
 __global__ __launch_bounds__((WPR < 4 ? 4 : WPR) * kWave) void nonlinear_backward_rows(NonlinearArgs a) {
     constexpr int NW = WPR < 4 ? 4 : WPR, RPW = NW / WPR, RT = WPR * kWave;
@@ -247,8 +248,10 @@ __global__ __launch_bounds__((WPR < 4 ? 4 : WPR) * kWave) void nonlinear_backwar
     // sums about an element of the row, so that a large common offset costs nothing
     const double c = (double)fn_pair<FN>((float)(int8_t)c4[0] * scales[0]).value;
     auto pairs = [](uint32_t codes, float scale, float4& value, float4& slope) {
-        const FnPair x = fn_pair<FN>((float)(int8_t)codes * scale), y = fn_pair<FN>((float)(int8_t)(codes >> 8) * scale);
-        const FnPair z = fn_pair<FN>((float)(int8_t)(codes >> 16) * scale), w = fn_pair<FN>((float)(int8_t)(codes >> 24) * scale);
+        const FnPair x = fn_pair<FN>((float)(int8_t)codes * scale);
+        const FnPair y = fn_pair<FN>((float)(int8_t)(codes >> 8) * scale);
+        const FnPair z = fn_pair<FN>((float)(int8_t)(codes >> 16) * scale);
+        const FnPair w = fn_pair<FN>((float)(int8_t)(codes >> 24) * scale);
         value = make_float4(x.value, y.value, z.value, w.value);
         slope = make_float4(x.slope, y.slope, z.slope, w.slope);
     };
@@ -314,8 +317,8 @@ __global__ __launch_bounds__((WPR < 4 ? 4 : WPR) * kWave) void nonlinear_backwar
     }
 }
 
-// Waves a row and float4 a lane.  A batch of few rows is the length of one row's chain: more waves share it, down to two
-// float4 a lane; a large one is bound by HBM.
+// Waves a row and float4 a lane.  A batch of few rows is the length of one row's chain: more waves share it, down to
+// two float4 a lane; a large one is bound by HBM.
 struct RowShape {
     int wpr, nv;
 };
@@ -324,8 +327,8 @@ static RowShape row_shape(int64_t M, int64_t K) {
     int wpr = 1, nv = 2;
     auto wider = [&]() { wpr = wpr == 1 ? 4 : wpr * 2; };
     while (wpr < 16 && K4 > (int64_t)wpr * kWave * 8) wider();
-    // (us, forward / backward: 32 x 8192 with 4, 8, 16 waves 4.9 / 6.8, 4.3 / 5.0, 4.6 / 5.6; 32 x 2048 with 1, 4, 8 4.4 / 6.6,
-    // 3.0 / 3.1, 3.4 / 3.5; 16384 x 8192 with 4, 8, 16 126 / 219, 144 / 216, 194 / 297)
+    // (us, forward / backward: 32 x 8192 with 4, 8, 16 waves 4.9 / 6.8, 4.3 / 5.0, 4.6 / 5.6; 32 x 2048 with 1, 4, 8
+    // 4.4 / 6.6, 3.0 / 3.1, 3.4 / 3.5; 16384 x 8192 with 4, 8, 16 126 / 219, 144 / 216, 194 / 297)
     while (wpr < 8 && M * wpr <= 1024 && K4 > (int64_t)wpr * kWave * 2) wider();
     if (const int v = tuning().quant_wpr)
         if ((v == 1 || v == 4 || v == 8 || v == 16) && K4 <= (int64_t)v * kWave * 8) wpr = v;

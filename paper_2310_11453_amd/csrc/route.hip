@@ -53,10 +53,10 @@ __global__ __launch_bounds__(route::kLarge) void route_count_kernel(RouteArgs a,
 }
 
 // The place of a choice inside its expert is the number of earlier choices of that expert: of earlier workgroups
-// (counts), of earlier rows of 64 of this workgroup (cnt, summed down the rows) and of lower lanes of its row (a ballot for
-// each bit of the expert's number).  Nothing depends on which wave is first.  Thread (p, e) sums a part of the rows and of
-// the other workgroups' counts for expert e.  (One thread an expert, walking 64 rows and 16 counts one after another: 12.9
-// us for 65528 choices of 64 experts, behind a count of 6.1.)
+// (counts), of earlier rows of 64 of this workgroup (cnt, summed down the rows) and of lower lanes of its row (a ballot
+// for each bit of the expert's number).  Nothing depends on which wave is first.  Thread (p, e) sums a part of the rows
+// and of the other workgroups' counts for expert e.  (One thread an expert, walking 64 rows and 16 counts one after
+// another: 12.9 us for 65528 choices of 64 experts, behind a count of 6.1.)
 template <int THREADS>
 __global__ __launch_bounds__(THREADS) void route_kernel(RouteArgs a, int bits) {
     using namespace route;
@@ -178,7 +178,8 @@ __device__ inline uint32_t bf16_rne(float v) {
     return u >> 16;
 }
 
-// A workgroup: a token and 256 pieces of its row, of four elements (VEC: N % 4 == 0) or one; items beyond the grid in turn.
+// A workgroup: a token and 256 pieces of its row, of four elements (VEC: N % 4 == 0) or one; items beyond the grid in
+// turn.
 template <bool VEC>
 __device__ inline void combine_piece(const CombineArgs& a, int64_t t, int64_t n) {
     constexpr int E = VEC ? 4 : 1;
@@ -224,7 +225,8 @@ __device__ inline void combine_backward_token(const CombineArgs& a, int64_t t, f
             if constexpr (VEC) {
                 const float4 v = *reinterpret_cast<const float4*>(g);
                 *reinterpret_cast<uint2*>(a.dSlots + o) =
-                    make_uint2(bf16_rne(wt * v.x) | bf16_rne(wt * v.y) << 16, bf16_rne(wt * v.z) | bf16_rne(wt * v.w) << 16);
+                    make_uint2(bf16_rne(wt * v.x) | bf16_rne(wt * v.y) << 16,
+                               bf16_rne(wt * v.z) | bf16_rne(wt * v.w) << 16);
                 if (a.dWeights) {
                     const float4 y = *reinterpret_cast<const float4*>(a.slots + o);
                     dot += (v.x * y.x + v.y * y.y) + (v.z * y.z + v.w * y.w);
@@ -263,7 +265,8 @@ hipError_t launch_combine(const CombineArgs& a, hipStream_t s) {
 }
 
 hipError_t launch_combine_backward(const CombineArgs& a, hipStream_t s) {
-    const bool vec = a.N % 4 == 0 && (((uintptr_t)a.slots | (uintptr_t)a.dY) & 15) == 0 && ((uintptr_t)a.dSlots & 7) == 0;
+    const bool vec = a.N % 4 == 0 && (((uintptr_t)a.slots | (uintptr_t)a.dY) & 15) == 0 &&
+                     ((uintptr_t)a.dSlots & 7) == 0;
     if (vec) combine_backward_kernel<true><<<token_grid(a.M), 256, 0, s>>>(a);
     else combine_backward_kernel<false><<<token_grid(a.M), 256, 0, s>>>(a);
     return hipGetLastError();
