@@ -325,7 +325,9 @@ int bitlinear_layernorm_backward(const float* dXhat, const float* X, int64_t M, 
  * Where an expert's slots begin stays in device memory (`offsets`): nothing waits for the router.
  * Slots behind offsets[experts] (choices that name no expert) are neither read nor written.
  * Limits: experts 1..256, top_k 1..64, M * top_k <= 2^30 (else BL_ERR_SHAPE); bitlinear_route takes up to
- * 2^24 choices, the products K <= 65536 (else BL_ERR_UNSUPPORTED).
+ * 2^24 choices, the products K <= 65536, bitlinear_quant_nonlinear and its backward M < 2^24 rows and M * K <=
+ * 2^36 (else BL_ERR_UNSUPPORTED, which is also the answer to operands that are read several elements at a time
+ * and not 16-byte aligned: codes, packed, U, check, dXhat, dU, and dY for a dX with N % 32 == 0).
  *   packed  `experts` consecutive blobs of bitlinear_packed_bytes(N, K, 0) bytes, one bitlinear_pack_weights
  *           call each (N % 16 == 0 and experts <= 64: bitlinear_pack_weights_grouped of the [experts * N, K]
  *           matrix with groups_n = experts writes the same bytes)
@@ -390,7 +392,7 @@ int bitlinear_combine_backward(const float* dY, const float* slots, const int32_
  *   U            in   fp32 [M,K], K <= 32768 (else BL_ERR_UNSUPPORTED)
  *   fn                a bl_fn
  *   rows         in   int32 [1] (device) or NULL: only rows below it are read and written (of a routed batch:
- *                     offsets + experts)
+ *                     offsets + experts); without any a gamma per tensor is its lower bound
  *   check        out  int8 [M,K] or NULL: rne(u * (127 / m)), m the largest magnitude of each 128
  *                     consecutive elements of a row (the last ones of a row may be fewer)
  *   check_scale  out  fp32 [M][(K + 127) / 128]: m / 127

@@ -607,7 +607,7 @@ def bitlinear_backward_ste_experts(dY: torch.Tensor, codes: torch.Tensor, gamma:
     M, top_k, T = _slots(codes, order, top_k)
     K, E, N = codes.shape[1], offsets.numel() - 1, dY.shape[1]
     dX = torch.empty((T, K), dtype=torch.float32, device=dev) if want_dx else None
-    dW = torch.empty((E, N, K), dtype=torch.float32, device=dev) if want_dw else None
+    dW = (torch.empty if T else torch.zeros)((E, N, K), dtype=torch.float32, device=dev) if want_dw else None
     ws, ws_bytes, _keep = _scratch(workspace_bytes_experts(OP_BACKWARD, M, top_k, N, K, E, per_tensor), workspace, dev)
     _check(lib.bitlinear_backward_ste_experts(
         _given(dev, dY, torch.bfloat16, T, N), M, top_k, N, K, _ptr(codes, torch.int8),
@@ -643,7 +643,8 @@ def bitlinear_combine_backward(dY: torch.Tensor, slots: torch.Tensor | None, pos
         out = torch.empty((M * top_k, N), dtype=torch.bfloat16, device=dev)
     dweights = None if slots is None else torch.empty((M, top_k), dtype=torch.float32, device=dev)
     _check(lib.bitlinear_combine_backward(
-        _given(dev, dY, torch.float32, M, N), None if slots is None else _given(dev, slots, torch.float32, M * top_k, N),
+        _given(dev, dY, torch.float32, M, N),
+        None if slots is None else _given(dev, slots, torch.float32, M * top_k, N),
         _given(dev, position, torch.int32, M, top_k),
         None if weights is None else _given(dev, weights, torch.float32, M, top_k), M, top_k, N,
         _given(dev, out, torch.bfloat16, M * top_k, N), _ptr(dweights), _stream()), "bitlinear_combine_backward")
@@ -671,9 +672,10 @@ def bitlinear_quant_nonlinear(U: torch.Tensor, fn: str = "gelu", ln_eps: float =
     need = workspace_bytes_experts(OP_QUANT_NONLINEAR, M, 1, 0, 0, 0, True) if per_tensor else 0
     ws, ws_bytes, _keep = _scratch(need, workspace, dev)
     _check(lib.bitlinear_quant_nonlinear(
-        _ptr(U, torch.float32), M, K, _function(fn), ln_eps, None if rows is None else _given(dev, rows, torch.int32, 1),
-        _gran(per_tensor), codes.data_ptr(), gamma.data_ptr(), rowsum.data_ptr(), _ptr(check), _ptr(scale), ws, ws_bytes,
-        _stream()), "bitlinear_quant_nonlinear")
+        _ptr(U, torch.float32), M, K, _function(fn), ln_eps,
+        None if rows is None else _given(dev, rows, torch.int32, 1), _gran(per_tensor), codes.data_ptr(),
+        gamma.data_ptr(), rowsum.data_ptr(), _ptr(check), _ptr(scale), ws, ws_bytes, _stream()),
+        "bitlinear_quant_nonlinear")
     return codes, gamma, rowsum, check, scale
 
 

@@ -23,6 +23,11 @@ bool weights_ok(int64_t N, int64_t K) {
 bool tokens_ok(int64_t M, int top_k) {
     return M >= 0 && M <= kMaxDim && top_k >= 1 && top_k <= kMaxTopK && M * top_k <= kMaxDim;
 }
+// operands read 4, 8 or 16 bytes at a time: an address that allows it
+template <class... P>
+bool aligned16(const P*... p) {
+    return ((... | (uintptr_t)p) & 15) == 0;
+}
 bool experts_ok(int experts) { return experts >= 1 && experts <= kMaxExperts; }
 
 size_t route_bytes(int64_t T, int experts) {
@@ -47,6 +52,8 @@ ExpertsArgs experts_args(const int8_t* codes, const float* gamma, int64_t M, int
     return a;
 }
 
+// a workgroup's threads times the rows stay below 2^32, which is what a launch takes
+bool nonlinear_rows_ok(int64_t M, int64_t K) { return M < ((int64_t)1 << 24) && M * K <= ((int64_t)1 << 36); }
 struct NonlinearWs {
     size_t rowstats, gmax, total;
 };
@@ -68,7 +75,7 @@ size_t bitlinear_workspace_bytes_experts(int op, int64_t M, int top_k, int64_t N
         case BL_OP_ROUTE:
             return experts_ok(experts) && M * top_k <= kMaxRouteSlots ? route_bytes(M * top_k, experts) : 0;
         case BL_OP_QUANT_NONLINEAR:
-            return granularity == BL_GAMMA_PER_TENSOR ? nonlinear_ws(M * top_k).total : 0;
+            return granularity == BL_GAMMA_PER_TENSOR && nonlinear_rows_ok(M * top_k, 0) ? nonlinear_ws(M * top_k).total : 0;
         case BL_OP_BACKWARD:
             if (experts_status(M, top_k, N, K, experts, granularity) != BL_OK) return 0;
             return experts_backward_bytes(M * top_k, N, K, experts) + 256;
@@ -96,6 +103,7 @@ int bitlinear_matmul_experts(const int8_t* codes, const float* gamma, const int3
     if (flags & ~BL_FLAG_OUT_ACC_I32) return BL_ERR_UNSUPPORTED;
     if (M == 0) return BL_OK;
     if (!codes || !gamma || !rowsum || !offsets || !packed || !beta || !Y) return BL_ERR_NULL;
+    if (!aligned16(codes, (const char*)packed)) return BL_ERR_UNSUPPORTED;
     ExpertsArgs a = experts_args(codes, gamma, M, top_k, N, K, order, offsets, experts, packed, beta, granularity);
     a.rowsum = rowsum;
     a.out_acc = (flags & BL_FLAG_OUT_ACC_I32) != 0;
@@ -112,7 +120,9 @@ int bitlinear_backward_ste_experts(const void* dY, int64_t M, int top_k, int64_t
     if (!dY || !gamma || !offsets) return BL_ERR_NULL;
     if (dX && (!packed || !beta)) return BL_ERR_NULL;
     if (dW && !codes) return BL_ERR_NULL;
-    if (dX && experts_dy_direct(N) && ((uintptr_t)dY & 15)) return BL_ERR_UNSUPPORTED;  // read 16 bytes at a time
+    if ((dX && experts_dy_direct(N) && !aligned16((const char*)dY)) || (dX && !aligned16((const char*)packed)) ||
+        (dW && !aligned16(codes)))
+        return BL_ERR_UNSUPPORTED;
     if (!workspace || workspace_bytes < experts_backward_bytes(M * top_k, N, K, experts) + 256) return BL_ERR_WORKSPACE;
     ExpertsArgs a = experts_args(codes, gamma, M, top_k, N, K, order, offsets, experts, packed, beta, granularity);
     a.dY = (const uint16_t*)dY; a.dX = dX; a.dW = dW;
@@ -121,8 +131,8 @@ int bitlinear_backward_ste_experts(const void* dY, int64_t M, int top_k, int64_t
     return check_hip(launch_experts_backward(a, (hipStream_t)stream));
 }
 
-int bitlinear_combine(const float* slots, const int32_t* position, const float* weights, int64_t M, int top_k, int64_t N,
-                      float* Y, void* stream) {
+int bitlinear_combine(const float* slots, const int32_t* position, const float* weights, int64_t M, int top_k,
+                      int64_t N, float* Y, void* stream) {
     if (!tokens_ok(M, top_k) || N <= 0 || N > kMaxDim) return BL_ERR_SHAPE;
     if (M == 0) return BL_OK;
     if (!slots || !position || !Y) return BL_ERR_NULL;
@@ -149,7 +159,9 @@ int bitlinear_quant_nonlinear(const float* U, int64_t M, int64_t K, int fn, floa
     if (M < 0 || M > kMaxDim || K <= 0 || K > kMaxDim || K % 32) return BL_ERR_SHAPE;
     if (!gran_ok(granularity) || fn < BL_FN_RELU || fn > BL_FN_SILU || K > kMaxNonlinearK) return BL_ERR_UNSUPPORTED;
     if (M == 0) return BL_OK;
+    if (!nonlinear_rows_ok(M, K)) return BL_ERR_UNSUPPORTED;
     if (!U || !codes || !gamma || (check && !check_scale)) return BL_ERR_NULL;
+    if (!aligned16(U, codes, check, (const char*)workspace)) return BL_ERR_UNSUPPORTED;
     const NonlinearWs ws = nonlinear_ws(M);
     const bool per_tensor = granularity == BL_GAMMA_PER_TENSOR;
     if (per_tensor && (!workspace || workspace_bytes < ws.total)) return BL_ERR_WORKSPACE;
@@ -163,13 +175,16 @@ int bitlinear_quant_nonlinear(const float* U, int64_t M, int64_t K, int fn, floa
     return check_hip(launch_quant_nonlinear(a, fn, (hipStream_t)stream));
 }
 
-int bitlinear_nonlinear_backward(const float* dXhat, const int8_t* check, const float* check_scale, int64_t M, int64_t K,
-                                 int fn, float ln_eps, const int32_t* rows, int type, void* dU, void* stream) {
+int bitlinear_nonlinear_backward(const float* dXhat, const int8_t* check, const float* check_scale, int64_t M,
+                                 int64_t K, int fn, float ln_eps, const int32_t* rows, int type, void* dU,
+                                 void* stream) {
     if (M < 0 || M > kMaxDim || K <= 0 || K > kMaxDim || K % 32) return BL_ERR_SHAPE;
     if (fn < BL_FN_RELU || fn > BL_FN_SILU || (type != BL_F32 && type != BL_BF16) || K > kMaxNonlinearK)
         return BL_ERR_UNSUPPORTED;
     if (M == 0) return BL_OK;
+    if (!nonlinear_rows_ok(M, K)) return BL_ERR_UNSUPPORTED;
     if (!dXhat || !check || !check_scale || !dU) return BL_ERR_NULL;
+    if (!aligned16(dXhat, check, (const char*)dU)) return BL_ERR_UNSUPPORTED;
     NonlinearArgs a{};
     a.dXhat = dXhat; a.check = const_cast<int8_t*>(check); a.check_scale = const_cast<float*>(check_scale);
     a.M = M; a.K = K; a.eps = ln_eps; a.rows = rows; a.dU = dU; a.bf16 = type == BL_BF16;

@@ -108,6 +108,11 @@ size_t experts_backward_bytes(int64_t T, int64_t N, int64_t K, int E);
 hipError_t launch_experts_backward(const ExpertsArgs& a, hipStream_t s);
 
 #ifdef __HIPCC__
+__device__ inline uint32_t bf16_word(float lo, float hi) {  // to nearest, ties to even
+    typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
+    const v2bf v = {(__bf16)lo, (__bf16)hi};
+    return __builtin_bit_cast(uint32_t, v);
+}
 // Segments come from memory: what is read of them is held to 0 .. T, so that no value of theirs leads out of a tensor.
 __device__ inline int slot_bound(const int32_t* offsets, int e, int T) {
     const int v = offsets[e];

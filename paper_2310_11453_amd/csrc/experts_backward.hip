@@ -39,11 +39,6 @@ struct Args {
 };
 }  // namespace exb
 
-__device__ inline uint32_t to_bf16(float v) {
-    uint32_t u = __float_as_uint(v);
-    u += 0x7fffu + ((u >> 16) & 1u);
-    return u >> 16;
-}
 // (block_offset of backward.hip)
 __device__ inline int64_t copy_offset(int64_t row, int64_t r, int64_t R) {
     return ((r >> 5) * R + row) * 32 + (r & 31);
@@ -100,7 +95,7 @@ __device__ inline void copy_tile(const exb::Args& a, const ExpertTiles& count, i
         if constexpr (CODES) {
             const uint32_t lo = v[it][0], hi = v[it][1];
             auto pair = [](uint32_t w, int sh) {
-                return to_bf16((float)(int8_t)(w >> sh)) | to_bf16((float)(int8_t)(w >> (sh + 8))) << 16;
+                return bf16_word((float)(int8_t)(w >> sh), (float)(int8_t)(w >> (sh + 8)));
             };
             v[it][0] = pair(lo, 0), v[it][1] = pair(lo, 16), v[it][2] = pair(hi, 0), v[it][3] = pair(hi, 16);
         } else {
@@ -111,8 +106,8 @@ __device__ inline void copy_tile(const exb::Args& a, const ExpertTiles& count, i
                 const float sc = gamma[it] / 128.0f;
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                    v[it][e] = to_bf16(__uint_as_float(v[it][e] << 16) * sc) |
-                               to_bf16(__uint_as_float(v[it][e] & 0xffff0000u) * sc) << 16;
+                    v[it][e] = bf16_word(__uint_as_float(v[it][e] << 16) * sc,
+                                         __uint_as_float(v[it][e] & 0xffff0000u) * sc);
             }
         }
         uint32_t* const t32 = reinterpret_cast<uint32_t*>(&tile[rl][cl]);

@@ -202,16 +202,12 @@ __global__ __launch_bounds__(1024) void nonlinear_fold(NonlinearArgs a) {
     __syncthreads();
     if (threadIdx.x >= kWave) return;
     most = fold_slots<NW>(sm, OpMax{});
-    if (threadIdx.x == 0) *a.gmax_bits = __float_as_uint(most);
+    if (threadIdx.x != 0) return;
+    *a.gmax_bits = __float_as_uint(most);
+    if (M <= 0) *a.gamma = 1e-5f;  // no row to write the lower bound of gamma
 }
 
 // ---- backward -----------------------------------------------------------------------------------------
-typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
-__device__ inline uint32_t bf16_word(float lo, float hi) {  // to nearest, ties to even
-    const v2bf v = {(__bf16)lo, (__bf16)hi};
-    return __builtin_bit_cast(uint32_t, v);
-}
-
 // One reading of the row: g, and of the checkpoint f(v) and f'(v), stay in registers; the four sums that the derivative
 // of the LayerNorm needs (of h, h^2, g and g h) are taken together.  With eight float4 a lane and 16 waves a row, which
 // have 128 registers, the pairs are evaluated a second time instead of kept (2000 x 28672: 473 us kept and spilled, 148

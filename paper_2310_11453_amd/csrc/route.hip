@@ -172,12 +172,6 @@ hipError_t launch_route(const RouteArgs& a, hipStream_t s) {
 }
 
 // ---- slots back to tokens ---------------------------------------------------------------------------
-__device__ inline uint32_t bf16_rne(float v) {
-    uint32_t u = __float_as_uint(v);
-    u += 0x7fffu + ((u >> 16) & 1u);
-    return u >> 16;
-}
-
 // A workgroup: a token and 256 pieces of its row, of four elements (VEC: N % 4 == 0) or one; items beyond the grid in
 // turn.
 template <bool VEC>
@@ -225,14 +219,13 @@ __device__ inline void combine_backward_token(const CombineArgs& a, int64_t t, f
             if constexpr (VEC) {
                 const float4 v = *reinterpret_cast<const float4*>(g);
                 *reinterpret_cast<uint2*>(a.dSlots + o) =
-                    make_uint2(bf16_rne(wt * v.x) | bf16_rne(wt * v.y) << 16,
-                               bf16_rne(wt * v.z) | bf16_rne(wt * v.w) << 16);
+                    make_uint2(bf16_word(wt * v.x, wt * v.y), bf16_word(wt * v.z, wt * v.w));
                 if (a.dWeights) {
                     const float4 y = *reinterpret_cast<const float4*>(a.slots + o);
                     dot += (v.x * y.x + v.y * y.y) + (v.z * y.z + v.w * y.w);
                 }
             } else {
-                a.dSlots[o] = (uint16_t)bf16_rne(wt * *g);
+                a.dSlots[o] = (uint16_t)bf16_word(wt * *g, 0.f);
                 if (a.dWeights) dot += *g * a.slots[o];
             }
         }

@@ -22,6 +22,7 @@ def lib(bl):
 
 
 ONE = ctypes.c_void_p(256)  # never dereferenced: every call below fails, or has nothing to do, before a launch
+ODD = ctypes.c_void_p(264)  # as little, and not 16-byte aligned
 BIG = 1 << 40
 
 
@@ -33,6 +34,7 @@ def test_sizes(bl):
     assert bl.workspace_bytes_experts(bl.OP_QUANT_NONLINEAR, 100, 1, 0, 0, 0) == 0
     assert bl.workspace_bytes_experts(bl.OP_QUANT_NONLINEAR, 100, 1, 0, 0, 0, True) >= 100 * 16 + 4
     assert bl.workspace_bytes_experts(bl.OP_BACKWARD, 100, 2, 512, 256, 8) > 0
+    assert bl.workspace_bytes_experts(bl.OP_QUANT_NONLINEAR, 1 << 24, 1, 0, 0, 0, True) == 0
     for bad in [(bl.OP_ROUTE, -1, 2, 0, 0, 8), (bl.OP_ROUTE, (1 << 24) + 1, 1, 0, 0, 8), (bl.OP_ROUTE, 8, 2, 0, 0, 257),
                 (bl.OP_BACKWARD, 8, 2, 512, 250, 8), (bl.OP_BACKWARD, 8, 0, 512, 256, 8), (bl.OP_BACKWARD, 8, 2, 0, 256, 8),
                 (bl.OP_BACKWARD, 8, 2, 512, 65568, 8), (bl.OP_FORWARD, 8, 2, 512, 256, 8), (99, 8, 2, 512, 256, 8)]:
@@ -61,10 +63,12 @@ def test_product_refusals(lib):
     assert product(lib, E=257) == -2 and product(lib, top_k=0) == -2 and product(lib, M=1 << 30, top_k=2) == -2
     assert product(lib, gran=2) == -3 and product(lib, flags=1) == -3 and product(lib, K=65568) == -3
     assert product(lib, codes=None) == -1 and product(lib, offsets=None) == -1 and product(lib, Y=None) == -1
+    assert product(lib, codes=ODD) == -3
     assert product(lib, M=0, codes=None, offsets=None, Y=None) == 0
 
 
-def backward(lib, M=8, top_k=2, N=48, K=64, gran=0, E=4, dY=ONE, codes=ONE, packed=ONE, dX=ONE, dW=ONE, ws=ONE, ws_bytes=BIG):
+def backward(lib, M=8, top_k=2, N=48, K=64, gran=0, E=4, dY=ONE, codes=ONE, packed=ONE, dX=ONE, dW=ONE, ws=ONE,
+             ws_bytes=BIG):
     return lib.bitlinear_backward_ste_experts(dY, M, top_k, N, K, codes, ONE, gran, ONE, ONE, E, packed, ONE, dX, dW, ws,
                                               ws_bytes, None)
 
@@ -73,6 +77,10 @@ def test_backward_refusals(lib, bl):
     assert backward(lib, K=40) == -2 and backward(lib, M=-1) == -2 and backward(lib, E=0) == -2
     assert backward(lib, gran=7) == -3 and backward(lib, K=65568) == -3
     assert backward(lib, dY=None) == -1 and backward(lib, packed=None) == -1 and backward(lib, codes=None) == -1
+    assert backward(lib, codes=ODD) == -3 and backward(lib, packed=ODD) == -3
+    # dY is read 16 bytes at a time where its rows are whole numbers of 32 columns and there is a dX; else not
+    assert backward(lib, N=64, dY=ODD) == -3
+    assert backward(lib, N=64, dY=ODD, dX=None, ws=None) == -4 and backward(lib, N=48, dY=ODD, ws=None) == -4
     need = bl.workspace_bytes_experts(bl.OP_BACKWARD, 8, 2, 48, 64, 4)
     assert backward(lib, ws=None, ws_bytes=0) == -4 and backward(lib, ws_bytes=need // 2) == -4
     assert backward(lib, M=0, dY=None) == 0 and backward(lib, dX=None, dW=None, dY=None) == 0
@@ -102,8 +110,10 @@ def test_nonlinear_refusals(lib, bl):
         assert call(M=-1) == -2 and call(K=48) == -2 and call(K=0) == -2
         assert call(fn=4) == -3 and call(fn=-1) == -3 and call(K=32800) == -3
         assert call(M=0) == 0
+        assert call(M=1 << 24) == -3 and call(M=(1 << 24) - 1, K=4128) == -3
     assert fwd(gran=2) == -3 and fwd(U=None) == -1 and fwd(scale=None) == -1 and bwd(check=None) == -1 and bwd(dU=None) == -1
-    assert bwd(kind=2) == -3
+    assert bwd(kind=2) == -3 and bwd(dX=ODD) == -3 and bwd(dU=ODD) == -3 and bwd(check=ODD) == -3
+    assert fwd(U=ODD) == -3 and fwd(check=ODD) == -3 and fwd(gran=1, ws=ODD) == -3
     assert fwd(gran=1, ws=None, ws_bytes=0) == -4 and fwd(gran=1, ws_bytes=8 * 16) == -4
 
 

@@ -140,6 +140,30 @@ def test_products_when_no_choice_has_an_expert(bl, tuning, tile):
     check_products(bl, 50, 2, 4, 96, 64, True, False, np.full((50, 2), -1, np.int32))
 
 
+# as many experts as there may be: the last of them, and each kind of tiles
+@pytest.mark.parametrize("tile", TILES)
+def test_products_of_256_experts(bl, tuning, tile):
+    tuning(f"experts_tile={tile}")
+    for M, only in ((900, None), (60, [0, 63, 64, 255])):
+        print(f"products of 256 experts M={M} tile={tile}", flush=True)
+        check_products(bl, M, 2, 256, 96, 144, True, False, choices(M, 2, 256, M, 0.1, only=only))
+
+
+def test_products_of_more_than_4_gib_of_codes(bl):
+    """Offsets into the codes pass 32 bits.  Checked on slots from both ends and around the border."""
+    T, K, N = 65540, 65536, 40
+    codes = torch.randint(-128, 128, (T, K), dtype=torch.int8, device="cuda")
+    rowsum = torch.cat([c.sum(1, dtype=torch.int32) for c in codes.split(4096)])
+    W = torch.randn(2, N, K, device="cuda")
+    packed, _, beta = bl.bitlinear_pack_weights_experts(W)
+    signs = [torch.from_numpy(unpack(bl, packed[e], N, K)).double() for e in range(2)]
+    offsets = torch.tensor([0, 40000, T], dtype=torch.int32, device="cuda")
+    got = bl.bitlinear_matmul_experts(codes, torch.ones(1, device="cuda"), rowsum, packed, N, beta, offsets,
+                                      per_tensor=True, flags=bl.FLAG_OUT_ACC_I32).cpu()
+    for s in (0, 1, 32767, 32768, 39999, 40000, 65535, 65536, 65537, T - 1):
+        assert torch.equal(got[s].double(), signs[int(s >= 40000)] @ codes[s].cpu().double())
+
+
 def check_products(bl, M, top_k, E, K, N, gather, per_tensor, ids):
     c = make(bl, M, top_k, E, K, N, gather, per_tensor, ids)
     acc = torch.full((c["T"], N), 77, dtype=torch.int32)
@@ -233,7 +257,39 @@ def test_backward_when_one_expert_has_all_slots(bl, M, only):
     check_backward(bl, M, 2, 5, 160, 136, True, True, choices(M, 2, 5, M, only=only))
 
 
-def check_backward(bl, M, top_k, E, K, N, gather, per_tensor, ids, integers=False):
+@pytest.mark.parametrize("per_tensor", [True, False])
+def test_backward_of_256_experts(bl, per_tensor):
+    check_backward(bl, 700, 2, 256, 64, 40, True, per_tensor, choices(700, 2, 256, 3, unrouted=0.1))
+
+
+@pytest.mark.parametrize("spec", ["", "bwd_splits=4", "bwd_ring=1", "bwd_ring=2"])
+def test_backward_when_nothing_is_routed(bl, tuning, spec):
+    """dW is zero whatever a gamma that no row has set holds; dX is left as it was."""
+    tuning(spec)
+    c = make(bl, 30, 2, 3, 96, 64, True, True, np.full((30, 2), -1, np.int32))
+    dY = torch.full((60, 64), float("nan"), device="cuda").to(torch.bfloat16)
+    _, dw = bl.bitlinear_backward_ste_experts(dY, c["codes"].cuda(), torch.full((1,), float("nan"), device="cuda"),
+                                              c["packed"], c["beta"], **c["calls"])
+    assert bool((dw == 0).all())
+
+
+def test_nothing_to_do(bl):
+    """No tokens: empty results, and a gradient of zeros for the weights."""
+    E, K, N, top_k = 3, 64, 48, 2
+    packed, _, beta = bl.bitlinear_pack_weights_experts(torch.randn(E, N, K, device="cuda"))
+    order, position, offsets = bl.bitlinear_route(torch.empty(0, top_k, dtype=torch.int32, device="cuda"), E)
+    codes, gamma, rowsum, check, scale = bl.bitlinear_quant_nonlinear(torch.empty(0, K, device="cuda"), checkpoint=True)
+    assert check.shape == (0, K) and scale.shape == (0, 1)
+    y = bl.bitlinear_matmul_experts(codes, gamma, rowsum, packed, N, beta, offsets, order, top_k)
+    assert y.shape == (0, N) and bl.bitlinear_combine(y, position).shape == (0, N)
+    dy, dw = bl.bitlinear_combine_backward(torch.empty(0, N, device="cuda"), y, position)
+    assert dy.shape == (0, N) and dw.shape == (0, top_k)
+    dX, dW = bl.bitlinear_backward_ste_experts(dy, codes, gamma, packed, beta, offsets, order, top_k)
+    assert dX.shape == (0, K) and bool((dW == 0).all()) and dW.shape == (E, N, K)
+    assert bl.bitlinear_nonlinear_backward(torch.empty(0, K, device="cuda"), check, scale).shape == (0, K)
+
+
+def check_backward(bl, M, top_k, E, K, N, gather, per_tensor, ids):
     c = make(bl, M, top_k, E, K, N, gather, per_tensor, ids)
     g = torch.Generator().manual_seed(7)
     dY = torch.randn(c["T"], N, generator=g).to(torch.bfloat16)
@@ -309,6 +365,15 @@ def test_combine_and_its_gradient(bl, M, top_k, N, weighted, unrouted):
     assert bool(((dw.cpu().double() - dots.sum(2)).abs() <= (N + 1) * F32 * dots.abs().sum(2)).all())
     again, none = bl.bitlinear_combine_backward(dY.cuda(), None, pos, wd, out=torch.full_like(out, 5.0))
     assert none is None and torch.equal(again, dslots)
+
+
+def test_combine_keeps_nan(bl):
+    """A gradient that is not a number stays none in bf16, whatever its payload."""
+    bits = torch.tensor([0x7fffffff, 0x7fc00000, -1, 0x7f800001], dtype=torch.int64).to(torch.int32).cuda()
+    dY = bits.view(torch.float32).repeat(3, 2)  # rows of eight, and of one by one
+    pos = torch.arange(3, dtype=torch.int32, device="cuda").view(3, 1)
+    for g in (dY, dY[:, :7].contiguous()):
+        assert bool(bl.bitlinear_combine_backward(g, None, pos)[0].isnan().all())
 
 
 def test_combine_at_any_alignment(bl):

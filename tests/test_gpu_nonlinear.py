@@ -210,6 +210,8 @@ def test_rows_behind_the_last_are_left_alone(bl, per_tensor):
             for a, b in zip((codes, rowsum, check, scale), (ref[0], ref[2], ref[3], ref[4])):
                 assert torch.equal(a[:n], b)
             assert torch.equal(gamma[: ref[1].numel()], ref[1])
+        elif per_tensor:
+            assert float(gamma) == torch.tensor(1e-5).item()  # its lower bound
         for t in (codes, rowsum, check, scale):
             assert bool((t[n:] == 9).all())
         if not per_tensor:
