@@ -1,7 +1,7 @@
 #!/usr/bin/env python3
 """Benchmark of the BitLinear hot path on one MI355X.
 
-    python bench.py [--gpus 1] [--steps K] [--warmup W] [--no-cpu] [--no-decode] [--no-train] [--no-prefill-30b]
+    python bench.py [--gpus 1] [--steps K] [--warmup W] [--no-cpu] [--no-decode] [--no-train] [--no-experts] [--no-prefill-30b]
 
 Workload at one GPU: the BitNet-6.7B-shaped prefill pair (4096->16384 and 16384->4096 at
 M = 2048 tokens, activations N(0,1) with 0.1 % outliers x20, weights N(0, 0.02^2)).
@@ -14,7 +14,8 @@ Prints ONE JSON line.  `value` is prefill TOPS (2*M*N*K summed over the step / s
 `roofline` describes the dominant kernel (the MFMA GEMM) from HIP-event timing of that
 kernel alone inside the timed loop; `decode` reports the packed-weight streaming rate of
 the small-M kernel on BitNet-30B-shaped layers; `training` times one forward + straight-through
-backward of the 4096->16384 layer at M = 8192; `cpu_baseline` times the CPU oracle on a bounded
+backward of the 4096->16384 layer at M = 8192; `experts` times a feed-forward network of eight
+BitLinear experts, two a token, at decoding batches and in a training step; `cpu_baseline` times the CPU oracle on a bounded
 sample of the same workload on this machine's host cores.
 """
 from __future__ import annotations
@@ -257,6 +258,81 @@ def decode_stacks(bl, torch, dev, decode):
         del stack, protos3, bufs3, wss3
 
 
+def experts_leg(bl, torch, dev):
+    """A feed-forward network of experts (2048 -> 8192 -> 2048, eight of them, two a token): one layer of a decoding
+    step, its packed weights not in a cache, and a training step from fp32 weights.  Returns (figures, whether the slots'
+    products agree with the plain layer's, bit for bit)."""
+    E, top_k, d, width, fn = 8, 2, 2048, 8192, "gelu"
+    g = torch.Generator(device=dev).manual_seed(11)
+    W1 = torch.randn(E, width, d, generator=g, device=dev) * 0.02
+    W2 = torch.randn(E, d, width, generator=g, device=dev) * 0.02
+    up, down = bl.bitlinear_pack_weights_experts(W1), bl.bitlinear_pack_weights_experts(W2)
+    nbytes = up[0].numel() + down[0].numel()
+    ncopy = int(np.ceil(512e6 / nbytes))  # more than L2 + Infinity Cache
+    ups, downs = ([p[0].clone() for _ in range(ncopy)] for p in (up, down))
+
+    def batch(M):
+        score = torch.randn(M, E, generator=g, device=dev)
+        weights, ids = score.softmax(1).topk(top_k, 1)
+        return torch.randn(M, d, generator=g, device=dev), ids.int(), weights.contiguous()
+
+    def forward(X, ids, weights, p1, p2, per_tensor, train):
+        order, position, offsets = bl.bitlinear_route(ids, E)
+        q1, g1, r1, _ = bl.bitlinear_quant_act(X, per_tensor=per_tensor)
+        u = bl.bitlinear_matmul_experts(q1, g1, r1, p1, width, up[2], offsets, order, top_k, per_tensor)
+        q2, g2, r2, check, scale = bl.bitlinear_quant_nonlinear(u, fn, per_tensor=per_tensor, checkpoint=train,
+                                                                rows=offsets[E:])
+        y = bl.bitlinear_matmul_experts(q2, g2, r2, p2, d, down[2], offsets, per_tensor=per_tensor)
+        return bl.bitlinear_combine(y, position, weights), (order, position, offsets, q1, g1, r1, u, q2, g2, check, scale, y)
+
+    ok, shapes = True, []
+    for M in (1, 16, 64):
+        X, ids, weights = batch(M)
+        _, (order, _, offsets, q1, g1, r1, u, *_) = forward(X, ids, weights, up[0], down[0], False, False)
+        for e, (a, b) in enumerate(zip(offsets.tolist(), offsets.tolist()[1:])):
+            if a < b:
+                rows = (order[a:b] // top_k).long()
+                ref = bl.bitlinear_matmul(q1[rows].contiguous(), g1[rows].contiguous(), r1[rows].contiguous(),
+                                          up[0][e], width, up[2][e:e + 1].contiguous())
+                ok = ok and torch.equal(u[a:b], ref)
+        t, mode = graph_ms(lambda i: forward(X, ids, weights, ups[i % ncopy], downs[i % ncopy], False, False),
+                           2 * ncopy, 5, torch)
+        used = int((offsets[1:] > offsets[:-1]).sum())  # experts that anybody chose
+        shapes.append(dict(M=M, us=t * 1e3, experts_read=used, gbs=used * nbytes / E / (t * 1e-3) / 1e9, timing=mode))
+
+    M = 4096
+    X, ids, weights = batch(M)
+    dY = torch.randn(M, d, generator=g, device=dev) * 1e-3
+    st = {}
+
+    def t_pack():
+        st["up"], st["down"] = bl.bitlinear_pack_weights_experts(W1), bl.bitlinear_pack_weights_experts(W2)
+
+    def t_fwd():
+        st["Y"], st["kept"] = forward(X, ids, weights, st["up"][0], st["down"][0], True, True)
+
+    def t_bwd():
+        order, position, offsets, q1, g1, _, _, q2, g2, check, scale, y = st["kept"]
+        dy, _ = bl.bitlinear_combine_backward(dY, y, position, weights)
+        dx2, st["dW2"] = bl.bitlinear_backward_ste_experts(dy, q2, g2, st["down"][0], down[2], offsets, per_tensor=True)
+        du = bl.bitlinear_nonlinear_backward(dx2, check, scale, fn, rows=offsets[E:])
+        dx1, st["dW1"] = bl.bitlinear_backward_ste_experts(du, q1, g1, st["up"][0], up[2], offsets, order, top_k, True)
+        st["dX"] = bl.bitlinear_layernorm_backward(bl.bitlinear_combine(dx1, position), X)
+
+    def t_all():
+        t_pack(), t_fwd(), t_bwd()
+
+    t_all(), t_all()
+    torch.cuda.synchronize()
+    parts = {n: event_ms(f, 5, torch) for n, f in
+             (("pack_ms", t_pack), ("forward_ms", t_fwd), ("backward_ms", t_bwd), ("step_ms", t_all))}
+    flops = 2 * 2.0 * M * top_k * d * width  # of both products
+    return dict(workload="experts: 8 x (2048 -> 8192 -> 2048), two a token, gelu; decode: quantiser, routing, both "
+                         "products, function and quantiser, combination; training: M = 4096, one gamma a tensor",
+                decode=shapes, training=dict(parts, forward_tops=flops / (parts["forward_ms"] * 1e-3) / 1e12,
+                                             backward_tflops=2 * flops / (parts["backward_ms"] * 1e-3) / 1e12)), ok
+
+
 def main():
     ap = argparse.ArgumentParser()
     ap.add_argument("--gpus", type=int, default=1)
@@ -265,6 +341,7 @@ def main():
     ap.add_argument("--no-cpu", action="store_true", help="skip the CPU-oracle baseline leg")
     ap.add_argument("--no-decode", action="store_true", help="skip the decode streaming leg")
     ap.add_argument("--no-train", action="store_true", help="skip the training-step leg")
+    ap.add_argument("--no-experts", action="store_true", help="skip the leg of the mixture of experts")
     ap.add_argument("--no-prefill-30b", action="store_true",
                     help="skip the 30B layers at M = 4096 (they run the 6.7B step's GEMM kernel at another "
                          "size: a per-kernel profile of the step wants them out)")
@@ -567,6 +644,13 @@ def main():
                           "transpose, two bf16 MFMA GEMMs")
         del W4, X4, dY4, Y4, wsb, st4
 
+    # ---- mixture-of-experts leg: one feed-forward layer, decoding and training -----------------
+    experts = None
+    if not args.no_experts:
+        experts, same = experts_leg(bl, torch, dev)
+        if not same:
+            parity = "FAILED"
+
     # ---- CPU oracle on a bounded sample of the same workload ---------------------------------
     # The same step (LN, quantise, integer GEMM, dequant through both layers) on the first
     # s_rows tokens, repeated `reps` times, sized from a small calibration run to about
@@ -628,7 +712,8 @@ def main():
                                "16384->4096, M=2048, per-token gamma, fp32 in/out",
                    "step": "LN+quantise+GEMM+dequant for both layers; weights packed beforehand"},
         "mfma_frac_of_peak": tops / I8_MFMA_PEAK_TOPS,
-        "kernels": kern, "roofline": roof, "weight_prep": prep, "decode": decode, "training": train, "energy_model": energy_model,
+        "kernels": kern, "roofline": roof, "weight_prep": prep, "decode": decode, "training": train,
+        "experts": experts, "energy_model": energy_model,
         "cpu_baseline": cpu, "parity": parity,
     }
     if parity != "ok":  # no number without parity
