@@ -118,10 +118,10 @@ __device__ inline int slot_bound(const int32_t* offsets, int e, int T) {
     const int v = offsets[e];
     return v < 0 ? 0 : v < T ? v : T;
 }
+__device__ inline uint32_t row_of(uint32_t r, uint32_t rows) { return r < rows ? r : rows - 1; }
 // the row of the codes that slot s reads
 __device__ inline uint32_t code_row(const int32_t* order, uint32_t top_k, uint32_t rows, uint32_t s) {
-    const uint32_t r = order ? (uint32_t)order[s] / top_k : s;
-    return r < rows ? r : rows - 1;
+    return row_of(order ? (uint32_t)order[s] / top_k : s, rows);
 }
 
 // Rows of tiles of BM slots: expert e has those from first[e] on, its slots are from[e] .. to[e] - 1.

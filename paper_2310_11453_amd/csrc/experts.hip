@@ -30,9 +30,11 @@ struct Args {
 // takes the 512-chunks w, w + W, ... of K; the weights are the row operand of v_mfma_i32_16x16x64_i8, the slots its
 // columns; a lane's 16 bytes of a packed tile hold 16 consecutive k of each of eight bit planes, (w >> i) & 0x01010101
 // is plane i as {0,1} bytes, and sum_k q s = 2 sum_k q b - sum_k q.  The waves' sums meet in LDS.
-// A launch is a chain of trips to memory: the experts' bounds, then the weights and (in two trips) the codes, whose
-// rows are known only with the order.  So the first chunk's weights are requested as soon as the expert is known and
-// the epilogue's operands with the codes.
+// A launch is a chain of trips to memory: the experts' bounds, then the weights and (in two trips) the codes, whose rows
+// are known only with the order.  Loads return in the order of their requests, so the order is asked for first, then a
+// quarter of the first chunk's weights, then the codes, which are what the matrix instructions wait for, then the rest of
+// the weights, which arrive while the first tiles are multiplied.  (All weights ahead of the order, and so of everything:
+// 96 slots, 16 experts, 4096 -> 4096 13.4 us a call, 11.7 so; 64, 32, 6144 -> 2048 13.9, 11.7.)
 template <int TILES>
 __global__ __launch_bounds__(rows::kMaxWaves* kWave) void experts_rows_kernel(rows::Args a) {
     using namespace rows;
@@ -67,20 +69,24 @@ __global__ __launch_bounds__(rows::kMaxWaves* kWave) void experts_rows_kernel(ro
     }
     if (e < 0) return;  // uniform: the grid is a bound
 
+    constexpr int kFirst = TILES > 4 ? TILES / 4 : 1;
     const uint32_t t0 = blockIdx.x * TILES, last = a.TN - 1;
     const uint32_t* const wbase = a.packed + e * a.blob;
-    auto load = [&](v4i (&q)[TILES], uint32_t c) {
+    auto load = [&](v4i (&q)[TILES], uint32_t c, int from, int to) {
 #pragma unroll
-        for (int t = 0; t < TILES; ++t) {
+        for (int t = from; t < to; ++t) {
             const uint32_t tn = t0 + t < last ? t0 + t : last;
             const uint32_t* const at = wbase + ((uint64_t)tn * a.TK + c) * 256 + l * 4;
             q[t] = __builtin_nontemporal_load(reinterpret_cast<const v4i*>(at));
         }
     };
     v4i q[TILES];
-    load(q, w);
     const int s = s0 + col < s1 ? s0 + col : s1 - 1;
-    const uint32_t row = code_row(a.order, a.top_k, a.rows, (uint32_t)s);
+    const int place = a.order ? a.order[s] : 0;
+    __builtin_amdgcn_sched_barrier(0);
+    load(q, w, 0, kFirst);
+    __builtin_amdgcn_sched_barrier(0);
+    const uint32_t row = row_of(a.order ? (uint32_t)place / a.top_k : (uint32_t)s, a.rows);
     const int8_t* const x = a.codes + (uint64_t)row * a.K + 16 * g;
     const int klast = (int)a.K - 16 - 16 * g;  // past the row its last 16 bytes again: the packed bits there are zero
     float gamma = 0.f;
@@ -92,14 +98,14 @@ __global__ __launch_bounds__(rows::kMaxWaves* kWave) void experts_rows_kernel(ro
     const float beta = a.beta[e];
 
     v4i acc[TILES] = {};
-    for (uint32_t c = w; c < a.TK; c += W) {
-        v4i act[8];
+    auto chunk = [&](v4i (&act)[8], uint32_t c) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const int k = (int)c * kChunkK + 64 * i;
             act[i] = *reinterpret_cast<const v4i*>(x + (k < klast ? k : klast));
         }
-        if (c != (uint32_t)w) load(q, c);
+    };
+    auto multiply = [&](const v4i(&act)[8]) {
 #pragma unroll
         for (int t = 0; t < TILES; ++t)
 #pragma unroll
@@ -109,6 +115,19 @@ __global__ __launch_bounds__(rows::kMaxWaves* kWave) void experts_rows_kernel(ro
                 for (int d = 0; d < 4; ++d) b[d] = (int)(((uint32_t)q[t][d] >> i) & 0x01010101u);
                 acc[t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(b, act[i], acc[t], 0, 0, 0);
             }
+    };
+    v4i act[8];
+    chunk(act, w);
+    __builtin_amdgcn_sched_barrier(0);
+    load(q, w, kFirst, TILES);
+    __builtin_amdgcn_sched_barrier(0);
+    multiply(act);
+    for (uint32_t c = w + W; c < a.TK; c += W) {
+        chunk(act, c);
+        __builtin_amdgcn_sched_barrier(0);
+        load(q, c, 0, TILES);
+        __builtin_amdgcn_sched_barrier(0);
+        multiply(act);
     }
     // lane: slot col, weight rows 4 g + r of each tile
 #pragma unroll
@@ -138,12 +157,12 @@ static void launch_rows(const ExpertsArgs& a, hipStream_t s) {
     const int64_t TN = tiles_n(a.N), TK = tiles_k(a.K);
     const int64_t A = a.T < a.E ? a.T : a.E, blocks = a.T / rows::kSlots + A;
     // Tiles of a workgroup: more of them share the fixed chain and the codes, fewer leave no CU idle; eight leave two
-    // workgroups of a long reduction on a CU.  us with 2 / 4 / 8, T slots of E experts: T = 32, E = 8, 2048 -> 2048 5.5
-    // / 6.1 / 7.4, 8192 -> 2048 9.7 / 8.4 / 10.9; T = 64, E = 32, 6144 -> 2048 18.2 / 15.8 / 14.2; T = 128, E = 32,
-    // 4096 -> 5120 32.1 / 26.1 / 25.0; T = 128, E = 16, 2048 -> 8192 18.3 / 16.4 / 17.7.
+    // workgroups of a long reduction on a CU.  us with 2 / 4 / 8, T slots of E experts: T = 8, E = 8, 4096 -> 1024 4.3 /
+    // 4.7 / 5.7, 4096 -> 2048 5.1 / 4.9 / 5.8; T = 128, E = 16, 4096 -> 1024 6.3 / 5.8 / 7.0, 2048 -> 8192 17.4 / 14.4 /
+    // 15.3; T = 64, E = 32, 6144 -> 2048 17.5 / 14.8 / 11.7; T = 128, E = 32, 4096 -> 5120 34.4 / 27.6 / 21.9.
     int tiles = tuning().decode_tiles;
     const int64_t all = blocks * TN;
-    if (!tiles) tiles = all < 512 ? 1 : all < 1280 || TK < 4 ? 2 : TK >= 8 && all > 4096 ? 8 : 4;
+    if (!tiles) tiles = all < 512 ? 1 : all < 1024 || TK < 4 ? 2 : TK >= 8 && all >= 2048 ? 8 : 4;
     rows::Args r{};
     r.codes = a.codes; r.packed = a.packed; r.offsets = a.offsets; r.order = a.order;
     r.T = (uint32_t)a.T; r.E = (uint32_t)a.E; r.top_k = (uint32_t)a.top_k; r.rows = (uint32_t)a.rows;
@@ -171,10 +190,10 @@ static void launch_rows(const ExpertsArgs& a, hipStream_t s) {
 //   256 x 256        -3.5 + rounds (17.5 + 0.62 n)
 //   128 x 128         0.2 + rounds (6.8 + 2.84 c / 2)
 //   64 x 128          0.6 + rounds (5.75 + 3.14 c / 4)
-//   16 slots at a time  2.8 + 1.3 c / 8 + (0.06 c + 0.19) per 16 x 16 outputs and CU
-// 0.9 % slower than the best of the five on average, 21 % at most (118 slots, 3 experts, 3232 -> 7902: 16.2, 13.4 as 64
-// x 128).  The extremes, 16 slots at a time / 128 x 256: 64 slots, 8 experts, 4096 -> 4096 10.0 / 29; 8900 slots, 12
-// experts, 3840 -> 4808 787 / 181.
+//   16 slots at a time  2.7 + 1.4 c / 8 + (0.05 c + 0.2) per 16 x 16 outputs and CU
+// 0.5 % slower than the best of the five on average over 210 more, 23 % at most (1552 slots, 6 experts, 3296 -> 1155:
+// 24.2, 19.6 as 128 x 128).  The extremes, 16 slots at a time / 128 x 256: 64 slots, 8 experts, 4096 -> 4096 10.0 / 29;
+// 8900 slots, 12 experts, 3840 -> 4808 787 / 181.
 static int experts_plan(const ExpertsArgs& a) {
     const double cus = num_cus(), T = (double)a.T, A = (double)(a.T < a.E ? a.T : a.E);
     const double c = (double)tiles_k(a.K), n = (double)((a.K + 63) / 64);
@@ -187,7 +206,7 @@ static int experts_plan(const ExpertsArgs& a) {
     const double us[5] = {0.3 + rounds(128, 256) * (7.3 + 0.37 * n), -3.5 + rounds(256, 256) * (17.5 + 0.62 * n),
                           0.2 + rounds(128, 128) * (6.8 + 2.84 * up(c / 2)),
                           0.6 + rounds(64, 128) * (5.75 + 3.14 * up(c / 4)),
-                          2.8 + 1.3 * up(c / 8) + (0.06 * c + 0.19) * small};
+                          2.7 + 1.4 * up(c / 8) + (0.05 * c + 0.2) * small};
     return 1 + (int)(std::min_element(us, us + 5) - us);
 }
 
