@@ -5,7 +5,7 @@
 // products), every operand is first written once in the layout they read:
 //   g    [T][Np]       rows of dY                                 (A operand of dX, reduction over N; not where N is a
 //                      multiple of 32: the product reads dY itself, at the same speed, and the copies for 8192 slots
-//                      2048 -> 8192 take 86 us instead of 105)
+//                      2048 -> 8192 take 81 us instead of 100)
 //   Sw   [E][Np/32][K] the signs of 32 weight rows of a column    (B operand of dX)
 //   gwT  [N][slots]    dY transposed, with a gamma per token scaled and rounded again   (A operand of dW)
 //   qT   [K][slots]    codes transposed, gathered through the order                     (B operand of dW)
