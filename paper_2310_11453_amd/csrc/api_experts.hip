@@ -32,7 +32,7 @@ bool experts_ok(int experts) { return experts >= 1 && experts <= kMaxExperts; }
 
 size_t route_bytes(int64_t T, int experts) {
     const int64_t blocks = route_blocks(T);
-    return blocks > 1 ? align256((size_t)blocks * experts * 4) : 0;
+    return blocks > 1 ? align256((size_t)(blocks + 1) * experts * 4) : 0;
 }
 
 // what both products check and describe alike

@@ -15,7 +15,7 @@ struct RouteArgs {
     const int32_t* expert;  // [T]
     uint32_t T, E;
     int32_t *order, *position, *offsets;
-    uint32_t* counts;  // [route_blocks][E], several blocks only
+    uint32_t* counts;  // [route_blocks][E] and behind them [E], several blocks only
 };
 int64_t route_blocks(int64_t T);
 hipError_t launch_route(const RouteArgs& a, hipStream_t s);

@@ -13,6 +13,7 @@ namespace bl {
 namespace route {
 constexpr int kRowsWave = 4;  // rows of 64 choices of a wave
 constexpr int kSmall = 256, kLarge = 1024;  // threads of a workgroup: up to 1024 choices, and more
+constexpr int kScan = 256, kScanned = 64;   // threads of the scan, and the workgroups above which there is one
 constexpr int chunk(int threads) { return threads * kRowsWave; }
 }  // namespace route
 
@@ -52,6 +53,36 @@ __global__ __launch_bounds__(route::kLarge) void route_count_kernel(RouteArgs a,
     if (threadIdx.x < a.E) a.counts[blockIdx.x * a.E + threadIdx.x] = sums[threadIdx.x];
 }
 
+// Of many workgroups' counts, where each workgroup's choices of an expert begin inside the expert, in place of the count,
+// and how many the expert has, behind them.  blockIdx.x: the expert.  (Each workgroup adding up what it needs is
+// quadratic in their number: 16777216 choices of 64 experts 779 us a call so, 134 with this, 4194304 83 and 48, 1048576
+// 29 and 27, and it would be a launch for nothing at 262144, 23.)
+__global__ __launch_bounds__(route::kScan) void route_scan_kernel(RouteArgs a, int blocks) {
+    using namespace route;
+    constexpr int kMost = (int)(kMaxRouteSlots / chunk(kLarge) / kScan);  // counts of a thread
+    __shared__ int ends[kScan / kWave];
+    const int per = (blocks + kScan - 1) / kScan, b0 = (int)threadIdx.x * per;
+    uint32_t* const at = a.counts + blockIdx.x;
+    uint32_t v[kMost];
+    uint32_t sum = 0;
+#pragma unroll
+    for (int i = 0; i < kMost; ++i) {
+        v[i] = i < per && b0 + i < blocks ? at[(int64_t)(b0 + i) * a.E] : 0;
+        sum += v[i];
+    }
+    const int end = wave_sums((int)sum), w = (int)threadIdx.x / kWave;
+    if (threadIdx.x % kWave == kWave - 1) ends[w] = end;
+    __syncthreads();
+    uint32_t before = (uint32_t)end - sum;
+    for (int i = 0; i < w; ++i) before += (uint32_t)ends[i];
+#pragma unroll
+    for (int i = 0; i < kMost; ++i) {
+        if (i < per && b0 + i < blocks) at[(int64_t)(b0 + i) * a.E] = before;
+        before += v[i];
+    }
+    if (threadIdx.x == kScan - 1) at[(int64_t)blocks * a.E] = before;
+}
+
 // The place of a choice inside its expert is the number of earlier choices of that expert: of earlier workgroups
 // (counts), of earlier rows of 64 of this workgroup (cnt, summed down the rows) and of lower lanes of its row (a ballot
 // for each bit of the expert's number).  Nothing depends on which wave is first.  Thread (p, e) sums a part of the rows
@@ -75,7 +106,9 @@ __global__ __launch_bounds__(THREADS) void route_kernel(RouteArgs a, int bits) {
     }
     const uint32_t e = threadIdx.x % kMaxExperts, p = threadIdx.x / kMaxExperts;
     uint32_t before = 0, all = 0;
-    if (gridDim.x > 1 && e < a.E) {
+    if (gridDim.x > kScanned) {
+        if (e < a.E && p == 0) before = a.counts[blockIdx.x * a.E + e], all = a.counts[gridDim.x * a.E + e];
+    } else if (gridDim.x > 1 && e < a.E) {
 #pragma unroll 4
         for (uint32_t b = p; b < gridDim.x; b += kParts) {
             const uint32_t c = a.counts[b * a.E + e];
@@ -166,6 +199,7 @@ hipError_t launch_route(const RouteArgs& a, hipStream_t s) {
     int bits = 0;
     while ((1u << bits) < a.E) ++bits;
     if (blocks > 1) route_count_kernel<<<blocks, kLarge, 0, s>>>(a, bits);
+    if (blocks > kScanned) route_scan_kernel<<<a.E, kScan, 0, s>>>(a, (int)blocks);
     if (a.T <= chunk(kSmall)) route_kernel<kSmall><<<1, kSmall, 0, s>>>(a, bits);
     else route_kernel<kLarge><<<blocks, kLarge, 0, s>>>(a, bits);
     return hipGetLastError();

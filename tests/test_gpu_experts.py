@@ -77,10 +77,10 @@ def unpack(bl, blob, N, K):
 
 
 # ---- routing ---------------------------------------------------------------------------------------
-# one choice; a row of 64 and its neighbours; a workgroup's 4096 and its neighbours; several workgroups; every expert
-# number of bits; experts that nobody chooses
+# one choice; a row of 64 and its neighbours; a workgroup's 4096 and its neighbours; several workgroups; around 64 of
+# them, above which their counts are scanned by a launch of its own; every expert number of bits; experts that nobody chooses
 ROUTES = [(1, 1, 1), (1, 2, 8), (63, 1, 3), (64, 1, 4), (65, 1, 5), (16, 4, 64), (333, 3, 7), (4096, 1, 16), (4097, 1, 17),
-          (2048, 2, 256), (5000, 8, 255), (8191, 8, 64), (70000, 2, 9)]
+          (2048, 2, 256), (5000, 8, 255), (8191, 8, 64), (70000, 2, 9), (131072, 2, 5), (131073, 2, 5), (400001, 1, 256)]
 
 
 @pytest.mark.parametrize("M,top_k,E", ROUTES)
