@@ -304,6 +304,8 @@ __device__ inline TailPlan tail_plan(int tiles, int x, int S, int stages, int sl
 // stage st+1 (s_waitcnt vmcnt(n), n counted by hand), meets the others at a bare s_barrier, and
 // the DMA of stage st+NS-1 goes to the buffer stage st-1 has left.
 //
+// T x TJ = 256 x 128 (experts): waves of 128 x 64, two workgroups per CU whose stores and barriers the other one's MFMAs
+// hide, where a tile has few stages; a ring of three stages is what fits twice.
 // Why four waves (T = 256).  With eight waves of 128 x 64 LDS sets the pace: every operand row is read by the
 // waves that share it, 96 KiB of reads and 32 KiB of DMA writes a stage, at 128 bytes a cycle as
 // long as the MFMAs of the stage take (1024 cycles).  128 x 128 waves read 64 KiB.  There is one wave
@@ -348,15 +350,32 @@ __device__ inline void wide_wait(v4i (&a)[2], v4i (&b)[2]) {
     asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(a[0]), "+v"(a[1]), "+v"(b[0]), "+v"(b[1]));
 }
 
-template <int T, int NS, bool SPLIT, bool EXP = false>
-__global__ __launch_bounds__(256, T == 256 ? 1 : 2) void gemm_tn_bf16_wide(const uint16_t* __restrict__ A,
+// 128 x 64 waves
+__device__ inline void wide_issue(v4i (&a)[4], v4i (&b)[2], uint32_t ad_a, uint32_t ad_b) {
+    asm volatile(
+        "ds_read_b128 %0, %6\n\t"
+        "ds_read_b128 %1, %6 offset:2048\n\t"
+        "ds_read_b128 %2, %6 offset:4096\n\t"
+        "ds_read_b128 %3, %6 offset:6144\n\t"
+        "ds_read_b128 %4, %7\n\t"
+        "ds_read_b128 %5, %7 offset:2048"
+        : "=&v"(a[0]), "=&v"(a[1]), "=&v"(a[2]), "=&v"(a[3]), "=&v"(b[0]), "=&v"(b[1])
+        : "v"(ad_a), "v"(ad_b));
+}
+__device__ inline void wide_wait(v4i (&a)[4], v4i (&b)[2]) {
+    asm volatile("s_waitcnt lgkmcnt(0)"
+                 : "+v"(a[0]), "+v"(a[1]), "+v"(a[2]), "+v"(a[3]), "+v"(b[0]), "+v"(b[1]));
+}
+
+template <int T, int NS, bool SPLIT, bool EXP = false, int TJ = T>
+__global__ __launch_bounds__(256, T + TJ == 512 ? 1 : 2) void gemm_tn_bf16_wide(const uint16_t* __restrict__ A,
                                                             const uint16_t* __restrict__ B,
                                                             int64_t I, int64_t J, int64_t Rp,
                                                             const float* __restrict__ scale_ptr,
                                                             float scale_mul, float* __restrict__ C,
                                                             int grid_i, int grid_j, int blk_i,
                                                             int blk_j, RingSlices sl, ExpertsRing ex) {
-    constexpr int BM = T, BN = T, WN = 2, THREADS = 256, WTM = T / 2, WTN = T / 2, MI = T / 64, NI = T / 64;
+    constexpr int BM = T, BN = TJ, WN = 2, THREADS = 256, WTM = T / 2, WTN = TJ / 2, MI = T / 64, NI = TJ / 64;
     constexpr int PA = BM * 4 / THREADS, PB = BN * 4 / THREADS, P = PA + PB;
     constexpr int A_BYTES = BM * 64, STAGE_BYTES = (BM + BN) * 64;
     static_assert((NS - 1) * P < 64, "vmcnt range");
@@ -452,15 +471,16 @@ __global__ __launch_bounds__(256, T == 256 ? 1 : 2) void gemm_tn_bf16_wide(const
     // stage `st` into ring slot st % NS; `src_st` is the stage whose bytes are read (== st, or
     // the last stage when st does not exist: the slot is filled with bytes nobody uses)
     // (piece q of A and of B)
-    static_assert(PA == PB && PA == MI, "one piece of each per row of MFMAs");
+    static_assert(PB <= PA && PA == MI, "a piece of A, and one of B or none, per row of MFMAs");
     auto issue_piece = [&](int st, int src_st, int q) {
         uint8_t* dst = sm + (st % NS) * STAGE_BYTES + lds_wave;
         __builtin_amdgcn_global_load_lds(
             (const void*)(baseA + src_st * I * 64 + goffA[q]),
             (__attribute__((address_space(3))) void*)(dst + q * THREADS * 16), 16, 0, 0);
-        __builtin_amdgcn_global_load_lds(
-            (const void*)(baseB + src_st * J * 64 + goffB[q]),
-            (__attribute__((address_space(3))) void*)(dst + A_BYTES + q * THREADS * 16), 16, 0, 0);
+        if (q < PB)
+            __builtin_amdgcn_global_load_lds(
+                (const void*)(baseB + src_st * J * 64 + goffB[q < PB ? q : 0]),
+                (__attribute__((address_space(3))) void*)(dst + A_BYTES + q * THREADS * 16), 16, 0, 0);
     };
     auto issue = [&](int st, int src_st) {
 #pragma unroll
@@ -562,7 +582,7 @@ __global__ __launch_bounds__(256, T == 256 ? 1 : 2) void gemm_tn_bf16_wide(const
         {
             const int64_t ib = i0 + __builtin_amdgcn_readfirstlane(wm * WTM);
             const int64_t jb = j0 + __builtin_amdgcn_readfirstlane(wn * WTN);
-            if constexpr (T < 256) {
+            if constexpr (MI * NI < 16) {
                 store_tile<MI, NI, true>(Cs + ib * J + jb, J, I - ib, J - jb, j, g2, [](int, int) {},
                                          [&](int mi, int r, int s) { return sc * acc[mi][s][r]; });
             } else  // with 256 accumulators the walk of store_tile spills 29 registers and gains nothing
@@ -1222,7 +1242,7 @@ __global__ __launch_bounds__(256) void fold_expert_weights(const float* __restri
 // average length.
 ExpertsBackwardPlan experts_backward_plan(int64_t T, int64_t N, int64_t K, int E) {
     constexpr RingCost kDxWide{0.615, 12.0, 5.0, 6.0}, kDxRows{0.33, 5.0, 5.0, 6.0}, kDxAlone{0.39, 2.0, 5.0, 6.0};
-    constexpr RingCost kDwWide{0.68, 12.8, 5.0, 6.0}, kDwSmall{0.172, 2.3, 5.0, 6.0}, kDwAlone{0.226, 3.6, 5.0, 6.0};
+    constexpr RingCost kDwSmall{0.172, 2.3, 5.0, 6.0}, kDwAlone{0.226, 3.6, 5.0, 6.0};
     const Tuning& t = tuning();
     const double cus = ring_cus(), A = (double)(T < E ? T : E);
     auto tiles_of = [](int64_t v, int64_t b) { return (double)((v + b - 1) / b); };
@@ -1251,21 +1271,23 @@ ExpertsBackwardPlan experts_backward_plan(int64_t T, int64_t N, int64_t K, int E
                          (n > 1 ? 5.0 + (wide ? 0.1 : 0.05) * tail * n : 0.0);
         if (v < dx_us) dx_us = v, p.dx_tile = tile, p.dx_slices = !cut ? 1 : force ? force : 16;
     }
-    for (int tile = 1; tile <= 2; ++tile)
-        for (int n = 1; n <= 16; n *= 2) {
-            const bool wide = tile == 1;
-            if ((t.bwd_ring && t.bwd_ring != tile) || (n > 1 && rst < 8 * n)) continue;
-            const double tiles = E * tiles_of(N, wide ? 256 : 128) * tiles_of(K, wide ? 256 : 128);
-            const RingCost c = wide ? kDwWide : tiles * n > cus ? kDwSmall : kDwAlone;
-            // operands that do not stay in the 256 MB cache cost the small tiles, which read them more often, more
-            // (8192 slots of 8 experts 2048 -> 8192, 168 MB: 657 in the large ones, 698; half the slots 410 / 384)
-            const double more = !wide && (double)(N + K) * (double)T * 2.0 > 1.4e8 ? 1.2 : 1.0;
-            const double rounds = tiles * n / cus + 0.2, bytes = (double)E * (double)N * (double)K * 4.0;
-            const double v = (rounds < 1.0 ? 1.0 : rounds) * (c.stage * more * rst / n + c.item) +
-                             (n > 1 ? c.fold + n * bytes * 2e-6 / c.rate : 0.0);
-            if (v < dw_us) dw_us = v, p.dw_tile = tile, p.dw_splits = n;
-        }
-    if (force) p.dw_splits = force;
+    // 256 x 128 tiles where there are four rounds of them and an expert's slots are six stages or more; slices only of the
+    // small ones.  dW alone with its copies, us in 128 x 128 / 256 x 128: 4270 slots of 5 experts 4992 -> 7936 438 / 400,
+    // 9554 of 18 2048 -> 4096 264 / 246; fewer tiles, 7510 of 29 704 -> 2656 90 / 106, or stages, 1880 of 16 4096 -> 4096
+    // 208 / 218.  (256 x 256, one workgroup a CU: 479 and 286.)
+    const double wide_tiles = E * tiles_of(N, 256) * tiles_of(K, 128);
+    p.dw_tile = wide_tiles >= 8 * cus && (double)T >= 192.0 * E ? 1 : 2;
+    if (t.bwd_ring == 1 || t.bwd_ring == 2) p.dw_tile = t.bwd_ring;
+    for (int n = 1; n <= 16 && p.dw_tile == 2; n *= 2) {
+        if (n > 1 && rst < 8 * n) break;
+        const double tiles = E * tiles_of(N, 128) * tiles_of(K, 128);
+        const RingCost c = tiles * n > cus ? kDwSmall : kDwAlone;
+        const double rounds = tiles * n / cus + 0.2, bytes = (double)E * (double)N * (double)K * 4.0;
+        const double v = (rounds < 1.0 ? 1.0 : rounds) * (c.stage * rst / n + c.item) +
+                         (n > 1 ? c.fold + n * bytes * 2e-6 / c.rate : 0.0);
+        if (v < dw_us) dw_us = v, p.dw_splits = n;
+    }
+    if (force && p.dw_tile == 2) p.dw_splits = force;
     return p;
 }
 
@@ -1293,15 +1315,15 @@ void launch_experts_dx(const ExpertsOperands& a, const ExpertsBackwardPlan& p, h
 }
 
 void launch_experts_dw(const ExpertsOperands& a, const ExpertsBackwardPlan& p, hipStream_t s) {
-    const int64_t T = p.dw_tile == 1 ? 256 : 128, gi = (a.N + T - 1) / T, gj = (a.K + T - 1) / T;
+    const int64_t T = p.dw_tile == 1 ? 256 : 128, gi = (a.N + T - 1) / T, gj = (a.K + 127) / 128;
     const ExpertsRing ex{a.offsets, a.E, (int)a.T, a.least, 0, 0, nullptr, 0};
     const RingSlices sl{p.dw_splits, 0};
-    const int64_t items = gi * gj * a.E * sl.splits, cap = (int64_t)ring_cus() * (T == 256 ? 1 : 2);
+    const int64_t items = gi * gj * a.E * sl.splits, cap = (int64_t)ring_cus() * 2;
     const unsigned grid = (unsigned)(items < cap ? items : cap);
     const bool cut = sl.splits > 1;
-    const auto kernel =
-        cut ? (T == 256 ? gemm_tn_bf16_wide<256, 4, true, true> : gemm_tn_bf16_wide<128, 4, true, true>)
-            : (T == 256 ? gemm_tn_bf16_wide<256, 4, false, true> : gemm_tn_bf16_wide<128, 4, false, true>);
+    const auto kernel = cut              ? gemm_tn_bf16_wide<128, 4, true, true>
+                        : p.dw_tile == 1 ? gemm_tn_bf16_wide<256, 3, false, true, 128>
+                                         : gemm_tn_bf16_wide<128, 4, false, true>;
     kernel<<<grid, 256, 0, s>>>(a.gwT, a.qT, a.N, a.K, 0, cut ? nullptr : a.gamma,
                                 a.gamma && !cut ? 1.0f / 128.0f : 1.0f, cut ? a.part : a.dW, (int)gi, (int)gj, 0, 0, sl, ex);
     if (!cut) return;
