@@ -284,8 +284,8 @@ __device__ inline TailPlan tail_plan(int tiles, int x, int S, int stages, int sl
     p.tail = len - p.full;
     p.n = 1;
     // Twice the slices while that saves more than their sums cost to write and read: with n of them 0.39 us a stage and
-    // 1 / n against 0.42 us for each of an XCD's tails and n (128 x 256 tiles; 256 x 256 0.62 and 0.84).  666 slots of
-    // 4 experts 1024 -> 4096 take 67 us in 16 slices, 51 in 4.  Two would gain what a CU's second workgroup is worth.
+    // 1 / n against 0.42 us for each of an XCD's tails and n (tiles of 128 x 256).  666 slots of 4 experts 1024 -> 4096
+    // take 67 us in 16 slices, 51 in 4.  Two would gain what a CU's second workgroup is worth.
     if (p.tail > 0)
         while (2 * p.n <= slices && 2 * p.n * p.tail <= S && stages >= 16 * p.n &&
                5 * stages > 12 * p.tail * p.n * p.n)
@@ -304,8 +304,8 @@ __device__ inline TailPlan tail_plan(int tiles, int x, int S, int stages, int sl
 // stage st+1 (s_waitcnt vmcnt(n), n counted by hand), meets the others at a bare s_barrier, and
 // the DMA of stage st+NS-1 goes to the buffer stage st-1 has left.
 //
-// T x TJ = 256 x 128 (experts): waves of 128 x 64, two workgroups per CU whose stores and barriers the other one's MFMAs
-// hide, where a tile has few stages; a ring of three stages is what fits twice.
+// T x TJ = 256 x 128 (experts): waves of 128 x 64, two workgroups per CU whose stores and barriers the other one's
+// MFMAs hide, where a tile has few stages; a ring of three stages is what fits twice.
 // Why four waves (T = 256).  With eight waves of 128 x 64 LDS sets the pace: every operand row is read by the
 // waves that share it, 96 KiB of reads and 32 KiB of DMA writes a stage, at 128 bytes a cycle as
 // long as the MFMAs of the stage take (1024 cycles).  128 x 128 waves read 64 KiB.  There is one wave
@@ -1180,10 +1180,9 @@ hipError_t launch_backward(const BackwardArgs& a, hipStream_t s) {
 // dX of the tiles that gemm_tn_signs_ring cut (tail_plan): the slices' sums added in the order 0, 1, ...  Whether there
 // are any is known here only, so the grid is small and its workgroups take 1024 elements of a tile in turn, those of
 // the XCD that wrote them; a thread has all its slices' loads in flight.
-template <int BM>
 __global__ __launch_bounds__(256) void fold_expert_tails(ExpertsRing ex, int S, int stages, int grid_j, int64_t J,
                                                          float* __restrict__ C) {
-    constexpr int BN = 256, PIECES = BM / 4;
+    constexpr int BM = 128, BN = 256, PIECES = BM / 4;
     __shared__ ExpertTiles count;
     const int tiles = expert_tiles(ex.offsets, ex.E, ex.T, BM, count) * grid_j, x = (int)blockIdx.x & 7;
     const TailPlan p = tail_plan(tiles, x, S, stages, ex.slices);
@@ -1241,51 +1240,37 @@ __global__ __launch_bounds__(256) void fold_expert_weights(const float* __restri
 // fall on the experts is not known here: an expert's last row of tiles is taken to be half full, its reduction of
 // average length.
 ExpertsBackwardPlan experts_backward_plan(int64_t T, int64_t N, int64_t K, int E) {
-    constexpr RingCost kDxWide{0.615, 12.0, 5.0, 6.0}, kDxRows{0.33, 5.0, 5.0, 6.0}, kDxAlone{0.39, 2.0, 5.0, 6.0};
     constexpr RingCost kDwSmall{0.172, 2.3, 5.0, 6.0}, kDwAlone{0.226, 3.6, 5.0, 6.0};
     const Tuning& t = tuning();
     const double cus = ring_cus(), A = (double)(T < E ? T : E);
     auto tiles_of = [](int64_t v, int64_t b) { return (double)((v + b - 1) / b); };
     const int force = t.bwd_splits < 0 ? 0 : t.bwd_splits < 16 ? t.bwd_splits : 16;
     const double nst = tiles_of(N, 32), rst = (double)T / 32.0 / E + 0.5;
-    ExpertsBackwardPlan p{1, 1, 1, 1};
-    double dx_us = 1e30, dw_us = 1e30;
-    for (int tile = 1; tile <= 2; ++tile) {
-        const bool wide = tile == 1;
-        if (t.bwd_dx && t.bwd_dx != tile) continue;
-        const double rows = (double)T / (wide ? 256 : 128) + 0.5 * A, slots = wide ? cus : 2.0 * cus;
-        const double tiles = (rows > 0.9 * A ? rows : 0.9 * A) * tiles_of(K, 256);
-        const double whole = (double)(int64_t)(tiles / slots), tail = tiles - whole * slots;
-        // Slices of the last round's tiles cost a launch, 4.5 us, also where the device finds nothing to cut: few
-        // tiles, or more than a round of long ones (a quarter of the rounds end so, and save most of 0.39 us a stage
-        // then).
-        const bool cut = force ? force > 1 : tiles < 0.3 * slots ? nst >= 32 && 5 * nst > 6 * tiles
-                                                                         : tiles > 0.9 * slots && nst >= 96;
-        int n = 1;  // as tail_plan does
-        while (cut && n < 16 && 2 * n * tail <= slots && nst >= 16 * n && 5 * nst > 1.5 * tail * n * n) n *= 2;
-        if (n < 4) n = 1;
-        const RingCost round = wide ? kDxWide : kDxRows, last = wide ? kDxWide : tail * n > cus ? kDxRows : kDxAlone;
-        const double per_slot = wide ? 1.0 : 2.0;
-        const double v = whole * per_slot * (round.stage * nst + round.item) +
-                         (wide || tail * n <= cus ? 1.0 : 2.0) * (last.stage * nst / n + last.item) +
-                         (n > 1 ? 5.0 + (wide ? 0.1 : 0.05) * tail * n : 0.0);
-        if (v < dx_us) dx_us = v, p.dx_tile = tile, p.dx_slices = !cut ? 1 : force ? force : 16;
-    }
-    // 256 x 128 tiles where there are four rounds of them and an expert's slots are six stages or more; slices only of the
-    // small ones.  dW alone with its copies, us in 128 x 128 / 256 x 128: 4270 slots of 5 experts 4992 -> 7936 438 / 400,
-    // 9554 of 18 2048 -> 4096 264 / 246; fewer tiles, 7510 of 29 704 -> 2656 90 / 106, or stages, 1880 of 16 4096 -> 4096
-    // 208 / 218.  (256 x 256, one workgroup a CU: 479 and 286.)
+    ExpertsBackwardPlan p{1, 1, 1};
+    // dX in 128 x 256 tiles (256 x 256, one workgroup a CU, were faster in 2 of 40 shapes, by 5 % at most).  Slices of
+    // the last round's tiles cost a launch, 4.5 us, also where the device finds nothing to cut: few tiles, or more than
+    // a round of long ones (a quarter of the rounds end so, and save most of 0.39 us a stage then).
+    const double rows = (double)T / 128 + 0.5 * A, slots = 2.0 * cus;
+    const double tiles = (rows > 0.9 * A ? rows : 0.9 * A) * tiles_of(K, 256);
+    const bool cut = force ? force > 1 : tiles < 0.3 * slots ? nst >= 32 && 5 * nst > 6 * tiles
+                                                             : tiles > 0.9 * slots && nst >= 96;
+    p.dx_slices = !cut ? 1 : force ? force : 16;
+    // 256 x 128 tiles where there are four rounds of them and an expert's slots are six stages or more; slices only of
+    // the small ones.  dW alone with its copies, us in 128 x 128 / 256 x 128: 4270 slots of 5 experts 4992 -> 7936 438
+    // / 400, 9554 of 18 2048 -> 4096 264 / 246; fewer tiles, 7510 of 29 704 -> 2656 90 / 106, or stages, 1880 of 16
+    // 4096 -> 4096 208 / 218.  (256 x 256, one workgroup a CU: 479 and 286.)
     const double wide_tiles = E * tiles_of(N, 256) * tiles_of(K, 128);
     p.dw_tile = wide_tiles >= 8 * cus && (double)T >= 192.0 * E ? 1 : 2;
     if (t.bwd_ring == 1 || t.bwd_ring == 2) p.dw_tile = t.bwd_ring;
+    double us = 1e30;
     for (int n = 1; n <= 16 && p.dw_tile == 2; n *= 2) {
         if (n > 1 && rst < 8 * n) break;
-        const double tiles = E * tiles_of(N, 128) * tiles_of(K, 128);
-        const RingCost c = tiles * n > cus ? kDwSmall : kDwAlone;
-        const double rounds = tiles * n / cus + 0.2, bytes = (double)E * (double)N * (double)K * 4.0;
+        const double items = E * tiles_of(N, 128) * tiles_of(K, 128) * n;
+        const RingCost c = items > cus ? kDwSmall : kDwAlone;
+        const double rounds = items / cus + 0.2, bytes = (double)E * (double)N * (double)K * 4.0;
         const double v = (rounds < 1.0 ? 1.0 : rounds) * (c.stage * rst / n + c.item) +
                          (n > 1 ? c.fold + n * bytes * 2e-6 / c.rate : 0.0);
-        if (v < dw_us) dw_us = v, p.dw_splits = n;
+        if (v < us) us = v, p.dw_splits = n;
     }
     if (force && p.dw_tile == 2) p.dw_splits = force;
     return p;
@@ -1293,12 +1278,12 @@ ExpertsBackwardPlan experts_backward_plan(int64_t T, int64_t N, int64_t K, int E
 
 // Workgroups of dX: a multiple of the XCDs, enough for the slices of few tiles.
 static int dx_grid(int64_t T, int64_t K, int E, const ExpertsBackwardPlan& p) {
-    const int64_t bm = p.dx_tile == 1 ? 256 : 128, cap = (int64_t)ring_cus() * (bm == 256 ? 1 : 2);
-    const int64_t most = most_tiles(T, E, (int)bm, 0) * ((K + 255) / 256) * p.dx_slices;
+    const int64_t cap = (int64_t)ring_cus() * 2;
+    const int64_t most = most_tiles(T, E, 128, 0) * ((K + 255) / 256) * p.dx_slices;
     return (int)((most < cap ? most : cap) + 7) / 8 * 8;
 }
 size_t experts_dx_part_bytes(int64_t T, int64_t K, int E, const ExpertsBackwardPlan& p) {
-    return p.dx_slices > 1 ? (size_t)dx_grid(T, K, E, p) * (p.dx_tile == 1 ? 256 : 128) * 256 * 4 : 0;
+    return p.dx_slices > 1 ? (size_t)dx_grid(T, K, E, p) * 128 * 256 * 4 : 0;
 }
 
 void launch_experts_dx(const ExpertsOperands& a, const ExpertsBackwardPlan& p, hipStream_t s) {
@@ -1306,12 +1291,10 @@ void launch_experts_dx(const ExpertsOperands& a, const ExpertsBackwardPlan& p, h
     ExpertsRing ex{a.offsets, a.E, (int)a.T, 0, 64, a.T * 64, a.part, p.dx_slices};
     if (a.direct) ex.a_pitch = (uint32_t)(a.N * 2), ex.a_step = 64;
     const int grid = dx_grid(a.T, a.K, a.E, p), S = grid / 8;
-    const auto kernel =
-        p.dx_tile == 1 ? gemm_tn_signs_ring<256, 4, false, true> : gemm_tn_signs_ring<128, 4, false, true>;
-    kernel<<<(unsigned)grid, 512, 0, s>>>(a.g, a.Sw, a.T, a.K, Np, a.beta, 1.0f, a.dX, 0, (int)gj, 0, 0, {}, ex);
+    gemm_tn_signs_ring<128, 4, false, true><<<(unsigned)grid, 512, 0, s>>>(a.g, a.Sw, a.T, a.K, Np, a.beta, 1.0f, a.dX, 0,
+                                                                          (int)gj, 0, 0, {}, ex);
     if (p.dx_slices < 4 || S < 4 || nst < 32) return;  // tail_plan cuts nothing
-    const auto fold = p.dx_tile == 1 ? fold_expert_tails<256> : fold_expert_tails<128>;
-    fold<<<1024, 256, 0, s>>>(ex, S, (int)nst, (int)gj, a.K, a.dX);
+    fold_expert_tails<<<1024, 256, 0, s>>>(ex, S, (int)nst, (int)gj, a.K, a.dX);
 }
 
 void launch_experts_dw(const ExpertsOperands& a, const ExpertsBackwardPlan& p, hipStream_t s) {

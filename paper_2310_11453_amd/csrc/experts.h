@@ -96,7 +96,7 @@ struct ExpertsOperands {
     float *dX, *dW, *part;      // part: sums of slices of the reductions
 };
 struct ExpertsBackwardPlan {
-    int dx_tile, dx_slices, dw_tile, dw_splits;  // dx_slices: at most, of a tile in dX's last round
+    int dx_slices, dw_tile, dw_splits;  // dx_slices: at most, of a tile in dX's last round
 };
 size_t experts_dx_part_bytes(int64_t T, int64_t K, int E, const ExpertsBackwardPlan& p);
 ExpertsBackwardPlan experts_backward_plan(int64_t T, int64_t N, int64_t K, int E);

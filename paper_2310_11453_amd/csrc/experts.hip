@@ -30,11 +30,11 @@ struct Args {
 // takes the 512-chunks w, w + W, ... of K; the weights are the row operand of v_mfma_i32_16x16x64_i8, the slots its
 // columns; a lane's 16 bytes of a packed tile hold 16 consecutive k of each of eight bit planes, (w >> i) & 0x01010101
 // is plane i as {0,1} bytes, and sum_k q s = 2 sum_k q b - sum_k q.  The waves' sums meet in LDS.
-// A launch is a chain of trips to memory: the experts' bounds, then the weights and (in two trips) the codes, whose rows
-// are known only with the order.  Loads return in the order of their requests, so the order is asked for first, then a
-// quarter of the first chunk's weights, then the codes, which are what the matrix instructions wait for, then the rest of
-// the weights, which arrive while the first tiles are multiplied.  (All weights ahead of the order, and so of everything:
-// 96 slots, 16 experts, 4096 -> 4096 13.4 us a call, 11.7 so; 64, 32, 6144 -> 2048 13.9, 11.7.)
+// A launch is a chain of trips to memory: the experts' bounds, then the weights and (in two trips) the codes, whose
+// rows are known only with the order.  Loads return in the order of their requests, so the order is asked for first,
+// then a quarter of the first chunk's weights, then the codes, which are what the matrix instructions wait for, then
+// the rest of the weights, which arrive while the first tiles are multiplied.  (All weights ahead of the order, and so
+// of everything: 96 slots, 16 experts, 4096 -> 4096 13.4 us a call, 11.7 so; 64, 32, 6144 -> 2048 13.9, 11.7.)
 template <int TILES>
 __global__ __launch_bounds__(rows::kMaxWaves* kWave) void experts_rows_kernel(rows::Args a) {
     using namespace rows;
@@ -157,9 +157,9 @@ static void launch_rows(const ExpertsArgs& a, hipStream_t s) {
     const int64_t TN = tiles_n(a.N), TK = tiles_k(a.K);
     const int64_t A = a.T < a.E ? a.T : a.E, blocks = a.T / rows::kSlots + A;
     // Tiles of a workgroup: more of them share the fixed chain and the codes, fewer leave no CU idle; eight leave two
-    // workgroups of a long reduction on a CU.  us with 2 / 4 / 8, T slots of E experts: T = 8, E = 8, 4096 -> 1024 4.3 /
-    // 4.7 / 5.7, 4096 -> 2048 5.1 / 4.9 / 5.8; T = 128, E = 16, 4096 -> 1024 6.3 / 5.8 / 7.0, 2048 -> 8192 17.4 / 14.4 /
-    // 15.3; T = 64, E = 32, 6144 -> 2048 17.5 / 14.8 / 11.7; T = 128, E = 32, 4096 -> 5120 34.4 / 27.6 / 21.9.
+    // workgroups of a long reduction on a CU.  us with 2 / 4 / 8, T slots of E experts: T = 8, E = 8, 4096 -> 1024 4.3
+    // / 4.7 / 5.7, 4096 -> 2048 5.1 / 4.9 / 5.8; T = 128, E = 16, 4096 -> 1024 6.3 / 5.8 / 7.0, 2048 -> 8192 17.4 /
+    // 14.4 / 15.3; T = 64, E = 32, 6144 -> 2048 17.5 / 14.8 / 11.7; T = 128, E = 32, 4096 -> 5120 34.4 / 27.6 / 21.9.
     int tiles = tuning().decode_tiles;
     const int64_t all = blocks * TN;
     if (!tiles) tiles = all < 512 ? 1 : all < 1024 || TK < 4 ? 2 : TK >= 8 && all >= 2048 ? 8 : 4;

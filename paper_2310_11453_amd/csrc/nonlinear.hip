@@ -7,9 +7,9 @@
 //              du = f'(v) * (g - mean g - n mean(g n)) / sqrt(var h + eps),  g = the gradient of x^
 // The backward is the derivative of the forward at v, exactly: its statistics are those of f(v), which come out of the
 // row that is in registers anyway, and nothing but the checkpoint has to be kept (1.03 bytes an element where u has
-// four).  f and f' are evaluated in fp32, the sums of a row in fp64 (as in the quantiser and in the LayerNorm backward).
-// Bound by HBM: 4 bytes read and 1 (with the checkpoint 2) written an element, twice the reading with a gamma per
-// tensor; backward 5 read, 2 or 4 written.
+// four).  f and f' are evaluated in fp32, the sums of a row in fp64 (as in the quantiser and in the LayerNorm
+// backward). Bound by HBM: 4 bytes read and 1 (with the checkpoint 2) written an element, twice the reading with a
+// gamma per tensor; backward 5 read, 2 or 4 written.
 #include "common.h"
 #include "experts.h"
 #include "kernels.h"
@@ -31,8 +31,8 @@ __device__ inline float fn_value(float u) {
 // f(v) and f'(v) of the backward, where they are factors of a gradient.  GELU: Phi(u) = (1 + erf(z)) / 2, z = u / sqrt
 // 2, with erf as in Abramowitz and Stegun 7.1.26 (erf z = 1 - (a1 t + ... + a5 t^5) e^(-z^2), t = 1 / (1 + p z), z >=
 // 0: off by at most 1.5e-7), which shares its exponential with f'.  The hardware's exponential and reciprocal are off
-// by an ulp.  (16384 x 8192 with the library's erff and expf 455 us, 219 so.  The forward would gain 14 %, and a code in
-// a million fall on the other side of a border.)
+// by an ulp.  (16384 x 8192 with the library's erff and expf 455 us, 219 so.  The forward would gain 14 %, and a code
+// in a million fall on the other side of a border.)
 struct FnPair {
     float value, slope;
 };

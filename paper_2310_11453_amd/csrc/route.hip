@@ -53,8 +53,8 @@ __global__ __launch_bounds__(route::kLarge) void route_count_kernel(RouteArgs a,
     if (threadIdx.x < a.E) a.counts[blockIdx.x * a.E + threadIdx.x] = sums[threadIdx.x];
 }
 
-// Of many workgroups' counts, where each workgroup's choices of an expert begin inside the expert, in place of the count,
-// and how many the expert has, behind them.  blockIdx.x: the expert.  (Each workgroup adding up what it needs is
+// Of many workgroups' counts, where each workgroup's choices of an expert begin inside the expert, in place of the
+// count, and how many the expert has, behind them.  blockIdx.x: the expert.  (Each workgroup adding up what it needs is
 // quadratic in their number: 16777216 choices of 64 experts 779 us a call so, 134 with this, 4194304 83 and 48, 1048576
 // 29 and 27, and it would be a launch for nothing at 262144, 23.)
 __global__ __launch_bounds__(route::kScan) void route_scan_kernel(RouteArgs a, int blocks) {
