@@ -164,6 +164,22 @@ def test_products_of_more_than_4_gib_of_codes(bl):
         assert torch.equal(got[s].double(), signs[int(s >= 40000)] @ codes[s].cpu().double())
 
 
+@pytest.mark.parametrize("tile", TILES)
+def test_products_of_more_than_2_to_32_outputs(bl, tuning, tile):
+    """Offsets into Y pass 32 bits.  Checked on slots from both ends and around the border."""
+    tuning(f"experts_tile={tile}")
+    T, K, N = 262400, 64, 16384
+    codes = torch.randint(-128, 128, (T, K), dtype=torch.int8, device="cuda")
+    rowsum = codes.sum(1, dtype=torch.int32)
+    packed, _, beta = bl.bitlinear_pack_weights_experts(torch.randn(2, N, K, device="cuda"))
+    signs = [torch.from_numpy(unpack(bl, packed[e], N, K)).double() for e in range(2)]
+    offsets = torch.tensor([0, 131000, T], dtype=torch.int32, device="cuda")
+    got = bl.bitlinear_matmul_experts(codes, torch.ones(1, device="cuda"), rowsum, packed, N, beta, offsets,
+                                      per_tensor=True, flags=bl.FLAG_OUT_ACC_I32)
+    for s in (0, 130999, 131000, 131071, 131072, 262143, 262144, 262145, T - 1):
+        assert torch.equal(got[s].cpu().double(), signs[int(s >= 131000)] @ codes[s].cpu().double())
+
+
 def check_products(bl, M, top_k, E, K, N, gather, per_tensor, ids):
     c = make(bl, M, top_k, E, K, N, gather, per_tensor, ids)
     acc = torch.full((c["T"], N), 77, dtype=torch.int32)
@@ -287,6 +303,33 @@ def test_nothing_to_do(bl):
     dX, dW = bl.bitlinear_backward_ste_experts(dy, codes, gamma, packed, beta, offsets, order, top_k)
     assert dX.shape == (0, K) and bool((dW == 0).all()) and dW.shape == (E, N, K)
     assert bl.bitlinear_nonlinear_backward(torch.empty(0, K, device="cuda"), check, scale).shape == (0, K)
+
+
+def test_backward_of_more_than_2_to_32_outputs(bl):
+    """Offsets into dX and into dW pass 32 bits.  On integers, so exact; checked at both ends and around the border."""
+    one, g = torch.ones(1, device="cuda"), torch.Generator().manual_seed(3)
+    T, K, N, E = 65664, 65536, 64, 2
+    packed, _, _ = bl.bitlinear_pack_weights_experts(torch.randn(E, N, K, device="cuda"))
+    signs = [torch.from_numpy(unpack(bl, packed[e], N, K)).double() for e in range(E)]
+    offsets = torch.tensor([0, 30000, T], dtype=torch.int32, device="cuda")
+    dY = torch.randint(-4, 5, (T, N), generator=g).to(torch.bfloat16)
+    codes = torch.zeros(T, K, dtype=torch.int8, device="cuda")  # dX does not read them
+    dX, _ = bl.bitlinear_backward_ste_experts(dY.cuda(), codes, one, packed, one.expand(E).contiguous(), offsets,
+                                              per_tensor=True, want_dw=False)
+    for s in (0, 29999, 30000, 32767, 32768, 65535, 65536, 65537, T - 1):
+        assert torch.equal(dX[s].cpu().double(), dY[s].double() @ signs[int(s >= 30000)])
+    del dX, codes
+    T, K, N, E = 200, 8192, 8192, 65
+    ids = np.random.default_rng(1).integers(0, E, (T, 1)).astype(np.int32)
+    order, _, offsets = bl.bitlinear_route(gpu(ids), E)
+    codes, dY = torch.randint(-128, 128, (T, K), generator=g, dtype=torch.int8), torch.randint(-4, 5, (T, N), generator=g)
+    _, dW = bl.bitlinear_backward_ste_experts(dY.to(torch.bfloat16).cuda(), codes.cuda(), 128 * one, None, None, offsets,
+                                              order, 1, True, want_dx=False)
+    at = offsets.tolist()
+    for e in (0, 31, 32, 63, 64):
+        mine = slice(at[e], at[e + 1])
+        ref = dY[mine].double().T @ codes[order[mine].cpu().long()].double()
+        assert torch.equal(dW[e].cpu().double(), ref)
 
 
 def check_backward(bl, M, top_k, E, K, N, gather, per_tensor, ids):
