@@ -494,7 +494,7 @@ def bitlinear_forward_nonneg(X: torch.Tensor, packed: torch.Tensor, N: int, beta
 def _given(dev, t: torch.Tensor, dtype, *shape):
     """Pointer of an operand that has to lie on `dev`, be contiguous and have this type and shape.  (One test for all: a
     call of a few tokens is as long as what Python does for it.)"""
-    if t.device == dev and t.shape == shape and t.dtype == dtype and t.is_contiguous():
+    if t.device == dev and t.shape == shape and t.dtype is dtype and t.is_contiguous():
         return t.data_ptr()
     if t.device != dev:
         raise BitLinearError(f"tensors on {dev} and {t.device}")
@@ -511,6 +511,11 @@ def _here(t: torch.Tensor):
     if dev.index != torch._C._cuda_getDevice():
         raise BitLinearError(f"tensor on {dev}, current device {torch.cuda.current_device()}")
     return dev
+
+
+def _queue(dev):
+    """The current stream of the current device, which _here found to be `dev`."""
+    return torch._C._cuda_getCurrentRawStream(dev.index)
 
 
 def _blob_bytes(N: int, K: int) -> int:
@@ -548,7 +553,7 @@ def bitlinear_pack_weights_experts(W: torch.Tensor, flags: int = 0):
     for e in range(E):
         _check(lib.bitlinear_pack_weights(src + 4 * e * N * K, N, K, flags, packed.data_ptr() + e * nbytes,
                                           alpha.data_ptr() + 4 * e, beta.data_ptr() + 4 * e, _ptr(ws), ws.numel(),
-                                          _stream()), "bitlinear_pack_weights")
+                                          _queue(dev)), "bitlinear_pack_weights")
     return packed, alpha, beta
 
 
@@ -564,7 +569,7 @@ def bitlinear_route(expert: torch.Tensor, experts: int, workspace: torch.Tensor 
     need = workspace_bytes_experts(OP_ROUTE, M, top_k, 0, 0, experts) if M * top_k > 4096 else 0
     ws, ws_bytes, _keep = _scratch(need, workspace, dev)
     _check(lib.bitlinear_route(_ptr(expert, torch.int32), M, top_k, experts, order.data_ptr(), position.data_ptr(),
-                               offsets.data_ptr(), ws, ws_bytes, _stream()), "bitlinear_route")
+                               offsets.data_ptr(), ws, ws_bytes, _queue(dev)), "bitlinear_route")
     return order, position, offsets
 
 
@@ -592,7 +597,7 @@ def bitlinear_matmul_experts(codes: torch.Tensor, gamma: torch.Tensor, rowsum: t
         _ptr(codes, torch.int8), _given(dev, gamma, torch.float32, 1 if per_tensor else M),
         _given(dev, rowsum, torch.int32, M), M, top_k, K, None if order is None else _given(dev, order, torch.int32, T),
         _given(dev, offsets, torch.int32, E + 1), E, _given(dev, packed, torch.uint8, E, _blob_bytes(N, K)), N,
-        _given(dev, beta, torch.float32, E), _gran(per_tensor), flags, _given(dev, out, dtype, T, N), _stream()),
+        _given(dev, beta, torch.float32, E), _gran(per_tensor), flags, _given(dev, out, dtype, T, N), _queue(dev)),
         "bitlinear_matmul_experts")
     return out
 
@@ -614,7 +619,7 @@ def bitlinear_backward_ste_experts(dY: torch.Tensor, codes: torch.Tensor, gamma:
         _given(dev, gamma, torch.float32, 1 if per_tensor else M), _gran(per_tensor),
         None if order is None else _given(dev, order, torch.int32, T), _given(dev, offsets, torch.int32, E + 1), E,
         None if packed is None else _given(dev, packed, torch.uint8, E, _blob_bytes(N, K)),
-        None if beta is None else _given(dev, beta, torch.float32, E), _ptr(dX), _ptr(dW), ws, ws_bytes, _stream()),
+        None if beta is None else _given(dev, beta, torch.float32, E), _ptr(dX), _ptr(dW), ws, ws_bytes, _queue(dev)),
         "bitlinear_backward_ste_experts")
     return dX, dW
 
@@ -629,7 +634,7 @@ def bitlinear_combine(slots: torch.Tensor, position: torch.Tensor, weights: torc
     _check(lib.bitlinear_combine(
         _given(dev, slots, torch.float32, M * top_k, N), _given(dev, position, torch.int32, M, top_k),
         None if weights is None else _given(dev, weights, torch.float32, M, top_k), M, top_k, N,
-        _given(dev, out, torch.float32, M, N), _stream()), "bitlinear_combine")
+        _given(dev, out, torch.float32, M, N), _queue(dev)), "bitlinear_combine")
     return out
 
 
@@ -647,7 +652,7 @@ def bitlinear_combine_backward(dY: torch.Tensor, slots: torch.Tensor | None, pos
         None if slots is None else _given(dev, slots, torch.float32, M * top_k, N),
         _given(dev, position, torch.int32, M, top_k),
         None if weights is None else _given(dev, weights, torch.float32, M, top_k), M, top_k, N,
-        _given(dev, out, torch.bfloat16, M * top_k, N), _ptr(dweights), _stream()), "bitlinear_combine_backward")
+        _given(dev, out, torch.bfloat16, M * top_k, N), _ptr(dweights), _queue(dev)), "bitlinear_combine_backward")
     return out, dweights
 
 
@@ -674,7 +679,7 @@ def bitlinear_quant_nonlinear(U: torch.Tensor, fn: str = "gelu", ln_eps: float =
     _check(lib.bitlinear_quant_nonlinear(
         _ptr(U, torch.float32), M, K, _function(fn), ln_eps,
         None if rows is None else _given(dev, rows, torch.int32, 1), _gran(per_tensor), codes.data_ptr(),
-        gamma.data_ptr(), rowsum.data_ptr(), _ptr(check), _ptr(scale), ws, ws_bytes, _stream()),
+        gamma.data_ptr(), rowsum.data_ptr(), _ptr(check), _ptr(scale), ws, ws_bytes, _queue(dev)),
         "bitlinear_quant_nonlinear")
     return codes, gamma, rowsum, check, scale
 
@@ -694,5 +699,5 @@ def bitlinear_nonlinear_backward(dXhat: torch.Tensor, check: torch.Tensor, check
         _ptr(dXhat, torch.float32), _given(dev, check, torch.int8, M, K),
         _given(dev, check_scale, torch.float32, M, (K + 127) // 128), M, K, _function(fn), ln_eps,
         None if rows is None else _given(dev, rows, torch.int32, 1), BF16 if dtype == torch.bfloat16 else F32,
-        _given(dev, out, dtype, M, K), _stream()), "bitlinear_nonlinear_backward")
+        _given(dev, out, dtype, M, K), _queue(dev)), "bitlinear_nonlinear_backward")
     return out
