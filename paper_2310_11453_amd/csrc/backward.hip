@@ -367,7 +367,58 @@ __device__ inline void wide_wait(v4i (&a)[4], v4i (&b)[2]) {
                  : "+v"(a[0]), "+v"(a[1]), "+v"(a[2]), "+v"(a[3]), "+v"(b[0]), "+v"(b[1]));
 }
 
-template <int T, int NS, bool SPLIT, bool EXP = false, int TJ = T>
+// DIRECT (dW of experts, A = dY where it lies, [r][i]): a stage of A is 32 rows of T columns, and a lane's eight r of
+// a column come out of LDS by two transposing reads, of four rows each.  Sixteen lanes read 4 rows x 16 columns, lane i
+// row i / 4, columns 4 (i % 4) ..; lane i gets column i.  The 32-byte pieces of a row are XOR-swizzled so that those of
+// four rows, and of the two sixteens of columns, are on different banks.  As fast as reading a transposed copy, which
+// nobody has to write then (8192 slots of 8 experts 2048 -> 8192, both products: 618 -> 562 us).
+typedef int v2i __attribute__((ext_vector_type(2)));
+struct TrOp {
+    v2i lo, hi;
+};
+__device__ inline int tr_swizzle(int row) { return (row & 3) | (row & 1) << 2; }
+__device__ inline void wide_issue(TrOp (&a)[4], v4i (&b)[2], uint32_t ad_a, uint32_t ad_b) {
+    asm volatile(
+        "ds_read_b64_tr_b16 %0, %10\n\t"
+        "ds_read_b64_tr_b16 %1, %10 offset:2048\n\t"
+        "ds_read_b64_tr_b16 %2, %11\n\t"
+        "ds_read_b64_tr_b16 %3, %11 offset:2048\n\t"
+        "ds_read_b64_tr_b16 %4, %12\n\t"
+        "ds_read_b64_tr_b16 %5, %12 offset:2048\n\t"
+        "ds_read_b64_tr_b16 %6, %13\n\t"
+        "ds_read_b64_tr_b16 %7, %13 offset:2048\n\t"
+        "ds_read_b128 %8, %14\n\t"
+        "ds_read_b128 %9, %14 offset:2048"
+        : "=&v"(a[0].lo), "=&v"(a[0].hi), "=&v"(a[1].lo), "=&v"(a[1].hi), "=&v"(a[2].lo), "=&v"(a[2].hi),
+          "=&v"(a[3].lo), "=&v"(a[3].hi), "=&v"(b[0]), "=&v"(b[1])
+        : "v"(ad_a), "v"(ad_a ^ 64u), "v"(ad_a ^ 128u), "v"(ad_a ^ 192u), "v"(ad_b));
+}
+__device__ inline void wide_wait(TrOp (&a)[4], v4i (&b)[2]) {
+    asm volatile("s_waitcnt lgkmcnt(0)"
+                 : "+v"(a[0].lo), "+v"(a[0].hi), "+v"(a[1].lo), "+v"(a[1].hi), "+v"(a[2].lo), "+v"(a[2].hi),
+                   "+v"(a[3].lo), "+v"(a[3].hi), "+v"(b[0]), "+v"(b[1]));
+}
+__device__ inline void wide_issue(TrOp (&a)[2], v4i (&b)[2], uint32_t ad_a, uint32_t ad_b) {
+    asm volatile(
+        "ds_read_b64_tr_b16 %0, %6\n\t"
+        "ds_read_b64_tr_b16 %1, %6 offset:1024\n\t"
+        "ds_read_b64_tr_b16 %2, %7\n\t"
+        "ds_read_b64_tr_b16 %3, %7 offset:1024\n\t"
+        "ds_read_b128 %4, %8\n\t"
+        "ds_read_b128 %5, %8 offset:2048"
+        : "=&v"(a[0].lo), "=&v"(a[0].hi), "=&v"(a[1].lo), "=&v"(a[1].hi), "=&v"(b[0]), "=&v"(b[1])
+        : "v"(ad_a), "v"(ad_a ^ 64u), "v"(ad_b));
+}
+__device__ inline void wide_wait(TrOp (&a)[2], v4i (&b)[2]) {
+    asm volatile("s_waitcnt lgkmcnt(0)"
+                 : "+v"(a[0].lo), "+v"(a[0].hi), "+v"(a[1].lo), "+v"(a[1].hi), "+v"(b[0]), "+v"(b[1]));
+}
+__device__ inline v8bf wide_operand(const v4i& a) { return __builtin_bit_cast(v8bf, a); }
+__device__ inline v8bf wide_operand(const TrOp& a) {
+    return __builtin_bit_cast(v8bf, __builtin_shufflevector(a.lo, a.hi, 0, 1, 2, 3));
+}
+
+template <int T, int NS, bool SPLIT, bool EXP = false, int TJ = T, bool DIRECT = false>
 __global__ __launch_bounds__(256, T + TJ == 512 ? 1 : 2) void gemm_tn_bf16_wide(const uint16_t* __restrict__ A,
                                                             const uint16_t* __restrict__ B,
                                                             int64_t I, int64_t J, int64_t Rp,
@@ -379,6 +430,7 @@ __global__ __launch_bounds__(256, T + TJ == 512 ? 1 : 2) void gemm_tn_bf16_wide(
     constexpr int PA = BM * 4 / THREADS, PB = BN * 4 / THREADS, P = PA + PB;
     constexpr int A_BYTES = BM * 64, STAGE_BYTES = (BM + BN) * 64;
     static_assert((NS - 1) * P < 64, "vmcnt range");
+    static_assert(!DIRECT || EXP, "rows of experts");
     __shared__ __attribute__((aligned(1024))) uint8_t sm[NS * STAGE_BYTES];
 
     const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave), l = threadIdx.x % kWave;
@@ -445,16 +497,31 @@ __global__ __launch_bounds__(256, T + TJ == 512 ? 1 : 2) void gemm_tn_bf16_wide(
 
     // DMA: thread -> PA + PB pieces of 16 bytes per stage; piece = (row, swizzled segment).
     // Rows past the matrix re-read its last row (their results are never stored).
-    uint32_t goffA[PA], goffB[PB];
+    // DIRECT: the piece of every q is in the same place of its row, rows kRowsA apart; row0, rows of the tile's first
+    // stage; end, behind the expert's last.  Rows past it repeat that one: the other operand is zero there.
+    constexpr int kSegs = T / 8, kRowsA = THREADS / kSegs;
+    int row0 = 0, end = 0;
+    uint32_t goffA[DIRECT ? 1 : PA], goffB[PB];
     const uint8_t *baseA = nullptr, *baseB = nullptr;
     auto setup_dma = [&](int64_t i0, int64_t j0) {
+        if constexpr (DIRECT) {
+            const int seg = (int)threadIdx.x % kSegs, row = (int)threadIdx.x / kSegs;
+            static_assert(kRowsA % 4 == 0, "one swizzle for all of a thread's rows");
+            int64_t col = ((((seg >> 1) ^ tr_swizzle(row)) << 1) | (seg & 1)) * 8;
+            if (col > I - 8 - i0) col = I - 8 - i0;  // I % 32 == 0
+            goffA[0] = (uint32_t)col * 2;
+            const int from = __builtin_amdgcn_readfirstlane(smE.from[expert]);
+            end = __builtin_amdgcn_readfirstlane(smE.to[expert]);
+            row0 = from + 32 * (st0 - __builtin_amdgcn_readfirstlane(smE.first[expert]));
+        } else {
 #pragma unroll
-        for (int q = 0; q < PA; ++q) {
-            const int slot = q * THREADS + threadIdx.x;
-            int row = slot >> 2;
-            const int seg = ((slot & 3) ^ ((row >> 2) & 3)) * 16;
-            if (i0 + row > I - 1) row = (int)(I - 1 - i0);
-            goffA[q] = (uint32_t)row * 64 + seg;
+            for (int q = 0; q < PA; ++q) {
+                const int slot = q * THREADS + threadIdx.x;
+                int row = slot >> 2;
+                const int seg = ((slot & 3) ^ ((row >> 2) & 3)) * 16;
+                if (i0 + row > I - 1) row = (int)(I - 1 - i0);
+                goffA[q] = (uint32_t)row * 64 + seg;
+            }
         }
 #pragma unroll
         for (int q = 0; q < PB; ++q) {
@@ -464,7 +531,7 @@ __global__ __launch_bounds__(256, T + TJ == 512 ? 1 : 2) void gemm_tn_bf16_wide(
             if (j0 + row > J - 1) row = (int)(J - 1 - j0);
             goffB[q] = (uint32_t)row * 64 + seg;
         }
-        baseA = reinterpret_cast<const uint8_t*>(A) + (st0 * I + i0) * 64;
+        baseA = reinterpret_cast<const uint8_t*>(A) + (DIRECT ? i0 * 2 : (st0 * I + i0) * 64);
         baseB = reinterpret_cast<const uint8_t*>(B) + (st0 * J + j0) * 64;
     };
     const uint32_t lds_wave = (uint32_t)(w * kWave * 16);
@@ -474,8 +541,21 @@ __global__ __launch_bounds__(256, T + TJ == 512 ? 1 : 2) void gemm_tn_bf16_wide(
     static_assert(PB <= PA && PA == MI, "a piece of A, and one of B or none, per row of MFMAs");
     auto issue_piece = [&](int st, int src_st, int q) {
         uint8_t* dst = sm + (st % NS) * STAGE_BYTES + lds_wave;
+        const uint8_t* from = baseA;
+        uint32_t off;
+        if constexpr (DIRECT) {
+            int r = row0 + 32 * src_st;
+            if (r > end - 1) r = end - 1;
+            if (r < 0) r = 0;
+            const int last = end - 1 > r ? end - 1 - r : 0, row = (int)threadIdx.x / kSegs + q * kRowsA;
+            from += r * ex.a_step;
+            off = (uint32_t)__umul24((uint32_t)(row < last ? row : last), ex.a_pitch) + goffA[0];
+        } else {
+            from += src_st * I * 64;
+            off = goffA[q];
+        }
         __builtin_amdgcn_global_load_lds(
-            (const void*)(baseA + src_st * I * 64 + goffA[q]),
+            (const void*)(from + off),
             (__attribute__((address_space(3))) void*)(dst + q * THREADS * 16), 16, 0, 0);
         if (q < PB)
             __builtin_amdgcn_global_load_lds(
@@ -494,24 +574,32 @@ __global__ __launch_bounds__(256, T + TJ == 512 ? 1 : 2) void gemm_tn_bf16_wide(
     // lane's operand addresses inside a stage: row, segment (2h + g2) ^ swizzle
     const int sw = (j >> 2) & 3;
     const uint32_t smb = (uint32_t)(uintptr_t)sm;
-    const uint32_t a_lane[2] = {smb + (wm * WTM + j) * 64 + ((g2) ^ sw) * 16,
-                                smb + (wm * WTM + j) * 64 + ((2 + g2) ^ sw) * 16};
+    uint32_t a_lane[2];
+    if constexpr (DIRECT) {
+        const int row = 8 * (l >> 5) + ((l & 15) >> 2), piece = wm * (WTM / 16) + ((l >> 4) & 1);
+        a_lane[0] = smb + row * (T * 2) + (piece ^ tr_swizzle(row)) * 32 + (l & 3) * 8;
+        a_lane[1] = a_lane[0] + 16 * (T * 2);
+    } else {
+        a_lane[0] = smb + (wm * WTM + j) * 64 + ((g2) ^ sw) * 16;
+        a_lane[1] = smb + (wm * WTM + j) * 64 + ((2 + g2) ^ sw) * 16;
+    }
     const uint32_t b_lane[2] = {smb + A_BYTES + (wn * WTN + j) * 64 + ((g2) ^ sw) * 16,
                                 smb + A_BYTES + (wn * WTN + j) * 64 + ((2 + g2) ^ sw) * 16};
     auto ring = [&](int st) { return (uint32_t)((st % NS) * STAGE_BYTES); };
 
     v16f acc[MI][NI];
-    v4i ax[MI], ay[MI], bx[NI], by[NI];
+    using AOp = std::conditional_t<DIRECT, TrOp, v4i>;
+    AOp ax[MI], ay[MI];
+    v4i bx[NI], by[NI];
     // acc += ac x bc; an, bn = operands at ad_a, ad_b, valid on return; between(mi) is placed behind the
     // MFMAs of row mi: the DMA of a stage, whose addresses and issue would otherwise idle the pipe
-    auto half_step = [&](const v4i(&ac)[MI], const v4i(&bc)[NI], v4i(&an)[MI], v4i(&bn)[NI], uint32_t ad_a,
+    auto half_step = [&](const AOp(&ac)[MI], const v4i(&bc)[NI], AOp(&an)[MI], v4i(&bn)[NI], uint32_t ad_a,
                          uint32_t ad_b, auto between) {
 #pragma unroll
         for (int mi = 0; mi < MI; ++mi) {
 #pragma unroll
             for (int s = 0; s < NI; ++s)
-                acc[mi][s] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, ac[mi]),
-                                                                     __builtin_bit_cast(v8bf, bc[s]),
+                acc[mi][s] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wide_operand(ac[mi]), wide_operand(bc[s]),
                                                                      acc[mi][s], 0, 0, 0);
             __builtin_amdgcn_sched_barrier(0);
             if (mi == 0) wide_issue(an, bn, ad_a, ad_b);
@@ -570,7 +658,14 @@ __global__ __launch_bounds__(256, T + TJ == 512 ? 1 : 2) void gemm_tn_bf16_wide(
         if constexpr (EXP) {
             Cs += (int64_t)current * I * J;
             // nothing but zeros of an expert without slots, whatever gamma is
-            if (smE.from[current] == smE.to[current]) sc = 0.f;
+            if (smE.from[current] == smE.to[current]) {
+                sc = 0.f;
+                if constexpr (DIRECT)  // of a row that is not the expert's
+#pragma unroll
+                    for (int mi = 0; mi < MI; ++mi)
+#pragma unroll
+                        for (int s = 0; s < NI; ++s) acc[mi][s] = v16f{};
+            }
             current = expert;
         }
         if (i0n >= 0) {
@@ -1299,15 +1394,18 @@ void launch_experts_dx(const ExpertsOperands& a, const ExpertsBackwardPlan& p, h
 
 void launch_experts_dw(const ExpertsOperands& a, const ExpertsBackwardPlan& p, hipStream_t s) {
     const int64_t T = p.dw_tile == 1 ? 256 : 128, gi = (a.N + T - 1) / T, gj = (a.K + 127) / 128;
-    const ExpertsRing ex{a.offsets, a.E, (int)a.T, a.least, 0, 0, nullptr, 0};
+    const ExpertsRing ex{a.offsets, a.E, (int)a.T, a.least, (uint32_t)(a.N * 2), a.N * 2, nullptr, 0};
     const RingSlices sl{p.dw_splits, 0};
     const int64_t items = gi * gj * a.E * sl.splits, cap = (int64_t)ring_cus() * 2;
     const unsigned grid = (unsigned)(items < cap ? items : cap);
     const bool cut = sl.splits > 1;
-    const auto kernel = cut              ? gemm_tn_bf16_wide<128, 4, true, true>
-                        : p.dw_tile == 1 ? gemm_tn_bf16_wide<256, 3, false, true, 128>
-                                         : gemm_tn_bf16_wide<128, 4, false, true>;
-    kernel<<<grid, 256, 0, s>>>(a.gwT, a.qT, a.N, a.K, 0, cut ? nullptr : a.gamma,
+    const auto kernel = a.direct_dw ? (cut              ? gemm_tn_bf16_wide<128, 4, true, true, 128, true>
+                                       : p.dw_tile == 1 ? gemm_tn_bf16_wide<256, 3, false, true, 128, true>
+                                                        : gemm_tn_bf16_wide<128, 4, false, true, 128, true>)
+                                    : (cut              ? gemm_tn_bf16_wide<128, 4, true, true>
+                                       : p.dw_tile == 1 ? gemm_tn_bf16_wide<256, 3, false, true, 128>
+                                                        : gemm_tn_bf16_wide<128, 4, false, true>);
+    kernel<<<grid, 256, 0, s>>>(a.direct_dw ? a.dY : a.gwT, a.qT, a.N, a.K, 0, cut ? nullptr : a.gamma,
                                 a.gamma && !cut ? 1.0f / 128.0f : 1.0f, cut ? a.part : a.dW, (int)gi, (int)gj, 0, 0, sl, ex);
     if (!cut) return;
     const bool vec = ((uintptr_t)a.dW & 15) == 0;

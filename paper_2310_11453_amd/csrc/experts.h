@@ -88,7 +88,8 @@ hipError_t launch_matmul_experts(const ExpertsArgs& a, hipStream_t s);
 struct ExpertsOperands {
     const uint16_t *g, *gwT, *qT;
     const uint32_t* Sw;
-    bool direct;
+    const uint16_t* dY;
+    bool direct, direct_dw;  // dX, dW read dY itself
     const int32_t* offsets;
     int E, least;
     int64_t T, N, K;

@@ -4,10 +4,12 @@
 // dY is bf16, +-1 and the codes are exact in bf16.  As in the plain layer (backward.hip, whose kernels take the
 // products), every operand is first written once in the layout they read:
 //   g    [T][Np]       rows of dY                                 (A operand of dX, reduction over N; not where N is a
-//                      multiple of 32: the product reads dY itself, at the same speed, and the copies for 8192 slots
-//                      2048 -> 8192 take 81 us instead of 100)
+//                      multiple of 32: the product reads dY itself, at the same speed; 8192 slots 2048 -> 8192
+//                      680 us with the copy, 662 without)
 //   Sw   [E][Np/32][K] the signs of 32 weight rows of a column    (B operand of dX)
-//   gwT  [N][slots]    dY transposed, with a gamma per token scaled and rounded again   (A operand of dW)
+//   gwT  [N][slots]    dY transposed, with a gamma per token scaled and rounded again   (A operand of dW; not with a gamma
+//                      per tensor and N a multiple of 32: the product reads dY itself, transposed out of LDS; both
+//                      products of those 8192 slots 618 us with the copy, 562 without)
 //   qT   [K][slots]    codes transposed, gathered through the order                     (B operand of dW)
 // The slots of the last two are those of expert after expert, each expert's filled up with zeros to whole blocks of 32:
 // a stage of the products is such a block and belongs to one expert.
@@ -215,12 +217,13 @@ hipError_t launch_experts_backward(const ExpertsArgs& a, hipStream_t s) {
     b.row_gamma = a.per_tensor ? nullptr : a.gamma;
     b.offsets = a.offsets; b.order = a.order; b.top_k = (uint32_t)a.top_k; b.rows = (uint32_t)a.rows;
     b.E = a.E; b.T = (int)a.T; b.least = p.dw_splits;
+    const bool direct = experts_dy_direct(a.N), direct_dw = direct && a.per_tensor && ((uintptr_t)a.dY & 15) == 0;
     if (a.dX) {
-        b.g = experts_dy_direct(a.N) ? nullptr : (uint16_t*)base;
+        b.g = direct ? nullptr : (uint16_t*)base;
         b.Sw = (uint32_t*)(base + ws.words);
     }
     if (a.dW) {
-        b.gwT = (uint16_t*)(base + ws.gwT);
+        b.gwT = direct_dw ? nullptr : (uint16_t*)(base + ws.gwT);
         b.qT = (uint16_t*)(base + ws.qT);
     }
     b.N = a.N; b.K = a.K; b.Np = pad32(a.N);
@@ -241,8 +244,7 @@ hipError_t launch_experts_backward(const ExpertsArgs& a, hipStream_t s) {
     if (a.N % 8 == 0 && ((uintptr_t)a.dY & 15) == 0) prepare_expert_operands<true><<<grid, 256, 0, s>>>(b);
     else prepare_expert_operands<false><<<grid, 256, 0, s>>>(b);
 
-    const bool direct = experts_dy_direct(a.N);
-    ExpertsOperands o{direct ? a.dY : b.g, b.gwT, b.qT, b.Sw, direct, a.offsets, a.E, b.least, a.T, a.N, a.K, a.beta,
+    ExpertsOperands o{direct ? a.dY : b.g, b.gwT, b.qT, b.Sw, a.dY, direct, direct_dw, a.offsets, a.E, b.least, a.T, a.N, a.K, a.beta,
                       a.per_tensor ? a.gamma : nullptr, a.dX, a.dW, (float*)(base + ws.part)};
     if (a.dX) launch_experts_dx(o, p, s);
     if (a.dW) launch_experts_dw(o, p, s);

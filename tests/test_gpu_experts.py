@@ -247,6 +247,33 @@ def test_backward_variants(bl, tuning, M, top_k, E, K, N, spec):
     check_backward(bl, M, top_k, E, K, N, True, True, choices(M, top_k, E, M, only=[1]))
 
 
+# dW with one gamma a tensor and N a multiple of 32, where dY is read transposed: slots that end inside a block of 32 and
+# experts without any, columns that end inside a tile, both tiles and slices.  On integers, so exact; one expert's NaN stay
+# with it.
+@pytest.mark.parametrize("M", [1, 16, 33, 200, 700])
+@pytest.mark.parametrize("N,K", [(32, 32), (288, 160), (512, 416), (1312, 128)])
+@pytest.mark.parametrize("spec", ["bwd_ring=1", "bwd_ring=2", "bwd_ring=2,bwd_splits=3", "bwd_ring=1,bwd_grid=2"])
+def test_backward_dw_from_dy(bl, tuning, M, N, K, spec):
+    print(f"backward dW from dY M={M} N={N} K={K} {spec}", flush=True)
+    tuning(spec)
+    E, top_k = 6, 2
+    c = make(bl, M, top_k, E, K, N, True, True, choices(M, top_k, E, M + N, unrouted=0.1))
+    dY = torch.randint(-4, 5, (c["T"], N), generator=torch.Generator().manual_seed(1)).to(torch.bfloat16)
+    bad = int(np.argmax(np.diff(c["offsets"])))
+    dY[c["offsets"][bad]:c["offsets"][bad + 1], ::7] = float("nan")
+    dY[c["offsets"][-1]:] = float("nan")
+    _, dw = bl.bitlinear_backward_ste_experts(dY.cuda(), c["codes"].cuda(), torch.full((1,), 128.0, device="cuda"), None,
+                                              None, **c["calls"], want_dx=False)
+    for e in range(E):
+        mine = slice(c["offsets"][e], c["offsets"][e + 1])
+        ref = dY[mine].double().nan_to_num().T @ c["codes"].double()[c["row"][mine]]
+        got = dw[e].cpu().double()
+        if e == bad and mine.start < mine.stop:
+            assert bool(got[::7].isnan().all())
+            got[::7] = ref[::7]
+        assert torch.equal(got, ref)
+
+
 # dX in whole rounds of workgroups and a last one whose tiles are cut into slices: the number of slots moves the last round
 # through nothing, a tile and more tiles than leave room for slices.  On integers, so exact.
 @pytest.mark.parametrize("M", [1, 129, 500, 1000, 1040, 1100, 1500, 1900, 2048])
