@@ -327,7 +327,7 @@ int bitlinear_layernorm_backward(const float* dXhat, const float* X, int64_t M, 
  * Limits: experts 1..256, top_k 1..64, M * top_k <= 2^30 (else BL_ERR_SHAPE); bitlinear_route takes up to
  * 2^24 choices, the products K <= 65536, bitlinear_quant_nonlinear and its backward M < 2^24 rows and M * K <=
  * 2^36 (else BL_ERR_UNSUPPORTED, which is also the answer to operands that are read several elements at a time
- * and not 16-byte aligned: codes, packed, U, check, dXhat, dU, and dY for a dX with N % 32 == 0).
+ * and not 16-byte aligned: codes, packed, U, check, dXhat, dU, and dY with N % 32 == 0).
  *   packed  `experts` consecutive blobs of bitlinear_packed_bytes(N, K, 0) bytes, one bitlinear_pack_weights
  *           call each (N % 16 == 0 and experts <= 64: bitlinear_pack_weights_grouped of the [experts * N, K]
  *           matrix with groups_n = experts writes the same bytes)

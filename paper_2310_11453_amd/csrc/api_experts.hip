@@ -75,10 +75,11 @@ size_t bitlinear_workspace_bytes_experts(int op, int64_t M, int top_k, int64_t N
         case BL_OP_ROUTE:
             return experts_ok(experts) && M * top_k <= kMaxRouteSlots ? route_bytes(M * top_k, experts) : 0;
         case BL_OP_QUANT_NONLINEAR:
-            return granularity == BL_GAMMA_PER_TENSOR && nonlinear_rows_ok(M * top_k, 0) ? nonlinear_ws(M * top_k).total : 0;
+            return granularity == BL_GAMMA_PER_TENSOR && nonlinear_rows_ok(M * top_k, 0)
+                       ? nonlinear_ws(M * top_k).total : 0;
         case BL_OP_BACKWARD:
             if (experts_status(M, top_k, N, K, experts, granularity) != BL_OK) return 0;
-            return experts_backward_bytes(M * top_k, N, K, experts) + 256;
+            return experts_backward_bytes(M * top_k, N, K, experts, granularity == BL_GAMMA_PER_TENSOR) + 256;
         default:
             return 0;
     }
@@ -120,10 +121,12 @@ int bitlinear_backward_ste_experts(const void* dY, int64_t M, int top_k, int64_t
     if (!dY || !gamma || !offsets) return BL_ERR_NULL;
     if (dX && (!packed || !beta)) return BL_ERR_NULL;
     if (dW && !codes) return BL_ERR_NULL;
-    if ((dX && experts_dy_direct(N) && !aligned16((const char*)dY)) || (dX && !aligned16((const char*)packed)) ||
+    if ((experts_dy_direct(N) && !aligned16((const char*)dY)) || (dX && !aligned16((const char*)packed)) ||
         (dW && !aligned16(codes)))
         return BL_ERR_UNSUPPORTED;
-    if (!workspace || workspace_bytes < experts_backward_bytes(M * top_k, N, K, experts) + 256) return BL_ERR_WORKSPACE;
+    const bool per_tensor = granularity == BL_GAMMA_PER_TENSOR;
+    if (!workspace || workspace_bytes < experts_backward_bytes(M * top_k, N, K, experts, per_tensor) + 256)
+        return BL_ERR_WORKSPACE;
     ExpertsArgs a = experts_args(codes, gamma, M, top_k, N, K, order, offsets, experts, packed, beta, granularity);
     a.dY = (const uint16_t*)dY; a.dX = dX; a.dW = dW;
     a.workspace = (void*)(((uintptr_t)workspace + 255) & ~(uintptr_t)255);

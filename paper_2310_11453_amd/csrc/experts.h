@@ -103,9 +103,9 @@ size_t experts_dx_part_bytes(int64_t T, int64_t K, int E, const ExpertsBackwardP
 ExpertsBackwardPlan experts_backward_plan(int64_t T, int64_t N, int64_t K, int E);
 void launch_experts_dx(const ExpertsOperands& a, const ExpertsBackwardPlan& p, hipStream_t s);
 void launch_experts_dw(const ExpertsOperands& a, const ExpertsBackwardPlan& p, hipStream_t s);
-// dX reads dY where it lies; else a copy in whole stages of 32 columns is made.
+// dX, and dW with one gamma a tensor, read dY where it lies; else copies in whole stages of 32 are made.
 inline bool experts_dy_direct(int64_t N) { return N % 32 == 0 && N < (1 << 23); }
-size_t experts_backward_bytes(int64_t T, int64_t N, int64_t K, int E);
+size_t experts_backward_bytes(int64_t T, int64_t N, int64_t K, int E, bool per_tensor);
 hipError_t launch_experts_backward(const ExpertsArgs& a, hipStream_t s);
 
 #ifdef __HIPCC__

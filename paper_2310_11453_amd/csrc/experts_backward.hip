@@ -188,13 +188,13 @@ int64_t pad32(int64_t v) { return (v + 31) / 32 * 32; }
 struct ExpertsWs {
     size_t words, gwT, qT, part, total;
 };
-ExpertsWs experts_ws(int64_t T, int64_t N, int64_t K, int E, const ExpertsBackwardPlan& p) {
+ExpertsWs experts_ws(int64_t T, int64_t N, int64_t K, int E, bool per_tensor, const ExpertsBackwardPlan& p) {
     auto al = [](size_t v) { return (v + 255) & ~(size_t)255; };
     const int64_t Np = pad32(N), slots = most_tiles(T, E, 32, p.dw_splits) * 32;
     ExpertsWs w{};
     w.words = experts_dy_direct(N) ? 0 : al((size_t)T * Np * 2);
     w.gwT = w.words + al((size_t)E * (Np / 32) * K * 4);
-    w.qT = w.gwT + al((size_t)N * slots * 2);
+    w.qT = w.gwT + (experts_dy_direct(N) && per_tensor ? 0 : al((size_t)N * slots * 2));
     w.part = w.qT + al((size_t)K * slots * 2);
     // one product after the other
     const size_t dx = experts_dx_part_bytes(T, K, E, p);
@@ -204,20 +204,20 @@ ExpertsWs experts_ws(int64_t T, int64_t N, int64_t K, int E, const ExpertsBackwa
 }
 }  // namespace
 
-size_t experts_backward_bytes(int64_t T, int64_t N, int64_t K, int E) {
-    return experts_ws(T, N, K, E, experts_backward_plan(T, N, K, E)).total;
+size_t experts_backward_bytes(int64_t T, int64_t N, int64_t K, int E, bool per_tensor) {
+    return experts_ws(T, N, K, E, per_tensor, experts_backward_plan(T, N, K, E)).total;
 }
 
 hipError_t launch_experts_backward(const ExpertsArgs& a, hipStream_t s) {
     const ExpertsBackwardPlan p = experts_backward_plan(a.T, a.N, a.K, a.E);
-    const ExpertsWs ws = experts_ws(a.T, a.N, a.K, a.E, p);
+    const ExpertsWs ws = experts_ws(a.T, a.N, a.K, a.E, a.per_tensor, p);
     char* const base = (char*)a.workspace;
     exb::Args b{};
     b.dY = a.dY; b.codes = a.codes; b.packed = a.packed;
     b.row_gamma = a.per_tensor ? nullptr : a.gamma;
     b.offsets = a.offsets; b.order = a.order; b.top_k = (uint32_t)a.top_k; b.rows = (uint32_t)a.rows;
     b.E = a.E; b.T = (int)a.T; b.least = p.dw_splits;
-    const bool direct = experts_dy_direct(a.N), direct_dw = direct && a.per_tensor && ((uintptr_t)a.dY & 15) == 0;
+    const bool direct = experts_dy_direct(a.N), direct_dw = direct && a.per_tensor;
     if (a.dX) {
         b.g = direct ? nullptr : (uint16_t*)base;
         b.Sw = (uint32_t*)(base + ws.words);
@@ -244,8 +244,8 @@ hipError_t launch_experts_backward(const ExpertsArgs& a, hipStream_t s) {
     if (a.N % 8 == 0 && ((uintptr_t)a.dY & 15) == 0) prepare_expert_operands<true><<<grid, 256, 0, s>>>(b);
     else prepare_expert_operands<false><<<grid, 256, 0, s>>>(b);
 
-    ExpertsOperands o{direct ? a.dY : b.g, b.gwT, b.qT, b.Sw, a.dY, direct, direct_dw, a.offsets, a.E, b.least, a.T, a.N, a.K, a.beta,
-                      a.per_tensor ? a.gamma : nullptr, a.dX, a.dW, (float*)(base + ws.part)};
+    const ExpertsOperands o{direct ? a.dY : b.g, b.gwT, b.qT, b.Sw, a.dY, direct, direct_dw, a.offsets, a.E, b.least, a.T,
+                            a.N, a.K, a.beta, a.per_tensor ? a.gamma : nullptr, a.dX, a.dW, (float*)(base + ws.part)};
     if (a.dX) launch_experts_dx(o, p, s);
     if (a.dW) launch_experts_dw(o, p, s);
     return hipGetLastError();
