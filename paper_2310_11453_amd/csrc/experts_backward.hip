@@ -37,7 +37,7 @@ struct Args {
     uint32_t* Sw;
     int64_t N, K, Np, blob;
     uint32_t bits_items, code_items, items;    // items: of all three parts
-    uint32_t bits_x, bits_y, code_x, dy_x;     // items in a row of each part; rows of sign words of an expert
+    uint32_t bits_x, bits_y, code_x, dy_x;     // items in a row of each part; pairs of rows of sign words of an expert
 };
 }  // namespace exb
 
@@ -132,26 +132,55 @@ __device__ inline void copy_tile(const exb::Args& a, const ExpertTiles& count, i
     }
 }
 
-// signs of 32 weight rows x 512 columns of an expert (the bit layout of a word: bits_transpose_tile of backward.hip)
-__device__ inline void words_tile(const exb::Args& a, int e, int64_t sw, int64_t tk, uint32_t (&sm)[2][256]) {
-    const int64_t TN = tiles_n(a.N), TK = tiles_k(a.K);
-    for (int t = 0; t < 2; ++t)
-        sm[t][threadIdx.x] =
-            2 * sw + t < TN ? a.packed[e * a.blob + tile_dword_offset(2 * sw + t, tk, TK) + threadIdx.x] : 0u;
-    __syncthreads();
-    for (int it = 0; it < 2; ++it) {
-        const int kl = it * 256 + (int)threadIdx.x;
-        const int64_t k = tk * kChunkK + kl;
-        if (k >= a.K) continue;
-        const int i = kl >> 6, g = (kl & 63) >> 4, d = (kl & 15) >> 2, j = kl & 3;
-        uint32_t word = 0;
+// 32 x 32 bits, row l of them in lane l (of each half of a wave), transposed: five exchanges with the lane whose number
+// differs in one bit.  What a rotation by s bits brings around lands where the lane keeps its own.
+struct BitTranspose {
+    uint32_t keep[5], turn[5];
+    __device__ inline explicit BitTranspose(int l) {
+        constexpr uint32_t kLow[5] = {0x55555555u, 0x33333333u, 0x0f0f0f0fu, 0x00ff00ffu, 0x0000ffffu};
 #pragma unroll
-        for (int r = 0; r < 32; ++r) {
-            const uint32_t dw = sm[r >> 4][(g * 16 + (r & 15)) * 4 + d];
-            const uint32_t minus = ((dw >> (8 * j + i)) & 1u) ^ 1u;
-            word |= minus << (8 * (r >> 4) + 4 * ((r & 15) >> 3) + ((r & 7) >> 1) + 16 * (r & 1));
+        for (int b = 0; b < 5; ++b) {
+            const bool high = (l >> b) & 1;
+            keep[b] = high ? ~kLow[b] : kLow[b];
+            turn[b] = high ? 1u << b : 32u - (1u << b);  // to the right
         }
-        a.Sw[(e * (a.Np / 32) + sw) * a.K + k] = word;
+    }
+    template <int B>
+    __device__ inline uint32_t step(uint32_t x) const {
+        const uint32_t t = (uint32_t)__builtin_amdgcn_ds_swizzle((int)x, (1 << B) << 10 | 0x1f);  // of lane l ^ 2^B
+        return (x & keep[B]) | (__builtin_amdgcn_alignbit(t, t, turn[B]) & ~keep[B]);
+    }
+    __device__ inline uint32_t operator()(uint32_t x) const {
+        return step<0>(step<1>(step<2>(step<3>(step<4>(x)))));
+    }
+};
+
+// signs of two times 32 weight rows x 512 columns of an expert (the bit layout of a word: bits_transpose_tile of
+// backward.hip).  A dword of a packed tile is a row's bits of 32 columns, and lane l takes the row that is bit l of a
+// word: a wave transposes four times 2 x 32 rows x 32 columns.  (A column's 32 bits picked one by one: the backward of 128
+// slots of 8 experts 2048 -> 8192 156 us, 146 so; of 8192 slots 552 and 543.)
+__device__ inline void words_tile(const exb::Args& a, int e, int64_t pair, int64_t tk, uint32_t (&sm)[2][8 * 68]) {
+    const int64_t TN = tiles_n(a.N), TK = tiles_k(a.K), words = a.Np / 32;
+    const int w = (int)threadIdx.x / kWave, l = (int)threadIdx.x & (kWave - 1), b = l & 31;
+    const int half = w >> 1, g = 2 * (w & 1) + (l >> 5);
+    const int row = ((b >> 4) & 1) | (b & 3) << 1 | ((b >> 2) & 1) << 3 | ((b >> 3) & 1) << 4;
+    const int64_t tn = 2 * (2 * pair + half) + (row >> 4);
+    uint32_t q[4] = {0, 0, 0, 0};
+    if (tn < TN) {
+        const uint4 v = *reinterpret_cast<const uint4*>(a.packed + e * a.blob + tile_dword_offset(tn, tk, TK) +
+                                                        (g * 16 + (row & 15)) * 4);
+        q[0] = v.x, q[1] = v.y, q[2] = v.z, q[3] = v.w;
+    }
+    const BitTranspose transpose(b);
+#pragma unroll
+    for (int d = 0; d < 4; ++d)  // bit 8 j + i of a dword: column 64 i + 16 g + 4 d + j
+        sm[half][(b & 7) * 68 + 16 * g + 4 * d + (b >> 3)] = ~transpose(q[d]);
+    __syncthreads();
+#pragma unroll
+    for (int it = 0; it < 4; ++it) {
+        const int kl = (it & 1) * 256 + (int)threadIdx.x;
+        const int64_t sw = 2 * pair + (it >> 1), k = tk * kChunkK + kl;
+        if (sw < words && k < a.K) a.Sw[(e * words + sw) * a.K + k] = sm[it >> 1][(kl >> 6) * 68 + (kl & 63)];
     }
 }
 
@@ -160,7 +189,7 @@ __global__ __launch_bounds__(256) void prepare_expert_operands(exb::Args a) {
     __shared__ ExpertTiles count;
     __shared__ __attribute__((aligned(16))) union {
         exb::CastTile tile;
-        uint32_t words[2][256];
+        uint32_t words[2][8 * 68];
     } sm;
     const int blocks = expert_tiles(a.offsets, a.E, a.T, 32, count, a.least);
     for (uint32_t it = blockIdx.x; it < a.items; it += gridDim.x) {
@@ -231,7 +260,7 @@ hipError_t launch_experts_backward(const ExpertsArgs& a, hipStream_t s) {
     auto tiles = [](int64_t v) { return (v + exb::kCols - 1) / exb::kCols; };
     const int64_t rows = (most_tiles(a.T, a.E, 32, b.least) + 1) / 2;
     b.bits_x = (uint32_t)tiles_k(a.K);
-    b.bits_y = (uint32_t)(b.Np / 32);
+    b.bits_y = (uint32_t)((b.Np / 32 + 1) / 2);
     b.code_x = (uint32_t)tiles(a.K);
     b.dy_x = (uint32_t)tiles(b.g ? b.Np : b.N);
     const int64_t bits = a.dX ? (int64_t)a.E * b.bits_y * b.bits_x : 0, codes = a.dW ? rows * b.code_x : 0;
