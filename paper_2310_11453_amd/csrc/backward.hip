@@ -264,8 +264,8 @@ struct RingSlices {
 struct ExpertsRing {
     const int32_t* offsets;
     int E, T, least;
-    uint32_t a_pitch;  // dX: bytes from a row of A to the next, and from a stage to the next
-    int64_t a_step;
+    uint32_t a_pitch;  // bytes from a row of A to the next (dX, and dW from dY itself);
+    int64_t a_step;    // dX: from a stage to the next; dW: a_pitch
     float* part;  // dX: room for a tile of every workgroup; slices (0, 1: none) of a tile at most
     int slices;
 };
@@ -449,8 +449,8 @@ __global__ __launch_bounds__(256, T + TJ == 512 ? 1 : 2) void gemm_tn_bf16_wide(
     auto tile_origin = [&](int t, int64_t& i0, int64_t& j0) {
         if constexpr (EXP) {
             // Each XCD gets a contiguous eighth of every expert's tiles.  (An eighth of all tiles is an expert each of
-            // eight, and the one with the most slots sets the time: 8192 slots of 8 experts, 2048 -> 8192, 524 us, so
-            // 346.)
+            // eight, and the one with the most slots sets the time: 8192 slots of 8 experts, 2048 -> 8192, 524 us in
+            // 256 x 256 tiles, so 346.)
             const int per = grid_i * grid_j;
             int tile = SPLIT ? t / sl.splits : t;
             expert = tile / per;
@@ -1308,8 +1308,8 @@ __global__ __launch_bounds__(256) void fold_expert_tails(ExpertsRing ex, int S, 
 }
 // dW of every expert; zeros where it has no slots, whatever gamma is
 template <bool VEC>
-__global__ __launch_bounds__(256) void fold_expert_weights(const float* __restrict__ part, int splits, int64_t count, int E,
-                                                           int T, const int32_t* __restrict__ offsets,
+__global__ __launch_bounds__(256) void fold_expert_weights(const float* __restrict__ part, int splits, int64_t count,
+                                                           int E, int T, const int32_t* __restrict__ offsets,
                                                            const float* __restrict__ gamma, float* __restrict__ out) {
     constexpr int W = VEC ? 4 : 1;
     const int e = (int)blockIdx.y;
@@ -1351,9 +1351,10 @@ ExpertsBackwardPlan experts_backward_plan(int64_t T, int64_t N, int64_t K, int E
                                                              : tiles > 0.9 * slots && nst >= 96;
     p.dx_slices = !cut ? 1 : force ? force : 16;
     // 256 x 128 tiles where there are four rounds of them and an expert's slots are six stages or more; slices only of
-    // the small ones.  dW alone with its copies, us in 128 x 128 / 256 x 128: 4270 slots of 5 experts 4992 -> 7936 438
-    // / 400, 9554 of 18 2048 -> 4096 264 / 246; fewer tiles, 7510 of 29 704 -> 2656 90 / 106, or stages, 1880 of 16
-    // 4096 -> 4096 208 / 218.  (256 x 256, one workgroup a CU: 479 and 286.)
+    // the small ones.  dW alone with its copies, a gamma per tensor, us in 128 x 128 / 256 x 128: 4270 slots of 5
+    // experts 4992 -> 7936 423 / 388, 9554 of 18 2048 -> 4096 236 / 222; fewer tiles, 7510 of 29 704 -> 2656 78 / 91,
+    // or stages, 1880 of 16 4096 -> 4096 212 / 220.  (256 x 256, one workgroup a CU, with a copy of dY: 479 and 286
+    // where 256 x 128 took 400 and 246.)
     const double wide_tiles = E * tiles_of(N, 256) * tiles_of(K, 128);
     p.dw_tile = wide_tiles >= 8 * cus && (double)T >= 192.0 * E ? 1 : 2;
     if (t.bwd_ring == 1 || t.bwd_ring == 2) p.dw_tile = t.bwd_ring;
@@ -1386,8 +1387,8 @@ void launch_experts_dx(const ExpertsOperands& a, const ExpertsBackwardPlan& p, h
     ExpertsRing ex{a.offsets, a.E, (int)a.T, 0, 64, a.T * 64, a.part, p.dx_slices};
     if (a.direct) ex.a_pitch = (uint32_t)(a.N * 2), ex.a_step = 64;
     const int grid = dx_grid(a.T, a.K, a.E, p), S = grid / 8;
-    gemm_tn_signs_ring<128, 4, false, true><<<(unsigned)grid, 512, 0, s>>>(a.g, a.Sw, a.T, a.K, Np, a.beta, 1.0f, a.dX, 0,
-                                                                          (int)gj, 0, 0, {}, ex);
+    gemm_tn_signs_ring<128, 4, false, true><<<(unsigned)grid, 512, 0, s>>>(a.g, a.Sw, a.T, a.K, Np, a.beta, 1.0f, a.dX,
+                                                                          0, (int)gj, 0, 0, {}, ex);
     if (p.dx_slices < 4 || S < 4 || nst < 32) return;  // tail_plan cuts nothing
     fold_expert_tails<<<1024, 256, 0, s>>>(ex, S, (int)nst, (int)gj, a.K, a.dX);
 }
@@ -1406,13 +1407,14 @@ void launch_experts_dw(const ExpertsOperands& a, const ExpertsBackwardPlan& p, h
                                        : p.dw_tile == 1 ? gemm_tn_bf16_wide<256, 3, false, true, 128>
                                                         : gemm_tn_bf16_wide<128, 4, false, true>);
     kernel<<<grid, 256, 0, s>>>(a.direct_dw ? a.dY : a.gwT, a.qT, a.N, a.K, 0, cut ? nullptr : a.gamma,
-                                a.gamma && !cut ? 1.0f / 128.0f : 1.0f, cut ? a.part : a.dW, (int)gi, (int)gj, 0, 0, sl, ex);
+                                a.gamma && !cut ? 1.0f / 128.0f : 1.0f, cut ? a.part : a.dW, (int)gi, (int)gj, 0, 0,
+                                sl, ex);
     if (!cut) return;
     const bool vec = ((uintptr_t)a.dW & 15) == 0;
     const int64_t count = a.N * a.K, wide = (count / (vec ? 4 : 1) + 255) / 256;
     const auto fold = vec ? fold_expert_weights<true> : fold_expert_weights<false>;
-    fold<<<dim3((unsigned)(wide < 4096 ? wide : 4096), (unsigned)a.E), 256, 0, s>>>(a.part, sl.splits, count, a.E, (int)a.T,
-                                                                                   a.offsets, a.gamma, a.dW);
+    fold<<<dim3((unsigned)(wide < 4096 ? wide : 4096), (unsigned)a.E), 256, 0, s>>>(
+        a.part, sl.splits, count, a.E, (int)a.T, a.offsets, a.gamma, a.dW);
 }
 
 }  // namespace bl
