@@ -164,9 +164,9 @@ int bitlinear_quant_nonlinear(const float* U, int64_t M, int64_t K, int fn, floa
     if (M == 0) return BL_OK;
     if (!nonlinear_rows_ok(M, K)) return BL_ERR_UNSUPPORTED;
     if (!U || !codes || !gamma || (check && !check_scale)) return BL_ERR_NULL;
-    if (!aligned16(U, codes, check, (const char*)workspace)) return BL_ERR_UNSUPPORTED;
     const NonlinearWs ws = nonlinear_ws(M);
     const bool per_tensor = granularity == BL_GAMMA_PER_TENSOR;
+    if (!aligned16(U, codes, check) || (per_tensor && !aligned16((const char*)workspace))) return BL_ERR_UNSUPPORTED;
     if (per_tensor && (!workspace || workspace_bytes < ws.total)) return BL_ERR_WORKSPACE;
     NonlinearArgs a{};
     a.U = U; a.M = M; a.K = K; a.eps = ln_eps; a.rows = rows; a.per_tensor = per_tensor;
