@@ -394,7 +394,8 @@ int bitlinear_combine_backward(const float* dY, const float* slots, const int32_
  *   rows         in   int32 [1] (device) or NULL: only rows below it are read and written (of a routed batch:
  *                     offsets + experts); without any a gamma per tensor is its lower bound
  *   check        out  int8 [M,K] or NULL: rne(u * (127 / m)), m the largest magnitude of each 128
- *                     consecutive elements of a row (the last ones of a row may be fewer)
+ *                     consecutive elements of a row (the last ones of a row may be fewer), or 127 * 2^-127 where
+ *                     it is smaller; zeros where all of them are zero
  *   check_scale  out  fp32 [M][(K + 127) / 128]: m / 127
  *   workspace         per tensor only: bitlinear_workspace_bytes_experts(BL_OP_QUANT_NONLINEAR, M, 1, ...) */
 int bitlinear_quant_nonlinear(const float* U, int64_t M, int64_t K, int fn, float ln_eps,

@@ -3,6 +3,7 @@
 // checkpoint of u; and the backward pass, from that checkpoint.
 //   forward    h = f(u), x^ = (h - mean h) / sqrt(var h + eps), gamma = max|x^|, code = clamp(rne(x^ * (128 / gamma)))
 //              checkpoint, per block b of 128 elements of a row: c = rne(u * (127 / amax_b)), kept beside amax_b / 127
+//              (amax_b, where not zero, at least kLeastMax)
 //   backward   v = c * (amax_b / 127), h = f(v), n = (h - mean h) / sqrt(var h + eps)
 //              du = f'(v) * (g - mean g - n mean(g n)) / sqrt(var h + eps),  g = the gradient of x^
 // The backward is the derivative of the forward at v, exactly: its statistics are those of f(v), which come out of the
@@ -68,6 +69,10 @@ __device__ inline float half_wave_max(float v) {
     return max_raw(lo, hi);
 }
 
+// Of a block of tiny values 127 / m passes the largest float (m < 3.7e-37), and its zeros would be 0 * inf: its step m / 127
+// is taken to be 2^-127.
+constexpr float kLeastMax = 127.f * 0x1p-127f;
+
 // WPR waves share a row, a lane holds NV float4 of it.  kRowStats and kRowApply: the two passes of a gamma per tensor;
 // the first leaves the row's statistics in rowstats and its largest magnitude where its codes will be, which nobody
 // writes before the second.
@@ -105,7 +110,8 @@ __global__ __launch_bounds__((WPR < 4 ? 4 : WPR) * kWave) void nonlinear_rows(No
             const bool in = idx < K4;
             const float4 x = v[j];
             const float mine = max_raw(max_raw(fabsf(x.x), fabsf(x.y)), max_raw(fabsf(x.z), fabsf(x.w)));
-            const float big = half_wave_max(in ? mine : 0.f);
+            float big = half_wave_max(in ? mine : 0.f);
+            big = big > 0.f ? max_raw(big, kLeastMax) : 0.f;
             const float up = big > 0.f ? 127.f / big : 0.f;
             if (in && live) {
                 c4[idx] = code_word(x.x * up, x.y * up, x.z * up, x.w * up, -127.f);

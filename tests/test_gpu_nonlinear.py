@@ -221,3 +221,37 @@ def test_rows_behind_the_last_are_left_alone(bl, per_tensor):
         out = torch.full((M, K), 9.0, dtype=torch.bfloat16, device="cuda")
         bl.bitlinear_nonlinear_backward(d, check, scale, "gelu", rows=rows, out=out)
         assert bool((out[n:] == 9).all()) and bool(torch.isfinite(out[:n].float()).all())
+
+
+# 127 / m would pass the largest float: the step of a block is 2^-127 or more
+LEAST = 127 * 2.0 ** -127
+
+
+def floored_check(u):
+    """The checkpoint of rows whose blocks may be tiny: m is LEAST at the least, but in a block of zeros."""
+    M, K = u.shape
+    blocks = torch.nn.functional.pad(u, (0, -K % 128)).view(M, -1, 128)
+    big = blocks.abs().amax(2, keepdim=True)
+    big = torch.where(big > 0, big.clamp_min(LEAST), big)
+    up = torch.where(big > 0, torch.full_like(big, 127.0) / big, 0.0)
+    return (blocks * up).round().view(M, -1)[:, :K].to(torch.int8), (big / torch.full_like(big, 127.0)).squeeze(2)
+
+
+@pytest.mark.parametrize("fn", FUNCTIONS)
+def test_checkpoint_of_tiny_blocks(bl, fn):
+    """Blocks whose largest magnitude is near the smallest floats, zeros among them, alone and beside ordinary blocks:
+    zeros stay zeros, the rest is rounded to the block's step, and the gradient goes through what is positive."""
+    g = torch.Generator().manual_seed(6)
+    u = torch.randn(8, 288, generator=g)
+    u[:, ::3] = 0.0
+    for r, m in enumerate((1e-38, 3e-37, 3.8e-37, 7.4e-37, 7.5e-37, 2.0 ** -126, 1e-41, 5e-45)):
+        u[r, :128] *= m / u[r, :128].abs().max()
+    u[5, 128:] *= 1e-38
+    check, scale = floored_check(u)
+    _, _, _, got, got_scale = bl.bitlinear_quant_nonlinear(u.cuda(), fn, checkpoint=True)
+    assert bool((got.cpu()[u == 0] == 0).all())
+    assert torch.equal(got.cpu(), check) and torch.equal(got_scale.cpu(), scale)
+    du = bl.bitlinear_nonlinear_backward(torch.randn(8, 288, generator=g).cuda(), got, got_scale, fn, dtype=torch.float32)
+    assert bool(torch.isfinite(du).all())
+    if fn == "relu":
+        assert torch.equal(du.cpu() != 0, check > 0)
