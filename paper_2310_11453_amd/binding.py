@@ -19,7 +19,7 @@ GAMMA_PER_TOKEN, GAMMA_PER_TENSOR = 0, 1
 FLAG_SKIP_LN, FLAG_OUT_ACC_I32, FLAG_BETA_CENTERED = 1, 2, 4
 OP_PACK, OP_QUANT, OP_FORWARD, OP_BACKWARD, OP_LN_BACKWARD, OP_FORWARD_NONNEG = 0, 1, 2, 3, 4, 5
 OP_MATMUL, OP_ROUTE, OP_QUANT_NONLINEAR = 6, 7, 8
-FUNCTIONS = {"relu": 0, "relu2": 1, "gelu": 2, "silu": 3}
+FUNCTIONS = {"relu": 0, "relu2": 1, "gelu": 2, "silu": 3, "relu_marked": 8}
 F32, BF16 = 0, 1
 
 EXPORTS = (
@@ -666,7 +666,9 @@ def bitlinear_quant_nonlinear(U: torch.Tensor, fn: str = "gelu", ln_eps: float =
                               checkpoint: bool = False, rows: torch.Tensor | None = None,
                               workspace: torch.Tensor | None = None):
     """Function, LayerNorm and quantiser of U [M, K] in one pass.  Returns (codes, gamma, rowsum, check int8 [M, K],
-    check_scale fp32 [M, ceil(K / 128)]), the last two None without `checkpoint`.  rows: int32 [1], rows that exist."""
+    check_scale fp32 [M, ceil(K / 128)]), the last two None without `checkpoint`.  rows: int32 [1], rows that exist.
+    To train with a rectifier take "relu_marked" in both calls: the checkpoint of "relu" loses the gradient of every positive
+    element that it rounds to zero."""
     lib, dev = load_library(), _here(U)
     M, K = U.shape
     codes = torch.empty((M, K), dtype=torch.int8, device=dev)

@@ -52,6 +52,7 @@ ExpertsArgs experts_args(const int8_t* codes, const float* gamma, int64_t M, int
     return a;
 }
 
+bool function_ok(int fn) { return (fn >= BL_FN_RELU && fn <= BL_FN_SILU) || fn == BL_FN_RELU_MARKED; }
 // a workgroup's threads times the rows stay below 2^32, which is what a launch takes
 bool nonlinear_rows_ok(int64_t M, int64_t K) { return M < ((int64_t)1 << 24) && M * K <= ((int64_t)1 << 36); }
 struct NonlinearWs {
@@ -160,7 +161,7 @@ int bitlinear_quant_nonlinear(const float* U, int64_t M, int64_t K, int fn, floa
                               int granularity, int8_t* codes, float* gamma, int32_t* rowsum, int8_t* check,
                               float* check_scale, void* workspace, size_t workspace_bytes, void* stream) {
     if (M < 0 || M > kMaxDim || K <= 0 || K > kMaxDim || K % 32) return BL_ERR_SHAPE;
-    if (!gran_ok(granularity) || fn < BL_FN_RELU || fn > BL_FN_SILU || K > kMaxNonlinearK) return BL_ERR_UNSUPPORTED;
+    if (!gran_ok(granularity) || !function_ok(fn) || K > kMaxNonlinearK) return BL_ERR_UNSUPPORTED;
     if (M == 0) return BL_OK;
     if (!nonlinear_rows_ok(M, K)) return BL_ERR_UNSUPPORTED;
     if (!U || !codes || !gamma || (check && !check_scale)) return BL_ERR_NULL;
@@ -182,8 +183,7 @@ int bitlinear_nonlinear_backward(const float* dXhat, const int8_t* check, const 
                                  int64_t K, int fn, float ln_eps, const int32_t* rows, int type, void* dU,
                                  void* stream) {
     if (M < 0 || M > kMaxDim || K <= 0 || K > kMaxDim || K % 32) return BL_ERR_SHAPE;
-    if (fn < BL_FN_RELU || fn > BL_FN_SILU || (type != BL_F32 && type != BL_BF16) || K > kMaxNonlinearK)
-        return BL_ERR_UNSUPPORTED;
+    if (!function_ok(fn) || (type != BL_F32 && type != BL_BF16) || K > kMaxNonlinearK) return BL_ERR_UNSUPPORTED;
     if (M == 0) return BL_OK;
     if (!nonlinear_rows_ok(M, K)) return BL_ERR_UNSUPPORTED;
     if (!dXhat || !check || !check_scale || !dU) return BL_ERR_NULL;

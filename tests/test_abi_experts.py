@@ -126,3 +126,17 @@ def test_binding_refuses_what_is_not_on_the_gpu(bl):
                  lambda: bl.bitlinear_nonlinear_backward(x, ids, x), lambda: bl.bitlinear_pack_weights_experts(x)):
         with pytest.raises(bl.BitLinearError):
             call()
+
+
+def test_functions(lib, bl):
+    """Which functions there are, and that any other number is refused before a pointer is looked at."""
+    def fwd(fn):
+        return lib.bitlinear_quant_nonlinear(None, 8, 64, fn, 1e-5, None, 0, ONE, ONE, ONE, ONE, ONE, ONE, BIG, None)
+
+    def bwd(fn):
+        return lib.bitlinear_nonlinear_backward(None, ONE, ONE, 8, 64, fn, 1e-5, None, 1, ONE, None)
+
+    known = set(bl.FUNCTIONS.values())
+    assert known == {0, 1, 2, 3, 8}
+    for fn in range(-2, 20):
+        assert fwd(fn) == bwd(fn) == (-1 if fn in known else -3)

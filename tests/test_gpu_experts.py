@@ -580,6 +580,24 @@ def test_mixture_forward_and_backward(bl, M, top_k, E, d, width, per_tensor):
         assert float((got.double() - ref).norm()) <= 3 * BF16 * float(ref.norm()) + 1e-12
 
 
+@pytest.mark.parametrize("per_tensor", [False, True])
+def test_mixture_with_a_marked_rectifier(bl, per_tensor):
+    """The same network as with the plain rectifier, whose gradient reaches exactly the positive inputs of the function."""
+    X, ids, weights, up, down = mixture(bl, 300, 2, 4, 256, 1056)
+    Y, s = mixture_forward(bl, X, ids, weights, up, down, "relu_marked", per_tensor, True)
+    assert torch.equal(Y, mixture_forward(bl, X, ids, weights, up, down, "relu", per_tensor, True)[0])
+    used = int(s["offsets"][-1])
+    dY = torch.randn(300, 256, device="cuda") * 1e-2
+    dy, _ = bl.bitlinear_combine_backward(dY, s["y"], s["position"], weights)
+    dx2, _ = bl.bitlinear_backward_ste_experts(dy, s["q2"], s["g2"], down[0], down[1], s["offsets"], per_tensor=per_tensor)
+    du = bl.bitlinear_nonlinear_backward(dx2, s["check"], s["scale"], "relu_marked", rows=s["offsets"][4:])
+    assert torch.equal(du[:used] != 0, s["u"][:used] > 0)
+    dX, dW1, dW2, dw = mixture_backward(bl, dY, X, ids, weights, up, down, "relu_marked", per_tensor, s)
+    ref = bl.bitlinear_backward_ste_experts(du, s["codes"], s["gamma"], up[0], up[1], s["offsets"], s["order"], 2, per_tensor)
+    assert torch.equal(dW1, ref[1]) and torch.equal(dX, bl.bitlinear_layernorm_backward(
+        bl.bitlinear_combine(ref[0], s["position"]), X))
+
+
 def test_mixture_in_a_graph_with_other_work_between_replays(bl):
     """Forward and backward captured; replayed with new tokens and new choices, with eager calls and other streams' work
     between the replays; every replay is the eager result, bit for bit."""

@@ -255,3 +255,74 @@ def test_checkpoint_of_tiny_blocks(bl, fn):
     assert bool(torch.isfinite(du).all())
     if fn == "relu":
         assert torch.equal(du.cpu() != 0, check > 0)
+
+
+# ---- a rectifier whose checkpoint keeps what is positive -------------------------------------------------------
+def marked_check(u):
+    """plain_check's, but -128 for what is positive and rounds to 0."""
+    check, scale = floored_check(u)
+    return torch.where((u > 0) & (check == 0), torch.full_like(check, -128), check), scale
+
+
+def make_sparse_u(M, K, seed, kind):
+    u = make_u(M, K, seed, "outliers" if kind == "outliers" else "normal")
+    return u - 2.0 * u.square().mean(1, keepdim=True).sqrt() if kind == "sparse" else u
+
+
+@pytest.mark.parametrize("M,K", [(1, 32), (5, 96), (33, 544), (9, 2080), (300, 2048), (300, 5472), (130, 8192), (2, 28672)])
+@pytest.mark.parametrize("kind", ["normal", "sparse", "outliers"])
+@pytest.mark.parametrize("per_tensor", [False, True])
+def test_marked_rectifier(bl, M, K, kind, per_tensor):
+    """The forward is the rectifier's, bit for bit; the checkpoint and its gradient keep which elements are positive.
+
+    The gradient against the derivative at the checkpoint with the slopes of u: eight fp32 roundings of what its terms'
+    magnitudes add up to.  And against the derivative at u itself: a checkpoint moves an element of h by half a step s of its
+    block at most, so the row's mean by mean(s / 2) and its deviation (a norm) by rms(s / 2); the differences of dU
+    follow without any approximation."""
+    print(f"marked rectifier M={M} K={K} {kind} per_tensor={per_tensor}", flush=True)
+    u = make_sparse_u(M, K, M + K, kind)
+    got = bl.bitlinear_quant_nonlinear(u.cuda(), "relu_marked", per_tensor=per_tensor, checkpoint=True)
+    ref = bl.bitlinear_quant_nonlinear(u.cuda(), "relu", per_tensor=per_tensor)
+    for a, b in zip(got[:3], ref[:3]):
+        assert torch.equal(a, b)
+    bare = bl.bitlinear_quant_nonlinear(u.cuda(), "relu_marked", per_tensor=per_tensor)
+    assert bare[3] is None and torch.equal(bare[0], ref[0])
+    check, scale = marked_check(u)
+    assert torch.equal(got[3].cpu(), check) and torch.equal(got[4].cpu(), scale)
+    d = torch.randn(M, K, generator=torch.Generator().manual_seed(3))
+    du = bl.bitlinear_nonlinear_backward(d.cuda(), got[3], got[4], "relu_marked", dtype=torch.float32).cpu().double()
+    off, d, h = scale.repeat_interleave(128, 1)[:, :K].double() * (0.5 + 64 * F32), d.double(), u.double().clamp_min(0)
+    dev = (h.var(1, correction=0, keepdim=True) + EPS).sqrt()
+    x, m1 = normal(h), d.mean(1, keepdim=True)
+    m2 = (d * x).mean(1, keepdim=True)
+    core = d - m1 - x * m2
+    dev_off = off.square().mean(1, keepdim=True).sqrt()
+    least = (dev - dev_off).clamp_min(EPS ** 0.5)
+    x_off = (off + off.mean(1, keepdim=True) + x.abs() * dev_off) / least
+    m2_off = (d.abs() * x_off).mean(1, keepdim=True)
+    allowed = dev_off / (dev * least) * core.abs() + (x_off * (m2.abs() + m2_off) + x.abs() * m2_off) / least
+    allowed = allowed + 8 * F32 / least * (d.abs() + m1.abs() + (x.abs() + x_off) * (m2.abs() + m2_off))
+    slope = (u > 0).double()
+    assert bool(((du - slope * core / dev).abs() <= slope * allowed).all())
+    v = (check.float() * scale.repeat_interleave(128, 1)[:, :K]).double().clamp_min(0)
+    x, dev = normal(v), (v.var(1, correction=0, keepdim=True) + EPS).sqrt()
+    m2 = (d * x).mean(1, keepdim=True)
+    most = d.abs() + m1.abs() + (x * m2).abs()
+    assert bool(((du - slope * (d - m1 - x * m2) / dev).abs() <= slope * 8 * F32 * most / dev).all())
+    half = bl.bitlinear_nonlinear_backward(d.float().cuda(), got[3], got[4], "relu_marked")
+    assert torch.equal(half.cpu(), du.float().to(torch.bfloat16))
+
+
+def test_marked_rectifier_of_tiny_and_no_values(bl):
+    """What is positive keeps its slope however small, zeros and what is below have none."""
+    u = torch.zeros(4, 160)
+    u[0, ::2] = 1e-41
+    u[1, ::2], u[1, 1::4] = 1e-30, -1e-30
+    u[2, 3], u[2, 4] = 1.0, 1e-38
+    u[2, 130:] = -1e-9
+    check, scale = marked_check(u)
+    _, _, _, got, got_scale = bl.bitlinear_quant_nonlinear(u.cuda(), "relu_marked", checkpoint=True)
+    assert torch.equal(got.cpu(), check) and torch.equal(got_scale.cpu(), scale)
+    d = torch.randn(4, 160, generator=torch.Generator().manual_seed(1)).cuda()
+    du = bl.bitlinear_nonlinear_backward(d, got, got_scale, "relu_marked", dtype=torch.float32)
+    assert torch.equal(du.cpu() != 0, u > 0)
