@@ -673,6 +673,8 @@ def bitlinear_quant_nonlinear(U: torch.Tensor, fn: str = "gelu", ln_eps: float =
     M, K = U.shape
     codes = torch.empty((M, K), dtype=torch.int8, device=dev)
     gamma = torch.empty(1 if per_tensor else M, dtype=torch.float32, device=dev)
+    if M == 0:
+        gamma.fill_(1e-5)  # the call leaves it alone
     rowsum = torch.empty(M, dtype=torch.int32, device=dev)
     check = torch.empty((M, K), dtype=torch.int8, device=dev) if checkpoint else None
     scale = torch.empty((M, (K + 127) // 128), dtype=torch.float32, device=dev) if checkpoint else None

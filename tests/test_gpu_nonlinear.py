@@ -326,3 +326,12 @@ def test_marked_rectifier_of_tiny_and_no_values(bl):
     d = torch.randn(4, 160, generator=torch.Generator().manual_seed(1)).cuda()
     du = bl.bitlinear_nonlinear_backward(d, got, got_scale, "relu_marked", dtype=torch.float32)
     assert torch.equal(du.cpu() != 0, u > 0)
+
+
+def test_no_rows_leave_the_lower_bound_of_gamma(bl):
+    """No rows at all, as with a `rows` of 0: a gamma per tensor is its lower bound, whatever memory it got."""
+    for fn in FUNCTIONS:
+        dirt = [torch.full((1,), 7.0, device="cuda") for _ in range(64)]
+        del dirt  # one of these blocks is the next call's
+        _, gamma, _, _, _ = bl.bitlinear_quant_nonlinear(torch.empty(0, 64, device="cuda"), fn, per_tensor=True)
+        assert gamma.tolist() == [torch.tensor(1e-5).item()]
