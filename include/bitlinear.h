@@ -325,6 +325,8 @@ int bitlinear_layernorm_backward(const float* dXhat, const float* X, int64_t M, 
  *   slots) -> bitlinear_layernorm_backward.
  * Where an expert's slots begin stays in device memory (`offsets`): nothing waits for the router.
  * Slots behind offsets[experts] (choices that name no expert) are neither read nor written.
+ * Without tokens (M == 0) nothing is written here either, as in every other call: not offsets, not dW, not a gamma per
+ * tensor, which a caller of such a batch sets (the PyTorch binding does: to zeros, zeros and gamma's lower bound).
  * Limits: experts 1..256, top_k 1..64, M * top_k <= 2^30 (else BL_ERR_SHAPE); bitlinear_route takes up to
  * 2^24 choices, the products K <= 65536, bitlinear_quant_nonlinear and its backward M < 2^24 rows and M * K <=
  * 2^36 (else BL_ERR_UNSUPPORTED, which is also the answer to operands that are read several elements at a time
@@ -364,7 +366,7 @@ int bitlinear_matmul_experts(const int8_t* codes, const float* gamma, const int3
 /* Section 2.2 for such a product (Sign, Clip and rounding are identity, alpha, beta, gamma constants):
  *   dX[s,k]   = beta_e sum_n dY[s,n] W~_e[n,k]                    fp32 [T,K], or NULL
  *   dW[e,n,k] = sum_{s of e} dY[s,n] codes[r,k] gamma_r / 128      fp32 [experts,N,K], or NULL;
- *               zeros for an expert without slots
+ *               zeros for an expert without slots (of a batch with tokens, see above)
  *   dY   in  bf16 [T,N] as bitlinear_combine_backward and bitlinear_nonlinear_backward write it
  * With a gamma per tensor both products are exact but for their fp32 sums; with one per token gamma_r / 128
  * is folded into row s of dY, which is then rounded to bf16 a second time. */
@@ -393,7 +395,7 @@ int bitlinear_combine_backward(const float* dY, const float* slots, const int32_
  *   U            in   fp32 [M,K], K <= 32768 (else BL_ERR_UNSUPPORTED)
  *   fn                a bl_fn
  *   rows         in   int32 [1] (device) or NULL: only rows below it are read and written (of a routed batch:
- *                     offsets + experts); without any a gamma per tensor is its lower bound
+ *                     offsets + experts); where there are none a gamma per tensor is its lower bound
  *   check        out  int8 [M,K] or NULL: rne(u * (127 / m)), m the largest magnitude of each 128
  *                     consecutive elements of a row (the last ones of a row may be fewer), or 127 * 2^-127 where
  *                     it is smaller; zeros where all of them are zero.
