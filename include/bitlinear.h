@@ -453,8 +453,9 @@ int bitlinear_probe_read(const void* src, size_t bytes, int workgroups, int thre
  *   bwd_splits=n        backward ring kernels: slices of the reduction (tiles of 256 columns)
  *   experts_tile=1|2|3|4|5  products of experts: 128 x 256, 256 x 256, 128 x 128 or 64 x 128 output tiles, or a
  *                       few rows at a time
- *   (decode_tiles, 1, 2, 4 or 8: also the weight tiles of a workgroup of that last kernel; bwd_ring, bwd_grid,
- *   bwd_splits and quant_wpr act on the operators of experts as on the plain ones)
+ *   (decode_tiles, 1, 2, 4 or 8: also the weight tiles of a workgroup of that last kernel.  bwd_ring, bwd_grid,
+ *   bwd_splits and quant_wpr also act on the operators of experts: bwd_splits on dW in 128 x 128 tiles, and on dX
+ *   from four slices on; quant_wpr with 1, 4 or 8; bwd_dx does not, their dX has tiles of 128 x 256 only)
  * Returns BL_OK, or BL_ERR_UNSUPPORTED (unknown name or bad syntax; nothing changes). */
 int bitlinear_set_tuning(const char* spec);
 

@@ -360,7 +360,7 @@ static RowShape row_shape(int64_t M, int64_t K) {
     // 4.4 / 6.6, 3.0 / 3.1, 3.4 / 3.5; 16384 x 8192 with 4, 8, 16 126 / 219, 144 / 216, 194 / 297)
     while (wpr < 8 && M * wpr <= 1024 && K4 > (int64_t)wpr * kWave * 2) wider();
     if (const int v = tuning().quant_wpr)
-        if ((v == 1 || v == 4 || v == 8 || v == 16) && K4 <= (int64_t)v * kWave * 8) wpr = v;
+        if ((v == 1 || v == 4 || v == 8) && K4 <= (int64_t)v * kWave * 8) wpr = v;
     while ((int64_t)wpr * kWave * nv < K4) nv *= 2;
     return {wpr, nv};
 }
@@ -393,9 +393,10 @@ static hipError_t launch_fn(const NonlinearArgs& a_in, bool backward, hipStream_
     if (q.wpr == W && q.nv == V) {                           \
         if (backward) launch_backward_rows<FN, W, V>(a, s);  \
         else launch_forward<FN, W, V>(a, s);                 \
-    }
+    } else
     BL_ROWS(1, 2) BL_ROWS(1, 4) BL_ROWS(1, 8) BL_ROWS(4, 2) BL_ROWS(4, 4) BL_ROWS(4, 8) BL_ROWS(8, 2) BL_ROWS(8, 4)
-    BL_ROWS(8, 8) BL_ROWS(16, 2) BL_ROWS(16, 4) BL_ROWS(16, 8)
+    BL_ROWS(8, 8) BL_ROWS(16, 8)  // (16 waves: more than 8 hold)
+    return hipErrorInvalidValue;
 #undef BL_ROWS
     return hipGetLastError();
 }

@@ -223,6 +223,19 @@ def test_rows_behind_the_last_are_left_alone(bl, per_tensor):
         assert bool((out[n:] == 9).all()) and bool(torch.isfinite(out[:n].float()).all())
 
 
+# every pair of waves a row and float4 a lane: batches of rows that fill the chip, whole and ragged, and the numbers of waves
+# that the library would not pick there
+@pytest.mark.parametrize("M,K,waves", [(300, 4096, 0), (300, 3104, 0), (300, 8192, 0), (300, 5472, 0), (5, 512, 4), (5, 544, 8),
+                                       (5, 2048, 1), (5, 2080, 8), (5, 4096, 4), (5, 8192, 4), (5, 12320, 8), (300, 2048, 8)])
+@pytest.mark.parametrize("fn", FUNCTIONS)
+def test_every_shape_of_a_row(bl, tuning, M, K, waves, fn):
+    tuning(f"quant_wpr={waves}")
+    for per_tensor in (False, True):
+        test_forward_and_checkpoint(bl, M, K, fn, per_tensor)
+    for dtype in (torch.float32, torch.bfloat16):
+        test_backward(bl, M, K, fn, dtype)
+
+
 # 127 / m would pass the largest float: the step of a block is 2^-127 or more
 LEAST = 127 * 2.0 ** -127
 
