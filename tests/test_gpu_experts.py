@@ -149,6 +149,18 @@ def test_products_of_256_experts(bl, tuning, tile):
         check_products(bl, M, 2, 256, 96, 144, True, False, choices(M, 2, 256, M, 0.1, only=only))
 
 
+# A few rows at a time: one to eight weight tiles a workgroup, the last of them beyond N, and K of more chunks of 512 than a
+# workgroup has waves.
+@pytest.mark.parametrize("M,top_k,E,K,N", [(1, 2, 8, 2048, 520), (33, 4, 100, 160, 48), (48, 2, 6, 4640, 300), (130, 2, 4, 1056, 257),
+                                           (20, 1, 3, 8224, 136)])
+@pytest.mark.parametrize("gather,per_tensor", [(True, False), (False, True)])
+@pytest.mark.parametrize("tiles", [1, 2, 4, 8])
+def test_products_a_few_rows_at_a_time(bl, tuning, M, top_k, E, K, N, gather, per_tensor, tiles):
+    print(f"products M={M} top_k={top_k} E={E} K={K} N={N} gather={gather} per_tensor={per_tensor} tiles={tiles}", flush=True)
+    tuning(f"experts_tile=5,decode_tiles={tiles}")
+    check_products(bl, M, top_k, E, K, N, gather, per_tensor, choices(M, top_k, E, M + K, unrouted=0.1))
+
+
 def test_products_of_more_than_4_gib_of_codes(bl):
     """Offsets into the codes pass 32 bits.  Checked on slots from both ends and around the border."""
     T, K, N = 65540, 65536, 40
