@@ -286,6 +286,26 @@ def test_backward_dw_from_dy(bl, tuning, M, N, K, spec):
         assert torch.equal(got, ref)
 
 
+# 64 tiles of dW an expert and more, which the XCDs share: numbers of them that eight does not divide, in both tiles, from dY
+# itself and from a scaled copy, whole rounds of workgroups and a few workgroups.  On integers, so exact.
+@pytest.mark.parametrize("N,K", [(2336, 1184), (2304, 1056), (2056, 1184)])
+@pytest.mark.parametrize("per_tensor", [True, False])
+@pytest.mark.parametrize("spec", ["bwd_ring=1", "bwd_ring=2", "bwd_ring=1,bwd_grid=16", "bwd_ring=2,bwd_grid=24"])
+def test_backward_dw_of_many_tiles(bl, tuning, N, K, per_tensor, spec):
+    print(f"backward dW of many tiles N={N} K={K} per_tensor={per_tensor} {spec}", flush=True)
+    tuning(spec)
+    M, top_k, E = 300, 2, 6
+    c = make(bl, M, top_k, E, K, N, True, per_tensor, choices(M, top_k, E, N, unrouted=0.1))
+    dY = torch.randint(-4, 5, (c["T"], N), generator=torch.Generator().manual_seed(1)).to(torch.bfloat16)
+    dY[c["offsets"][-1]:] = float("nan")
+    _, dw = bl.bitlinear_backward_ste_experts(dY.cuda(), c["codes"].cuda(), torch.full_like(c["gamma"], 128.0).cuda(), None,
+                                              None, **c["calls"], want_dx=False)
+    for e in range(E):
+        mine = slice(c["offsets"][e], c["offsets"][e + 1])
+        # in fp32: sums of a few hundred products of at most 512 are exact
+        assert torch.equal(dw[e].cpu(), dY[mine].float().T @ c["codes"].float()[c["row"][mine]])
+
+
 # dX in whole rounds of workgroups and a last one whose tiles are cut into slices: the number of slots moves the last round
 # through nothing, a tile and more tiles than leave room for slices.  On integers, so exact.
 @pytest.mark.parametrize("M", [1, 129, 500, 1000, 1040, 1100, 1500, 1900, 2048])
