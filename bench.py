@@ -288,13 +288,15 @@ def experts_leg(bl, torch, dev):
     ok, shapes = True, []
     for M in (1, 16, 64):
         X, ids, weights = batch(M)
-        _, (order, _, offsets, q1, g1, r1, u, *_) = forward(X, ids, weights, up[0], down[0], False, False)
+        _, (order, _, offsets, q1, g1, r1, u, q2, g2, _, _, y) = forward(X, ids, weights, up[0], down[0], False, False)
         for e, (a, b) in enumerate(zip(offsets.tolist(), offsets.tolist()[1:])):
             if a < b:
                 rows = (order[a:b] // top_k).long()
                 ref = bl.bitlinear_matmul(q1[rows].contiguous(), g1[rows].contiguous(), r1[rows].contiguous(),
                                           up[0][e], width, up[2][e:e + 1].contiguous())
-                ok = ok and torch.equal(u[a:b], ref)
+                back = bl.bitlinear_matmul(q2[a:b].contiguous(), g2[a:b].contiguous(), q2[a:b].sum(1, dtype=torch.int32),
+                                           down[0][e], d, down[2][e:e + 1].contiguous())
+                ok = ok and torch.equal(u[a:b], ref) and torch.equal(y[a:b], back)
         t, mode = graph_ms(lambda i: forward(X, ids, weights, ups[i % ncopy], downs[i % ncopy], False, False),
                            2 * ncopy, 5, torch)
         used = int((offsets[1:] > offsets[:-1]).sum())  # experts that anybody chose
