@@ -369,7 +369,8 @@ int bitlinear_matmul_experts(const int8_t* codes, const float* gamma, const int3
  *               zeros for an expert without slots (of a batch with tokens, see above)
  *   dY   in  bf16 [T,N] as bitlinear_combine_backward and bitlinear_nonlinear_backward write it
  * With a gamma per tensor both products are exact but for their fp32 sums; with one per token gamma_r / 128
- * is folded into row s of dY, which is then rounded to bf16 a second time. */
+ * is folded into row s of dY, which is then rounded to bf16 a second time.  An infinity in dY may leave NaN instead of
+ * infinities in its expert's dW. */
 int bitlinear_backward_ste_experts(const void* dY, int64_t M, int top_k, int64_t N, int64_t K,
                                    const int8_t* codes, const float* gamma, int granularity,
                                    const int32_t* order, const int32_t* offsets, int experts,
@@ -413,7 +414,8 @@ int bitlinear_quant_nonlinear(const float* U, int64_t M, int64_t K, int fn, floa
  * u itself the checkpoint costs 0.4 to 0.7 % of dU's norm for u of N(0,1) and 1.3 to 5.3 % for sparse ones and outliers
  * (BL_FN_RELU2, BL_FN_GELU, BL_FN_SILU), but 9 to 26 % for BL_FN_RELU, which loses the gradient of every small positive
  * u: train with BL_FN_RELU_MARKED (0.02 to 0.3 %).  dU: [M,K] of `type` (BL_BF16: as bitlinear_backward_ste_experts reads
- * it, rounded once; BL_F32: as bitlinear_backward_ste reads it); 16-byte aligned, not on dXhat.  rows as above. */
+ * it, rounded once; BL_F32: as bitlinear_backward_ste reads it); 16-byte aligned, not on dXhat.  rows as above.  GELU's f
+ * and f' are off by at most 3e-7 (1 + |v|) here. */
 int bitlinear_nonlinear_backward(const float* dXhat, const int8_t* check, const float* check_scale,
                                  int64_t M, int64_t K, int fn, float ln_eps, const int32_t* rows,
                                  int type, void* dU, void* stream);
