@@ -66,14 +66,15 @@ enum {
 /* Operation selector for bitlinear_workspace_bytes. */
 typedef enum { BL_OP_PACK = 0, BL_OP_QUANT = 1, BL_OP_FORWARD = 2, BL_OP_BACKWARD = 3,
                BL_OP_LN_BACKWARD = 4, BL_OP_FORWARD_NONNEG = 5, BL_OP_MATMUL = 6, BL_OP_ROUTE = 7,
-               BL_OP_QUANT_NONLINEAR = 8 } bl_op;
+               BL_OP_QUANT_NONLINEAR = 8, BL_OP_QUANT_RMSNORM = 9, BL_OP_RMSNORM_BACKWARD = 10,
+               BL_OP_MATMUL_I8 = 11, BL_OP_BACKWARD_I8 = 12 } bl_op;
 
 /* Non-linear functions of bitlinear_quant_nonlinear: max(u, 0), max(u, 0)^2, u Phi(u), u / (1 + e^-u).
  * BL_FN_RELU_MARKED is max(u, 0) whose checkpoint tells what is positive from what is not, for training. */
 typedef enum { BL_FN_RELU = 0, BL_FN_RELU2 = 1, BL_FN_GELU = 2, BL_FN_SILU = 3, BL_FN_RELU_MARKED = 8 } bl_fn;
 
 /* Element types where a call offers a choice. */
-typedef enum { BL_F32 = 0, BL_BF16 = 1 } bl_type;
+typedef enum { BL_F32 = 0, BL_BF16 = 1, BL_I8 = 2 } bl_type;
 
 /* host: size in bytes of the packed-weight blob for an [N,K] matrix (0 on bad
  * shape).  The blob is the library's own tiled 1-bit layout (1 bit per weight,
@@ -419,6 +420,81 @@ int bitlinear_quant_nonlinear(const float* U, int64_t M, int64_t K, int fn, floa
 int bitlinear_nonlinear_backward(const float* dXhat, const int8_t* check, const float* check_scale,
                                  int64_t M, int64_t K, int fn, float ln_eps, const int32_t* rows,
                                  int type, void* dU, void* stream);
+
+/* ---- The 8-bit linear layer and what stands around it --------------------------------------------
+ * Layers that are not binarised (the paper holds its input and output embeddings in 8 bits) take the same 8-bit
+ * activations and int8 weights with a scale for each output channel:
+ *   bitlinear_quant_rmsnorm (or bitlinear_quant_act) -> bitlinear_matmul_i8
+ * and their backward
+ *   bitlinear_backward_ste_i8 -> bitlinear_rmsnorm_backward.
+ * The codes, gamma and row sums of bitlinear_quant_rmsnorm are those of bitlinear_quant_act with another norm: the
+ * 1-bit products (bitlinear_matmul, bitlinear_matmul_experts) take them too.
+ * Shapes as above: K % 32 == 0, M, N, K <= 2^30, M * K and N * K <= 2^40, K <= 65536 for the product and its backward
+ * (else BL_ERR_UNSUPPORTED).  Operands that are read or written several elements at a time have to be 16-byte aligned
+ * (BL_ERR_UNSUPPORTED): X, residual, H, gain, codes, xhat_dump, dXhat, dresidual, dH, W, packed, out, dY, dX.
+ * bitlinear_workspace_bytes(op, M, N, K, granularity, 0) with BL_OP_QUANT_RMSNORM (per tensor; 0 per token),
+ * BL_OP_RMSNORM_BACKWARD (needed with dgain only), BL_OP_MATMUL_I8 (optional, 0 for most shapes) and
+ * BL_OP_BACKWARD_I8 (part of it optional); N is of no account for the first two. */
+
+/* The residual's addition, root-mean-square norm and Eq. 4-5's quantiser in one pass:
+ *   h = x + r, rounded to the type of the residual,   x^ = h / sqrt(mean(h^2) + eps) * gain
+ * and gamma, codes of x^ as in bitlinear_quant_act.
+ *   X          in   [M,K] of x_type (BL_F32, BL_BF16)
+ *   residual   in   [M,K] of h_type or NULL: h = x, and H has to be NULL
+ *   gain       in   fp32 [K] or NULL (ones)
+ *   eps             >= 0 and finite (else BL_ERR_UNSUPPORTED); a row of zeros has x^ = 0 with any
+ *   H          out  h, [M,K] of h_type, or NULL; may be the same buffer as X or residual where the type is the same
+ *   codes, gamma, rowsum (or NULL), xhat_dump (or NULL)   as in bitlinear_quant_act */
+int bitlinear_quant_rmsnorm(const void* X, int x_type, const void* residual, int h_type, int64_t M, int64_t K,
+                            const float* gain, float eps, int granularity, void* H, int8_t* codes, float* gamma,
+                            int32_t* rowsum, float* xhat_dump, void* workspace, size_t workspace_bytes,
+                            void* stream);
+
+/* Its backward (straight-through: the quantiser is identity).  With n = h / rms, t = dXhat * gain:
+ *   dH = (t - n * mean(t * n)) / rms + dresidual,   dgain[k] = sum_m dXhat[m,k] * n[m,k]
+ * dH is the gradient of x and of r alike.
+ *   dXhat      in   [M,K] of g_type (what bitlinear_backward_ste or bitlinear_backward_ste_i8 writes as dX)
+ *   H          in   [M,K] of h_type, what the forward call wrote (or X without a residual); gain, eps as there
+ *   dresidual  in   [M,K] of d_type or NULL: the gradient that reaches h past the norm
+ *   dH         out  [M,K] of d_type; may be the same buffer as dresidual, dXhat or H where the type is the same
+ *   dgain      out  fp32 [K] or NULL (sums in fp64, in a fixed order) */
+int bitlinear_rmsnorm_backward(const void* dXhat, int g_type, const void* H, int h_type, const void* dresidual,
+                               int d_type, int64_t M, int64_t K, const float* gain, float eps, void* dH,
+                               float* dgain, void* workspace, size_t workspace_bytes, void* stream);
+
+/* host: bytes of the packed int8 weights (tiles of 16 x 64 codes, N padded to 16 and K to 64; 0 on a bad shape). */
+size_t bitlinear_packed_bytes_i8(int64_t N, int64_t K);
+
+/* 8-bit weights with a scale for each output channel: m = max_k |W[n,k]|, scale[n] = m / 127, codes
+ * clamp(rne(W[n,k] * (127 / m)), -127, 127).  (m is taken to be at least 127 * 2^-127 in a row that is not all zeros, so
+ * that 127 / m is a number; a row of zeros has scale 0.)
+ *   W       in   [N,K] of w_type: BL_F32, BL_BF16, or BL_I8: these are the codes (any int8), `scale` is left alone (or NULL)
+ *   packed  out  bitlinear_packed_bytes_i8(N, K) bytes;   scale  out  fp32 [N] */
+int bitlinear_pack_weights_i8(const void* W, int w_type, int64_t N, int64_t K, void* packed, float* scale,
+                              void* stream);
+/* Back: [N,K] of `type`, the codes (BL_I8; scale may be NULL) or the values codes * scale that they stand for. */
+int bitlinear_unpack_weights_i8(const void* packed, const float* scale, int64_t N, int64_t K, int type, void* out,
+                                void* stream);
+
+/* Y[m,n] = (sum_k codes[m,k] * w[n,k]) * (scale[n] * (gamma_m / 128)).
+ *   codes int8 [M,K], gamma fp32 [M] (or [1]) as the quantisers write them; packed, scale as above
+ *   Y   out  [M,N] of y_type (BL_F32, BL_BF16), or the int32 sums with BL_FLAG_OUT_ACC_I32 (y_type BL_F32; gamma and
+ *            scale may be NULL then)
+ *   workspace   optional: with it a long K may be split over workgroups; same result bit for bit */
+int bitlinear_matmul_i8(const int8_t* codes, const float* gamma, int64_t M, int64_t K, const void* packed,
+                        int64_t N, const float* scale, int granularity, unsigned flags, int y_type, void* Y,
+                        void* workspace, size_t workspace_bytes, void* stream);
+
+/* Straight-through backward of that product (rounding is identity, gamma and scale are constants):
+ *   dX[m,k] = sum_n (dY[m,n] * scale[n]) w[n,k]    [M,K] of dx_type, or NULL
+ *   dW[n,k] = sum_m dY[m,n] (codes[m,k] * gamma_m / 128)    fp32 [N,K], or NULL
+ *   dY   in  [M,N] of dy_type
+ * bf16 operands, fp32 sums: dY * scale is rounded to bf16 for dX; for dW dY is (a bf16 dY is exact), or with a gamma per
+ * token dY * gamma_m / 128.  The codes are exact. */
+int bitlinear_backward_ste_i8(const void* dY, int dy_type, int64_t M, int64_t N, int64_t K, const int8_t* codes,
+                              const float* gamma, int granularity, const void* packed, const float* scale,
+                              void* dX, int dx_type, float* dW, void* workspace, size_t workspace_bytes,
+                              void* stream);
 
 /* Measurement aid, no part of the layer: one launch that only reads `bytes` (a multiple of 16)
  * of device memory at `src` with the access pattern of the small-batch GEMM's weight stream

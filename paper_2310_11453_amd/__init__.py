@@ -17,4 +17,7 @@ from .binding import (  # noqa: F401
     bitlinear_backward_ste_experts, bitlinear_combine, bitlinear_combine_backward, bitlinear_matmul_experts,
     bitlinear_nonlinear_backward, bitlinear_pack_weights_experts, bitlinear_quant_nonlinear, bitlinear_route,
     workspace_bytes_experts,
+    I8, OP_BACKWARD_I8, OP_MATMUL_I8, OP_QUANT_RMSNORM, OP_RMSNORM_BACKWARD,
+    bitlinear_backward_ste_i8, bitlinear_matmul_i8, bitlinear_pack_weights_i8, bitlinear_quant_rmsnorm,
+    bitlinear_rmsnorm_backward, bitlinear_unpack_weights_i8, packed_bytes_i8,
 )

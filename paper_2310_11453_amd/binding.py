@@ -19,8 +19,10 @@ GAMMA_PER_TOKEN, GAMMA_PER_TENSOR = 0, 1
 FLAG_SKIP_LN, FLAG_OUT_ACC_I32, FLAG_BETA_CENTERED = 1, 2, 4
 OP_PACK, OP_QUANT, OP_FORWARD, OP_BACKWARD, OP_LN_BACKWARD, OP_FORWARD_NONNEG = 0, 1, 2, 3, 4, 5
 OP_MATMUL, OP_ROUTE, OP_QUANT_NONLINEAR = 6, 7, 8
+OP_QUANT_RMSNORM, OP_RMSNORM_BACKWARD, OP_MATMUL_I8, OP_BACKWARD_I8 = 9, 10, 11, 12
 FUNCTIONS = {"relu": 0, "relu2": 1, "gelu": 2, "silu": 3, "relu_marked": 8}
-F32, BF16 = 0, 1
+F32, BF16, I8 = 0, 1, 2
+_TYPES = {torch.float32: F32, torch.bfloat16: BF16, torch.int8: I8}
 
 EXPORTS = (
     "bitlinear_packed_bytes", "bitlinear_workspace_bytes", "bitlinear_pack_weights",
@@ -36,6 +38,8 @@ EXPORTS = (
     "bitlinear_workspace_bytes_experts", "bitlinear_route", "bitlinear_matmul_experts",
     "bitlinear_backward_ste_experts", "bitlinear_combine", "bitlinear_combine_backward",
     "bitlinear_quant_nonlinear", "bitlinear_nonlinear_backward",
+    "bitlinear_quant_rmsnorm", "bitlinear_rmsnorm_backward", "bitlinear_packed_bytes_i8", "bitlinear_pack_weights_i8",
+    "bitlinear_unpack_weights_i8", "bitlinear_matmul_i8", "bitlinear_backward_ste_i8",
 )
 
 _lib = None
@@ -124,6 +128,20 @@ def load_library() -> ctypes.CDLL:
     lib.bitlinear_quant_nonlinear.argtypes = [vp, i64, i64, ci, cf, vp, ci, vp, vp, vp, vp, vp, vp, sz, vp]
     lib.bitlinear_nonlinear_backward.restype = ci
     lib.bitlinear_nonlinear_backward.argtypes = [vp, vp, vp, i64, i64, ci, cf, vp, ci, vp, vp]
+    lib.bitlinear_quant_rmsnorm.restype = ci
+    lib.bitlinear_quant_rmsnorm.argtypes = [vp, ci, vp, ci, i64, i64, vp, cf, ci, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.bitlinear_rmsnorm_backward.restype = ci
+    lib.bitlinear_rmsnorm_backward.argtypes = [vp, ci, vp, ci, vp, ci, i64, i64, vp, cf, vp, vp, vp, sz, vp]
+    lib.bitlinear_packed_bytes_i8.restype = sz
+    lib.bitlinear_packed_bytes_i8.argtypes = [i64, i64]
+    lib.bitlinear_pack_weights_i8.restype = ci
+    lib.bitlinear_pack_weights_i8.argtypes = [vp, ci, i64, i64, vp, vp, vp]
+    lib.bitlinear_unpack_weights_i8.restype = ci
+    lib.bitlinear_unpack_weights_i8.argtypes = [vp, vp, i64, i64, ci, vp, vp]
+    lib.bitlinear_matmul_i8.restype = ci
+    lib.bitlinear_matmul_i8.argtypes = [vp, vp, i64, i64, vp, i64, vp, ci, u32, ci, vp, vp, sz, vp]
+    lib.bitlinear_backward_ste_i8.restype = ci
+    lib.bitlinear_backward_ste_i8.argtypes = [vp, ci, i64, i64, i64, vp, vp, ci, vp, vp, vp, ci, vp, vp, sz, vp]
     lib.bitlinear_probe_read.restype = ci
     lib.bitlinear_probe_read.argtypes = [vp, sz, ci, ci, vp, vp]
     lib.bitlinear_forward_workspace_layout.restype = ci
@@ -705,3 +723,152 @@ def bitlinear_nonlinear_backward(dXhat: torch.Tensor, check: torch.Tensor, check
         None if rows is None else _given(dev, rows, torch.int32, 1), BF16 if dtype == torch.bfloat16 else F32,
         _given(dev, out, dtype, M, K), _queue(dev)), "bitlinear_nonlinear_backward")
     return out
+
+
+# ---- The 8-bit linear layer and what stands around it -----------------------------------------
+def _float_type(dtype: torch.dtype) -> int:
+    if dtype is torch.float32:
+        return F32
+    if dtype is torch.bfloat16:
+        return BF16
+    raise BitLinearError(f"expected torch.bfloat16 or torch.float32, got {dtype}")
+
+
+def packed_bytes_i8(N: int, K: int) -> int:
+    return int(load_library().bitlinear_packed_bytes_i8(N, K))
+
+
+def _blob_bytes_i8(N: int, K: int) -> int:
+    """packed_bytes_i8(N, K) of a shape that the call itself checks."""
+    return (N + 15) // 16 * ((K + 63) // 64) * 1024
+
+
+def bitlinear_quant_rmsnorm(X: torch.Tensor, residual: torch.Tensor | None = None, gain: torch.Tensor | None = None,
+                            eps: float = 1e-5, per_tensor: bool = False, want_xhat: bool = False,
+                            out: torch.Tensor | None = None, workspace: torch.Tensor | None = None):
+    """h = X + residual, root-mean-square norm and Eq. 4-5.  X and residual fp32 or bf16, h of the residual's type; `out`
+    may be X or residual.  Returns (codes int8 [M, K], gamma, rowsum int32 [M], h, xhat or None); h is X itself without a
+    residual."""
+    lib, dev = load_library(), _here(X)
+    M, K = X.shape
+    x_type = _float_type(X.dtype)
+    codes = torch.empty((M, K), dtype=torch.int8, device=dev)
+    gamma = torch.empty(1 if per_tensor else M, dtype=torch.float32, device=dev)
+    if M == 0:
+        gamma.fill_(1e-5)  # the call leaves it alone
+    rowsum = torch.empty(M, dtype=torch.int32, device=dev)
+    xhat = torch.empty((M, K), dtype=torch.float32, device=dev) if want_xhat else None
+    h, h_type, res, h_ptr = X, x_type, None, None
+    if residual is not None:
+        h_type, res = _float_type(residual.dtype), _given(dev, residual, residual.dtype, M, K)
+        h = torch.empty((M, K), dtype=residual.dtype, device=dev) if out is None else out
+        h_ptr = _given(dev, h, residual.dtype, M, K)
+    elif out is not None:
+        raise BitLinearError("out without a residual: h is X")
+    ws, ws_bytes, _keep = _scratch(workspace_bytes(OP_QUANT_RMSNORM, M, 1, K, True) if per_tensor else 0, workspace, dev)
+    _check(lib.bitlinear_quant_rmsnorm(
+        _ptr(X), x_type, res, h_type, M, K, None if gain is None else _given(dev, gain, torch.float32, K), eps,
+        _gran(per_tensor), h_ptr, codes.data_ptr(), gamma.data_ptr(), rowsum.data_ptr(), _ptr(xhat), ws, ws_bytes,
+        _queue(dev)), "bitlinear_quant_rmsnorm")
+    return codes, gamma, rowsum, h, xhat
+
+
+def bitlinear_rmsnorm_backward(dXhat: torch.Tensor, H: torch.Tensor, gain: torch.Tensor | None = None, eps: float = 1e-5,
+                               dresidual: torch.Tensor | None = None, want_dgain: bool = False,
+                               dtype: torch.dtype | None = None, out: torch.Tensor | None = None,
+                               workspace: torch.Tensor | None = None):
+    """From the gradient of the normalised input to that of h (of X and the residual alike), with `dresidual`, the
+    gradient that reaches h past the norm, added.  Of `dtype` (default: dresidual's type, or dXhat's).  Returns dH, or
+    (dH, dgain) with want_dgain."""
+    lib, dev = load_library(), _here(dXhat)
+    M, K = dXhat.shape
+    if dtype is None:
+        dtype = dXhat.dtype if dresidual is None else dresidual.dtype
+    d_type = _float_type(dtype)
+    if out is None:
+        out = torch.empty((M, K), dtype=dtype, device=dev)
+    dgain = (torch.empty if M else torch.zeros)(K, dtype=torch.float32, device=dev) if want_dgain else None
+    need = workspace_bytes(OP_RMSNORM_BACKWARD, M, 1, K) if want_dgain else 0
+    ws, ws_bytes, _keep = _scratch(need, workspace, dev)
+    _check(lib.bitlinear_rmsnorm_backward(
+        _ptr(dXhat), _float_type(dXhat.dtype), _given(dev, H, H.dtype, M, K), _float_type(H.dtype),
+        None if dresidual is None else _given(dev, dresidual, dtype, M, K), d_type, M, K,
+        None if gain is None else _given(dev, gain, torch.float32, K), eps, _given(dev, out, dtype, M, K), _ptr(dgain), ws,
+        ws_bytes, _queue(dev)), "bitlinear_rmsnorm_backward")
+    return (out, dgain) if want_dgain else out
+
+
+def bitlinear_pack_weights_i8(W: torch.Tensor):
+    """8-bit weights with a scale for each row of W [N, K] (fp32 or bf16), or codes (int8) as they are.  Returns (packed
+    uint8 blob, scale [N], None for codes)."""
+    lib, dev = load_library(), _here(W)
+    N, K = W.shape
+    if W.dtype not in _TYPES:
+        raise BitLinearError(f"expected torch.float32, torch.bfloat16 or torch.int8, got {W.dtype}")
+    nbytes = packed_bytes_i8(N, K)
+    if nbytes == 0:
+        _check(-2, "bitlinear_pack_weights_i8")
+    packed = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+    scale = None if W.dtype is torch.int8 else torch.empty(N, dtype=torch.float32, device=dev)
+    _check(lib.bitlinear_pack_weights_i8(_ptr(W), _TYPES[W.dtype], N, K, packed.data_ptr(), _ptr(scale), _queue(dev)),
+           "bitlinear_pack_weights_i8")
+    return packed, scale
+
+
+def bitlinear_unpack_weights_i8(packed: torch.Tensor, scale: torch.Tensor | None, N: int, K: int,
+                                dtype: torch.dtype = torch.int8) -> torch.Tensor:
+    """The codes [N, K] (int8; scale may be None) or the values that they stand for (fp32, bf16)."""
+    lib, dev = load_library(), _here(packed)
+    if dtype not in _TYPES:
+        raise BitLinearError(f"expected torch.float32, torch.bfloat16 or torch.int8, got {dtype}")
+    out = torch.empty((N, K), dtype=dtype, device=dev)
+    _check(lib.bitlinear_unpack_weights_i8(
+        _given(dev, packed, torch.uint8, _blob_bytes_i8(N, K)),
+        None if scale is None else _given(dev, scale, torch.float32, N), N, K, _TYPES[dtype], out.data_ptr(), _queue(dev)),
+        "bitlinear_unpack_weights_i8")
+    return out
+
+
+def bitlinear_matmul_i8(codes: torch.Tensor, gamma: torch.Tensor | None, packed: torch.Tensor, N: int,
+                        scale: torch.Tensor | None, per_tensor: bool = False, flags: int = 0,
+                        dtype: torch.dtype = torch.float32, out: torch.Tensor | None = None,
+                        workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """Codes [M, K] x int8 weights, scaled by token (gamma) and channel (scale): [M, N] of `dtype` (fp32, bf16), or the
+    int32 sums with FLAG_OUT_ACC_I32 (gamma and scale may be None then)."""
+    lib, dev = load_library(), _here(codes)
+    M, K = codes.shape
+    y_type = _float_type(dtype)
+    dtype = torch.int32 if flags & FLAG_OUT_ACC_I32 else dtype
+    if out is None:
+        out = torch.empty((M, N), dtype=dtype, device=dev)
+    ws, ws_bytes, _keep = _scratch(workspace_bytes(OP_MATMUL_I8, M, N, K), workspace, dev)
+    _check(lib.bitlinear_matmul_i8(
+        _ptr(codes, torch.int8), None if gamma is None else _given(dev, gamma, torch.float32, 1 if per_tensor else M), M, K,
+        _given(dev, packed, torch.uint8, _blob_bytes_i8(N, K)), N,
+        None if scale is None else _given(dev, scale, torch.float32, N), _gran(per_tensor), flags, y_type,
+        _given(dev, out, dtype, M, N), ws, ws_bytes, _queue(dev)), "bitlinear_matmul_i8")
+    return out
+
+
+def bitlinear_backward_ste_i8(dY: torch.Tensor, codes: torch.Tensor | None, gamma: torch.Tensor | None,
+                              packed: torch.Tensor | None, scale: torch.Tensor | None, K: int | None = None,
+                              per_tensor: bool = False, want_dx: bool = True, want_dw: bool = True,
+                              dtype: torch.dtype = torch.float32, workspace: torch.Tensor | None = None):
+    """Straight-through backward of bitlinear_matmul_i8, dY [M, N] fp32 or bf16.  Returns (dX [M, K] of `dtype` or None, dW
+    fp32 [N, K] or None).  K: needed without `codes` (want_dw=False)."""
+    lib, dev = load_library(), _here(dY)
+    M, N = dY.shape
+    if codes is not None:
+        K = codes.shape[1]
+    elif K is None:
+        raise BitLinearError("K is not known without codes")
+    dX = torch.empty((M, K), dtype=dtype, device=dev) if want_dx else None
+    dW = (torch.empty if M else torch.zeros)((N, K), dtype=torch.float32, device=dev) if want_dw else None
+    ws, ws_bytes, _keep = _scratch(workspace_bytes(OP_BACKWARD_I8, M, N, K), workspace, dev)
+    _check(lib.bitlinear_backward_ste_i8(
+        _ptr(dY), _float_type(dY.dtype), M, N, K, None if codes is None else _given(dev, codes, torch.int8, M, K),
+        None if gamma is None else _given(dev, gamma, torch.float32, 1 if per_tensor else M), _gran(per_tensor),
+        None if packed is None else _given(dev, packed, torch.uint8, _blob_bytes_i8(N, K)),
+        None if scale is None else _given(dev, scale, torch.float32, N), _ptr(dX), _float_type(dtype), _ptr(dW), ws, ws_bytes,
+        _queue(dev)), "bitlinear_backward_ste_i8")
+    return dX, dW

@@ -16,7 +16,8 @@ OBJ = PKG / "_build"
 LIB = PKG / "libbitlinear.so"
 SOURCES = ["pack.hip", "quant.hip", "gemm_decode.hip", "gemm_tokens.hip", "gemm_prefill.hip", "gemm_mid.hip",
            "gemm_stream.hip", "backward.hip", "ln_backward.hip", "route.hip", "experts.hip",
-           "experts_backward.hip", "nonlinear.hip", "api.hip", "api_experts.hip"]
+           "experts_backward.hip", "nonlinear.hip", "rmsnorm.hip", "pack_i8.hip", "gemm_i8.hip", "backward_i8.hip", "api.hip",
+           "api_experts.hip", "api_i8.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [

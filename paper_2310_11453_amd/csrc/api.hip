@@ -286,7 +286,7 @@ size_t bitlinear_workspace_bytes(int op, int64_t M, int64_t N, int64_t K, int gr
             // 0 for most shapes: nothing is needed
             return std::max(M <= 64 ? gemm_split_ws_bytes(M, N, K) : 0, prefill_split_bytes(M, N, K, true));
         default:
-            return 0;
+            return workspace_bytes_i8(op, M, N, K, granularity);
     }
 }
 

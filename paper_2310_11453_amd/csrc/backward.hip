@@ -1189,8 +1189,10 @@ static RingPlan dw_plan(int64_t I, int64_t J, int64_t Rp) {
     return small < (full < 2 ? 1.0 : 1.02) * wide ? ring_plan(I, J, Rp, 128, 128) : p;
 }
 
+size_t gemm_tn_slices_bytes(int64_t I, int64_t J, int64_t Rp) { return slices_bytes(dw_plan(I, J, Rp), I, J); }
+
 // C[I][J] = scale * A[I][:] . B[J][:], in slices of r where the plan has them and `part` has room
-static void launch_gemm_tn(const uint16_t* A, const uint16_t* B, int64_t I, int64_t J, int64_t Rp,
+void launch_gemm_tn(const uint16_t* A, const uint16_t* B, int64_t I, int64_t J, int64_t Rp,
                            const float* scale_ptr, float scale_mul, float* C, float* part,
                            size_t part_bytes, hipStream_t s) {
     RingPlan p = dw_plan(I, J, Rp);
