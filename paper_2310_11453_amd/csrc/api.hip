@@ -30,6 +30,7 @@ const TuningField kTuningFields[] = {
     {"bwd_grid", &Tuning::bwd_grid},             {"bwd_rowmajor", &Tuning::bwd_rowmajor},
     {"bwd_splits", &Tuning::bwd_splits},         {"bwd_dx", &Tuning::bwd_dx},
     {"mid_kernel", &Tuning::mid_kernel},         {"experts_tile", &Tuning::experts_tile},
+    {"i8_tile", &Tuning::i8_tile},               {"i8_splits", &Tuning::i8_splits},
 };
 Tuning g_tuning{};
 bool g_tuning_init = false;
