@@ -31,6 +31,7 @@ const TuningField kTuningFields[] = {
     {"bwd_splits", &Tuning::bwd_splits},         {"bwd_dx", &Tuning::bwd_dx},
     {"mid_kernel", &Tuning::mid_kernel},         {"experts_tile", &Tuning::experts_tile},
     {"i8_tile", &Tuning::i8_tile},               {"i8_splits", &Tuning::i8_splits},
+    {"i8_rows", &Tuning::i8_rows},
 };
 Tuning g_tuning{};
 bool g_tuning_init = false;

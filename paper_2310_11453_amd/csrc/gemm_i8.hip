@@ -270,37 +270,147 @@ __global__ __launch_bounds__(256) void fold_i8(GemmI8Args a, int splits) {
     }
 }
 
-// A wave takes 16 rows of weights and 16 tokens; both operands come from memory as the MFMA wants them.
-__global__ __launch_bounds__(256) void gemm_i8_plain(GemmI8Args a, int64_t items, int64_t tn) {
-    const int w = threadIdx.x / kWave, l = threadIdx.x % kWave, c = l & 15, g = l >> 4;
-    const int64_t TK = i8_tiles_k(a.K);
-    for (int64_t it = (int64_t)blockIdx.x * 4 + w; it < items; it += (int64_t)gridDim.x * 4) {
-        const int64_t tile = it % tn, m0 = it / tn * 16;
-        const int64_t m = m0 + c < a.M ? m0 + c : a.M - 1;
-        const v4i* wt = reinterpret_cast<const v4i*>(a.packed + tile * TK * 1024) + l;
-        const int8_t* q = a.codes + m * a.K;
-        v4i acc = {0, 0, 0, 0};
-        for (int64_t t = 0; t < TK; ++t) {
-            int64_t k = t * 64 + 16 * g;
-            if (k >= a.K) k = 0;  // the weights there are zeros
-            acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(wt[t * 64], *reinterpret_cast<const v4i*>(q + k), acc, 0, 0, 0);
-        }
-        if (m0 + c >= a.M) continue;
-        const float gm = a.out_acc ? 0.f : (a.per_tensor ? *a.gamma : a.gamma[m]) * (1.0f / 128.0f);  // (null with out_acc)
+// ---- up to 64 tokens: the weights' stream ------------------------------------------------------------------
+// Bound by reading the weights once.  A workgroup takes TN rows of tiles (16 TN channels) and all of K, or a slice of it; its W
+// waves share the tiles of K evenly.  A wave loads S tiles of each row with 16 bytes a lane, which is the operand of
+// v_mfma_i32_16x16x64_i8 as it lies, and the codes of MB blocks of 16 tokens beside them (from L2), while it multiplies the ones
+// before.  The waves' sums meet in LDS.  A lane has four consecutive channels of one token.
+template <int TN, int MB, int S, int W>
+__global__ __launch_bounds__(W * 64, W * TN * MB <= 32 ? 4 : 2) void gemm_i8_stream(GemmI8Args a, int out) {
+    __shared__ v4i red[W][TN * MB][kWave];
+    const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave), l = threadIdx.x % kWave, c = l & 15, g = l >> 4;
+    const int K = (int)a.K, TK = (int)i8_tiles_k(K);
+    const int64_t rows = tiles_n(a.N);
+    const int ns = (int)gridDim.y, from_s = TK * (int)blockIdx.y / ns, in_s = TK * ((int)blockIdx.y + 1) / ns - from_s;
+    const int from = from_s + in_s * w / W, to = from_s + in_s * (w + 1) / W;
+    uint32_t row[MB];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int64_t n = tile * 16 + 4 * g + r;
-            if (n >= a.N) continue;
-            const int64_t at = m * a.N + n;
-            if (a.out_acc) {
-                static_cast<int32_t*>(a.Y)[at] = acc[r];
-            } else {
-                const float y = (float)acc[r] * (a.scale[n] * gm);
-                if (a.y_bf16) static_cast<uint16_t*>(a.Y)[at] = (uint16_t)bf16_pair(y, 0.f);
-                else static_cast<float*>(a.Y)[at] = y;
+    for (int b = 0; b < MB; ++b) row[b] = (uint32_t)(16 * b + c < (int)a.M ? 16 * b + c : (int)a.M - 1) * (uint32_t)K;
+    const bool odd = (K & 63) != 0;  // the last tile's second half is behind K
+
+    // (one item a workgroup but for more channels than a launch takes)
+    for (int64_t tile0 = (int64_t)blockIdx.x * TN; tile0 < rows; tile0 += (int64_t)gridDim.x * TN) {
+    const uint8_t* wt[TN];
+#pragma unroll
+    for (int t = 0; t < TN; ++t) wt[t] = a.packed + (tile0 + t < rows ? tile0 + t : rows - 1) * TK * 1024;
+    struct Step {
+        v4i w[S][TN], q[S][MB];
+    } A, B;
+    v4i acc[TN][MB];
+#pragma unroll
+    for (int t = 0; t < TN; ++t)
+#pragma unroll
+        for (int b = 0; b < MB; ++b) acc[t][b] = v4i{0, 0, 0, 0};
+    auto load = [&](Step& x, int at) {
+#pragma unroll
+        for (int s = 0; s < S; ++s) {
+            const int t = at + s < to ? at + s : to - 1;
+#pragma unroll
+            for (int r = 0; r < TN; ++r)
+                x.w[s][r] = __builtin_nontemporal_load(reinterpret_cast<const v4i*>(wt[r] + (uint32_t)t * 1024u) + l);
+            const uint32_t k = (uint32_t)t * 64 + (odd && t == TK - 1 ? 16 * (g & 1) : 16 * g);  // (against zeros)
+#pragma unroll
+            for (int b = 0; b < MB; ++b) x.q[s][b] = *reinterpret_cast<const v4i*>(a.codes + (row[b] + k));
+        }
+    };
+    auto multiply = [&](const Step& x, int at) {
+#pragma unroll
+        for (int s = 0; s < S; ++s)
+            if (at + s < to) {  // uniform
+#pragma unroll
+                for (int r = 0; r < TN; ++r)
+#pragma unroll
+                    for (int b = 0; b < MB; ++b)
+                        acc[r][b] = __builtin_amdgcn_mfma_i32_16x16x64_i8(x.w[s][r], x.q[s][b], acc[r][b], 0, 0, 0);
             }
+    };
+    if (from < to) {
+        int at = from;
+        load(A, at);
+        for (; at + 2 * S < to; at += 2 * S) {
+            load(B, at + S);
+            multiply(A, at);
+            load(A, at + 2 * S);
+            multiply(B, at + S);
+        }
+        if (at + S < to) {
+            load(B, at + S);
+            multiply(A, at);
+            multiply(B, at + S);
+        } else {
+            multiply(A, at);
         }
     }
+#pragma unroll
+    for (int r = 0; r < TN; ++r)
+#pragma unroll
+        for (int b = 0; b < MB; ++b) red[w][r * MB + b][l] = acc[r][b];
+    __syncthreads();
+    for (int i = threadIdx.x; i < TN * MB * kWave; i += W * kWave) {
+        const int slot = i / kWave, r = slot / MB, m = 16 * (slot % MB) + (i & 15);
+        const int64_t n = (tile0 + r) * 16 + 4 * (i % kWave >> 4);
+        v4i v = red[0][slot][i % kWave];
+#pragma unroll
+        for (int k = 1; k < W; ++k) v += red[k][slot][i % kWave];
+        if (m >= (int)a.M || n >= a.N) continue;
+        const int64_t o = (int64_t)m * a.N + n;
+        const int left = a.N - n < 4 ? (int)(a.N - n) : 4;
+        if (out == kOutPart || out == kOutAcc) {
+            int32_t* y = out == kOutPart ? a.part + (int64_t)blockIdx.y * a.M * a.N + o : static_cast<int32_t*>(a.Y) + o;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (e < left) y[e] = v[e];
+            continue;
+        }
+        const float gm = (a.per_tensor ? *a.gamma : a.gamma[m]) * (1.0f / 128.0f);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (e < left) {
+                const float y = (float)v[e] * (a.scale[n + e] * gm);
+                if (out == kOutBF16) static_cast<uint16_t*>(a.Y)[o + e] = (uint16_t)bf16_pair(y, 0.f);
+                else static_cast<float*>(a.Y)[o + e] = y;
+            }
+    }
+    __syncthreads();
+    }
+}
+
+struct StreamPlan {
+    int tn, mb, waves, slices;
+};
+static StreamPlan stream_plan(int64_t M, int64_t N, int64_t K) {
+    StreamPlan p{};
+    const int64_t rows = tiles_n(N), TK = i8_tiles_k(K), cus = num_cus();
+    p.mb = (int)((M + 15) / 16);
+    const Tuning& t = tuning();
+    p.tn = rows >= 4 * cus ? 4 : rows >= 2 * cus ? 2 : 1;
+    if (t.i8_rows == 1 || t.i8_rows == 2 || t.i8_rows == 4) p.tn = t.i8_rows;
+    p.waves = 8;
+    const int64_t wgs = (rows + p.tn - 1) / p.tn;
+    int64_t n = 1;
+    if (wgs * 2 <= cus) n = cus / wgs;
+    if (n > TK / 32) n = TK / 32;
+    if (n > 16) n = 16;
+    if (t.i8_splits > 0) n = t.i8_splits < TK ? t.i8_splits : TK;
+    p.slices = (int)(n < 1 ? 1 : n);
+    return p;
+}
+static void launch_stream(const GemmI8Args& a, const StreamPlan& p, int out, hipStream_t s) {
+    const int64_t wgs = (tiles_n(a.N) + p.tn - 1) / p.tn;
+    const dim3 grid((unsigned)(wgs < (1 << 18) ? wgs : (1 << 18)), (unsigned)p.slices);
+    auto go = [&](auto tn, auto mb) {
+        constexpr int TN = decltype(tn)::value, MB = decltype(mb)::value, S = 8 / TN < 4 ? 8 / TN : 4;
+        gemm_i8_stream<TN, MB, S, 8><<<grid, 512, 0, s>>>(a, out);
+    };
+    auto rows = [&](auto tn) {
+        if (p.mb == 1) go(tn, std::integral_constant<int, 1>{});
+        else if (p.mb == 2) go(tn, std::integral_constant<int, 2>{});
+        else if (p.mb == 3) go(tn, std::integral_constant<int, 3>{});
+        else go(tn, std::integral_constant<int, 4>{});
+    };
+    if (p.tn == 1) rows(std::integral_constant<int, 1>{});
+    else if (p.tn == 2) rows(std::integral_constant<int, 2>{});
+    else rows(std::integral_constant<int, 4>{});
 }
 
 // Cost in us of tiles in slices: rounds of workgroups, each of `per` stages.
@@ -338,21 +448,28 @@ static I8Plan unsliced(I8Plan p, int64_t K) {
     return p;
 }
 static bool few_tokens(int64_t M) { return M <= 64; }
+static size_t slices_bytes(int64_t slices, int64_t M, int64_t N) { return slices > 1 ? (size_t)slices * M * N * 4 : 0; }
 
 size_t gemm_i8_part_bytes(int64_t M, int64_t N, int64_t K) {
-    if (M == 0 || few_tokens(M)) return 0;
-    const I8Plan p = i8_plan(M, N, K);
-    return p.splits > 1 ? (size_t)p.splits * (size_t)M * (size_t)N * 4 : 0;
+    if (M == 0) return 0;
+    return slices_bytes(few_tokens(M) ? stream_plan(M, N, K).slices : i8_plan(M, N, K).splits, M, N);
+}
+static void launch_fold(const GemmI8Args& a, int splits, int out, hipStream_t s) {
+    const int64_t wgs = (a.M * a.N + 255) / 256;
+    const auto fold = out == kOutAcc ? fold_i8<kOutAcc> : out == kOutBF16 ? fold_i8<kOutBF16> : fold_i8<kOutF32>;
+    fold<<<(unsigned)(wgs < (1 << 16) ? wgs : (1 << 16)), 256, 0, s>>>(a, splits);
 }
 hipError_t launch_gemm_i8(const GemmI8Args& a, hipStream_t s) {
     const int out = a.out_acc ? kOutAcc : a.y_bf16 ? kOutBF16 : kOutF32;
     if (few_tokens(a.M)) {
-        const int64_t tn = tiles_n(a.N), items = tn * ((a.M + 15) / 16), wgs = (items + 3) / 4;
-        gemm_i8_plain<<<(unsigned)(wgs < (1 << 20) ? wgs : (1 << 20)), 256, 0, s>>>(a, items, tn);
+        StreamPlan p = stream_plan(a.M, a.N, a.K);
+        if (slices_bytes(p.slices, a.M, a.N) > a.part_bytes) p.slices = 1;
+        launch_stream(a, p, p.slices > 1 ? kOutPart : out, s);
+        if (p.slices > 1) launch_fold(a, p.slices, out, s);
         return hipGetLastError();
     }
     I8Plan p = i8_plan(a.M, a.N, a.K);
-    if (p.splits > 1 && (size_t)p.splits * (size_t)a.M * (size_t)a.N * 4 > a.part_bytes) p = unsliced(p, a.K);
+    if (slices_bytes(p.splits, a.M, a.N) > a.part_bytes) p = unsliced(p, a.K);
     const int kind = p.splits > 1 ? kOutPart : out;
     auto pick = [&](auto t) {
         constexpr int T = decltype(t)::value;
@@ -363,11 +480,7 @@ hipError_t launch_gemm_i8(const GemmI8Args& a, hipStream_t s) {
     };
     const auto kernel = p.tile == 256 ? pick(std::integral_constant<int, 256>{}) : pick(std::integral_constant<int, 128>{});
     kernel<<<(unsigned)p.grid, 256, 0, s>>>(a, p);
-    if (p.splits > 1) {
-        const int64_t wgs = (a.M * a.N + 255) / 256;
-        const auto fold = out == kOutAcc ? fold_i8<kOutAcc> : out == kOutBF16 ? fold_i8<kOutBF16> : fold_i8<kOutF32>;
-        fold<<<(unsigned)(wgs < (1 << 16) ? wgs : (1 << 16)), 256, 0, s>>>(a, p.splits);
-    }
+    if (p.splits > 1) launch_fold(a, p.splits, out, s);
     return hipGetLastError();
 }
 

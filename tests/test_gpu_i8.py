@@ -126,6 +126,16 @@ def test_product_tiles(bl, tuning, M, K, N, tile, splits):
     check_product(bl, M, K, N, per_tensor=splits == 1)
 
 
+@pytest.mark.parametrize("M,K,N", [(1, 32, 1), (1, 2048, 100), (4, 608, 17), (17, 96, 200), (30, 2080, 79), (33, 1056, 64),
+                                   (48, 544, 300), (64, 4128, 130)])
+@pytest.mark.parametrize("rows", [1, 2, 4])
+@pytest.mark.parametrize("splits", [0, 1, 2, 7])
+def test_product_of_few_tokens(bl, tuning, M, K, N, rows, splits):
+    print(f"matmul_i8 M={M} K={K} N={N} rows={rows} splits={splits}", flush=True)
+    tuning(f"i8_rows={rows},i8_splits={splits}")
+    check_product(bl, M, K, N, per_tensor=splits == 1)
+
+
 def test_product_of_the_largest_sums(bl):
     """All codes -128 at the largest K: 2^30."""
     for M in (1, 20, 100, 300):
