@@ -8,7 +8,7 @@
 namespace bl {
 
 // ---- tiles ---------------------------------------------------------------------------------------------
-// T x T of the output a workgroup, four waves of T/2 x T/2 on v_mfma_i32_32x32x32_i8, persistent over the tiles.  A stage is 64 k: a
+// TM x TN of the output a workgroup, four waves of a quarter each on v_mfma_i32_32x32x32_i8, persistent over the tiles.  A stage is 64 k: a
 // row of codes has 64 bytes of it, 16 channels a tile of the packed weights, both streamed global -> LDS by
 // global_load_lds_dwordx4 into a ring of NS stages.  The 16-byte pieces of a row of codes are XOR-swizzled with (row / 4) % 4;
 // the weights' tiles are the operands' own layout and need no swizzle.  The schedule is that of the bf16 product of backward.hip,
@@ -44,22 +44,33 @@ __device__ inline void i8_issue(v4i (&a)[2], v4i (&b)[2], uint32_t ad_a, uint32_
 __device__ inline void i8_wait(v4i (&a)[2], v4i (&b)[2]) {
     asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(a[0]), "+v"(a[1]), "+v"(b[0]), "+v"(b[1]));
 }
+__device__ inline void i8_issue(v4i (&a)[1], v4i (&b)[2], uint32_t ad_a, uint32_t ad_b) {
+    asm volatile(
+        "ds_read_b128 %0, %3\n\t"
+        "ds_read_b128 %1, %4\n\t"
+        "ds_read_b128 %2, %4 offset:2048"
+        : "=&v"(a[0]), "=&v"(b[0]), "=&v"(b[1])
+        : "v"(ad_a), "v"(ad_b));
+}
+__device__ inline void i8_wait(v4i (&a)[1], v4i (&b)[2]) {
+    asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(a[0]), "+v"(b[0]), "+v"(b[1]));
+}
 
 enum I8Out { kOutF32 = 0, kOutBF16 = 1, kOutAcc = 2, kOutPart = 3 };  // kOutPart: a slice's int32 sums
 struct I8Plan {
-    int tile, grid, gm, gn;  // rows and columns of tiles
+    int tile, grid, gm, gn;  // which tile (kTiles); workgroups; rows and columns of tiles
     int splits, per;         // slices of K, of `per` stages
 };
 
-template <int T, int NS, int OUT>
-__global__ __launch_bounds__(256, T == 256 ? 1 : 2) void gemm_i8_tiles(GemmI8Args a, I8Plan p) {
-    constexpr int THREADS = 256, WT = T / 2, MI = T / 64, PA = T * 4 / THREADS, P = 2 * PA;
-    constexpr int A_BYTES = T * 64, STAGE_BYTES = 2 * A_BYTES;
+template <int TM, int TN, int NS, int OUT>
+__global__ __launch_bounds__(256, TM == 256 ? 1 : 2) void gemm_i8_tiles(GemmI8Args a, I8Plan p) {
+    constexpr int THREADS = 256, WTM = TM / 2, WTN = TN / 2, MI = WTM / 32, NI = WTN / 32;
+    constexpr int PA = TM / 64, PB = TN / 64, P = PA + PB;
+    constexpr int A_BYTES = TM * 64, STAGE_BYTES = A_BYTES + TN * 64;
     constexpr bool SPLIT = OUT == kOutPart;
     static_assert((NS - 1) * P < 64, "vmcnt range");
-    static_assert(PA == MI, "a piece of the codes and one of the weights for each row of MFMAs");
     __shared__ __attribute__((aligned(1024))) uint8_t sm[NS * STAGE_BYTES];
-    __shared__ float sm_gamma[2][T];
+    __shared__ float sm_gamma[2][TM];
 
     const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave), l = threadIdx.x % kWave;
     const int wm = w / 2, wn = w % 2, j = l & 31, g2 = l >> 5;
@@ -89,13 +100,13 @@ __global__ __launch_bounds__(256, T == 256 ? 1 : 2) void gemm_i8_tiles(GemmI8Arg
         main_groups = nst >= 2 * NS - 1 ? (nst - (2 * NS - 1)) / NS + 1 : 0;
         const int band = tile / (H * p.gn), rem = tile - band * H * p.gn;
         const int rows = p.gm - band * H < H ? p.gm - band * H : H;
-        m0 = (int64_t)(band * H + rem % rows) * T;
-        n0 = (int64_t)(rem / rows) * T;
+        m0 = (int64_t)(band * H + rem % rows) * TM;
+        n0 = (int64_t)(rem / rows) * TN;
     };
 
-    // thread -> PA pieces of 16 bytes of each operand.  Rows past the last token re-read it, tiles past the last one
+    // thread -> PA + PB pieces of 16 bytes.  Rows past the last token re-read it, tiles past the last one
     // that one: their results are never stored.
-    uint32_t goffA[PA], goffB[PA];
+    uint32_t goffA[PA], goffB[PB];
     const uint8_t *baseA = nullptr, *baseB = nullptr;
     const int seg = (((int)threadIdx.x & 3) ^ (((int)threadIdx.x >> 4) & 3)) * 16;  // the same in all of a thread's rows
     auto setup_dma = [&](int64_t m0, int64_t n0) {
@@ -104,6 +115,9 @@ __global__ __launch_bounds__(256, T == 256 ? 1 : 2) void gemm_i8_tiles(GemmI8Arg
             int row = (q * THREADS + (int)threadIdx.x) >> 2;
             if (m0 + row > a.M - 1) row = (int)(a.M - 1 - m0);
             goffA[q] = (uint32_t)row * (uint32_t)K + (uint32_t)seg;
+        }
+#pragma unroll
+        for (int q = 0; q < PB; ++q) {
             int tile = q * 4 + w;
             const int last = (int)(tiles_n(a.N) - 1 - n0 / 16);
             if (tile > last) tile = last;
@@ -117,38 +131,43 @@ __global__ __launch_bounds__(256, T == 256 ? 1 : 2) void gemm_i8_tiles(GemmI8Arg
     // exist: the slot is filled with bytes nobody uses).  The second half of the odd last stage is behind the row: the
     // first half again, against zeros.
     auto issue_piece = [&](int st, int src, int q) {
-        uint8_t* dst = sm + (st % NS) * STAGE_BYTES + lds_wave + q * THREADS * 16;
-        uint32_t off = goffA[q];
-        if (odd && st0 + src == nst_all - 1) off -= (uint32_t)(seg & 32);  // uniform
-        __builtin_amdgcn_global_load_lds((const void*)(baseA + src * 64 + off),
-                                         (__attribute__((address_space(3))) void*)dst, 16, 0, 0);
-        __builtin_amdgcn_global_load_lds((const void*)(baseB + src * 1024 + goffB[q]),
-                                         (__attribute__((address_space(3))) void*)(dst + A_BYTES), 16, 0, 0);
+        uint8_t* dst = sm + (st % NS) * STAGE_BYTES + lds_wave;
+        if (q < PA) {
+            uint32_t off = goffA[q < PA ? q : 0];
+            if (odd && st0 + src == nst_all - 1) off -= (uint32_t)(seg & 32);  // uniform
+            __builtin_amdgcn_global_load_lds((const void*)(baseA + src * 64 + off),
+                                             (__attribute__((address_space(3))) void*)(dst + q * THREADS * 16), 16, 0, 0);
+        } else {
+            const int b = q < PA ? 0 : q - PA;
+            __builtin_amdgcn_global_load_lds((const void*)(baseB + src * 1024 + goffB[b]),
+                                             (__attribute__((address_space(3))) void*)(dst + A_BYTES + b * THREADS * 16), 16, 0,
+                                             0);
+        }
     };
     auto issue_tile_start = [&]() {
 #pragma unroll
         for (int s = 0; s < NS - 1; ++s)
 #pragma unroll
-            for (int q = 0; q < PA; ++q) issue_piece(s, s < nst ? s : nst - 1, q);
+            for (int q = 0; q < P; ++q) issue_piece(s, s < nst ? s : nst - 1, q);
     };
 
     // lane's operand addresses inside a stage, for either half
     const uint32_t smb = (uint32_t)(uintptr_t)sm;
     const int sw = (j >> 2) & 3;
-    const uint32_t a_row = smb + (wm * WT + j) * 64;
+    const uint32_t a_row = smb + (wm * WTM + j) * 64;
     const uint32_t a_lane[2] = {a_row + (g2 ^ sw) * 16, a_row + ((2 + g2) ^ sw) * 16};
-    const uint32_t b_row = smb + A_BYTES + (wn * (WT / 16) + (j >> 4)) * 1024 + (j & 15) * 16;
+    const uint32_t b_row = smb + A_BYTES + (wn * (WTN / 16) + (j >> 4)) * 1024 + (j & 15) * 16;
     const uint32_t b_lane[2] = {b_row + g2 * 256, b_row + (2 + g2) * 256};
     auto ring = [&](int st) { return (uint32_t)((st % NS) * STAGE_BYTES); };
 
-    v16i acc[MI][MI];
-    v4i ax[MI], ay[MI], bx[MI], by[MI];
-    auto half_step = [&](const v4i(&ac)[MI], const v4i(&bc)[MI], v4i(&an)[MI], v4i(&bn)[MI], uint32_t ad_a, uint32_t ad_b,
+    v16i acc[MI][NI];
+    v4i ax[MI], ay[MI], bx[NI], by[NI];
+    auto half_step = [&](const v4i(&ac)[MI], const v4i(&bc)[NI], v4i(&an)[MI], v4i(&bn)[NI], uint32_t ad_a, uint32_t ad_b,
                          auto between) {
 #pragma unroll
         for (int mi = 0; mi < MI; ++mi) {
 #pragma unroll
-            for (int s = 0; s < MI; ++s) acc[mi][s] = __builtin_amdgcn_mfma_i32_32x32x32_i8(ac[mi], bc[s], acc[mi][s], 0, 0, 0);
+            for (int s = 0; s < NI; ++s) acc[mi][s] = __builtin_amdgcn_mfma_i32_32x32x32_i8(ac[mi], bc[s], acc[mi][s], 0, 0, 0);
             __builtin_amdgcn_sched_barrier(0);
             if (mi == 0) i8_issue(an, bn, ad_a, ad_b);
             between(mi);
@@ -163,7 +182,9 @@ __global__ __launch_bounds__(256, T == 256 ? 1 : 2) void gemm_i8_tiles(GemmI8Arg
         else wait_vmcnt<0>();
         block_barrier();
         half_step(ay, by, ax, bx, a_lane[0] + ring(st + 1), b_lane[0] + ring(st + 1), [&](int mi) {
-            if (ahead) issue_piece(st + NS - 1, st + NS - 1, mi);
+            if (ahead)
+#pragma unroll
+                for (int q = mi * P / MI; q < (mi + 1) * P / MI; ++q) issue_piece(st + NS - 1, st + NS - 1, q);
         });
     };
 
@@ -176,7 +197,7 @@ __global__ __launch_bounds__(256, T == 256 ? 1 : 2) void gemm_i8_tiles(GemmI8Arg
 #pragma unroll
         for (int mi = 0; mi < MI; ++mi)
 #pragma unroll
-            for (int s = 0; s < MI; ++s)
+            for (int s = 0; s < NI; ++s)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) acc[mi][s][r] = 0;
         wait_vmcnt<(NS - 2) * P>();  // younger than stage 0: stages 1 .. NS - 2
@@ -190,15 +211,15 @@ __global__ __launch_bounds__(256, T == 256 ? 1 : 2) void gemm_i8_tiles(GemmI8Arg
 
         // the tile's factors, behind the waits of its stages
         if constexpr (OUT == kOutF32 || OUT == kOutBF16) {
-            if (threadIdx.x < T) {
+            if (threadIdx.x < TM) {
                 const int64_t m = m0 + threadIdx.x;
                 sm_gamma[parity][threadIdx.x] = (a.per_tensor ? *a.gamma : a.gamma[m < a.M ? m : a.M - 1]) * (1.0f / 128.0f);
             }
         }
-        float sc[MI];
+        float sc[NI];
 #pragma unroll
-        for (int s = 0; s < MI; ++s) {
-            const int64_t n = n0 + wn * WT + 32 * s + j;
+        for (int s = 0; s < NI; ++s) {
+            const int64_t n = n0 + wn * WTN + 32 * s + j;
             sc[s] = OUT == kOutF32 || OUT == kOutBF16 ? a.scale[n < a.N ? n : a.N - 1] : 0.f;
         }
         // every wave is done with the ring (and sees the factors): start the next tile's stream, then store
@@ -212,8 +233,8 @@ __global__ __launch_bounds__(256, T == 256 ? 1 : 2) void gemm_i8_tiles(GemmI8Arg
             setup_dma(m0, n0);
             issue_tile_start();
         }
-        const int64_t mb = mt + __builtin_amdgcn_readfirstlane(wm * WT), nb = nt + __builtin_amdgcn_readfirstlane(wn * WT);
-        const float* gm = sm_gamma[parity] + wm * WT + 4 * g2;
+        const int64_t mb = mt + __builtin_amdgcn_readfirstlane(wm * WTM), nb = nt + __builtin_amdgcn_readfirstlane(wn * WTN);
+        const float* gm = sm_gamma[parity] + wm * WTM + 4 * g2;
         if constexpr (OUT == kOutBF16) {
 #pragma unroll
             for (int mi = 0; mi < MI; ++mi)
@@ -223,7 +244,7 @@ __global__ __launch_bounds__(256, T == 256 ? 1 : 2) void gemm_i8_tiles(GemmI8Arg
                     const float g = gm[32 * mi + 8 * (r >> 2) + (r & 3)];
                     if (m >= a.M) continue;
 #pragma unroll
-                    for (int s = 0; s < MI; ++s) {
+                    for (int s = 0; s < NI; ++s) {
                         const int64_t n = nb + 32 * s + j;
                         if (n < a.N)
                             static_cast<uint16_t*>(a.Y)[m * a.N + n] = (uint16_t)bf16_pair((float)acc[mi][s][r] * (sc[s] * g), 0.f);
@@ -238,7 +259,7 @@ __global__ __launch_bounds__(256, T == 256 ? 1 : 2) void gemm_i8_tiles(GemmI8Arg
                     const float g = OUT == kOutF32 ? gm[32 * mi + 8 * (r >> 2) + (r & 3)] : 0.f;
                     if (m >= a.M) continue;
 #pragma unroll
-                    for (int s = 0; s < MI; ++s) {
+                    for (int s = 0; s < NI; ++s) {
                         const int64_t n = nb + 32 * s + j;
                         if (n >= a.N) continue;
                         if constexpr (OUT == kOutPart) a.part[((int64_t)sl * a.M + m) * a.N + n] = acc[mi][s][r];
@@ -413,28 +434,34 @@ static void launch_stream(const GemmI8Args& a, const StreamPlan& p, int out, hip
     else rows(std::integral_constant<int, 4>{});
 }
 
-// Cost in us of tiles in slices: rounds of workgroups, each of `per` stages.
+// The tiles: 256 x 256 with one workgroup a CU, 128 x 128 and 64 x 128 with two.  Cost in us: rounds of workgroups, each of
+// `per` stages; `alone`: a stage with one workgroup on a CU.
+struct I8Tile {
+    int tm, tn, wgs;  // wgs: a CU's
+    double stage, alone, item;
+};
+constexpr I8Tile kTiles[3] = {{256, 256, 1, 0.62, 0.62, 12.0}, {128, 128, 2, 0.385, 0.22, 4.5}, {64, 128, 2, 0.3, 0.18, 3.5}};
 static I8Plan i8_plan(int64_t M, int64_t N, int64_t K) {
     const Tuning& t = tuning();
     const int64_t cus = num_cus(), nst = i8_tiles_k(K);
     I8Plan best{};
     double least = 1e30;
-    for (int T = 256; T >= 128; T /= 2) {
-        if (t.i8_tile && t.i8_tile != (T == 256 ? 1 : 2)) continue;
-        const int64_t gm = (M + T - 1) / T, gn = (N + T - 1) / T, tiles = gm * gn;
+    for (int k = 0; k < 3; ++k) {
+        if (t.i8_tile >= 1 && t.i8_tile <= 3 && t.i8_tile != k + 1) continue;
+        const I8Tile& T = kTiles[k];
+        const int64_t gm = (M + T.tm - 1) / T.tm, gn = (N + T.tn - 1) / T.tn, tiles = gm * gn;
         const int64_t force = t.i8_splits > 0 ? t.i8_splits : 0;
         for (int64_t n = force ? force : 1; n <= (force ? force : 16); ++n) {
             const int64_t per = (nst + n - 1) / n, splits = (nst + per - 1) / per, items = tiles * splits;
             if (n > 1 && !force && (per < 4 || splits != n || items > 4 * cus)) continue;
-            const double stage = T == 256 ? 0.62 : 0.22, item = T == 256 ? 12.0 : 4.5;
-            const int64_t slots = T == 256 ? cus : items > cus ? 2 * cus : cus;
+            const int64_t slots = items > cus ? T.wgs * cus : cus;
             const int64_t rounds = (items + slots - 1) / slots;
-            double cost = (double)rounds * (stage * (slots > cus ? 1.75 : 1.0) * (double)per + item);
+            double cost = (double)rounds * ((slots > cus ? T.stage : T.alone) * (double)per + T.item);
             if (splits > 1) cost += 4.0 + (double)(M * N) * 4.0 * (double)splits * 2e-6 / 5.0;
             if (cost < least) {
                 least = cost;
-                const int64_t cap = T == 256 ? cus : 2 * cus, up = (items + 7) / 8 * 8;
-                best = I8Plan{T, (int)(up < cap ? up : cap), (int)gm, (int)gn, (int)splits, (int)per};
+                const int64_t cap = T.wgs * cus, up = (items + 7) / 8 * 8;
+                best = I8Plan{k, (int)(up < cap ? up : cap), (int)gm, (int)gn, (int)splits, (int)per};
             }
         }
     }
@@ -447,7 +474,10 @@ static I8Plan unsliced(I8Plan p, int64_t K) {
     p.per = (int)i8_tiles_k(K);
     return p;
 }
-static bool few_tokens(int64_t M) { return M <= 64; }
+static bool few_tokens(int64_t M) {
+    const int t = tuning().i8_tile;
+    return M <= 64 && (t < 1 || t > 3);
+}
 static size_t slices_bytes(int64_t slices, int64_t M, int64_t N) { return slices > 1 ? (size_t)slices * M * N * 4 : 0; }
 
 size_t gemm_i8_part_bytes(int64_t M, int64_t N, int64_t K) {
@@ -471,14 +501,18 @@ hipError_t launch_gemm_i8(const GemmI8Args& a, hipStream_t s) {
     I8Plan p = i8_plan(a.M, a.N, a.K);
     if (slices_bytes(p.splits, a.M, a.N) > a.part_bytes) p = unsliced(p, a.K);
     const int kind = p.splits > 1 ? kOutPart : out;
-    auto pick = [&](auto t) {
-        constexpr int T = decltype(t)::value;
-        return kind == kOutPart ? gemm_i8_tiles<T, 4, kOutPart>
-             : kind == kOutAcc  ? gemm_i8_tiles<T, 4, kOutAcc>
-             : kind == kOutBF16 ? gemm_i8_tiles<T, 4, kOutBF16>
-                                : gemm_i8_tiles<T, 4, kOutF32>;
+    auto pick = [&](auto tm, auto tn, auto ns) {
+        constexpr int TM = decltype(tm)::value, TN = decltype(tn)::value, NS = decltype(ns)::value;
+        return kind == kOutPart ? gemm_i8_tiles<TM, TN, NS, kOutPart>
+             : kind == kOutAcc  ? gemm_i8_tiles<TM, TN, NS, kOutAcc>
+             : kind == kOutBF16 ? gemm_i8_tiles<TM, TN, NS, kOutBF16>
+                                : gemm_i8_tiles<TM, TN, NS, kOutF32>;
     };
-    const auto kernel = p.tile == 256 ? pick(std::integral_constant<int, 256>{}) : pick(std::integral_constant<int, 128>{});
+    using std::integral_constant;
+    const auto kernel =
+        p.tile == 0   ? pick(integral_constant<int, 256>{}, integral_constant<int, 256>{}, integral_constant<int, 4>{})
+        : p.tile == 1 ? pick(integral_constant<int, 128>{}, integral_constant<int, 128>{}, integral_constant<int, 4>{})
+                      : pick(integral_constant<int, 64>{}, integral_constant<int, 128>{}, integral_constant<int, 6>{});
     kernel<<<(unsigned)p.grid, 256, 0, s>>>(a, p);
     if (p.splits > 1) launch_fold(a, p.splits, out, s);
     return hipGetLastError();
