@@ -33,17 +33,17 @@ bool aligned16(const P*... p) {
     return ((... | (uintptr_t)p) & 15) == 0;
 }
 
-// per tensor: 1/rms and the largest magnitude of each row
+// per tensor: 1/rms of each row, and the largest magnitudes
 struct RmsWs {
     size_t most, total;
 };
 RmsWs rms_ws(int64_t M) {
     RmsWs w{};
     w.most = align256((size_t)M * 8);
-    w.total = w.most + align256((size_t)M * 4) + 256;
+    w.total = w.most + kRmsMostBytes + 256;
     return w;
 }
-size_t rms_backward_bytes(int64_t M, int64_t K) { return (size_t)rms_backward_groups(M, K) * (size_t)K * 8 + 256; }
+size_t rms_backward_bytes(int64_t M, int64_t K) { return rms_backward_part_bytes(M, K) + 256; }
 int product_status(int64_t M, int64_t N, int64_t K) {
     if (M < 0 || M > kMaxDim || !weights_ok(N, K)) return BL_ERR_SHAPE;
     return K > kMaxGemmK ? BL_ERR_UNSUPPORTED : BL_OK;

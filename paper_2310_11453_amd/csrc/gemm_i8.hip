@@ -132,14 +132,16 @@ __global__ __launch_bounds__(256, TM == 256 ? 1 : 2) void gemm_i8_tiles(GemmI8Ar
     // first half again, against zeros.
     auto issue_piece = [&](int st, int src, int q) {
         uint8_t* dst = sm + (st % NS) * STAGE_BYTES + lds_wave;
-        if (q < PA) {
-            uint32_t off = goffA[q < PA ? q : 0];
+        // in turn: codes, weights, codes, ... where there are as many of both
+        const bool first_kind = PA == PB ? q % 2 == 0 : q < PA;
+        const int b = PA == PB ? q / 2 : q < PA ? q : q - PA;
+        if (first_kind) {
+            uint32_t off = goffA[b < PA ? b : 0];
             if (odd && st0 + src == nst_all - 1) off -= (uint32_t)(seg & 32);  // uniform
             __builtin_amdgcn_global_load_lds((const void*)(baseA + src * 64 + off),
-                                             (__attribute__((address_space(3))) void*)(dst + q * THREADS * 16), 16, 0, 0);
+                                             (__attribute__((address_space(3))) void*)(dst + b * THREADS * 16), 16, 0, 0);
         } else {
-            const int b = q < PA ? 0 : q - PA;
-            __builtin_amdgcn_global_load_lds((const void*)(baseB + src * 1024 + goffB[b]),
+            __builtin_amdgcn_global_load_lds((const void*)(baseB + src * 1024 + goffB[b < PB ? b : 0]),
                                              (__attribute__((address_space(3))) void*)(dst + A_BYTES + b * THREADS * 16), 16, 0,
                                              0);
         }

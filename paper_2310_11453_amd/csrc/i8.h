@@ -53,8 +53,10 @@ struct QuantRmsArgs {
     int32_t* rowsum;  // or null
     float* xhat;      // or null
     double* rstd;     // per tensor: [M]
-    float* most;      // per tensor: [M]
+    float* most;      // per tensor: the largest magnitude of each workgroup's rows, kRmsMostBytes
+    int groups;       // how many of those (set by the launcher)
 };
+constexpr size_t kRmsMostBytes = 2048 * 4;
 hipError_t launch_quant_rmsnorm(const QuantRmsArgs& a, hipStream_t s);
 
 struct RmsBackwardArgs {
@@ -66,9 +68,9 @@ struct RmsBackwardArgs {
     const float* gain;  // or null
     double eps, inv_k;
     float* dgain;      // [K] or null
-    double* partials;  // with dgain: [rms_backward_groups][K]
+    void* partials;    // with dgain: rms_backward_part_bytes
 };
-int rms_backward_groups(int64_t M, int64_t K);
+size_t rms_backward_part_bytes(int64_t M, int64_t K);
 hipError_t launch_rmsnorm_backward(const RmsBackwardArgs& a, hipStream_t s);
 
 // gemm_i8.hip

@@ -13,7 +13,167 @@ namespace bl {
 
 enum RmsMode { kRmsFull = 0, kRmsStats = 1, kRmsApply = 2 };
 
-// A workgroup walks a row from memory once per step.
+// Per tensor the first pass leaves the largest magnitude of each workgroup's rows, and every workgroup of the second folds them:
+// no launch between the two.  The second pass goes through the rows from the end, which are still in the caches.
+constexpr int kRmsGroups = kRmsMostBytes / 4;
+
+__device__ inline float4 rounded(float4 v, const uint16_t*) {
+    const uint32_t a = bf16_pair(v.x, v.y), b = bf16_pair(v.z, v.w);
+    return make_float4(__uint_as_float(a << 16), __uint_as_float(a & 0xffff0000u), __uint_as_float(b << 16),
+                       __uint_as_float(b & 0xffff0000u));
+}
+__device__ inline float4 rounded(float4 v, const float*) { return v; }
+__device__ inline float4 add4(const float4& a, const float4& b) {
+    return make_float4(a.x + b.x, a.y + b.y, a.z + b.z, a.w + b.w);
+}
+__device__ inline float4 mul4(const float4& a, const float4& b) {
+    return make_float4(a.x * b.x, a.y * b.y, a.z * b.z, a.w * b.w);
+}
+__device__ inline float4 times(const float4& v, double f) {
+    return make_float4((float)((double)v.x * f), (float)((double)v.y * f), (float)((double)v.z * f), (float)((double)v.w * f));
+}
+__device__ inline void add_squares(double& q, const float4& v) {
+    q = fma((double)v.x, (double)v.x, q);
+    q = fma((double)v.y, (double)v.y, q);
+    q = fma((double)v.z, (double)v.z, q);
+    q = fma((double)v.w, (double)v.w, q);
+}
+__device__ inline float most4(float m, const float4& v) {
+    return fmaxf(m, fmaxf(fmaxf(fabsf(v.x), fabsf(v.y)), fmaxf(fabsf(v.z), fabsf(v.w))));
+}
+__device__ inline double rms_inverse(double mean_square, double eps) {
+    const double v = mean_square + eps;
+    return v > 0.0 ? rsqrt64(v) : 0.0;  // (a row of zeros with eps = 0)
+}
+// the largest of what the first pass left, in every lane; NW waves
+template <int NW>
+__device__ inline float tensor_most(const QuantRmsArgs& a, float* sm) {
+    float m = 0.f;
+    for (int i = threadIdx.x; i < a.groups; i += NW * kWave) m = fmaxf(m, a.most[i]);
+    return block_max<NW>(m, sm);
+}
+
+// WPR waves share a row, which lies in their registers (NV float4 a lane) from its one reading on; workgroups have four waves at
+// least, so short rows are handled several to a workgroup, without a barrier.  Bound by HBM for large batches, by the length of a
+// row's chain for small ones (one reduction without a gain: the largest |x^| is then that of the largest |h|).
+template <typename XT, typename RT, bool RES, int WPR, int NV>
+__global__ __launch_bounds__((WPR < 4 ? 4 : WPR) * kWave, 4) void quant_rms_rows(QuantRmsArgs a, int mode) {
+    constexpr int NW = WPR < 4 ? 4 : WPR, RPW = NW / WPR, LANES = WPR * kWave;
+    __shared__ double smd[NW];
+    __shared__ float smf[2][NW];
+    __shared__ int smi[NW];
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave), rw = wave / WPR, wr = wave % WPR;
+    const int t = wr * kWave + (threadIdx.x & (kWave - 1)), K4 = (int)(a.K / 4);
+    float gamma = 0.f, best = 0.f;
+    if (mode == kRmsApply) {
+        gamma = fmaxf(tensor_most<NW>(a, smf[0]), 1e-5f);
+        if (blockIdx.x == 0 && threadIdx.x == 0) *a.gamma = gamma;
+    }
+    for (int64_t row0 = (int64_t)blockIdx.x * RPW; row0 < a.M; row0 += (int64_t)gridDim.x * RPW) {
+        int64_t row = row0 + rw;
+        const bool live = row < a.M;
+        if (!live) {
+            if (WPR == 1) break;  // no barriers behind
+            row = a.M - 1;
+        }
+        if (mode == kRmsApply) row = a.M - 1 - row;
+        const XT* x = static_cast<const XT*>(a.X) + row * a.K;
+        const RT* r = RES ? static_cast<const RT*>(a.R) + row * a.K : nullptr;
+        float4 v[NV], u[RES ? NV : 1];
+        // unconditional (the last piece again past the row), so that all are in flight before the first is needed
+#pragma unroll
+        for (int j = 0; j < NV; ++j) v[j] = load4(x, t + j * LANES < K4 ? t + j * LANES : K4 - 1);
+        if constexpr (RES)
+#pragma unroll
+            for (int j = 0; j < NV; ++j) u[j] = load4(r, t + j * LANES < K4 ? t + j * LANES : K4 - 1);
+        double q = 0.0;
+        float m = 0.f;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            if constexpr (RES) v[j] = rounded(add4(v[j], u[j]), r);
+            if (K4 < (j + 1) * LANES && t + j * LANES >= K4) v[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (mode != kRmsApply) {
+                add_squares(q, v[j]);
+                m = most4(m, v[j]);
+            }
+        }
+        if constexpr (RES)
+            if (a.H && live) {
+                RT* h = static_cast<RT*>(a.H) + row * a.K;
+#pragma unroll
+                for (int j = 0; j < NV; ++j)
+                    if (t + j * LANES < K4) store4(h, t + j * LANES, v[j]);
+            }
+        double rstd;
+        if (mode == kRmsApply) {
+            rstd = a.rstd[row];
+        } else {
+            q = wave_reduce(q, OpSum{});
+            m = wave_reduce(m, OpMax{});
+            if constexpr (WPR > 1) {
+                if ((threadIdx.x & (kWave - 1)) == 0) {
+                    smd[wave] = q;
+                    smf[0][wave] = m;
+                }
+                __syncthreads();
+                q = fold_slots<WPR>(smd + rw * WPR, OpSum{});
+                m = fold_slots<WPR>(smf[0] + rw * WPR, OpMax{});
+            }
+            rstd = rms_inverse(q * a.inv_k, a.eps);
+            m = (float)((double)m * rstd);
+        }
+        // (hidden from the optimiser, which would keep the converted copies of all elements alive)
+        if constexpr (NV > 2)
+#pragma unroll
+            for (int j = 0; j < NV; ++j) asm volatile("" : "+v"(v[j].x), "+v"(v[j].y), "+v"(v[j].z), "+v"(v[j].w));
+        if (mode != kRmsStats || a.gain) {
+#pragma unroll
+            for (int j = 0; j < NV; ++j) v[j] = times(v[j], rstd);
+            if (a.gain) {
+                m = 0.f;
+#pragma unroll
+                for (int j = 0; j < NV; ++j) {
+                    v[j] = mul4(v[j], load4(a.gain, t + j * LANES < K4 ? t + j * LANES : K4 - 1));
+                    m = most4(m, v[j]);
+                }
+                if (mode != kRmsApply) m = row_reduce<WPR>(m, OpMax{}, smf[1], rw, wr);
+            }
+        }
+        if (mode == kRmsStats) {
+            best = fmaxf(best, m);  // (rows past the last one repeat it)
+            if (t == 0 && live) a.rstd[row] = rstd;
+            if (WPR > 1) __syncthreads();  // the slots are read
+            continue;
+        }
+        if (mode == kRmsFull) gamma = fmaxf(m, 1e-5f);
+        const float scale = 128.0f / gamma;
+        int rs = 0;
+        uint32_t* c4 = reinterpret_cast<uint32_t*>(a.codes + row * a.K);
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const int i = t + j * LANES;
+            const uint32_t w = code_word(v[j].x * scale, v[j].y * scale, v[j].z * scale, v[j].w * scale);
+            rs = __builtin_amdgcn_sdot4((int)w, 0x01010101, rs, false);  // (zeros past the row)
+            if (live && i < K4) {
+                c4[i] = w;
+                if (a.xhat) store4(a.xhat + row * a.K, i, v[j]);
+            }
+        }
+        if (a.rowsum) {
+            rs = row_reduce<WPR>(rs, OpSum{}, smi, rw, wr);
+            if (t == 0 && live) a.rowsum[row] = rs;
+        }
+        if (t == 0 && live && mode == kRmsFull) a.gamma[row] = gamma;
+        if (WPR > 1) __syncthreads();
+    }
+    if (mode == kRmsStats) {
+        __syncthreads();
+        best = block_max<NW>(best, smf[0]);
+        if (threadIdx.x == 0) a.most[blockIdx.x] = best;
+    }
+}
+
+// Rows past registers (K > 32768): a workgroup walks a row from memory once per step.
 template <typename XT, typename RT, bool RES>
 __global__ __launch_bounds__(512) void quant_rms_long(QuantRmsArgs a, int mode) {
     constexpr int NW = 8, T = NW * kWave;
@@ -22,21 +182,18 @@ __global__ __launch_bounds__(512) void quant_rms_long(QuantRmsArgs a, int mode) 
     __shared__ int smi[NW];
     const int t = threadIdx.x;
     const int64_t K4 = a.K / 4;
+    float gamma = 0.f, best = 0.f;
+    if (mode == kRmsApply) {
+        gamma = fmaxf(tensor_most<NW>(a, smf), 1e-5f);
+        if (blockIdx.x == 0 && t == 0) *a.gamma = gamma;
+    }
     for (int64_t row = blockIdx.x; row < a.M; row += gridDim.x) {
         const XT* x = static_cast<const XT*>(a.X) + row * a.K;
         const RT* r = RES ? static_cast<const RT*>(a.R) + row * a.K : nullptr;
         RT* h = RES && a.H ? static_cast<RT*>(a.H) + row * a.K : nullptr;
         auto sum_at = [&](int64_t i) {
-            float4 v = load4(x, i);
-            if constexpr (RES) {
-                const float4 u = load4(r, i);
-                v.x += u.x; v.y += u.y; v.z += u.z; v.w += u.w;
-                if constexpr (sizeof(RT) == 2) {
-                    const uint2 w = make_uint2(bf16_pair(v.x, v.y), bf16_pair(v.z, v.w));
-                    v = make_float4(__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xffff0000u),
-                                    __uint_as_float(w.y << 16), __uint_as_float(w.y & 0xffff0000u));
-                }
-            }
+            const float4 v = load4(x, i);
+            if constexpr (RES) return rounded(add4(v, load4(r, i)), r);
             return v;
         };
         double rstd;
@@ -44,43 +201,21 @@ __global__ __launch_bounds__(512) void quant_rms_long(QuantRmsArgs a, int mode) 
             rstd = a.rstd[row];
         } else {
             double q = 0.0;
-            for (int64_t i = t; i < K4; i += T) {
-                const float4 v = sum_at(i);
-                q = fma((double)v.x, (double)v.x, q);
-                q = fma((double)v.y, (double)v.y, q);
-                q = fma((double)v.z, (double)v.z, q);
-                q = fma((double)v.w, (double)v.w, q);
-            }
-            q = block_sum<NW>(q, smd) * a.inv_k + a.eps;
-            rstd = q > 0.0 ? rsqrt64(q) : 0.0;
+            for (int64_t i = t; i < K4; i += T) add_squares(q, sum_at(i));
+            rstd = rms_inverse(block_sum<NW>(q, smd) * a.inv_k, a.eps);
         }
-        // (h may be x or r: an element is read and written by the same thread, and not read there again)
-        auto hat_at = [&](float4 v, int64_t i) {
-            v.x = (float)((double)v.x * rstd);
-            v.y = (float)((double)v.y * rstd);
-            v.z = (float)((double)v.z * rstd);
-            v.w = (float)((double)v.w * rstd);
-            if (a.gain) {
-                const float4 g = load4(a.gain, i);
-                v.x *= g.x; v.y *= g.y; v.z *= g.z; v.w *= g.w;
-            }
-            return v;
+        auto hat = [&](const float4& v, int64_t i) {
+            const float4 o = times(v, rstd);
+            return a.gain ? mul4(o, load4(a.gain, i)) : o;
         };
-        float gamma;
-        if (mode == kRmsApply) {
-            gamma = *a.gamma;
-        } else {
+        // (h may be x or r: an element is read and written by the same thread, and not read there again)
+        if (mode != kRmsApply) {
             float m = 0.f;
-            for (int64_t i = t; i < K4; i += T) {
-                const float4 v = sum_at(i), o = hat_at(v, i);
-                m = fmaxf(m, fmaxf(fmaxf(fabsf(o.x), fabsf(o.y)), fmaxf(fabsf(o.z), fabsf(o.w))));
-            }
+            for (int64_t i = t; i < K4; i += T) m = most4(m, hat(sum_at(i), i));
             m = block_max<NW>(m, smf);
             if (mode == kRmsStats) {
-                if (t == 0) {
-                    a.rstd[row] = rstd;
-                    a.most[row] = m;
-                }
+                best = fmaxf(best, m);
+                if (t == 0) a.rstd[row] = rstd;
                 if (h)
                     for (int64_t i = t; i < K4; i += T) store4(h, i, sum_at(i));
                 __syncthreads();  // the slots of the reductions are read
@@ -92,7 +227,7 @@ __global__ __launch_bounds__(512) void quant_rms_long(QuantRmsArgs a, int mode) 
         uint32_t* c4 = reinterpret_cast<uint32_t*>(a.codes + row * a.K);
         int rs = 0;
         for (int64_t i = t; i < K4; i += T) {
-            const float4 v = sum_at(i), o = hat_at(v, i);
+            const float4 v = sum_at(i), o = hat(v, i);
             if (h) store4(h, i, v);
             if (a.xhat) store4(a.xhat + row * a.K, i, o);
             const uint32_t w = code_word(o.x * scale, o.y * scale, o.z * scale, o.w * scale);
@@ -106,97 +241,216 @@ __global__ __launch_bounds__(512) void quant_rms_long(QuantRmsArgs a, int mode) 
         if (t == 0 && mode == kRmsFull) a.gamma[row] = gamma;
         __syncthreads();
     }
+    if (mode == kRmsStats && t == 0) a.most[blockIdx.x] = best;
 }
 
-// gamma of the tensor from the rows' largest values
-__global__ __launch_bounds__(1024) void fold_most(const float* __restrict__ most, int64_t M, float* __restrict__ gamma) {
-    constexpr int NW = 16;
-    __shared__ float sm[NW];
-    float m = 0.f;
-    for (int64_t i = threadIdx.x; i < M; i += 1024) m = fmaxf(m, most[i]);
-    m = block_max<NW>(m, sm);
-    if (threadIdx.x == 0) *gamma = fmaxf(m, 1e-5f);
+// Waves a row and float4 a lane: up to eight float4; more waves where the batch alone would leave SIMDs idle.
+struct RmsShape {
+    int wpr, nv;
+};
+static RmsShape rms_shape(int64_t M, int64_t K) {
+    const int64_t K4 = K / 4;
+    int wpr = 1;
+    while (wpr < 16 && K4 > (int64_t)wpr * kWave * 8) wpr *= 4;
+    while (wpr < 16 && M * wpr < 1024 && K4 >= (int64_t)wpr * kWave * 4) wpr *= 4;
+    if (wpr > 16) wpr = 16;
+    const int64_t per_lane = (K4 + wpr * kWave - 1) / (wpr * kWave);
+    int nv = 1;
+    while (nv < per_lane) nv *= 2;
+    return {wpr, nv};
+}
+static unsigned rms_groups(int64_t M, int rpw) {
+    const int64_t g = (M + rpw - 1) / rpw;
+    return (unsigned)(g < kRmsGroups ? g : kRmsGroups);
 }
 
 template <typename XT, typename RT, bool RES>
-static void launch_rms_typed(const QuantRmsArgs& a, int mode, hipStream_t s) {
-    const unsigned grid = (unsigned)(a.M < (1 << 20) ? a.M : (1 << 20));
-    quant_rms_long<XT, RT, RES><<<grid, 512, 0, s>>>(a, mode);
-}
-static void launch_rms(const QuantRmsArgs& a, int mode, hipStream_t s) {
-    if (!a.R) {
-        if (a.x_bf16) launch_rms_typed<uint16_t, uint16_t, false>(a, mode, s);
-        else launch_rms_typed<float, float, false>(a, mode, s);
-    } else if (a.x_bf16) {
-        if (a.h_bf16) launch_rms_typed<uint16_t, uint16_t, true>(a, mode, s);
-        else launch_rms_typed<uint16_t, float, true>(a, mode, s);
-    } else {
-        if (a.h_bf16) launch_rms_typed<float, uint16_t, true>(a, mode, s);
-        else launch_rms_typed<float, float, true>(a, mode, s);
+static int launch_rms_typed(const QuantRmsArgs& a, int mode, hipStream_t s) {
+    if (a.K > 32768) {
+        const unsigned grid = rms_groups(a.M, 1);
+        quant_rms_long<XT, RT, RES><<<grid, 512, 0, s>>>(a, mode);
+        return (int)grid;
     }
+    const RmsShape sh = rms_shape(a.M, a.K);
+    const int nw = sh.wpr < 4 ? 4 : sh.wpr, rpw = nw / sh.wpr;
+    const int64_t wgs = (a.M + rpw - 1) / rpw;
+    const unsigned grid = mode == kRmsFull ? (unsigned)(wgs < (1 << 20) ? wgs : (1 << 20)) : rms_groups(a.M, rpw);
+#define BL_RMS_CASE(W, V) \
+    if (sh.wpr == W && sh.nv == V) quant_rms_rows<XT, RT, RES, W, V><<<grid, nw * kWave, 0, s>>>(a, mode); else
+    BL_RMS_CASE(1, 1) BL_RMS_CASE(1, 2) BL_RMS_CASE(1, 4) BL_RMS_CASE(1, 8)
+    BL_RMS_CASE(4, 1) BL_RMS_CASE(4, 2) BL_RMS_CASE(4, 4) BL_RMS_CASE(4, 8)
+    BL_RMS_CASE(16, 1) BL_RMS_CASE(16, 2) BL_RMS_CASE(16, 4) BL_RMS_CASE(16, 8)
+    return -1;
+#undef BL_RMS_CASE
+    return (int)grid;
+}
+static int launch_rms(const QuantRmsArgs& a, int mode, hipStream_t s) {
+    if (!a.R)
+        return a.x_bf16 ? launch_rms_typed<uint16_t, uint16_t, false>(a, mode, s)
+                        : launch_rms_typed<float, float, false>(a, mode, s);
+    if (a.x_bf16)
+        return a.h_bf16 ? launch_rms_typed<uint16_t, uint16_t, true>(a, mode, s)
+                        : launch_rms_typed<uint16_t, float, true>(a, mode, s);
+    return a.h_bf16 ? launch_rms_typed<float, uint16_t, true>(a, mode, s) : launch_rms_typed<float, float, true>(a, mode, s);
 }
 
 hipError_t launch_quant_rmsnorm(const QuantRmsArgs& a_in, hipStream_t s) {
     QuantRmsArgs a = a_in;
     a.inv_k = 1.0 / (double)a.K;
-    if (!a.per_tensor) {
-        launch_rms(a, kRmsFull, s);
-        return hipGetLastError();
-    }
-    launch_rms(a, kRmsStats, s);
-    fold_most<<<1, 1024, 0, s>>>(a.most, a.M, a.gamma);
+    if (!a.per_tensor) return launch_rms(a, kRmsFull, s) < 0 ? hipErrorInvalidValue : hipGetLastError();
+    a.groups = launch_rms(a, kRmsStats, s);
     if (a.R && a.H) {  // x + r is there now
         a.X = a.H;
         a.x_bf16 = a.h_bf16;
         a.R = nullptr;
         a.H = nullptr;
     }
-    launch_rms(a, kRmsApply, s);
-    return hipGetLastError();
+    return a.groups < 0 || launch_rms(a, kRmsApply, s) < 0 ? hipErrorInvalidValue : hipGetLastError();
 }
 
 // ---- backward -----------------------------------------------------------------------------------------
-// Workgroup b takes rows b, b + groups, ...; a thread has the same columns of all of them, so their share of dgain is
-// summed where only it writes.
-int rms_backward_groups(int64_t M, int64_t K) {
-    (void)K;
-    return (int)(M < 256 ? M : 256);
+// The workgroups are as many as fill the chip and go through the rows; a lane has the same columns of all its rows, so that
+// their share of dgain is summed (fp64) in its registers, and each workgroup leaves one sum a column for fold_dgain.  A row is
+// read once.
+// Rows past registers take half the workgroups and 64 bits.
+constexpr int64_t kRmsBackwardK = 16384;
+static int rms_backward_groups(int64_t M, int64_t K) {
+    const int64_t most = K > kRmsBackwardK ? 256 : 512;
+    return (int)(M < most ? M : most);
 }
+size_t rms_backward_part_bytes(int64_t M, int64_t K) {
+    return (size_t)rms_backward_groups(M, K) * (size_t)K * (K > kRmsBackwardK ? 8 : 4);
+}
+template <typename GT, typename HT, typename DT, int WPR, int NV>
+__global__ __launch_bounds__((WPR < 8 ? 8 : WPR) * kWave, 4) void rms_backward_rows(RmsBackwardArgs a) {
+    constexpr int NW = WPR < 8 ? 8 : WPR, RPW = NW / WPR, LANES = WPR * kWave;
+    __shared__ double smd[2][2][NW];
+    __shared__ float smg[RPW > 1 ? RPW - 1 : 1][NV][LANES][4];
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave), rw = wave / WPR, wr = wave % WPR;
+    const int t = wr * kWave + (threadIdx.x & (kWave - 1)), K4 = (int)(a.K / 4);
+    double dg[NV][4];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) dg[j][0] = dg[j][1] = dg[j][2] = dg[j][3] = 0.0;
+    int parity = 0;
+    for (int64_t row0 = (int64_t)blockIdx.x * RPW; row0 < a.M; row0 += (int64_t)gridDim.x * RPW) {
+        int64_t row = row0 + rw;
+        const bool live = row < a.M;
+        if (!live) {
+            if (WPR == 1) break;  // no barriers behind
+            row = a.M - 1;
+        }
+        const GT* g = static_cast<const GT*>(a.G) + row * a.K;
+        const HT* h = static_cast<const HT*>(a.H) + row * a.K;
+        const DT* dr = a.dR ? static_cast<const DT*>(a.dR) + row * a.K : nullptr;
+        float4 v[NV], u[NV], w[NV];
+#pragma unroll
+        for (int j = 0; j < NV; ++j) v[j] = load4(h, t + j * LANES < K4 ? t + j * LANES : K4 - 1);
+#pragma unroll
+        for (int j = 0; j < NV; ++j) u[j] = load4(g, t + j * LANES < K4 ? t + j * LANES : K4 - 1);
+        if (dr)
+#pragma unroll
+            for (int j = 0; j < NV; ++j) w[j] = load4(dr, t + j * LANES < K4 ? t + j * LANES : K4 - 1);
+        else
+#pragma unroll
+            for (int j = 0; j < NV; ++j) w[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+        double q = 0.0, c = 0.0;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            if (K4 < (j + 1) * LANES && t + j * LANES >= K4) v[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+            const float4 s = a.gain ? mul4(u[j], load4(a.gain, t + j * LANES < K4 ? t + j * LANES : K4 - 1)) : u[j];
+            add_squares(q, v[j]);
+            c = fma((double)v[j].x, (double)s.x, c);
+            c = fma((double)v[j].y, (double)s.y, c);
+            c = fma((double)v[j].z, (double)s.z, c);
+            c = fma((double)v[j].w, (double)s.w, c);
+        }
+        q = wave_reduce(q, OpSum{});
+        c = wave_reduce(c, OpSum{});
+        if constexpr (WPR > 1) {
+            if ((threadIdx.x & (kWave - 1)) == 0) {
+                smd[parity][0][wave] = q;
+                smd[parity][1][wave] = c;
+            }
+            __syncthreads();
+            q = fold_slots<WPR>(smd[parity][0] + rw * WPR, OpSum{});
+            c = fold_slots<WPR>(smd[parity][1] + rw * WPR, OpSum{});
+            parity ^= 1;  // read before the barrier of the next row, written behind it
+        }
+        const double rstd = rms_inverse(q * a.inv_k, a.eps);
+        const float inv = (float)rstd, along = (float)(c * a.inv_k * rstd * rstd);  // mean(t n) / rms
+        // (hidden from the optimiser, which would keep the converted copies of all elements alive)
+#pragma unroll
+        for (int j = 0; j < NV; ++j) asm volatile("" : "+v"(v[j].x), "+v"(v[j].y), "+v"(v[j].z), "+v"(v[j].w));
+        DT* dh = static_cast<DT*>(a.dH) + row * a.K;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const int i = t + j * LANES;
+            if (i < K4 && live) {
+                const float4 s = a.gain ? mul4(u[j], load4(a.gain, i)) : u[j];
+                float4 d;
+                d.x = (s.x - v[j].x * along) * inv + w[j].x;
+                d.y = (s.y - v[j].y * along) * inv + w[j].y;
+                d.z = (s.z - v[j].z * along) * inv + w[j].z;
+                d.w = (s.w - v[j].w * along) * inv + w[j].w;
+                store4(dh, i, d);
+                if (a.dgain) {
+                    dg[j][0] = fma((double)(u[j].x * v[j].x), rstd, dg[j][0]);
+                    dg[j][1] = fma((double)(u[j].y * v[j].y), rstd, dg[j][1]);
+                    dg[j][2] = fma((double)(u[j].z * v[j].z), rstd, dg[j][2]);
+                    dg[j][3] = fma((double)(u[j].w * v[j].w), rstd, dg[j][3]);
+                }
+            }
+        }
+    }
+    if (!a.dgain) return;
+    // the rows of the workgroup's waves together
+    if constexpr (RPW > 1) {
+        if (rw > 0)
+#pragma unroll
+            for (int j = 0; j < NV; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) smg[rw - 1][j][t][e] = (float)dg[j][e];
+        __syncthreads();
+        if (rw > 0) return;
+#pragma unroll
+        for (int p = 0; p < RPW - 1; ++p)
+#pragma unroll
+            for (int j = 0; j < NV; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) dg[j][e] += (double)smg[p][j][t][e];
+    }
+    float* part = static_cast<float*>(a.partials) + (int64_t)blockIdx.x * a.K;
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+        if (t + j * LANES < K4)
+            store4(part, t + j * LANES, make_float4((float)dg[j][0], (float)dg[j][1], (float)dg[j][2], (float)dg[j][3]));
+}
+
+// Rows past registers: each is walked twice, and the columns' sums (fp64) lie in memory, where only one thread writes them.
 template <typename GT, typename HT, typename DT>
 __global__ __launch_bounds__(512) void rms_backward_long(RmsBackwardArgs a) {
     constexpr int NW = 8, T = NW * kWave;
     __shared__ double smd[2][NW];
     const int t = threadIdx.x;
     const int64_t K4 = a.K / 4;
-    double* const part = a.dgain ? a.partials + (int64_t)blockIdx.x * a.K : nullptr;
+    double* const part = a.dgain ? static_cast<double*>(a.partials) + (int64_t)blockIdx.x * a.K : nullptr;
     for (int64_t row = blockIdx.x; row < a.M; row += gridDim.x) {
         const GT* g = static_cast<const GT*>(a.G) + row * a.K;
         const HT* h = static_cast<const HT*>(a.H) + row * a.K;
         const DT* dr = a.dR ? static_cast<const DT*>(a.dR) + row * a.K : nullptr;
         DT* dh = static_cast<DT*>(a.dH) + row * a.K;
-        auto scaled = [&](float4 v, int64_t i) {
-            if (a.gain) {
-                const float4 w = load4(a.gain, i);
-                v.x *= w.x; v.y *= w.y; v.z *= w.z; v.w *= w.w;
-            }
-            return v;
-        };
+        auto scaled = [&](const float4& v, int64_t i) { return a.gain ? mul4(v, load4(a.gain, i)) : v; };
         double q = 0.0, c = 0.0;
         for (int64_t i = t; i < K4; i += T) {
             const float4 v = load4(h, i), u = scaled(load4(g, i), i);
-            q = fma((double)v.x, (double)v.x, q);
-            q = fma((double)v.y, (double)v.y, q);
-            q = fma((double)v.z, (double)v.z, q);
-            q = fma((double)v.w, (double)v.w, q);
+            add_squares(q, v);
             c = fma((double)v.x, (double)u.x, c);
             c = fma((double)v.y, (double)u.y, c);
             c = fma((double)v.z, (double)u.z, c);
             c = fma((double)v.w, (double)u.w, c);
         }
-        q = block_sum<NW>(q, smd[0]) * a.inv_k + a.eps;
-        c = block_sum<NW>(c, smd[1]) * a.inv_k;
-        const double rstd = q > 0.0 ? rsqrt64(q) : 0.0;
-        const double along = c * rstd * rstd;  // mean(t n) / rms
+        const double rstd = rms_inverse(block_sum<NW>(q, smd[0]) * a.inv_k, a.eps);
+        const double along = block_sum<NW>(c, smd[1]) * a.inv_k * rstd * rstd;  // mean(t n) / rms
         for (int64_t i = t; i < K4; i += T) {
             const float4 v = load4(h, i), u0 = load4(g, i), u = scaled(u0, i);
             double d[4] = {((double)u.x - (double)v.x * along) * rstd, ((double)u.y - (double)v.y * along) * rstd,
@@ -218,34 +472,67 @@ __global__ __launch_bounds__(512) void rms_backward_long(RmsBackwardArgs a) {
         __syncthreads();
     }
 }
-__global__ __launch_bounds__(256) void fold_dgain(const double* __restrict__ part, int groups, int64_t K,
-                                                  float* __restrict__ dgain) {
-    for (int64_t k = (int64_t)blockIdx.x * 256 + threadIdx.x; k < K; k += (int64_t)gridDim.x * 256) {
+// 32 columns a workgroup, the groups' sums dealt to 32 lanes of each
+template <typename PT>
+__global__ __launch_bounds__(1024) void fold_dgain(const PT* __restrict__ part, int groups, int64_t K,
+                                                   float* __restrict__ dgain) {
+    __shared__ double sm[32][33];
+    const int c = threadIdx.x & 31, p = threadIdx.x >> 5;
+    for (int64_t k0 = (int64_t)blockIdx.x * 32; k0 < K; k0 += (int64_t)gridDim.x * 32) {
         double s = 0.0;
-        for (int b = 0; b < groups; ++b) s += part[b * K + k];
-        dgain[k] = (float)s;
+#pragma unroll 4
+        for (int b = p; b < groups; b += 32) s += (double)part[b * K + k0 + c];
+        sm[p][c] = s;
+        __syncthreads();
+        if (p == 0) {
+#pragma unroll
+            for (int i = 1; i < 32; ++i) s += sm[i][c];
+            dgain[k0 + c] = (float)s;
+        }
+        __syncthreads();
     }
 }
 
+template <typename GT, typename HT, typename DT>
+static int launch_rms_backward_typed(const RmsBackwardArgs& a, hipStream_t s) {
+    if (a.K > kRmsBackwardK) {
+        const int grid = rms_backward_groups(a.M, a.K);
+        rms_backward_long<GT, HT, DT><<<(unsigned)grid, 512, 0, s>>>(a);
+        return grid;
+    }
+    // two float4 a lane as long as eight waves hold a row so, then four
+    const int64_t K4 = a.K / 4;
+    int wpr = 1;
+    while (wpr < 8 && K4 > (int64_t)wpr * kWave * 2) wpr *= 2;
+    if (K4 > 8 * kWave * 4) wpr = 16;
+    const int nv = K4 <= kWave ? 1 : K4 <= (int64_t)wpr * kWave * 2 ? 2 : 4;
+    const int rpw = wpr < 8 ? 8 / wpr : 1, threads = wpr < 8 ? 512 : wpr * kWave;
+    const int64_t wgs = (a.M + rpw - 1) / rpw;
+    const int most = rms_backward_groups(a.M, a.K), grid = (int)(wgs < most ? wgs : most);
+#define BL_RMS_CASE(W, V) \
+    if (wpr == W && nv == V) rms_backward_rows<GT, HT, DT, W, V><<<(unsigned)grid, threads, 0, s>>>(a); else
+    BL_RMS_CASE(1, 1) BL_RMS_CASE(1, 2) BL_RMS_CASE(2, 2) BL_RMS_CASE(4, 2) BL_RMS_CASE(8, 2) BL_RMS_CASE(8, 4)
+    BL_RMS_CASE(16, 4) return -1;
+#undef BL_RMS_CASE
+    return grid;
+}
 template <typename GT, typename HT>
-static void launch_rms_backward_typed(const RmsBackwardArgs& a, unsigned grid, hipStream_t s) {
-    if (a.d_bf16) rms_backward_long<GT, HT, uint16_t><<<grid, 512, 0, s>>>(a);
-    else rms_backward_long<GT, HT, float><<<grid, 512, 0, s>>>(a);
+static int launch_rms_backward(const RmsBackwardArgs& a, hipStream_t s) {
+    return a.d_bf16 ? launch_rms_backward_typed<GT, HT, uint16_t>(a, s) : launch_rms_backward_typed<GT, HT, float>(a, s);
 }
 hipError_t launch_rmsnorm_backward(const RmsBackwardArgs& a_in, hipStream_t s) {
     RmsBackwardArgs a = a_in;
     a.inv_k = 1.0 / (double)a.K;
-    const unsigned grid = (unsigned)rms_backward_groups(a.M, a.K);
-    if (a.g_bf16) {
-        if (a.h_bf16) launch_rms_backward_typed<uint16_t, uint16_t>(a, grid, s);
-        else launch_rms_backward_typed<uint16_t, float>(a, grid, s);
-    } else {
-        if (a.h_bf16) launch_rms_backward_typed<float, uint16_t>(a, grid, s);
-        else launch_rms_backward_typed<float, float>(a, grid, s);
-    }
+    const int groups = a.g_bf16 ? a.h_bf16 ? launch_rms_backward<uint16_t, uint16_t>(a, s)
+                                           : launch_rms_backward<uint16_t, float>(a, s)
+                     : a.h_bf16 ? launch_rms_backward<float, uint16_t>(a, s)
+                                : launch_rms_backward<float, float>(a, s);
+    if (groups < 0) return hipErrorInvalidValue;
     if (a.dgain) {
-        const int64_t wgs = (a.K + 255) / 256;
-        fold_dgain<<<(unsigned)(wgs < 65536 ? wgs : 65536), 256, 0, s>>>(a.partials, (int)grid, a.K, a.dgain);
+        const int64_t wgs = a.K / 32;
+        const unsigned grid = (unsigned)(wgs < 65536 ? wgs : 65536);
+        if (a.K > kRmsBackwardK) fold_dgain<<<grid, 1024, 0, s>>>(static_cast<const double*>(a.partials), groups, a.K, a.dgain);
+        else fold_dgain<<<grid, 1024, 0, s>>>(static_cast<const float*>(a.partials), groups, a.K, a.dgain);
     }
     return hipGetLastError();
 }
