@@ -489,8 +489,8 @@ int bitlinear_matmul_i8(const int8_t* codes, const float* gamma, int64_t M, int6
  *   dX[m,k] = sum_n (dY[m,n] * scale[n]) w[n,k]    [M,K] of dx_type, or NULL
  *   dW[n,k] = sum_m dY[m,n] (codes[m,k] * gamma_m / 128)    fp32 [N,K], or NULL
  *   dY   in  [M,N] of dy_type
- * bf16 operands, fp32 sums: dY * scale is rounded to bf16 for dX; for dW dY is (a bf16 dY is exact), or with a gamma per
- * token dY * gamma_m / 128.  The codes are exact. */
+ * bf16 operands, fp32 sums; what is rounded is rounded once: for dX the weights' values code * scale with a bf16 dY, dY * scale
+ * with an fp32 one; for dW dY (a bf16 dY is exact), or with a gamma per token dY * gamma_m / 128.  The codes are exact. */
 int bitlinear_backward_ste_i8(const void* dY, int dy_type, int64_t M, int64_t N, int64_t K, const int8_t* codes,
                               const float* gamma, int granularity, const void* packed, const float* scale,
                               void* dX, int dx_type, float* dW, void* workspace, size_t workspace_bytes,

@@ -1,10 +1,12 @@
 // Straight-through backward of the 8-bit product (rounding is identity, the scales are constants):
 //   dX[M,K] = (dY * scale) W            dW[N,K] = dY^T (q * gamma / 128)
-// on the bf16 product of backward.hip, C[I][J] = sum_r A[I][r] B[J][r]: int8 codes of either operand are exact in bf16, dY is
-// rounded once, with the factor that belongs to the reduction index (scale_n for dX; gamma_m / 128 for dW where gamma is
-// per token).  The operands are copied first into that product's layout (blocks of 32 reduction indices, padded with zeros):
-//   g   [M][Np]  dY * scale       (A of dX)       wT [K][Np]  weights transposed  (B of dX)
-//   gwT [N][Mp]  dY transposed    (A of dW)       qT [K][Mp]  codes transposed    (B of dW)
+// on the bf16 product of backward.hip, C[I][J] = sum_r A[I][r] B[J][r].  int8 codes are exact in bf16, and what is rounded is
+// rounded once: of a bf16 dY the weights' values code * scale (dX), of an fp32 dY the product dY * scale; for dW dY, with
+// gamma_m / 128 where gamma is per token (exact for a bf16 dY and one gamma a tensor).  The operands are copied into that product's
+// layout (blocks of 32 reduction indices, padded with zeros):
+//   wT [K][Np]  weights transposed     (B of dX)      qT [K][Mp]  codes transposed   (B of dW)
+//   g   [M][Np]  dY                     (A of dX)      gwT [N][Mp]  dY transposed      (A of dW)
+// g is not made where the product can read a bf16 dY as it lies (N a multiple of 32).
 #include "common.h"
 #include "i8.h"
 #include "kernels.h"
@@ -16,73 +18,146 @@ static inline int64_t pad32(int64_t v) { return (v + 31) / 32 * 32; }
 __device__ inline int64_t copy_offset(int64_t row, int64_t r, int64_t R) { return ((r >> 5) * R + row) * 32 + (r & 31); }
 __device__ inline float element(const float* p, int64_t i) { return p[i]; }
 __device__ inline float element(const uint16_t* p, int64_t i) { return __uint_as_float((uint32_t)p[i] << 16); }
-__device__ inline float element(const int8_t* p, int64_t i) { return (float)p[i]; }
 
-// in[R][C] -> rows[R][Cp] = bf16(in * col_scale) and tr[C][Rp] = bf16(in * row_gamma / 128), either null: tiles of 64 x 64
-template <typename IN>
-__global__ __launch_bounds__(256) void copy_operand(const IN* __restrict__ in, int64_t R, int64_t C,
-                                                    const float* __restrict__ col_scale,
-                                                    const float* __restrict__ row_gamma, uint16_t* __restrict__ rows,
-                                                    uint16_t* __restrict__ tr, int64_t tiles_c, int64_t items) {
-    __shared__ uint16_t tile[64][66];
-    const int64_t Cp = (C + 31) / 32 * 32, Rp = (R + 31) / 32 * 32;
-    for (int64_t it = blockIdx.x; it < items; it += gridDim.x) {
-        const int64_t r0 = it / tiles_c * 64, c0 = it % tiles_c * 64;
-        __syncthreads();
-        for (int e = threadIdx.x; e < 64 * 64; e += 256) {
-            const int64_t r = r0 + e / 64, c = c0 + e % 64;
-            const float v = r < R && c < C ? element(in, r * C + c) : 0.f;
-            if (rows && r < R && c < Cp)
-                rows[copy_offset(r, c, R)] = (uint16_t)bf16_pair(col_scale && c < C ? v * col_scale[c] : v, 0.f);
-            tile[e / 64][e % 64] = (uint16_t)bf16_pair(row_gamma && r < R ? v * (row_gamma[r] / 128.0f) : v, 0.f);
-        }
-        __syncthreads();
-        if (!tr) continue;
-        for (int e = threadIdx.x; e < 64 * 64; e += 256) {
-            const int64_t c = c0 + e / 64, r = r0 + e % 64;
-            if (c < C && r < Rp) tr[copy_offset(c, r, C)] = tile[e % 64][e / 64];
-        }
+struct CopyI8Args {
+    const void* dY;
+    const int8_t* codes;
+    const uint8_t* packed;
+    const float* w_scale;    // of the weights' values, or null: the codes
+    const float* col_scale;  // of g, or null
+    const float* row_gamma;  // of gwT, or null
+    uint16_t *wT, *qT, *g, *gwT;  // what is not wanted is null
+    int64_t M, N, K, Np, Mp;
+    uint32_t w_items, q_items, items, k_x, dy_x;  // items of the weights, of the codes, of all; in a row of them, of dY
+};
+
+// Bytes of 32 rows x 256 columns -> the transposed copy, 64 bytes a column.  A thread takes four columns of eight rows as
+// dwords.  LDS rows are 272 bytes.
+typedef uint8_t ByteTile[32][272];
+__device__ inline void transpose_bytes(const ByteTile& tile, uint16_t* __restrict__ out, int64_t r0, int64_t k0, int64_t K,
+                                       const float (&scale)[8]) {
+    const int rg = (int)threadIdx.x & 3, kq = (int)threadIdx.x >> 2;
+    if (k0 + 4 * kq >= K) return;  // K % 32 == 0
+    uint32_t w[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w[i] = *reinterpret_cast<const uint32_t*>(&tile[8 * rg + i][4 * kq]);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        uint32_t o[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            o[i] = bf16_pair((float)(int8_t)(w[2 * i] >> (8 * j)) * scale[2 * i],
+                             (float)(int8_t)(w[2 * i + 1] >> (8 * j)) * scale[2 * i + 1]);
+        *reinterpret_cast<uint4*>(out + copy_offset(k0 + 4 * kq + j, r0 + 8 * rg, K)) = make_uint4(o[0], o[1], o[2], o[3]);
     }
 }
-template <typename IN>
-static void launch_copy(const IN* in, int64_t R, int64_t C, const float* col_scale, const float* row_gamma,
-                        uint16_t* rows, uint16_t* tr, hipStream_t s) {
-    const int64_t tc = (C + 63) / 64, items = tc * ((R + 63) / 64);
-    copy_operand<IN><<<(unsigned)(items < (1 << 20) ? items : (1 << 20)), 256, 0, s>>>(in, R, C, col_scale, row_gamma, rows,
-                                                                                   tr, tc, items);
-}
-// tiles of the blob -> wT[K][Np]: a workgroup takes 32 rows x 64 columns
-__global__ __launch_bounds__(256) void copy_weights(const uint8_t* __restrict__ packed, int64_t N, int64_t K,
-                                                    uint16_t* __restrict__ wT, int64_t items) {
-    __shared__ uint8_t sm[2][1024];
-    const int64_t TN = tiles_n(N), TK = i8_tiles_k(K);
-    for (int64_t it = blockIdx.x; it < items; it += gridDim.x) {
-        const int64_t nb = it / TK, tk = it % TK;
-        __syncthreads();
-        for (int e = threadIdx.x; e < 512; e += 256) {
-            const int t = e / 256;
-            const uint32_t v = 2 * nb + t < TN
-                ? reinterpret_cast<const uint32_t*>(packed + ((2 * nb + t) * TK + tk) * 1024)[e % 256] : 0u;
-            reinterpret_cast<uint32_t*>(sm[t])[e % 256] = v;
+
+// dY -> g and gwT: 64 x 64, a thread's 4 x 4 elements loaded before the first is used.  VEC: four elements are one load.
+typedef uint16_t HalfTile[64][66];
+template <typename IN, bool VEC>
+__device__ inline void copy_dy(const CopyI8Args& a, int64_t r0, int64_t c0, HalfTile& tile) {
+    const IN* const in = static_cast<const IN*>(a.dY);
+    const int cl = ((int)threadIdx.x & 15) * 4;
+    const int64_t c = c0 + cl, R = a.M, C = a.N;
+    float v[4][4], gamma[4];
+#pragma unroll
+    for (int it = 0; it < 4; ++it) {
+        const int64_t r = r0 + it * 16 + ((int)threadIdx.x >> 4), at = r < R ? r : R - 1;
+        if constexpr (VEC) {
+            const float4 t = load4(in + at * C, (c < C ? c : C - 4) / 4);
+            v[it][0] = t.x, v[it][1] = t.y, v[it][2] = t.z, v[it][3] = t.w;
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[it][e] = element(in, at * C + (c + e < C ? c + e : C - 1));
         }
-        __syncthreads();
-        for (int e = threadIdx.x; e < 64 * 32; e += 256) {
-            const int kl = e / 32, n = e % 32;
-            const int64_t k = tk * 64 + kl;
-            if (k >= K) continue;
-            const int8_t v = (int8_t)sm[n / 16][(kl / 16) * 256 + (n % 16) * 16 + kl % 16];
-            wT[copy_offset(k, nb * 32 + n, K)] = (uint16_t)bf16_pair((float)v, 0.f);
-        }
+        gamma[it] = a.row_gamma ? a.row_gamma[at] * (1.0f / 128.0f) : 1.0f;  // uniform
+    }
+    float sc[4] = {1.0f, 1.0f, 1.0f, 1.0f};
+    if (a.col_scale)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sc[e] = a.col_scale[c + e < C ? c + e : C - 1];
+#pragma unroll
+    for (int it = 0; it < 4; ++it) {
+        const int rl = it * 16 + ((int)threadIdx.x >> 4);
+        const int64_t r = r0 + rl;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[it][e] = r < R && c + e < C ? v[it][e] : 0.f;
+        if (a.g && r < R && c < a.Np)
+            *reinterpret_cast<uint2*>(a.g + copy_offset(r, c, R)) =
+                make_uint2(bf16_pair(v[it][0] * sc[0], v[it][1] * sc[1]), bf16_pair(v[it][2] * sc[2], v[it][3] * sc[3]));
+        uint32_t* t32 = reinterpret_cast<uint32_t*>(&tile[rl][cl]);
+        t32[0] = bf16_pair(v[it][0] * gamma[it], v[it][1] * gamma[it]);
+        t32[1] = bf16_pair(v[it][2] * gamma[it], v[it][3] * gamma[it]);
+    }
+    if (!a.gwT) return;
+    __syncthreads();
+#pragma unroll
+    for (int it = 0; it < 4; ++it) {
+        const int idx = it * 256 + (int)threadIdx.x, col = idx >> 4, rl = (idx & 15) * 4;
+        if (c0 + col < C && r0 + rl < a.Mp)
+            *reinterpret_cast<uint2*>(a.gwT + copy_offset(c0 + col, r0 + rl, C)) =
+                make_uint2((uint32_t)tile[rl][col] | ((uint32_t)tile[rl + 1][col] << 16),
+                           (uint32_t)tile[rl + 2][col] | ((uint32_t)tile[rl + 3][col] << 16));
     }
 }
-__global__ __launch_bounds__(256) void round_to_bf16(const float* __restrict__ in, uint16_t* __restrict__ out, int64_t n4) {
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n4; i += (int64_t)gridDim.x * 256)
-        store4(out, i, load4(in, i));
+
+// All of it in one launch, the small parts first (behind dY they would be the tail).
+template <typename IN, bool VEC>
+__global__ __launch_bounds__(256) void copy_i8_operands(CopyI8Args a) {
+    __shared__ __attribute__((aligned(16))) union {
+        ByteTile bytes;
+        HalfTile halves;
+    } sm;
+    const int tid = (int)threadIdx.x;
+    for (uint32_t it = blockIdx.x; it < a.items; it += gridDim.x) {
+        if (it != blockIdx.x) __syncthreads();  // the item before has been read
+        uint32_t i = it;
+        if (i < a.w_items) {  // 32 channels x 256 k: tiles of 16 x 64
+            const int64_t nb = i / a.k_x, k0 = (int64_t)(i % a.k_x) * 256, TK = i8_tiles_k(a.K), TN = tiles_n(a.N);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int64_t tn = 2 * nb + h, tk = k0 / 64 + tid / 64;
+                uint4 v = make_uint4(0, 0, 0, 0);
+                if (tn < TN && tk < TK) v = *reinterpret_cast<const uint4*>(a.packed + (tn * TK + tk) * 1024 + (tid & 63) * 16);
+                *reinterpret_cast<uint4*>(&sm.bytes[16 * h + (tid & 15)][tid / 64 * 64 + (tid >> 4 & 3) * 16]) = v;
+            }
+            float sc[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int64_t n = nb * 32 + 8 * (tid & 3) + e;
+                sc[e] = a.w_scale ? a.w_scale[n < a.N ? n : a.N - 1] : 1.0f;  // (zeros past N)
+            }
+            __syncthreads();
+            transpose_bytes(sm.bytes, a.wT, nb * 32, k0, a.K, sc);
+            continue;
+        }
+        i -= a.w_items;
+        if (i < a.q_items) {  // 32 tokens x 256 k
+            const int64_t mb = i / a.k_x, k0 = (int64_t)(i % a.k_x) * 256;
+            const int64_t m = mb * 32 + tid / 8;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int kl = (tid & 7) * 16 + h * 128;
+                uint4 v = make_uint4(0, 0, 0, 0);
+                if (m < a.M && k0 + kl < a.K) v = *reinterpret_cast<const uint4*>(a.codes + m * a.K + k0 + kl);
+                *reinterpret_cast<uint4*>(&sm.bytes[tid / 8][kl]) = v;
+            }
+            __syncthreads();
+            const float one[8] = {1.0f, 1.0f, 1.0f, 1.0f, 1.0f, 1.0f, 1.0f, 1.0f};
+            transpose_bytes(sm.bytes, a.qT, mb * 32, k0, a.K, one);
+            continue;
+        }
+        i -= a.q_items;
+        copy_dy<IN, VEC>(a, (int64_t)(i / a.dy_x) * 64, (int64_t)(i % a.dy_x) * 64, sm.halves);
+    }
 }
 
-// Copies, each 256-byte aligned, then room for the fp32 sums of a bf16 dX, then (optional) for the products' slices.
+// Whether the product reads dY where it lies: whole stages, and offsets of a tile's rows in 32 bits.
+static bool dy_direct(bool bf16, int64_t N) { return bf16 && N % 32 == 0 && N < (1 << 22); }
+
+// The copies, each 256-byte aligned, then (optional) room for the products' slices.  What is asked for does not go by the types.
 struct BackwardI8Ws {
-    size_t wT, gwT, qT, dx, total;
+    size_t wT, gwT, qT, total;
 };
 static BackwardI8Ws backward_i8_ws(int64_t M, int64_t N, int64_t K) {
     const int64_t Np = pad32(N), Mp = pad32(M);
@@ -91,8 +166,7 @@ static BackwardI8Ws backward_i8_ws(int64_t M, int64_t N, int64_t K) {
     w.wT = al((size_t)M * Np * 2);
     w.gwT = w.wT + al((size_t)K * Np * 2);
     w.qT = w.gwT + al((size_t)N * Mp * 2);
-    w.dx = w.qT + al((size_t)K * Mp * 2);
-    w.total = w.dx + al((size_t)M * K * 4);
+    w.total = w.qT + al((size_t)K * Mp * 2);
     return w;
 }
 size_t backward_i8_min_bytes(int64_t M, int64_t N, int64_t K) { return backward_i8_ws(M, N, K).total; }
@@ -107,26 +181,48 @@ hipError_t launch_backward_i8(const BackwardI8Args& a, hipStream_t s) {
     char* base = (char*)a.workspace;
     uint16_t *g = (uint16_t*)base, *wT = (uint16_t*)(base + ws.wT), *gwT = (uint16_t*)(base + ws.gwT),
              *qT = (uint16_t*)(base + ws.qT);
-    float* part = (float*)(base + ws.total);
-    const size_t part_bytes = a.workspace_bytes > ws.total ? a.workspace_bytes - ws.total : 0;
-    uint16_t *rows = a.dX ? g : nullptr, *tr = a.dW ? gwT : nullptr;
-    const float* row_gamma = a.per_tensor ? nullptr : a.gamma;
-    if (a.dy_bf16) launch_copy((const uint16_t*)a.dY, M, N, a.scale, row_gamma, rows, tr, s);
-    else launch_copy((const float*)a.dY, M, N, a.scale, row_gamma, rows, tr, s);
+    const bool direct = dy_direct(a.dy_bf16, N);
+    CopyI8Args c{};
+    c.dY = a.dY; c.codes = a.codes; c.packed = a.packed; c.M = M; c.N = N; c.K = K; c.Np = Np; c.Mp = Mp;
+    c.w_scale = a.dy_bf16 ? a.scale : nullptr;
+    c.col_scale = a.dy_bf16 ? nullptr : a.scale;
+    c.row_gamma = a.per_tensor ? nullptr : a.gamma;
+    c.wT = a.dX ? wT : nullptr;
+    c.g = a.dX && !direct ? g : nullptr;
+    c.qT = a.dW ? qT : nullptr;
+    c.gwT = a.dW ? gwT : nullptr;
+    auto tiles = [](int64_t v, int64_t t) { return (v + t - 1) / t; };
+    c.k_x = (uint32_t)tiles(K, 256);
+    c.dy_x = (uint32_t)tiles(c.g ? Np : N, 64);
+    const int64_t w_items = c.wT ? Np / 32 * c.k_x : 0, q_items = c.qT ? Mp / 32 * c.k_x : 0;
+    const int64_t items = w_items + q_items + (c.g || c.gwT ? tiles(c.gwT ? Mp : M, 64) * c.dy_x : 0);
+    if (items >= (int64_t)1 << 32) return hipErrorInvalidValue;
+    c.w_items = (uint32_t)w_items; c.q_items = (uint32_t)q_items; c.items = (uint32_t)items;
+    const unsigned grid = (unsigned)(items < (1 << 22) ? items : (1 << 22));
+    const bool vec = N % 4 == 0;
+    if (a.dy_bf16) {
+        if (vec) copy_i8_operands<uint16_t, true><<<grid, 256, 0, s>>>(c);
+        else copy_i8_operands<uint16_t, false><<<grid, 256, 0, s>>>(c);
+    } else {
+        if (vec) copy_i8_operands<float, true><<<grid, 256, 0, s>>>(c);
+        else copy_i8_operands<float, false><<<grid, 256, 0, s>>>(c);
+    }
+    TnArgs t{};
+    t.part = (float*)(base + ws.total);
+    t.part_bytes = a.workspace_bytes > ws.total ? a.workspace_bytes - ws.total : 0;
+    t.J = K;
     if (a.dX) {
-        const int64_t items = (Np / 32) * i8_tiles_k(K);
-        copy_weights<<<(unsigned)(items < (1 << 20) ? items : (1 << 20)), 256, 0, s>>>(a.packed, N, K, wT, items);
-        float* out = a.dx_bf16 ? (float*)(base + ws.dx) : (float*)a.dX;
-        launch_gemm_tn(g, wT, M, K, Np, nullptr, 1.0f, out, part, part_bytes, s);
-        if (a.dx_bf16) {
-            const int64_t n4 = M * K / 4, wgs = (n4 + 255) / 256;
-            round_to_bf16<<<(unsigned)(wgs < (1 << 16) ? wgs : (1 << 16)), 256, 0, s>>>(out, (uint16_t*)a.dX, n4);
-        }
+        t.A = direct ? (const uint16_t*)a.dY : g;
+        t.a_pitch = direct ? (uint32_t)(N * 2) : 0;
+        t.B = wT; t.I = M; t.Rp = Np; t.scale_mul = 1.0f; t.C = a.dX; t.c_bf16 = a.dx_bf16;
+        launch_gemm_tn(t, s);
     }
     if (a.dW) {
-        launch_copy(a.codes, M, K, nullptr, nullptr, nullptr, qT, s);
-        launch_gemm_tn(gwT, qT, N, K, Mp, a.per_tensor ? a.gamma : nullptr, a.per_tensor ? 1.0f / 128.0f : 1.0f, a.dW, part,
-                       part_bytes, s);
+        t.A = gwT; t.a_pitch = 0; t.B = qT; t.I = N; t.Rp = Mp;
+        t.scale_ptr = a.per_tensor ? a.gamma : nullptr;
+        t.scale_mul = a.per_tensor ? 1.0f / 128.0f : 1.0f;
+        t.C = a.dW; t.c_bf16 = false;
+        launch_gemm_tn(t, s);
     }
     return hipGetLastError();
 }
