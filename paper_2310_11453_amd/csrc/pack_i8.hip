@@ -1,6 +1,8 @@
 // The quantiser of 8-bit weights, a scale for each output channel:
 //   m_n = max_k |W_nk|,  scale_n = m_n / 127,  code_nk = clamp(rne(W_nk * (127 / m_n)), -127, 127)
 // into the tiles of i8.h, and back to the values that the codes stand for.
+#include <type_traits>
+
 #include "common.h"
 #include "i8.h"
 #include "rowops.h"
@@ -10,47 +12,93 @@ namespace bl {
 // m below this has no 127 / m in fp32: its codes have a step of 2^-127
 constexpr float kLeastMost = 127.f * 0x1p-127f;
 
-// One wave a row, eight rows of a tile a workgroup: 128 bytes, a line, of every 16 columns.
-template <typename T>
-__global__ __launch_bounds__(512) void pack_i8_rows(PackI8Args a) {
-    const int w = threadIdx.x / kWave, l = threadIdx.x % kWave;
+// Eight rows, half a tile, a workgroup: WR waves a row, whose 16 float4 a lane lie in registers, so that rows of 4096 WR are read
+// once; of longer ones all but the last chunk is read again, from the end, out of the caches.  The codes go through LDS and leave
+// as whole lines of 128 bytes: eight rows of 16 columns.  Bound by HBM.
+__device__ inline uint32_t load_codes(const int8_t* p, int64_t i4) { return reinterpret_cast<const uint32_t*>(p)[i4]; }
+template <typename T, int WR>
+__global__ __launch_bounds__(512 * WR, 4) void pack_i8_rows(PackI8Args a) {
+    constexpr int NV = 16, LANES = 64 * WR, CHUNK = LANES * NV * 4;
+    constexpr bool CODES = sizeof(T) == 1;
+    using Element = std::conditional_t<CODES, uint32_t, float4>;
+    __shared__ __attribute__((aligned(16))) uint8_t codes[8][CHUNK + 16];
+    __shared__ float most[8][WR];
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave), r = wave / WR;
+    const int t = wave % WR * kWave + ((int)threadIdx.x & (kWave - 1));
     const int64_t K4 = a.K / 4, TK = i8_tiles_k(a.K), rows = tiles_n(a.N) * 16;
-    for (int64_t n = (int64_t)blockIdx.x * 8 + w; n < rows; n += (int64_t)gridDim.x * 8) {
+    const int chunks = (int)((a.K + CHUNK - 1) / CHUNK);
+    for (int64_t n0 = (int64_t)blockIdx.x * 8; n0 < rows; n0 += (int64_t)gridDim.x * 8) {
+        const int64_t n = n0 + r;
         const bool in = n < a.N;
-        const T* src = static_cast<const T*>(a.W) + (in ? n : 0) * a.K;
-        uint8_t* dst = a.packed + (n / 16) * TK * 1024 + (n % 16) * 16;
-        float m = 0.f;
-        if constexpr (sizeof(T) != 1) {
-            for (int64_t i = l; i < K4; i += kWave) {
-                const float4 v = load4(src, i);
-                m = fmaxf(m, fmaxf(fmaxf(fabsf(v.x), fabsf(v.y)), fmaxf(fabsf(v.z), fabsf(v.w))));
-            }
-            m = wave_max(m);
-        }
-        if (m > 0.f) m = fmaxf(m, kLeastMost);
-        const float up = m > 0.f ? 127.0f / m : 0.f;
-        for (int64_t i = l; i < TK * 16; i += kWave) {
-            uint32_t c = 0;
-            if (in && i < K4) {
-                if constexpr (sizeof(T) == 1) {
-                    c = reinterpret_cast<const uint32_t*>(src)[i];
-                } else {
-                    const float4 v = load4(src, i);
-                    c = code_word(v.x * up, v.y * up, v.z * up, v.w * up, -127.f);
+        const T* src = static_cast<const T*>(a.W) + (in ? n : a.N - 1) * a.K;
+        Element v[NV];
+        auto load = [&](int c) {
+            const int64_t first = (int64_t)c * (CHUNK / 4);
+#pragma unroll
+            for (int j = 0; j < NV; ++j)
+                if (first + j * LANES < K4) {  // uniform
+                    const int64_t i = first + j * LANES + t;
+                    if constexpr (CODES) v[j] = load_codes(src, i < K4 ? i : K4 - 1);
+                    else v[j] = load4(src, i < K4 ? i : K4 - 1);
                 }
+        };
+        float m = 0.f;
+        for (int c = 0; c < chunks; ++c) {
+            if (CODES && c < chunks - 1) continue;
+            load(c);
+            if constexpr (!CODES) {
+                const int64_t first = (int64_t)c * (CHUNK / 4);
+#pragma unroll
+                for (int j = 0; j < NV; ++j)  // (the row's last element again past it)
+                    if (first + j * LANES < K4)
+                        m = fmaxf(m, fmaxf(fmaxf(fabsf(v[j].x), fabsf(v[j].y)), fmaxf(fabsf(v[j].z), fabsf(v[j].w))));
             }
-            *reinterpret_cast<uint32_t*>(dst + (i / 16) * 1024 + (i % 16 / 4) * 256 + (i % 4) * 4) = c;
         }
-        if constexpr (sizeof(T) != 1)
-            if (l == 0 && in) a.scale[n] = m / 127.0f;
+        float up = 0.f;
+        if constexpr (!CODES) {
+            m = wave_reduce(m, OpMax{});
+            if constexpr (WR > 1) {
+                if ((threadIdx.x & (kWave - 1)) == 0) most[r][wave % WR] = m;
+                __syncthreads();
+                m = fold_slots<WR>(most[r], OpMax{});
+            }
+            if (m > 0.f) m = fmaxf(m, kLeastMost);
+            up = m > 0.f ? 127.0f / m : 0.f;
+            if (t == 0 && in) a.scale[n] = m / 127.0f;
+        }
+        for (int c = chunks - 1; c >= 0; --c) {
+            if (c < chunks - 1) load(c);
+            const int64_t first = (int64_t)c * (CHUNK / 4);
+#pragma unroll
+            for (int j = 0; j < NV; ++j)
+                if (first + j * LANES < TK * 16) {  // uniform
+                    uint32_t w;
+                    if constexpr (CODES) w = v[j];
+                    else w = code_word(v[j].x * up, v[j].y * up, v[j].z * up, v[j].w * up, -127.f);
+                    // zeros in what is filled up
+                    *reinterpret_cast<uint32_t*>(&codes[r][(j * LANES + t) * 4]) = in && first + j * LANES + t < K4 ? w : 0u;
+                }
+            __syncthreads();
+            const int64_t units = TK * 4 - (int64_t)c * (CHUNK / 16);
+            uint8_t* dst = a.packed + (n0 / 16 * TK + (int64_t)c * (CHUNK / 64)) * 1024 + n0 % 16 * 16;
+            for (int i = threadIdx.x; i < CHUNK / 16 * 8 && i / 8 < units; i += 512 * WR)
+                *reinterpret_cast<uint4*>(dst + i / 8 * 256 + i % 8 * 16) =
+                    *reinterpret_cast<const uint4*>(&codes[i % 8][i / 8 * 16]);
+            __syncthreads();
+        }
     }
 }
-hipError_t launch_pack_i8(const PackI8Args& a, hipStream_t s) {
+template <typename T>
+static void launch_pack_typed(const PackI8Args& a, hipStream_t s) {
     const int64_t wgs = tiles_n(a.N) * 2;
     const unsigned grid = (unsigned)(wgs < (1 << 20) ? wgs : (1 << 20));
-    if (a.type == kF32) pack_i8_rows<float><<<grid, 512, 0, s>>>(a);
-    else if (a.type == kBF16) pack_i8_rows<uint16_t><<<grid, 512, 0, s>>>(a);
-    else pack_i8_rows<int8_t><<<grid, 512, 0, s>>>(a);
+    if (a.K <= 4096) pack_i8_rows<T, 1><<<grid, 512, 0, s>>>(a);
+    else pack_i8_rows<T, 2><<<grid, 1024, 0, s>>>(a);
+}
+hipError_t launch_pack_i8(const PackI8Args& a, hipStream_t s) {
+    if (a.type == kF32) launch_pack_typed<float>(a, s);
+    else if (a.type == kBF16) launch_pack_typed<uint16_t>(a, s);
+    else launch_pack_typed<int8_t>(a, s);
     return hipGetLastError();
 }
 

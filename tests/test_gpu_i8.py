@@ -249,9 +249,13 @@ def test_backward(bl, M, K, N, dy_type, dx_type, per_tensor):
 
 
 @pytest.mark.parametrize("dy_type", [F, B])
-def test_backward_exact_on_integers(bl, dy_type):
-    """Integer dY, powers of two as scales: every sum is exact in fp32."""
-    for M, K, N in [(40, 96, 50), (300, 544, 260), (1100, 288, 1040)]:
+@pytest.mark.parametrize("spec", ["", "bwd_ring=1", "bwd_ring=2", "bwd_splits=2", "bwd_splits=16", "bwd_grid=8"])
+def test_backward_exact_on_integers(bl, tuning, dy_type, spec):
+    """Integer dY, powers of two as scales: every sum is exact in fp32.  N a multiple of 32 (dY read where it lies) and not,
+    each tile, slices of the reductions, more tiles than workgroups."""
+    tuning(spec)
+    for M, K, N in [(1, 32, 32), (40, 96, 50), (40, 96, 64), (300, 544, 260), (300, 544, 288), (1100, 288, 1040),
+                    (1100, 288, 1056), (33, 2080, 544), (2080, 160, 2048)]:
         g = torch.Generator().manual_seed(M)
         dY = torch.randint(-3, 4, (M, N), generator=g).to(dy_type)
         q, w = (torch.randint(-9, 10, s, generator=g).to(I8) for s in ((M, K), (N, K)))
