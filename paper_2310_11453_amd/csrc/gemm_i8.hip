@@ -44,6 +44,20 @@ __device__ inline void i8_issue(v4i (&a)[2], v4i (&b)[2], uint32_t ad_a, uint32_
 __device__ inline void i8_wait(v4i (&a)[2], v4i (&b)[2]) {
     asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(a[0]), "+v"(a[1]), "+v"(b[0]), "+v"(b[1]));
 }
+__device__ inline void i8_issue(v4i (&a)[4], v4i (&b)[2], uint32_t ad_a, uint32_t ad_b) {
+    asm volatile(
+        "ds_read_b128 %0, %6\n\t"
+        "ds_read_b128 %1, %6 offset:2048\n\t"
+        "ds_read_b128 %2, %6 offset:4096\n\t"
+        "ds_read_b128 %3, %6 offset:6144\n\t"
+        "ds_read_b128 %4, %7\n\t"
+        "ds_read_b128 %5, %7 offset:2048"
+        : "=&v"(a[0]), "=&v"(a[1]), "=&v"(a[2]), "=&v"(a[3]), "=&v"(b[0]), "=&v"(b[1])
+        : "v"(ad_a), "v"(ad_b));
+}
+__device__ inline void i8_wait(v4i (&a)[4], v4i (&b)[2]) {
+    asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(a[0]), "+v"(a[1]), "+v"(a[2]), "+v"(a[3]), "+v"(b[0]), "+v"(b[1]));
+}
 __device__ inline void i8_issue(v4i (&a)[1], v4i (&b)[2], uint32_t ad_a, uint32_t ad_b) {
     asm volatile(
         "ds_read_b128 %0, %3\n\t"
@@ -57,20 +71,102 @@ __device__ inline void i8_wait(v4i (&a)[1], v4i (&b)[2]) {
 }
 
 enum I8Out { kOutF32 = 0, kOutBF16 = 1, kOutAcc = 2, kOutPart = 3 };  // kOutPart: a slice's int32 sums
+
+// Stores a wave's blocks of 32 x 32: lane (j, g2) holds columns 32 s + j, rows 32 mi + 8 rq + 4 g2 + rr.  `rowp`, a scalar that is
+// hidden from the optimiser (which would compute all the addresses ahead and spill), walks the rows; a lane's place in a row is one
+// 32-bit offset.  With the rows' bounds, a 64-bit product and branches at every store the instructions around the stores took 12 us of a
+// 256 x 256 tile.  bf16, two columns to a dword: a lane packs its values of two rows, exchanges with its neighbour and stores two
+// columns of one of them, if rows begin at even elements of a 4-byte aligned output.  The output is streamed past the caches, where
+// the operands are.
+template <int OUT>
+struct I8Store {
+    typedef __attribute__((address_space(1))) uint8_t* gptr;
+    static constexpr int ES = OUT == kOutBF16 ? 2 : 4;
+    uint64_t first;
+    int64_t pitch, rows, cols;
+    int j, g2;
+    bool pairs;
+    __device__ I8Store(const GemmI8Args& a, int slice, int64_t mb, int64_t nb, int64_t rows_, int64_t cols_, int j_, int g2_)
+        : pitch(a.N * ES), rows(rows_), cols(cols_), j(j_), g2(g2_) {
+        uint8_t* base = OUT == kOutPart ? reinterpret_cast<uint8_t*>(a.part) + slice * a.M * a.N * 4 : static_cast<uint8_t*>(a.Y);
+        const uint64_t at = (uint64_t)(uintptr_t)(base + mb * pitch + nb * ES);
+        first = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)at) |
+                (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(at >> 32)) << 32;
+        pairs = OUT == kOutBF16 && a.N % 2 == 0 && ((uintptr_t)a.Y & 3) == 0;
+    }
+    template <int MI, int NI, class GAMMA, class SC, class ACC>
+    __device__ void all(GAMMA&& gamma, const SC& sc, const ACC& acc) const {
+        const bool whole = rows >= 32 * MI && cols >= 32 * NI;  // uniform
+        if constexpr (OUT == kOutBF16) {
+            if (pairs) {
+                if (whole) walk<MI, NI, false, true>(gamma, sc, acc);
+                else walk<MI, NI, true, true>(gamma, sc, acc);
+                return;
+            }
+        }
+        if (whole) walk<MI, NI, false, false>(gamma, sc, acc);
+        else walk<MI, NI, true, false>(gamma, sc, acc);
+    }
+    template <int MI, int NI, bool RAGGED, bool PAIRS, class GAMMA, class SC, class ACC>
+    __device__ void walk(GAMMA&& gamma, const SC& sc, const ACC& acc) const {
+        gptr rowp = (gptr)first;
+        const int odd = PAIRS ? j & 1 : 0, col = j - odd;
+        const int64_t lane = (4 * g2 + odd) * pitch + col * ES;
+        const int mine = (int)(rows < 32 * MI ? rows : 32 * MI) - 4 * g2 - odd;  // this lane's rows end here
+        const int last = (int)(cols < 32 * NI ? cols : 32 * NI) - col;           // and its columns
+        const uint32_t pick = odd ? 0x03020706u : 0x05040100u;  // the neighbour's second row and its own; its own first and the neighbour's
+#pragma unroll
+        for (int mi = 0; mi < MI; ++mi)
+#pragma unroll
+            for (int rq = 0; rq < 4; ++rq) {
+                v4f g{};
+                if constexpr (OUT == kOutF32 || OUT == kOutBF16) g = gamma(mi, rq);
+#pragma unroll
+                for (int rr = 0; rr < 4; rr += PAIRS ? 2 : 1) {
+                    asm volatile("" : "+s"(rowp));
+                    const bool in = !RAGGED || 32 * mi + 8 * rq + rr < mine;
+#pragma unroll
+                    for (int s = 0; s < NI; ++s) {
+                        const int r = 4 * rq + rr;
+                        if constexpr (PAIRS) {
+                            const uint32_t p = bf16_pair((float)acc[mi][s][r] * (sc[s] * g[rr]),
+                                                         (float)acc[mi][s][r + 1] * (sc[s] * g[rr + 1]));
+                            const uint32_t q = (uint32_t)__builtin_amdgcn_mov_dpp((int)p, 0xB1, 0xF, 0xF, true);
+                            const uint32_t v = __builtin_amdgcn_perm(q, p, pick);
+                            if (in && (!RAGGED || 32 * s < last))
+                                __builtin_nontemporal_store(v, (__attribute__((address_space(1))) uint32_t*)(rowp + lane + 64 * s));
+                        } else if (in && (!RAGGED || 32 * s < last)) {
+                            const gptr at = rowp + lane + 32 * ES * s;
+                            if constexpr (OUT == kOutBF16)
+                                __builtin_nontemporal_store((uint16_t)bf16_pair((float)acc[mi][s][r] * (sc[s] * g[rr]), 0.f),
+                                                            (__attribute__((address_space(1))) uint16_t*)at);
+                            else if constexpr (OUT == kOutF32)
+                                __builtin_nontemporal_store((float)acc[mi][s][r] * (sc[s] * g[rr]),
+                                                            (__attribute__((address_space(1))) float*)at);
+                            else *(__attribute__((address_space(1))) int32_t*)at = acc[mi][s][r];
+                        }
+                    }
+                    rowp += (PAIRS ? 2 : 1) * pitch;
+                }
+                rowp += 4 * pitch;
+            }
+    }
+};
+
 struct I8Plan {
     int tile, grid, gm, gn;  // which tile (kTiles); workgroups; rows and columns of tiles
     int splits, per;         // slices of K, of `per` stages
 };
 
 template <int TM, int TN, int NS, int OUT>
-__global__ __launch_bounds__(256, TM == 256 ? 1 : 2) void gemm_i8_tiles(GemmI8Args a, I8Plan p) {
+__global__ __launch_bounds__(256, TM + TN == 512 ? 1 : 2) void gemm_i8_tiles(GemmI8Args a, I8Plan p) {
     constexpr int THREADS = 256, WTM = TM / 2, WTN = TN / 2, MI = WTM / 32, NI = WTN / 32;
     constexpr int PA = TM / 64, PB = TN / 64, P = PA + PB;
     constexpr int A_BYTES = TM * 64, STAGE_BYTES = A_BYTES + TN * 64;
     constexpr bool SPLIT = OUT == kOutPart;
     static_assert((NS - 1) * P < 64, "vmcnt range");
     __shared__ __attribute__((aligned(1024))) uint8_t sm[NS * STAGE_BYTES];
-    __shared__ float sm_gamma[2][TM];
+    __shared__ __attribute__((aligned(16))) float sm_gamma[2][TM];
 
     const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave), l = threadIdx.x % kWave;
     const int wm = w / 2, wn = w % 2, j = l & 31, g2 = l >> 5;
@@ -236,59 +332,46 @@ __global__ __launch_bounds__(256, TM == 256 ? 1 : 2) void gemm_i8_tiles(GemmI8Ar
             issue_tile_start();
         }
         const int64_t mb = mt + __builtin_amdgcn_readfirstlane(wm * WTM), nb = nt + __builtin_amdgcn_readfirstlane(wn * WTN);
+        I8Store<OUT> st(a, sl, mb, nb, a.M - mb, a.N - nb, j, g2);
         const float* gm = sm_gamma[parity] + wm * WTM + 4 * g2;
-        if constexpr (OUT == kOutBF16) {
-#pragma unroll
-            for (int mi = 0; mi < MI; ++mi)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const int64_t m = mb + 32 * mi + 8 * (r >> 2) + 4 * g2 + (r & 3);
-                    const float g = gm[32 * mi + 8 * (r >> 2) + (r & 3)];
-                    if (m >= a.M) continue;
-#pragma unroll
-                    for (int s = 0; s < NI; ++s) {
-                        const int64_t n = nb + 32 * s + j;
-                        if (n < a.N)
-                            static_cast<uint16_t*>(a.Y)[m * a.N + n] = (uint16_t)bf16_pair((float)acc[mi][s][r] * (sc[s] * g), 0.f);
-                    }
-                }
-        } else {
-#pragma unroll
-            for (int mi = 0; mi < MI; ++mi)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const int64_t m = mb + 32 * mi + 8 * (r >> 2) + 4 * g2 + (r & 3);
-                    const float g = OUT == kOutF32 ? gm[32 * mi + 8 * (r >> 2) + (r & 3)] : 0.f;
-                    if (m >= a.M) continue;
-#pragma unroll
-                    for (int s = 0; s < NI; ++s) {
-                        const int64_t n = nb + 32 * s + j;
-                        if (n >= a.N) continue;
-                        if constexpr (OUT == kOutPart) a.part[((int64_t)sl * a.M + m) * a.N + n] = acc[mi][s][r];
-                        else if constexpr (OUT == kOutAcc) static_cast<int32_t*>(a.Y)[m * a.N + n] = acc[mi][s][r];
-                        else __builtin_nontemporal_store((float)acc[mi][s][r] * (sc[s] * g), &static_cast<float*>(a.Y)[m * a.N + n]);
-                    }
-                }
-        }
+        st.template all<MI, NI>([&](int mi, int rq) { return *reinterpret_cast<const v4f*>(gm + 32 * mi + 8 * rq); }, sc, acc);
         if (!more) break;
         parity ^= 1;
     }
 }
 
 // ---- slices of K added, then scaled ----------------------------------------------------------------------
-template <int OUT>
+// A thread takes four channels of a token (VEC: 16 bytes of every slice, N a multiple of 4), all slices' loads in flight.
+template <int OUT, bool VEC>
 __global__ __launch_bounds__(256) void fold_i8(GemmI8Args a, int splits) {
-    const int64_t count = a.M * a.N;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < count; i += (int64_t)gridDim.x * 256) {
-        int32_t v = a.part[i];
-        for (int s = 1; s < splits; ++s) v += a.part[s * count + i];
-        if constexpr (OUT == kOutAcc) {
-            static_cast<int32_t*>(a.Y)[i] = v;
+    constexpr int E = VEC ? 4 : 1;
+    const int64_t count = a.M * a.N, n = ((int64_t)blockIdx.x * 256 + threadIdx.x) * E;
+    if (n >= a.N) return;
+    for (int64_t m = blockIdx.y; m < a.M; m += gridDim.y) {
+        const int64_t i = m * a.N + n;
+        int32_t v[E];
+        if constexpr (VEC) {
+            v4i t = *reinterpret_cast<const v4i*>(a.part + i);
+#pragma unroll 4
+            for (int s = 1; s < splits; ++s) t += *reinterpret_cast<const v4i*>(a.part + s * count + i);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = t[e];
         } else {
-            const int64_t m = i / a.N, n = i - m * a.N;
-            const float y = (float)v * (a.scale[n] * ((a.per_tensor ? *a.gamma : a.gamma[m]) * (1.0f / 128.0f)));
-            if constexpr (OUT == kOutBF16) static_cast<uint16_t*>(a.Y)[i] = (uint16_t)bf16_pair(y, 0.f);
-            else static_cast<float*>(a.Y)[i] = y;
+            v[0] = a.part[i];
+            for (int s = 1; s < splits; ++s) v[0] += a.part[s * count + i];
+        }
+        if constexpr (OUT == kOutAcc) {
+#pragma unroll
+            for (int e = 0; e < E; ++e) static_cast<int32_t*>(a.Y)[i + e] = v[e];
+        } else {
+            const float gm = (a.per_tensor ? *a.gamma : a.gamma[m]) * (1.0f / 128.0f);
+            float y[E];
+#pragma unroll
+            for (int e = 0; e < E; ++e) y[e] = (float)v[e] * (a.scale[n + e] * gm);
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                if constexpr (OUT == kOutBF16) static_cast<uint16_t*>(a.Y)[i + e] = (uint16_t)bf16_pair(y[e], 0.f);
+                else static_cast<float*>(a.Y)[i + e] = y[e];
         }
     }
 }
@@ -442,14 +525,15 @@ struct I8Tile {
     int tm, tn, wgs;  // wgs: a CU's
     double stage, alone, item;
 };
-constexpr I8Tile kTiles[3] = {{256, 256, 1, 0.62, 0.62, 12.0}, {128, 128, 2, 0.385, 0.22, 4.5}, {64, 128, 2, 0.3, 0.18, 3.5}};
+constexpr I8Tile kTiles[4] = {
+    {256, 256, 1, 0.62, 0.62, 12.0}, {128, 128, 2, 0.385, 0.22, 4.5}, {64, 128, 2, 0.3, 0.18, 3.5}, {256, 128, 2, 0.6, 0.4, 6.0}};
 static I8Plan i8_plan(int64_t M, int64_t N, int64_t K) {
     const Tuning& t = tuning();
     const int64_t cus = num_cus(), nst = i8_tiles_k(K);
     I8Plan best{};
     double least = 1e30;
-    for (int k = 0; k < 3; ++k) {
-        if (t.i8_tile >= 1 && t.i8_tile <= 3 && t.i8_tile != k + 1) continue;
+    for (int k = 0; k < 4; ++k) {
+        if (t.i8_tile >= 1 && t.i8_tile <= 4 && t.i8_tile != k + 1) continue;
         const I8Tile& T = kTiles[k];
         const int64_t gm = (M + T.tm - 1) / T.tm, gn = (N + T.tn - 1) / T.tn, tiles = gm * gn;
         const int64_t force = t.i8_splits > 0 ? t.i8_splits : 0;
@@ -478,7 +562,7 @@ static I8Plan unsliced(I8Plan p, int64_t K) {
 }
 static bool few_tokens(int64_t M) {
     const int t = tuning().i8_tile;
-    return M <= 64 && (t < 1 || t > 3);
+    return M <= 64 && (t < 1 || t > 4);
 }
 static size_t slices_bytes(int64_t slices, int64_t M, int64_t N) { return slices > 1 ? (size_t)slices * M * N * 4 : 0; }
 
@@ -486,10 +570,16 @@ size_t gemm_i8_part_bytes(int64_t M, int64_t N, int64_t K) {
     if (M == 0) return 0;
     return slices_bytes(few_tokens(M) ? stream_plan(M, N, K).slices : i8_plan(M, N, K).splits, M, N);
 }
+template <bool VEC>
+static void launch_fold_as(const GemmI8Args& a, int splits, int out, hipStream_t s) {
+    const int64_t per = VEC ? 1024 : 256;
+    const dim3 grid((unsigned)((a.N + per - 1) / per), (unsigned)(a.M < 32768 ? a.M : 32768));
+    const auto fold = out == kOutAcc ? fold_i8<kOutAcc, VEC> : out == kOutBF16 ? fold_i8<kOutBF16, VEC> : fold_i8<kOutF32, VEC>;
+    fold<<<grid, 256, 0, s>>>(a, splits);
+}
 static void launch_fold(const GemmI8Args& a, int splits, int out, hipStream_t s) {
-    const int64_t wgs = (a.M * a.N + 255) / 256;
-    const auto fold = out == kOutAcc ? fold_i8<kOutAcc> : out == kOutBF16 ? fold_i8<kOutBF16> : fold_i8<kOutF32>;
-    fold<<<(unsigned)(wgs < (1 << 16) ? wgs : (1 << 16)), 256, 0, s>>>(a, splits);
+    if (a.N % 4 == 0) launch_fold_as<true>(a, splits, out, s);
+    else launch_fold_as<false>(a, splits, out, s);
 }
 hipError_t launch_gemm_i8(const GemmI8Args& a, hipStream_t s) {
     const int out = a.out_acc ? kOutAcc : a.y_bf16 ? kOutBF16 : kOutF32;
@@ -514,7 +604,8 @@ hipError_t launch_gemm_i8(const GemmI8Args& a, hipStream_t s) {
     const auto kernel =
         p.tile == 0   ? pick(integral_constant<int, 256>{}, integral_constant<int, 256>{}, integral_constant<int, 4>{})
         : p.tile == 1 ? pick(integral_constant<int, 128>{}, integral_constant<int, 128>{}, integral_constant<int, 4>{})
-                      : pick(integral_constant<int, 64>{}, integral_constant<int, 128>{}, integral_constant<int, 6>{});
+        : p.tile == 2 ? pick(integral_constant<int, 64>{}, integral_constant<int, 128>{}, integral_constant<int, 6>{})
+                      : pick(integral_constant<int, 256>{}, integral_constant<int, 128>{}, integral_constant<int, 3>{});
     kernel<<<(unsigned)p.grid, 256, 0, s>>>(a, p);
     if (p.splits > 1) launch_fold(a, p.splits, out, s);
     return hipGetLastError();
