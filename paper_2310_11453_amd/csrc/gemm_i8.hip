@@ -15,59 +15,22 @@ namespace bl {
 // whose operands and stages have the same bytes: a half-step (32 k) is one MFMA for each pair of blocks, the next one's operands
 // are read behind the first row of them, and between the half-steps of stage st every wave waits for its own DMA of stage st + 1,
 // meets the others at a bare barrier and requests stage st + NS - 1 into the buffer that stage st - 1 has left.
-__device__ inline void i8_issue(v4i (&a)[4], v4i (&b)[4], uint32_t ad_a, uint32_t ad_b) {
-    asm volatile(
-        "ds_read_b128 %0, %8\n\t"
-        "ds_read_b128 %1, %8 offset:2048\n\t"
-        "ds_read_b128 %2, %8 offset:4096\n\t"
-        "ds_read_b128 %3, %8 offset:6144\n\t"
-        "ds_read_b128 %4, %9\n\t"
-        "ds_read_b128 %5, %9 offset:2048\n\t"
-        "ds_read_b128 %6, %9 offset:4096\n\t"
-        "ds_read_b128 %7, %9 offset:6144"
-        : "=&v"(a[0]), "=&v"(a[1]), "=&v"(a[2]), "=&v"(a[3]), "=&v"(b[0]), "=&v"(b[1]), "=&v"(b[2]), "=&v"(b[3])
-        : "v"(ad_a), "v"(ad_b));
+// One operand at a time, from block B of 32 rows (2 KiB in either operand); what waits for them is i8_wait.
+template <int B>
+__device__ inline void i8_read(v4i& x, uint32_t ad) {
+    asm volatile("ds_read_b128 %0, %1 offset:%2" : "=&v"(x) : "v"(ad), "n"(B * 2048));
 }
-__device__ inline void i8_wait(v4i (&a)[4], v4i (&b)[4]) {
-    asm volatile("s_waitcnt lgkmcnt(0)"
-                 : "+v"(a[0]), "+v"(a[1]), "+v"(a[2]), "+v"(a[3]), "+v"(b[0]), "+v"(b[1]), "+v"(b[2]), "+v"(b[3]));
-}
-__device__ inline void i8_issue(v4i (&a)[2], v4i (&b)[2], uint32_t ad_a, uint32_t ad_b) {
-    asm volatile(
-        "ds_read_b128 %0, %4\n\t"
-        "ds_read_b128 %1, %4 offset:2048\n\t"
-        "ds_read_b128 %2, %5\n\t"
-        "ds_read_b128 %3, %5 offset:2048"
-        : "=&v"(a[0]), "=&v"(a[1]), "=&v"(b[0]), "=&v"(b[1])
-        : "v"(ad_a), "v"(ad_b));
-}
-__device__ inline void i8_wait(v4i (&a)[2], v4i (&b)[2]) {
-    asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(a[0]), "+v"(a[1]), "+v"(b[0]), "+v"(b[1]));
-}
-__device__ inline void i8_issue(v4i (&a)[4], v4i (&b)[2], uint32_t ad_a, uint32_t ad_b) {
-    asm volatile(
-        "ds_read_b128 %0, %6\n\t"
-        "ds_read_b128 %1, %6 offset:2048\n\t"
-        "ds_read_b128 %2, %6 offset:4096\n\t"
-        "ds_read_b128 %3, %6 offset:6144\n\t"
-        "ds_read_b128 %4, %7\n\t"
-        "ds_read_b128 %5, %7 offset:2048"
-        : "=&v"(a[0]), "=&v"(a[1]), "=&v"(a[2]), "=&v"(a[3]), "=&v"(b[0]), "=&v"(b[1])
-        : "v"(ad_a), "v"(ad_b));
-}
-__device__ inline void i8_wait(v4i (&a)[4], v4i (&b)[2]) {
-    asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(a[0]), "+v"(a[1]), "+v"(a[2]), "+v"(a[3]), "+v"(b[0]), "+v"(b[1]));
-}
-__device__ inline void i8_issue(v4i (&a)[1], v4i (&b)[2], uint32_t ad_a, uint32_t ad_b) {
-    asm volatile(
-        "ds_read_b128 %0, %3\n\t"
-        "ds_read_b128 %1, %4\n\t"
-        "ds_read_b128 %2, %4 offset:2048"
-        : "=&v"(a[0]), "=&v"(b[0]), "=&v"(b[1])
-        : "v"(ad_a), "v"(ad_b));
-}
-__device__ inline void i8_wait(v4i (&a)[1], v4i (&b)[2]) {
-    asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(a[0]), "+v"(b[0]), "+v"(b[1]));
+template <int MI, int NI>
+__device__ inline void i8_wait(v4i (&a)[MI], v4i (&b)[NI]) {
+    if constexpr (MI == 4 && NI == 4)
+        asm volatile("s_waitcnt lgkmcnt(0)"
+                     : "+v"(a[0]), "+v"(a[1]), "+v"(a[2]), "+v"(a[3]), "+v"(b[0]), "+v"(b[1]), "+v"(b[2]), "+v"(b[3]));
+    else if constexpr (MI == 4)
+        asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(a[0]), "+v"(a[1]), "+v"(a[2]), "+v"(a[3]), "+v"(b[0]), "+v"(b[1]));
+    else if constexpr (MI == 2)
+        asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(a[0]), "+v"(a[1]), "+v"(b[0]), "+v"(b[1]));
+    else
+        asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(a[0]), "+v"(b[0]), "+v"(b[1]));
 }
 
 enum I8Out { kOutF32 = 0, kOutBF16 = 1, kOutAcc = 2, kOutPart = 3 };  // kOutPart: a slice's int32 sums
@@ -260,17 +223,35 @@ __global__ __launch_bounds__(256, TM + TN == 512 ? 1 : 2) void gemm_i8_tiles(Gem
 
     v16i acc[MI][NI];
     v4i ax[MI], ay[MI], bx[NI], by[NI];
+    // acc += ac x bc; an, bn = the operands at ad_a, ad_b, valid on return: one read behind each of the first MFMAs (all
+    // behind one another they fill the LDS queue, and the wave's next MFMA waits for its place in it), then, one by one too,
+    // between(q), the DMA of a stage
     auto half_step = [&](const v4i(&ac)[MI], const v4i(&bc)[NI], v4i(&an)[MI], v4i(&bn)[NI], uint32_t ad_a, uint32_t ad_b,
                          auto between) {
-#pragma unroll
-        for (int mi = 0; mi < MI; ++mi) {
-#pragma unroll
-            for (int s = 0; s < NI; ++s) acc[mi][s] = __builtin_amdgcn_mfma_i32_32x32x32_i8(ac[mi], bc[s], acc[mi][s], 0, 0, 0);
+        constexpr int MFMAS = MI * NI, READS = MI + NI, PER = (READS + MFMAS - 1) / MFMAS, LATER = MFMAS - READS / PER;
+        static_for<0, MFMAS>([&](auto ic) {
+            constexpr int i = decltype(ic)::value, mi = i / NI, s = i % NI;
+            acc[mi][s] = __builtin_amdgcn_mfma_i32_32x32x32_i8(ac[mi], bc[s], acc[mi][s], 0, 0, 0);
             __builtin_amdgcn_sched_barrier(0);
-            if (mi == 0) i8_issue(an, bn, ad_a, ad_b);
-            between(mi);
+            static_for<i * PER, (i + 1) * PER>([&](auto rc) {
+                constexpr int r = decltype(rc)::value;
+                // in turn, so that the first MFMAs of the next half-step have both
+                if constexpr (MI == NI) {
+                    if constexpr (r < READS && r % 2 == 0) i8_read<r / 2>(an[r / 2], ad_a);
+                    else if constexpr (r < READS) i8_read<r / 2>(bn[r / 2], ad_b);
+                } else {
+                    if constexpr (r < MI) i8_read<r>(an[r], ad_a);
+                    else if constexpr (r < READS) i8_read<r - MI>(bn[r - MI], ad_b);
+                }
+            });
+            if constexpr (LATER >= P) {
+                if constexpr (i >= MFMAS - P) between(i - (MFMAS - P));
+            } else {
+#pragma unroll
+                for (int q = i * P / MFMAS; q < (i + 1) * P / MFMAS; ++q) between(q);
+            }
             __builtin_amdgcn_sched_barrier(0);
-        }
+        });
         i8_wait(an, bn);
     };
     // In: ax/bx = operands of (st, half 0).  Out: operands of (st + 1, half 0); for the last stage stale bytes that nobody uses.
@@ -279,10 +260,8 @@ __global__ __launch_bounds__(256, TM + TN == 512 ? 1 : 2) void gemm_i8_tiles(Gem
         if (ahead) wait_vmcnt<(NS - 3) * P>();  // younger than stage st + 1: stages st + 2 .. st + NS - 2
         else wait_vmcnt<0>();
         block_barrier();
-        half_step(ay, by, ax, bx, a_lane[0] + ring(st + 1), b_lane[0] + ring(st + 1), [&](int mi) {
-            if (ahead)
-#pragma unroll
-                for (int q = mi * P / MI; q < (mi + 1) * P / MI; ++q) issue_piece(st + NS - 1, st + NS - 1, q);
+        half_step(ay, by, ax, bx, a_lane[0] + ring(st + 1), b_lane[0] + ring(st + 1), [&](int q) {
+            if (ahead) issue_piece(st + NS - 1, st + NS - 1, q);
         });
     };
 
@@ -300,7 +279,8 @@ __global__ __launch_bounds__(256, TM + TN == 512 ? 1 : 2) void gemm_i8_tiles(Gem
                 for (int r = 0; r < 16; ++r) acc[mi][s][r] = 0;
         wait_vmcnt<(NS - 2) * P>();  // younger than stage 0: stages 1 .. NS - 2
         block_barrier();
-        i8_issue(ax, bx, a_lane[0], b_lane[0]);
+        static_for<0, MI>([&](auto ic) { i8_read<decltype(ic)::value>(ax[decltype(ic)::value], a_lane[0]); });
+        static_for<0, NI>([&](auto ic) { i8_read<decltype(ic)::value>(bx[decltype(ic)::value], b_lane[0]); });
         i8_wait(ax, bx);
 
         for (int gidx = 0; gidx < main_groups; ++gidx)
