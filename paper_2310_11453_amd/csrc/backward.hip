@@ -336,6 +336,11 @@ __device__ inline void wide_wait(v4i (&a)[4], v4i (&b)[4]) {
                    "+v"(b[3]));
 }
 
+// one operand, of block B of 32 rows
+template <int B, class OP>
+__device__ inline void wide_read(OP& x, uint32_t ad) {
+    asm volatile("ds_read_b128 %0, %1 offset:%2" : "=&v"(x) : "v"(ad), "n"(B * 2048));
+}
 // the same for 64 x 64 waves
 __device__ inline void wide_issue(v4i (&a)[2], v4i (&b)[2], uint32_t ad_a, uint32_t ad_b) {
     asm volatile(
@@ -597,9 +602,31 @@ __global__ __launch_bounds__(256, T + TJ == 512 ? 1 : 2) void gemm_tn_bf16_wide(
     AOp ax[MI], ay[MI];
     v4i bx[NI], by[NI];
     // acc += ac x bc; an, bn = operands at ad_a, ad_b, valid on return; between(mi) is placed behind the
-    // MFMAs of row mi: the DMA of a stage, whose addresses and issue would otherwise idle the pipe
+    // MFMAs of row mi: the DMA of a stage, whose addresses and issue would otherwise idle the pipe.  The operands are read one
+    // behind each of the first MFMAs: all behind one another they fill the LDS queue, and the wave's next MFMA waits.  (Not where
+    // A is transposed out of LDS, by two reads an operand.)
     auto half_step = [&](const AOp(&ac)[MI], const v4i(&bc)[NI], AOp(&an)[MI], v4i(&bn)[NI], uint32_t ad_a,
                          uint32_t ad_b, auto between) {
+        if constexpr (!DIRECT && MI == NI) {
+            static_for<0, MI>([&](auto mc) {
+                constexpr int mi = decltype(mc)::value;
+                static_for<0, NI>([&](auto sc) {
+                    constexpr int s = decltype(sc)::value, r = mi * NI + s;
+                    acc[mi][s] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wide_operand(ac[mi]), wide_operand(bc[s]),
+                                                                         acc[mi][s], 0, 0, 0);
+                    __builtin_amdgcn_sched_barrier(0);
+                    if constexpr (r < MI + NI) {
+                        if constexpr (r % 2 == 0) wide_read<r / 2>(an[r / 2], ad_a);
+                        else wide_read<r / 2>(bn[r / 2], ad_b);
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+                });
+                between(mi);
+                __builtin_amdgcn_sched_barrier(0);
+            });
+            wide_wait(an, bn);
+            return;
+        }
 #pragma unroll
         for (int mi = 0; mi < MI; ++mi) {
 #pragma unroll
