@@ -25,8 +25,6 @@ __device__ inline void i8_wait(v4i (&a)[MI], v4i (&b)[NI]) {
     if constexpr (MI == 4 && NI == 4)
         asm volatile("s_waitcnt lgkmcnt(0)"
                      : "+v"(a[0]), "+v"(a[1]), "+v"(a[2]), "+v"(a[3]), "+v"(b[0]), "+v"(b[1]), "+v"(b[2]), "+v"(b[3]));
-    else if constexpr (MI == 4)
-        asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(a[0]), "+v"(a[1]), "+v"(a[2]), "+v"(a[3]), "+v"(b[0]), "+v"(b[1]));
     else if constexpr (MI == 2)
         asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(a[0]), "+v"(a[1]), "+v"(b[0]), "+v"(b[1]));
     else
@@ -127,7 +125,9 @@ __global__ __launch_bounds__(256, TM + TN == 512 ? 1 : 2) void gemm_i8_tiles(Gem
     constexpr int PA = TM / 64, PB = TN / 64, P = PA + PB;
     constexpr int A_BYTES = TM * 64, STAGE_BYTES = A_BYTES + TN * 64;
     constexpr bool SPLIT = OUT == kOutPart;
-    static_assert((NS - 1) * P < 64, "vmcnt range");
+    constexpr bool WHOLE = TM + TN < 512;         // a stage's operands in registers at once
+    constexpr int AHEAD = WHOLE ? NS : NS - 1;    // stages requested ahead
+    static_assert(AHEAD * P < 64, "vmcnt range");
     __shared__ __attribute__((aligned(1024))) uint8_t sm[NS * STAGE_BYTES];
     __shared__ __attribute__((aligned(16))) float sm_gamma[2][TM];
 
@@ -156,7 +156,7 @@ __global__ __launch_bounds__(256, TM + TN == 512 ? 1 : 2) void gemm_i8_tiles(Gem
             st0 = slice * p.per;
             nst = nst_all - st0 < p.per ? nst_all - st0 : p.per;
         }
-        main_groups = nst >= 2 * NS - 1 ? (nst - (2 * NS - 1)) / NS + 1 : 0;
+        main_groups = nst >= NS + AHEAD ? (nst - NS - AHEAD) / NS + 1 : 0;  // of NS stages whose look-ahead exists
         const int band = tile / (H * p.gn), rem = tile - band * H * p.gn;
         const int rows = p.gm - band * H < H ? p.gm - band * H : H;
         m0 = (int64_t)(band * H + rem % rows) * TM;
@@ -207,7 +207,7 @@ __global__ __launch_bounds__(256, TM + TN == 512 ? 1 : 2) void gemm_i8_tiles(Gem
     };
     auto issue_tile_start = [&]() {
 #pragma unroll
-        for (int s = 0; s < NS - 1; ++s)
+        for (int s = 0; s < AHEAD; ++s)
 #pragma unroll
             for (int q = 0; q < P; ++q) issue_piece(s, s < nst ? s : nst - 1, q);
     };
@@ -222,7 +222,8 @@ __global__ __launch_bounds__(256, TM + TN == 512 ? 1 : 2) void gemm_i8_tiles(Gem
     auto ring = [&](int st) { return (uint32_t)((st % NS) * STAGE_BYTES); };
 
     v16i acc[MI][NI];
-    v4i ax[MI], ay[MI], bx[NI], by[NI];
+    v4i ax[MI], ay[MI], bx[NI], by[NI];                              // of a half-step and the next
+    v4i sa[WHOLE ? 2 : 1][2][MI], sb[WHOLE ? 2 : 1][2][NI];          // WHOLE: of the halves of a stage and of the next one
     // acc += ac x bc; an, bn = the operands at ad_a, ad_b, valid on return: one read behind each of the first MFMAs (all
     // behind one another they fill the LDS queue, and the wave's next MFMA waits for its place in it), then, one by one too,
     // between(q), the DMA of a stage
@@ -265,6 +266,33 @@ __global__ __launch_bounds__(256, TM + TN == 512 ? 1 : 2) void gemm_i8_tiles(Gem
         });
     };
 
+    // WHOLE: the operands of stage st are in registers F, those of st + 1 are read into 1 - F behind its MFMAs, and the stage
+    // st + NS goes where st was, which every wave has read when it meets the others.  (With the operands of a half-step at a
+    // time, 2 or 4 MFMAs do not hide a trip to LDS.)
+    auto whole_stage = [&](auto fc, int st, bool ahead) {
+        constexpr int F = decltype(fc)::value, G = 1 - F, MFMAS = 2 * MI * NI, READS = 2 * (MI + NI);
+        constexpr int PER = (READS + MFMAS - 1) / MFMAS;
+        if (ahead) wait_vmcnt<(NS - 2) * P>();  // younger than stage st + 1: stages st + 2 .. st + NS - 1
+        else wait_vmcnt<0>();
+        block_barrier();
+        static_for<0, MFMAS>([&](auto ic) {
+            constexpr int i = decltype(ic)::value, h = i / (MI * NI), mi = i % (MI * NI) / NI, s = i % NI;
+            acc[mi][s] = __builtin_amdgcn_mfma_i32_32x32x32_i8(sa[F][h][mi], sb[F][h][s], acc[mi][s], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
+            static_for<i * PER, (i + 1) * PER>([&](auto rc) {
+                constexpr int r = decltype(rc)::value, hr = r / (MI + NI), k = r % (MI + NI);
+                if constexpr (r < READS && k < MI) i8_read<k>(sa[G][hr][k], a_lane[hr] + ring(st + 1));
+                else if constexpr (r < READS) i8_read<k - MI>(sb[G][hr][k - MI], b_lane[hr] + ring(st + 1));
+            });
+            if (ahead)
+#pragma unroll
+                for (int q = i * P / MFMAS; q < (i + 1) * P / MFMAS; ++q) issue_piece(st + NS, st + NS, q);
+            __builtin_amdgcn_sched_barrier(0);
+        });
+        i8_wait(sa[G][0], sb[G][0]);
+        i8_wait(sa[G][1], sb[G][1]);
+    };
+
     int64_t m0, n0;
     origin(q_item, m0, n0);
     setup_dma(m0, n0);
@@ -277,15 +305,37 @@ __global__ __launch_bounds__(256, TM + TN == 512 ? 1 : 2) void gemm_i8_tiles(Gem
             for (int s = 0; s < NI; ++s)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) acc[mi][s][r] = 0;
-        wait_vmcnt<(NS - 2) * P>();  // younger than stage 0: stages 1 .. NS - 2
+        wait_vmcnt<(AHEAD - 1) * P>();  // younger than stage 0: stages 1 .. AHEAD - 1
         block_barrier();
-        static_for<0, MI>([&](auto ic) { i8_read<decltype(ic)::value>(ax[decltype(ic)::value], a_lane[0]); });
-        static_for<0, NI>([&](auto ic) { i8_read<decltype(ic)::value>(bx[decltype(ic)::value], b_lane[0]); });
-        i8_wait(ax, bx);
-
-        for (int gidx = 0; gidx < main_groups; ++gidx)
-            static_for<0, NS>([&](auto ic) { stage(gidx * NS + decltype(ic)::value, true); });
-        for (int st = main_groups * NS; st < nst; ++st) stage(st, st + NS - 1 < nst);
+        if constexpr (WHOLE) {
+            static_for<0, 2>([&](auto hc) {
+                constexpr int h = decltype(hc)::value;
+                static_for<0, MI>([&](auto ic) { i8_read<decltype(ic)::value>(sa[0][h][decltype(ic)::value], a_lane[h]); });
+                static_for<0, NI>([&](auto ic) { i8_read<decltype(ic)::value>(sb[0][h][decltype(ic)::value], b_lane[h]); });
+            });
+            i8_wait(sa[0][0], sb[0][0]);
+            i8_wait(sa[0][1], sb[0][1]);
+            static_assert(NS % 2 == 0, "the registers take turns");
+            using Even = std::integral_constant<int, 0>;
+            using Odd = std::integral_constant<int, 1>;
+            for (int gidx = 0; gidx < main_groups; ++gidx)
+                static_for<0, NS>([&](auto ic) {
+                    whole_stage(std::integral_constant<int, decltype(ic)::value % 2>{}, gidx * NS + decltype(ic)::value, true);
+                });
+            int st = main_groups * NS;
+            for (; st + 1 < nst; st += 2) {
+                whole_stage(Even{}, st, st + NS < nst);
+                whole_stage(Odd{}, st + 1, st + 1 + NS < nst);
+            }
+            if (st < nst) whole_stage(Even{}, st, false);
+        } else {
+            static_for<0, MI>([&](auto ic) { i8_read<decltype(ic)::value>(ax[decltype(ic)::value], a_lane[0]); });
+            static_for<0, NI>([&](auto ic) { i8_read<decltype(ic)::value>(bx[decltype(ic)::value], b_lane[0]); });
+            i8_wait(ax, bx);
+            for (int gidx = 0; gidx < main_groups; ++gidx)
+                static_for<0, NS>([&](auto ic) { stage(gidx * NS + decltype(ic)::value, true); });
+            for (int st = main_groups * NS; st < nst; ++st) stage(st, st + NS - 1 < nst);
+        }
 
         // the tile's factors, behind the waits of its stages
         if constexpr (OUT == kOutF32 || OUT == kOutBF16) {
@@ -505,15 +555,14 @@ struct I8Tile {
     int tm, tn, wgs;  // wgs: a CU's
     double stage, alone, item;
 };
-constexpr I8Tile kTiles[4] = {
-    {256, 256, 1, 0.62, 0.62, 12.0}, {128, 128, 2, 0.385, 0.22, 4.5}, {64, 128, 2, 0.3, 0.18, 3.5}, {256, 128, 2, 0.6, 0.4, 6.0}};
+constexpr I8Tile kTiles[3] = {{256, 256, 1, 0.62, 0.62, 12.0}, {128, 128, 2, 0.385, 0.22, 4.5}, {64, 128, 2, 0.3, 0.18, 3.5}};
 static I8Plan i8_plan(int64_t M, int64_t N, int64_t K) {
     const Tuning& t = tuning();
     const int64_t cus = num_cus(), nst = i8_tiles_k(K);
     I8Plan best{};
     double least = 1e30;
-    for (int k = 0; k < 4; ++k) {
-        if (t.i8_tile >= 1 && t.i8_tile <= 4 && t.i8_tile != k + 1) continue;
+    for (int k = 0; k < 3; ++k) {
+        if (t.i8_tile >= 1 && t.i8_tile <= 3 && t.i8_tile != k + 1) continue;
         const I8Tile& T = kTiles[k];
         const int64_t gm = (M + T.tm - 1) / T.tm, gn = (N + T.tn - 1) / T.tn, tiles = gm * gn;
         const int64_t force = t.i8_splits > 0 ? t.i8_splits : 0;
@@ -542,7 +591,7 @@ static I8Plan unsliced(I8Plan p, int64_t K) {
 }
 static bool few_tokens(int64_t M) {
     const int t = tuning().i8_tile;
-    return M <= 64 && (t < 1 || t > 4);
+    return M <= 64 && (t < 1 || t > 3);
 }
 static size_t slices_bytes(int64_t slices, int64_t M, int64_t N) { return slices > 1 ? (size_t)slices * M * N * 4 : 0; }
 
@@ -584,8 +633,7 @@ hipError_t launch_gemm_i8(const GemmI8Args& a, hipStream_t s) {
     const auto kernel =
         p.tile == 0   ? pick(integral_constant<int, 256>{}, integral_constant<int, 256>{}, integral_constant<int, 4>{})
         : p.tile == 1 ? pick(integral_constant<int, 128>{}, integral_constant<int, 128>{}, integral_constant<int, 4>{})
-        : p.tile == 2 ? pick(integral_constant<int, 64>{}, integral_constant<int, 128>{}, integral_constant<int, 6>{})
-                      : pick(integral_constant<int, 256>{}, integral_constant<int, 128>{}, integral_constant<int, 3>{});
+                      : pick(integral_constant<int, 64>{}, integral_constant<int, 128>{}, integral_constant<int, 6>{});
     kernel<<<(unsigned)p.grid, 256, 0, s>>>(a, p);
     if (p.splits > 1) launch_fold(a, p.splits, out, s);
     return hipGetLastError();
