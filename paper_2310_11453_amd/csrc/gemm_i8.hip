@@ -120,7 +120,7 @@ struct I8Plan {
 };
 
 template <int TM, int TN, int NS, int OUT>
-__global__ __launch_bounds__(256, TM + TN == 512 ? 1 : 2) void gemm_i8_tiles(GemmI8Args a, I8Plan p) {
+__global__ __launch_bounds__(256, NS * (TM + TN) * 64 > 80 * 1024 ? 1 : 2) void gemm_i8_tiles(GemmI8Args a, I8Plan p) {
     constexpr int THREADS = 256, WTM = TM / 2, WTN = TN / 2, MI = WTM / 32, NI = WTN / 32;
     constexpr int PA = TM / 64, PB = TN / 64, P = PA + PB;
     constexpr int A_BYTES = TM * 64, STAGE_BYTES = A_BYTES + TN * 64;
@@ -255,11 +255,23 @@ __global__ __launch_bounds__(256, TM + TN == 512 ? 1 : 2) void gemm_i8_tiles(Gem
         });
         i8_wait(an, bn);
     };
+    // the wait of a stage behind which nothing is requested any more: `younger` stages may still be on their way
+    auto wait_last = [&](int younger) {
+        bool waited = false;
+        static_for<0, AHEAD - 1>([&](auto ic) {
+            constexpr int y = AHEAD - 2 - decltype(ic)::value;
+            if (!waited && younger >= y) {  // uniform
+                wait_vmcnt<y * P>();
+                waited = true;
+            }
+        });
+        if (!waited) wait_vmcnt<0>();
+    };
     // In: ax/bx = operands of (st, half 0).  Out: operands of (st + 1, half 0); for the last stage stale bytes that nobody uses.
     auto stage = [&](int st, bool ahead) {
         half_step(ax, bx, ay, by, a_lane[1] + ring(st), b_lane[1] + ring(st), [](int) {});
         if (ahead) wait_vmcnt<(NS - 3) * P>();  // younger than stage st + 1: stages st + 2 .. st + NS - 2
-        else wait_vmcnt<0>();
+        else wait_last(nst - 2 - st);
         block_barrier();
         half_step(ay, by, ax, bx, a_lane[0] + ring(st + 1), b_lane[0] + ring(st + 1), [&](int q) {
             if (ahead) issue_piece(st + NS - 1, st + NS - 1, q);
@@ -273,7 +285,7 @@ __global__ __launch_bounds__(256, TM + TN == 512 ? 1 : 2) void gemm_i8_tiles(Gem
         constexpr int F = decltype(fc)::value, G = 1 - F, MFMAS = 2 * MI * NI, READS = 2 * (MI + NI);
         constexpr int PER = (READS + MFMAS - 1) / MFMAS;
         if (ahead) wait_vmcnt<(NS - 2) * P>();  // younger than stage st + 1: stages st + 2 .. st + NS - 1
-        else wait_vmcnt<0>();
+        else wait_last(nst - 2 - st);
         block_barrier();
         static_for<0, MFMAS>([&](auto ic) {
             constexpr int i = decltype(ic)::value, h = i / (MI * NI), mi = i % (MI * NI) / NI, s = i % NI;
@@ -633,7 +645,7 @@ hipError_t launch_gemm_i8(const GemmI8Args& a, hipStream_t s) {
     const auto kernel =
         p.tile == 0   ? pick(integral_constant<int, 256>{}, integral_constant<int, 256>{}, integral_constant<int, 4>{})
         : p.tile == 1 ? pick(integral_constant<int, 128>{}, integral_constant<int, 128>{}, integral_constant<int, 4>{})
-                      : pick(integral_constant<int, 64>{}, integral_constant<int, 128>{}, integral_constant<int, 6>{});
+                      : pick(integral_constant<int, 64>{}, integral_constant<int, 128>{}, integral_constant<int, 4>{});
     kernel<<<(unsigned)p.grid, 256, 0, s>>>(a, p);
     if (p.splits > 1) launch_fold(a, p.splits, out, s);
     return hipGetLastError();
