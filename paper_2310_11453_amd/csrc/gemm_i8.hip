@@ -1,5 +1,7 @@
 // int8 x int8 product with scales for each token and channel:
 //   acc[m][n] = sum_k q[m][k] * w[n][k]  (int32, at most 2^14 K <= 2^30),   Y[m][n] = float(acc) * (scale_n * (gamma_m / 128))
+#include <math.h>
+
 #include "common.h"
 #include "i8.h"
 #include "kernels.h"
@@ -418,7 +420,7 @@ __global__ __launch_bounds__(256) void fold_i8(GemmI8Args a, int splits) {
     }
 }
 
-// ---- up to 64 tokens: the weights' stream ------------------------------------------------------------------
+// ---- up to 32 tokens: the weights' stream ------------------------------------------------------------------
 // Bound by reading the weights once.  A workgroup takes TN rows of tiles (16 TN channels) and all of K, or a slice of it; its W
 // waves share the tiles of K evenly.  A wave loads S tiles of each row with 16 bytes a lane, which is the operand of
 // v_mfma_i32_16x16x64_i8 as it lies, and the codes of MB blocks of 16 tokens beside them (from L2), while it multiplies the ones
@@ -523,24 +525,96 @@ __global__ __launch_bounds__(W * 64, W * TN * MB <= 32 ? 4 : 2) void gemm_i8_str
     }
 }
 
-struct StreamPlan {
-    int tn, mb, waves, slices;
+// The tiles: 256 x 256 with one workgroup a CU, 128 x 128 and 64 x 128 with two.  What a call costs, in us: rounds of workgroups
+// with `per` stages each (`two` us a stage with all of a CU's workgroups, `one` with a single one) and their start and stores
+// (`item`), or the operands and the output at the memory's rate; slices of K, their launch and their sums.  The constants were
+// fitted by what the choice costs, over 300 shapes of 65 to 8192 tokens, K to 16384, N to 28672: 0.6 % slower than the best of
+// 18 variants on average, 22 % at most; over 150 others 0.7 % and 14 %.  Any one tile less costs 1.4 to 10 % on average; 256 x 256 in
+// slices would gain 0.1 %.
+struct I8Tile {
+    int tm, tn, wgs;  // wgs: a CU's
+    double two, one, item, item_one;
 };
-static StreamPlan stream_plan(int64_t M, int64_t N, int64_t K) {
-    StreamPlan p{};
-    const int64_t rows = tiles_n(N), TK = i8_tiles_k(K), cus = num_cus();
-    p.mb = (int)((M + 15) / 16);
+constexpr I8Tile kTiles[3] = {{256, 256, 1, 0.679, 0.539, 9.7, 15.4}, {128, 128, 2, 0.485, 0.26, 2.96, 2.75},
+                              {64, 128, 2, 0.339, 0.138, 1.41, 1.75}};
+constexpr double kCallUs = 2.61, kTrafficPerUs = 3.56e6, kFoldUs = 1.78, kFoldSliceUs = 0.26, kFoldPerByte = 3.86e-7;
+constexpr int kMostSlices = 8;
+static double fold_us(double outputs, int64_t splits) {
+    return splits > 1 ? kFoldUs + (double)splits * (kFoldSliceUs + outputs * 4.0 * kFoldPerByte) : 0.0;
+}
+static I8Plan i8_plan(int64_t M, int64_t N, int64_t K, double* us = nullptr) {
     const Tuning& t = tuning();
-    p.tn = rows >= 4 * cus ? 4 : rows >= 2 * cus ? 2 : 1;
-    if (t.i8_rows == 1 || t.i8_rows == 2 || t.i8_rows == 4) p.tn = t.i8_rows;
-    p.waves = 8;
-    const int64_t wgs = (rows + p.tn - 1) / p.tn;
-    int64_t n = 1;
-    if (wgs * 2 <= cus) n = cus / wgs;
-    if (n > TK / 32) n = TK / 32;
-    if (n > 16) n = 16;
-    if (t.i8_splits > 0) n = t.i8_splits < TK ? t.i8_splits : TK;
-    p.slices = (int)(n < 1 ? 1 : n);
+    const int64_t cus = num_cus(), nst = i8_tiles_k(K);
+    const double outputs = (double)M * (double)N;
+    const double floor = ((double)M * (double)K + (double)N * (double)K + 2.0 * outputs) / kTrafficPerUs;
+    I8Plan best{};
+    double least = 1e300;
+    for (int k = 0; k < 3; ++k) {
+        if (t.i8_tile >= 1 && t.i8_tile <= 3 ? t.i8_tile != k + 1 : k == 0 && M <= 192) continue;
+        const I8Tile& T = kTiles[k];
+        const int64_t gm = (M + T.tm - 1) / T.tm, gn = (N + T.tn - 1) / T.tn, tiles = gm * gn;
+        const int64_t force = t.i8_splits > 0 ? t.i8_splits : 0;
+        for (int64_t n = force ? force : 1; n <= (force ? force : kMostSlices); ++n) {
+            const int64_t per = (nst + n - 1) / n, splits = k == 0 ? 1 : (nst + per - 1) / per, items = tiles * splits;
+            if (n > 1 && !force && (k == 0 || per < 3 || splits != n || items > 4 * cus)) continue;
+            const int64_t slots = T.wgs * cus, full = items / slots, rest = items % slots, stages = k == 0 ? nst : per;
+            double cost = (double)full * (T.two * (double)stages + T.item);
+            if (rest) cost += rest > cus ? T.two * (double)stages + T.item : T.one * (double)stages + T.item_one;
+            cost = kCallUs + (cost > floor ? cost : floor) + fold_us(outputs, splits);
+            if (cost < least) {
+                least = cost;
+                const int64_t up = (items + 7) / 8 * 8;
+                best = I8Plan{k, (int)(up < slots ? up : slots), (int)gm, (int)gn, (int)splits, (int)stages};
+            }
+        }
+    }
+    if (us) *us = least;
+    return best;
+}
+static I8Plan unsliced(I8Plan p, int64_t K) {
+    const int64_t tiles = (int64_t)p.gm * p.gn, up = (tiles + 7) / 8 * 8;
+    if (p.grid > up) p.grid = (int)up;
+    p.splits = 1;
+    p.per = (int)i8_tiles_k(K);
+    return p;
+}
+struct StreamPlan {
+    int tn, mb, slices;  // rows of tiles a workgroup (0: tiles it is, of i8_plan), blocks of 16 tokens, slices of K
+};
+// Up to 32 tokens: the stream with the rows of tiles and slices that cost least, or tiles where those do.  us: `call`, and `tile` for
+// each tile of K that a wave has, (workgroups / CUs)^power where there are more than CUs; or the weights at `rate` MB/us.  Fitted to 126
+// shapes of 1 to 32 tokens: 2.4 % slower than the best of 20 variants on average, 44 % at most; over 126 others 3.7 % and 61 %.
+struct StreamCost {
+    double call, tile, rate, power;
+};
+constexpr StreamCost kStream[2][3] = {{{4.336, 0.231, 5.265, 1.41}, {4.187, 0.394, 5.77, 1.63}, {3.993, 0.716, 5.32, 1.03}},
+                                      {{4.631, 0.055, 2.953, 1.82}, {6.803, 0.594, 2.847, 1.56}, {4.004, 1.05, 3.83, 0.81}}};
+static StreamPlan stream_plan(int64_t M, int64_t N, int64_t K) {
+    const Tuning& t = tuning();
+    StreamPlan p{};
+    if (M > 32 || (t.i8_tile >= 1 && t.i8_tile <= 3)) return p;
+    const int64_t rows = tiles_n(N), TK = i8_tiles_k(K), cus = num_cus();
+    const int mb = M > 16 ? 2 : 1;
+    double least = 1e300;
+    for (int r = 0; r < 3; ++r) {
+        if ((t.i8_rows == 1 || t.i8_rows == 2 || t.i8_rows == 4) && t.i8_rows != 1 << r) continue;
+        const StreamCost& c = kStream[mb - 1][r];
+        const int64_t force = t.i8_splits > 0 ? (t.i8_splits < TK ? t.i8_splits : TK) : 0, wgs = (rows + (1 << r) - 1) >> r;
+        for (int64_t n = force ? force : 1; n <= (force ? force : 8); n *= 2) {
+            if (n > 1 && !force && (wgs * n > 2 * cus || TK < 8 * n)) break;
+            const double load = (double)(wgs * n) / (double)cus, tiles = (double)((TK + 8 * n - 1) / (8 * n));
+            double cost = c.tile * tiles * (load > 1.0 ? pow(load, c.power) : 1.0);
+            const double bytes = (double)N * (double)K * 1e-6 / c.rate;
+            cost = c.call + (cost > bytes ? cost : bytes);
+            if (n > 1) cost += 1.09 + (double)n * (0.23 + (double)M * (double)N * 4.85e-6);
+            if (cost < least) least = cost, p = StreamPlan{1 << r, mb, (int)n};
+        }
+    }
+    double tiles_us;
+    if (t.i8_tile != 4 && t.i8_rows == 0 && rows > 8) {
+        i8_plan(M, N, K, &tiles_us);
+        if (tiles_us < least) p.tn = 0;
+    }
     return p;
 }
 static void launch_stream(const GemmI8Args& a, const StreamPlan& p, int out, hipStream_t s) {
@@ -552,64 +626,19 @@ static void launch_stream(const GemmI8Args& a, const StreamPlan& p, int out, hip
     };
     auto rows = [&](auto tn) {
         if (p.mb == 1) go(tn, std::integral_constant<int, 1>{});
-        else if (p.mb == 2) go(tn, std::integral_constant<int, 2>{});
-        else if (p.mb == 3) go(tn, std::integral_constant<int, 3>{});
-        else go(tn, std::integral_constant<int, 4>{});
+        else go(tn, std::integral_constant<int, 2>{});
     };
     if (p.tn == 1) rows(std::integral_constant<int, 1>{});
     else if (p.tn == 2) rows(std::integral_constant<int, 2>{});
     else rows(std::integral_constant<int, 4>{});
 }
 
-// The tiles: 256 x 256 with one workgroup a CU, 128 x 128 and 64 x 128 with two.  Cost in us: rounds of workgroups, each of
-// `per` stages; `alone`: a stage with one workgroup on a CU.
-struct I8Tile {
-    int tm, tn, wgs;  // wgs: a CU's
-    double stage, alone, item;
-};
-constexpr I8Tile kTiles[3] = {{256, 256, 1, 0.62, 0.62, 12.0}, {128, 128, 2, 0.385, 0.22, 4.5}, {64, 128, 2, 0.3, 0.18, 3.5}};
-static I8Plan i8_plan(int64_t M, int64_t N, int64_t K) {
-    const Tuning& t = tuning();
-    const int64_t cus = num_cus(), nst = i8_tiles_k(K);
-    I8Plan best{};
-    double least = 1e30;
-    for (int k = 0; k < 3; ++k) {
-        if (t.i8_tile >= 1 && t.i8_tile <= 3 && t.i8_tile != k + 1) continue;
-        const I8Tile& T = kTiles[k];
-        const int64_t gm = (M + T.tm - 1) / T.tm, gn = (N + T.tn - 1) / T.tn, tiles = gm * gn;
-        const int64_t force = t.i8_splits > 0 ? t.i8_splits : 0;
-        for (int64_t n = force ? force : 1; n <= (force ? force : 16); ++n) {
-            const int64_t per = (nst + n - 1) / n, splits = (nst + per - 1) / per, items = tiles * splits;
-            if (n > 1 && !force && (per < 4 || splits != n || items > 4 * cus)) continue;
-            const int64_t slots = items > cus ? T.wgs * cus : cus;
-            const int64_t rounds = (items + slots - 1) / slots;
-            double cost = (double)rounds * ((slots > cus ? T.stage : T.alone) * (double)per + T.item);
-            if (splits > 1) cost += 4.0 + (double)(M * N) * 4.0 * (double)splits * 2e-6 / 5.0;
-            if (cost < least) {
-                least = cost;
-                const int64_t cap = T.wgs * cus, up = (items + 7) / 8 * 8;
-                best = I8Plan{k, (int)(up < cap ? up : cap), (int)gm, (int)gn, (int)splits, (int)per};
-            }
-        }
-    }
-    return best;
-}
-static I8Plan unsliced(I8Plan p, int64_t K) {
-    const int64_t tiles = (int64_t)p.gm * p.gn, up = (tiles + 7) / 8 * 8;
-    if (p.grid > up) p.grid = (int)up;
-    p.splits = 1;
-    p.per = (int)i8_tiles_k(K);
-    return p;
-}
-static bool few_tokens(int64_t M) {
-    const int t = tuning().i8_tile;
-    return M <= 64 && (t < 1 || t > 3);
-}
 static size_t slices_bytes(int64_t slices, int64_t M, int64_t N) { return slices > 1 ? (size_t)slices * M * N * 4 : 0; }
 
 size_t gemm_i8_part_bytes(int64_t M, int64_t N, int64_t K) {
     if (M == 0) return 0;
-    return slices_bytes(few_tokens(M) ? stream_plan(M, N, K).slices : i8_plan(M, N, K).splits, M, N);
+    const StreamPlan p = stream_plan(M, N, K);
+    return slices_bytes(p.tn ? p.slices : i8_plan(M, N, K).splits, M, N);
 }
 template <bool VEC>
 static void launch_fold_as(const GemmI8Args& a, int splits, int out, hipStream_t s) {
@@ -624,8 +653,7 @@ static void launch_fold(const GemmI8Args& a, int splits, int out, hipStream_t s)
 }
 hipError_t launch_gemm_i8(const GemmI8Args& a, hipStream_t s) {
     const int out = a.out_acc ? kOutAcc : a.y_bf16 ? kOutBF16 : kOutF32;
-    if (few_tokens(a.M)) {
-        StreamPlan p = stream_plan(a.M, a.N, a.K);
+    if (StreamPlan p = stream_plan(a.M, a.N, a.K); p.tn) {
         if (slices_bytes(p.slices, a.M, a.N) > a.part_bytes) p.slices = 1;
         launch_stream(a, p, p.slices > 1 ? kOutPart : out, s);
         if (p.slices > 1) launch_fold(a, p.slices, out, s);
@@ -634,18 +662,19 @@ hipError_t launch_gemm_i8(const GemmI8Args& a, hipStream_t s) {
     I8Plan p = i8_plan(a.M, a.N, a.K);
     if (slices_bytes(p.splits, a.M, a.N) > a.part_bytes) p = unsliced(p, a.K);
     const int kind = p.splits > 1 ? kOutPart : out;
-    auto pick = [&](auto tm, auto tn, auto ns) {
-        constexpr int TM = decltype(tm)::value, TN = decltype(tn)::value, NS = decltype(ns)::value;
-        return kind == kOutPart ? gemm_i8_tiles<TM, TN, NS, kOutPart>
-             : kind == kOutAcc  ? gemm_i8_tiles<TM, TN, NS, kOutAcc>
-             : kind == kOutBF16 ? gemm_i8_tiles<TM, TN, NS, kOutBF16>
-                                : gemm_i8_tiles<TM, TN, NS, kOutF32>;
+    auto pick = [&](auto tm, auto tn) {
+        constexpr int TM = decltype(tm)::value, TN = decltype(tn)::value;
+        if constexpr (TM < 256)
+            if (kind == kOutPart) return gemm_i8_tiles<TM, TN, 4, kOutPart>;
+        return kind == kOutAcc    ? gemm_i8_tiles<TM, TN, 4, kOutAcc>
+               : kind == kOutBF16 ? gemm_i8_tiles<TM, TN, 4, kOutBF16>
+                                  : gemm_i8_tiles<TM, TN, 4, kOutF32>;
     };
     using std::integral_constant;
     const auto kernel =
-        p.tile == 0   ? pick(integral_constant<int, 256>{}, integral_constant<int, 256>{}, integral_constant<int, 4>{})
-        : p.tile == 1 ? pick(integral_constant<int, 128>{}, integral_constant<int, 128>{}, integral_constant<int, 4>{})
-                      : pick(integral_constant<int, 64>{}, integral_constant<int, 128>{}, integral_constant<int, 4>{});
+        p.tile == 0   ? pick(integral_constant<int, 256>{}, integral_constant<int, 256>{})
+        : p.tile == 1 ? pick(integral_constant<int, 128>{}, integral_constant<int, 128>{})
+                      : pick(integral_constant<int, 64>{}, integral_constant<int, 128>{});
     kernel<<<(unsigned)p.grid, 256, 0, s>>>(a, p);
     if (p.splits > 1) launch_fold(a, p.splits, out, s);
     return hipGetLastError();

@@ -31,9 +31,9 @@ struct Tuning {
     int group_slices;      // grouped layer, M <= 64: every K-group a slice of the grid (work item) of its own
     int mid_kernel;        // accepted, without effect
     int experts_tile;      // products of experts: 1 .. 4 as prefill_tile, 5 = a few rows at a time
-    int i8_tile;           // 8-bit product: 1 = 256 x 256 tiles, 2 = 128 x 128, 3 = 64 x 128, 4 = the stream (M <= 64)
+    int i8_tile;           // 8-bit product: 1 = 256 x 256 tiles, 2 = 128 x 128, 3 = 64 x 128, 4 = the stream (M <= 32)
     int i8_splits;         // 8-bit product: slices of K
-    int i8_rows;           // 8-bit product, M <= 64: rows of tiles a workgroup (1, 2, 4)
+    int i8_rows;           // 8-bit product, M <= 32: rows of tiles a workgroup (1, 2, 4)
 };
 const Tuning& tuning();
 
