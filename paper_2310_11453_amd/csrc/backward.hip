@@ -336,11 +336,6 @@ __device__ inline void wide_wait(v4i (&a)[4], v4i (&b)[4]) {
                    "+v"(b[3]));
 }
 
-// one operand, of block B of 32 rows
-template <int B, class OP>
-__device__ inline void wide_read(OP& x, uint32_t ad) {
-    asm volatile("ds_read_b128 %0, %1 offset:%2" : "=&v"(x) : "v"(ad), "n"(B * 2048));
-}
 // the same for 64 x 64 waves
 __device__ inline void wide_issue(v4i (&a)[2], v4i (&b)[2], uint32_t ad_a, uint32_t ad_b) {
     asm volatile(
@@ -423,9 +418,7 @@ __device__ inline v8bf wide_operand(const TrOp& a) {
     return __builtin_bit_cast(v8bf, __builtin_shufflevector(a.lo, a.hi, 0, 1, 2, 3));
 }
 
-// ROWS: A lies by rows of ex.a_pitch bytes instead of in blocks (R is a multiple of 32 then).  CT: fp32, or bf16 bits (C is
-// then rounded as it is stored; not in slices).
-template <int T, int NS, bool SPLIT, bool EXP = false, int TJ = T, bool DIRECT = false, bool ROWS = false, typename CT = float>
+template <int T, int NS, bool SPLIT, bool EXP = false, int TJ = T, bool DIRECT = false>
 __global__ __launch_bounds__(256, T + TJ == 512 ? 1 : 2) void gemm_tn_bf16_wide(const uint16_t* __restrict__ A,
                                                             const uint16_t* __restrict__ B,
                                                             int64_t I, int64_t J, int64_t Rp,
@@ -438,8 +431,6 @@ __global__ __launch_bounds__(256, T + TJ == 512 ? 1 : 2) void gemm_tn_bf16_wide(
     constexpr int A_BYTES = BM * 64, STAGE_BYTES = (BM + BN) * 64;
     static_assert((NS - 1) * P < 64, "vmcnt range");
     static_assert(!DIRECT || EXP, "rows of experts");
-    static_assert(!ROWS || !EXP, "the plain product");
-    static_assert(sizeof(CT) == 4 || (!SPLIT && !EXP), "whole sums");
     __shared__ __attribute__((aligned(1024))) uint8_t sm[NS * STAGE_BYTES];
 
     const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave), l = threadIdx.x % kWave;
@@ -529,7 +520,7 @@ __global__ __launch_bounds__(256, T + TJ == 512 ? 1 : 2) void gemm_tn_bf16_wide(
                 int row = slot >> 2;
                 const int seg = ((slot & 3) ^ ((row >> 2) & 3)) * 16;
                 if (i0 + row > I - 1) row = (int)(I - 1 - i0);
-                goffA[q] = (uint32_t)row * (ROWS ? ex.a_pitch : 64u) + seg;
+                goffA[q] = (uint32_t)row * 64 + seg;
             }
         }
 #pragma unroll
@@ -540,8 +531,7 @@ __global__ __launch_bounds__(256, T + TJ == 512 ? 1 : 2) void gemm_tn_bf16_wide(
             if (j0 + row > J - 1) row = (int)(J - 1 - j0);
             goffB[q] = (uint32_t)row * 64 + seg;
         }
-        baseA = reinterpret_cast<const uint8_t*>(A) +
-                (DIRECT ? i0 * 2 : ROWS ? i0 * ex.a_pitch + (int64_t)st0 * 64 : (st0 * I + i0) * 64);
+        baseA = reinterpret_cast<const uint8_t*>(A) + (DIRECT ? i0 * 2 : (st0 * I + i0) * 64);
         baseB = reinterpret_cast<const uint8_t*>(B) + (st0 * J + j0) * 64;
     };
     const uint32_t lds_wave = (uint32_t)(w * kWave * 16);
@@ -561,7 +551,7 @@ __global__ __launch_bounds__(256, T + TJ == 512 ? 1 : 2) void gemm_tn_bf16_wide(
             from += r * ex.a_step;
             off = (uint32_t)__umul24((uint32_t)(row < last ? row : last), ex.a_pitch) + goffA[0];
         } else {
-            from += ROWS ? (int64_t)src_st * 64 : src_st * I * 64;
+            from += src_st * I * 64;
             off = goffA[q];
         }
         __builtin_amdgcn_global_load_lds(
@@ -602,31 +592,9 @@ __global__ __launch_bounds__(256, T + TJ == 512 ? 1 : 2) void gemm_tn_bf16_wide(
     AOp ax[MI], ay[MI];
     v4i bx[NI], by[NI];
     // acc += ac x bc; an, bn = operands at ad_a, ad_b, valid on return; between(mi) is placed behind the
-    // MFMAs of row mi: the DMA of a stage, whose addresses and issue would otherwise idle the pipe.  The operands are read one
-    // behind each of the first MFMAs: all behind one another they fill the LDS queue, and the wave's next MFMA waits.  (Not where
-    // A is transposed out of LDS, by two reads an operand.)
+    // MFMAs of row mi: the DMA of a stage, whose addresses and issue would otherwise idle the pipe
     auto half_step = [&](const AOp(&ac)[MI], const v4i(&bc)[NI], AOp(&an)[MI], v4i(&bn)[NI], uint32_t ad_a,
                          uint32_t ad_b, auto between) {
-        if constexpr (!DIRECT && MI == NI) {
-            static_for<0, MI>([&](auto mc) {
-                constexpr int mi = decltype(mc)::value;
-                static_for<0, NI>([&](auto sc) {
-                    constexpr int s = decltype(sc)::value, r = mi * NI + s;
-                    acc[mi][s] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wide_operand(ac[mi]), wide_operand(bc[s]),
-                                                                         acc[mi][s], 0, 0, 0);
-                    __builtin_amdgcn_sched_barrier(0);
-                    if constexpr (r < MI + NI) {
-                        if constexpr (r % 2 == 0) wide_read<r / 2>(an[r / 2], ad_a);
-                        else wide_read<r / 2>(bn[r / 2], ad_b);
-                        __builtin_amdgcn_sched_barrier(0);
-                    }
-                });
-                between(mi);
-                __builtin_amdgcn_sched_barrier(0);
-            });
-            wide_wait(an, bn);
-            return;
-        }
 #pragma unroll
         for (int mi = 0; mi < MI; ++mi) {
 #pragma unroll
@@ -709,20 +677,7 @@ __global__ __launch_bounds__(256, T + TJ == 512 ? 1 : 2) void gemm_tn_bf16_wide(
         {
             const int64_t ib = i0 + __builtin_amdgcn_readfirstlane(wm * WTM);
             const int64_t jb = j0 + __builtin_amdgcn_readfirstlane(wn * WTN);
-            if constexpr (sizeof(CT) == 2) {
-#pragma unroll
-                for (int mi = 0; mi < MI; ++mi)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        const int64_t i = i0 + wm * WTM + 32 * mi + 8 * (r >> 2) + 4 * g2 + (r & 3);
-                        if (i >= I) continue;
-#pragma unroll
-                        for (int s = 0; s < NI; ++s) {
-                            const int64_t jj = j0 + wn * WTN + 32 * s + j;
-                            if (jj < J) reinterpret_cast<__bf16*>(C)[i * J + jj] = (__bf16)(sc * acc[mi][s][r]);
-                        }
-                    }
-            } else if constexpr (MI * NI < 16) {
+            if constexpr (MI * NI < 16) {
                 store_tile<MI, NI, true>(Cs + ib * J + jb, J, I - ib, J - jb, j, g2, [](int, int) {},
                                          [&](int mi, int r, int s) { return sc * acc[mi][s][r]; });
             } else  // with 256 accumulators the walk of store_tile spills 29 registers and gains nothing
@@ -1046,10 +1001,10 @@ __global__ __launch_bounds__(512, BM == 256 ? 2 : 4) void gemm_tn_signs_ring(con
 // out = scale * (slice 0 + slice 1 + ...), the sums a split product left.  HBM- (mostly cache-) bound.
 // VEC: 16 bytes per lane; the slices always allow it (their rows are a multiple of 32 wide), `out`
 // when it is 16-byte aligned.
-template <bool VEC, typename CT = float>
+template <bool VEC>
 __global__ __launch_bounds__(256) void fold_slices(const float* __restrict__ part, int splits,
                                                    int64_t count, const float* __restrict__ scale_ptr,
-                                                   float scale_mul, CT* __restrict__ out) {
+                                                   float scale_mul, float* __restrict__ out) {
     constexpr int E = VEC ? 4 : 1;
     const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * E;
     if (i >= count) return;
@@ -1058,13 +1013,11 @@ __global__ __launch_bounds__(256) void fold_slices(const float* __restrict__ par
         v4f v = *reinterpret_cast<const v4f*>(part + i);
 #pragma unroll 4
         for (int s = 1; s < splits; ++s) v += *reinterpret_cast<const v4f*>(part + s * count + i);
-        typedef CT v4c __attribute__((ext_vector_type(4)));
-        if constexpr (sizeof(CT) == 2) *reinterpret_cast<v4c*>(out + i) = __builtin_convertvector(v * scale, v4c);
-        else *reinterpret_cast<v4f*>(out + i) = v * scale;
+        *reinterpret_cast<v4f*>(out + i) = v * scale;
     } else {
         float v = part[i];
         for (int s = 1; s < splits; ++s) v += part[s * count + i];
-        out[i] = (CT)(v * scale);
+        out[i] = v * scale;
     }
 }
 
@@ -1236,39 +1189,22 @@ static RingPlan dw_plan(int64_t I, int64_t J, int64_t Rp) {
     return small < (full < 2 ? 1.0 : 1.02) * wide ? ring_plan(I, J, Rp, 128, 128) : p;
 }
 
-size_t gemm_tn_slices_bytes(int64_t I, int64_t J, int64_t Rp) { return slices_bytes(dw_plan(I, J, Rp), I, J); }
-
 // C[I][J] = scale * A[I][:] . B[J][:], in slices of r where the plan has them and `part` has room
-template <bool ROWS, typename CT>
-static void launch_gemm_tn_as(const TnArgs& t, hipStream_t s) {
-    RingPlan p = dw_plan(t.I, t.J, t.Rp);
-    if (slices_bytes(p, t.I, t.J) > t.part_bytes) p = unsliced(p, t.Rp);
-    ExpertsRing ex{};
-    ex.a_pitch = t.a_pitch;
+static void launch_gemm_tn(const uint16_t* A, const uint16_t* B, int64_t I, int64_t J, int64_t Rp,
+                           const float* scale_ptr, float scale_mul, float* C, float* part,
+                           size_t part_bytes, hipStream_t s) {
+    RingPlan p = dw_plan(I, J, Rp);
+    if (slices_bytes(p, I, J) > part_bytes) p = unsliced(p, Rp);
     if (p.sl.splits > 1) {
-        gemm_tn_bf16_wide<256, 4, true, false, 256, false, ROWS><<<(unsigned)p.grid, 256, 0, s>>>(
-            t.A, t.B, t.I, t.J, t.Rp, nullptr, 1.0f, t.part, p.gi, p.gj, 0, 0, p.sl, ex);
-        if constexpr (sizeof(CT) == 4) {
-            launch_fold(t.part, p, t.I * t.J, t.scale_ptr, t.scale_mul, (float*)t.C, s);
-        } else {  // (a multiple of 32 elements, 16-byte aligned)
-            const int64_t count = t.I * t.J;
-            fold_slices<true, __bf16><<<(unsigned)((count / 4 + 255) / 256), 256, 0, s>>>(t.part, p.sl.splits, count, t.scale_ptr,
-                                                                                  t.scale_mul, (__bf16*)t.C);
-        }
-        return;
-    }
-    const auto kernel = p.tile == 256 ? gemm_tn_bf16_wide<256, 4, false, false, 256, false, ROWS, CT>
-                                      : gemm_tn_bf16_wide<128, 4, false, false, 128, false, ROWS, CT>;
-    kernel<<<(unsigned)p.grid, 256, 0, s>>>(t.A, t.B, t.I, t.J, t.Rp, t.scale_ptr, t.scale_mul, (float*)t.C, p.gi, p.gj,
-                                            p.blk_i, p.blk_j, p.sl, ex);
-}
-void launch_gemm_tn(const TnArgs& t, hipStream_t s) {
-    if (t.c_bf16) {
-        if (t.a_pitch) launch_gemm_tn_as<true, uint16_t>(t, s);
-        else launch_gemm_tn_as<false, uint16_t>(t, s);
+        gemm_tn_bf16_wide<256, 4, true><<<(unsigned)p.grid, 256, 0, s>>>(
+            A, B, I, J, Rp, nullptr, 1.0f, part, p.gi, p.gj, 0, 0, p.sl, {});
+        launch_fold(part, p, I * J, scale_ptr, scale_mul, C, s);
+    } else if (p.tile == 256) {
+        gemm_tn_bf16_wide<256, 4, false><<<(unsigned)p.grid, 256, 0, s>>>(
+            A, B, I, J, Rp, scale_ptr, scale_mul, C, p.gi, p.gj, p.blk_i, p.blk_j, p.sl, {});
     } else {
-        if (t.a_pitch) launch_gemm_tn_as<true, float>(t, s);
-        else launch_gemm_tn_as<false, float>(t, s);
+        gemm_tn_bf16_wide<128, 4, false><<<(unsigned)p.grid, 256, 0, s>>>(
+            A, B, I, J, Rp, scale_ptr, scale_mul, C, p.gi, p.gj, p.blk_i, p.blk_j, p.sl, {});
     }
 }
 
@@ -1329,10 +1265,8 @@ hipError_t launch_backward(const BackwardArgs& a, hipStream_t s) {
         }
     }
     if (a.dW) {
-        TnArgs t{gwT, qT, N, K, Mp, a.per_tensor ? a.gamma : nullptr, a.per_tensor ? 1.0f / 128.0f : 1.0f, a.dW};
-        t.part = part;
-        t.part_bytes = part_bytes;
-        launch_gemm_tn(t, s);
+        launch_gemm_tn(gwT, qT, N, K, Mp, a.per_tensor ? a.gamma : nullptr,
+                       a.per_tensor ? 1.0f / 128.0f : 1.0f, a.dW, part, part_bytes, s);
     }
     return hipGetLastError();
 }

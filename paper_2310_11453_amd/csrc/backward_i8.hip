@@ -1,15 +1,13 @@
 // Straight-through backward of the 8-bit product (rounding is identity, the scales are constants):
 //   dX[M,K] = (dY * scale) W            dW[N,K] = dY^T (q * gamma / 128)
-// on the bf16 product of backward.hip, C[I][J] = sum_r A[I][r] B[J][r].  int8 codes are exact in bf16, and what is rounded is
-// rounded once: of a bf16 dY the weights' values code * scale (dX), of an fp32 dY the product dY * scale; for dW dY, with
-// gamma_m / 128 where gamma is per token (exact for a bf16 dY and one gamma a tensor).  The operands are copied into that product's
-// layout (blocks of 32 reduction indices, padded with zeros):
-//   wT [K][Np]  weights transposed     (B of dX)      qT [K][Mp]  codes transposed   (B of dW)
-//   g   [M][Np]  dY                     (A of dX)      gwT [N][Mp]  dY transposed      (A of dW)
+// on the tiles of gemm_i8.hip with bf16 operands.  int8 codes are exact in bf16, and what is rounded is rounded once: of a bf16 dY the
+// weights' values code * scale (dX), of an fp32 dY the product dY * scale; for dW dY, with gamma_m / 128 where gamma is per token
+// (exact for a bf16 dY and one gamma a tensor).  The operands are copied first, in blocks of 32 reduction indices padded with zeros:
+//   wT [Np/32][K/16] tiles of weights transposed (B of dX)      qT [Mp/32][K/16] tiles of codes transposed (B of dW)
+//   g  [Np/32][M][32] dY                          (A of dX)      gwT [Mp/32][N][32] dY transposed             (A of dW)
 // g is not made where the product can read a bf16 dY as it lies (N a multiple of 32).
 #include "common.h"
 #include "i8.h"
-#include "kernels.h"
 
 namespace bl {
 
@@ -31,8 +29,8 @@ struct CopyI8Args {
     uint32_t w_items, q_items, items, k_x, dy_x;  // items of the weights, of the codes, of all; in a row of them, of dY
 };
 
-// Bytes of 32 rows x 256 columns -> the transposed copy, 64 bytes a column.  A thread takes four columns of eight rows as
-// dwords.  LDS rows are 272 bytes.
+// Bytes of 32 rows x 256 columns -> tiles of the transposed copy: 16 columns a KiB, eight rows of a column 16 bytes.  A thread takes
+// four columns of eight rows as dwords.  LDS rows are 272 bytes.
 typedef uint8_t ByteTile[32][272];
 __device__ inline void transpose_bytes(const ByteTile& tile, uint16_t* __restrict__ out, int64_t r0, int64_t k0, int64_t K,
                                        const float (&scale)[8]) {
@@ -48,7 +46,8 @@ __device__ inline void transpose_bytes(const ByteTile& tile, uint16_t* __restric
         for (int i = 0; i < 4; ++i)
             o[i] = bf16_pair((float)(int8_t)(w[2 * i] >> (8 * j)) * scale[2 * i],
                              (float)(int8_t)(w[2 * i + 1] >> (8 * j)) * scale[2 * i + 1]);
-        *reinterpret_cast<uint4*>(out + copy_offset(k0 + 4 * kq + j, r0 + 8 * rg, K)) = make_uint4(o[0], o[1], o[2], o[3]);
+        const int64_t k = k0 + 4 * kq + j, tile = (r0 >> 5) * (K >> 4) + (k >> 4);
+        *reinterpret_cast<uint4*>(out + tile * 512 + (rg * 16 + (int)(k & 15)) * 8) = make_uint4(o[0], o[1], o[2], o[3]);
     }
 }
 
@@ -171,7 +170,7 @@ static BackwardI8Ws backward_i8_ws(int64_t M, int64_t N, int64_t K) {
 }
 size_t backward_i8_min_bytes(int64_t M, int64_t N, int64_t K) { return backward_i8_ws(M, N, K).total; }
 size_t backward_i8_bytes(int64_t M, int64_t N, int64_t K) {
-    const size_t dx = gemm_tn_slices_bytes(M, K, pad32(N)), dw = gemm_tn_slices_bytes(N, K, pad32(M));
+    const size_t dx = gemm_bf16_part_bytes(M, K, pad32(N) / 32), dw = gemm_bf16_part_bytes(N, K, pad32(M) / 32);
     return backward_i8_ws(M, N, K).total + (dx > dw ? dx : dw);
 }
 
@@ -207,22 +206,22 @@ hipError_t launch_backward_i8(const BackwardI8Args& a, hipStream_t s) {
         if (vec) copy_i8_operands<float, true><<<grid, 256, 0, s>>>(c);
         else copy_i8_operands<float, false><<<grid, 256, 0, s>>>(c);
     }
-    TnArgs t{};
-    t.part = (float*)(base + ws.total);
+    GemmBF16Args t{};
+    t.part = base + ws.total;
     t.part_bytes = a.workspace_bytes > ws.total ? a.workspace_bytes - ws.total : 0;
-    t.J = K;
+    t.N = K;
     if (a.dX) {
-        t.A = direct ? (const uint16_t*)a.dY : g;
-        t.a_pitch = direct ? (uint32_t)(N * 2) : 0;
-        t.B = wT; t.I = M; t.Rp = Np; t.scale_mul = 1.0f; t.C = a.dX; t.c_bf16 = a.dx_bf16;
-        launch_gemm_tn(t, s);
+        t.A = direct ? a.dY : g; t.B = wT;
+        t.a_pitch = direct ? N * 2 : 64; t.a_step = direct ? 64 : M * 64;
+        t.M = M; t.stages = (int)(Np / 32); t.times = 1.0f; t.y_bf16 = a.dx_bf16; t.Y = a.dX;
+        if (const hipError_t e = launch_gemm_bf16(t, s); e != hipSuccess) return e;
     }
     if (a.dW) {
-        t.A = gwT; t.a_pitch = 0; t.B = qT; t.I = N; t.Rp = Mp;
-        t.scale_ptr = a.per_tensor ? a.gamma : nullptr;
-        t.scale_mul = a.per_tensor ? 1.0f / 128.0f : 1.0f;
-        t.C = a.dW; t.c_bf16 = false;
-        launch_gemm_tn(t, s);
+        t.A = gwT; t.B = qT; t.a_pitch = 64; t.a_step = N * 64;
+        t.M = N; t.stages = (int)(Mp / 32);
+        t.factor = a.per_tensor ? a.gamma : nullptr; t.times = a.per_tensor ? 1.0f / 128.0f : 1.0f;
+        t.y_bf16 = false; t.Y = a.dW;
+        if (const hipError_t e = launch_gemm_bf16(t, s); e != hipSuccess) return e;
     }
     return hipGetLastError();
 }

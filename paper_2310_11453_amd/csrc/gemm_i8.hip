@@ -1,4 +1,4 @@
-// int8 x int8 product with scales for each token and channel:
+// int8 x int8 product with scales for each token and channel, and, in the same tiles, the bf16 products of its backward:
 //   acc[m][n] = sum_k q[m][k] * w[n][k]  (int32, at most 2^14 K <= 2^30),   Y[m][n] = float(acc) * (scale_n * (gamma_m / 128))
 #include <math.h>
 
@@ -33,7 +33,22 @@ __device__ inline void i8_wait(v4i (&a)[MI], v4i (&b)[NI]) {
         asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(a[0]), "+v"(b[0]), "+v"(b[1]));
 }
 
-enum I8Out { kOutF32 = 0, kOutBF16 = 1, kOutAcc = 2, kOutPart = 3 };  // kOutPart: a slice's int32 sums
+typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
+
+enum I8Out { kOutF32 = 0, kOutBF16 = 1, kOutAcc = 2, kOutPart = 3 };  // kOutPart: a slice's sums
+// What the tiles work on (REAL: bf16 operands, else int8).  A: 64 bytes of a row are a stage; B: 1 KiB of 16 rows.
+struct TileArgs {
+    const uint8_t *A, *B;
+    int64_t a_pitch, a_step, b_pitch, b_step;  // bytes from row to row (tile to tile), from stage to stage
+    int64_t M, N;
+    int stages;
+    bool odd;  // the last stage is half a stage: the second half of A is behind its rows, of B zeros
+    // int8: Y = float(acc) * (scale[n] * (gamma[m] / 128)); REAL: acc * (*gamma (null: 1) * times)
+    const float *gamma, *scale;
+    bool per_tensor;
+    float times;
+    void *Y, *part;
+};
 
 // Stores a wave's blocks of 32 x 32: lane (j, g2) holds columns 32 s + j, rows 32 mi + 8 rq + 4 g2 + rr.  `rowp`, a scalar that is
 // hidden from the optimiser (which would compute all the addresses ahead and spill), walks the rows; a lane's place in a row is one
@@ -41,7 +56,7 @@ enum I8Out { kOutF32 = 0, kOutBF16 = 1, kOutAcc = 2, kOutPart = 3 };  // kOutPar
 // 256 x 256 tile.  bf16, two columns to a dword: a lane packs its values of two rows, exchanges with its neighbour and stores two
 // columns of one of them, if rows begin at even elements of a 4-byte aligned output.  The output is streamed past the caches, where
 // the operands are.
-template <int OUT>
+template <bool REAL, int OUT>
 struct I8Store {
     typedef __attribute__((address_space(1))) uint8_t* gptr;
     static constexpr int ES = OUT == kOutBF16 ? 2 : 4;
@@ -49,9 +64,9 @@ struct I8Store {
     int64_t pitch, rows, cols;
     int j, g2;
     bool pairs;
-    __device__ I8Store(const GemmI8Args& a, int slice, int64_t mb, int64_t nb, int64_t rows_, int64_t cols_, int j_, int g2_)
+    __device__ I8Store(const TileArgs& a, int slice, int64_t mb, int64_t nb, int64_t rows_, int64_t cols_, int j_, int g2_)
         : pitch(a.N * ES), rows(rows_), cols(cols_), j(j_), g2(g2_) {
-        uint8_t* base = OUT == kOutPart ? reinterpret_cast<uint8_t*>(a.part) + slice * a.M * a.N * 4 : static_cast<uint8_t*>(a.Y);
+        uint8_t* base = OUT == kOutPart ? static_cast<uint8_t*>(a.part) + slice * a.M * a.N * 4 : static_cast<uint8_t*>(a.Y);
         const uint64_t at = (uint64_t)(uintptr_t)(base + mb * pitch + nb * ES);
         first = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)at) |
                 (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(at >> 32)) << 32;
@@ -83,7 +98,11 @@ struct I8Store {
 #pragma unroll
             for (int rq = 0; rq < 4; ++rq) {
                 v4f g{};
-                if constexpr (OUT == kOutF32 || OUT == kOutBF16) g = gamma(mi, rq);
+                if constexpr (!REAL && (OUT == kOutF32 || OUT == kOutBF16)) g = gamma(mi, rq);
+                auto value = [&](int s, int rr) {
+                    if constexpr (REAL) return acc[mi][s][4 * rq + rr] * sc[s];
+                    else return (float)acc[mi][s][4 * rq + rr] * (sc[s] * g[rr]);
+                };
 #pragma unroll
                 for (int rr = 0; rr < 4; rr += PAIRS ? 2 : 1) {
                     asm volatile("" : "+s"(rowp));
@@ -92,8 +111,7 @@ struct I8Store {
                     for (int s = 0; s < NI; ++s) {
                         const int r = 4 * rq + rr;
                         if constexpr (PAIRS) {
-                            const uint32_t p = bf16_pair((float)acc[mi][s][r] * (sc[s] * g[rr]),
-                                                         (float)acc[mi][s][r + 1] * (sc[s] * g[rr + 1]));
+                            const uint32_t p = bf16_pair(value(s, rr), value(s, rr + 1));
                             const uint32_t q = (uint32_t)__builtin_amdgcn_mov_dpp((int)p, 0xB1, 0xF, 0xF, true);
                             const uint32_t v = __builtin_amdgcn_perm(q, p, pick);
                             if (in && (!RAGGED || 32 * s < last))
@@ -101,11 +119,11 @@ struct I8Store {
                         } else if (in && (!RAGGED || 32 * s < last)) {
                             const gptr at = rowp + lane + 32 * ES * s;
                             if constexpr (OUT == kOutBF16)
-                                __builtin_nontemporal_store((uint16_t)bf16_pair((float)acc[mi][s][r] * (sc[s] * g[rr]), 0.f),
+                                __builtin_nontemporal_store((uint16_t)bf16_pair(value(s, rr), 0.f),
                                                             (__attribute__((address_space(1))) uint16_t*)at);
                             else if constexpr (OUT == kOutF32)
-                                __builtin_nontemporal_store((float)acc[mi][s][r] * (sc[s] * g[rr]),
-                                                            (__attribute__((address_space(1))) float*)at);
+                                __builtin_nontemporal_store(value(s, rr), (__attribute__((address_space(1))) float*)at);
+                            else if constexpr (REAL) *(__attribute__((address_space(1))) float*)at = acc[mi][s][r];
                             else *(__attribute__((address_space(1))) int32_t*)at = acc[mi][s][r];
                         }
                     }
@@ -121,8 +139,8 @@ struct I8Plan {
     int splits, per;         // slices of K, of `per` stages
 };
 
-template <int TM, int TN, int NS, int OUT>
-__global__ __launch_bounds__(256, NS * (TM + TN) * 64 > 80 * 1024 ? 1 : 2) void gemm_i8_tiles(GemmI8Args a, I8Plan p) {
+template <bool REAL, int TM, int TN, int NS, int OUT>
+__global__ __launch_bounds__(256, NS * (TM + TN) * 64 > 80 * 1024 ? 1 : 2) void gemm_i8_tiles(TileArgs a, I8Plan p) {
     constexpr int THREADS = 256, WTM = TM / 2, WTN = TN / 2, MI = WTM / 32, NI = WTN / 32;
     constexpr int PA = TM / 64, PB = TN / 64, P = PA + PB;
     constexpr int A_BYTES = TM * 64, STAGE_BYTES = A_BYTES + TN * 64;
@@ -135,9 +153,8 @@ __global__ __launch_bounds__(256, NS * (TM + TN) * 64 > 80 * 1024 ? 1 : 2) void 
 
     const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave), l = threadIdx.x % kWave;
     const int wm = w / 2, wn = w % 2, j = l & 31, g2 = l >> 5;
-    const int64_t K = a.K, TK = i8_tiles_k(K);
-    const int nst_all = (int)TK;
-    const bool odd = (K & 63) != 0;  // the last stage is half a stage
+    const int nst_all = a.stages;
+    const bool odd = !REAL && a.odd;
     int nst = nst_all, st0 = 0;
     int main_groups = 0;
 
@@ -175,17 +192,17 @@ __global__ __launch_bounds__(256, NS * (TM + TN) * 64 > 80 * 1024 ? 1 : 2) void 
         for (int q = 0; q < PA; ++q) {
             int row = (q * THREADS + (int)threadIdx.x) >> 2;
             if (m0 + row > a.M - 1) row = (int)(a.M - 1 - m0);
-            goffA[q] = (uint32_t)row * (uint32_t)K + (uint32_t)seg;
+            goffA[q] = (uint32_t)row * (uint32_t)a.a_pitch + (uint32_t)seg;
         }
 #pragma unroll
         for (int q = 0; q < PB; ++q) {
             int tile = q * 4 + w;
             const int last = (int)(tiles_n(a.N) - 1 - n0 / 16);
             if (tile > last) tile = last;
-            goffB[q] = (uint32_t)tile * (uint32_t)(TK * 1024) + (uint32_t)l * 16;
+            goffB[q] = (uint32_t)tile * (uint32_t)a.b_pitch + (uint32_t)l * 16;
         }
-        baseA = reinterpret_cast<const uint8_t*>(a.codes) + m0 * K + (int64_t)st0 * 64;
-        baseB = a.packed + (n0 / 16 * TK + st0) * 1024;
+        baseA = a.A + m0 * a.a_pitch + st0 * a.a_step;
+        baseB = a.B + n0 / 16 * a.b_pitch + st0 * a.b_step;
     };
     const uint32_t lds_wave = (uint32_t)(w * kWave * 16);
     // stage `st` into ring slot st % NS; `src` is the stage whose bytes are read (== st, or the last one when st does not
@@ -199,10 +216,10 @@ __global__ __launch_bounds__(256, NS * (TM + TN) * 64 > 80 * 1024 ? 1 : 2) void 
         if (first_kind) {
             uint32_t off = goffA[b < PA ? b : 0];
             if (odd && st0 + src == nst_all - 1) off -= (uint32_t)(seg & 32);  // uniform
-            __builtin_amdgcn_global_load_lds((const void*)(baseA + src * 64 + off),
+            __builtin_amdgcn_global_load_lds((const void*)(baseA + src * a.a_step + off),
                                              (__attribute__((address_space(3))) void*)(dst + b * THREADS * 16), 16, 0, 0);
         } else {
-            __builtin_amdgcn_global_load_lds((const void*)(baseB + src * 1024 + goffB[b < PB ? b : 0]),
+            __builtin_amdgcn_global_load_lds((const void*)(baseB + src * a.b_step + goffB[b < PB ? b : 0]),
                                              (__attribute__((address_space(3))) void*)(dst + A_BYTES + b * THREADS * 16), 16, 0,
                                              0);
         }
@@ -223,7 +240,11 @@ __global__ __launch_bounds__(256, NS * (TM + TN) * 64 > 80 * 1024 ? 1 : 2) void 
     const uint32_t b_lane[2] = {b_row + g2 * 256, b_row + (2 + g2) * 256};
     auto ring = [&](int st) { return (uint32_t)((st % NS) * STAGE_BYTES); };
 
-    v16i acc[MI][NI];
+    std::conditional_t<REAL, v16f, v16i> acc[MI][NI];
+    auto mfma = [&](const v4i& x, const v4i& y, auto& c) {
+        if constexpr (REAL) c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, x), __builtin_bit_cast(v8bf, y), c, 0, 0, 0);
+        else c = __builtin_amdgcn_mfma_i32_32x32x32_i8(x, y, c, 0, 0, 0);
+    };
     v4i ax[MI], ay[MI], bx[NI], by[NI];                              // of a half-step and the next
     v4i sa[WHOLE ? 2 : 1][2][MI], sb[WHOLE ? 2 : 1][2][NI];          // WHOLE: of the halves of a stage and of the next one
     // acc += ac x bc; an, bn = the operands at ad_a, ad_b, valid on return: one read behind each of the first MFMAs (all
@@ -234,7 +255,7 @@ __global__ __launch_bounds__(256, NS * (TM + TN) * 64 > 80 * 1024 ? 1 : 2) void 
         constexpr int MFMAS = MI * NI, READS = MI + NI, PER = (READS + MFMAS - 1) / MFMAS, LATER = MFMAS - READS / PER;
         static_for<0, MFMAS>([&](auto ic) {
             constexpr int i = decltype(ic)::value, mi = i / NI, s = i % NI;
-            acc[mi][s] = __builtin_amdgcn_mfma_i32_32x32x32_i8(ac[mi], bc[s], acc[mi][s], 0, 0, 0);
+            mfma(ac[mi], bc[s], acc[mi][s]);
             __builtin_amdgcn_sched_barrier(0);
             static_for<i * PER, (i + 1) * PER>([&](auto rc) {
                 constexpr int r = decltype(rc)::value;
@@ -291,7 +312,7 @@ __global__ __launch_bounds__(256, NS * (TM + TN) * 64 > 80 * 1024 ? 1 : 2) void 
         block_barrier();
         static_for<0, MFMAS>([&](auto ic) {
             constexpr int i = decltype(ic)::value, h = i / (MI * NI), mi = i % (MI * NI) / NI, s = i % NI;
-            acc[mi][s] = __builtin_amdgcn_mfma_i32_32x32x32_i8(sa[F][h][mi], sb[F][h][s], acc[mi][s], 0, 0, 0);
+            mfma(sa[F][h][mi], sb[F][h][s], acc[mi][s]);
             __builtin_amdgcn_sched_barrier(0);
             static_for<i * PER, (i + 1) * PER>([&](auto rc) {
                 constexpr int r = decltype(rc)::value, hr = r / (MI + NI), k = r % (MI + NI);
@@ -352,7 +373,7 @@ __global__ __launch_bounds__(256, NS * (TM + TN) * 64 > 80 * 1024 ? 1 : 2) void 
         }
 
         // the tile's factors, behind the waits of its stages
-        if constexpr (OUT == kOutF32 || OUT == kOutBF16) {
+        if constexpr (!REAL && (OUT == kOutF32 || OUT == kOutBF16)) {
             if (threadIdx.x < TM) {
                 const int64_t m = m0 + threadIdx.x;
                 sm_gamma[parity][threadIdx.x] = (a.per_tensor ? *a.gamma : a.gamma[m < a.M ? m : a.M - 1]) * (1.0f / 128.0f);
@@ -362,7 +383,8 @@ __global__ __launch_bounds__(256, NS * (TM + TN) * 64 > 80 * 1024 ? 1 : 2) void 
 #pragma unroll
         for (int s = 0; s < NI; ++s) {
             const int64_t n = n0 + wn * WTN + 32 * s + j;
-            sc[s] = OUT == kOutF32 || OUT == kOutBF16 ? a.scale[n < a.N ? n : a.N - 1] : 0.f;
+            if constexpr (REAL) sc[s] = (a.gamma ? *a.gamma : 1.0f) * a.times;
+            else sc[s] = OUT == kOutF32 || OUT == kOutBF16 ? a.scale[n < a.N ? n : a.N - 1] : 0.f;
         }
         // every wave is done with the ring (and sees the factors): start the next tile's stream, then store
         __syncthreads();
@@ -376,7 +398,7 @@ __global__ __launch_bounds__(256, NS * (TM + TN) * 64 > 80 * 1024 ? 1 : 2) void 
             issue_tile_start();
         }
         const int64_t mb = mt + __builtin_amdgcn_readfirstlane(wm * WTM), nb = nt + __builtin_amdgcn_readfirstlane(wn * WTN);
-        I8Store<OUT> st(a, sl, mb, nb, a.M - mb, a.N - nb, j, g2);
+        I8Store<REAL, OUT> st(a, sl, mb, nb, a.M - mb, a.N - nb, j, g2);
         const float* gm = sm_gamma[parity] + wm * WTM + 4 * g2;
         st.template all<MI, NI>([&](int mi, int rq) { return *reinterpret_cast<const v4f*>(gm + 32 * mi + 8 * rq); }, sc, acc);
         if (!more) break;
@@ -386,32 +408,41 @@ __global__ __launch_bounds__(256, NS * (TM + TN) * 64 > 80 * 1024 ? 1 : 2) void 
 
 // ---- slices of K added, then scaled ----------------------------------------------------------------------
 // A thread takes four channels of a token (VEC: 16 bytes of every slice, N a multiple of 4), all slices' loads in flight.
-template <int OUT, bool VEC>
-__global__ __launch_bounds__(256) void fold_i8(GemmI8Args a, int splits) {
+template <bool REAL, int OUT, bool VEC>
+__global__ __launch_bounds__(256) void fold_i8(TileArgs a, int splits) {
     constexpr int E = VEC ? 4 : 1;
+    using Sum = std::conditional_t<REAL, float, int32_t>;
+    typedef Sum Sums __attribute__((ext_vector_type(4)));
+    const Sum* const part = static_cast<const Sum*>(a.part);
     const int64_t count = a.M * a.N, n = ((int64_t)blockIdx.x * 256 + threadIdx.x) * E;
     if (n >= a.N) return;
     for (int64_t m = blockIdx.y; m < a.M; m += gridDim.y) {
         const int64_t i = m * a.N + n;
-        int32_t v[E];
+        Sum v[E];
         if constexpr (VEC) {
-            v4i t = *reinterpret_cast<const v4i*>(a.part + i);
+            Sums t = *reinterpret_cast<const Sums*>(part + i);
 #pragma unroll 4
-            for (int s = 1; s < splits; ++s) t += *reinterpret_cast<const v4i*>(a.part + s * count + i);
+            for (int s = 1; s < splits; ++s) t += *reinterpret_cast<const Sums*>(part + s * count + i);
 #pragma unroll
             for (int e = 0; e < 4; ++e) v[e] = t[e];
         } else {
-            v[0] = a.part[i];
-            for (int s = 1; s < splits; ++s) v[0] += a.part[s * count + i];
+            v[0] = part[i];
+            for (int s = 1; s < splits; ++s) v[0] += part[s * count + i];
         }
         if constexpr (OUT == kOutAcc) {
 #pragma unroll
-            for (int e = 0; e < E; ++e) static_cast<int32_t*>(a.Y)[i + e] = v[e];
+            for (int e = 0; e < E; ++e) static_cast<int32_t*>(a.Y)[i + e] = (int32_t)v[e];
         } else {
-            const float gm = (a.per_tensor ? *a.gamma : a.gamma[m]) * (1.0f / 128.0f);
             float y[E];
+            if constexpr (REAL) {
+                const float sc = (a.gamma ? *a.gamma : 1.0f) * a.times;
 #pragma unroll
-            for (int e = 0; e < E; ++e) y[e] = (float)v[e] * (a.scale[n + e] * gm);
+                for (int e = 0; e < E; ++e) y[e] = v[e] * sc;
+            } else {
+                const float gm = (a.per_tensor ? *a.gamma : a.gamma[m]) * (1.0f / 128.0f);
+#pragma unroll
+                for (int e = 0; e < E; ++e) y[e] = (float)v[e] * (a.scale[n + e] * gm);
+            }
 #pragma unroll
             for (int e = 0; e < E; ++e)
                 if constexpr (OUT == kOutBF16) static_cast<uint16_t*>(a.Y)[i + e] = (uint16_t)bf16_pair(y[e], 0.f);
@@ -542,11 +573,10 @@ constexpr int kMostSlices = 8;
 static double fold_us(double outputs, int64_t splits) {
     return splits > 1 ? kFoldUs + (double)splits * (kFoldSliceUs + outputs * 4.0 * kFoldPerByte) : 0.0;
 }
-static I8Plan i8_plan(int64_t M, int64_t N, int64_t K, double* us = nullptr) {
+static I8Plan i8_plan(int64_t M, int64_t N, int64_t nst, double bytes, double* us = nullptr) {
     const Tuning& t = tuning();
-    const int64_t cus = num_cus(), nst = i8_tiles_k(K);
-    const double outputs = (double)M * (double)N;
-    const double floor = ((double)M * (double)K + (double)N * (double)K + 2.0 * outputs) / kTrafficPerUs;
+    const int64_t cus = num_cus();
+    const double outputs = (double)M * (double)N, floor = bytes / kTrafficPerUs;
     I8Plan best{};
     double least = 1e300;
     for (int k = 0; k < 3; ++k) {
@@ -571,11 +601,19 @@ static I8Plan i8_plan(int64_t M, int64_t N, int64_t K, double* us = nullptr) {
     if (us) *us = least;
     return best;
 }
-static I8Plan unsliced(I8Plan p, int64_t K) {
+static I8Plan i8_plan_of(int64_t M, int64_t N, int64_t K, double* us = nullptr) {
+    const double m = (double)M, n = (double)N, k = (double)K;
+    return i8_plan(M, N, i8_tiles_k(K), (m + n) * k + 2.0 * m * n, us);
+}
+static I8Plan bf16_plan(int64_t M, int64_t N, int64_t stages) {
+    const double m = (double)M, n = (double)N;
+    return i8_plan(M, N, stages, (m + n) * 64.0 * (double)stages + 4.0 * m * n);
+}
+static I8Plan unsliced(I8Plan p, int stages) {
     const int64_t tiles = (int64_t)p.gm * p.gn, up = (tiles + 7) / 8 * 8;
     if (p.grid > up) p.grid = (int)up;
     p.splits = 1;
-    p.per = (int)i8_tiles_k(K);
+    p.per = stages;
     return p;
 }
 struct StreamPlan {
@@ -612,7 +650,7 @@ static StreamPlan stream_plan(int64_t M, int64_t N, int64_t K) {
     }
     double tiles_us;
     if (t.i8_tile != 4 && t.i8_rows == 0 && rows > 8) {
-        i8_plan(M, N, K, &tiles_us);
+        i8_plan_of(M, N, K, &tiles_us);
         if (tiles_us < least) p.tn = 0;
     }
     return p;
@@ -638,37 +676,33 @@ static size_t slices_bytes(int64_t slices, int64_t M, int64_t N) { return slices
 size_t gemm_i8_part_bytes(int64_t M, int64_t N, int64_t K) {
     if (M == 0) return 0;
     const StreamPlan p = stream_plan(M, N, K);
-    return slices_bytes(p.tn ? p.slices : i8_plan(M, N, K).splits, M, N);
+    return slices_bytes(p.tn ? p.slices : i8_plan_of(M, N, K).splits, M, N);
 }
-template <bool VEC>
-static void launch_fold_as(const GemmI8Args& a, int splits, int out, hipStream_t s) {
-    const int64_t per = VEC ? 1024 : 256;
+template <bool REAL>
+static void launch_fold(const TileArgs& a, int splits, int out, hipStream_t s) {
+    const bool vec = a.N % 4 == 0;
+    const int64_t per = vec ? 1024 : 256;
     const dim3 grid((unsigned)((a.N + per - 1) / per), (unsigned)(a.M < 32768 ? a.M : 32768));
-    const auto fold = out == kOutAcc ? fold_i8<kOutAcc, VEC> : out == kOutBF16 ? fold_i8<kOutBF16, VEC> : fold_i8<kOutF32, VEC>;
+    auto pick = [&](auto v) {
+        constexpr bool VEC = decltype(v)::value;
+        if constexpr (!REAL)
+            if (out == kOutAcc) return fold_i8<REAL, kOutAcc, VEC>;
+        return out == kOutBF16 ? fold_i8<REAL, kOutBF16, VEC> : fold_i8<REAL, kOutF32, VEC>;
+    };
+    const auto fold = vec ? pick(std::true_type{}) : pick(std::false_type{});
     fold<<<grid, 256, 0, s>>>(a, splits);
 }
-static void launch_fold(const GemmI8Args& a, int splits, int out, hipStream_t s) {
-    if (a.N % 4 == 0) launch_fold_as<true>(a, splits, out, s);
-    else launch_fold_as<false>(a, splits, out, s);
-}
-hipError_t launch_gemm_i8(const GemmI8Args& a, hipStream_t s) {
-    const int out = a.out_acc ? kOutAcc : a.y_bf16 ? kOutBF16 : kOutF32;
-    if (StreamPlan p = stream_plan(a.M, a.N, a.K); p.tn) {
-        if (slices_bytes(p.slices, a.M, a.N) > a.part_bytes) p.slices = 1;
-        launch_stream(a, p, p.slices > 1 ? kOutPart : out, s);
-        if (p.slices > 1) launch_fold(a, p.slices, out, s);
-        return hipGetLastError();
-    }
-    I8Plan p = i8_plan(a.M, a.N, a.K);
-    if (slices_bytes(p.splits, a.M, a.N) > a.part_bytes) p = unsliced(p, a.K);
+template <bool REAL>
+static hipError_t launch_tiles(const TileArgs& a, I8Plan p, int out, size_t part_bytes, hipStream_t s) {
+    if (slices_bytes(p.splits, a.M, a.N) > part_bytes) p = unsliced(p, a.stages);
     const int kind = p.splits > 1 ? kOutPart : out;
     auto pick = [&](auto tm, auto tn) {
         constexpr int TM = decltype(tm)::value, TN = decltype(tn)::value;
         if constexpr (TM < 256)
-            if (kind == kOutPart) return gemm_i8_tiles<TM, TN, 4, kOutPart>;
-        return kind == kOutAcc    ? gemm_i8_tiles<TM, TN, 4, kOutAcc>
-               : kind == kOutBF16 ? gemm_i8_tiles<TM, TN, 4, kOutBF16>
-                                  : gemm_i8_tiles<TM, TN, 4, kOutF32>;
+            if (kind == kOutPart) return gemm_i8_tiles<REAL, TM, TN, 4, kOutPart>;
+        if constexpr (!REAL)
+            if (kind == kOutAcc) return gemm_i8_tiles<REAL, TM, TN, 4, kOutAcc>;
+        return kind == kOutBF16 ? gemm_i8_tiles<REAL, TM, TN, 4, kOutBF16> : gemm_i8_tiles<REAL, TM, TN, 4, kOutF32>;
     };
     using std::integral_constant;
     const auto kernel =
@@ -676,8 +710,31 @@ hipError_t launch_gemm_i8(const GemmI8Args& a, hipStream_t s) {
         : p.tile == 1 ? pick(integral_constant<int, 128>{}, integral_constant<int, 128>{})
                       : pick(integral_constant<int, 64>{}, integral_constant<int, 128>{});
     kernel<<<(unsigned)p.grid, 256, 0, s>>>(a, p);
-    if (p.splits > 1) launch_fold(a, p.splits, out, s);
+    if (p.splits > 1) launch_fold<REAL>(a, p.splits, out, s);
     return hipGetLastError();
+}
+
+hipError_t launch_gemm_i8(const GemmI8Args& a, hipStream_t s) {
+    const int out = a.out_acc ? kOutAcc : a.y_bf16 ? kOutBF16 : kOutF32;
+    const int64_t TK = i8_tiles_k(a.K);
+    TileArgs t{reinterpret_cast<const uint8_t*>(a.codes), a.packed, a.K, 64, TK * 1024, 1024, a.M, a.N, (int)TK, (a.K & 63) != 0,
+               a.gamma, a.scale, a.per_tensor, 1.0f, a.Y, a.part};
+    if (StreamPlan p = stream_plan(a.M, a.N, a.K); p.tn) {
+        if (slices_bytes(p.slices, a.M, a.N) > a.part_bytes) p.slices = 1;
+        launch_stream(a, p, p.slices > 1 ? kOutPart : out, s);
+        if (p.slices > 1) launch_fold<false>(t, p.slices, out, s);
+        return hipGetLastError();
+    }
+    return launch_tiles<false>(t, i8_plan_of(a.M, a.N, a.K), out, a.part_bytes, s);
+}
+
+size_t gemm_bf16_part_bytes(int64_t M, int64_t N, int64_t stages) {
+    return M > 0 && stages > 0 ? slices_bytes(bf16_plan(M, N, stages).splits, M, N) : 0;
+}
+hipError_t launch_gemm_bf16(const GemmBF16Args& a, hipStream_t s) {
+    const TileArgs t{static_cast<const uint8_t*>(a.A), static_cast<const uint8_t*>(a.B), a.a_pitch, a.a_step, 1024, a.N / 16 * 1024,
+                     a.M, a.N, a.stages, false, a.factor, nullptr, false, a.times, a.Y, a.part};
+    return launch_tiles<true>(t, bf16_plan(a.M, a.N, a.stages), a.y_bf16 ? kOutBF16 : kOutF32, a.part_bytes, s);
 }
 
 }  // namespace bl

@@ -190,21 +190,6 @@ struct BackwardArgs {
 size_t backward_workspace_min_bytes(int64_t M, int64_t N, int64_t K);
 size_t backward_workspace_bytes(int64_t M, int64_t N, int64_t K);
 hipError_t launch_backward(const BackwardArgs& a, hipStream_t s);
-// C[I][J] = scale_mul * *scale_ptr (null: 1) * sum_r A[I][r] B[J][r] of bf16 copies in blocks of 32 r (element (row, r) of a
-// copy with R rows at ((r / 32) * R + row) * 32 + r % 32), Rp a multiple of 32
-struct TnArgs {
-    const uint16_t *A, *B;
-    int64_t I, J, Rp;
-    const float* scale_ptr;
-    float scale_mul;
-    void* C;           // fp32, or bf16 (J a multiple of 32 then, 16-byte aligned)
-    bool c_bf16;
-    uint32_t a_pitch;  // 0: A is such a copy; else it lies by rows of so many bytes, a multiple of 64, 256 of them below 2^32
-    float* part;       // room for the sums of gemm_tn_slices_bytes, or less
-    size_t part_bytes;
-};
-size_t gemm_tn_slices_bytes(int64_t I, int64_t J, int64_t Rp);
-void launch_gemm_tn(const TnArgs& t, hipStream_t s);
 
 // api_i8.hip
 size_t workspace_bytes_i8(int op, int64_t M, int64_t N, int64_t K, int granularity);

@@ -249,7 +249,7 @@ def test_backward(bl, M, K, N, dy_type, dx_type, per_tensor):
 
 
 @pytest.mark.parametrize("dy_type", [F, B])
-@pytest.mark.parametrize("spec", ["", "bwd_ring=1", "bwd_ring=2", "bwd_splits=2", "bwd_splits=16", "bwd_grid=8"])
+@pytest.mark.parametrize("spec", ["", "i8_tile=1", "i8_tile=2", "i8_tile=3", "i8_tile=2,i8_splits=3", "i8_tile=3,i8_splits=7"])
 def test_backward_exact_on_integers(bl, tuning, dy_type, spec):
     """Integer dY, powers of two as scales: every sum is exact in fp32.  N a multiple of 32 (dY read where it lies) and not,
     each tile, slices of the reductions, more tiles than workgroups."""
