@@ -71,11 +71,8 @@ __global__ __launch_bounds__((WPR < 4 ? 4 : WPR) * kWave, 4) void quant_rms_rows
     }
     for (int64_t row0 = (int64_t)blockIdx.x * RPW; row0 < a.M; row0 += (int64_t)gridDim.x * RPW) {
         int64_t row = row0 + rw;
-        const bool live = row < a.M;
-        if (!live) {
-            if (WPR == 1) break;  // no barriers behind
-            row = a.M - 1;
-        }
+        static_assert(WPR == 1 || RPW == 1, "no barriers where a workgroup has rows past the last one");
+        if (row >= a.M) break;
         if (mode == kRmsApply) row = a.M - 1 - row;
         const XT* x = static_cast<const XT*>(a.X) + row * a.K;
         const RT* r = RES ? static_cast<const RT*>(a.R) + row * a.K : nullptr;
@@ -98,7 +95,7 @@ __global__ __launch_bounds__((WPR < 4 ? 4 : WPR) * kWave, 4) void quant_rms_rows
             }
         }
         if constexpr (RES)
-            if (a.H && live) {
+            if (a.H) {
                 RT* h = static_cast<RT*>(a.H) + row * a.K;
 #pragma unroll
                 for (int j = 0; j < NV; ++j)
@@ -140,8 +137,8 @@ __global__ __launch_bounds__((WPR < 4 ? 4 : WPR) * kWave, 4) void quant_rms_rows
             }
         }
         if (mode == kRmsStats) {
-            best = fmaxf(best, m);  // (rows past the last one repeat it)
-            if (t == 0 && live) a.rstd[row] = rstd;
+            best = fmaxf(best, m);
+            if (t == 0) a.rstd[row] = rstd;
             if (WPR > 1) __syncthreads();  // the slots are read
             continue;
         }
@@ -154,16 +151,16 @@ __global__ __launch_bounds__((WPR < 4 ? 4 : WPR) * kWave, 4) void quant_rms_rows
             const int i = t + j * LANES;
             const uint32_t w = code_word(v[j].x * scale, v[j].y * scale, v[j].z * scale, v[j].w * scale);
             rs = __builtin_amdgcn_sdot4((int)w, 0x01010101, rs, false);  // (zeros past the row)
-            if (live && i < K4) {
+            if (i < K4) {
                 c4[i] = w;
                 if (a.xhat) store4(a.xhat + row * a.K, i, v[j]);
             }
         }
         if (a.rowsum) {
             rs = row_reduce<WPR>(rs, OpSum{}, smi, rw, wr);
-            if (t == 0 && live) a.rowsum[row] = rs;
+            if (t == 0) a.rowsum[row] = rs;
         }
-        if (t == 0 && live && mode == kRmsFull) a.gamma[row] = gamma;
+        if (t == 0 && mode == kRmsFull) a.gamma[row] = gamma;
         if (WPR > 1) __syncthreads();
     }
     if (mode == kRmsStats) {
