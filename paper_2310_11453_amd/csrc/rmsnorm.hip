@@ -5,6 +5,8 @@
 //   dh = (t - n * mean(t n)) / rms (+ the residual's own gradient),  dgain = sum over rows of g * n
 // The mean square and 1/rms are fp64, so that the fp32 value handed to the rounding is the correctly rounded one; what
 // decides a code behind it are single fp32 operations, as in the LayerNorm's quantiser.
+#include <type_traits>
+
 #include "common.h"
 #include "i8.h"
 #include "rowops.h"
@@ -250,7 +252,8 @@ static RmsShape rms_shape(int64_t M, int64_t K) {
     int wpr = 1;
     while (wpr < 16 && K4 > (int64_t)wpr * kWave * 8) wpr *= 4;
     while (wpr < 16 && M * wpr < 1024 && K4 >= (int64_t)wpr * kWave * 4) wpr *= 4;
-    if (wpr > 16) wpr = 16;
+    // eight waves, so that a CU holds two rows: 3705 x 9056 bf16 61 us, with sixteen 78
+    if (wpr == 16 && M > 512 && K4 <= 8 * kWave * 8) wpr = 8;
     const int64_t per_lane = (K4 + wpr * kWave - 1) / (wpr * kWave);
     int nv = 1;
     while (nv < per_lane) nv *= 2;
@@ -276,6 +279,7 @@ static int launch_rms_typed(const QuantRmsArgs& a, int mode, hipStream_t s) {
     if (sh.wpr == W && sh.nv == V) quant_rms_rows<XT, RT, RES, W, V><<<grid, nw * kWave, 0, s>>>(a, mode); else
     BL_RMS_CASE(1, 1) BL_RMS_CASE(1, 2) BL_RMS_CASE(1, 4) BL_RMS_CASE(1, 8)
     BL_RMS_CASE(4, 1) BL_RMS_CASE(4, 2) BL_RMS_CASE(4, 4) BL_RMS_CASE(4, 8)
+    BL_RMS_CASE(8, 8)
     BL_RMS_CASE(16, 1) BL_RMS_CASE(16, 2) BL_RMS_CASE(16, 4) BL_RMS_CASE(16, 8)
     return -1;
 #undef BL_RMS_CASE
@@ -307,13 +311,17 @@ hipError_t launch_quant_rmsnorm(const QuantRmsArgs& a_in, hipStream_t s) {
 
 // ---- backward -----------------------------------------------------------------------------------------
 // The workgroups are as many as fill the chip and go through the rows; a lane has the same columns of all its rows, so that
-// their share of dgain is summed (fp64) in its registers, and each workgroup leaves one sum a column for fold_dgain.  A row is
-// read once.
-// Rows past registers take half the workgroups and 64 bits.
-constexpr int64_t kRmsBackwardK = 16384;
+// their share of dgain is summed in its registers, and each workgroup leaves one sum a column for fold_dgain.  A row is
+// read once; bound by HBM.  8192 x 4096, fp32 gradient, bf16 h: 66 us (5.5 TB/s); 2048 x 16384 bf16 62 us.
+// The sums are fp64, but with eight float4 a lane (K > 16384) fp32, for which there is room, over 64 rows at most: there are
+// as many workgroups as that takes, and their sums are added in fp64.  The gradient is then read again, out of the cache,
+// where it is used, instead of kept: 1600 x 20480 bf16 76 us, against 159 with both in registers, which spill, and 193 with
+// the sums in memory.  Rows past registers (K > 32768): fp64 sums in memory.
+constexpr int64_t kRmsBackwardWide = 16384, kRmsBackwardK = 32768;
 static int rms_backward_groups(int64_t M, int64_t K) {
-    const int64_t most = K > kRmsBackwardK ? 256 : 512;
-    return (int)(M < most ? M : most);
+    if (K <= kRmsBackwardWide) return (int)(M < 512 ? M : 512);
+    const int64_t g = M < 256 ? M : 256, rows = (M + 63) / 64;
+    return (int)(K <= kRmsBackwardK && rows > g ? rows : g);
 }
 size_t rms_backward_part_bytes(int64_t M, int64_t K) {
     return (size_t)rms_backward_groups(M, K) * (size_t)K * (K > kRmsBackwardK ? 8 : 4);
@@ -321,15 +329,20 @@ size_t rms_backward_part_bytes(int64_t M, int64_t K) {
 template <typename GT, typename HT, typename DT, int WPR, int NV>
 __global__ __launch_bounds__((WPR < 8 ? 8 : WPR) * kWave, 4) void rms_backward_rows(RmsBackwardArgs a) {
     constexpr int NW = WPR < 8 ? 8 : WPR, RPW = NW / WPR, LANES = WPR * kWave;
+    constexpr bool WIDE = NV > 4;  // 32-bit sums; the residual's gradient is read where it is added
     __shared__ double smd[2][2][NW];
     __shared__ float smg[RPW > 1 ? RPW - 1 : 1][NV][LANES][4];
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave), rw = wave / WPR, wr = wave % WPR;
-    const int t = wr * kWave + (threadIdx.x & (kWave - 1)), K4 = (int)(a.K / 4);
-    double dg[NV][4];
+    int t = wr * kWave + (threadIdx.x & (kWave - 1));
+    const int K4 = (int)(a.K / 4);
+    using Sum = std::conditional_t<WIDE, float, double>;
+    Sum dg[NV][4];
 #pragma unroll
-    for (int j = 0; j < NV; ++j) dg[j][0] = dg[j][1] = dg[j][2] = dg[j][3] = 0.0;
+    for (int j = 0; j < NV; ++j) dg[j][0] = dg[j][1] = dg[j][2] = dg[j][3] = 0;
     int parity = 0;
     for (int64_t row0 = (int64_t)blockIdx.x * RPW; row0 < a.M; row0 += (int64_t)gridDim.x * RPW) {
+        // (addresses and gains are not kept from row to row, which would spill: 4096 x 8192 95 -> 79 us)
+        if constexpr (NV >= 4) asm volatile("" : "+v"(t));
         int64_t row = row0 + rw;
         const bool live = row < a.M;
         if (!live) {
@@ -339,17 +352,19 @@ __global__ __launch_bounds__((WPR < 8 ? 8 : WPR) * kWave, 4) void rms_backward_r
         const GT* g = static_cast<const GT*>(a.G) + row * a.K;
         const HT* h = static_cast<const HT*>(a.H) + row * a.K;
         const DT* dr = a.dR ? static_cast<const DT*>(a.dR) + row * a.K : nullptr;
-        float4 v[NV], u[NV], w[NV];
+        float4 v[NV], u[NV], w[WIDE ? 1 : NV];
 #pragma unroll
         for (int j = 0; j < NV; ++j) v[j] = load4(h, t + j * LANES < K4 ? t + j * LANES : K4 - 1);
 #pragma unroll
         for (int j = 0; j < NV; ++j) u[j] = load4(g, t + j * LANES < K4 ? t + j * LANES : K4 - 1);
-        if (dr)
+        if constexpr (!WIDE) {
+            if (dr)
 #pragma unroll
-            for (int j = 0; j < NV; ++j) w[j] = load4(dr, t + j * LANES < K4 ? t + j * LANES : K4 - 1);
-        else
+                for (int j = 0; j < NV; ++j) w[j] = load4(dr, t + j * LANES < K4 ? t + j * LANES : K4 - 1);
+            else
 #pragma unroll
-            for (int j = 0; j < NV; ++j) w[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+                for (int j = 0; j < NV; ++j) w[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+        }
         double q = 0.0, c = 0.0;
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
@@ -378,23 +393,28 @@ __global__ __launch_bounds__((WPR < 8 ? 8 : WPR) * kWave, 4) void rms_backward_r
         // (hidden from the optimiser, which would keep the converted copies of all elements alive)
 #pragma unroll
         for (int j = 0; j < NV; ++j) asm volatile("" : "+v"(v[j].x), "+v"(v[j].y), "+v"(v[j].z), "+v"(v[j].w));
+        if constexpr (WIDE) asm volatile("" : "+v"(t));
         DT* dh = static_cast<DT*>(a.dH) + row * a.K;
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             const int i = t + j * LANES;
             if (i < K4 && live) {
+                if constexpr (WIDE) u[j] = load4(g, i);
                 const float4 s = a.gain ? mul4(u[j], load4(a.gain, i)) : u[j];
+                float4 r = w[WIDE ? 0 : j];
+                if constexpr (WIDE) r = dr ? load4(dr, i) : make_float4(0.f, 0.f, 0.f, 0.f);
                 float4 d;
-                d.x = (s.x - v[j].x * along) * inv + w[j].x;
-                d.y = (s.y - v[j].y * along) * inv + w[j].y;
-                d.z = (s.z - v[j].z * along) * inv + w[j].z;
-                d.w = (s.w - v[j].w * along) * inv + w[j].w;
+                d.x = (s.x - v[j].x * along) * inv + r.x;
+                d.y = (s.y - v[j].y * along) * inv + r.y;
+                d.z = (s.z - v[j].z * along) * inv + r.z;
+                d.w = (s.w - v[j].w * along) * inv + r.w;
                 store4(dh, i, d);
                 if (a.dgain) {
-                    dg[j][0] = fma((double)(u[j].x * v[j].x), rstd, dg[j][0]);
-                    dg[j][1] = fma((double)(u[j].y * v[j].y), rstd, dg[j][1]);
-                    dg[j][2] = fma((double)(u[j].z * v[j].z), rstd, dg[j][2]);
-                    dg[j][3] = fma((double)(u[j].w * v[j].w), rstd, dg[j][3]);
+                    const Sum f = WIDE ? (Sum)inv : (Sum)rstd;
+                    dg[j][0] += (Sum)(u[j].x * v[j].x) * f;
+                    dg[j][1] += (Sum)(u[j].y * v[j].y) * f;
+                    dg[j][2] += (Sum)(u[j].z * v[j].z) * f;
+                    dg[j][3] += (Sum)(u[j].w * v[j].w) * f;
                 }
             }
         }
@@ -414,7 +434,7 @@ __global__ __launch_bounds__((WPR < 8 ? 8 : WPR) * kWave, 4) void rms_backward_r
 #pragma unroll
             for (int j = 0; j < NV; ++j)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) dg[j][e] += (double)smg[p][j][t][e];
+                for (int e = 0; e < 4; ++e) dg[j][e] += (Sum)smg[p][j][t][e];
     }
     float* part = static_cast<float*>(a.partials) + (int64_t)blockIdx.x * a.K;
 #pragma unroll
@@ -497,19 +517,19 @@ static int launch_rms_backward_typed(const RmsBackwardArgs& a, hipStream_t s) {
         rms_backward_long<GT, HT, DT><<<(unsigned)grid, 512, 0, s>>>(a);
         return grid;
     }
-    // two float4 a lane as long as eight waves hold a row so, then four
+    // two float4 a lane as long as eight waves hold a row so, then four, then sixteen waves
     const int64_t K4 = a.K / 4;
     int wpr = 1;
     while (wpr < 8 && K4 > (int64_t)wpr * kWave * 2) wpr *= 2;
     if (K4 > 8 * kWave * 4) wpr = 16;
-    const int nv = K4 <= kWave ? 1 : K4 <= (int64_t)wpr * kWave * 2 ? 2 : 4;
+    const int nv = K4 <= kWave ? 1 : K4 <= (int64_t)wpr * kWave * 2 ? 2 : K4 <= (int64_t)wpr * kWave * 4 ? 4 : 8;
     const int rpw = wpr < 8 ? 8 / wpr : 1, threads = wpr < 8 ? 512 : wpr * kWave;
     const int64_t wgs = (a.M + rpw - 1) / rpw;
     const int most = rms_backward_groups(a.M, a.K), grid = (int)(wgs < most ? wgs : most);
 #define BL_RMS_CASE(W, V) \
     if (wpr == W && nv == V) rms_backward_rows<GT, HT, DT, W, V><<<(unsigned)grid, threads, 0, s>>>(a); else
     BL_RMS_CASE(1, 1) BL_RMS_CASE(1, 2) BL_RMS_CASE(2, 2) BL_RMS_CASE(4, 2) BL_RMS_CASE(8, 2) BL_RMS_CASE(8, 4)
-    BL_RMS_CASE(16, 4) return -1;
+    BL_RMS_CASE(16, 4) BL_RMS_CASE(16, 8) return -1;
 #undef BL_RMS_CASE
     return grid;
 }

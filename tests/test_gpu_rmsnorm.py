@@ -186,7 +186,7 @@ def test_backward(bl, M, K, g_type, h_type, d_type):
 
 def test_backward_gain_over_many_rows(bl):
     """More rows than workgroups, and rows of zeros among them."""
-    for M, K in [(257, 96), (3001, 160), (1024, 2048), (5000, 32)]:
+    for M, K in [(257, 96), (3001, 160), (1024, 2048), (5000, 32), (600, 9056), (513, 16384)]:
         g, h = make(M, K, F, M), make(M, K, F, K)
         h[::7] = 0.0
         d_h, d_gain = bl.bitlinear_rmsnorm_backward(g.cuda(), h.cuda(), want_dgain=True, eps=0.0 if M % 2 else EPS)
@@ -196,7 +196,29 @@ def test_backward_gain_over_many_rows(bl):
         assert torch.equal(first, d_gain)  # a fixed order
 
 
-@pytest.mark.parametrize("K", [64, 4096, 40000])
+@pytest.mark.parametrize("M,K", [(300, 20480), (1100, 16416), (17000, 16416), (700, 32768)])
+def test_backward_of_wide_rows(bl, M, K):
+    """K > 16384: a column's products are summed in fp32 over a workgroup's rows: 64 at most, ceil(M / 256) where there are
+    fewer, each sum one rounding more of the sum of magnitudes; h a multiple of one row, so that the check needs little memory."""
+    gen = torch.Generator().manual_seed(K)
+    base, size = make(1, K, F, M), torch.exp(torch.randn(M, 1, generator=gen)).cuda()
+    g0 = make(1, K, F, K, 1e-3)
+    h, g = base.cuda() * size, g0.cuda() * torch.randn(M, 1, generator=gen).cuda()
+    d_h, d_gain = bl.bitlinear_rmsnorm_backward(g, h, want_dgain=True)
+    some = [0, 1, M // 2, M - 1]
+    check_backward(g[some].cpu(), h[some].cpu(), None, None, F, d_h[some], None)
+    dg, mag = torch.zeros(K, dtype=torch.float64, device="cuda"), torch.zeros(K, dtype=torch.float64, device="cuda")
+    for i in range(0, M, 500):
+        hd, gd = h[i:i + 500].double(), g[i:i + 500].double()
+        p = gd * hd / (hd.square().mean(1, keepdim=True) + EPS).sqrt()
+        dg += p.sum(0)
+        mag += p.abs().sum(0)
+    rows = min(64, -(-M // 256))
+    assert bool(((d_gain.double() - dg).abs() <= (3 + rows) * F32 * mag + F32 * dg.abs() + 1e-44).all())
+    assert torch.equal(bl.bitlinear_rmsnorm_backward(g, h, want_dgain=True)[1], d_gain)
+
+
+@pytest.mark.parametrize("K", [64, 4096, 20480, 40000])
 def test_backward_in_place(bl, K):
     """dH over the gradient of the residual, of x^, or over h."""
     for dtype in (F, B):
