@@ -443,7 +443,9 @@ int bitlinear_nonlinear_backward(const float* dXhat, const int8_t* check, const 
  *   residual   in   [M,K] of h_type or NULL: h = x, and H has to be NULL
  *   gain       in   fp32 [K] or NULL (ones)
  *   eps             >= 0 and finite (else BL_ERR_UNSUPPORTED); a row of zeros has x^ = 0 with any
- *   H          out  h, [M,K] of h_type, or NULL; may be the same buffer as X or residual where the type is the same
+ *   H          out  h, [M,K] of h_type, or NULL; may be the same buffer as X or residual where the type is the same (else
+ *                   BL_ERR_UNSUPPORTED)
+ * An infinity or a NaN spoils its row (with one gamma for the tensor everything but H), no other.
  *   codes, gamma, rowsum (or NULL), xhat_dump (or NULL)   as in bitlinear_quant_act */
 int bitlinear_quant_rmsnorm(const void* X, int x_type, const void* residual, int h_type, int64_t M, int64_t K,
                             const float* gain, float eps, int granularity, void* H, int8_t* codes, float* gamma,
@@ -456,8 +458,10 @@ int bitlinear_quant_rmsnorm(const void* X, int x_type, const void* residual, int
  *   dXhat      in   [M,K] of g_type (what bitlinear_backward_ste or bitlinear_backward_ste_i8 writes as dX)
  *   H          in   [M,K] of h_type, what the forward call wrote (or X without a residual); gain, eps as there
  *   dresidual  in   [M,K] of d_type or NULL: the gradient that reaches h past the norm
- *   dH         out  [M,K] of d_type; may be the same buffer as dresidual, dXhat or H where the type is the same
- *   dgain      out  fp32 [K] or NULL (sums in fp64, in a fixed order) */
+ *   dH         out  [M,K] of d_type; may be the same buffer as dresidual, dXhat or H where the type is the same (else
+ *                   BL_ERR_UNSUPPORTED)
+ *   dgain      out  fp32 [K] or NULL: sums in fp64, for 16384 < K <= 32768 of sums of up to 64 rows in fp32, in a fixed
+ *                   order */
 int bitlinear_rmsnorm_backward(const void* dXhat, int g_type, const void* H, int h_type, const void* dresidual,
                                int d_type, int64_t M, int64_t K, const float* gain, float eps, void* dH,
                                float* dgain, void* workspace, size_t workspace_bytes, void* stream);
@@ -531,6 +535,10 @@ int bitlinear_probe_read(const void* src, size_t bytes, int workgroups, int thre
  *   bwd_splits=n        backward ring kernels: slices of the reduction (tiles of 256 columns)
  *   experts_tile=1|2|3|4|5  products of experts: 128 x 256, 256 x 256, 128 x 128 or 64 x 128 output tiles, or a
  *                       few rows at a time
+ *   i8_tile=1|2|3|4     8-bit product: 256 x 256, 128 x 128 or 64 x 128 output tiles (also those of its backward), or, up
+ *                       to 32 tokens, the stream of the weights
+ *   i8_splits=n         8-bit product and its backward: slices of K (not in tiles of 256 x 256)
+ *   i8_rows=1|2|4       8-bit product, up to 32 tokens: rows of weight tiles a workgroup of the stream
  *   (decode_tiles, 1, 2, 4 or 8: also the weight tiles of a workgroup of that last kernel.  bwd_ring, bwd_grid,
  *   bwd_splits and quant_wpr also act on the operators of experts: bwd_splits on dW in 128 x 128 tiles, and on dX
  *   from four slices on; quant_wpr with 1, 4 or 8; bwd_dx does not, their dX has tiles of 128 x 256 only)

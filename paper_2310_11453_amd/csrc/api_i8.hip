@@ -84,6 +84,7 @@ int bitlinear_quant_rmsnorm(const void* X, int x_type, const void* residual, int
     if (!aligned16((const char*)X, (const char*)residual, (const char*)H, (const char*)gain, (const char*)codes,
                    (const char*)xhat_dump))
         return BL_ERR_UNSUPPORTED;
+    if (H && H == X && x_type != h_type) return BL_ERR_UNSUPPORTED;
     const bool per_tensor = granularity == BL_GAMMA_PER_TENSOR;
     const RmsWs ws = rms_ws(M);
     if (per_tensor && (!workspace || workspace_bytes < ws.total)) return BL_ERR_WORKSPACE;
@@ -108,6 +109,7 @@ int bitlinear_rmsnorm_backward(const void* dXhat, int g_type, const void* H, int
     if (!dXhat || !H || !dH) return BL_ERR_NULL;
     if (!aligned16((const char*)dXhat, (const char*)H, (const char*)dresidual, (const char*)gain, (const char*)dH))
         return BL_ERR_UNSUPPORTED;
+    if ((dH == dXhat && d_type != g_type) || (dH == H && d_type != h_type)) return BL_ERR_UNSUPPORTED;
     if (dgain && (!workspace || workspace_bytes < rms_backward_bytes(M, K))) return BL_ERR_WORKSPACE;
     RmsBackwardArgs a{};
     a.G = dXhat; a.H = H; a.dR = dresidual; a.dH = dH;

@@ -24,6 +24,7 @@ def lib(bl):
 
 ONE = ctypes.c_void_p(256)  # never dereferenced: every call below fails, or has nothing to do, before a launch
 ODD = ctypes.c_void_p(264)  # as little, and not 16-byte aligned
+TWO = ctypes.c_void_p(512)  # as little
 BIG = 1 << 40
 
 
@@ -44,7 +45,7 @@ def test_sizes(bl):
         assert bl.workspace_bytes(op, 8, 0, 256) == 0 and bl.workspace_bytes(op, 8, 512, 65568) == 0
 
 
-def rms(lib, X=ONE, x_type=0, R=ONE, h_type=1, M=8, K=64, gain=ONE, eps=1e-5, gran=0, H=ONE, codes=ONE, gamma=ONE,
+def rms(lib, X=ONE, x_type=0, R=ONE, h_type=1, M=8, K=64, gain=ONE, eps=1e-5, gran=0, H=TWO, codes=ONE, gamma=ONE,
         xhat=None, ws=ONE, ws_bytes=BIG):
     return lib.bitlinear_quant_rmsnorm(X, x_type, R, h_type, M, K, gain, eps, gran, H, codes, gamma, ONE, xhat, ws, ws_bytes,
                                        None)
@@ -57,13 +58,14 @@ def test_quant_rmsnorm_refusals(lib):
         assert rms(lib, eps=eps) == -3
     assert rms(lib, X=None) == -1 and rms(lib, codes=None) == -1 and rms(lib, gamma=None) == -1
     assert rms(lib, R=None) == -3  # H without a residual
+    assert rms(lib, H=ONE) == -3 and rms(lib, H=ONE, x_type=1, gran=1, ws=None) == -4  # over x of another type, of its own
     for odd in ("X", "R", "H", "gain", "codes", "xhat"):
         assert rms(lib, **{odd: ODD}) == -3
     assert rms(lib, gran=1, ws=None, ws_bytes=0) == -4 and rms(lib, gran=1, ws_bytes=32) == -4
     assert rms(lib, M=0, X=None, codes=None, gran=1, ws=None) == 0
 
 
-def rms_backward(lib, G=ONE, g_type=0, H=ONE, h_type=0, dR=ONE, d_type=0, M=8, K=64, gain=ONE, eps=1e-5, dH=ONE, dgain=ONE,
+def rms_backward(lib, G=ONE, g_type=0, H=ONE, h_type=0, dR=ONE, d_type=0, M=8, K=64, gain=ONE, eps=1e-5, dH=TWO, dgain=ONE,
                  ws=ONE, ws_bytes=BIG):
     return lib.bitlinear_rmsnorm_backward(G, g_type, H, h_type, dR, d_type, M, K, gain, eps, dH, dgain, ws, ws_bytes, None)
 
@@ -75,6 +77,9 @@ def test_rmsnorm_backward_refusals(lib):
     assert rms_backward(lib, G=None) == -1 and rms_backward(lib, H=None) == -1 and rms_backward(lib, dH=None) == -1
     for odd in ("G", "H", "dR", "gain", "dH"):
         assert rms_backward(lib, **{odd: ODD}) == -3
+    for over in ("G", "H"):  # over an operand of another type
+        assert rms_backward(lib, d_type=1, **{over: TWO}) == -3
+        assert rms_backward(lib, **{over: TWO}, ws=None) == -4
     assert rms_backward(lib, ws=None, ws_bytes=0) == -4 and rms_backward(lib, ws_bytes=64) == -4
     assert rms_backward(lib, M=0, G=None, ws=None) == 0
 

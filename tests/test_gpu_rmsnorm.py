@@ -85,12 +85,39 @@ def test_forward(bl, M, K, x_type, h_type, per_tensor):
     assert bare[4] is None and all(torch.equal(p, q) for p, q in zip(bare[:4], got[:4]))
 
 
-@pytest.mark.parametrize("K", [64, 4096, 40000])
+@pytest.mark.parametrize("M,K", [(600, 8224), (513, 16384), (2100, 8224)])
+@pytest.mark.parametrize("x_type,h_type", TYPES)
+@pytest.mark.parametrize("per_tensor", [False, True])
+def test_forward_of_many_wide_rows(bl, M, K, x_type, h_type, per_tensor):
+    """Rows that need more than four waves, and more of them than a call per tensor has workgroups; multiples of one row, so
+    that making them is quick."""
+    gen = torch.Generator().manual_seed(M)
+    size = torch.exp(torch.randn(M, 1, generator=gen))
+    x, r = (None if t is None else (make(1, K, F, K + i) * size).to(t) for i, t in enumerate((x_type, h_type)))
+    gain = 1 + 0.3 * torch.randn(K, generator=gen) if M % 2 else None
+    check_forward(x, r, gain, per_tensor, bl.bitlinear_quant_rmsnorm(x.cuda(), cuda(r), gain=cuda(gain), per_tensor=per_tensor))
+
+
+@pytest.mark.parametrize("K", [96, 4096, 9056, 20480, 40000])
+def test_a_row_of_no_numbers_stays_in_it(bl, K):
+    """Infinities and NaN in a row leave every other row's results (per token) as they are."""
+    x, r, g = make(9, K, B, 1), make(9, K, B, 2), make(9, K, B, 3)
+    bad, bad_g = x.clone(), g.clone()
+    bad[2, 5], bad[6, K - 1], bad_g[4, 7] = float("inf"), float("nan"), float("nan")
+    for rows, p, q in (([0, 1, 3, 4, 5, 7, 8], bad, g), ([0, 1, 2, 3, 5, 6, 7, 8], x, bad_g)):
+        ref, got = (bl.bitlinear_quant_rmsnorm(t.cuda(), r.cuda()) for t in (x, p))
+        assert all(torch.equal(s[rows], t[rows]) for s, t in zip(ref[:4], got[:4]))
+        ref, got = (bl.bitlinear_rmsnorm_backward(t.cuda(), h) for t, h in ((g, ref[3]), (q, got[3])))
+        assert torch.equal(ref[rows], got[rows])
+
+
+@pytest.mark.parametrize("K", [64, 4096, 9056, 40000])
 @pytest.mark.parametrize("per_tensor", [False, True])
 def test_forward_in_place(bl, K, per_tensor):
     """h written over the residual, or over x."""
     for dtype in (F, B):
-        x, r = make(37, K, dtype, 1), make(37, K, dtype, 2)
+        M = 600 if K == 9056 else 37
+        x, r = make(M, K, dtype, 1), make(M, K, dtype, 2)
         ref = bl.bitlinear_quant_rmsnorm(x.cuda(), r.cuda(), per_tensor=per_tensor)
         for over in (0, 1):
             pair = [x.cuda(), r.cuda()]
