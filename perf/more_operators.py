@@ -179,9 +179,9 @@ def _run_own(st):
             out["h"] = h
         return out
     if kind == "norm_backward":
-        d_h, d_gain = bl.bitlinear_rmsnorm_backward(st["g_"], st["h_"], gain=st["gain_"], eps=EPS, dresidual=st["d_"],
-                                                    want_dgain=st["gain"], dtype=TYPES[st["d"]])
-        return {"d_h": d_h, "d_gain": d_gain} if st["gain"] else {"d_h": d_h}
+        got = bl.bitlinear_rmsnorm_backward(st["g_"], st["h_"], gain=st["gain_"], eps=EPS, dresidual=st["d_"],
+                                            want_dgain=st["gain"], dtype=TYPES[st["d"]])
+        return {"d_h": got[0], "d_gain": got[1]} if st["gain"] else {"d_h": got}
     if kind == "pack":
         packed, scale = bl.bitlinear_pack_weights_i8(st["W"])
         return {"values": bl.bitlinear_unpack_weights_i8(packed, scale, st["N"], st["K"], dtype=torch.bfloat16),
