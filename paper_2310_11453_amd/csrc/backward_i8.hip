@@ -206,24 +206,19 @@ hipError_t launch_backward_i8(const BackwardI8Args& a, hipStream_t s) {
         if (vec) copy_i8_operands<float, true><<<grid, 256, 0, s>>>(c);
         else copy_i8_operands<float, false><<<grid, 256, 0, s>>>(c);
     }
-    GemmBF16Args t{};
-    t.part = base + ws.total;
-    t.part_bytes = a.workspace_bytes > ws.total ? a.workspace_bytes - ws.total : 0;
-    t.N = K;
-    if (a.dX) {
-        t.A = direct ? a.dY : g; t.B = wT;
-        t.a_pitch = direct ? N * 2 : 64; t.a_step = direct ? 64 : M * 64;
-        t.M = M; t.stages = (int)(Np / 32); t.times = 1.0f; t.y_bf16 = a.dx_bf16; t.Y = a.dX;
-        if (const hipError_t e = launch_gemm_bf16(t, s); e != hipSuccess) return e;
-    }
-    if (a.dW) {
-        t.A = gwT; t.B = qT; t.a_pitch = 64; t.a_step = N * 64;
-        t.M = N; t.stages = (int)(Mp / 32);
-        t.factor = a.per_tensor ? a.gamma : nullptr; t.times = a.per_tensor ? 1.0f / 128.0f : 1.0f;
-        t.y_bf16 = false; t.Y = a.dW;
-        if (const hipError_t e = launch_gemm_bf16(t, s); e != hipSuccess) return e;
-    }
-    return hipGetLastError();
+    GemmBF16Args x{};
+    x.part = base + ws.total;
+    x.part_bytes = a.workspace_bytes > ws.total ? a.workspace_bytes - ws.total : 0;
+    GemmBF16Args w = x;
+    x.A = direct ? a.dY : g; x.B = wT;
+    x.a_pitch = direct ? N * 2 : 64; x.a_step = direct ? 64 : M * 64;
+    x.M = M; x.N = K; x.stages = (int)(Np / 32); x.times = 1.0f; x.y_bf16 = a.dx_bf16; x.Y = a.dX;
+    w.A = gwT; w.B = qT; w.a_pitch = 64; w.a_step = N * 64;
+    w.M = N; w.N = K; w.stages = (int)(Mp / 32);
+    w.factor = a.per_tensor ? a.gamma : nullptr; w.times = a.per_tensor ? 1.0f / 128.0f : 1.0f;
+    w.y_bf16 = false; w.Y = a.dW;
+    if (a.dX && a.dW) return launch_gemm_bf16_two(x, w, s);
+    return launch_gemm_bf16(a.dX ? x : w, s);
 }
 
 }  // namespace bl

@@ -139,8 +139,13 @@ struct I8Plan {
     int splits, per;         // slices of K, of `per` stages
 };
 
-template <bool REAL, int TM, int TN, int NS, int OUT>
-__global__ __launch_bounds__(256, NS * (TM + TN) * 64 > 80 * 1024 ? 1 : 2) void gemm_i8_tiles(TileArgs a, I8Plan p) {
+struct SecondProduct {
+    TileArgs a;
+    I8Plan p;
+};
+// SECOND: nothing, or a SecondProduct (REAL, into kOutF32, in one slice), whose workgroups are those behind the first p.grid.
+template <bool REAL, int TM, int TN, int NS, int OUT, class... SECOND>
+__global__ __launch_bounds__(256, NS * (TM + TN) * 64 > 80 * 1024 ? 1 : 2) void gemm_i8_tiles(TileArgs a, I8Plan p, SECOND... other) {
     constexpr int THREADS = 256, WTM = TM / 2, WTN = TN / 2, MI = WTM / 32, NI = WTN / 32;
     constexpr int PA = TM / 64, PB = TN / 64, P = PA + PB;
     constexpr int A_BYTES = TM * 64, STAGE_BYTES = A_BYTES + TN * 64;
@@ -151,6 +156,17 @@ __global__ __launch_bounds__(256, NS * (TM + TN) * 64 > 80 * 1024 ? 1 : 2) void 
     __shared__ __attribute__((aligned(1024))) uint8_t sm[NS * STAGE_BYTES];
     __shared__ __attribute__((aligned(16))) float sm_gamma[2][TM];
 
+    constexpr bool TWO = sizeof...(SECOND) > 0;
+    int block = (int)blockIdx.x, grid = (int)gridDim.x;
+    bool second = false;
+    if constexpr (TWO) {
+        second = block >= p.grid;  // uniform
+        if (second) {
+            block -= p.grid;
+            (..., (a = other.a, p = other.p));
+        }
+        grid = p.grid;
+    }
     const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave), l = threadIdx.x % kWave;
     const int wm = w / 2, wn = w % 2, j = l & 31, g2 = l >> 5;
     const int nst_all = a.stages;
@@ -160,10 +176,10 @@ __global__ __launch_bounds__(256, NS * (TM + TN) * 64 > 80 * 1024 ? 1 : 2) void 
 
     // An XCD's workgroups (every eighth) take a contiguous eighth of the items: slice by slice, in bands of H rows of
     // tiles with the rows fastest, so that what an XCD runs together is about square and shares its operands in one L2.
-    const int ntiles = p.gm * p.gn, nitems = ntiles * (SPLIT ? p.splits : 1), G8 = (int)gridDim.x >> 3;
-    const int x = (int)blockIdx.x & 7;
+    const int ntiles = p.gm * p.gn, nitems = ntiles * (SPLIT ? p.splits : 1), G8 = grid >> 3;
+    const int x = block & 7;
     const int first = (int)((int64_t)nitems * x / 8), len = (int)((int64_t)nitems * (x + 1) / 8) - first;
-    int q_item = (int)blockIdx.x >> 3;
+    int q_item = block >> 3;
     if (q_item >= len) return;  // uniform for the whole workgroup
     int slice = 0;
     auto origin = [&](int item, int64_t& m0, int64_t& n0) {
@@ -398,9 +414,13 @@ __global__ __launch_bounds__(256, NS * (TM + TN) * 64 > 80 * 1024 ? 1 : 2) void 
             issue_tile_start();
         }
         const int64_t mb = mt + __builtin_amdgcn_readfirstlane(wm * WTM), nb = nt + __builtin_amdgcn_readfirstlane(wn * WTN);
-        I8Store<REAL, OUT> st(a, sl, mb, nb, a.M - mb, a.N - nb, j, g2);
         const float* gm = sm_gamma[parity] + wm * WTM + 4 * g2;
-        st.template all<MI, NI>([&](int mi, int rq) { return *reinterpret_cast<const v4f*>(gm + 32 * mi + 8 * rq); }, sc, acc);
+        auto store = [&](auto out) {
+            I8Store<REAL, decltype(out)::value> st(a, sl, mb, nb, a.M - mb, a.N - nb, j, g2);
+            st.template all<MI, NI>([&](int mi, int rq) { return *reinterpret_cast<const v4f*>(gm + 32 * mi + 8 * rq); }, sc, acc);
+        };
+        if (TWO && second) store(std::integral_constant<int, kOutF32>{});
+        else store(std::integral_constant<int, OUT>{});
         if (!more) break;
         parity ^= 1;
     }
@@ -573,14 +593,15 @@ constexpr int kMostSlices = 8;
 static double fold_us(double outputs, int64_t splits) {
     return splits > 1 ? kFoldUs + (double)splits * (kFoldSliceUs + outputs * 4.0 * kFoldPerByte) : 0.0;
 }
-static I8Plan i8_plan(int64_t M, int64_t N, int64_t nst, double bytes, double* us = nullptr) {
+static I8Plan i8_plan(int64_t M, int64_t N, int64_t nst, double bytes, double* us = nullptr, int only = -1) {
     const Tuning& t = tuning();
+    if (only < 0 && t.i8_tile >= 1 && t.i8_tile <= 3) only = t.i8_tile - 1;
     const int64_t cus = num_cus();
     const double outputs = (double)M * (double)N, floor = bytes / kTrafficPerUs;
     I8Plan best{};
     double least = 1e300;
     for (int k = 0; k < 3; ++k) {
-        if (t.i8_tile >= 1 && t.i8_tile <= 3 ? t.i8_tile != k + 1 : k == 0 && M <= 192) continue;
+        if (only >= 0 ? only != k : k == 0 && M <= 192) continue;
         const I8Tile& T = kTiles[k];
         const int64_t gm = (M + T.tm - 1) / T.tm, gn = (N + T.tn - 1) / T.tn, tiles = gm * gn;
         const int64_t force = t.i8_splits > 0 ? t.i8_splits : 0;
@@ -605,9 +626,9 @@ static I8Plan i8_plan_of(int64_t M, int64_t N, int64_t K, double* us = nullptr) 
     const double m = (double)M, n = (double)N, k = (double)K;
     return i8_plan(M, N, i8_tiles_k(K), (m + n) * k + 2.0 * m * n, us);
 }
-static I8Plan bf16_plan(int64_t M, int64_t N, int64_t stages) {
+static I8Plan bf16_plan(int64_t M, int64_t N, int64_t stages, int only = -1) {
     const double m = (double)M, n = (double)N;
-    return i8_plan(M, N, stages, (m + n) * 64.0 * (double)stages + 4.0 * m * n);
+    return i8_plan(M, N, stages, (m + n) * 64.0 * (double)stages + 4.0 * m * n, nullptr, only);
 }
 static I8Plan unsliced(I8Plan p, int stages) {
     const int64_t tiles = (int64_t)p.gm * p.gn, up = (tiles + 7) / 8 * 8;
@@ -729,12 +750,46 @@ hipError_t launch_gemm_i8(const GemmI8Args& a, hipStream_t s) {
 }
 
 size_t gemm_bf16_part_bytes(int64_t M, int64_t N, int64_t stages) {
-    return M > 0 && stages > 0 ? slices_bytes(bf16_plan(M, N, stages).splits, M, N) : 0;
+    if (M <= 0 || stages <= 0) return 0;
+    const size_t alone = slices_bytes(bf16_plan(M, N, stages).splits, M, N), beside = slices_bytes(bf16_plan(M, N, stages, 2).splits, M, N);
+    return alone > beside ? alone : beside;
+}
+static TileArgs tile_args(const GemmBF16Args& a) {
+    return TileArgs{static_cast<const uint8_t*>(a.A), static_cast<const uint8_t*>(a.B), a.a_pitch, a.a_step, 1024, a.N / 16 * 1024,
+                    a.M, a.N, a.stages, false, a.factor, nullptr, false, a.times, a.Y, a.part};
 }
 hipError_t launch_gemm_bf16(const GemmBF16Args& a, hipStream_t s) {
-    const TileArgs t{static_cast<const uint8_t*>(a.A), static_cast<const uint8_t*>(a.B), a.a_pitch, a.a_step, 1024, a.N / 16 * 1024,
-                     a.M, a.N, a.stages, false, a.factor, nullptr, false, a.times, a.Y, a.part};
-    return launch_tiles<true>(t, bf16_plan(a.M, a.N, a.stages), a.y_bf16 ? kOutBF16 : kOutF32, a.part_bytes, s);
+    return launch_tiles<true>(tile_args(a), bf16_plan(a.M, a.N, a.stages), a.y_bf16 ? kOutBF16 : kOutF32, a.part_bytes, s);
+}
+// One launch for both, in tiles that both take, where together they are at most two rounds of workgroups: 333 x 2048 x 2048 (M, N, K of
+// the layer) 31.4 -> 28.5 us, 1000 x 1024 x 1024 25.1 -> 18.3, 64 x 2048 x 2048 24.2 -> 20.7; up to four rounds it costs: 333 x 4096 x
+// 4096 64.5 -> 67.0, 256 x 8192 x 4096 91 -> 96.
+hipError_t launch_gemm_bf16_two(const GemmBF16Args& a, const GemmBF16Args& a2, hipStream_t s) {
+    I8Plan p = bf16_plan(a.M, a.N, a.stages), p2 = bf16_plan(a2.M, a2.N, a2.stages);
+    if (p.tile + p2.tile == 3) {  // 128 x 128 and 64 x 128
+        p = bf16_plan(a.M, a.N, a.stages, 2);
+        p2 = bf16_plan(a2.M, a2.N, a2.stages, 2);
+    }
+    if (slices_bytes(p.splits, a.M, a.N) > a.part_bytes) p = unsliced(p, a.stages);
+    const int64_t slots = (int64_t)num_cus() * kTiles[p.tile].wgs;
+    const int64_t items = (int64_t)p.gm * p.gn * p.splits + (int64_t)p2.gm * p2.gn;
+    if (p.tile == 0 || p.tile != p2.tile || p2.splits > 1 || a2.y_bf16 || items > 2 * slots) {
+        if (const hipError_t e = launch_gemm_bf16(a, s); e != hipSuccess) return e;
+        return launch_gemm_bf16(a2, s);
+    }
+    const TileArgs t = tile_args(a);
+    const SecondProduct t2{tile_args(a2), p2};
+    const int out = a.y_bf16 ? kOutBF16 : kOutF32, kind = p.splits > 1 ? kOutPart : out;
+    auto pick = [&](auto tm) {
+        constexpr int TM = decltype(tm)::value;
+        return kind == kOutPart   ? gemm_i8_tiles<true, TM, 128, 4, kOutPart, SecondProduct>
+               : kind == kOutBF16 ? gemm_i8_tiles<true, TM, 128, 4, kOutBF16, SecondProduct>
+                                  : gemm_i8_tiles<true, TM, 128, 4, kOutF32, SecondProduct>;
+    };
+    const auto kernel = p.tile == 1 ? pick(std::integral_constant<int, 128>{}) : pick(std::integral_constant<int, 64>{});
+    kernel<<<(unsigned)(p.grid + p2.grid), 256, 0, s>>>(t, p, t2);
+    if (p.splits > 1) launch_fold<true>(t, p.splits, out, s);
+    return hipGetLastError();
 }
 
 }  // namespace bl

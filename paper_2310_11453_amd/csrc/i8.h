@@ -105,6 +105,8 @@ struct GemmBF16Args {
 };
 size_t gemm_bf16_part_bytes(int64_t M, int64_t N, int64_t stages);
 hipError_t launch_gemm_bf16(const GemmBF16Args& a, hipStream_t s);
+// two products that do not need each other; the second is not cut into slices where they share a launch
+hipError_t launch_gemm_bf16_two(const GemmBF16Args& a, const GemmBF16Args& a2, hipStream_t s);
 
 // backward_i8.hip
 struct BackwardI8Args {
