@@ -552,6 +552,7 @@ def _scratch(need: int, workspace: torch.Tensor | None, dev):
         if not need:
             return None, 0, None
         workspace = _workspace(need, dev)
+        return workspace.data_ptr(), need, workspace
     return _given(dev, workspace, torch.uint8, workspace.numel()), workspace.numel(), workspace
 
 
