@@ -1,8 +1,9 @@
 // Straight-through backward of the 8-bit product (rounding is identity, the scales are constants):
 //   dX[M,K] = (dY * scale) W            dW[N,K] = dY^T (q * gamma / 128)
-// on the tiles of gemm_i8.hip with bf16 operands.  int8 codes are exact in bf16, and what is rounded is rounded once: of a bf16 dY the
-// weights' values code * scale (dX), of an fp32 dY the product dY * scale; for dW dY, with gamma_m / 128 where gamma is per token
-// (exact for a bf16 dY and one gamma a tensor).  The operands are copied first, in blocks of 32 reduction indices padded with zeros:
+// on the tiles of gemm_i8.hip with bf16 operands.  int8 codes are exact in bf16, and what is rounded is rounded once: of
+// a bf16 dY the weights' values code * scale (dX), of an fp32 dY the product dY * scale; for dW dY, with gamma_m / 128
+// where gamma is per token (exact for a bf16 dY and one gamma a tensor).  The operands are copied first, in blocks of 32
+// reduction indices padded with zeros:
 //   wT [Np/32][K/16] tiles of weights transposed (B of dX)      qT [Mp/32][K/16] tiles of codes transposed (B of dW)
 //   g  [Np/32][M][32] dY                          (A of dX)      gwT [Mp/32][N][32] dY transposed             (A of dW)
 // g is not made where the product can read a bf16 dY as it lies (N a multiple of 32).
@@ -29,9 +30,10 @@ struct CopyI8Args {
     uint32_t w_items, q_items, items, k_x, dy_x;  // items of the weights, of the codes, of all; in a row of them, of dY
 };
 
-// Bytes of 32 rows x 256 columns -> tiles of the transposed copy: 16 columns a KiB, eight rows of a column 16 bytes.  A wave takes
-// 64 columns and stores a tile at a time, whole lines; four lanes read the same dwords and take a byte each
-// (with stores of 16 bytes 64 apart all copies took 161 us instead of 141, 8192 x 16384 x 4096).  LDS rows are 272 bytes.
+// Bytes of 32 rows x 256 columns -> tiles of the transposed copy: 16 columns a KiB, eight rows of a column 16 bytes.  A
+// wave takes 64 columns and stores a tile at a time, whole lines; four lanes read the same dwords and take a byte each
+// (with stores of 16 bytes 64 apart all copies took 161 us instead of 141, 8192 x 16384 x 4096).  LDS rows are 272
+// bytes.
 typedef uint8_t ByteTile[32][272];
 __device__ inline void transpose_bytes(const ByteTile& tile, uint16_t* __restrict__ out, int64_t r0, int64_t k0, int64_t K,
                                        const float (&scale)[8]) {
@@ -104,8 +106,8 @@ __device__ inline void copy_dy(const CopyI8Args& a, int64_t r0, int64_t c0, Half
     }
 }
 
-// All of it in one launch, the small parts first (behind dY they would be the tail).  Bound by HBM: 8192 x 16384 x 4096, bf16 dY,
-// 840 MB in 141 us; 333 x 2048 x 2048 in 8.8 us, a chain of two trips to memory.
+// All of it in one launch, the small parts first (behind dY they would be the tail).  Bound by HBM: 8192 x 16384 x 4096,
+// bf16 dY, 840 MB in 141 us; 333 x 2048 x 2048 in 8.8 us, a chain of two trips to memory.
 template <typename IN, bool VEC>
 __global__ __launch_bounds__(256) void copy_i8_operands(CopyI8Args a) {
     __shared__ __attribute__((aligned(16))) union {
@@ -159,7 +161,8 @@ __global__ __launch_bounds__(256) void copy_i8_operands(CopyI8Args a) {
 // Whether the product reads dY where it lies: whole stages, and offsets of a tile's rows in 32 bits.
 static bool dy_direct(bool bf16, int64_t N) { return bf16 && N % 32 == 0 && N < (1 << 22); }
 
-// The copies, each 256-byte aligned, then (optional) room for the products' slices.  What is asked for does not go by the types.
+// The copies, each 256-byte aligned, then (optional) room for the products' slices.  What is asked for does not go by
+// the types.
 struct BackwardI8Ws {
     size_t wT, gwT, qT, total;
 };

@@ -10,13 +10,17 @@
 namespace bl {
 
 // ---- tiles ---------------------------------------------------------------------------------------------
-// TM x TN of the output a workgroup, four waves of a quarter each on v_mfma_i32_32x32x32_i8, persistent over the tiles.  A stage is 64 k: a
-// row of codes has 64 bytes of it, 16 channels a tile of the packed weights, both streamed global -> LDS by
-// global_load_lds_dwordx4 into a ring of NS stages.  The 16-byte pieces of a row of codes are XOR-swizzled with (row / 4) % 4;
-// the weights' tiles are the operands' own layout and need no swizzle.  The schedule is that of the bf16 product of backward.hip,
-// whose operands and stages have the same bytes: a half-step (32 k) is one MFMA for each pair of blocks, the next one's operands
-// are read behind the first row of them, and between the half-steps of stage st every wave waits for its own DMA of stage st + 1,
-// meets the others at a bare barrier and requests stage st + NS - 1 into the buffer that stage st - 1 has left.
+// TM x TN of the output a workgroup, four waves of a quarter each on v_mfma_i32_32x32x32_i8, persistent over the tiles.
+// A stage is 64 k: a row of codes has 64 bytes of it, 16 channels a tile of the packed weights, both streamed global ->
+// LDS by global_load_lds_dwordx4 into a ring of NS stages.  The 16-byte pieces of a row of codes are XOR-swizzled with
+// (row / 4) % 4; the weights' tiles are the operands' own layout and need no swizzle.  The schedule is that of the bf16
+// product of backward.hip, whose operands and stages have the same bytes: a half-step (32 k) is one MFMA for each pair
+// of blocks, the next one's operands are read one behind each of them (all behind the first ones they fill the LDS
+// queue: 4096 x 4096 -> 16384 264 us, so 254), and between the half-steps of stage st every wave waits for its own DMA
+// of stage st + 1, meets the others at a bare barrier and requests stage st + NS - 1 into the buffer that stage st - 1
+// has left.  Measured, N x K: 8192 tokens, 8192 x 8192 447 us = 2.46 POP/s; 4096 tokens, 16384 x 4096, bf16 out 246 us =
+// 2.23 POP/s, in four rounds of tiles whose starts and stores are a fifth of it; the matrix pipe is busy 56 % of the
+// cycles at 1.83 GHz, without LDS bank conflicts.  bf16 operands, 8192 x 16384 x 4096: 1.28 PFLOP/s, busy 73 % at 1.63 GHz.
 // One operand at a time, from block B of 32 rows (2 KiB in either operand); what waits for them is i8_wait.
 template <int B>
 __device__ inline void i8_read(v4i& x, uint32_t ad) {
@@ -50,12 +54,12 @@ struct TileArgs {
     void *Y, *part;
 };
 
-// Stores a wave's blocks of 32 x 32: lane (j, g2) holds columns 32 s + j, rows 32 mi + 8 rq + 4 g2 + rr.  `rowp`, a scalar that is
-// hidden from the optimiser (which would compute all the addresses ahead and spill), walks the rows; a lane's place in a row is one
-// 32-bit offset.  With the rows' bounds, a 64-bit product and branches at every store the instructions around the stores took 12 us of a
-// 256 x 256 tile.  bf16, two columns to a dword: a lane packs its values of two rows, exchanges with its neighbour and stores two
-// columns of one of them, if rows begin at even elements of a 4-byte aligned output.  The output is streamed past the caches, where
-// the operands are.
+// Stores a wave's blocks of 32 x 32: lane (j, g2) holds columns 32 s + j, rows 32 mi + 8 rq + 4 g2 + rr.  `rowp`, a
+// scalar that is hidden from the optimiser (which would compute all the addresses ahead and spill), walks the rows; a
+// lane's place in a row is one 32-bit offset.  With the rows' bounds, a 64-bit product and branches at every store the
+// instructions around the stores took 12 us of a 256 x 256 tile.  bf16, two columns to a dword: a lane packs its values
+// of two rows, exchanges with its neighbour and stores two columns of one of them, if rows begin at even elements of a
+// 4-byte aligned output.  The output is streamed past the caches, where the operands are.
 template <bool REAL, int OUT>
 struct I8Store {
     typedef __attribute__((address_space(1))) uint8_t* gptr;
@@ -92,7 +96,8 @@ struct I8Store {
         const int64_t lane = (4 * g2 + odd) * pitch + col * ES;
         const int mine = (int)(rows < 32 * MI ? rows : 32 * MI) - 4 * g2 - odd;  // this lane's rows end here
         const int last = (int)(cols < 32 * NI ? cols : 32 * NI) - col;           // and its columns
-        const uint32_t pick = odd ? 0x03020706u : 0x05040100u;  // the neighbour's second row and its own; its own first and the neighbour's
+        // the neighbour's second row and its own; its own first and the neighbour's
+        const uint32_t pick = odd ? 0x03020706u : 0x05040100u;
 #pragma unroll
         for (int mi = 0; mi < MI; ++mi)
 #pragma unroll
@@ -145,7 +150,8 @@ struct SecondProduct {
 };
 // SECOND: nothing, or a SecondProduct (REAL, into kOutF32, in one slice), whose workgroups are those behind the first p.grid.
 template <bool REAL, int TM, int TN, int NS, int OUT, class... SECOND>
-__global__ __launch_bounds__(256, NS * (TM + TN) * 64 > 80 * 1024 ? 1 : 2) void gemm_i8_tiles(TileArgs a, I8Plan p, SECOND... other) {
+__global__ __launch_bounds__(256, NS * (TM + TN) * 64 > 80 * 1024 ? 1 : 2) void gemm_i8_tiles(
+    TileArgs a, I8Plan p, SECOND... other) {
     constexpr int THREADS = 256, WTM = TM / 2, WTN = TN / 2, MI = WTM / 32, NI = WTN / 32;
     constexpr int PA = TM / 64, PB = TN / 64, P = PA + PB;
     constexpr int A_BYTES = TM * 64, STAGE_BYTES = A_BYTES + TN * 64;
@@ -258,8 +264,10 @@ __global__ __launch_bounds__(256, NS * (TM + TN) * 64 > 80 * 1024 ? 1 : 2) void 
 
     std::conditional_t<REAL, v16f, v16i> acc[MI][NI];
     auto mfma = [&](const v4i& x, const v4i& y, auto& c) {
-        if constexpr (REAL) c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, x), __builtin_bit_cast(v8bf, y), c, 0, 0, 0);
-        else c = __builtin_amdgcn_mfma_i32_32x32x32_i8(x, y, c, 0, 0, 0);
+        if constexpr (REAL)
+            c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, x), __builtin_bit_cast(v8bf, y), c, 0, 0, 0);
+        else
+            c = __builtin_amdgcn_mfma_i32_32x32x32_i8(x, y, c, 0, 0, 0);
     };
     v4i ax[MI], ay[MI], bx[NI], by[NI];                              // of a half-step and the next
     v4i sa[WHOLE ? 2 : 1][2][MI], sb[WHOLE ? 2 : 1][2][NI];          // WHOLE: of the halves of a stage and of the next one
@@ -306,7 +314,8 @@ __global__ __launch_bounds__(256, NS * (TM + TN) * 64 > 80 * 1024 ? 1 : 2) void 
         });
         if (!waited) wait_vmcnt<0>();
     };
-    // In: ax/bx = operands of (st, half 0).  Out: operands of (st + 1, half 0); for the last stage stale bytes that nobody uses.
+    // In: ax/bx = operands of (st, half 0).  Out: operands of (st + 1, half 0); for the last stage stale bytes that
+    // nobody uses.
     auto stage = [&](int st, bool ahead) {
         half_step(ax, bx, ay, by, a_lane[1] + ring(st), b_lane[1] + ring(st), [](int) {});
         if (ahead) wait_vmcnt<(NS - 3) * P>();  // younger than stage st + 1: stages st + 2 .. st + NS - 2
@@ -472,10 +481,12 @@ __global__ __launch_bounds__(256) void fold_i8(TileArgs a, int splits) {
 }
 
 // ---- up to 32 tokens: the weights' stream ------------------------------------------------------------------
-// Bound by reading the weights once.  A workgroup takes TN rows of tiles (16 TN channels) and all of K, or a slice of it; its W
-// waves share the tiles of K evenly.  A wave loads S tiles of each row with 16 bytes a lane, which is the operand of
-// v_mfma_i32_16x16x64_i8 as it lies, and the codes of MB blocks of 16 tokens beside them (from L2), while it multiplies the ones
-// before.  The waves' sums meet in LDS.  A lane has four consecutive channels of one token.
+// Bound by reading the weights once.  A workgroup takes TN rows of tiles (16 TN channels) and all of K, or a slice of
+// it; its W waves share the tiles of K evenly.  A wave loads S tiles of each row with 16 bytes a lane, which is the
+// operand of v_mfma_i32_16x16x64_i8 as it lies, and the codes of MB blocks of 16 tokens beside them (from L2), while it
+// multiplies the ones before.  The waves' sums meet in LDS.  A lane has four consecutive channels of one token.
+// One token, 28672 x 7168: 33 us = 6.2 TB/s; 16 tokens 36 us; 8192 x 2048, one token: 4.6 us, an empty launch and two trips
+// to memory.
 template <int TN, int MB, int S, int W>
 __global__ __launch_bounds__(W * 64, W * TN * MB <= 32 ? 4 : 2) void gemm_i8_stream(GemmI8Args a, int out) {
     __shared__ v4i red[W][TN * MB][kWave];
@@ -576,12 +587,12 @@ __global__ __launch_bounds__(W * 64, W * TN * MB <= 32 ? 4 : 2) void gemm_i8_str
     }
 }
 
-// The tiles: 256 x 256 with one workgroup a CU, 128 x 128 and 64 x 128 with two.  What a call costs, in us: rounds of workgroups
-// with `per` stages each (`two` us a stage with all of a CU's workgroups, `one` with a single one) and their start and stores
-// (`item`), or the operands and the output at the memory's rate; slices of K, their launch and their sums.  The constants were
-// fitted by what the choice costs, over 300 shapes of 65 to 8192 tokens, K to 16384, N to 28672: 0.6 % slower than the best of
-// 18 variants on average, 22 % at most; over 150 others 0.7 % and 14 %.  Any one tile less costs 1.4 to 10 % on average; 256 x 256 in
-// slices would gain 0.1 %.
+// The tiles: 256 x 256 with one workgroup a CU, 128 x 128 and 64 x 128 with two.  What a call costs, in us: rounds of
+// workgroups with `per` stages each (`two` us a stage with all of a CU's workgroups, `one` with a single one) and their
+// start and stores (`item`), or the operands and the output at the memory's rate; slices of K, their launch and their
+// sums.  The constants were fitted by what the choice costs, over 300 shapes of 65 to 8192 tokens, K to 16384, N to
+// 28672: 0.6 % slower than the best of 18 variants on average, 22 % at most; over 150 others 0.7 % and 14 %.  Any one
+// tile less costs 1.4 to 10 % on average; 256 x 256 in slices would gain 0.1 %.
 struct I8Tile {
     int tm, tn, wgs;  // wgs: a CU's
     double two, one, item, item_one;
@@ -640,9 +651,10 @@ static I8Plan unsliced(I8Plan p, int stages) {
 struct StreamPlan {
     int tn, mb, slices;  // rows of tiles a workgroup (0: tiles it is, of i8_plan), blocks of 16 tokens, slices of K
 };
-// Up to 32 tokens: the stream with the rows of tiles and slices that cost least, or tiles where those do.  us: `call`, and `tile` for
-// each tile of K that a wave has, (workgroups / CUs)^power where there are more than CUs; or the weights at `rate` MB/us.  Fitted to 126
-// shapes of 1 to 32 tokens: 2.4 % slower than the best of 20 variants on average, 44 % at most; over 126 others 3.7 % and 61 %.
+// Up to 32 tokens: the stream with the rows of tiles and slices that cost least, or tiles where those do.  us: `call`,
+// and `tile` for each tile of K that a wave has, (workgroups / CUs)^power where there are more than CUs; or the weights
+// at `rate` MB/us.  Fitted to 126 shapes of 1 to 32 tokens: 2.4 % slower than the best of 20 variants on average, 44 %
+// at most; over 126 others 3.7 % and 61 %.
 struct StreamCost {
     double call, tile, rate, power;
 };
@@ -751,7 +763,8 @@ hipError_t launch_gemm_i8(const GemmI8Args& a, hipStream_t s) {
 
 size_t gemm_bf16_part_bytes(int64_t M, int64_t N, int64_t stages) {
     if (M <= 0 || stages <= 0) return 0;
-    const size_t alone = slices_bytes(bf16_plan(M, N, stages).splits, M, N), beside = slices_bytes(bf16_plan(M, N, stages, 2).splits, M, N);
+    const size_t alone = slices_bytes(bf16_plan(M, N, stages).splits, M, N);
+    const size_t beside = slices_bytes(bf16_plan(M, N, stages, 2).splits, M, N);
     return alone > beside ? alone : beside;
 }
 static TileArgs tile_args(const GemmBF16Args& a) {
@@ -761,9 +774,9 @@ static TileArgs tile_args(const GemmBF16Args& a) {
 hipError_t launch_gemm_bf16(const GemmBF16Args& a, hipStream_t s) {
     return launch_tiles<true>(tile_args(a), bf16_plan(a.M, a.N, a.stages), a.y_bf16 ? kOutBF16 : kOutF32, a.part_bytes, s);
 }
-// One launch for both, in tiles that both take, where together they are at most two rounds of workgroups: 333 x 2048 x 2048 (M, N, K of
-// the layer) 31.4 -> 28.5 us, 1000 x 1024 x 1024 25.1 -> 18.3, 64 x 2048 x 2048 24.2 -> 20.7; up to four rounds it costs: 333 x 4096 x
-// 4096 64.5 -> 67.0, 256 x 8192 x 4096 91 -> 96.
+// One launch for both, in tiles that both take, where together they are at most two rounds of workgroups: 333 x 2048 x
+// 2048 (M, N, K of the layer) 31.4 -> 28.5 us, 1000 x 1024 x 1024 25.1 -> 18.3, 64 x 2048 x 2048 24.2 -> 20.7; up to
+// four rounds it costs: 333 x 4096 x 4096 64.5 -> 67.0, 256 x 8192 x 4096 91 -> 96.
 hipError_t launch_gemm_bf16_two(const GemmBF16Args& a, const GemmBF16Args& a2, hipStream_t s) {
     I8Plan p = bf16_plan(a.M, a.N, a.stages), p2 = bf16_plan(a2.M, a2.N, a2.stages);
     if (p.tile + p2.tile == 3) {  // 128 x 128 and 64 x 128

@@ -88,10 +88,10 @@ struct GemmI8Args {
 size_t gemm_i8_part_bytes(int64_t M, int64_t N, int64_t K);
 hipError_t launch_gemm_i8(const GemmI8Args& a, hipStream_t s);
 
-// The same tiles for the bf16 products of the backward, Y[m][n] = factor * sum_r A[m][r] B[n][r]: stages of 32 r.  A: 64 bytes of
-// a row are a stage, a_pitch bytes from row to row (256 of them below 2^32), a_step from a stage to the next, all 16-byte aligned;
-// B: 16 rows of a stage are a tile of 1 KiB, lane g*16 + c of it the elements 8 g .. 8 g + 7 of row c; tiles one after another
-// [stage][N / 16], N a multiple of 16.
+// The same tiles for the bf16 products of the backward, Y[m][n] = factor * sum_r A[m][r] B[n][r]: stages of 32 r.  A: 64
+// bytes of a row are a stage, a_pitch bytes from row to row (256 of them below 2^32), a_step from a stage to the next,
+// all 16-byte aligned; B: 16 rows of a stage are a tile of 1 KiB, lane g*16 + c of it the elements 8 g .. 8 g + 7 of row
+// c; tiles one after another [stage][N / 16], N a multiple of 16.
 struct GemmBF16Args {
     const void *A, *B;
     int64_t a_pitch, a_step, M, N;

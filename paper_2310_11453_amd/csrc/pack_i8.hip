@@ -12,9 +12,10 @@ namespace bl {
 // m below this has no 127 / m in fp32: its codes have a step of 2^-127
 constexpr float kLeastMost = 127.f * 0x1p-127f;
 
-// Eight rows, half a tile, a workgroup: WR waves a row, whose 16 float4 a lane lie in registers, so that rows of 4096 WR are read
-// once; of longer ones all but the last chunk is read again, from the end, out of the caches.  The codes go through LDS and leave
-// as whole lines of 128 bytes: eight rows of 16 columns.  Bound by HBM.
+// Eight rows, half a tile, a workgroup: WR waves a row, whose 16 float4 a lane lie in registers, so that rows of 4096 WR
+// are read once; of longer ones all but the last chunk is read again, from the end, out of the caches.  The codes go
+// through LDS and leave as whole lines of 128 bytes: eight rows of 16 columns.  Bound by HBM: 16384 x 4096 fp32
+// 75 us (4.5 TB/s), 2048 x 8192 bf16 14 us (3.6).
 __device__ inline uint32_t load_codes(const int8_t* p, int64_t i4) { return reinterpret_cast<const uint32_t*>(p)[i4]; }
 template <typename T, int WR>
 __global__ __launch_bounds__(512 * WR, 4) void pack_i8_rows(PackI8Args a) {
@@ -102,8 +103,9 @@ hipError_t launch_pack_i8(const PackI8Args& a, hipStream_t s) {
     return hipGetLastError();
 }
 
-// A workgroup takes 2048 columns of the eight rows that share lines of 128 bytes, a wave a row: eight dwords a lane, all in flight
-// before the first is used.  (Rows dealt to workgroups without regard to the lines: with the quantiser 107 -> 131 us, 16384 x 4096.)
+// A workgroup takes 2048 columns of the eight rows that share lines of 128 bytes, a wave a row: eight dwords a lane, all
+// in flight before the first is used: 16384 x 4096 to bf16 32 us (6.3 TB/s).  (Rows dealt to workgroups without regard to the lines: with the quantiser 107 ->
+// 131 us, 16384 x 4096.)
 constexpr int kUnpackColumns = 2048;
 template <int TYPE>
 __global__ __launch_bounds__(512) void unpack_i8_rows(UnpackI8Args a, int64_t items, int64_t pieces) {
