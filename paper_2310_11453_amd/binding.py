@@ -763,7 +763,7 @@ def bitlinear_quant_rmsnorm(X: torch.Tensor, residual: torch.Tensor | None = Non
     if residual is not None:
         h_type, res = _float_type(residual.dtype), _given(dev, residual, residual.dtype, M, K)
         h = torch.empty((M, K), dtype=residual.dtype, device=dev) if out is None else out
-        h_ptr = _given(dev, h, residual.dtype, M, K)
+        h_ptr = h.data_ptr() if out is None else _given(dev, h, residual.dtype, M, K)
     elif out is not None:
         raise BitLinearError("out without a residual: h is X")
     ws, ws_bytes, _keep = _scratch(workspace_bytes(OP_QUANT_RMSNORM, M, 1, K, True) if per_tensor else 0, workspace, dev)
@@ -788,13 +788,16 @@ def bitlinear_rmsnorm_backward(dXhat: torch.Tensor, H: torch.Tensor, gain: torch
     d_type = _float_type(dtype)
     if out is None:
         out = torch.empty((M, K), dtype=dtype, device=dev)
+        d_h = out.data_ptr()
+    else:
+        d_h = _given(dev, out, dtype, M, K)
     dgain = (torch.empty if M else torch.zeros)(K, dtype=torch.float32, device=dev) if want_dgain else None
     need = workspace_bytes(OP_RMSNORM_BACKWARD, M, 1, K) if want_dgain else 0
     ws, ws_bytes, _keep = _scratch(need, workspace, dev)
     _check(lib.bitlinear_rmsnorm_backward(
         _ptr(dXhat), _float_type(dXhat.dtype), _given(dev, H, H.dtype, M, K), _float_type(H.dtype),
         None if dresidual is None else _given(dev, dresidual, dtype, M, K), d_type, M, K,
-        None if gain is None else _given(dev, gain, torch.float32, K), eps, _given(dev, out, dtype, M, K), _ptr(dgain), ws,
+        None if gain is None else _given(dev, gain, torch.float32, K), eps, d_h, None if dgain is None else dgain.data_ptr(), ws,
         ws_bytes, _queue(dev)), "bitlinear_rmsnorm_backward")
     return (out, dgain) if want_dgain else out
 
@@ -842,12 +845,15 @@ def bitlinear_matmul_i8(codes: torch.Tensor, gamma: torch.Tensor | None, packed:
     dtype = torch.int32 if flags & FLAG_OUT_ACC_I32 else dtype
     if out is None:
         out = torch.empty((M, N), dtype=dtype, device=dev)
+        y = out.data_ptr()
+    else:
+        y = _given(dev, out, dtype, M, N)
     ws, ws_bytes, _keep = _scratch(workspace_bytes(OP_MATMUL_I8, M, N, K), workspace, dev)
     _check(lib.bitlinear_matmul_i8(
         _ptr(codes, torch.int8), None if gamma is None else _given(dev, gamma, torch.float32, 1 if per_tensor else M), M, K,
         _given(dev, packed, torch.uint8, _blob_bytes_i8(N, K)), N,
-        None if scale is None else _given(dev, scale, torch.float32, N), _gran(per_tensor), flags, y_type,
-        _given(dev, out, dtype, M, N), ws, ws_bytes, _queue(dev)), "bitlinear_matmul_i8")
+        None if scale is None else _given(dev, scale, torch.float32, N), _gran(per_tensor), flags, y_type, y, ws,
+        ws_bytes, _queue(dev)), "bitlinear_matmul_i8")
     return out
 
 
