@@ -381,6 +381,47 @@ def test_a_training_step(bl, M, per_tensor):
     assert bool(((dW.cpu().double() - ww.grad).abs() <= (once + (M + 4) * F32) * (dy.double().abs().T @ q.abs())).all())
 
 
+@pytest.mark.parametrize("M,K,N", [(1, 96, 40), (20, 4096, 72), (333, 2080, 520), (700, 256, 1000), (70, 8192, 264)])
+@pytest.mark.parametrize("per_tensor", [False, True])
+def test_workspaces_need_no_clearing(bl, M, K, N, per_tensor):
+    """Whatever the workspaces hold, NaN in every format among it, the results are the same."""
+    g = torch.Generator().manual_seed(M)
+    packed, scale = bl.bitlinear_pack_weights_i8((0.02 * torch.randn(N, K, generator=g)).cuda())
+    x, r = torch.randn(M, K, generator=g).cuda(), torch.randn(M, K, generator=g).cuda()
+    dy = torch.randn(M, N, generator=g).cuda()
+    sizes = (bl.workspace_bytes(bl.OP_QUANT_RMSNORM, M, 1, K, True), bl.workspace_bytes(bl.OP_MATMUL_I8, M, N, K),
+             bl.workspace_bytes(bl.OP_BACKWARD_I8, M, N, K), bl.workspace_bytes(bl.OP_RMSNORM_BACKWARD, M, 1, K))
+    results = []
+    for byte in (0, 255):
+        ws = [torch.full((max(n, 256),), byte, dtype=torch.uint8, device="cuda") for n in sizes]
+        codes, gamma, rowsum, h, _ = bl.bitlinear_quant_rmsnorm(x, r, per_tensor=per_tensor, workspace=ws[0])
+        y = bl.bitlinear_matmul_i8(codes, gamma, packed, N, scale, per_tensor=per_tensor, workspace=ws[1])
+        got = [codes, gamma, rowsum, h, y]
+        for grad in (dy, dy.to(B)):
+            ws[2].fill_(byte)
+            dX, dW = bl.bitlinear_backward_ste_i8(grad, codes, gamma, packed, scale, per_tensor=per_tensor, workspace=ws[2])
+            got += [dX, dW, *bl.bitlinear_rmsnorm_backward(dX, h, want_dgain=True, workspace=ws[3].fill_(byte))]
+        results.append(got)
+    assert all(torch.equal(p, q) and bool(p.isfinite().all()) for p, q in zip(*results))
+
+
+@pytest.mark.parametrize("dx_type", [F, B])
+@pytest.mark.parametrize("M,K,N", [(333, 2048, 2048), (64, 2048, 2048), (1000, 1024, 1024), (333, 4096, 1024), (2048, 1024, 1024)])
+def test_backward_together_and_apart(bl, M, K, N, dx_type):
+    """Both gradients of a call against those of a call for each; dY and the scale are powers of two and small integers, so
+    that every sum is exact in fp32 and a bf16 result rounds the same number."""
+    g = torch.Generator().manual_seed(M + N)
+    codes = torch.randint(-128, 128, (M, K), generator=g, dtype=I8).cuda()
+    packed, _ = bl.bitlinear_pack_weights_i8(torch.randint(-127, 128, (N, K), generator=g, dtype=I8).cuda())
+    gamma, scale = torch.full((1,), 0.5, device="cuda"), torch.full((N,), 0.25, device="cuda")
+    dy = torch.randint(-4, 5, (M, N), generator=g).to(B).cuda()
+    call = lambda **kw: bl.bitlinear_backward_ste_i8(dy, codes, gamma, packed, scale, per_tensor=True, dtype=dx_type, **kw)  # noqa: E731
+    dX, dW = call()
+    assert torch.equal(dX, call(want_dw=False)[0]) and torch.equal(dW, call(want_dx=False)[1])
+    tight = torch.empty(bl.workspace_bytes(bl.OP_BACKWARD_I8, M, N, K), dtype=torch.uint8, device="cuda")
+    assert all(torch.equal(p, q) for p, q in zip((dX, dW), call(workspace=tight)))
+
+
 @pytest.mark.parametrize("M", [1, 40, 200])
 def test_captured_and_replayed(bl, M):
     """A layer and its backward in a graph, replayed with other inputs and eager work between the replays, on a stream of its
