@@ -59,7 +59,7 @@ __device__ inline float tensor_most(const QuantRmsArgs& a, float* sm) {
 // WPR waves share a row, which lies in their registers (NV float4 a lane) from its one reading on; workgroups have four
 // waves at least, so short rows are handled several to a workgroup, without a barrier.  Bound by HBM for large batches,
 // by the length of a row's chain for small ones (one reduction without a gain: the largest |x^| is then that of the
-// largest |h|).  8192 x 4096, fp32, residual, per token 79 us (5.5 TB/s); per tensor two passes of 72 and 42 us; one row of
+// largest |h|).  8192 x 4096, fp32, residual, per token 79 us (5.5 TB/s); per tensor both passes 102 us; one row of
 // 2048 2.8 us.
 template <typename XT, typename RT, bool RES, int WPR, int NV>
 __global__ __launch_bounds__((WPR < 4 ? 4 : WPR) * kWave, 4) void quant_rms_rows(QuantRmsArgs a, int mode) {
@@ -69,22 +69,28 @@ __global__ __launch_bounds__((WPR < 4 ? 4 : WPR) * kWave, 4) void quant_rms_rows
     __shared__ int smi[NW];
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave), rw = wave / WPR, wr = wave % WPR;
     const int t = wr * kWave + (threadIdx.x & (kWave - 1)), K4 = (int)(a.K / 4);
+    // a row's loads before the last one's sum and barriers (with a residual there is no room for them)
+    constexpr bool AHEAD = !RES;
     float gamma = 0.f, best = 0.f;
+    float4 v[NV];
+    // unconditional (the last piece again past the row), so that all are in flight before the first is needed
+    auto load_x = [&](int64_t row) {
+        const XT* x = static_cast<const XT*>(a.X) + (mode == kRmsApply ? a.M - 1 - row : row) * a.K;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) v[j] = load4(x, t + j * LANES < K4 ? t + j * LANES : K4 - 1);
+    };
+    const int64_t first = (int64_t)blockIdx.x * RPW + rw, stride = (int64_t)gridDim.x * RPW;
+    if (AHEAD) load_x(first < a.M ? first : a.M - 1);
     if (mode == kRmsApply) {
         gamma = fmaxf(tensor_most<NW>(a, smf[0]), 1e-5f);
         if (blockIdx.x == 0 && threadIdx.x == 0) *a.gamma = gamma;
     }
-    for (int64_t row0 = (int64_t)blockIdx.x * RPW; row0 < a.M; row0 += (int64_t)gridDim.x * RPW) {
-        int64_t row = row0 + rw;
-        static_assert(WPR == 1 || RPW == 1, "no barriers where a workgroup has rows past the last one");
-        if (row >= a.M) break;
-        if (mode == kRmsApply) row = a.M - 1 - row;
-        const XT* x = static_cast<const XT*>(a.X) + row * a.K;
+    static_assert(WPR == 1 || RPW == 1, "no barriers where a workgroup has rows past the last one");
+    for (int64_t at = first; at < a.M; at += stride) {
+        const int64_t row = mode == kRmsApply ? a.M - 1 - at : at;
         const RT* r = RES ? static_cast<const RT*>(a.R) + row * a.K : nullptr;
-        float4 v[NV], u[RES ? NV : 1];
-        // unconditional (the last piece again past the row), so that all are in flight before the first is needed
-#pragma unroll
-        for (int j = 0; j < NV; ++j) v[j] = load4(x, t + j * LANES < K4 ? t + j * LANES : K4 - 1);
+        float4 u[RES ? NV : 1];
+        if (!AHEAD) load_x(at);
         if constexpr (RES)
 #pragma unroll
             for (int j = 0; j < NV; ++j) u[j] = load4(r, t + j * LANES < K4 ? t + j * LANES : K4 - 1);
@@ -144,6 +150,7 @@ __global__ __launch_bounds__((WPR < 4 ? 4 : WPR) * kWave, 4) void quant_rms_rows
         if (mode == kRmsStats) {
             best = fmaxf(best, m);
             if (t == 0) a.rstd[row] = rstd;
+            if (AHEAD && at + stride < a.M) load_x(at + stride);
             if (WPR > 1) __syncthreads();  // the slots are read
             continue;
         }
@@ -161,6 +168,7 @@ __global__ __launch_bounds__((WPR < 4 ? 4 : WPR) * kWave, 4) void quant_rms_rows
                 if (a.xhat) store4(a.xhat + row * a.K, i, v[j]);
             }
         }
+        if (AHEAD && at + stride < a.M) load_x(at + stride);
         if (a.rowsum) {
             rs = row_reduce<WPR>(rs, OpSum{}, smi, rw, wr);
             if (t == 0) a.rowsum[row] = rs;
@@ -277,7 +285,10 @@ static int launch_rms_typed(const QuantRmsArgs& a, int mode, hipStream_t s) {
     const RmsShape sh = rms_shape(a.M, a.K);
     const int nw = sh.wpr < 4 ? 4 : sh.wpr, rpw = nw / sh.wpr;
     const int64_t wgs = (a.M + rpw - 1) / rpw;
-    const unsigned grid = mode == kRmsFull ? (unsigned)(wgs < (1 << 20) ? wgs : (1 << 20)) : rms_groups(a.M, rpw);
+    // (the second pass: four workgroups a CU, whose next rows are on their way: 8192 x 4096 bf16 both passes 64 us, without 67;
+    // with two workgroups a CU 74)
+    const int64_t most = mode == kRmsFull ? 1 << 20 : mode == kRmsApply ? 1024 : kRmsGroups;
+    const unsigned grid = (unsigned)(wgs < most ? wgs : most);
 #define BL_RMS_CASE(W, V) \
     if (sh.wpr == W && sh.nv == V) quant_rms_rows<XT, RT, RES, W, V><<<grid, nw * kWave, 0, s>>>(a, mode); else
     BL_RMS_CASE(1, 1) BL_RMS_CASE(1, 2) BL_RMS_CASE(1, 4) BL_RMS_CASE(1, 8)
