@@ -15,13 +15,22 @@ constexpr float kLeastMost = 127.f * 0x1p-127f;
 // Eight rows, half a tile, a workgroup: WR waves a row, whose 16 float4 a lane lie in registers, so that rows of 4096 WR
 // are read once; of longer ones all but the last chunk is read again, from the end, out of the caches.  The codes go
 // through LDS and leave as whole lines of 128 bytes: eight rows of 16 columns.  Bound by HBM: 16384 x 4096 fp32
-// 75 us (4.5 TB/s), 2048 x 8192 bf16 14 us (3.6).
-__device__ inline uint32_t load_codes(const int8_t* p, int64_t i4) { return reinterpret_cast<const uint32_t*>(p)[i4]; }
+// 75 us (4.5 TB/s), 16384 x 4096 bf16 35 us (5.7; 46 where the
+// registers held bf16 as fp32), 2048 x 8192 bf16 14 us (3.7).
+template <typename T>
+struct Four {  // four elements as they lie
+    using Raw = std::conditional_t<sizeof(T) == 1, uint32_t, std::conditional_t<sizeof(T) == 2, uint2, float4>>;
+};
+__device__ inline float4 values(const float4& v) { return v; }
+__device__ inline float4 values(const uint2& w) {
+    return make_float4(__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xffff0000u), __uint_as_float(w.y << 16),
+                       __uint_as_float(w.y & 0xffff0000u));
+}
 template <typename T, int WR>
-__global__ __launch_bounds__(512 * WR, 4) void pack_i8_rows(PackI8Args a) {
+__global__ __launch_bounds__(512 * WR, sizeof(T) < 4 ? 8 : 4) void pack_i8_rows(PackI8Args a) {
     constexpr int NV = 16, LANES = 64 * WR, CHUNK = LANES * NV * 4;
     constexpr bool CODES = sizeof(T) == 1;
-    using Element = std::conditional_t<CODES, uint32_t, float4>;
+    using Raw = typename Four<T>::Raw;
     __shared__ __attribute__((aligned(16))) uint8_t codes[8][CHUNK + 16];
     __shared__ float most[8][WR];
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave), r = wave / WR;
@@ -32,15 +41,14 @@ __global__ __launch_bounds__(512 * WR, 4) void pack_i8_rows(PackI8Args a) {
         const int64_t n = n0 + r;
         const bool in = n < a.N;
         const T* src = static_cast<const T*>(a.W) + (in ? n : a.N - 1) * a.K;
-        Element v[NV];
+        Raw v[NV];
         auto load = [&](int c) {
             const int64_t first = (int64_t)c * (CHUNK / 4);
 #pragma unroll
             for (int j = 0; j < NV; ++j)
                 if (first + j * LANES < K4) {  // uniform
                     const int64_t i = first + j * LANES + t;
-                    if constexpr (CODES) v[j] = load_codes(src, i < K4 ? i : K4 - 1);
-                    else v[j] = load4(src, i < K4 ? i : K4 - 1);
+                    v[j] = reinterpret_cast<const Raw*>(src)[i < K4 ? i : K4 - 1];
                 }
         };
         float m = 0.f;
@@ -51,8 +59,10 @@ __global__ __launch_bounds__(512 * WR, 4) void pack_i8_rows(PackI8Args a) {
                 const int64_t first = (int64_t)c * (CHUNK / 4);
 #pragma unroll
                 for (int j = 0; j < NV; ++j)  // (the row's last element again past it)
-                    if (first + j * LANES < K4)
-                        m = fmaxf(m, fmaxf(fmaxf(fabsf(v[j].x), fabsf(v[j].y)), fmaxf(fabsf(v[j].z), fabsf(v[j].w))));
+                    if (first + j * LANES < K4) {
+                        const float4 f = values(v[j]);
+                        m = fmaxf(m, fmaxf(fmaxf(fabsf(f.x), fabsf(f.y)), fmaxf(fabsf(f.z), fabsf(f.w))));
+                    }
             }
         }
         float up = 0.f;
@@ -74,8 +84,12 @@ __global__ __launch_bounds__(512 * WR, 4) void pack_i8_rows(PackI8Args a) {
             for (int j = 0; j < NV; ++j)
                 if (first + j * LANES < TK * 16) {  // uniform
                     uint32_t w;
-                    if constexpr (CODES) w = v[j];
-                    else w = code_word(v[j].x * up, v[j].y * up, v[j].z * up, v[j].w * up, -127.f);
+                    if constexpr (CODES) {
+                        w = v[j];
+                    } else {
+                        const float4 f = values(v[j]);
+                        w = code_word(f.x * up, f.y * up, f.z * up, f.w * up, -127.f);
+                    }
                     // zeros in what is filled up
                     *reinterpret_cast<uint32_t*>(&codes[r][(j * LANES + t) * 4]) = in && first + j * LANES + t < K4 ? w : 0u;
                 }
