@@ -12,11 +12,6 @@ namespace bl {
 // m below this has no 127 / m in fp32: its codes have a step of 2^-127
 constexpr float kLeastMost = 127.f * 0x1p-127f;
 
-// Eight rows, half a tile, a workgroup: WR waves a row, whose 16 float4 a lane lie in registers, so that rows of 4096 WR
-// are read once; of longer ones all but the last chunk is read again, from the end, out of the caches.  The codes go
-// through LDS and leave as whole lines of 128 bytes: eight rows of 16 columns.  Bound by HBM: 16384 x 4096 fp32
-// 75 us (4.5 TB/s), 16384 x 4096 bf16 35 us (5.7; 46 where the
-// registers held bf16 as fp32), 2048 x 8192 bf16 14 us (3.7).
 template <typename T>
 struct Four {  // four elements as they lie
     using Raw = std::conditional_t<sizeof(T) == 1, uint32_t, std::conditional_t<sizeof(T) == 2, uint2, float4>>;
@@ -26,6 +21,12 @@ __device__ inline float4 values(const uint2& w) {
     return make_float4(__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xffff0000u), __uint_as_float(w.y << 16),
                        __uint_as_float(w.y & 0xffff0000u));
 }
+
+// Eight rows, half a tile, a workgroup: WR waves a row, whose 16 float4 a lane lie in registers, so that rows of 4096 WR
+// are read once; of longer ones all but the last chunk is read again, from the end, out of the caches.  The codes go
+// through LDS and leave as whole lines of 128 bytes: eight rows of 16 columns.  Bound by HBM: 16384 x 4096 fp32
+// 75 us (4.5 TB/s), bf16 35 us (5.7; 46 where the registers held it as fp32), 2048 x 8192 bf16 14 us (3.7); rows past
+// registers, 4096 x 16384 fp32, 92 us (3.7).
 template <typename T, int WR>
 __global__ __launch_bounds__(512 * WR, sizeof(T) < 4 ? 8 : 4) void pack_i8_rows(PackI8Args a) {
     constexpr int NV = 16, LANES = 64 * WR, CHUNK = LANES * NV * 4;
