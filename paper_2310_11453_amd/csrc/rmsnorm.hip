@@ -254,7 +254,8 @@ __global__ __launch_bounds__(512) void quant_rms_long(QuantRmsArgs a, int mode) 
     if (mode == kRmsStats && t == 0) a.most[blockIdx.x] = best;
 }
 
-// Waves a row and float4 a lane: up to eight float4; more waves where the batch alone would leave SIMDs idle.
+// Waves a row and float4 a lane (1, 2, 3, 4, 6, 8: with powers of two alone 5784 x 5472 bf16 took 45 us instead of 38, 1600 x
+// 20480 66 instead of 55); more waves where the batch alone would leave SIMDs idle.
 struct RmsShape {
     int wpr, nv;
 };
@@ -263,11 +264,13 @@ static RmsShape rms_shape(int64_t M, int64_t K) {
     int wpr = 1;
     while (wpr < 16 && K4 > (int64_t)wpr * kWave * 8) wpr *= 4;
     while (wpr < 16 && M * wpr < 1024 && K4 >= (int64_t)wpr * kWave * 4) wpr *= 4;
-    // eight waves, so that a CU holds two rows: 3705 x 9056 bf16 61 us, with sixteen 78
+    // eight waves, so that a CU holds two rows: 3705 x 9056 bf16 61 us, with sixteen 78 (with eight float4 a lane;
+    // now 46)
     if (wpr == 16 && M > 512 && K4 <= 8 * kWave * 8) wpr = 8;
     const int64_t per_lane = (K4 + wpr * kWave - 1) / (wpr * kWave);
     int nv = 1;
     while (nv < per_lane) nv *= 2;
+    if (nv >= 4 && per_lane <= nv / 4 * 3) nv = nv / 4 * 3;
     return {wpr, nv};
 }
 static unsigned rms_groups(int64_t M, int rpw) {
@@ -291,10 +294,10 @@ static int launch_rms_typed(const QuantRmsArgs& a, int mode, hipStream_t s) {
     const unsigned grid = (unsigned)(wgs < most ? wgs : most);
 #define BL_RMS_CASE(W, V) \
     if (sh.wpr == W && sh.nv == V) quant_rms_rows<XT, RT, RES, W, V><<<grid, nw * kWave, 0, s>>>(a, mode); else
-    BL_RMS_CASE(1, 1) BL_RMS_CASE(1, 2) BL_RMS_CASE(1, 4) BL_RMS_CASE(1, 8)
-    BL_RMS_CASE(4, 1) BL_RMS_CASE(4, 2) BL_RMS_CASE(4, 4) BL_RMS_CASE(4, 8)
-    BL_RMS_CASE(8, 8)
-    BL_RMS_CASE(16, 1) BL_RMS_CASE(16, 2) BL_RMS_CASE(16, 4) BL_RMS_CASE(16, 8)
+    BL_RMS_CASE(1, 1) BL_RMS_CASE(1, 2) BL_RMS_CASE(1, 3) BL_RMS_CASE(1, 4) BL_RMS_CASE(1, 6) BL_RMS_CASE(1, 8)
+    BL_RMS_CASE(4, 1) BL_RMS_CASE(4, 2) BL_RMS_CASE(4, 3) BL_RMS_CASE(4, 4) BL_RMS_CASE(4, 6) BL_RMS_CASE(4, 8)
+    BL_RMS_CASE(8, 6) BL_RMS_CASE(8, 8)
+    BL_RMS_CASE(16, 1) BL_RMS_CASE(16, 2) BL_RMS_CASE(16, 3) BL_RMS_CASE(16, 4) BL_RMS_CASE(16, 6) BL_RMS_CASE(16, 8)
     return -1;
 #undef BL_RMS_CASE
     return (int)grid;
@@ -327,10 +330,10 @@ hipError_t launch_quant_rmsnorm(const QuantRmsArgs& a_in, hipStream_t s) {
 // The workgroups are as many as fill the chip and go through the rows; a lane has the same columns of all its rows, so that
 // their share of dgain is summed in its registers, and each workgroup leaves one sum a column for fold_dgain.  A row is
 // read once; bound by HBM.  8192 x 4096, fp32 gradient, bf16 h: 66 us (5.5 TB/s); 2048 x 16384 bf16 62 us.
-// The sums are fp64, but with eight float4 a lane (K > 16384) fp32, for which there is room, over 64 rows at most: there are
+// The sums are fp64, but with six or eight float4 a lane (K > 16384) fp32, for which there is room, over 64 rows at most: there are
 // as many workgroups as that takes, and their sums are added in fp64.  The gradient is then read again, out of the cache,
-// where it is used, instead of kept: 1600 x 20480 bf16 76 us, against 159 with both in registers, which spill, and 193 with
-// the sums in memory.  Rows past registers (K > 32768): fp64 sums in memory.
+// where it is used, instead of kept: 1600 x 20480 bf16 70 us (76 with eight float4 a lane, 159 with both
+// in registers, which spill, 193 with the sums in memory).  Rows past registers (K > 32768): fp64 sums in memory.
 constexpr int64_t kRmsBackwardWide = 16384, kRmsBackwardK = 32768;
 static int rms_backward_groups(int64_t M, int64_t K) {
     if (K <= kRmsBackwardWide) return (int)(M < 512 ? M : 512);
@@ -531,19 +534,20 @@ static int launch_rms_backward_typed(const RmsBackwardArgs& a, hipStream_t s) {
         rms_backward_long<GT, HT, DT><<<(unsigned)grid, 512, 0, s>>>(a);
         return grid;
     }
-    // two float4 a lane as long as eight waves hold a row so, then four, then sixteen waves
+    // two float4 a lane as long as eight waves hold a row so, then three or four, then sixteen waves
     const int64_t K4 = a.K / 4;
     int wpr = 1;
     while (wpr < 8 && K4 > (int64_t)wpr * kWave * 2) wpr *= 2;
     if (K4 > 8 * kWave * 4) wpr = 16;
-    const int nv = K4 <= kWave ? 1 : K4 <= (int64_t)wpr * kWave * 2 ? 2 : K4 <= (int64_t)wpr * kWave * 4 ? 4 : 8;
+    int nv = K4 <= kWave ? 1 : K4 <= (int64_t)wpr * kWave * 2 ? 2 : K4 <= (int64_t)wpr * kWave * 4 ? 4 : 8;
+    if (nv >= 4 && K4 <= (int64_t)wpr * kWave * (nv / 4 * 3)) nv = nv / 4 * 3;
     const int rpw = wpr < 8 ? 8 / wpr : 1, threads = wpr < 8 ? 512 : wpr * kWave;
     const int64_t wgs = (a.M + rpw - 1) / rpw;
     const int most = rms_backward_groups(a.M, a.K), grid = (int)(wgs < most ? wgs : most);
 #define BL_RMS_CASE(W, V) \
     if (wpr == W && nv == V) rms_backward_rows<GT, HT, DT, W, V><<<(unsigned)grid, threads, 0, s>>>(a); else
-    BL_RMS_CASE(1, 1) BL_RMS_CASE(1, 2) BL_RMS_CASE(2, 2) BL_RMS_CASE(4, 2) BL_RMS_CASE(8, 2) BL_RMS_CASE(8, 4)
-    BL_RMS_CASE(16, 4) BL_RMS_CASE(16, 8) return -1;
+    BL_RMS_CASE(1, 1) BL_RMS_CASE(1, 2) BL_RMS_CASE(2, 2) BL_RMS_CASE(4, 2) BL_RMS_CASE(8, 2) BL_RMS_CASE(8, 3)
+    BL_RMS_CASE(8, 4) BL_RMS_CASE(16, 3) BL_RMS_CASE(16, 4) BL_RMS_CASE(16, 6) BL_RMS_CASE(16, 8) return -1;
 #undef BL_RMS_CASE
     return grid;
 }

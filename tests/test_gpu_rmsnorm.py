@@ -63,7 +63,8 @@ def check_forward(x, r, gain, per_tensor, got, eps=EPS):
 
 # one to sixteen waves a row, ragged pieces, rows past registers, more rows than fit at once
 SHAPES = [(1, 32), (1, 2048), (5, 96), (3, 256), (33, 544), (64, 1024), (9, 2080), (2500, 2048), (40, 4096), (7, 5472),
-          (130, 8192), (3, 12320), (2, 28672), (1, 32768), (3, 40000)]
+          (130, 8192), (3, 12320), (2, 28672), (1, 32768), (3, 40000), (1100, 704), (1030, 1376), (300, 5472), (40, 10240),
+          (300, 20480)]
 TYPES = [(F, None), (B, None), (F, F), (F, B), (B, F), (B, B)]
 
 
