@@ -27,7 +27,8 @@
  *     on the host before any launch, in the order shape, flags, pointers,
  *     workspace.  M == 0 is a successful no-op (pointers are not looked at).
  *   - Inputs are never written; outputs must not alias inputs.  NaN/Inf in W
- *     or X is undefined behaviour.  Results are deterministic run to run.
+ *     or X is undefined behaviour (unless a call says what comes of it).
+ *     Results are deterministic run to run.
  *   - Scratch memory is passed in as `workspace` (size from
  *     bitlinear_workspace_bytes); calls sharing one workspace must be ordered
  *     on one stream.
@@ -445,7 +446,8 @@ int bitlinear_nonlinear_backward(const float* dXhat, const int8_t* check, const 
  *   eps             >= 0 and finite (else BL_ERR_UNSUPPORTED); a row of zeros has x^ = 0 with any
  *   H          out  h, [M,K] of h_type, or NULL; may be the same buffer as X or residual where the type is the same (else
  *                   BL_ERR_UNSUPPORTED)
- * An infinity or a NaN spoils its row (with one gamma for the tensor everything but H), no other.
+ * An infinity or a NaN in a row of h spoils that row and no other: gamma is NaN, the codes are any, and products of them NaN.
+ * With one gamma for the tensor that is everything but H; with a gain that is not finite, gamma is not in any row.
  *   codes, gamma, rowsum (or NULL), xhat_dump (or NULL)   as in bitlinear_quant_act */
 int bitlinear_quant_rmsnorm(const void* X, int x_type, const void* residual, int h_type, int64_t M, int64_t K,
                             const float* gain, float eps, int granularity, void* H, int8_t* codes, float* gamma,
@@ -460,6 +462,7 @@ int bitlinear_quant_rmsnorm(const void* X, int x_type, const void* residual, int
  *   dresidual  in   [M,K] of d_type or NULL: the gradient that reaches h past the norm
  *   dH         out  [M,K] of d_type; may be the same buffer as dresidual, dXhat or H where the type is the same (else
  *                   BL_ERR_UNSUPPORTED)
+ * An infinity or a NaN in a row of H makes that row of dH NaN, and all of dgain.
  *   dgain      out  fp32 [K] or NULL: sums in fp64, for 16384 < K <= 32768 of sums of up to 64 rows in fp32, in a fixed
  *                   order */
 int bitlinear_rmsnorm_backward(const void* dXhat, int g_type, const void* H, int h_type, const void* dresidual,

@@ -95,7 +95,7 @@ int bitlinear_quant_rmsnorm(const void* X, int x_type, const void* residual, int
     if (per_tensor) {
         char* at = (char*)(((uintptr_t)workspace + 255) & ~(uintptr_t)255);
         a.rstd = (double*)at;
-        a.most = (float*)(at + ws.most);
+        a.most = (int*)(at + ws.most);
     }
     return check_hip(launch_quant_rmsnorm(a, (hipStream_t)stream));
 }

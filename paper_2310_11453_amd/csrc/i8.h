@@ -53,7 +53,7 @@ struct QuantRmsArgs {
     int32_t* rowsum;  // or null
     float* xhat;      // or null
     double* rstd;     // per tensor: [M]
-    float* most;      // per tensor: the largest magnitude of each workgroup's rows, kRmsMostBytes
+    int* most;        // per tensor: the largest magnitude of each workgroup's rows (most_bits), kRmsMostBytes
     int groups;       // how many of those (set by the launcher)
 };
 constexpr size_t kRmsMostBytes = 2048 * 4;
@@ -143,6 +143,15 @@ __device__ inline float4 load4(const uint16_t* p, int64_t i4) {
 __device__ inline void store4(float* p, int64_t i4, const float4& v) { reinterpret_cast<float4*>(p)[i4] = v; }
 __device__ inline void store4(uint16_t* p, int64_t i4, const float4& v) {
     reinterpret_cast<uint2*>(p)[i4] = make_uint2(bf16_pair(v.x, v.y), bf16_pair(v.z, v.w));
+}
+// The largest magnitude as the bits of a float: ordered as the numbers are, and an infinity and then NaN behind them all, which
+// a maximum of floats would drop.
+struct OpMostBits {
+    __device__ int operator()(int a, int b) const { return a > b ? a : b; }
+};
+__device__ inline int most_bits(int m, float v) { return OpMostBits{}(m, __float_as_int(v) & 0x7fffffff); }
+__device__ inline int most_bits(int m, const float4& v) {
+    return most_bits(most_bits(most_bits(most_bits(m, v.x), v.y), v.z), v.w);
 }
 #endif
 

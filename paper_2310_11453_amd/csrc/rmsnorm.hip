@@ -41,19 +41,30 @@ __device__ inline void add_squares(double& q, const float4& v) {
     q = fma((double)v.z, (double)v.z, q);
     q = fma((double)v.w, (double)v.w, q);
 }
-__device__ inline float most4(float m, const float4& v) {
-    return fmaxf(m, fmaxf(fmaxf(fabsf(v.x), fabsf(v.y)), fmaxf(fabsf(v.z), fabsf(v.w))));
-}
+// (of an infinity and of NaN: NaN, the step's 0 * inf, so that x^ and gamma are NaN)
 __device__ inline double rms_inverse(double mean_square, double eps) {
     const double v = mean_square + eps;
-    return v > 0.0 ? rsqrt64(v) : 0.0;  // (a row of zeros with eps = 0)
+    return v == 0.0 ? 0.0 : rsqrt64_step(v, __builtin_amdgcn_rsq(v));  // (a row of zeros with eps = 0)
+}
+// gamma: at least 1e-5; a NaN stays
+__device__ inline float gamma_of(int most) {
+    const float m = __int_as_float(most);
+    return m < 1e-5f ? 1e-5f : m;
+}
+template <int NW>
+__device__ inline int block_most(int m, int* sm) {
+    m = wave_reduce(m, OpMostBits{});
+    __syncthreads();
+    if ((threadIdx.x & (kWave - 1)) == 0) sm[threadIdx.x / kWave] = m;
+    __syncthreads();
+    return fold_slots<NW>(sm, OpMostBits{});
 }
 // the largest of what the first pass left, in every lane; NW waves
 template <int NW>
-__device__ inline float tensor_most(const QuantRmsArgs& a, float* sm) {
-    float m = 0.f;
-    for (int i = threadIdx.x; i < a.groups; i += NW * kWave) m = fmaxf(m, a.most[i]);
-    return block_max<NW>(m, sm);
+__device__ inline int tensor_most(const QuantRmsArgs& a, int* sm) {
+    int m = 0;
+    for (int i = threadIdx.x; i < a.groups; i += NW * kWave) m = OpMostBits{}(m, a.most[i]);
+    return block_most<NW>(m, sm);
 }
 
 // WPR waves share a row, which lies in their registers (NV float4 a lane) from its one reading on; workgroups have four
@@ -65,13 +76,14 @@ template <typename XT, typename RT, bool RES, int WPR, int NV>
 __global__ __launch_bounds__((WPR < 4 ? 4 : WPR) * kWave, 4) void quant_rms_rows(QuantRmsArgs a, int mode) {
     constexpr int NW = WPR < 4 ? 4 : WPR, RPW = NW / WPR, LANES = WPR * kWave;
     __shared__ double smd[NW];
-    __shared__ float smf[2][NW];
+    __shared__ int smm[2][NW];
     __shared__ int smi[NW];
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave), rw = wave / WPR, wr = wave % WPR;
     const int t = wr * kWave + (threadIdx.x & (kWave - 1)), K4 = (int)(a.K / 4);
     // a row's loads before the last one's sum and barriers (with a residual there is no room for them)
     constexpr bool AHEAD = !RES;
-    float gamma = 0.f, best = 0.f;
+    float gamma = 0.f;
+    int best = 0;
     float4 v[NV];
     // unconditional (the last piece again past the row), so that all are in flight before the first is needed
     auto load_x = [&](int64_t row) {
@@ -82,7 +94,7 @@ __global__ __launch_bounds__((WPR < 4 ? 4 : WPR) * kWave, 4) void quant_rms_rows
     const int64_t first = (int64_t)blockIdx.x * RPW + rw, stride = (int64_t)gridDim.x * RPW;
     if (AHEAD) load_x(first < a.M ? first : a.M - 1);
     if (mode == kRmsApply) {
-        gamma = fmaxf(tensor_most<NW>(a, smf[0]), 1e-5f);
+        gamma = gamma_of(tensor_most<NW>(a, smm[0]));
         if (blockIdx.x == 0 && threadIdx.x == 0) *a.gamma = gamma;
     }
     static_assert(WPR == 1 || RPW == 1, "no barriers where a workgroup has rows past the last one");
@@ -95,14 +107,14 @@ __global__ __launch_bounds__((WPR < 4 ? 4 : WPR) * kWave, 4) void quant_rms_rows
 #pragma unroll
             for (int j = 0; j < NV; ++j) u[j] = load4(r, t + j * LANES < K4 ? t + j * LANES : K4 - 1);
         double q = 0.0;
-        float m = 0.f;
+        int m = 0;
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             if constexpr (RES) v[j] = rounded(add4(v[j], u[j]), r);
             if (K4 < (j + 1) * LANES && t + j * LANES >= K4) v[j] = make_float4(0.f, 0.f, 0.f, 0.f);
             if (mode != kRmsApply) {
                 add_squares(q, v[j]);
-                m = most4(m, v[j]);
+                m = most_bits(m, v[j]);
             }
         }
         if constexpr (RES)
@@ -117,18 +129,18 @@ __global__ __launch_bounds__((WPR < 4 ? 4 : WPR) * kWave, 4) void quant_rms_rows
             rstd = a.rstd[row];
         } else {
             q = wave_reduce(q, OpSum{});
-            m = wave_reduce(m, OpMax{});
+            m = wave_reduce(m, OpMostBits{});
             if constexpr (WPR > 1) {
                 if ((threadIdx.x & (kWave - 1)) == 0) {
                     smd[wave] = q;
-                    smf[0][wave] = m;
+                    smm[0][wave] = m;
                 }
                 __syncthreads();
                 q = fold_slots<WPR>(smd + rw * WPR, OpSum{});
-                m = fold_slots<WPR>(smf[0] + rw * WPR, OpMax{});
+                m = fold_slots<WPR>(smm[0] + rw * WPR, OpMostBits{});
             }
             rstd = rms_inverse(q * a.inv_k, a.eps);
-            m = (float)((double)m * rstd);
+            m = most_bits(0, (float)((double)__int_as_float(m) * rstd));
         }
         // (hidden from the optimiser, which would keep the converted copies of all elements alive)
         if constexpr (NV > 2)
@@ -138,23 +150,23 @@ __global__ __launch_bounds__((WPR < 4 ? 4 : WPR) * kWave, 4) void quant_rms_rows
 #pragma unroll
             for (int j = 0; j < NV; ++j) v[j] = times(v[j], rstd);
             if (a.gain) {
-                m = 0.f;
+                m = 0;
 #pragma unroll
                 for (int j = 0; j < NV; ++j) {
                     v[j] = mul4(v[j], load4(a.gain, t + j * LANES < K4 ? t + j * LANES : K4 - 1));
-                    m = most4(m, v[j]);
+                    m = most_bits(m, v[j]);
                 }
-                if (mode != kRmsApply) m = row_reduce<WPR>(m, OpMax{}, smf[1], rw, wr);
+                if (mode != kRmsApply) m = row_reduce<WPR>(m, OpMostBits{}, smm[1], rw, wr);
             }
         }
         if (mode == kRmsStats) {
-            best = fmaxf(best, m);
+            best = OpMostBits{}(best, m);
             if (t == 0) a.rstd[row] = rstd;
             if (AHEAD && at + stride < a.M) load_x(at + stride);
             if (WPR > 1) __syncthreads();  // the slots are read
             continue;
         }
-        if (mode == kRmsFull) gamma = fmaxf(m, 1e-5f);
+        if (mode == kRmsFull) gamma = gamma_of(m);
         const float scale = 128.0f / gamma;
         int rs = 0;
         uint32_t* c4 = reinterpret_cast<uint32_t*>(a.codes + row * a.K);
@@ -178,7 +190,7 @@ __global__ __launch_bounds__((WPR < 4 ? 4 : WPR) * kWave, 4) void quant_rms_rows
     }
     if (mode == kRmsStats) {
         __syncthreads();
-        best = block_max<NW>(best, smf[0]);
+        best = block_most<NW>(best, smm[0]);
         if (threadIdx.x == 0) a.most[blockIdx.x] = best;
     }
 }
@@ -188,13 +200,14 @@ template <typename XT, typename RT, bool RES>
 __global__ __launch_bounds__(512) void quant_rms_long(QuantRmsArgs a, int mode) {
     constexpr int NW = 8, T = NW * kWave;
     __shared__ double smd[NW];
-    __shared__ float smf[NW];
+    __shared__ int smm[NW];
     __shared__ int smi[NW];
     const int t = threadIdx.x;
     const int64_t K4 = a.K / 4;
-    float gamma = 0.f, best = 0.f;
+    float gamma = 0.f;
+    int best = 0;
     if (mode == kRmsApply) {
-        gamma = fmaxf(tensor_most<NW>(a, smf), 1e-5f);
+        gamma = gamma_of(tensor_most<NW>(a, smm));
         if (blockIdx.x == 0 && t == 0) *a.gamma = gamma;
     }
     for (int64_t row = blockIdx.x; row < a.M; row += gridDim.x) {
@@ -220,18 +233,18 @@ __global__ __launch_bounds__(512) void quant_rms_long(QuantRmsArgs a, int mode) 
         };
         // (h may be x or r: an element is read and written by the same thread, and not read there again)
         if (mode != kRmsApply) {
-            float m = 0.f;
-            for (int64_t i = t; i < K4; i += T) m = most4(m, hat(sum_at(i), i));
-            m = block_max<NW>(m, smf);
+            int m = 0;
+            for (int64_t i = t; i < K4; i += T) m = most_bits(m, hat(sum_at(i), i));
+            m = block_most<NW>(m, smm);
             if (mode == kRmsStats) {
-                best = fmaxf(best, m);
+                best = OpMostBits{}(best, m);
                 if (t == 0) a.rstd[row] = rstd;
                 if (h)
                     for (int64_t i = t; i < K4; i += T) store4(h, i, sum_at(i));
                 __syncthreads();  // the slots of the reductions are read
                 continue;
             }
-            gamma = fmaxf(m, 1e-5f);
+            gamma = gamma_of(m);
         }
         const float scale = 128.0f / gamma;
         uint32_t* c4 = reinterpret_cast<uint32_t*>(a.codes + row * a.K);

@@ -177,10 +177,12 @@ __device__ inline float normalised(const RowNorm& n, double d) { return (float)f
 // 1 / sqrt(v) for v >= 0: the hardware's estimate (a relative error below 2^-22) and one step of third order.  Off by at
 // most 0.99 ulp, 0.33 rms, over 2 * 10^7 values in an emulation with estimates of that error; a square root and a
 // division, each rounded, are off by up to 1.49 (0.44 rms), and four times the instructions, one after another.
-__device__ inline double rsqrt64(double v) {
-    const double y = __builtin_amdgcn_rsq(v);
+__device__ inline double rsqrt64_step(double v, double y) {
     const double e = fma(-(v * y), y, 1.0);
-    const double r = fma(y * e, fma(e, 0.375, 0.5), y);
+    return fma(y * e, fma(e, 0.375, 0.5), y);
+}
+__device__ inline double rsqrt64(double v) {
+    const double y = __builtin_amdgcn_rsq(v), r = rsqrt64_step(v, y);
     return v > 0.0 ? r : y;
 }
 // inv_k = 1 / K.  lo and hi: the row's smallest and largest x^.

@@ -322,3 +322,69 @@ def test_binding_refuses(bl):
                  lambda: bl.bitlinear_rmsnorm_backward(x, r, out=r), lambda: bl.bitlinear_rmsnorm_backward(x, r, gain=x)):
         with pytest.raises(bl.BitLinearError):
             call()
+
+
+# every width of a row: one wave, four, eight, sixteen, rows past registers
+BAD_SHAPES = [(9, 96), (1100, 2048), (300, 4096), (9, 4096), (600, 9056), (9, 20480), (9, 40000)]
+
+
+@pytest.mark.parametrize("M,K", BAD_SHAPES)
+@pytest.mark.parametrize("h_type", [None, F, B])
+@pytest.mark.parametrize("with_gain", [False, True])
+def test_a_row_of_no_numbers_is_seen(bl, M, K, h_type, with_gain):
+    """A row with an infinity or a NaN has a gamma of NaN, so that products of its codes are NaN and nothing passes for a
+    token; per tensor the one gamma is.  The other rows (per token) and h are as they were."""
+    x = make(M, K, F, 1).cuda()
+    r = None if h_type is None else make(M, K, h_type, 2).cuda()
+    gain = (1 + 0.3 * torch.randn(K, generator=torch.Generator().manual_seed(3))).cuda() if with_gain else None
+    ref = bl.bitlinear_quant_rmsnorm(x, r, gain=gain)
+    bad = x.clone()
+    bad[1, 5], bad[3, K - 1], bad[7, K // 2] = float("inf"), float("nan"), float("-inf")
+    if M > 9:
+        bad[M - 1] = float("nan")
+    spoilt = ~bad.isfinite().all(1)
+    got = bl.bitlinear_quant_rmsnorm(bad, r, gain=gain)
+    assert bool(got[1][spoilt].isnan().all()) and bool(got[1][~spoilt].isfinite().all())
+    assert all(torch.equal(p[~spoilt], q[~spoilt]) for p, q in zip(got[:4], ref[:4]))
+    packed, scale = bl.bitlinear_pack_weights_i8(torch.ones(16, K, device="cuda"))
+    y = bl.bitlinear_matmul_i8(got[0], got[1], packed, 16, scale)
+    assert bool(y[spoilt].isnan().all()) and bool(y[~spoilt].isfinite().all())
+    one = bl.bitlinear_quant_rmsnorm(bad, r, gain=gain, per_tensor=True)
+    assert bool(one[1].isnan().all())
+    for h in (got[3], one[3]):
+        want = bad if r is None else (bad + r.float()).to(h_type)
+        assert torch.equal(h.nan_to_num(1.5, 2.5, 3.5), want.nan_to_num(1.5, 2.5, 3.5))
+
+
+@pytest.mark.parametrize("K", [96, 4096, 20480, 40000])
+@pytest.mark.parametrize("per_tensor", [False, True])
+def test_a_gain_of_no_numbers_is_seen(bl, K, per_tensor):
+    """It is in every row."""
+    x = make(9, K, B, 1).cuda()
+    for bad in (float("nan"), float("inf")):
+        gain = torch.ones(K, device="cuda")
+        gain[K - 3] = bad
+        assert not bool(bl.bitlinear_quant_rmsnorm(x, gain=gain, per_tensor=per_tensor)[1].isfinite().any())
+
+
+@pytest.mark.parametrize("per_tensor", [False, True])
+def test_a_sum_past_the_largest_number_is_seen(bl, per_tensor):
+    """x and the residual are numbers, their sum in the residual's type is not."""
+    x, r = make(4, 256, F, 1), make(4, 256, B, 2)
+    x[2, 9], r[2, 9] = 3.3e38, torch.tensor(3.3e38).to(B)
+    codes, gamma, _, h, _ = bl.bitlinear_quant_rmsnorm(x.cuda(), r.cuda(), per_tensor=per_tensor)
+    assert bool(h[2, 9].isinf()) and bool(gamma[0 if per_tensor else 2].isnan())
+    assert per_tensor or bool(gamma[[0, 1, 3]].isfinite().all())
+
+
+@pytest.mark.parametrize("K", [96, 4096, 9056, 20480, 40000])
+def test_backward_of_a_row_of_no_numbers(bl, K):
+    """dh is NaN in all of such a row and in no other; the gain's gradient, a sum over rows, is."""
+    g, h = make(20, K, F, 1).cuda(), make(20, K, F, 2).cuda()
+    ref = bl.bitlinear_rmsnorm_backward(g, h)
+    for value in (float("nan"), float("inf")):
+        bad = h.clone()
+        bad[6, 11] = value
+        d_h, d_gain = bl.bitlinear_rmsnorm_backward(g, bad, want_dgain=True)
+        rows = [i for i in range(20) if i != 6]
+        assert torch.equal(d_h[rows], ref[rows]) and bool(d_h[6].isnan().all()) and bool(d_gain.isnan().all())
