@@ -474,7 +474,8 @@ size_t bitlinear_packed_bytes_i8(int64_t N, int64_t K);
 
 /* 8-bit weights with a scale for each output channel: m = max_k |W[n,k]|, scale[n] = m / 127, codes
  * clamp(rne(W[n,k] * (127 / m)), -127, 127).  (m is taken to be at least 127 * 2^-127 in a row that is not all zeros, so
- * that 127 / m is a number; a row of zeros has scale 0.)
+ * that 127 / m is a number; a row of zeros has scale 0.)  A row with a NaN has a scale of NaN, one with an infinity an infinite one,
+ * and no value or product of it is a number; its codes are any.
  *   W       in   [N,K] of w_type: BL_F32, BL_BF16, or BL_I8: these are the codes (any int8), `scale` is left alone (or NULL)
  *   packed  out  bitlinear_packed_bytes_i8(N, K) bytes;   scale  out  fp32 [N] */
 int bitlinear_pack_weights_i8(const void* W, int w_type, int64_t N, int64_t K, void* packed, float* scale,

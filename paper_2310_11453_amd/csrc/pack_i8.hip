@@ -33,7 +33,7 @@ __global__ __launch_bounds__(512 * WR, sizeof(T) < 4 ? 8 : 4) void pack_i8_rows(
     constexpr bool CODES = sizeof(T) == 1;
     using Raw = typename Four<T>::Raw;
     __shared__ __attribute__((aligned(16))) uint8_t codes[8][CHUNK + 16];
-    __shared__ float most[8][WR];
+    __shared__ int most[8][WR];
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave), r = wave / WR;
     const int t = wave % WR * kWave + ((int)threadIdx.x & (kWave - 1));
     const int64_t K4 = a.K / 4, TK = i8_tiles_k(a.K), rows = tiles_n(a.N) * 16;
@@ -52,7 +52,7 @@ __global__ __launch_bounds__(512 * WR, sizeof(T) < 4 ? 8 : 4) void pack_i8_rows(
                     v[j] = reinterpret_cast<const Raw*>(src)[i < K4 ? i : K4 - 1];
                 }
         };
-        float m = 0.f;
+        int bits = 0;
         for (int c = 0; c < chunks; ++c) {
             if (CODES && c < chunks - 1) continue;
             load(c);
@@ -60,20 +60,18 @@ __global__ __launch_bounds__(512 * WR, sizeof(T) < 4 ? 8 : 4) void pack_i8_rows(
                 const int64_t first = (int64_t)c * (CHUNK / 4);
 #pragma unroll
                 for (int j = 0; j < NV; ++j)  // (the row's last element again past it)
-                    if (first + j * LANES < K4) {
-                        const float4 f = values(v[j]);
-                        m = fmaxf(m, fmaxf(fmaxf(fabsf(f.x), fabsf(f.y)), fmaxf(fabsf(f.z), fabsf(f.w))));
-                    }
+                    if (first + j * LANES < K4) bits = most_bits(bits, values(v[j]));
             }
         }
         float up = 0.f;
         if constexpr (!CODES) {
-            m = wave_reduce(m, OpMax{});
+            bits = wave_reduce(bits, OpMostBits{});
             if constexpr (WR > 1) {
-                if ((threadIdx.x & (kWave - 1)) == 0) most[r][wave % WR] = m;
+                if ((threadIdx.x & (kWave - 1)) == 0) most[r][wave % WR] = bits;
                 __syncthreads();
-                m = fold_slots<WR>(most[r], OpMax{});
+                bits = fold_slots<WR>(most[r], OpMostBits{});
             }
+            float m = __int_as_float(bits);  // (a NaN stays one, and so does the scale)
             if (m > 0.f) m = fmaxf(m, kLeastMost);
             up = m > 0.f ? 127.0f / m : 0.f;
             if (t == 0 && in) a.scale[n] = m / 127.0f;

@@ -496,3 +496,23 @@ def test_binding_refuses(bl):
                  lambda: bl.bitlinear_backward_ste_i8(dY.half(), c, g, packed, scale)):
         with pytest.raises(bl.BitLinearError):
             call()
+
+
+@pytest.mark.parametrize("K", [96, 4096, 8192, 16384, 40000])
+@pytest.mark.parametrize("dtype", [F, B])
+def test_pack_of_no_numbers_is_seen(bl, K, dtype):
+    """A channel with a NaN has a scale of NaN, one with an infinity an infinite one: its values are no weights, and products
+    with it no numbers.  The other channels are as they were."""
+    W = torch.randn(20, K, generator=torch.Generator().manual_seed(K)).to(dtype).cuda()
+    ref, scale_ref = bl.bitlinear_pack_weights_i8(W)
+    W[2, 7], W[5, K - 1], W[9] = float("nan"), float("-inf"), float("nan")
+    packed, scale = bl.bitlinear_pack_weights_i8(W)
+    assert bool(scale[[2, 9]].isnan().all()) and bool(scale[5].isinf())
+    rest = [n for n in range(20) if n not in (2, 5, 9)]
+    codes, codes_ref = (bl.bitlinear_unpack_weights_i8(p, None, 20, K) for p in (packed, ref))
+    assert torch.equal(scale[rest], scale_ref[rest]) and torch.equal(codes[rest], codes_ref[rest])
+    values = bl.bitlinear_unpack_weights_i8(packed, scale, 20, K, dtype=dtype)
+    assert not bool(values[[2, 5, 9]].isfinite().any()) and bool(values[rest].isfinite().all())
+    q = torch.ones(3, K, dtype=I8, device="cuda")
+    y = bl.bitlinear_matmul_i8(q, torch.ones(3, device="cuda"), packed, 20, scale)
+    assert not bool(y[:, [2, 5, 9]].isfinite().any()) and bool(y[:, rest].isfinite().all())
