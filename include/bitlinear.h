@@ -463,8 +463,9 @@ int bitlinear_quant_rmsnorm(const void* X, int x_type, const void* residual, int
  *   dH         out  [M,K] of d_type; may be the same buffer as dresidual, dXhat or H where the type is the same (else
  *                   BL_ERR_UNSUPPORTED)
  * An infinity or a NaN in a row of H makes that row of dH NaN, and all of dgain.
- *   dgain      out  fp32 [K] or NULL: sums in fp64, for 16384 < K <= 32768 of sums of up to 64 rows in fp32, in a fixed
- *                   order */
+ *   dgain      out  fp32 [K] or NULL: products and a workgroup's sums in fp64, for 16384 < K <= 32768 in fp32 over up to 64
+ *                   rows; up to K = 32768 the workgroups' sums are rounded to fp32 (and, of short rows, those of its waves), and
+ *                   then added in fp64, in a fixed order */
 int bitlinear_rmsnorm_backward(const void* dXhat, int g_type, const void* H, int h_type, const void* dresidual,
                                int d_type, int64_t M, int64_t K, const float* gain, float eps, void* dH,
                                float* dgain, void* workspace, size_t workspace_bytes, void* stream);

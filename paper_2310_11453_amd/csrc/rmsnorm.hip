@@ -343,8 +343,9 @@ hipError_t launch_quant_rmsnorm(const QuantRmsArgs& a_in, hipStream_t s) {
 // The workgroups are as many as fill the chip and go through the rows; a lane has the same columns of all its rows, so that
 // their share of dgain is summed in its registers, and each workgroup leaves one sum a column for fold_dgain.  A row is
 // read once; bound by HBM.  8192 x 4096, fp32 gradient, bf16 h: 66 us (5.5 TB/s); 2048 x 16384 bf16 62 us.
-// The sums are fp64, but with six or eight float4 a lane (K > 16384) fp32, for which there is room, over 64 rows at most: there are
-// as many workgroups as that takes, and their sums are added in fp64.  The gradient is then read again, out of the cache,
+// A lane's sums are fp64, but with six or eight float4 a lane (K > 16384) fp32, for which there is room, over 64 rows at most:
+// there are as many workgroups as that takes.  What leaves a wave for LDS and a workgroup for memory is rounded to fp32, half the
+// bytes: two roundings of parts of the sum beside the result's own; fold_dgain adds in fp64.  The gradient is then read again, out of the cache,
 // where it is used, instead of kept: 1600 x 20480 bf16 70 us (76 with eight float4 a lane, 159 with both
 // in registers, which spill, 193 with the sums in memory).  Rows past registers (K > 32768): fp64 sums in memory.
 constexpr int64_t kRmsBackwardWide = 16384, kRmsBackwardK = 32768;
@@ -439,12 +440,12 @@ __global__ __launch_bounds__((WPR < 8 ? 8 : WPR) * kWave, 4) void rms_backward_r
                 d.z = (s.z - v[j].z * along) * inv + r.z;
                 d.w = (s.w - v[j].w * along) * inv + r.w;
                 store4(dh, i, d);
-                if (a.dgain) {
+                if (a.dgain) {  // (n first: g h may be past the largest float, or have lost its digits)
                     const Sum f = WIDE ? (Sum)inv : (Sum)rstd;
-                    dg[j][0] += (Sum)(u[j].x * v[j].x) * f;
-                    dg[j][1] += (Sum)(u[j].y * v[j].y) * f;
-                    dg[j][2] += (Sum)(u[j].z * v[j].z) * f;
-                    dg[j][3] += (Sum)(u[j].w * v[j].w) * f;
+                    dg[j][0] = fma((Sum)u[j].x, (Sum)v[j].x * f, dg[j][0]);
+                    dg[j][1] = fma((Sum)u[j].y, (Sum)v[j].y * f, dg[j][1]);
+                    dg[j][2] = fma((Sum)u[j].z, (Sum)v[j].z * f, dg[j][2]);
+                    dg[j][3] = fma((Sum)u[j].w, (Sum)v[j].w * f, dg[j][3]);
                 }
             }
         }

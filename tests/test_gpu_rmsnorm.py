@@ -388,3 +388,18 @@ def test_backward_of_a_row_of_no_numbers(bl, K):
         d_h, d_gain = bl.bitlinear_rmsnorm_backward(g, bad, want_dgain=True)
         rows = [i for i in range(20) if i != 6]
         assert torch.equal(d_h[rows], ref[rows]) and bool(d_h[6].isnan().all()) and bool(d_gain.isnan().all())
+
+
+SIZES_K = [96, 480, 2048, 8192, 12320, 20480, 28672, 40000]
+
+
+@pytest.mark.parametrize("K", SIZES_K)
+@pytest.mark.parametrize("g_type,h_type", [(F, F), (B, B)])
+def test_backward_gain_of_large_and_small_rows(bl, K, g_type, h_type):
+    """Products g h that are no numbers, or have lost their digits, where g h / rms is an ordinary number."""
+    for size, grad in ((1e30, 1e10), (1e-30, 1e-12)):
+        g, h = make(37, K, g_type, K, grad), make(37, K, h_type, K + 1)
+        h = (h.float() / h.float().abs().amax(1, keepdim=True) * size).to(h_type)
+        gain = 1 + 0.3 * torch.randn(K, generator=torch.Generator().manual_seed(K))
+        d_h, d_gain = bl.bitlinear_rmsnorm_backward(g.cuda(), h.cuda(), gain=gain.cuda(), eps=0.0, want_dgain=True, dtype=F)
+        check_backward(g, h, gain, None, F, d_h, d_gain, 0.0)
