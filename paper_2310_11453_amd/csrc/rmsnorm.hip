@@ -420,7 +420,21 @@ __global__ __launch_bounds__((WPR < 8 ? 8 : WPR) * kWave, 4) void rms_backward_r
             parity ^= 1;  // read before the barrier of the next row, written behind it
         }
         const double rstd = rms_inverse(q * a.inv_k, a.eps);
-        const float inv = (float)rstd, along = (float)(c * a.inv_k * rstd * rstd);  // mean(t n) / rms
+        // 1/rms of a row below 2^-60 or above 2^60, or what is made of it, may be past fp32's range or have lost digits there: it
+        // is taken as inv64 * half then, half a power of two of half its exponent, and h as h * half (uniform in a row).  The branch
+        // costs 0 to 3 % (5784 x 5472 51.2 -> 52.8 us); powers of two in every row's arithmetic, or a loop of its own for such
+        // rows, 1 to 8 %
+        double inv64 = rstd;
+        float half = 1.0f;
+        if (__builtin_amdgcn_readfirstlane(rstd != 0.0 && !(rstd > 0x1p-60 && rstd < 0x1p60))) {
+            int e;
+            frexp(rstd, &e);
+            half = (float)ldexp(1.0, e / 2);
+            inv64 = rstd * ldexp(1.0, -(e / 2));
+#pragma unroll
+            for (int j = 0; j < NV; ++j) v[j] = make_float4(v[j].x * half, v[j].y * half, v[j].z * half, v[j].w * half);
+        }
+        const float inv = (float)inv64, along = (float)(c * a.inv_k * rstd * inv64);  // mean(t n) / rms (/ half)
         // (hidden from the optimiser, which would keep the converted copies of all elements alive)
 #pragma unroll
         for (int j = 0; j < NV; ++j) asm volatile("" : "+v"(v[j].x), "+v"(v[j].y), "+v"(v[j].z), "+v"(v[j].w));
@@ -434,14 +448,14 @@ __global__ __launch_bounds__((WPR < 8 ? 8 : WPR) * kWave, 4) void rms_backward_r
                 const float4 s = a.gain ? mul4(u[j], load4(a.gain, i)) : u[j];
                 float4 r = w[WIDE ? 0 : j];
                 if constexpr (WIDE) r = dr ? load4(dr, i) : make_float4(0.f, 0.f, 0.f, 0.f);
-                float4 d;
-                d.x = (s.x - v[j].x * along) * inv + r.x;
-                d.y = (s.y - v[j].y * along) * inv + r.y;
-                d.z = (s.z - v[j].z * along) * inv + r.z;
-                d.w = (s.w - v[j].w * along) * inv + r.w;
+                float4 d;  // (with half = 1 the sum)
+                d.x = fmaf((s.x - v[j].x * along) * inv, half, r.x);
+                d.y = fmaf((s.y - v[j].y * along) * inv, half, r.y);
+                d.z = fmaf((s.z - v[j].z * along) * inv, half, r.z);
+                d.w = fmaf((s.w - v[j].w * along) * inv, half, r.w);
                 store4(dh, i, d);
                 if (a.dgain) {  // (n first: g h may be past the largest float, or have lost its digits)
-                    const Sum f = WIDE ? (Sum)inv : (Sum)rstd;
+                    const Sum f = WIDE ? (Sum)inv : (Sum)inv64;
                     dg[j][0] = fma((Sum)u[j].x, (Sum)v[j].x * f, dg[j][0]);
                     dg[j][1] = fma((Sum)u[j].y, (Sum)v[j].y * f, dg[j][1]);
                     dg[j][2] = fma((Sum)u[j].z, (Sum)v[j].z * f, dg[j][2]);

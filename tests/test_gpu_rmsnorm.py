@@ -403,3 +403,16 @@ def test_backward_gain_of_large_and_small_rows(bl, K, g_type, h_type):
         gain = 1 + 0.3 * torch.randn(K, generator=torch.Generator().manual_seed(K))
         d_h, d_gain = bl.bitlinear_rmsnorm_backward(g.cuda(), h.cuda(), gain=gain.cuda(), eps=0.0, want_dgain=True, dtype=F)
         check_backward(g, h, gain, None, F, d_h, d_gain, 0.0)
+
+
+@pytest.mark.parametrize("K", SIZES_K)
+@pytest.mark.parametrize("g_type,h_type", [(F, F), (B, B)])
+def test_backward_of_rows_at_the_ends_of_the_range(bl, K, g_type, h_type):
+    """Rows so small that 1 / rms is past the largest float (eps = 0), or so large that it has lost digits, with gradients that
+    are ordinary numbers."""
+    for size, grad in ((1e-39, 1e-6), (1e35, 1e-3), (3e38, 1e4)):
+        g, h = make(37, K, g_type, K, grad), make(37, K, F, K + 1)
+        h = (h.sign() * size * (0.5 + 0.5 * h.abs() / h.abs().amax(1, keepdim=True))).to(h_type)
+        gain = 1 + 0.3 * torch.randn(K, generator=torch.Generator().manual_seed(K))
+        d_h, d_gain = bl.bitlinear_rmsnorm_backward(g.cuda(), h.cuda(), gain=gain.cuda(), eps=0.0, want_dgain=True, dtype=F)
+        check_backward(g, h, gain, None, F, d_h, d_gain, 0.0)
