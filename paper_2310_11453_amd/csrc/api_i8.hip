@@ -45,7 +45,7 @@ RmsWs rms_ws(int64_t M) {
 }
 size_t rms_backward_bytes(int64_t M, int64_t K) { return rms_backward_part_bytes(M, K) + 256; }
 int product_status(int64_t M, int64_t N, int64_t K) {
-    if (M < 0 || M > kMaxDim || !weights_ok(N, K)) return BL_ERR_SHAPE;
+    if (!rows_ok(M, K) || !weights_ok(N, K)) return BL_ERR_SHAPE;
     return K > kMaxGemmK ? BL_ERR_UNSUPPORTED : BL_OK;
 }
 

@@ -137,3 +137,12 @@ def test_binding_refuses_what_is_not_on_the_gpu(bl):
                  lambda: bl.bitlinear_backward_ste_i8(x, c, None, None, None)):
         with pytest.raises(bl.BitLinearError):
             call()
+
+
+def test_more_tokens_than_a_size_can_hold(bl, lib):
+    """M * K past 2^40, N * K within it."""
+    assert product(lib, M=1 << 30, K=2048, N=16) == -2 and backward(lib, M=1 << 30, K=2048, N=16) == -2
+    for op in (bl.OP_MATMUL_I8, bl.OP_BACKWARD_I8):
+        assert bl.workspace_bytes(op, 1 << 30, 16, 2048) == 0
+    # at the bound the next argument is looked at
+    assert product(lib, M=1 << 29, K=2048, N=16, codes=None) == -1 and backward(lib, M=1 << 29, K=2048, N=16, dY=None) == -1
