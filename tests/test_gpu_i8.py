@@ -516,3 +516,48 @@ def test_pack_of_no_numbers_is_seen(bl, K, dtype):
     q = torch.ones(3, K, dtype=I8, device="cuda")
     y = bl.bitlinear_matmul_i8(q, torch.ones(3, device="cuda"), packed, 20, scale)
     assert not bool(y[:, [2, 5, 9]].isfinite().any()) and bool(y[:, rest].isfinite().all())
+
+
+# i8_tile; M, K, N: more tiles than workgroups in both products (256 x 256: 306 for 256, 128 x 128: 595 for 512, 64 x 128: 1173),
+# then in the first one of two that share a launch (128 x 128: 595 + 391, 64 x 128: the same)
+@pytest.mark.parametrize("tile,M,K,N", [(1, 4400, 4128, 4390), (1, 4400, 4128, 4384), (2, 4400, 2080, 4390), (3, 4400, 2080, 4390),
+                                        (2, 4400, 2080, 2900), (3, 2200, 2080, 1450)])
+@pytest.mark.parametrize("dy_type,dx_type", [(B, B), (B, F), (F, B)])
+def test_backward_of_more_tiles_than_workgroups(bl, tuning, tile, M, K, N, dy_type, dx_type):
+    """Integer dY, powers of two as scales: every sum is a number of 24 bits, exact in fp32 in any order."""
+    print(f"backward_i8 tile={tile} M={M} K={K} N={N} {dy_type} {dx_type}", flush=True)
+    tuning(f"i8_tile={tile},i8_splits=1")
+    g = torch.Generator(device="cuda").manual_seed(M + N)
+    dY = torch.randint(-3, 4, (M, N), generator=g, device="cuda").to(dy_type)
+    q, w = (torch.randint(-9, 10, s, generator=g, device="cuda").to(I8) for s in ((M, K), (N, K)))
+    scale, gamma = 2.0 ** torch.randint(-2, 3, (N,), generator=g, device="cuda").float(), torch.tensor([256.0], device="cuda")
+    packed, _ = bl.bitlinear_pack_weights_i8(w)
+    dX, dW = bl.bitlinear_backward_ste_i8(dY, q, gamma, packed, scale, per_tensor=True, dtype=dx_type)
+    assert torch.equal(dX, ((dY.double() * scale.double()) @ w.double()).to(F).to(dx_type))
+    assert torch.equal(dW.double(), dY.double().T.contiguous() @ (2 * q.double()))
+
+
+@pytest.mark.parametrize("dy_type,dx_type", [(B, B), (F, F)])
+def test_backward_in_one_launch_with_slices(bl, dy_type, dx_type):
+    """Shapes whose first product is cut into slices and shares its launch with the second one, in 128 x 128 tiles (the first
+    two) and 64 x 128."""
+    for M, K, N in [(1302, 800, 11788), (1302, 800, 11776), (333, 2048, 2048), (90, 1024, 3000)]:
+        print(f"backward_i8 M={M} K={K} N={N} {dy_type} {dx_type}", flush=True)
+        g = torch.Generator(device="cuda").manual_seed(M + N)
+        dY = torch.randint(-3, 4, (M, N), generator=g, device="cuda").to(dy_type)
+        q, w = (torch.randint(-9, 10, s, generator=g, device="cuda").to(I8) for s in ((M, K), (N, K)))
+        scale, gamma = 2.0 ** torch.randint(-1, 2, (N,), generator=g, device="cuda").float(), torch.tensor([64.0], device="cuda")
+        packed, _ = bl.bitlinear_pack_weights_i8(w)
+        dX, dW = bl.bitlinear_backward_ste_i8(dY, q, gamma, packed, scale, per_tensor=True, dtype=dx_type)
+        assert torch.equal(dX, ((dY.double() * scale.double()) @ w.double()).to(F).to(dx_type))
+        assert torch.equal(dW.double(), dY.double().T.contiguous() @ (0.5 * q.double()))
+
+
+@pytest.mark.parametrize("M,K,N", [(16, 2080, 77), (31, 4128, 129), (32, 2080, 500), (32, 1056, 515)])
+@pytest.mark.parametrize("rows", [1, 2, 4])
+@pytest.mark.parametrize("splits", [0, 1, 2, 7])
+def test_product_of_whole_blocks_of_tokens(bl, tuning, M, K, N, rows, splits):
+    """Up to the stream's last token: 16 and 32 leave no row of a block to fill up."""
+    print(f"matmul_i8 M={M} K={K} N={N} rows={rows} splits={splits}", flush=True)
+    tuning(f"i8_tile=4,i8_rows={rows},i8_splits={splits}")
+    check_product(bl, M, K, N, per_tensor=splits == 1)

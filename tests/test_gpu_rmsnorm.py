@@ -324,6 +324,25 @@ def test_binding_refuses(bl):
             call()
 
 
+# the kernels that no shape above takes: 2 and 4 float4 a lane of one wave, 4 and 8 of four, also with more rows than a call has
+# workgroups, as at a training step; many rows are multiples of a few, so that making them is quick
+@pytest.mark.parametrize("M,K", [(20, 480), (40, 960), (300, 4096), (300, 8192), (2100, 4096), (2100, 8192)])
+@pytest.mark.parametrize("x_type,h_type", TYPES)
+def test_rows_of_the_other_kernels(bl, M, K, x_type, h_type):
+    gen = torch.Generator().manual_seed(M + K)
+    size = torch.exp(torch.randn(M, 1, generator=gen))
+    some = lambda t, seed, s=1.0: (make(20, K, F, seed, s).repeat(M // 20, 1) * size).to(t)  # noqa: E731
+    x, r = some(x_type, 1), None if h_type is None else some(h_type, 2)
+    gain = 1 + 0.3 * torch.randn(K, generator=gen) if h_type is not B else None
+    for per_tensor in (False, True):
+        print(f"quant_rmsnorm M={M} K={K} {x_type} {h_type} per_tensor={per_tensor}", flush=True)
+        check_forward(x, r, gain, per_tensor, bl.bitlinear_quant_rmsnorm(x.cuda(), cuda(r), gain=cuda(gain), per_tensor=per_tensor))
+    if r is not None:
+        g = some(x_type, 3, 1e-3)
+        got = bl.bitlinear_rmsnorm_backward(g.cuda(), r.cuda(), gain=cuda(gain), want_dgain=True, dtype=F)
+        check_backward(g, r, gain, None, F, *got)
+
+
 # every width of a row: one wave, four, eight, sixteen, rows past registers
 BAD_SHAPES = [(9, 96), (1100, 2048), (300, 4096), (9, 4096), (600, 9056), (9, 20480), (9, 40000)]
 
