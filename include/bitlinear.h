@@ -543,7 +543,8 @@ int bitlinear_probe_read(const void* src, size_t bytes, int workgroups, int thre
  *   i8_tile=1|2|3|4     8-bit product: 256 x 256, 128 x 128 or 64 x 128 output tiles (also those of its backward), or, up
  *                       to 32 tokens, the stream of the weights
  *   i8_splits=n         8-bit product and its backward: slices of K (not in tiles of 256 x 256)
- *   i8_rows=1|2|4       8-bit product, up to 32 tokens: rows of weight tiles a workgroup of the stream
+ *   i8_rows=1|2|4       8-bit product, up to 32 tokens: rows of weight tiles a workgroup of the stream (2: up to 16
+ *                       tokens)
  *   (decode_tiles, 1, 2, 4 or 8: also the weight tiles of a workgroup of that last kernel.  bwd_ring, bwd_grid,
  *   bwd_splits and quant_wpr also act on the operators of experts: bwd_splits on dW in 128 x 128 tiles, and on dX
  *   from four slices on; quant_wpr with 1, 4 or 8; bwd_dx does not, their dX has tiles of 128 x 256 only)

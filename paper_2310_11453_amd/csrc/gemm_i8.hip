@@ -654,12 +654,13 @@ struct StreamPlan {
 // Up to 32 tokens: the stream with the rows of tiles and slices that cost least, or tiles where those do.  us: `call`,
 // and `tile` for each tile of K that a wave has, (workgroups / CUs)^power where there are more than CUs; or the weights
 // at `rate` MB/us.  Fitted to 126 shapes of 1 to 32 tokens: 2.4 % slower than the best of 20 variants on average, 44 %
-// at most; over 126 others 3.7 % and 61 %.
+// at most; over 126 others 3.7 % and 61 %.  From 17 tokens on there are no two rows a workgroup: 26 registers spill in the
+// stream's loop (32 x 8384 -> 14656 44 us, four rows 28, one 46), and of 300000 shapes to N = 2 * 10^6 none took them.
 struct StreamCost {
     double call, tile, rate, power;
 };
 constexpr StreamCost kStream[2][3] = {{{4.336, 0.231, 5.265, 1.41}, {4.187, 0.394, 5.77, 1.63}, {3.993, 0.716, 5.32, 1.03}},
-                                      {{4.631, 0.055, 2.953, 1.82}, {6.803, 0.594, 2.847, 1.56}, {4.004, 1.05, 3.83, 0.81}}};
+                                      {{4.631, 0.055, 2.953, 1.82}, {}, {4.004, 1.05, 3.83, 0.81}}};
 static StreamPlan stream_plan(int64_t M, int64_t N, int64_t K) {
     const Tuning& t = tuning();
     StreamPlan p{};
@@ -667,8 +668,9 @@ static StreamPlan stream_plan(int64_t M, int64_t N, int64_t K) {
     const int64_t rows = tiles_n(N), TK = i8_tiles_k(K), cus = num_cus();
     const int mb = M > 16 ? 2 : 1;
     double least = 1e300;
+    const int only = t.i8_rows == 1 || t.i8_rows == 4 || (t.i8_rows == 2 && mb == 1) ? t.i8_rows : 0;
     for (int r = 0; r < 3; ++r) {
-        if ((t.i8_rows == 1 || t.i8_rows == 2 || t.i8_rows == 4) && t.i8_rows != 1 << r) continue;
+        if (only ? only != 1 << r : r == 1 && mb == 2) continue;
         const StreamCost& c = kStream[mb - 1][r];
         const int64_t force = t.i8_splits > 0 ? (t.i8_splits < TK ? t.i8_splits : TK) : 0, wgs = (rows + (1 << r) - 1) >> r;
         for (int64_t n = force ? force : 1; n <= (force ? force : 8); n *= 2) {
@@ -700,7 +702,7 @@ static void launch_stream(const GemmI8Args& a, const StreamPlan& p, int out, hip
         else go(tn, std::integral_constant<int, 2>{});
     };
     if (p.tn == 1) rows(std::integral_constant<int, 1>{});
-    else if (p.tn == 2) rows(std::integral_constant<int, 2>{});
+    else if (p.tn == 2) go(std::integral_constant<int, 2>{}, std::integral_constant<int, 1>{});
     else rows(std::integral_constant<int, 4>{});
 }
 
