@@ -150,13 +150,14 @@ __global__ __launch_bounds__((WPR < 4 ? 4 : WPR) * kWave, 4) void quant_rms_rows
 #pragma unroll
             for (int j = 0; j < NV; ++j) v[j] = times(v[j], rstd);
             if (a.gain) {
-                m = 0;
 #pragma unroll
-                for (int j = 0; j < NV; ++j) {
-                    v[j] = mul4(v[j], load4(a.gain, t + j * LANES < K4 ? t + j * LANES : K4 - 1));
-                    m = most_bits(m, v[j]);
+                for (int j = 0; j < NV; ++j) v[j] = mul4(v[j], load4(a.gain, t + j * LANES < K4 ? t + j * LANES : K4 - 1));
+                if (mode != kRmsApply) {
+                    m = 0;
+#pragma unroll
+                    for (int j = 0; j < NV; ++j) m = most_bits(m, v[j]);
+                    m = row_reduce<WPR>(m, OpMostBits{}, smm[1], rw, wr);
                 }
-                if (mode != kRmsApply) m = row_reduce<WPR>(m, OpMostBits{}, smm[1], rw, wr);
             }
         }
         if (mode == kRmsStats) {
