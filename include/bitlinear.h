@@ -438,7 +438,7 @@ int bitlinear_nonlinear_backward(const float* dXhat, const int8_t* check, const 
  * BL_OP_BACKWARD_I8 (part of it optional); N is of no account for the first two. */
 
 /* The residual's addition, root-mean-square norm and Eq. 4-5's quantiser in one pass:
- *   h = x + r, rounded to the type of the residual,   x^ = h / sqrt(mean(h^2) + eps) * gain
+ *   h = x + r in fp32, rounded to the type of the residual,   x^ = h / sqrt(mean(h^2) + eps) * gain
  * and gamma, codes of x^ as in bitlinear_quant_act.
  *   X          in   [M,K] of x_type (BL_F32, BL_BF16)
  *   residual   in   [M,K] of h_type or NULL: h = x, and H has to be NULL
@@ -475,8 +475,8 @@ size_t bitlinear_packed_bytes_i8(int64_t N, int64_t K);
 
 /* 8-bit weights with a scale for each output channel: m = max_k |W[n,k]|, scale[n] = m / 127, codes
  * clamp(rne(W[n,k] * (127 / m)), -127, 127).  (m is taken to be at least 127 * 2^-127 in a row that is not all zeros, so
- * that 127 / m is a number; a row of zeros has scale 0.)  A row with a NaN has a scale of NaN, one with an infinity an infinite one,
- * and no value or product of it is a number; its codes are any.
+ * that 127 / m is a number; a row of zeros has scale 0.)  A row with a NaN has a scale of NaN, one with an infinity an
+ * infinite one, and no value or product of it is finite; its codes are any.
  *   W       in   [N,K] of w_type: BL_F32, BL_BF16, or BL_I8: these are the codes (any int8), `scale` is left alone (or NULL)
  *   packed  out  bitlinear_packed_bytes_i8(N, K) bytes;   scale  out  fp32 [N] */
 int bitlinear_pack_weights_i8(const void* W, int w_type, int64_t N, int64_t K, void* packed, float* scale,
@@ -499,7 +499,8 @@ int bitlinear_matmul_i8(const int8_t* codes, const float* gamma, int64_t M, int6
  *   dW[n,k] = sum_m dY[m,n] (codes[m,k] * gamma_m / 128)    fp32 [N,K], or NULL
  *   dY   in  [M,N] of dy_type
  * bf16 operands, fp32 sums; what is rounded is rounded once: for dX the weights' values code * scale with a bf16 dY, dY * scale
- * with an fp32 one; for dW dY (a bf16 dY is exact), or with a gamma per token dY * gamma_m / 128.  The codes are exact. */
+ * with an fp32 one; for dW dY (a bf16 dY is exact), or with a gamma per token dY * gamma_m / 128.  The codes are exact.
+ * A gamma that is NaN (of a row with an infinity or a NaN) makes dW NaN, also where that row of dY is zero. */
 int bitlinear_backward_ste_i8(const void* dY, int dy_type, int64_t M, int64_t N, int64_t K, const int8_t* codes,
                               const float* gamma, int granularity, const void* packed, const float* scale,
                               void* dX, int dx_type, float* dW, void* workspace, size_t workspace_bytes,

@@ -115,7 +115,7 @@ int bitlinear_rmsnorm_backward(const void* dXhat, int g_type, const void* H, int
     a.G = dXhat; a.H = H; a.dR = dresidual; a.dH = dH;
     a.g_bf16 = g_type == BL_BF16; a.h_bf16 = h_type == BL_BF16; a.d_bf16 = d_type == BL_BF16;
     a.M = M; a.K = K; a.gain = gain; a.eps = (double)eps; a.dgain = dgain;
-    a.partials = dgain ? (double*)(((uintptr_t)workspace + 255) & ~(uintptr_t)255) : nullptr;
+    a.partials = dgain ? (void*)(((uintptr_t)workspace + 255) & ~(uintptr_t)255) : nullptr;
     return check_hip(launch_rmsnorm_backward(a, (hipStream_t)stream));
 }
 

@@ -485,8 +485,8 @@ __global__ __launch_bounds__(256) void fold_i8(TileArgs a, int splits) {
 // it; its W waves share the tiles of K evenly.  A wave loads S tiles of each row with 16 bytes a lane, which is the
 // operand of v_mfma_i32_16x16x64_i8 as it lies, and the codes of MB blocks of 16 tokens beside them (from L2), while it
 // multiplies the ones before.  The waves' sums meet in LDS.  A lane has four consecutive channels of one token.
-// One token, 28672 x 7168: 33 us = 6.2 TB/s; 16 tokens 36 us; 8192 x 2048, one token: 4.6 us, an empty launch and two trips
-// to memory.
+// One token, 28672 x 7168, weights that no cache holds: 35 us = 5.8 TB/s; 16 tokens 45, 32 tokens 53; 8192 x 2048, one token:
+// 4.7 us, an empty launch and two trips to memory.
 template <int TN, int MB, int S, int W>
 __global__ __launch_bounds__(W * 64, W * TN * MB <= 32 ? 4 : 2) void gemm_i8_stream(GemmI8Args a, int out) {
     __shared__ v4i red[W][TN * MB][kWave];
@@ -591,8 +591,10 @@ __global__ __launch_bounds__(W * 64, W * TN * MB <= 32 ? 4 : 2) void gemm_i8_str
 // workgroups with `per` stages each (`two` us a stage with all of a CU's workgroups, `one` with a single one) and their
 // start and stores (`item`), or the operands and the output at the memory's rate; slices of K, their launch and their
 // sums.  The constants were fitted by what the choice costs, over 300 shapes of 65 to 8192 tokens, K to 16384, N to
-// 28672: 0.6 % slower than the best of 18 variants on average, 22 % at most; over 150 others 0.7 % and 14 %.  Any one
-// tile less costs 1.4 to 10 % on average; 256 x 256 in slices would gain 0.1 %.
+// 28672: 0.6 % slower than the best of 18 variants on average, 22 % at most; over 150 others 0.7 % and 14 %.  They serve 33 to
+// 64 tokens too, where the choice is 4.5 % and 51 % slower (36 x 15360 -> 12084, left uncut, 68 us, two slices 45): one rate of
+// the memory for any number of workgroups is too low with all CUs at work and too high with few.  Any one tile less costs 1.4
+// to 10 % on average; 256 x 256 in slices would gain 0.1 %.
 struct I8Tile {
     int tm, tn, wgs;  // wgs: a CU's
     double two, one, item, item_one;
@@ -654,7 +656,8 @@ struct StreamPlan {
 // Up to 32 tokens: the stream with the rows of tiles and slices that cost least, or tiles where those do.  us: `call`,
 // and `tile` for each tile of K that a wave has, (workgroups / CUs)^power where there are more than CUs; or the weights
 // at `rate` MB/us.  Fitted to 126 shapes of 1 to 32 tokens: 2.4 % slower than the best of 20 variants on average, 44 %
-// at most; over 126 others 3.7 % and 61 %.  From 17 tokens on there are no two rows a workgroup: 26 registers spill in the
+// at most; over 126 others 3.7 % and 61 %; the 52 shapes of 17 to 32 tokens among them alone 8.3 % and 61 %, those of 1 to 16
+// 1.8 % and 34 %.  From 17 tokens on there are no two rows a workgroup: 26 registers spill in the
 // stream's loop (32 x 8384 -> 14656 44 us, four rows 28, one 46), and of 300000 shapes to N = 2 * 10^6 none took them.
 struct StreamCost {
     double call, tile, rate, power;

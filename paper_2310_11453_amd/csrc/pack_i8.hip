@@ -117,8 +117,8 @@ hipError_t launch_pack_i8(const PackI8Args& a, hipStream_t s) {
 }
 
 // A workgroup takes 2048 columns of the eight rows that share lines of 128 bytes, a wave a row: eight dwords a lane, all
-// in flight before the first is used: 16384 x 4096 to bf16 32 us (6.3 TB/s).  (Rows dealt to workgroups without regard to the lines: with the quantiser 107 ->
-// 131 us, 16384 x 4096.)
+// in flight before the first is used: 16384 x 4096 to bf16 32 us (6.3 TB/s).  (Rows dealt to workgroups without regard to
+// the lines: with the quantiser 107 -> 131 us, 16384 x 4096.)
 constexpr int kUnpackColumns = 2048;
 template <int TYPE>
 __global__ __launch_bounds__(512) void unpack_i8_rows(UnpackI8Args a, int64_t items, int64_t pieces) {

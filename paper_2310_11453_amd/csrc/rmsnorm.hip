@@ -70,7 +70,7 @@ __device__ inline int tensor_most(const QuantRmsArgs& a, int* sm) {
 // WPR waves share a row, which lies in their registers (NV float4 a lane) from its one reading on; workgroups have four
 // waves at least, so short rows are handled several to a workgroup, without a barrier.  Bound by HBM for large batches,
 // by the length of a row's chain for small ones (one reduction without a gain: the largest |x^| is then that of the
-// largest |h|).  8192 x 4096, fp32, residual, per token 79 us (5.5 TB/s); per tensor both passes 102 us; one row of
+// largest |h|).  8192 x 4096, fp32, residual, per token 78 us (5.6 TB/s); per tensor both passes 101 us; one row of
 // 2048 2.8 us.
 template <typename XT, typename RT, bool RES, int WPR, int NV>
 __global__ __launch_bounds__((WPR < 4 ? 4 : WPR) * kWave, 4) void quant_rms_rows(QuantRmsArgs a, int mode) {
@@ -343,12 +343,14 @@ hipError_t launch_quant_rmsnorm(const QuantRmsArgs& a_in, hipStream_t s) {
 // ---- backward -----------------------------------------------------------------------------------------
 // The workgroups are as many as fill the chip and go through the rows; a lane has the same columns of all its rows, so that
 // their share of dgain is summed in its registers, and each workgroup leaves one sum a column for fold_dgain.  A row is
-// read once; bound by HBM.  8192 x 4096, fp32 gradient, bf16 h: 66 us (5.5 TB/s); 2048 x 16384 bf16 62 us.
+// read once; bound by HBM.  8192 x 4096, fp32 gradients, bf16 h, a residual's gradient: 86 us (5.5 TB/s), with dgain
+// 93; all bf16, with dgain, 8192 x 4096 62 us (4.3), 2048 x 16384 82 us (3.3).
 // A lane's sums are fp64, but with six or eight float4 a lane (K > 16384) fp32, for which there is room, over 64 rows at most:
 // there are as many workgroups as that takes.  What leaves a wave for LDS and a workgroup for memory is rounded to fp32, half the
-// bytes: two roundings of parts of the sum beside the result's own; fold_dgain adds in fp64.  The gradient is then read again, out of the cache,
-// where it is used, instead of kept: 1600 x 20480 bf16 70 us (76 with eight float4 a lane, 159 with both
-// in registers, which spill, 193 with the sums in memory).  Rows past registers (K > 32768): fp64 sums in memory.
+// bytes: two roundings of parts of the sum beside the result's own; fold_dgain adds in fp64.  With six or eight the gradient is
+// read again, out of the cache, where it is used, instead of kept: 1600 x 20480 bf16 70 us (76 with eight float4 a lane, 159 with
+// both in registers, which spill, 193 with the sums in memory), all with h as the residual's gradient; with one of its own 96.
+// Rows past registers (K > 32768): fp64 sums in memory.
 constexpr int64_t kRmsBackwardWide = 16384, kRmsBackwardK = 32768;
 static int rms_backward_groups(int64_t M, int64_t K) {
     if (K <= kRmsBackwardWide) return (int)(M < 512 ? M : 512);
@@ -422,9 +424,9 @@ __global__ __launch_bounds__((WPR < 8 ? 8 : WPR) * kWave, 4) void rms_backward_r
         }
         const double rstd = rms_inverse(q * a.inv_k, a.eps);
         // 1/rms of a row below 2^-60 or above 2^60, or what is made of it, may be past fp32's range or have lost digits there: it
-        // is taken as inv64 * half then, half a power of two of half its exponent, and h as h * half (uniform in a row).  The branch
-        // costs 0 to 3 % (5784 x 5472 51.2 -> 52.8 us); powers of two in every row's arithmetic, or a loop of its own for such
-        // rows, 1 to 8 %
+        // is taken as inv64 * half then, half a power of two of half its exponent, and h as h * half (uniform in a row).  The
+        // branch costs 0 to 3 % (5784 x 5472 58.3 -> 60.1 us); powers of two in every row's arithmetic, or a loop of its own for
+        // such rows, 1 to 8 %.
         double inv64 = rstd;
         float half = 1.0f;
         if (__builtin_amdgcn_readfirstlane(rstd != 0.0 && !(rstd > 0x1p-60 && rstd < 0x1p60))) {
